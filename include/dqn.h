@@ -329,6 +329,187 @@ const char *dqn_last_error(const dqn_ctx *ctx);
 
 int32_t dqn_destroy(dqn_ctx *ctx);
 
+/* ---- operators of a recurrent Q-network ----
+ *
+ * What a network with a memory of its episode needs next to the calls above:
+ * blocks of a normalised residual stream, projections and a gated linear
+ * recurrence over time, trained over sequences with AdamW and stepped once per
+ * environment step while acting.  None needs a context.  Errors are reported by
+ * dqn_last_error(NULL).  Data pointers are device pointers aligned to their
+ * elements (weaker than the 256 bytes above); strides count elements, rows are
+ * contiguous.  A stride may be larger than the row, so that a tensor can be a
+ * part of a wider one.  Inputs and outputs of a call must not overlap except
+ * where it says so.  Structs of arguments are host pointers, read during the
+ * call.  Nothing is allocated; every call can be recorded into a HIP graph. */
+
+/* dtype of activations and their gradients: fp32, or bf16 with sums, states and
+ * statistics in fp32. */
+enum { DQN_F32 = 0, DQN_BF16 = 1 };
+
+/* Gated linear recurrence over time, per channel, with a_t = sigmoid(f_t):
+ *   h_t = a_t k_t h_{t-1} + (1 - a_t) x_t,   t = 0 .. T-1,   h_{-1} = h0
+ * k_t = 0 where reset_t != 0 (step t is the first of an episode: whatever the
+ * state was, a NaN too, is forgotten), else 1.  The state is fp32.  T = 1 is the
+ * step of an acting agent; h_last may be h0 then, and for any T. */
+typedef struct {
+    int32_t dtype;                      /* DQN_F32 / DQN_BF16, of f, x, h           */
+    int32_t B, C;                       /* sequences, channels; >= 0                */
+    int64_t T;                          /* steps, >= 0 (0: h_last = h0)             */
+    const void *f, *x;                  /* [B][T][C]                                */
+    int64_t f_bs, f_ts, x_bs, x_ts;     /* strides of a sequence and of a step      */
+    const float *h0;                    /* [B][C], or NULL = zeros                  */
+    const uint8_t *reset;               /* [B][T], or NULL = no episode starts      */
+    int64_t reset_bs, reset_ts;
+    void *h;                            /* [B][T][C]                                */
+    int64_t h_bs, h_ts;
+    float *h_last;                      /* [B][C], or NULL                          */
+    float *carry;                       /* for dqn_scan_backward, or NULL: states at
+                                           some of the steps, bytes from
+                                           dqn_scan_sizes                           */
+    void *workspace;                    /* bytes from dqn_scan_sizes, 16-byte aligned;
+                                           free for other use after the call         */
+} dqn_scan_args;
+
+/* Gradients of the recurrence.  With l_t = dh_t + a_{t+1} k_{t+1} l_{t+1}
+ * (h_last adds dlast to the last):
+ *   dx_t = (1 - a_t) l_t,  df_t = a_t (1 - a_t) l_t (k_t h_{t-1} - x_t),  dh0 = a_0 k_0 l_0.
+ * The states are computed again from `carry` as the forward call left it. */
+typedef struct {
+    int32_t dtype, B, C;
+    int64_t T;
+    const void *f, *x;
+    int64_t f_bs, f_ts, x_bs, x_ts;
+    const float *carry;
+    const uint8_t *reset;
+    int64_t reset_bs, reset_ts;
+    const void *dh;                     /* [B][T][C]                                */
+    int64_t dh_bs, dh_ts;
+    const float *dlast;                 /* [B][C], or NULL = zeros                  */
+    void *df, *dx;                      /* [B][T][C]                                */
+    int64_t df_bs, df_ts, dx_bs, dx_ts;
+    float *dh0;                         /* [B][C], or NULL                          */
+    void *workspace;
+} dqn_scan_grad_args;
+
+/* Bytes of `carry` and of `workspace` (of either call) for these sizes. */
+int32_t dqn_scan_sizes(int32_t dtype, int32_t B, int64_t T, int32_t C, size_t *carry, size_t *workspace);
+int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream);
+int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream);
+
+/* Root-mean-square norm with the residual's addition, per row of C elements:
+ *   r = x + residual,  y = weight r rstd,  rstd = 1 / sqrt(mean(r^2) + eps)
+ * y is taken of the fp32 sum, r is rounded once as it is stored.  Either y (in
+ * dtype) or q and scale are written: 8-bit numbers (e4m3) with y ~ q scale and
+ * scale = max |y| / 448 (a row of zeros has scale 0), the rows dqn_rows_product
+ * reads.  A row that holds a NaN or an infinity has a NaN as scale. */
+typedef struct {
+    int32_t dtype, C;                   /* 1 <= C <= DQN_NORM_MAX                   */
+    int64_t M;                          /* rows, >= 0                               */
+    const void *x, *residual;           /* [M][C]; residual may be NULL             */
+    int64_t x_rs, residual_rs;          /* strides of a row                         */
+    const float *weight;                /* [C]                                      */
+    float eps;                          /* >= 0                                     */
+    void *r;                            /* [M][C], or NULL; may be x or residual    */
+    int64_t r_rs;
+    void *y;                            /* [M][C], or NULL                          */
+    int64_t y_rs;
+    uint8_t *q;                         /* [M][C], or NULL; q_rs a multiple of 16,
+                                           q 16-byte aligned; the bytes from C to the
+                                           next multiple of 16 are set to zero       */
+    int64_t q_rs;
+    float *scale;                       /* [M]                                      */
+    float *rstd;                        /* [M], or NULL                             */
+} dqn_norm_args;
+#define DQN_NORM_MAX 16384
+
+/* Gradients of the norm, from the stored r and rstd: with xh = r rstd, g = weight dy,
+ *   dx = rstd (g - xh mean(g xh)) + dr   (of x and of the residual alike)
+ *   dw = sum over rows of dy xh          (in a fixed order) */
+typedef struct {
+    int32_t dtype, C;
+    int64_t M;
+    const void *dy, *r, *dr;            /* [M][C]; dr may be NULL                   */
+    int64_t dy_rs, r_rs, dr_rs;
+    const float *weight, *rstd;
+    void *dx;                           /* [M][C]; may be dr                        */
+    int64_t dx_rs;
+    float *dw;                          /* [C]; M = 0 gives zeros                   */
+    void *workspace;                    /* bytes from dqn_norm_sizes, 16-byte aligned */
+} dqn_norm_grad_args;
+
+int32_t dqn_norm_sizes(int64_t M, int32_t C, size_t *workspace);
+int32_t dqn_norm_forward(const dqn_norm_args *args, void *stream);
+int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream);
+
+/* Rows [M][K] to 8 bits, as dqn_norm_forward writes them: scale = max |x| / 448 per row. */
+int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, int64_t x_rs, uint8_t *q,
+                          int64_t q_rs, float *scale, void *stream);
+
+/* Product of 8-bit rows with 8-bit weights, y[m][n] = a_scale[m] w_scale[n] sum_k a[m][k] w[n][k] + bias[n]:
+ * e4m3 numbers, fp32 sums, y fp32 or bf16.  Row strides of a and w are multiples of 16 bytes and
+ * the rows 16-byte aligned; what lies between K and the next multiple of 16 may be read but does
+ * not count. */
+typedef struct {
+    int32_t dtype, N, K;                /* of y; N >= 0, K >= 0                     */
+    int64_t M;                          /* >= 0                                     */
+    const uint8_t *a, *w;               /* [M][K], [N][K]                           */
+    int64_t a_rs, w_rs;
+    const float *a_scale, *w_scale;     /* [M], [N]                                 */
+    const float *bias;                  /* [N], or NULL                             */
+    void *y;                            /* [M][N]                                   */
+    int64_t y_rs;
+} dqn_product_args;
+int32_t dqn_rows_product(const dqn_product_args *args, void *stream);
+
+/* AdamW over many tensors in one launch, decoupled weight decay:
+ *   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2
+ *   p <- p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+ * Parameters are fp32.  The moments of all tensors lie one behind the other, a
+ * tensor beginning at a multiple of 256 elements (the places between hold the
+ * caller's zeros).  bits = 32: fp32.  bits = 8: m as e4m3, v as e5m2, each with one fp32
+ * scale per 256 elements, scale = largest / 448 and largest / 57344; the step is
+ * computed in fp32 and p takes the moments before they are rounded.  They are rounded
+ * up or down at random, in proportion, since one step changes v by about 0.1 %,
+ * far less than half the distance of two 8-bit numbers, and rounding to the nearest
+ * would keep v where it is for ever; a v that is not zero stays so.  The random bits of
+ * element i of the buffer of moments come from the library's counter-based draws:
+ * 32 bits of output i / 2 for `seed` (the lower half for even i), the lower 16 for
+ * m, the upper 16 for v, so a step is a function of its arguments alone.  A gradient
+ * that is not finite spoils its parameter as with 32 bits, and with 8 the moments of its 256
+ * elements. */
+typedef struct {
+    float *param;                       /* [n]                                      */
+    const void *grad;                   /* [n], in the optimizer's grad_dtype       */
+    uint16_t *copy;                     /* [n] bf16 copy of the new param, or NULL  */
+    int64_t n;                          /* >= 0                                     */
+    float decay;
+} dqn_adamw_tensor;
+
+typedef struct {
+    int64_t elements;                   /* of each buffer of moments                */
+    size_t m, v, m_scale, v_scale;      /* bytes; the scales are 0 for 32 bits      */
+    size_t plan;                        /* bytes of the device table of tensors     */
+} dqn_adamw_bytes;
+
+typedef struct {
+    void *m, *v;                        /* 256-byte aligned, like the others; the   */
+    float *m_scale, *v_scale;           /* caller sets them (zeros at the start)    */
+    void *plan;
+} dqn_adamw_buffers;
+
+typedef struct dqn_adamw dqn_adamw;
+
+/* `tensors`: host array of `count` descriptions, 1 <= count <= 65536; its device pointers must
+ * stay valid.  The handle owns host-side bookkeeping only; the table is copied to `plan`
+ * on `stream` during dqn_adamw_init, which waits for the copy. */
+int32_t dqn_adamw_sizes(const dqn_adamw_tensor *tensors, int32_t count, int32_t bits, dqn_adamw_bytes *out);
+int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t count, int32_t bits,
+                       int32_t grad_dtype, const dqn_adamw_buffers *bufs, void *stream);
+/* One step, number `step` >= 1.  `seed` is used with 8 bits and should differ from step to step. */
+int32_t dqn_adamw_step(dqn_adamw *opt, double lr, double beta_m, double beta_v, double eps, int64_t step,
+                       uint64_t seed, void *stream);
+int32_t dqn_adamw_destroy(dqn_adamw *opt);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,7 @@
 #include "gemm_split.h"
 #include "kernels_misc.h"
 #include "net.h"
+#include "seq_common.h"
 
 // Scratch memory of dqn_act_static, the entry point for callers that cannot allocate: activations and
 // fc1 partial sums of up to DQN_ACT_STATIC_MAX observations.  Each GPU the library runs on holds its own
@@ -1237,6 +1238,16 @@ void backward_bf16(dqn_ctx *c, int B, const Pass &ps, int *ns1, int *ns2, int *n
 }  // namespace
 
 // ============================================================================
+// errors of the calls in seq_api.hip, which need no context
+int32_t dqn_seq_fail(int32_t code, const char *call, const char *why)
+{
+    try {
+        g_err = std::string(call) + ": " + why;
+    } catch (...) {   // no memory for the text: the code alone says it
+    }
+    return code;
+}
+
 extern "C" {
 
 const char *dqn_last_error(const dqn_ctx *ctx) { return ctx ? ctx->err.c_str() : g_err.c_str(); }

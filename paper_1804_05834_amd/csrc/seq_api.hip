@@ -1,0 +1,361 @@
+// C ABI of the recurrent network's operators (see include/dqn.h): checks of arguments and launches.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "../../include/dqn.h"
+#include "adamw.h"
+#include "norm.h"
+#include "rows_product.h"
+#include "scan.h"
+
+struct dqn_adamw {
+    seq::AdamArgs args;
+    int64_t chunks;
+    int bits, grad_dtype;
+};
+
+namespace {
+
+int32_t bad(const char *call, const char *why) { return dqn_seq_fail(DQN_ERR_INVALID_ARG, call, why); }
+
+int32_t launched(const char *call)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? (int32_t)DQN_OK : dqn_seq_fail(DQN_ERR_HIP, call, hipGetErrorString(e));
+}
+
+bool dtype_ok(int32_t d) { return d == DQN_F32 || d == DQN_BF16; }
+size_t bytes_of(int32_t d) { return d == DQN_F32 ? 4 : 2; }
+bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
+constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
+
+bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && (!a || !b || a * b <= MOST) && (!a || !b || !c || a * b <= MOST / c); }
+
+// Called with elements present: a [B][T][C] tensor, its strides no shorter than what they step over, and apart for a
+// tensor that is written (no element twice).
+const char *check_steps(const void *p, int64_t bs, int64_t ts, const dqn_scan_args &s, bool written)
+{
+    if (!p || !at(p, bytes_of(s.dtype))) return "a tensor is NULL or not aligned to its elements";
+    if (bs < 0 || ts < 0 || bs > MOST || ts > MOST) return "a stride is negative or too large";
+    if (ts > 0 && s.T - 1 > MOST / ts) return "T times a stride is too large";
+    if (bs > 0 && s.B - 1 > MOST / bs) return "B times a stride is too large";
+    if (!written) return nullptr;
+    const bool apart = (s.T == 1 || ts >= s.C) && (s.B == 1 || bs >= s.C) &&
+                       (s.T == 1 || s.B == 1 || bs >= (s.T - 1) * ts + s.C || ts >= (s.B - 1) * bs + s.C);
+    return apart ? nullptr : "rows of an output lie on top of each other";
+}
+
+const char *check_scan(const dqn_scan_args &s)
+{
+    if (!dtype_ok(s.dtype)) return "dtype must be DQN_F32 or DQN_BF16";
+    if (s.B < 0 || s.C < 0 || s.T < 0 || s.B > 65535 || !size_ok(s.B, s.T, s.C)) return "B must be in 0..65535, T and C >= 0";
+    if (!at(s.h0, 4) || !at(s.h_last, 4) || !at(s.carry, 4)) return "a state is not aligned to its elements";
+    if (s.reset && (s.reset_bs < 0 || s.reset_ts < 0 || s.reset_bs > MOST || s.reset_ts > MOST ||
+                    (s.reset_ts > 0 && s.T - 1 > MOST / s.reset_ts))) return "a stride of reset is negative or too large";
+    return nullptr;
+}
+
+long scan_tiles(int64_t T) { return (T + seq::SCAN_CARRY - 1) / seq::SCAN_CARRY; }
+
+const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
+{
+    if (!p || !at(p, bytes_of(dtype))) return "a tensor is NULL or not aligned to its elements";
+    if (rs < 0 || rs > MOST || (rs > 0 && M - 1 > MOST / rs)) return "a stride is negative or too large";
+    return !written || M == 1 || rs >= C ? nullptr : "rows of an output lie on top of each other";
+}
+
+const char *check_rows8(const void *p, int64_t rs, int64_t M, int64_t K)
+{
+    if (!p || !at(p, 16) || rs % 16 || rs < 0 || rs > MOST || (rs > 0 && M - 1 > MOST / rs)) return "8-bit rows must be 16-byte aligned, strides multiples of 16";
+    return M == 1 || rs >= K ? nullptr : "the stride of 8-bit rows is shorter than a row";
+}
+
+template <class E> void launch_norm(const seq::NormArgs &N, hipStream_t st) { seq::k_norm<E><<<dim3((unsigned)N.M), 256, 0, st>>>(N); }
+
+int norm_parts(int64_t M) { return (int)std::min<int64_t>(seq::NORM_PARTS, (M + 15) / 16); }
+
+const char *check_tensors(const dqn_adamw_tensor *t, int32_t count, int32_t bits)
+{
+    if (!t || count < 1 || count > 65536) return "count must be in 1..65536, tensors not NULL";
+    if (bits != 8 && bits != 32) return "bits must be 8 or 32";
+    int64_t sum = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (t[i].n < 0 || t[i].n > (1ll << 38)) return "a tensor's size is out of range";
+        sum += (t[i].n + seq::ADAM_BLOCK - 1) / seq::ADAM_BLOCK * seq::ADAM_BLOCK;
+        if (sum > (1ll << 38)) return "too many elements";
+        if (t[i].n && (!t[i].param || !t[i].grad || !at(t[i].param, 4) || !at(t[i].copy, 2))) return "a tensor's pointer is NULL or not aligned to its elements";
+        if (!(t[i].decay >= 0.f) || std::isinf(t[i].decay)) return "decay must be finite and >= 0";
+    }
+    return nullptr;
+}
+
+struct AdamSizes {
+    int64_t elements, chunks;
+};
+AdamSizes adamw_sizes(const dqn_adamw_tensor *t, int32_t count)
+{
+    AdamSizes s{0, 0};
+    for (int32_t i = 0; i < count; ++i) {
+        s.elements += (t[i].n + seq::ADAM_BLOCK - 1) / seq::ADAM_BLOCK * seq::ADAM_BLOCK;
+        s.chunks += (t[i].n + seq::ADAM_CHUNK - 1) / seq::ADAM_CHUNK;
+    }
+    return s;
+}
+size_t plan_bytes(const AdamSizes &s, int32_t count) { return ((size_t)count * sizeof(seq::AdamTensor) + (size_t)s.chunks * sizeof(seq::AdamChunk) + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" {
+
+// ------------------------------------------------------------ gated linear recurrence
+int32_t dqn_scan_sizes(int32_t dtype, int32_t B, int64_t T, int32_t C, size_t *carry, size_t *workspace)
+{
+    static const char *call = "dqn_scan_sizes";
+    dqn_scan_args s{};
+    s.dtype = dtype; s.B = B; s.T = T; s.C = C;
+    if (!carry || !workspace) return bad(call, "NULL argument");
+    if (const char *m = check_scan(s)) return bad(call, m);
+    *carry = (size_t)B * scan_tiles(T) * C * 4;
+    *workspace = 0;
+    return DQN_OK;
+}
+
+int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream)
+{
+    static const char *call = "dqn_scan_forward";
+    if (!args) return bad(call, "NULL argument");
+    const dqn_scan_args &s = *args;
+    if (const char *m = check_scan(s)) return bad(call, m);
+    if (!s.B || !s.C) return DQN_OK;
+    if (s.T) {
+        for (const char *m : {check_steps(s.f, s.f_bs, s.f_ts, s, false), check_steps(s.x, s.x_bs, s.x_ts, s, false), check_steps(s.h, s.h_bs, s.h_ts, s, true)})
+            if (m) return bad(call, m);
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last, s.carry, s.T, s.B, s.C};
+    const dim3 grid((unsigned)((s.C + 63) / 64), (unsigned)s.B);
+    if (s.dtype == DQN_F32) seq::k_scan<float><<<grid, 64, 0, st>>>(A);
+    else seq::k_scan<seq::bf16><<<grid, 64, 0, st>>>(A);
+    return launched(call);
+}
+
+int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream)
+{
+    static const char *call = "dqn_scan_backward";
+    if (!args) return bad(call, "NULL argument");
+    const dqn_scan_grad_args &g = *args;
+    dqn_scan_args s{};
+    s.dtype = g.dtype; s.B = g.B; s.T = g.T; s.C = g.C;
+    s.reset = g.reset; s.reset_bs = g.reset_bs; s.reset_ts = g.reset_ts;
+    if (const char *m = check_scan(s)) return bad(call, m);
+    if (!at(g.carry, 4) || !at(g.dlast, 4) || !at(g.dh0, 4)) return bad(call, "a state is not aligned to its elements");
+    if (!s.B || !s.C) return DQN_OK;
+    if (s.T) {
+        if (!g.carry) return bad(call, "carry is NULL");
+        for (const char *m : {check_steps(g.f, g.f_bs, g.f_ts, s, false), check_steps(g.x, g.x_bs, g.x_ts, s, false), check_steps(g.dh, g.dh_bs, g.dh_ts, s, false),
+                              check_steps(g.df, g.df_bs, g.df_ts, s, true), check_steps(g.dx, g.dx_bs, g.dx_ts, s, true)})
+            if (m) return bad(call, m);
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const seq::ScanGradArgs A{g.f, g.x, g.dh, g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.carry, g.dlast, g.reset, g.reset_bs, g.reset_ts,
+                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C};
+    const dim3 grid((unsigned)((s.C + 63) / 64), (unsigned)s.B);
+    if (s.dtype == DQN_F32) seq::k_scan_grad<float><<<grid, 64, 0, st>>>(A);
+    else seq::k_scan_grad<seq::bf16><<<grid, 64, 0, st>>>(A);
+    return launched(call);
+}
+
+// ------------------------------------------------------------ norm, rows of 8-bit numbers
+int32_t dqn_norm_sizes(int64_t M, int32_t C, size_t *workspace)
+{
+    static const char *call = "dqn_norm_sizes";
+    if (!workspace) return bad(call, "NULL argument");
+    if (M < 0 || M > INT32_MAX || C < 1 || C > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, C in 1..DQN_NORM_MAX");
+    *workspace = (size_t)norm_parts(M) * C * 4;
+    return DQN_OK;
+}
+
+int32_t dqn_norm_forward(const dqn_norm_args *args, void *stream)
+{
+    static const char *call = "dqn_norm_forward";
+    if (!args) return bad(call, "NULL argument");
+    const dqn_norm_args &n = *args;
+    if (!dtype_ok(n.dtype)) return bad(call, "dtype must be DQN_F32 or DQN_BF16");
+    if (n.M < 0 || n.M > INT32_MAX || n.C < 1 || n.C > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, C in 1..DQN_NORM_MAX");
+    if (!(n.eps >= 0.f) || std::isinf(n.eps)) return bad(call, "eps must be finite and >= 0");
+    if (!n.M) return DQN_OK;
+    if (!n.y == !n.q) return bad(call, "one of y and q must be given");
+    if (!n.weight || !at(n.weight, 4) || !at(n.rstd, 4)) return bad(call, "weight is NULL or a pointer is not aligned to its elements");
+    for (const char *m : {check_rows(n.x, n.x_rs, n.M, n.C, n.dtype, false), n.residual ? check_rows(n.residual, n.residual_rs, n.M, n.C, n.dtype, false) : nullptr,
+                          n.r ? check_rows(n.r, n.r_rs, n.M, n.C, n.dtype, true) : nullptr, n.y ? check_rows(n.y, n.y_rs, n.M, n.C, n.dtype, true) : nullptr,
+                          n.q ? check_rows8(n.q, n.q_rs, n.M, n.C) : nullptr})
+        if (m) return bad(call, m);
+    if (n.q && (!n.scale || !at(n.scale, 4))) return bad(call, "scale is NULL or not aligned to its elements");
+    const seq::NormArgs A{n.x, n.residual, n.x_rs, n.residual_rs, n.weight, n.eps, n.r, n.y, n.r_rs, n.y_rs, n.q, n.q_rs, n.scale, n.rstd, n.M, n.C};
+    if (n.dtype == DQN_F32) launch_norm<float>(A, (hipStream_t)stream);
+    else launch_norm<seq::bf16>(A, (hipStream_t)stream);
+    return launched(call);
+}
+
+int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream)
+{
+    static const char *call = "dqn_norm_backward";
+    if (!args) return bad(call, "NULL argument");
+    const dqn_norm_grad_args &n = *args;
+    if (!dtype_ok(n.dtype)) return bad(call, "dtype must be DQN_F32 or DQN_BF16");
+    if (n.M < 0 || n.M > INT32_MAX || n.C < 1 || n.C > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, C in 1..DQN_NORM_MAX");
+    if (!n.dw || !at(n.dw, 4)) return bad(call, "dw is NULL or not aligned to its elements");
+    hipStream_t st = (hipStream_t)stream;
+    const int parts = norm_parts(n.M);
+    if (n.M) {
+        if (!n.weight || !n.rstd || !at(n.weight, 4) || !at(n.rstd, 4)) return bad(call, "weight or rstd is NULL or not aligned to its elements");
+        if (!n.workspace || !at(n.workspace, 16)) return bad(call, "workspace is NULL or not 16-byte aligned");
+        for (const char *m : {check_rows(n.dy, n.dy_rs, n.M, n.C, n.dtype, false), check_rows(n.r, n.r_rs, n.M, n.C, n.dtype, false),
+                              n.dr ? check_rows(n.dr, n.dr_rs, n.M, n.C, n.dtype, false) : nullptr, check_rows(n.dx, n.dx_rs, n.M, n.C, n.dtype, true)})
+            if (m) return bad(call, m);
+        const seq::NormGradArgs A{n.dy, n.r, n.dr, n.dy_rs, n.r_rs, n.dr_rs, n.weight, n.rstd, n.dx, n.dx_rs, n.dw, (float *)n.workspace, n.M, n.C, parts};
+        const dim3 grid((unsigned)((n.C + 255) / 256), (unsigned)parts);
+        if (n.dtype == DQN_F32) {
+            seq::k_norm_grad_weight<float><<<grid, 256, 0, st>>>(A);
+            seq::k_norm_grad<float><<<dim3((unsigned)n.M), 256, 0, st>>>(A);
+        } else {
+            seq::k_norm_grad_weight<seq::bf16><<<grid, 256, 0, st>>>(A);
+            seq::k_norm_grad<seq::bf16><<<dim3((unsigned)n.M), 256, 0, st>>>(A);
+        }
+    }
+    seq::k_norm_grad_join<<<dim3((unsigned)((n.C + 255) / 256)), 256, 0, st>>>((const float *)n.workspace, parts, n.C, n.dw);
+    return launched(call);
+}
+
+int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, int64_t x_rs, uint8_t *q, int64_t q_rs, float *scale, void *stream)
+{
+    static const char *call = "dqn_rows_quantize";
+    if (!dtype_ok(dtype)) return bad(call, "dtype must be DQN_F32 or DQN_BF16");
+    if (M < 0 || M > INT32_MAX || K < 1 || K > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, K in 1..DQN_NORM_MAX");
+    if (!M) return DQN_OK;
+    if (!scale || !at(scale, 4)) return bad(call, "scale is NULL or not aligned to its elements");
+    for (const char *m : {check_rows(x, x_rs, M, K, dtype, false), check_rows8(q, q_rs, M, K)})
+        if (m) return bad(call, m);
+    const seq::NormArgs A{x, nullptr, x_rs, 0, nullptr, 0.f, nullptr, nullptr, 0, 0, q, q_rs, scale, nullptr, M, K};
+    if (dtype == DQN_F32) launch_norm<float>(A, (hipStream_t)stream);
+    else launch_norm<seq::bf16>(A, (hipStream_t)stream);
+    return launched(call);
+}
+
+// ------------------------------------------------------------ product of 8-bit rows
+int32_t dqn_rows_product(const dqn_product_args *args, void *stream)
+{
+    static const char *call = "dqn_rows_product";
+    if (!args) return bad(call, "NULL argument");
+    const dqn_product_args &p = *args;
+    if (!dtype_ok(p.dtype)) return bad(call, "dtype must be DQN_F32 or DQN_BF16");
+    if (p.M < 0 || p.N < 0 || p.K < 0 || p.M > INT32_MAX - 1024 || p.N > (1 << 20) || p.K > (1 << 24)) return bad(call, "M must be in 0..2^31-1025, N in 0..2^20, K in 0..2^24");
+    if (!p.M || !p.N) return DQN_OK;
+    for (const char *m : {p.K ? check_rows8(p.a, p.a_rs, p.M, p.K) : nullptr, p.K ? check_rows8(p.w, p.w_rs, p.N, p.K) : nullptr,
+                          check_rows(p.y, p.y_rs, p.M, p.N, p.dtype, true)})
+        if (m) return bad(call, m);
+    if (!p.a_scale || !p.w_scale || !at(p.a_scale, 4) || !at(p.w_scale, 4) || !at(p.bias, 4)) return bad(call, "a scale is NULL or a pointer is not aligned to its elements");
+    hipStream_t st = (hipStream_t)stream;
+    const seq::ProductArgs A{p.a, p.w, p.a_rs, p.w_rs, p.a_scale, p.w_scale, p.bias, p.y, p.y_rs, p.M, p.N, p.K};
+    const dim3 grid((unsigned)((p.M + 15) / 16), (unsigned)((p.N + 15) / 16));
+    if (p.dtype == DQN_F32) seq::k_product<float><<<grid, 64, 0, st>>>(A);
+    else seq::k_product<seq::bf16><<<grid, 64, 0, st>>>(A);
+    return launched(call);
+}
+
+// ------------------------------------------------------------ AdamW
+int32_t dqn_adamw_sizes(const dqn_adamw_tensor *tensors, int32_t count, int32_t bits, dqn_adamw_bytes *out)
+{
+    static const char *call = "dqn_adamw_sizes";
+    if (!out) return bad(call, "NULL argument");
+    if (const char *m = check_tensors(tensors, count, bits)) return bad(call, m);
+    const AdamSizes s = adamw_sizes(tensors, count);
+    *out = dqn_adamw_bytes{};
+    out->elements = s.elements;
+    out->m = out->v = (size_t)s.elements * (bits / 8);
+    out->m_scale = out->v_scale = bits == 8 ? (size_t)s.elements / seq::ADAM_BLOCK * 4 : 0;
+    out->plan = plan_bytes(s, count);
+    return DQN_OK;
+}
+
+int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t count, int32_t bits, int32_t grad_dtype,
+                       const dqn_adamw_buffers *bufs, void *stream)
+{
+    static const char *call = "dqn_adamw_init";
+    if (!out || !bufs) return bad(call, "NULL argument");
+    *out = nullptr;
+    if (const char *m = check_tensors(tensors, count, bits)) return bad(call, m);
+    if (!dtype_ok(grad_dtype)) return bad(call, "grad_dtype must be DQN_F32 or DQN_BF16");
+    const AdamSizes s = adamw_sizes(tensors, count);
+    for (const void *p : {(const void *)bufs->plan, s.elements ? (const void *)bufs->m : bufs->plan, s.elements ? (const void *)bufs->v : bufs->plan,
+                          s.elements && bits == 8 ? (const void *)bufs->m_scale : bufs->plan, s.elements && bits == 8 ? (const void *)bufs->v_scale : bufs->plan})
+        if (!p || !at(p, 256)) return bad(call, "a buffer is NULL or not 256-byte aligned");
+    for (int32_t i = 0; i < count; ++i)
+        if (tensors[i].n && !at(tensors[i].grad, bytes_of(grad_dtype))) return bad(call, "a gradient is not aligned to its elements");
+    if (s.chunks > INT32_MAX) return bad(call, "too many elements");
+    dqn_adamw *o = nullptr;
+    try {
+        std::vector<uint8_t> table(plan_bytes(s, count), 0);
+        seq::AdamTensor *t = reinterpret_cast<seq::AdamTensor *>(table.data());
+        seq::AdamChunk *c = reinterpret_cast<seq::AdamChunk *>(t + count);
+        int64_t place = 0;
+        for (int32_t i = 0; i < count; ++i) {
+            const dqn_adamw_tensor &u = tensors[i];
+            const bool wide = at(u.param, 16) && at(u.grad, 4 * bytes_of(grad_dtype)) && at(u.copy, 8);
+            t[i] = seq::AdamTensor{u.param, u.grad, u.copy, (long)u.n, (long)place, u.decay, wide};
+            place += (u.n + seq::ADAM_BLOCK - 1) / seq::ADAM_BLOCK * seq::ADAM_BLOCK;
+            for (int64_t k = 0; k < (u.n + seq::ADAM_CHUNK - 1) / seq::ADAM_CHUNK; ++k) *c++ = seq::AdamChunk{i, (int)k};
+        }
+        hipStream_t st = (hipStream_t)stream;
+        if (hipMemcpyAsync(bufs->plan, table.data(), table.size(), hipMemcpyHostToDevice, st) != hipSuccess || hipStreamSynchronize(st) != hipSuccess) {
+            (void)hipGetLastError();
+            return dqn_seq_fail(DQN_ERR_HIP, call, "copying the table of tensors failed");
+        }
+        o = new dqn_adamw{};
+    } catch (...) {
+        return dqn_seq_fail(DQN_ERR_OOM, call, "out of host memory");
+    }
+    o->args.tensors = (const seq::AdamTensor *)bufs->plan;
+    o->args.chunks = (const seq::AdamChunk *)(o->args.tensors + count);
+    o->args.m = bufs->m; o->args.v = bufs->v; o->args.ms = bufs->m_scale; o->args.vs = bufs->v_scale;
+    o->chunks = s.chunks; o->bits = bits; o->grad_dtype = grad_dtype;
+    *out = o;
+    return DQN_OK;
+}
+
+int32_t dqn_adamw_step(dqn_adamw *opt, double lr, double beta_m, double beta_v, double eps, int64_t step, uint64_t seed, void *stream)
+{
+    static const char *call = "dqn_adamw_step";
+    if (!opt) return bad(call, "NULL argument");
+    if (!(lr >= 0.0) || lr > 1e30 || !(eps >= 1e-30) || eps > 1e30) return bad(call, "lr in 0..1e30 and eps in 1e-30..1e30 required");
+    if (!(beta_m >= 0.0 && beta_m < 1.0 && beta_v >= 0.0 && beta_v < 1.0)) return bad(call, "beta_m and beta_v must be in [0, 1)");
+    if (step < 1) return bad(call, "step must be >= 1");
+    if (!opt->chunks) return DQN_OK;
+    seq::AdamArgs A = opt->args;
+    // doubles: 1 - b of the float next to 0.999 is 1.3e-5 off
+    A.lr = (float)lr; A.b1 = (float)beta_m; A.c1 = (float)(1.0 - beta_m); A.b2 = (float)beta_v; A.c2 = (float)(1.0 - beta_v); A.eps = (float)eps;
+    A.rate = (float)(lr / (1.0 - std::pow(beta_m, (double)step)));
+    A.root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta_v, (double)step)));
+    A.seed = seed;
+    const dim3 grid((unsigned)opt->chunks);
+    hipStream_t st = (hipStream_t)stream;
+    if (opt->grad_dtype == DQN_F32) {
+        if (opt->bits == 8) seq::k_adamw<float, 8><<<grid, 256, 0, st>>>(A);
+        else seq::k_adamw<float, 32><<<grid, 256, 0, st>>>(A);
+    } else {
+        if (opt->bits == 8) seq::k_adamw<seq::bf16, 8><<<grid, 256, 0, st>>>(A);
+        else seq::k_adamw<seq::bf16, 32><<<grid, 256, 0, st>>>(A);
+    }
+    return launched(call);
+}
+
+int32_t dqn_adamw_destroy(dqn_adamw *opt)
+{
+    delete opt;
+    return DQN_OK;
+}
+
+}  // extern "C"

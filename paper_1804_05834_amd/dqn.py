@@ -19,7 +19,9 @@ EXPORTS = ["dqn_query_sizes", "dqn_init", "dqn_act", "dqn_train_step", "per_samp
            "per_fill", "dqn_replay_write", "dqn_replay_gather", "dqn_sync_target", "dqn_get_params",
            "dqn_set_params", "dqn_profile_begin", "dqn_profile_end", "dqn_last_error", "dqn_destroy",
            "dqn_replay_store", "dqn_replay_state", "dqn_schedule_default", "dqn_schedule_at", "dqn_preprocess",
-           "dqn_get_activations", "dqn_act_static", "dqn_selftest_fused_conv_schedule", "dqn_replay_store_envs"]
+           "dqn_get_activations", "dqn_act_static", "dqn_selftest_fused_conv_schedule", "dqn_replay_store_envs",
+           "dqn_scan_sizes", "dqn_scan_forward", "dqn_scan_backward", "dqn_norm_sizes", "dqn_norm_forward", "dqn_norm_backward",
+           "dqn_rows_quantize", "dqn_rows_product", "dqn_adamw_sizes", "dqn_adamw_init", "dqn_adamw_step", "dqn_adamw_destroy"]
 
 
 class DqnConfig(C.Structure):
@@ -118,6 +120,19 @@ def lib():
             "dqn_profile_begin": [vp],
             "dqn_profile_end": [vp, i32, C.POINTER(C.c_char_p), C.POINTER(i64), C.POINTER(C.c_double)],
             "dqn_destroy": [vp],
+            # the operators of seq.py; their structs of arguments are built there
+            "dqn_scan_sizes": [i32, i32, i64, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "dqn_scan_forward": [vp, vp],
+            "dqn_scan_backward": [vp, vp],
+            "dqn_norm_sizes": [i64, i32, C.POINTER(C.c_size_t)],
+            "dqn_norm_forward": [vp, vp],
+            "dqn_norm_backward": [vp, vp],
+            "dqn_rows_quantize": [i32, i64, i32, vp, i64, vp, i64, vp, vp],
+            "dqn_rows_product": [vp, vp],
+            "dqn_adamw_sizes": [vp, i32, i32, vp],
+            "dqn_adamw_init": [C.POINTER(vp), vp, i32, i32, i32, vp, vp],
+            "dqn_adamw_step": [vp, C.c_double, C.c_double, C.c_double, C.c_double, i64, u64, vp],
+            "dqn_adamw_destroy": [vp],
         }
         for name, argtypes in sig.items():
             fn = getattr(L, name)
