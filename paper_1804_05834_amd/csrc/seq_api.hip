@@ -2,6 +2,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <algorithm>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -58,7 +60,66 @@ const char *check_scan(const dqn_scan_args &s)
     return nullptr;
 }
 
-long scan_tiles(int64_t T) { return (T + seq::SCAN_CARRY - 1) / seq::SCAN_CARRY; }
+// How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
+struct ScanCut {
+    int waves, ranges;   // waves of a workgroup; ranges over time
+    long tile, tiles;    // steps of a tile, tiles of a sequence
+    long range;          // steps of a range
+};
+ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
+{
+    ScanCut c{};
+    if (T <= seq::SCAN_SHORT) {
+        c = ScanCut{0, 1, seq::SCAN_SHORT, T ? 1 : 0, (long)T};
+        return c;
+    }
+    c.waves = 1;
+    while (c.waves < seq::SCAN_WAVES && 16 * c.waves < T) c.waves *= 2;
+    c.tile = 16 * c.waves;
+    c.tiles = (T + c.tile - 1) / c.tile;
+    const int64_t strips = (int64_t)B * ((C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP);
+    // enough workgroups for two per compute unit, but ranges of four tiles at least
+    const int64_t want = std::min<int64_t>(std::min<int64_t>(256, strips ? (512 + strips - 1) / strips : 1), std::max<int64_t>(1, c.tiles / 4));
+    const long per = (c.tiles + want - 1) / want;
+    c.range = per * c.tile;
+    c.ranges = (int)((c.tiles + per - 1) / per);
+    return c;
+}
+size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C) { return c.ranges > 1 ? ((size_t)B * c.ranges * 2 * C * 4 + 15) / 16 * 16 : 0; }
+
+// whether four elements of every tensor can be taken at once
+bool four(int32_t dtype, int32_t C, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, std::initializer_list<const void *> states)
+{
+    if (C % 4) return false;
+    for (const void *p : tensors)
+        if (!at(p, 4 * bytes_of(dtype))) return false;
+    for (int64_t s : strides)
+        if (s % 4) return false;
+    for (const void *p : states)
+        if (!at(p, 16)) return false;
+    return true;
+}
+
+template <class E, int V> void launch_scan(const seq::ScanArgs &A, const ScanCut &c, hipStream_t st)
+{
+    if (!c.waves) {
+        seq::k_scan_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
+        return;
+    }
+    const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
+    if (c.ranges > 1) seq::k_scan<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
+    seq::k_scan<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
+}
+template <class E, int V> void launch_scan_grad(const seq::ScanGradArgs &A, const ScanCut &c, hipStream_t st)
+{
+    if (!c.waves) {
+        seq::k_scan_grad_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
+        return;
+    }
+    const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
+    if (c.ranges > 1) seq::k_scan_grad<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
+    seq::k_scan_grad<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
+}
 
 const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
 {
@@ -118,8 +179,9 @@ int32_t dqn_scan_sizes(int32_t dtype, int32_t B, int64_t T, int32_t C, size_t *c
     s.dtype = dtype; s.B = B; s.T = T; s.C = C;
     if (!carry || !workspace) return bad(call, "NULL argument");
     if (const char *m = check_scan(s)) return bad(call, m);
-    *carry = (size_t)B * scan_tiles(T) * C * 4;
-    *workspace = 0;
+    const ScanCut cut = scan_cut(B, T, C);
+    *carry = (size_t)B * cut.tiles * C * 4;
+    *workspace = scan_workspace(cut, B, C);
     return DQN_OK;
 }
 
@@ -135,10 +197,13 @@ int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream)
             if (m) return bad(call, m);
     }
     hipStream_t st = (hipStream_t)stream;
-    const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last, s.carry, s.T, s.B, s.C};
-    const dim3 grid((unsigned)((s.C + 63) / 64), (unsigned)s.B);
-    if (s.dtype == DQN_F32) seq::k_scan<float><<<grid, 64, 0, st>>>(A);
-    else seq::k_scan<seq::bf16><<<grid, 64, 0, st>>>(A);
+    const ScanCut cut = scan_cut(s.B, s.T, s.C);
+    if (scan_workspace(cut, s.B, s.C) && (!s.workspace || !at(s.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
+    const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last,
+                          s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.range, cut.ranges, (float *)s.workspace, cut.tiles};
+    const bool v4 = four(s.dtype, s.C, {s.f, s.x, s.h}, {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts}, {s.h0, s.h_last, s.carry});
+    if (s.dtype == DQN_F32) v4 ? launch_scan<float, 4>(A, cut, st) : launch_scan<float, 1>(A, cut, st);
+    else v4 ? launch_scan<seq::bf16, 4>(A, cut, st) : launch_scan<seq::bf16, 1>(A, cut, st);
     return launched(call);
 }
 
@@ -160,11 +225,14 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream)
             if (m) return bad(call, m);
     }
     hipStream_t st = (hipStream_t)stream;
+    const ScanCut cut = scan_cut(s.B, s.T, s.C);
+    if (scan_workspace(cut, s.B, s.C) && (!g.workspace || !at(g.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanGradArgs A{g.f, g.x, g.dh, g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.carry, g.dlast, g.reset, g.reset_bs, g.reset_ts,
-                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C};
-    const dim3 grid((unsigned)((s.C + 63) / 64), (unsigned)s.B);
-    if (s.dtype == DQN_F32) seq::k_scan_grad<float><<<grid, 64, 0, st>>>(A);
-    else seq::k_scan_grad<seq::bf16><<<grid, 64, 0, st>>>(A);
+                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.range, cut.ranges, (float *)g.workspace, cut.tiles};
+    const bool v4 = four(g.dtype, g.C, {g.f, g.x, g.dh, g.df, g.dx}, {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts},
+                         {g.carry, g.dlast, g.dh0});
+    if (s.dtype == DQN_F32) v4 ? launch_scan_grad<float, 4>(A, cut, st) : launch_scan_grad<float, 1>(A, cut, st);
+    else v4 ? launch_scan_grad<seq::bf16, 4>(A, cut, st) : launch_scan_grad<seq::bf16, 1>(A, cut, st);
     return launched(call);
 }
 

@@ -34,7 +34,10 @@ __device__ __forceinline__ void unpack_e5m2(uint32_t w, float (&o)[4])
     o[0] = lo[0]; o[1] = lo[1]; o[2] = hi[0]; o[3] = hi[1];
 }
 
-// the largest of the wave, a NaN if one holds a NaN
+// Barrier that orders LDS traffic only: global loads and stores stay in flight across it.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// the larger one, or a NaN if one is a NaN
 __device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : (b > a || b != b) ? b : a; }
 
 }  // namespace seq
