@@ -353,10 +353,11 @@ enum { DQN_F32 = 0, DQN_BF16 = 1 };
  * step of an acting agent; h_last may be h0 then, and for any T. */
 typedef struct {
     int32_t dtype;                      /* DQN_F32 / DQN_BF16, of f, x, h           */
-    int32_t B, C;                       /* sequences, channels; >= 0                */
+    int32_t B, C;                       /* sequences 0..65535, channels 0..2^24     */
     int64_t T;                          /* steps, >= 0 (0: h_last = h0)             */
     const void *f, *x;                  /* [B][T][C]                                */
-    int64_t f_bs, f_ts, x_bs, x_ts;     /* strides of a sequence and of a step      */
+    int64_t f_bs, f_ts, x_bs, x_ts;     /* strides of a sequence and of a step; that
+                                           of a step at most 2^24                   */
     const float *h0;                    /* [B][C], or NULL = zeros                  */
     const uint8_t *reset;               /* [B][T], or NULL = no episode starts      */
     int64_t reset_bs, reset_ts;

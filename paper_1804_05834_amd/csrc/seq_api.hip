@@ -41,7 +41,7 @@ bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 
 const char *check_steps(const void *p, int64_t bs, int64_t ts, const dqn_scan_args &s, bool written)
 {
     if (!p || !at(p, bytes_of(s.dtype))) return "a tensor is NULL or not aligned to its elements";
-    if (bs < 0 || ts < 0 || bs > MOST || ts > MOST) return "a stride is negative or too large";
+    if (bs < 0 || ts < 0 || bs > MOST || ts > 1 << 24) return "a stride is negative or too large";   // 16 rows are within 2^30 bytes
     if (ts > 0 && s.T - 1 > MOST / ts) return "T times a stride is too large";
     if (bs > 0 && s.B - 1 > MOST / bs) return "B times a stride is too large";
     if (!written) return nullptr;
@@ -53,7 +53,7 @@ const char *check_steps(const void *p, int64_t bs, int64_t ts, const dqn_scan_ar
 const char *check_scan(const dqn_scan_args &s)
 {
     if (!dtype_ok(s.dtype)) return "dtype must be DQN_F32 or DQN_BF16";
-    if (s.B < 0 || s.C < 0 || s.T < 0 || s.B > 65535 || !size_ok(s.B, s.T, s.C)) return "B must be in 0..65535, T and C >= 0";
+    if (s.B < 0 || s.C < 0 || s.T < 0 || s.B > 65535 || s.C > 1 << 24 || !size_ok(s.B, s.T, s.C)) return "B must be in 0..65535, C in 0..2^24, T >= 0";
     if (!at(s.h0, 4) || !at(s.h_last, 4) || !at(s.carry, 4)) return "a state is not aligned to its elements";
     if (s.reset && (s.reset_bs < 0 || s.reset_ts < 0 || s.reset_bs > MOST || s.reset_ts > MOST ||
                     (s.reset_ts > 0 && s.T - 1 > MOST / s.reset_ts))) return "a stride of reset is negative or too large";
@@ -87,38 +87,44 @@ ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 }
 size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C) { return c.ranges > 1 ? ((size_t)B * c.ranges * 2 * C * 4 + 15) / 16 * 16 : 0; }
 
-// whether four elements of every tensor can be taken at once
-bool four(int32_t dtype, int32_t C, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, std::initializer_list<const void *> states)
+// whether `n` elements of every tensor can be taken at once
+bool together(int n, int32_t dtype, int32_t C, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, std::initializer_list<const void *> states)
 {
-    if (C % 4) return false;
+    if (C % n) return false;
     for (const void *p : tensors)
-        if (!at(p, 4 * bytes_of(dtype))) return false;
+        if (!at(p, n * bytes_of(dtype))) return false;
     for (int64_t s : strides)
-        if (s % 4) return false;
+        if (s % n) return false;
     for (const void *p : states)
-        if (!at(p, 16)) return false;
+        if (!at(p, n * 4)) return false;
     return true;
 }
 
+template <class E, int V> void launch_short(const seq::ScanArgs &A, hipStream_t st)
+{
+    seq::k_scan_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
+}
+template <class E, int V> void launch_short(const seq::ScanGradArgs &A, hipStream_t st)
+{
+    seq::k_scan_grad_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
+}
 template <class E, int V> void launch_scan(const seq::ScanArgs &A, const ScanCut &c, hipStream_t st)
 {
-    if (!c.waves) {
-        seq::k_scan_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
-        return;
-    }
     const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
     if (c.ranges > 1) seq::k_scan<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
     seq::k_scan<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
 }
-template <class E, int V> void launch_scan_grad(const seq::ScanGradArgs &A, const ScanCut &c, hipStream_t st)
+template <class E, int V> void launch_scan(const seq::ScanGradArgs &A, const ScanCut &c, hipStream_t st)
 {
-    if (!c.waves) {
-        seq::k_scan_grad_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
-        return;
-    }
     const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
     if (c.ranges > 1) seq::k_scan_grad<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
     seq::k_scan_grad<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
+}
+// fits(n): whether n channels can be taken at once
+template <class E, class Args, class F> void launch_recurrence(const Args &A, const ScanCut &c, F &&fits, hipStream_t st)
+{
+    if (c.waves) fits(2) ? launch_scan<E, 2>(A, c, st) : launch_scan<E, 1>(A, c, st);
+    else fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
 }
 
 const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
@@ -201,9 +207,8 @@ int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream)
     if (scan_workspace(cut, s.B, s.C) && (!s.workspace || !at(s.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last,
                           s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.range, cut.ranges, (float *)s.workspace, cut.tiles};
-    const bool v4 = four(s.dtype, s.C, {s.f, s.x, s.h}, {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts}, {s.h0, s.h_last, s.carry});
-    if (s.dtype == DQN_F32) v4 ? launch_scan<float, 4>(A, cut, st) : launch_scan<float, 1>(A, cut, st);
-    else v4 ? launch_scan<seq::bf16, 4>(A, cut, st) : launch_scan<seq::bf16, 1>(A, cut, st);
+    auto fits = [&](int n) { return together(n, s.dtype, s.C, {s.f, s.x, s.h}, {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts}, {s.h0, s.h_last, s.carry}); };
+    s.dtype == DQN_F32 ? launch_recurrence<float>(A, cut, fits, st) : launch_recurrence<seq::bf16>(A, cut, fits, st);
     return launched(call);
 }
 
@@ -229,10 +234,11 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream)
     if (scan_workspace(cut, s.B, s.C) && (!g.workspace || !at(g.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanGradArgs A{g.f, g.x, g.dh, g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.carry, g.dlast, g.reset, g.reset_bs, g.reset_ts,
                               g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.range, cut.ranges, (float *)g.workspace, cut.tiles};
-    const bool v4 = four(g.dtype, g.C, {g.f, g.x, g.dh, g.df, g.dx}, {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts},
-                         {g.carry, g.dlast, g.dh0});
-    if (s.dtype == DQN_F32) v4 ? launch_scan_grad<float, 4>(A, cut, st) : launch_scan_grad<float, 1>(A, cut, st);
-    else v4 ? launch_scan_grad<seq::bf16, 4>(A, cut, st) : launch_scan_grad<seq::bf16, 1>(A, cut, st);
+    auto fits = [&](int n) {
+        return together(n, g.dtype, g.C, {g.f, g.x, g.dh, g.df, g.dx}, {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts},
+                        {g.carry, g.dlast, g.dh0});
+    };
+    s.dtype == DQN_F32 ? launch_recurrence<float>(A, cut, fits, st) : launch_recurrence<seq::bf16>(A, cut, fits, st);
     return launched(call);
 }
 
