@@ -423,14 +423,16 @@ typedef struct {
 } dqn_norm_args;
 #define DQN_NORM_MAX 16384
 
-/* Gradients of the norm, from the stored r and rstd: with xh = r rstd, g = weight dy,
+/* Gradients of the norm, from rstd and the same x and residual: with xh = (x + residual)
+ * rstd, g = weight dy,
  *   dx = rstd (g - xh mean(g xh)) + dr   (of x and of the residual alike)
- *   dw = sum over rows of dy xh          (in a fixed order) */
+ *   dw = sum over rows of dy xh          (in a fixed order)
+ * With fp32 the stored r may be given as x, without a residual. */
 typedef struct {
     int32_t dtype, C;
     int64_t M;
-    const void *dy, *r, *dr;            /* [M][C]; dr may be NULL                   */
-    int64_t dy_rs, r_rs, dr_rs;
+    const void *dy, *x, *residual, *dr; /* [M][C]; residual and dr may be NULL      */
+    int64_t dy_rs, x_rs, residual_rs, dr_rs;
     const float *weight, *rstd;
     void *dx;                           /* [M][C]; may be dr                        */
     int64_t dx_rs;

@@ -94,7 +94,7 @@ template <class G, int BITS> __global__ __launch_bounds__(256) void k_adamw(Adam
         }
         if constexpr (BITS == 8) {
             for (int o = 32; o; o >>= 1) { mt = nan_max(mt, __shfl_xor(mt, o)); vt = nan_max(vt, __shfl_xor(vt, o)); }
-            const float mi = mt > 0.f ? E4M3_MAX / mt : 0.f, vi = vt > 0.f ? E5M2_MAX / vt : 0.f;
+            const float mi = mt > 0.f ? product(1.f / mt, E4M3_MAX) : 0.f, vi = vt > 0.f ? product(1.f / vt, E5M2_MAX) : 0.f;
             float mq[4], vq[4];
             for (int j = 0; j < 4; ++j) {
                 const uint64_t z = misc::mix64(A.seed, (uint64_t)(place + j) >> 1);
@@ -107,7 +107,7 @@ template <class G, int BITS> __global__ __launch_bounds__(256) void k_adamw(Adam
                 ((uint32_t *)A.m)[place / 4] = pack_e4m3(mq[0], mq[1], mq[2], mq[3]);
                 ((uint32_t *)A.v)[place / 4] = pack_e5m2(vq[0], vq[1], vq[2], vq[3]);
             }
-            if (lane == 0) { A.ms[place / ADAM_BLOCK] = mt / E4M3_MAX; A.vs[place / ADAM_BLOCK] = vt / E5M2_MAX; }
+            if (lane == 0) { A.ms[place / ADAM_BLOCK] = mt * (1.f / E4M3_MAX); A.vs[place / ADAM_BLOCK] = vt * (1.f / E5M2_MAX); }
         } else {
             for (int j = 0; j < count; ++j) { ((float *)A.m)[place + j] = m[j]; ((float *)A.v)[place + j] = v[j]; }
         }

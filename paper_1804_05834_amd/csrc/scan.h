@@ -75,23 +75,6 @@ template <int V> struct Lane {
     __device__ Lane(int first, int C) : c(min(first, C - V)), live(first < C) {}
 };
 
-template <int V, class T> __device__ __forceinline__ vec<T, V> load(const T *p)
-{
-    if constexpr (V == 1) return vec<T, 1>{*p};
-    else return *reinterpret_cast<const vec<T, V> *>(p);
-}
-template <int V, class T> __device__ __forceinline__ void store(T *p, vec<T, V> v)
-{
-    if constexpr (V == 1) *p = v[0];
-    else *reinterpret_cast<vec<T, V> *>(p) = v;
-}
-template <class E, int V> __device__ __forceinline__ vec<E, V> narrow(const float (&v)[V])
-{
-    vec<E, V> o;
-#pragma unroll
-    for (int k = 0; k < V; ++k) o[k] = (E)v[k];
-    return o;
-}
 template <int V> __device__ __forceinline__ void state(const float *p, float (&s)[V])
 {
     const auto v = load<V>(p);
@@ -209,14 +192,6 @@ struct Resets {
     }
     __device__ __forceinline__ unsigned flags() const { return (unsigned)__ballot(v != 0); }
 };
-
-// x of the lower and of the upper half of the wave, in both
-__device__ __forceinline__ void halves(float x, float &lo, float &hi)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
-    lo = __int_as_float((int)r[0]);
-    hi = __int_as_float((int)r[1]);
-}
 
 // s through a map (a, h) that starts an episode (cut) or not
 __device__ __forceinline__ float through(float s, float a, float h, bool cut) { return cut ? h : fmaf(a, s, h); }

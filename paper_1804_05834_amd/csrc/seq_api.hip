@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <initializer_list>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/dqn.h"
@@ -140,9 +141,56 @@ const char *check_rows8(const void *p, int64_t rs, int64_t M, int64_t K)
     return M == 1 || rs >= K ? nullptr : "the stride of 8-bit rows is shorter than a row";
 }
 
-template <class E> void launch_norm(const seq::NormArgs &N, hipStream_t st) { seq::k_norm<E><<<dim3((unsigned)N.M), 256, 0, st>>>(N); }
+int norm_parts(int64_t M) { return (int)std::min<int64_t>(seq::NORM_PARTS, (M + seq::NORM_ROWS - 1) / seq::NORM_ROWS); }
 
-int norm_parts(int64_t M) { return (int)std::min<int64_t>(seq::NORM_PARTS, (M + 15) / 16); }
+// The smallest form of a norm kernel that holds a row of C elements (8-bit rows: up to the next multiple of 16), V being
+// 16 bytes' worth of elements or 1.  go(V, K, W, lanes) launches it.  A row is one wave's up to 32 (V = 1: 16) elements per
+// lane, four waves' up to four times that; a workgroup of sixteen waves takes longer ones.
+template <int N> using Int = std::integral_constant<int, N>;
+template <class E, class F> void norm_form(bool wide, int C, F &&go)
+{
+    constexpr int V = 16 / (int)sizeof(E);
+    auto lanes = [&](int per) {
+        int n = 1;
+        while (n * per < C) n *= 2;
+        return n;
+    };
+    if (wide) {
+        if (C <= 64 * V) go(Int<V>{}, Int<1>{}, Int<1>{}, lanes(V));
+        else if (C <= 128 * V) go(Int<V>{}, Int<2>{}, Int<1>{}, 64);
+        else if (C <= 64 * 32) go(Int<V>{}, Int<32 / V>{}, Int<1>{}, 64);
+        else if (C <= 256 * 32) go(Int<V>{}, Int<32 / V>{}, Int<4>{}, 64);
+        else go(Int<V>{}, Int<16 / V>{}, Int<16>{}, 64);
+    } else {
+        if (C <= 64) go(Int<1>{}, Int<1>{}, Int<1>{}, lanes(1));
+        else if (C <= 256) go(Int<1>{}, Int<4>{}, Int<1>{}, 64);
+        else if (C <= 1024) go(Int<1>{}, Int<16>{}, Int<1>{}, 64);
+        else if (C <= 4096) go(Int<1>{}, Int<16>{}, Int<4>{}, 64);
+        else go(Int<1>{}, Int<16>{}, Int<16>{}, 64);
+    }
+}
+static_assert(DQN_NORM_MAX == 16 * 64 * 16, "the longest rows that norm_form can hold");
+
+template <class E, bool EIGHT> void launch_norm(seq::NormArgs A, hipStream_t st)
+{
+    constexpr int n = 16 / (int)sizeof(E);
+    const bool wide = together(n, sizeof(E) == 4 ? DQN_F32 : DQN_BF16, A.C, {A.x, A.residual, A.r, A.y}, {A.x_rs, A.residual_rs, A.r_rs, A.y_rs}, {A.weight});
+    norm_form<E>(wide, EIGHT ? (A.C + 15) / 16 * 16 : A.C, [&](auto V, auto K, auto W, int lanes) {
+        A.lanes = lanes;
+        const int64_t rows = W.value > 1 ? 1 : 256 / lanes;
+        const unsigned grid = (unsigned)std::min<int64_t>((A.M + rows - 1) / rows, 1 << 20);
+        seq::k_norm<E, V.value, K.value, W.value, EIGHT><<<dim3(grid), W.value == 1 ? 256 : 64 * W.value, 0, st>>>(A);
+    });
+}
+template <class E> void launch_norm_grad(seq::NormGradArgs A, int parts, hipStream_t st)
+{
+    constexpr int n = 16 / (int)sizeof(E);
+    const bool wide = together(n, sizeof(E) == 4 ? DQN_F32 : DQN_BF16, A.C, {A.dy, A.x, A.residual, A.dr, A.dx}, {A.dy_rs, A.x_rs, A.residual_rs, A.dr_rs, A.dx_rs}, {A.weight});
+    norm_form<E>(wide, A.C, [&](auto V, auto K, auto W, int lanes) {
+        A.lanes = lanes;
+        seq::k_norm_grad<E, V.value, K.value, W.value><<<dim3((unsigned)parts), W.value == 1 ? 256 : 64 * W.value, 0, st>>>(A);
+    });
+}
 
 const char *check_tensors(const dqn_adamw_tensor *t, int32_t count, int32_t bits)
 {
@@ -268,9 +316,10 @@ int32_t dqn_norm_forward(const dqn_norm_args *args, void *stream)
                           n.q ? check_rows8(n.q, n.q_rs, n.M, n.C) : nullptr})
         if (m) return bad(call, m);
     if (n.q && (!n.scale || !at(n.scale, 4))) return bad(call, "scale is NULL or not aligned to its elements");
-    const seq::NormArgs A{n.x, n.residual, n.x_rs, n.residual_rs, n.weight, n.eps, n.r, n.y, n.r_rs, n.y_rs, n.q, n.q_rs, n.scale, n.rstd, n.M, n.C};
-    if (n.dtype == DQN_F32) launch_norm<float>(A, (hipStream_t)stream);
-    else launch_norm<seq::bf16>(A, (hipStream_t)stream);
+    const seq::NormArgs A{n.x, n.residual, n.x_rs, n.residual_rs, n.weight, n.eps, n.r, n.y, n.r_rs, n.y_rs, n.q, n.q_rs, n.scale, n.rstd, n.M, n.C, 0};
+    hipStream_t st = (hipStream_t)stream;
+    if (n.dtype == DQN_F32) n.q ? launch_norm<float, true>(A, st) : launch_norm<float, false>(A, st);
+    else n.q ? launch_norm<seq::bf16, true>(A, st) : launch_norm<seq::bf16, false>(A, st);
     return launched(call);
 }
 
@@ -287,20 +336,15 @@ int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream)
     if (n.M) {
         if (!n.weight || !n.rstd || !at(n.weight, 4) || !at(n.rstd, 4)) return bad(call, "weight or rstd is NULL or not aligned to its elements");
         if (!n.workspace || !at(n.workspace, 16)) return bad(call, "workspace is NULL or not 16-byte aligned");
-        for (const char *m : {check_rows(n.dy, n.dy_rs, n.M, n.C, n.dtype, false), check_rows(n.r, n.r_rs, n.M, n.C, n.dtype, false),
+        for (const char *m : {check_rows(n.dy, n.dy_rs, n.M, n.C, n.dtype, false), check_rows(n.x, n.x_rs, n.M, n.C, n.dtype, false),
+                              n.residual ? check_rows(n.residual, n.residual_rs, n.M, n.C, n.dtype, false) : nullptr,
                               n.dr ? check_rows(n.dr, n.dr_rs, n.M, n.C, n.dtype, false) : nullptr, check_rows(n.dx, n.dx_rs, n.M, n.C, n.dtype, true)})
             if (m) return bad(call, m);
-        const seq::NormGradArgs A{n.dy, n.r, n.dr, n.dy_rs, n.r_rs, n.dr_rs, n.weight, n.rstd, n.dx, n.dx_rs, n.dw, (float *)n.workspace, n.M, n.C, parts};
-        const dim3 grid((unsigned)((n.C + 255) / 256), (unsigned)parts);
-        if (n.dtype == DQN_F32) {
-            seq::k_norm_grad_weight<float><<<grid, 256, 0, st>>>(A);
-            seq::k_norm_grad<float><<<dim3((unsigned)n.M), 256, 0, st>>>(A);
-        } else {
-            seq::k_norm_grad_weight<seq::bf16><<<grid, 256, 0, st>>>(A);
-            seq::k_norm_grad<seq::bf16><<<dim3((unsigned)n.M), 256, 0, st>>>(A);
-        }
+        const seq::NormGradArgs A{n.dy, n.x, n.residual, n.dr, n.dy_rs, n.x_rs, n.residual_rs, n.dr_rs, n.weight, n.rstd, n.dx, n.dx_rs, n.dw, (float *)n.workspace, n.M, n.C, 0};
+        if (n.dtype == DQN_F32) launch_norm_grad<float>(A, parts, st);
+        else launch_norm_grad<seq::bf16>(A, parts, st);
     }
-    seq::k_norm_grad_join<<<dim3((unsigned)((n.C + 255) / 256)), 256, 0, st>>>((const float *)n.workspace, parts, n.C, n.dw);
+    seq::k_norm_grad_join<<<dim3((unsigned)((n.C + 15) / 16)), 1024, 0, st>>>((const float *)n.workspace, parts, n.C, n.dw);
     return launched(call);
 }
 
@@ -313,9 +357,9 @@ int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, in
     if (!scale || !at(scale, 4)) return bad(call, "scale is NULL or not aligned to its elements");
     for (const char *m : {check_rows(x, x_rs, M, K, dtype, false), check_rows8(q, q_rs, M, K)})
         if (m) return bad(call, m);
-    const seq::NormArgs A{x, nullptr, x_rs, 0, nullptr, 0.f, nullptr, nullptr, 0, 0, q, q_rs, scale, nullptr, M, K};
-    if (dtype == DQN_F32) launch_norm<float>(A, (hipStream_t)stream);
-    else launch_norm<seq::bf16>(A, (hipStream_t)stream);
+    const seq::NormArgs A{x, nullptr, x_rs, 0, nullptr, 0.f, nullptr, nullptr, 0, 0, q, q_rs, scale, nullptr, M, K, 0};
+    if (dtype == DQN_F32) launch_norm<float, true>(A, (hipStream_t)stream);
+    else launch_norm<seq::bf16, true>(A, (hipStream_t)stream);
     return launched(call);
 }
 

@@ -40,6 +40,59 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // the larger one, or a NaN if one is a NaN
 __device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : (b > a || b != b) ? b : a; }
 
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// V elements from or to an address that allows V at once
+template <int V, class T> __device__ __forceinline__ vec<T, V> load(const T *p)
+{
+    if constexpr (V == 1) return vec<T, 1>{*p};
+    else return *reinterpret_cast<const vec<T, V> *>(p);
+}
+template <int V, class T> __device__ __forceinline__ void store(T *p, vec<T, V> v)
+{
+    if constexpr (V == 1) *p = v[0];
+    else *reinterpret_cast<vec<T, V> *>(p) = v;
+}
+template <class E, int V> __device__ __forceinline__ vec<E, V> narrow(const float (&v)[V])
+{
+    vec<E, V> o;
+#pragma unroll
+    for (int k = 0; k < V; ++k) o[k] = (E)v[k];
+    return o;
+}
+
+// x of the lower and of the upper half of the wave, in both
+__device__ __forceinline__ void halves(float x, float &lo, float &hi)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
+    lo = __int_as_float((int)r[0]);
+    hi = __int_as_float((int)r[1]);
+}
+
+// f over the values of a group of `lanes` (a power of two) neighbouring lanes, in all of them, f commutative.  By operand
+// permutations and swaps: each is a few cycles, an exchange through LDS about a hundred.
+template <int CTRL> __device__ __forceinline__ float permuted(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+template <class F> __device__ __forceinline__ float group_fold(float v, int lanes, F f)
+{
+    if (lanes > 1) v = f(v, permuted<0xB1>(v));     // lane ^ 1
+    if (lanes > 2) v = f(v, permuted<0x4E>(v));     // lane ^ 2
+    if (lanes > 4) v = f(v, permuted<0x141>(v));    // 7 - lane of eight: the other four hold one value
+    if (lanes > 8) v = f(v, permuted<0x140>(v));    // 15 - lane of sixteen
+    if (lanes > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+        v = f(__int_as_float((int)r[0]), __int_as_float((int)r[1]));
+    }
+    if (lanes > 32) {
+        float lo, hi;
+        halves(v, lo, hi);
+        v = f(lo, hi);
+    }
+    return v;
+}
+
 }  // namespace seq
 
 // Sets what dqn_last_error(NULL) says on this thread and returns `code`.

@@ -120,15 +120,15 @@ def lib():
             "dqn_profile_begin": [vp],
             "dqn_profile_end": [vp, i32, C.POINTER(C.c_char_p), C.POINTER(i64), C.POINTER(C.c_double)],
             "dqn_destroy": [vp],
-            # the operators of seq.py; their structs of arguments are built there
+            # the operators of seq.py, which packs their structs of arguments into bytes
             "dqn_scan_sizes": [i32, i32, i64, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
-            "dqn_scan_forward": [vp, vp],
-            "dqn_scan_backward": [vp, vp],
+            "dqn_scan_forward": [C.c_char_p, vp],
+            "dqn_scan_backward": [C.c_char_p, vp],
             "dqn_norm_sizes": [i64, i32, C.POINTER(C.c_size_t)],
-            "dqn_norm_forward": [vp, vp],
-            "dqn_norm_backward": [vp, vp],
+            "dqn_norm_forward": [C.c_char_p, vp],
+            "dqn_norm_backward": [C.c_char_p, vp],
             "dqn_rows_quantize": [i32, i64, i32, vp, i64, vp, i64, vp, vp],
-            "dqn_rows_product": [vp, vp],
+            "dqn_rows_product": [C.c_char_p, vp],
             "dqn_adamw_sizes": [vp, i32, i32, vp],
             "dqn_adamw_init": [C.POINTER(vp), vp, i32, i32, i32, vp, vp],
             "dqn_adamw_step": [vp, C.c_double, C.c_double, C.c_double, C.c_double, i64, u64, vp],

@@ -12,6 +12,8 @@ and scales float32.  The last dimension of a tensor has stride 1, the others any
 A wrong shape, type or device raises ValueError; what the library refuses raises dqn.DqnError.
 """
 import ctypes as C
+import functools
+import struct
 
 import torch
 
@@ -19,36 +21,15 @@ from .dqn import DqnError, _current_device, _raw_stream, lib
 
 F32, BF16 = 0, 1
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16}
-_vp, _i32, _i64, _f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+_vp, _i64, _f32 = C.c_void_p, C.c_int64, C.c_float
 
-
-class _ScanArgs(C.Structure):
-    _fields_ = [("dtype", _i32), ("B", _i32), ("C", _i32), ("T", _i64), ("f", _vp), ("x", _vp), ("f_bs", _i64), ("f_ts", _i64),
-                ("x_bs", _i64), ("x_ts", _i64), ("h0", _vp), ("reset", _vp), ("reset_bs", _i64), ("reset_ts", _i64),
-                ("h", _vp), ("h_bs", _i64), ("h_ts", _i64), ("h_last", _vp), ("carry", _vp), ("workspace", _vp)]
-
-
-class _ScanGradArgs(C.Structure):
-    _fields_ = [("dtype", _i32), ("B", _i32), ("C", _i32), ("T", _i64), ("f", _vp), ("x", _vp), ("f_bs", _i64), ("f_ts", _i64),
-                ("x_bs", _i64), ("x_ts", _i64), ("carry", _vp), ("reset", _vp), ("reset_bs", _i64), ("reset_ts", _i64),
-                ("dh", _vp), ("dh_bs", _i64), ("dh_ts", _i64), ("dlast", _vp), ("df", _vp), ("dx", _vp),
-                ("df_bs", _i64), ("df_ts", _i64), ("dx_bs", _i64), ("dx_ts", _i64), ("dh0", _vp), ("workspace", _vp)]
-
-
-class _NormArgs(C.Structure):
-    _fields_ = [("dtype", _i32), ("C", _i32), ("M", _i64), ("x", _vp), ("residual", _vp), ("x_rs", _i64), ("residual_rs", _i64),
-                ("weight", _vp), ("eps", _f32), ("r", _vp), ("r_rs", _i64), ("y", _vp), ("y_rs", _i64), ("q", _vp), ("q_rs", _i64),
-                ("scale", _vp), ("rstd", _vp)]
-
-
-class _NormGradArgs(C.Structure):
-    _fields_ = [("dtype", _i32), ("C", _i32), ("M", _i64), ("dy", _vp), ("r", _vp), ("dr", _vp), ("dy_rs", _i64), ("r_rs", _i64),
-                ("dr_rs", _i64), ("weight", _vp), ("rstd", _vp), ("dx", _vp), ("dx_rs", _i64), ("dw", _vp), ("workspace", _vp)]
-
-
-class _ProductArgs(C.Structure):
-    _fields_ = [("dtype", _i32), ("N", _i32), ("K", _i32), ("M", _i64), ("a", _vp), ("w", _vp), ("a_rs", _i64), ("w_rs", _i64),
-                ("a_scale", _vp), ("w_scale", _vp), ("bias", _vp), ("y", _vp), ("y_rs", _i64)]
+# The structs of arguments of include/dqn.h, as bytes: a call reads them and keeps nothing, and packing them costs a third of
+# filling a ctypes.Structure.  i: int32, q: int64, f: float, P: pointer, in C's own layout.
+SCAN_ARGS = struct.Struct("iiiqPPqqqqPPqqPqqPPP")
+SCAN_GRAD_ARGS = struct.Struct("iiiqPPqqqqPPqqPqqPPPqqqqPP")
+NORM_ARGS = struct.Struct("iiqPPqqPfPqPqPqPP")
+NORM_GRAD_ARGS = struct.Struct("iiqPPPPqqqqPPPqPP")
+PRODUCT_ARGS = struct.Struct("iiiqPPqqPPPPq")
 
 
 class _AdamWTensor(C.Structure):
@@ -69,58 +50,60 @@ def _call(rc):
         raise DqnError(rc, (lib().dqn_last_error(None) or b"").decode())
 
 
-def _need(t, name, dtype, shape):
+def _need(t, name, dtype, shape, device):
     """t's address, after a look at what it is."""
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError("%s: %s of shape %s expected, got %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-    if t.get_device() != _current_device():
+    if t.get_device() != device:
         raise ValueError("%s: not on the current GPU" % name)
-    if t.ndim and t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError("%s: the last dimension must have stride 1" % name)
     return t.data_ptr()
 
 
-def _flat(t, name, dtype, shape):
-    """The same for a tensor that must lie in one piece, or None."""
-    if t is None:
-        return None
+def _rows(t, name, dtype, shape, device):
+    """(address, strides) of a tensor whose last dimension lies in one piece."""
+    p, st = _need(t, name, dtype, shape, device), t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s: the last dimension must have stride 1" % name)
+    return p, st
+
+
+def _flat(t, name, dtype, shape, device):
+    """The address of a tensor that must lie in one piece."""
     if not t.is_contiguous():
         raise ValueError("%s: must be contiguous" % name)
-    return _need(t, name, dtype, shape)
+    return _need(t, name, dtype, shape, device)
 
 
-def _dtype(t, name):
-    if t.dtype not in _TYPES:
+def _kind(t, name):
+    k = _TYPES.get(t.dtype)
+    if k is None:
         raise ValueError("%s: float32 or bfloat16 expected, got %s" % (name, t.dtype))
-    return t.dtype
-
-
-def _stream():
-    return _raw_stream(_current_device())
+    return k
 
 
 def _scratch(n, device):
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
+    """(a workspace of n bytes or None, its address or 0)"""
+    if not n:
+        return None, 0
+    t = torch.empty(n, dtype=torch.uint8, device=device)
+    return t, t.data_ptr()
 
 
 # ------------------------------------------------------------------ gated linear recurrence
+@functools.lru_cache(maxsize=256)
 def _scan_sizes(kind, B, T, Ch):
     carry, work = C.c_size_t(), C.c_size_t()
     _call(lib().dqn_scan_sizes(kind, B, T, Ch, C.byref(carry), C.byref(work)))
     return carry.value, work.value
 
 
-def _reset(reset, B, T):
+def _reset(reset, B, T, device):
     """(address, stride of a sequence, stride of a step)"""
     if reset is None:
-        return None, 0, 0
-    if reset.dtype not in (torch.uint8, torch.bool) or reset.shape != (B, T) or reset.get_device() != _current_device():
+        return 0, 0, 0
+    if reset.dtype not in (torch.uint8, torch.bool) or reset.shape != (B, T) or reset.get_device() != device:
         raise ValueError("reset: uint8 or bool of shape (%d, %d) on the current GPU expected" % (B, T))
-    return reset.data_ptr(), reset.stride(0), reset.stride(1)
+    return (reset.data_ptr(), *reset.stride())
 
 
 def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
@@ -129,135 +112,160 @@ def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
     f, x: [B][T][C]; h0: [B][C] float32 or None (zeros); reset: [B][T] uint8 / bool or None.  out: a tensor for h;
     last: one for the final state, which may be h0 itself.  -> (h, final state [B][C] float32), and with save=True a
     third value that scan_backward needs."""
-    dt = _dtype(f, "f")
-    if f.ndim != 3:
+    kind, dt, shape, dev = _kind(f, "f"), f.dtype, f.shape, _current_device()
+    if len(shape) != 3:
         raise ValueError("f: [B][T][C] expected")
-    shape = f.shape
     B, T, Ch = shape
-    kind = _TYPES[dt]
-    fp, xp = _need(f, "f", dt, shape), _need(x, "x", dt, shape)
-    h0p = _flat(h0, "h0", torch.float32, (B, Ch))
-    rp, rb, rt = _reset(reset, B, T)
+    fp, fs = _rows(f, "f", dt, shape, dev)
+    xp, xs = _rows(x, "x", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
     h = torch.empty(shape, dtype=dt, device=f.device) if out is None else out
-    hp = _need(h, "out", dt, shape)
+    hp, hs = _rows(h, "out", dt, shape, dev)
     if last is None:
-        last = torch.empty(B, Ch, dtype=torch.float32, device=f.device)
-    lp = _flat(last, "last", torch.float32, (B, Ch))
+        last = torch.empty((B, Ch), dtype=torch.float32, device=f.device)
     carry = torch.empty(carry_n // 4, dtype=torch.float32, device=f.device) if save else None
-    work = _scratch(work_n, f.device)
-    fs, xs, hs = f.stride(), x.stride(), h.stride()
-    a = _ScanArgs(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1], h0p, rp, rb, rt, hp, hs[0], hs[1], lp, _at(carry), _at(work))
-    _call(lib().dqn_scan_forward(C.byref(a), _stream()))
+    work, wp = _scratch(work_n, f.device)
+    rp, rb, rt = _reset(reset, B, T, dev)
+    args = SCAN_ARGS.pack(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1],
+                          0 if h0 is None else _flat(h0, "h0", torch.float32, (B, Ch), dev), rp, rb, rt, hp, hs[0], hs[1],
+                          _flat(last, "last", torch.float32, (B, Ch), dev), carry.data_ptr() if save else 0, wp)
+    _call(lib().dqn_scan_forward(args, _raw_stream(dev)))
     return (h, last, carry) if save else (h, last)
 
 
 def scan_backward(dh, f, x, carry, reset=None, dlast=None, out=None):
     """Gradients of scan: dh [B][T][C] of h, dlast [B][C] float32 of the final state (or None), f, x, reset as they were,
     carry from scan(save=True).  out: (df, dx) to write into.  -> (df, dx, dh0 [B][C] float32)"""
-    dt = _dtype(f, "f")
-    if f.ndim != 3:
+    kind, dt, shape, dev = _kind(f, "f"), f.dtype, f.shape, _current_device()
+    if len(shape) != 3:
         raise ValueError("f: [B][T][C] expected")
-    shape = f.shape
     B, T, Ch = shape
-    kind = _TYPES[dt]
-    fp, xp, gp = _need(f, "f", dt, shape), _need(x, "x", dt, shape), _need(dh, "dh", dt, shape)
-    rp, rb, rt = _reset(reset, B, T)
+    fp, fs = _rows(f, "f", dt, shape, dev)
+    xp, xs = _rows(x, "x", dt, shape, dev)
+    gp, gs = _rows(dh, "dh", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
-    cp = _flat(carry, "carry", torch.float32, (carry_n // 4,))
-    dlp = _flat(dlast, "dlast", torch.float32, (B, Ch))
     df, dx = (torch.empty(shape, dtype=dt, device=f.device), torch.empty(shape, dtype=dt, device=f.device)) if out is None else out
-    dfp, dxp = _need(df, "df", dt, shape), _need(dx, "dx", dt, shape)
-    dh0 = torch.empty(B, Ch, dtype=torch.float32, device=f.device)
-    work = _scratch(work_n, f.device)
-    fs, xs, gs, ds, es = f.stride(), x.stride(), dh.stride(), df.stride(), dx.stride()
-    a = _ScanGradArgs(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1], cp, rp, rb, rt, gp, gs[0], gs[1], dlp, dfp, dxp,
-                      ds[0], ds[1], es[0], es[1], dh0.data_ptr(), _at(work))
-    _call(lib().dqn_scan_backward(C.byref(a), _stream()))
+    dfp, dfs = _rows(df, "df", dt, shape, dev)
+    dxp, dxs = _rows(dx, "dx", dt, shape, dev)
+    dh0 = torch.empty((B, Ch), dtype=torch.float32, device=f.device)
+    work, wp = _scratch(work_n, f.device)
+    rp, rb, rt = _reset(reset, B, T, dev)
+    args = SCAN_GRAD_ARGS.pack(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1], _flat(carry, "carry", torch.float32, (carry_n // 4,), dev),
+                               rp, rb, rt, gp, gs[0], gs[1], 0 if dlast is None else _flat(dlast, "dlast", torch.float32, (B, Ch), dev),
+                               dfp, dxp, dfs[0], dfs[1], dxs[0], dxs[1], dh0.data_ptr(), wp)
+    _call(lib().dqn_scan_backward(args, _raw_stream(dev)))
     return df, dx, dh0
 
 
 # ------------------------------------------------------------------ norm
-def _rows_of(x):
-    if x.ndim != 2:
-        raise ValueError("x: [M][C] expected")
-    return _dtype(x, "x"), x.shape
+def _matrix(t, name):
+    k, shape = _kind(t, name), t.shape
+    if len(shape) != 2:
+        raise ValueError("%s: [M][C] expected" % name)
+    return k, shape
 
 
-def _new_rows8(M, K, device):
-    """8-bit rows as the library lays them out: a stride that is a multiple of 16."""
-    return torch.empty(M, (K + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device=device)[:, :K]
+def _rows8(M, K, device):
+    """8-bit rows as the library lays them out, their stride a multiple of 16: (the rows, that stride)"""
+    st = (K + 15) & -16
+    q = torch.empty((M, st), dtype=torch.float8_e4m3fn, device=device)
+    return (q if st == K else q[:, :K]), st
 
 
-def _norm(x, weight, residual, eps, eight):
-    dt, shape = _rows_of(x)
-    M, Ch = shape
-    xp, wp = _need(x, "x", dt, shape), _flat(weight, "weight", torch.float32, (Ch,))
-    r = y = q = scale = rstd = rp = None
-    if residual is not None:
-        rp = _need(residual, "residual", dt, shape)
-        r = torch.empty(shape, dtype=dt, device=x.device)
-    if eight:
-        q, scale = _new_rows8(M, Ch, x.device), torch.empty(M, dtype=torch.float32, device=x.device)
-    else:
-        y, rstd = torch.empty(shape, dtype=dt, device=x.device), torch.empty(M, dtype=torch.float32, device=x.device)
-    a = _NormArgs(_TYPES[dt], Ch, M, xp, rp, x.stride(0), residual.stride(0) if residual is not None else 0, wp, eps,
-                  _at(r), Ch, _at(y), Ch, _at(q), q.stride(0) if eight else 0, _at(scale), _at(rstd))
-    _call(lib().dqn_norm_forward(C.byref(a), _stream()))
-    r = x if r is None else r
-    return (q, scale, r) if eight else (y, r, rstd)
+def _residual(x, residual, shape, dev):
+    """(address, stride, r to write, its address); nothing of it without a residual"""
+    if residual is None:
+        return 0, 0, x, 0
+    p, st = _rows(residual, "residual", x.dtype, shape, dev)
+    r = torch.empty(shape, dtype=x.dtype, device=x.device)
+    return p, st[0], r, r.data_ptr()
 
 
 def norm(x, weight, residual=None, eps=1e-6):
-    """Per row of x [M][C]: r = x + residual, y = weight r / sqrt(mean r^2 + eps).  -> (y, r, 1 / sqrt(...) [M]);
+    """Per row of x [M][C]: r = x + residual, y = weight r / sqrt(mean r^2 + eps).  -> (y, r, what norm_backward needs);
     without a residual r is x."""
-    return _norm(x, weight, residual, eps, False)
+    (kind, shape), dev = _matrix(x, "x"), _current_device()
+    M, Ch = shape
+    xp, xs = _rows(x, "x", x.dtype, shape, dev)
+    sp, ss, r, rp = _residual(x, residual, shape, dev)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    rstd = torch.empty(M, dtype=torch.float32, device=x.device)
+    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, Ch,
+                          y.data_ptr(), Ch, 0, 0, 0, rstd.data_ptr())
+    _call(lib().dqn_norm_forward(args, _raw_stream(dev)))
+    # in bf16 the backward pass forms the sum again from its two terms, since r is rounded
+    return y, r, (rstd, x, residual) if kind == BF16 else (rstd, r, None)
 
 
 def norm_rows(x, weight, residual=None, eps=1e-6):
     """The same with y in 8 bits: -> (q [M][C] e4m3, scale [M], r) with y ~ q scale[:, None]."""
-    return _norm(x, weight, residual, eps, True)
-
-
-def norm_backward(dy, r, rstd, weight, dr=None):
-    """dy of y and dr of r (or None) -> (gradient of x and of the residual alike [M][C], of the weight [C])."""
-    dt, shape = _rows_of(r)
+    (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, Ch = shape
-    work_n = C.c_size_t()
-    _call(lib().dqn_norm_sizes(M, Ch, C.byref(work_n)))
-    dx, dw = torch.empty(shape, dtype=dt, device=r.device), torch.empty(Ch, dtype=torch.float32, device=r.device)
-    work = _scratch(work_n.value, r.device)
-    a = _NormGradArgs(_TYPES[dt], Ch, M, _need(dy, "dy", dt, shape), _need(r, "r", dt, shape),
-                      None if dr is None else _need(dr, "dr", dt, shape), dy.stride(0), r.stride(0), 0 if dr is None else dr.stride(0),
-                      _flat(weight, "weight", torch.float32, (Ch,)), _flat(rstd, "rstd", torch.float32, (M,)), dx.data_ptr(), Ch,
-                      dw.data_ptr(), _at(work))
-    _call(lib().dqn_norm_backward(C.byref(a), _stream()))
+    xp, xs = _rows(x, "x", x.dtype, shape, dev)
+    sp, ss, r, rp = _residual(x, residual, shape, dev)
+    q, qs = _rows8(M, Ch, x.device)
+    scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, Ch,
+                          0, 0, q.data_ptr(), qs, scale.data_ptr(), 0)
+    _call(lib().dqn_norm_forward(args, _raw_stream(dev)))
+    return q, scale, r
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_sizes(M, Ch):
+    work = C.c_size_t()
+    _call(lib().dqn_norm_sizes(M, Ch, C.byref(work)))
+    return work.value
+
+
+def norm_backward(dy, r, saved, weight, dr=None):
+    """dy of y and dr of r (or None), r and saved from norm() -> (gradient of x and of the residual alike [M][C], of the
+    weight [C])."""
+    (kind, shape), dev = _matrix(r, "r"), _current_device()
+    M, Ch = shape
+    dt = r.dtype
+    rstd, x, residual = saved
+    gp, gs = _rows(dy, "dy", dt, shape, dev)
+    xp, xs = _rows(x, "x", dt, shape, dev)
+    sp, ss = (0, (0,)) if residual is None else _rows(residual, "residual", dt, shape, dev)
+    rp, rs = (0, (0,)) if dr is None else _rows(dr, "dr", dt, shape, dev)
+    dx = torch.empty(shape, dtype=dt, device=r.device)
+    dw = torch.empty(Ch, dtype=torch.float32, device=r.device)
+    work, wp = _scratch(_norm_sizes(M, Ch), r.device)
+    args = NORM_GRAD_ARGS.pack(kind, Ch, M, gp, xp, sp, rp, gs[0], xs[0], ss[0], rs[0], _flat(weight, "weight", torch.float32, (Ch,), dev),
+                               _flat(rstd, "rstd", torch.float32, (M,), dev), dx.data_ptr(), Ch, dw.data_ptr(), wp)
+    _call(lib().dqn_norm_backward(args, _raw_stream(dev)))
     return dx, dw
 
 
 # ------------------------------------------------------------------ 8-bit rows and their product
 def rows(x):
     """x [M][K] in 8 bits: -> (q [M][K] e4m3, scale [M]) with x ~ q scale[:, None]."""
-    dt, (M, K) = _rows_of(x)
-    xp = _need(x, "x", dt, (M, K))
-    q, scale = _new_rows8(M, K, x.device), torch.empty(M, dtype=torch.float32, device=x.device)
-    _call(lib().dqn_rows_quantize(_TYPES[dt], M, K, xp, x.stride(0), q.data_ptr(), q.stride(0), scale.data_ptr(), _stream()))
+    (kind, shape), dev = _matrix(x, "x"), _current_device()
+    M, K = shape
+    xp, xs = _rows(x, "x", x.dtype, shape, dev)
+    q, qs = _rows8(M, K, x.device)
+    scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    _call(lib().dqn_rows_quantize(kind, M, K, xp, xs[0], q.data_ptr(), qs, scale.data_ptr(), _raw_stream(dev)))
     return q, scale
 
 
 def product(a, w, bias=None, dtype=torch.bfloat16, out=None):
     """a = (q [M][K], scale [M]) and w = (q [N][K], scale [N]) as rows() and norm_rows() give them, bias [N] float32 or None
     -> y [M][N] of `dtype`."""
-    (qa, sa), (qw, sw) = a, w
-    M, K = qa.shape
-    N = qw.shape[0]
-    if dtype not in _TYPES:
-        raise ValueError("dtype: float32 or bfloat16 expected")
-    y = torch.empty(M, N, dtype=dtype, device=qa.device) if out is None else out
-    args = _ProductArgs(_TYPES[dtype], N, K, M, _need(qa, "a", torch.float8_e4m3fn, (M, K)), _need(qw, "w", torch.float8_e4m3fn, (N, K)),
-                        qa.stride(0), qw.stride(0), _flat(sa, "a's scale", torch.float32, (M,)), _flat(sw, "w's scale", torch.float32, (N,)),
-                        _flat(bias, "bias", torch.float32, (N,)), _need(y, "out", dtype, (M, N)), y.stride(0))
-    _call(lib().dqn_rows_product(C.byref(args), _stream()))
+    (qa, sa), (qw, sw), dev = a, w, _current_device()
+    kind = _TYPES.get(dtype)
+    if kind is None or qa.ndim != 2 or qw.ndim != 2:
+        raise ValueError("dtype: float32 or bfloat16 expected; rows: [M][K] and [N][K]")
+    (M, K), N = qa.shape, qw.shape[0]
+    ap, as_ = _rows(qa, "a", torch.float8_e4m3fn, (M, K), dev)
+    wp, ws = _rows(qw, "w", torch.float8_e4m3fn, (N, K), dev)
+    y = torch.empty((M, N), dtype=dtype, device=qa.device) if out is None else out
+    yp, ys = _rows(y, "out", dtype, (M, N), dev)
+    args = PRODUCT_ARGS.pack(kind, N, K, M, ap, wp, as_[0], ws[0], _flat(sa, "a's scale", torch.float32, (M,), dev),
+                             _flat(sw, "w's scale", torch.float32, (N,), dev), 0 if bias is None else _flat(bias, "bias", torch.float32, (N,), dev),
+                             yp, ys[0])
+    _call(lib().dqn_rows_product(args, _raw_stream(dev)))
     return y
 
 
@@ -275,35 +283,34 @@ class AdamW:
         copies = list(copies) if copies is not None else [None] * n
         if not n or len(grads) != n or len(decays) != n or len(copies) != n:
             raise ValueError("one gradient, weight decay and copy per parameter expected")
-        gt = _dtype(grads[0], "grads")
+        kind, gt, dev, device = _kind(grads[0], "grads"), grads[0].dtype, _current_device(), params[0].device
         table = (_AdamWTensor * n)()
         for i, (p, g, d, c) in enumerate(zip(params, grads, decays, copies)):
-            table[i] = _AdamWTensor(_flat(p, "params", torch.float32, p.shape), _flat(g, "grads", gt, p.shape),
-                                    _flat(c, "copies", torch.bfloat16, p.shape), p.numel(), d)
+            table[i] = _AdamWTensor(_flat(p, "params", torch.float32, p.shape, dev), _flat(g, "grads", gt, p.shape, dev),
+                                    None if c is None else _flat(c, "copies", torch.bfloat16, p.shape, dev), p.numel(), d)
         self._keep = (list(params), list(grads), copies)     # the table holds their addresses
-        dev = params[0].device
         sz = _AdamWBytes()
         _call(lib().dqn_adamw_sizes(table, n, bits, C.byref(sz)))
         P, eight = sz.elements, bits == 8
         mt, vt = (torch.float8_e4m3fn, torch.float8_e5m2) if eight else (torch.float32, torch.float32)
         if state is None:
-            state = (torch.zeros(P, device=dev).to(mt), torch.zeros(P, device=dev).to(vt),
-                     torch.zeros(P // 256, device=dev) if eight else None, torch.zeros(P // 256, device=dev) if eight else None)
+            state = (torch.zeros(P, device=device).to(mt), torch.zeros(P, device=device).to(vt),
+                     torch.zeros(P // 256, device=device) if eight else None, torch.zeros(P // 256, device=device) if eight else None)
         self.m, self.v, self.m_scale, self.v_scale = state
-        b = _AdamWBuffers(_flat(self.m, "m", mt, (P,)), _flat(self.v, "v", vt, (P,)),
-                          _flat(self.m_scale, "m_scale", torch.float32, (P // 256,)) if eight else None,
-                          _flat(self.v_scale, "v_scale", torch.float32, (P // 256,)) if eight else None)
-        self._plan = torch.empty(sz.plan, dtype=torch.uint8, device=dev)
+        b = _AdamWBuffers(_flat(self.m, "m", mt, (P,), dev), _flat(self.v, "v", vt, (P,), dev),
+                          _flat(self.m_scale, "m_scale", torch.float32, (P // 256,), dev) if eight else None,
+                          _flat(self.v_scale, "v_scale", torch.float32, (P // 256,), dev) if eight else None)
+        self._plan = torch.empty(sz.plan, dtype=torch.uint8, device=device)
         b.plan = self._plan.data_ptr()
         self.lr, self.betas, self.eps, self.bits = lr, betas, eps, bits
         h = C.c_void_p()
-        _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, _TYPES[gt], C.byref(b), _stream()))
+        _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, kind, C.byref(b), _raw_stream(dev)))
         self._h = h
 
     def step(self, step, seed=0, lr=None):
         """Step number `step` (from 1).  seed: of the random rounding of 8-bit moments, another one for each step."""
         _call(lib().dqn_adamw_step(self._h, self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, step,
-                                   seed & 0xFFFFFFFFFFFFFFFF, _stream()))
+                                   seed & 0xFFFFFFFFFFFFFFFF, _raw_stream(_current_device())))
 
     def close(self):
         if getattr(self, "_h", None):

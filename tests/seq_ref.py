@@ -69,7 +69,7 @@ def norm(x, weight, residual=None, eps=1e-6):
     return r, y, rstd[:, 0], er, np.abs(y) * (erel + 4 * U), erel
 
 
-def norm_backward(dy, r, rstd, weight, dr=None):
+def norm_backward(dy, r, rstd, weight, dr=None):     # r: the sum before it is rounded
     """-> (dx, dw), their bounds"""
     M, C = r.shape
     xh, g = r * rstd[:, None], dy * weight
@@ -117,7 +117,7 @@ def moments8(m, v, seed):
     for x, top, word, mantissa, lowest in ((m, 448.0, bits & 0xFFFF, 3, -6), (v, 57344.0, bits >> 16, 2, -14)):
         b = x.reshape(-1, 256)
         most = np.abs(b).max(1)
-        inv = np.where(most > 0, np.float32(top) / np.where(most > 0, most, 1).astype(np.float32), np.float32(0)).astype(np.float32)
+        inv = np.where(most > 0, np.float32(1) / np.where(most > 0, most, 1).astype(np.float32) * np.float32(top), np.float32(0)).astype(np.float32)
         q = np.abs((b * inv[:, None]).astype(np.float32)).reshape(-1)
         # above 2^lowest the lattice of 32-bit numbers themselves, their lower bits being the part that is rounded
         drop = 23 - mantissa
@@ -127,5 +127,5 @@ def moments8(m, v, seed):
         q = np.minimum(np.where(q < 2.0 ** lowest, small, up), np.float32(top))
         if mantissa == 2:
             q = np.where(x > 0, np.maximum(q, unit), q)
-        out += [np.copysign(q, x), (most / np.float32(top)).astype(np.float32)]
+        out += [np.copysign(q, x), (most * (np.float32(1) / np.float32(top))).astype(np.float32)]
     return out

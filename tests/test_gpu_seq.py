@@ -191,7 +191,8 @@ def test_norm(seq, M, C, residual, layout, dtype):
     print("case norm", M, C, residual, layout, dtype, flush=True)
     bf = dtype == "bf16"
     x, res, w = norm_case(M, C, residual, dtype, layout)
-    y, r, rstd = seq.norm(x, w, residual=res)
+    y, r, saved = seq.norm(x, w, residual=res)
+    rstd = saved[0]
     wr, wy, wrstd, er, ey, erel = ref.norm(host(x), host(w), host(res))
     close(r, wr, ref.stored(er, wr, bf), "r")
     close(y, wy, ref.stored(ey, wy, bf), "y")
@@ -207,13 +208,13 @@ def test_norm(seq, M, C, residual, layout, dtype):
     assert q.stride(0) == pad
     whole = q.as_strided((M, pad), (pad, 1)).view(torch.uint8)
     assert int(whole[:, C:].sum()) == 0
-    # gradients, from the r and rstd that are handed over
+    # gradients, from the rstd that is handed over and the sum as it is before it is rounded
     dy, dr = rnd(50, M, C, dtype=TYPES[dtype]), rnd(51, M, C, dtype=TYPES[dtype]) if residual else None
-    dx, dw = seq.norm_backward(dy, r, rstd, w, dr=dr)
-    (wdx, wdw), (edx, edw) = ref.norm_backward(host(dy), host(r), host(rstd), host(w), host(dr))
+    dx, dw = seq.norm_backward(dy, r, saved, w, dr=dr)
+    (wdx, wdw), (edx, edw) = ref.norm_backward(host(dy), wr, host(rstd), host(w), host(dr))
     close(dx, wdx, ref.stored(edx, wdx, bf), "dx")
     close(dw, wdw, edw + 1e-37, "dw")
-    dx2, dw2 = seq.norm_backward(dy, r, rstd, w, dr=dr)
+    dx2, dw2 = seq.norm_backward(dy, r, saved, w, dr=dr)
     assert torch.equal(dx, dx2) and torch.equal(dw, dw2)      # no order that changes
 
 
@@ -502,7 +503,7 @@ def test_refusals(seq):
     for call in (lambda: seq.scan(f, x[:, :3]), lambda: seq.scan(f, x.to(torch.bfloat16)), lambda: seq.scan(f.half(), x.half()),
                  lambda: seq.scan(f, x.cpu()), lambda: seq.scan(f, x, h0=rnd(3, 2, 9)), lambda: seq.scan(f, x, reset=torch.zeros(2, 5, device="cuda")),
                  lambda: seq.scan(f.transpose(1, 2), x.transpose(1, 2)), lambda: seq.scan_backward(f, f, x, rnd(1, 3)),
-                 lambda: seq.norm(f.view(8, 8), rnd(1, 7)), lambda: seq.norm(f, rnd(1, 8)), lambda: seq.norm_backward(rnd(1, 2, 4), rnd(1, 2, 4), rnd(1, 3), rnd(1, 4)),
+                 lambda: seq.norm(f.view(8, 8), rnd(1, 7)), lambda: seq.norm(f, rnd(1, 8)), lambda: seq.norm_backward(rnd(1, 2, 4), rnd(1, 2, 4), (rnd(1, 3), rnd(1, 2, 4), None), rnd(1, 4)),
                  lambda: seq.product(seq.rows(rnd(1, 3, 16)), seq.rows(rnd(1, 3, 17))), lambda: seq.product(seq.rows(rnd(1, 3, 16)), seq.rows(rnd(1, 3, 16)), bias=rnd(1, 4)),
                  lambda: seq.AdamW([f], []), lambda: seq.AdamW([f], [x[0]]), lambda: seq.AdamW([f.to(torch.bfloat16)], [x])):
         with pytest.raises(ValueError):

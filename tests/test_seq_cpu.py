@@ -40,74 +40,68 @@ def test_sizes_and_null_arguments(lib):
 P = 1 << 20      # an address that is aligned; no call below gets as far as using it
 
 
+def packed(layout, fields, kw):
+    """The bytes of a struct of arguments from its fields' values, some of them replaced."""
+    assert set(kw) <= set(fields)
+    return layout.pack(*(kw.get(k, v) or 0 for k, v in fields.items()))
+
+
 def scan_args(**kw):
-    a = seq._ScanArgs(0, 2, 8, 4, P, P, 32, 8, 32, 8, None, None, 0, 0, P, 32, 8, None, None, None)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return a
+    return packed(seq.SCAN_ARGS, dict(dtype=0, B=2, C=8, T=4, f=P, x=P, f_bs=32, f_ts=8, x_bs=32, x_ts=8, h0=0, reset=0, reset_bs=0, reset_ts=0, h=P, h_bs=32, h_ts=8,
+                                      h_last=0, carry=0, workspace=0), kw)
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=5), dict(B=-1), dict(B=70000), dict(C=-2), dict(T=-1), dict(f=None), dict(x=None), dict(h=None), dict(f=P + 2),
-                                dict(h=P + 1), dict(f_bs=-1), dict(x_ts=-8), dict(h_ts=7), dict(h_bs=8), dict(f_ts=1 << 60), dict(h0=P + 2), dict(h_last=P + 1),
+                                dict(h=P + 1), dict(f_bs=-1), dict(x_ts=-8), dict(h_ts=7), dict(h_bs=8), dict(f_ts=1 << 60), dict(h0=P + 2), dict(h_last=P + 1), dict(f_ts=(1 << 24) + 1), dict(B=60000, C=60000),
                                 dict(carry=P + 2), dict(reset=P, reset_ts=-1), dict(reset=P, reset_bs=1 << 60)])
 def test_scan_refuses(lib, kw):
-    assert lib.dqn_scan_forward(C.byref(scan_args(**kw)), None) == dqn.ERR_INVALID_ARG and "dqn_scan_forward" in said(lib)
+    assert lib.dqn_scan_forward(scan_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_scan_forward" in said(lib)
 
 
 def test_scan_of_nothing_does_nothing(lib):
-    assert lib.dqn_scan_forward(C.byref(scan_args(B=0)), None) == lib.dqn_scan_forward(C.byref(scan_args(C=0, f=None)), None) == dqn.OK
+    assert lib.dqn_scan_forward(scan_args(B=0), None) == lib.dqn_scan_forward(scan_args(C=0, f=None), None) == dqn.OK
 
 
 def grad_args(**kw):
-    a = seq._ScanGradArgs(0, 2, 8, 4, P, P, 32, 8, 32, 8, P, None, 0, 0, P, 32, 8, None, P, P, 32, 8, 32, 8, None, None)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return a
+    return packed(seq.SCAN_GRAD_ARGS, dict(dtype=0, B=2, C=8, T=4, f=P, x=P, f_bs=32, f_ts=8, x_bs=32, x_ts=8, carry=P, reset=0, reset_bs=0, reset_ts=0, dh=P, dh_bs=32, dh_ts=8,
+                                           dlast=0, df=P, dx=P, df_bs=32, df_ts=8, dx_bs=32, dx_ts=8, dh0=0, workspace=0), kw)
 
 
 @pytest.mark.parametrize("kw", [dict(carry=None), dict(dh=None), dict(df=None), dict(dx=P + 2), dict(df_ts=4), dict(dx_bs=0), dict(dh_ts=-1), dict(dlast=P + 2), dict(dh0=P + 3)])
 def test_scan_backward_refuses(lib, kw):
-    assert lib.dqn_scan_backward(C.byref(grad_args(**kw)), None) == dqn.ERR_INVALID_ARG and "dqn_scan_backward" in said(lib)
+    assert lib.dqn_scan_backward(grad_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_scan_backward" in said(lib)
 
 
 def norm_args(**kw):
-    a = seq._NormArgs(0, 8, 4, P, None, 8, 0, P, 1e-6, None, 0, P, 8, None, 0, None, None)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return a
+    return packed(seq.NORM_ARGS, dict(dtype=0, C=8, M=4, x=P, residual=0, x_rs=8, residual_rs=0, weight=P, eps=1e-6, r=0, r_rs=0, y=P, y_rs=8, q=0, q_rs=0, scale=0, rstd=0), kw)
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=2), dict(C=0), dict(C=16385), dict(M=-1), dict(eps=-1.0), dict(eps=float("nan")), dict(x=None), dict(x=P + 2), dict(weight=None), dict(y=None),
                                 dict(y=P, q=P, q_rs=16, scale=P), dict(y=None, q=P, q_rs=16), dict(y=None, q=P + 8, q_rs=16, scale=P), dict(y=None, q=P, q_rs=8, scale=P),
                                 dict(y_rs=7), dict(x_rs=-1), dict(r=P, r_rs=4), dict(residual=P + 1), dict(x_rs=1 << 60)])
 def test_norm_refuses(lib, kw):
-    assert lib.dqn_norm_forward(C.byref(norm_args(**kw)), None) == dqn.ERR_INVALID_ARG and "dqn_norm_forward" in said(lib)
+    assert lib.dqn_norm_forward(norm_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_norm_forward" in said(lib)
 
 
 def norm_grad_args(**kw):
-    a = seq._NormGradArgs(0, 8, 4, P, P, None, 8, 8, 0, P, P, P, 8, P, P)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return a
+    return packed(seq.NORM_GRAD_ARGS, dict(dtype=0, C=8, M=4, dy=P, x=P, residual=0, dr=0, dy_rs=8, x_rs=8, residual_rs=0, dr_rs=0, weight=P, rstd=P, dx=P, dx_rs=8, dw=P,
+                                           workspace=P), kw)
 
 
-@pytest.mark.parametrize("kw", [dict(dy=None), dict(r=None), dict(rstd=None), dict(weight=None), dict(dx=None), dict(dx_rs=7), dict(dw=None), dict(workspace=None), dict(workspace=P + 4),
+@pytest.mark.parametrize("kw", [dict(dy=None), dict(x=None), dict(residual=P + 2), dict(rstd=None), dict(weight=None), dict(dx=None), dict(dx_rs=7), dict(dw=None), dict(workspace=None), dict(workspace=P + 4),
                                 dict(dr=P + 2), dict(C=0), dict(M=-3)])
 def test_norm_backward_refuses(lib, kw):
-    assert lib.dqn_norm_backward(C.byref(norm_grad_args(**kw)), None) == dqn.ERR_INVALID_ARG and "dqn_norm_backward" in said(lib)
+    assert lib.dqn_norm_backward(norm_grad_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_norm_backward" in said(lib)
 
 
 def product_args(**kw):
-    a = seq._ProductArgs(1, 8, 20, 4, P, P, 32, 32, P, P, None, P, 8)
-    for k, v in kw.items():
-        setattr(a, k, v)
-    return a
+    return packed(seq.PRODUCT_ARGS, dict(dtype=1, N=8, K=20, M=4, a=P, w=P, a_rs=32, w_rs=32, a_scale=P, w_scale=P, bias=0, y=P, y_rs=8), kw)
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=9), dict(M=-1), dict(N=-1), dict(K=-1), dict(N=1 << 21), dict(a=None), dict(a=P + 8), dict(w=P + 1), dict(a_rs=24), dict(w_rs=16), dict(a_scale=None),
                                 dict(w_scale=P + 2), dict(bias=P + 1), dict(y=None), dict(y_rs=7), dict(y=P + 1)])
 def test_product_refuses(lib, kw):
-    assert lib.dqn_rows_product(C.byref(product_args(**kw)), None) == dqn.ERR_INVALID_ARG and "dqn_rows_product" in said(lib)
+    assert lib.dqn_rows_product(product_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_rows_product" in said(lib)
 
 
 def test_adamw_refuses(lib):
