@@ -1,26 +1,29 @@
 // AdamW over many tensors in one launch, moments in 32 or 8 bits.
+//
+// Bound by memory: 28 bytes per element with 32-bit moments and fp32 gradients, 14.06 with 8-bit moments and bf16 gradients.
+// A wave takes blocks of 256 elements, four per lane: the elements that share a scale, so that the largest is found within
+// the wave.  A workgroup's share, a chunk, has a record of its own in the plan (addresses, length, decay): a look-up
+// of the chunk's tensor and then of the tensor would be two trips to memory before the first element is asked for.
 #pragma once
 #include "seq_common.h"
 #include "sumtree.h"
 
 namespace seq {
 
-constexpr int ADAM_BLOCK = 256;          // elements that share a scale: one wave, four elements per lane
-constexpr int ADAM_CHUNK = 2048;         // elements of a workgroup
+constexpr int ADAM_BLOCK = 256;   // elements that share a scale: one wave, four elements per lane
+constexpr int ADAM_DEEP = 2;      // blocks of a wave, all of whose loads are in flight together
+constexpr int ADAM_CHUNK = 4 * ADAM_DEEP * ADAM_BLOCK;   // elements of a workgroup of four waves
 
-struct AdamTensor {
+struct AdamChunk {
     float *param;
     const void *grad;
     uint16_t *copy;
-    long n, at;      // elements; place of its moments in the buffers of moments
+    long at;         // place of its first moment in the buffers of moments
+    int n;           // elements, up to ADAM_CHUNK
     float decay;
-    int wide;        // every pointer allows four elements at a time
-};
-struct AdamChunk {
-    int tensor, block;   // first block of the chunk within the tensor, in units of ADAM_CHUNK
+    int wide, pad;   // whether every pointer allows four elements at a time
 };
 struct AdamArgs {
-    const AdamTensor *tensors;
     const AdamChunk *chunks;
     void *m, *v;
     float *ms, *vs;
@@ -28,15 +31,27 @@ struct AdamArgs {
     uint64_t seed;
 };
 
-// |x| >= 0 to MANTISSA bits (below 2^LOWEST: to multiples of the smallest number of the type), up where the 16 random
-// bits are the larger and down where they are not, so that x is kept on average
-template <int MANTISSA, int LOWEST> __device__ __forceinline__ float rounded(float x, uint32_t bits)
+// |x| to MANTISSA bits (below 2^LOWEST: to multiples of the smallest number of the type), up where the 16 random bits are
+// the larger and down where they are not, so that x is kept on average.  Numbers that small are rare: a wave
+// without any skips their form (zero comes out of both).
+template <int MANTISSA, int LOWEST> __device__ __forceinline__ void rounded(float (&x)[4], const uint32_t (&bits)[4])
 {
     constexpr int drop = 23 - MANTISSA;
-    const float unit = __int_as_float((127 + LOWEST - MANTISSA) << 23);   // 2^(LOWEST - MANTISSA)
-    const float normal = __uint_as_float((__float_as_uint(x) + (bits << (drop - 16))) & ~((1u << drop) - 1));
-    const float small = floorf(x * (1.f / unit) + (float)bits * (1.f / 65536.f)) * unit;
-    return x < __int_as_float((127 + LOWEST) << 23) ? small : normal;
+    const float lowest = __int_as_float((127 + LOWEST) << 23), unit = __int_as_float((127 + LOWEST - MANTISSA) << 23);
+    float y[4];
+    bool small = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        y[j] = __uint_as_float((__float_as_uint(x[j]) + (bits[j] << (drop - 16))) & ~((1u << drop) - 1));
+        small |= x[j] < lowest && x[j] != 0.f;
+    }
+    if (__any(small)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (x[j] < lowest) y[j] = floorf(x[j] * (1.f / unit) + (float)bits[j] * (1.f / 65536.f)) * unit;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = y[j];
 }
 
 // The new moments, every product and sum rounded by itself (no contraction into fused forms): what is rounded to 8 bits at
@@ -52,64 +67,131 @@ __device__ __forceinline__ float product(float a, float b)
 #pragma clang fp contract(off)
     return a * b;
 }
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN if one is a NaN
+
+// What a lane holds of a block: four elements and their moments.
+template <class G, int BITS> struct AdamLane {
+    using Word = std::conditional_t<BITS == 8, uint32_t, vec<float, 4>>;
+    vec<float, 4> p;
+    vec<G, 4> g;
+    Word m, v;
+    float ms, vs;
+    int first, count;   // place in the chunk, elements of the lane
+    bool whole;         // of the wave's whole block: four elements at a time
+
+    __device__ __forceinline__ void fetch(const AdamArgs &A, const AdamChunk &ch, int block)
+    {
+        const int base = block * ADAM_BLOCK;
+        first = base + 4 * (threadIdx.x & 63);
+        count = min(4, max(0, ch.n - first));
+        whole = ch.wide && ch.n >= base + ADAM_BLOCK;
+        if (whole) {
+            p = load<4>(ch.param + first);
+            g = load<4>((const G *)ch.grad + first);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p[j] = j < count ? ch.param[first + j] : 0.f;
+                g[j] = j < count ? ((const G *)ch.grad)[first + j] : (G)0.f;
+            }
+        }
+        const long place = ch.at + first;     // the buffers of moments go on to the end of the block
+        m = reinterpret_cast<const Word *>(A.m)[place / 4];
+        v = reinterpret_cast<const Word *>(A.v)[place / 4];
+        if constexpr (BITS == 8) {
+            ms = A.ms[place / ADAM_BLOCK];
+            vs = A.vs[place / ADAM_BLOCK];
+        }
+    }
+
+    __device__ __forceinline__ void step(const AdamArgs &A, const AdamChunk &ch, float keep, int lane)
+    {
+        float mn[4], vn[4];
+        if constexpr (BITS == 8) {
+            unpack_e4m3(m, mn);
+            unpack_e5m2(v, vn);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { mn[j] = product(mn[j], ms); vn[j] = product(vn[j], vs); }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { mn[j] = m[j]; vn[j] = v[j]; }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            moments(mn[j], vn[j], (float)g[j], A.b1, A.c1, A.b2, A.c2);
+            p[j] = p[j] * keep - A.rate * mn[j] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(vn[j]), A.root, A.eps));
+        }
+        if (whole) {
+            store<4>(ch.param + first, p);
+            if (ch.copy) store<4>((bf16 *)ch.copy + first, __builtin_convertvector(p, vec<bf16, 4>));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j < count) {
+                    ch.param[first + j] = p[j];
+                    if (ch.copy) ((bf16 *)ch.copy)[first + j] = (bf16)p[j];
+                } else {
+                    mn[j] = vn[j] = 0.f;
+                }
+            }
+        }
+        const long place = ch.at + first;
+        if constexpr (BITS == 8) {
+            float mt = 0.f, vt = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { mt = larger(mt, fabsf(mn[j])); vt = larger(vt, vn[j]); }
+            mt = group_fold(mt, 64, larger);
+            vt = group_fold(vt, 64, larger);
+            const float mi = mt > 0.f ? product(1.f / mt, E4M3_MAX) : 0.f, vi = vt > 0.f ? product(1.f / vt, E5M2_MAX) : 0.f;
+            uint32_t mb[4], vb[4];
+            float mq[4], vq[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t z = misc::mix64(A.seed, (uint64_t)(place + j) >> 1);
+                const uint32_t bits = (uint32_t)(j & 1 ? z >> 32 : z);
+                mb[j] = bits & 0xFFFF;
+                vb[j] = bits >> 16;
+                mq[j] = fabsf(product(mn[j], mi));
+                vq[j] = product(vn[j], vi);
+            }
+            rounded<3, -6>(mq, mb);
+            rounded<2, -14>(vq, vb);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                mq[j] = copysignf(fminf(mq[j], E4M3_MAX), mn[j]);
+                vq[j] = fminf(vn[j] > 0.f ? fmaxf(vq[j], 1.f / 65536.f) : vq[j], E5M2_MAX);   // one that is not zero does not become zero
+            }
+            if (count) {
+                reinterpret_cast<uint32_t *>(A.m)[place / 4] = pack_e4m3(mq[0], mq[1], mq[2], mq[3]);
+                reinterpret_cast<uint32_t *>(A.v)[place / 4] = pack_e5m2(vq[0], vq[1], vq[2], vq[3]);
+            }
+            if (lane == 0) {
+                A.ms[place / ADAM_BLOCK] = mt * (1.f / E4M3_MAX);
+                A.vs[place / ADAM_BLOCK] = vt * (1.f / E5M2_MAX);
+            }
+        } else if (count) {
+            reinterpret_cast<vec<float, 4> *>(A.m)[place / 4] = vec<float, 4>{mn[0], mn[1], mn[2], mn[3]};
+            reinterpret_cast<vec<float, 4> *>(A.v)[place / 4] = vec<float, 4>{vn[0], vn[1], vn[2], vn[3]};
+        }
+    }
+};
 
 template <class G, int BITS> __global__ __launch_bounds__(256) void k_adamw(AdamArgs A)
 {
     const AdamChunk ch = A.chunks[blockIdx.x];
-    const AdamTensor T = A.tensors[ch.tensor];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const G *grad = (const G *)T.grad;
-    const float keep = 1.f - A.lr * T.decay;
-    for (int k = wave; k < ADAM_CHUNK / ADAM_BLOCK; k += 4) {
-        const long first = (long)ch.block * ADAM_CHUNK + (long)k * ADAM_BLOCK + 4 * lane;   // in the tensor
-        if (first - 4 * lane >= T.n) break;
-        const long place = T.at + first;
-        const int count = (int)min(4l, max(0l, T.n - first));
-        float p[4], g[4], m[4], v[4], ms = 0.f, vs = 0.f;
-        for (int j = 0; j < 4; ++j) {
-            p[j] = j < count ? T.param[first + j] : 0.f;
-            g[j] = j < count ? (float)grad[first + j] : 0.f;
-            m[j] = v[j] = 0.f;
-        }
-        if constexpr (BITS == 8) {
-            ms = A.ms[place / ADAM_BLOCK];
-            vs = A.vs[place / ADAM_BLOCK];
-            unpack_e4m3(((const uint32_t *)A.m)[place / 4], m);
-            unpack_e5m2(((const uint32_t *)A.v)[place / 4], v);
-            for (int j = 0; j < 4; ++j) { m[j] = product(m[j], ms); v[j] = product(v[j], vs); }
-        } else {
-            for (int j = 0; j < count; ++j) { m[j] = ((const float *)A.m)[place + j]; v[j] = ((const float *)A.v)[place + j]; }
-        }
-        float mt = 0.f, vt = 0.f;
-        for (int j = 0; j < 4; ++j) {
-            moments(m[j], v[j], g[j], A.b1, A.c1, A.b2, A.c2);
-            if (j >= count) m[j] = v[j] = 0.f;
-            mt = nan_max(mt, fabsf(m[j]));
-            vt = nan_max(vt, v[j]);
-            p[j] = p[j] * keep - A.rate * m[j] / (sqrtf(v[j]) * A.root + A.eps);
-            if (j < count) {
-                T.param[first + j] = p[j];
-                if (T.copy) ((bf16 *)T.copy)[first + j] = (bf16)p[j];
-            }
-        }
-        if constexpr (BITS == 8) {
-            for (int o = 32; o; o >>= 1) { mt = nan_max(mt, __shfl_xor(mt, o)); vt = nan_max(vt, __shfl_xor(vt, o)); }
-            const float mi = mt > 0.f ? product(1.f / mt, E4M3_MAX) : 0.f, vi = vt > 0.f ? product(1.f / vt, E5M2_MAX) : 0.f;
-            float mq[4], vq[4];
-            for (int j = 0; j < 4; ++j) {
-                const uint64_t z = misc::mix64(A.seed, (uint64_t)(place + j) >> 1);
-                const uint32_t bits = (uint32_t)(j & 1 ? z >> 32 : z);
-                mq[j] = copysignf(fminf(rounded<3, -6>(fabsf(product(m[j], mi)), bits & 0xFFFF), E4M3_MAX), m[j]);
-                vq[j] = fminf(rounded<2, -14>(product(v[j], vi), bits >> 16), E5M2_MAX);
-                if (v[j] > 0.f) vq[j] = fmaxf(vq[j], 1.f / 65536.f);
-            }
-            if (count) {
-                ((uint32_t *)A.m)[place / 4] = pack_e4m3(mq[0], mq[1], mq[2], mq[3]);
-                ((uint32_t *)A.v)[place / 4] = pack_e5m2(vq[0], vq[1], vq[2], vq[3]);
-            }
-            if (lane == 0) { A.ms[place / ADAM_BLOCK] = mt * (1.f / E4M3_MAX); A.vs[place / ADAM_BLOCK] = vt * (1.f / E5M2_MAX); }
-        } else {
-            for (int j = 0; j < count; ++j) { ((float *)A.m)[place + j] = m[j]; ((float *)A.v)[place + j] = v[j]; }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float keep = 1.f - A.lr * ch.decay;
+    const int first = wave * ADAM_DEEP, blocks = min(ADAM_DEEP, (ch.n + ADAM_BLOCK - 1) / ADAM_BLOCK - first);
+    AdamLane<G, BITS> b[ADAM_DEEP];
+    if (blocks == ADAM_DEEP) {
+#pragma unroll
+        for (int k = 0; k < ADAM_DEEP; ++k) b[k].fetch(A, ch, first + k);
+#pragma unroll
+        for (int k = 0; k < ADAM_DEEP; ++k) b[k].step(A, ch, keep, lane);
+    } else {
+        for (int k = 0; k < blocks; ++k) {
+            b[0].fetch(A, ch, first + k);
+            b[0].step(A, ch, keep, lane);
         }
     }
 }

@@ -10,8 +10,6 @@
 // Bound by memory: forward reads f and x and writes h once, backward reads f, x and dh and writes df and dx; the
 // states are not kept but computed again from one in every tile of steps (`carry`).
 #pragma once
-#include <type_traits>
-
 #include "seq_common.h"
 
 namespace seq {

@@ -219,7 +219,7 @@ AdamSizes adamw_sizes(const dqn_adamw_tensor *t, int32_t count)
     }
     return s;
 }
-size_t plan_bytes(const AdamSizes &s, int32_t count) { return ((size_t)count * sizeof(seq::AdamTensor) + (size_t)s.chunks * sizeof(seq::AdamChunk) + 255) / 256 * 256; }
+size_t plan_bytes(const AdamSizes &s) { return ((size_t)std::max<int64_t>(s.chunks, 1) * sizeof(seq::AdamChunk) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -395,7 +395,7 @@ int32_t dqn_adamw_sizes(const dqn_adamw_tensor *tensors, int32_t count, int32_t 
     out->elements = s.elements;
     out->m = out->v = (size_t)s.elements * (bits / 8);
     out->m_scale = out->v_scale = bits == 8 ? (size_t)s.elements / seq::ADAM_BLOCK * 4 : 0;
-    out->plan = plan_bytes(s, count);
+    out->plan = plan_bytes(s);
     return DQN_OK;
 }
 
@@ -416,16 +416,16 @@ int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t
     if (s.chunks > INT32_MAX) return bad(call, "too many elements");
     dqn_adamw *o = nullptr;
     try {
-        std::vector<uint8_t> table(plan_bytes(s, count), 0);
-        seq::AdamTensor *t = reinterpret_cast<seq::AdamTensor *>(table.data());
-        seq::AdamChunk *c = reinterpret_cast<seq::AdamChunk *>(t + count);
+        std::vector<uint8_t> table(plan_bytes(s), 0);
+        seq::AdamChunk *c = reinterpret_cast<seq::AdamChunk *>(table.data());
         int64_t place = 0;
         for (int32_t i = 0; i < count; ++i) {
             const dqn_adamw_tensor &u = tensors[i];
             const bool wide = at(u.param, 16) && at(u.grad, 4 * bytes_of(grad_dtype)) && at(u.copy, 8);
-            t[i] = seq::AdamTensor{u.param, u.grad, u.copy, (long)u.n, (long)place, u.decay, wide};
+            for (int64_t k = 0; k < u.n; k += seq::ADAM_CHUNK)
+                *c++ = seq::AdamChunk{u.param + k, (const uint8_t *)u.grad + k * bytes_of(grad_dtype), u.copy ? u.copy + k : nullptr, (long)(place + k),
+                                      (int)std::min<int64_t>(seq::ADAM_CHUNK, u.n - k), u.decay, wide, 0};
             place += (u.n + seq::ADAM_BLOCK - 1) / seq::ADAM_BLOCK * seq::ADAM_BLOCK;
-            for (int64_t k = 0; k < (u.n + seq::ADAM_CHUNK - 1) / seq::ADAM_CHUNK; ++k) *c++ = seq::AdamChunk{i, (int)k};
         }
         hipStream_t st = (hipStream_t)stream;
         if (hipMemcpyAsync(bufs->plan, table.data(), table.size(), hipMemcpyHostToDevice, st) != hipSuccess || hipStreamSynchronize(st) != hipSuccess) {
@@ -436,8 +436,7 @@ int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t
     } catch (...) {
         return dqn_seq_fail(DQN_ERR_OOM, call, "out of host memory");
     }
-    o->args.tensors = (const seq::AdamTensor *)bufs->plan;
-    o->args.chunks = (const seq::AdamChunk *)(o->args.tensors + count);
+    o->args.chunks = (const seq::AdamChunk *)bufs->plan;
     o->args.m = bufs->m; o->args.v = bufs->v; o->args.ms = bufs->m_scale; o->args.vs = bufs->v_scale;
     o->chunks = s.chunks; o->bits = bits; o->grad_dtype = grad_dtype;
     *out = o;
