@@ -454,7 +454,7 @@ int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, in
  * not count. */
 typedef struct {
     int32_t dtype, N, K;                /* of y; N >= 0, K >= 0                     */
-    int64_t M;                          /* >= 0                                     */
+    int64_t M;                          /* >= 0; ceil(M / 256) ceil(N / 256) <= 2^22 */
     const uint8_t *a, *w;               /* [M][K], [N][K]                           */
     int64_t a_rs, w_rs;
     const float *a_scale, *w_scale;     /* [M], [N]                                 */

@@ -3,6 +3,7 @@
 
 #include <cmath>
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 #include <new>
 #include <type_traits>
@@ -192,6 +193,42 @@ template <class E> void launch_norm_grad(seq::NormGradArgs A, int parts, hipStre
     });
 }
 
+// A tile kernel needs more LDS than a workgroup gets without asking; asked for once per kernel (and again by a racing thread, which does no harm).
+template <class E, int BM, int BN, int WM, int WN> bool launch_tile(const seq::ProductArgs &A, hipStream_t st)
+{
+    constexpr int bytes = 2 * (BM + BN) * 128;
+    auto kernel = seq::k_product_tile<E, BM, BN, WM, WN>;
+    if (bytes > 65536) {
+        static std::atomic<uint64_t> granted{0};   // a bit per device
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev > 63) return false;
+        if (!(granted.load(std::memory_order_relaxed) >> dev & 1)) {
+            if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+                (void)hipGetLastError();
+                return false;
+            }
+            granted.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+    }
+    const int64_t tiles = (A.M + BM - 1) / BM * ((A.N + BN - 1) / BN);
+    kernel<<<dim3((unsigned)tiles), 64 * WM * WN, bytes, st>>>(A);
+    return true;
+}
+template <class E, int MI, int NI> bool launch_few(const seq::ProductArgs &A, hipStream_t st)
+{
+    const int64_t tiles = (A.M + 16 * MI - 1) / (16 * MI) * ((A.N + 16 * NI - 1) / (16 * NI));
+    seq::k_product_few<E, MI, NI><<<dim3((unsigned)tiles), 64 * seq::FEW_WAVES, 0, st>>>(A);
+    return true;
+}
+template <class E> bool launch_product(const seq::ProductArgs &A, hipStream_t st)
+{
+    const int64_t tiles128 = (A.M + 127) / 128 * ((A.N + 127) / 128), tiles256 = (A.M + 255) / 256 * ((A.N + 255) / 256);
+    if (tiles256 >= 192) return launch_tile<E, 256, 256, 2, 4>(A, st);
+    if (A.M > 64 && tiles128 >= 64) return launch_tile<E, 128, 128, 2, 2>(A, st);
+    if (A.M <= 16) return launch_few<E, 1, 1>(A, st);
+    return launch_few<E, 2, 2>(A, st);
+}
+
 const char *check_tensors(const dqn_adamw_tensor *t, int32_t count, int32_t bits)
 {
     if (!t || count < 1 || count > 65536) return "count must be in 1..65536, tensors not NULL";
@@ -371,17 +408,17 @@ int32_t dqn_rows_product(const dqn_product_args *args, void *stream)
     const dqn_product_args &p = *args;
     if (!dtype_ok(p.dtype)) return bad(call, "dtype must be DQN_F32 or DQN_BF16");
     if (p.M < 0 || p.N < 0 || p.K < 0 || p.M > INT32_MAX - 1024 || p.N > (1 << 20) || p.K > (1 << 24)) return bad(call, "M must be in 0..2^31-1025, N in 0..2^20, K in 0..2^24");
+    if ((p.M + 255) / 256 * ((p.N + 255) / 256) > 1 << 22) return bad(call, "ceil(M / 256) times ceil(N / 256) must be at most 2^22");
     if (!p.M || !p.N) return DQN_OK;
     for (const char *m : {p.K ? check_rows8(p.a, p.a_rs, p.M, p.K) : nullptr, p.K ? check_rows8(p.w, p.w_rs, p.N, p.K) : nullptr,
                           check_rows(p.y, p.y_rs, p.M, p.N, p.dtype, true)})
         if (m) return bad(call, m);
     if (!p.a_scale || !p.w_scale || !at(p.a_scale, 4) || !at(p.w_scale, 4) || !at(p.bias, 4)) return bad(call, "a scale is NULL or a pointer is not aligned to its elements");
     hipStream_t st = (hipStream_t)stream;
-    const seq::ProductArgs A{p.a, p.w, p.a_rs, p.w_rs, p.a_scale, p.w_scale, p.bias, p.y, p.y_rs, p.M, p.N, p.K};
-    const dim3 grid((unsigned)((p.M + 15) / 16), (unsigned)((p.N + 15) / 16));
-    if (p.dtype == DQN_F32) seq::k_product<float><<<grid, 64, 0, st>>>(A);
-    else seq::k_product<seq::bf16><<<grid, 64, 0, st>>>(A);
-    return launched(call);
+    const seq::ProductArgs A{p.a, p.w, p.a_rs, p.w_rs, p.a_scale, p.w_scale, p.bias, p.y, p.y_rs, p.M, p.N, p.K,
+                             p.y_rs % 4 == 0 && at(p.y, 4 * bytes_of(p.dtype))};
+    const bool ok = p.dtype == DQN_F32 ? launch_product<float>(A, st) : launch_product<seq::bf16>(A, st);
+    return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }
 
 // ------------------------------------------------------------ AdamW
