@@ -20,7 +20,7 @@ struct ProductArgs {
     void *y;
     long y_rs, M;
     int N, K;
-    int wide;   // whether four columns of y can be stored at once
+    int wide;   // columns of y that can be stored at once: 1, 4 or, in bf16, 8
 };
 
 using Bytes32 = vec<int, 8>;
@@ -82,7 +82,7 @@ template <class E> __device__ __forceinline__ void put(const ProductArgs &A, lon
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = (E)(s[j] * sa * w[j] + b[j]);
     E *p = (E *)A.y + m * A.y_rs + n;
-    if (A.wide && n + 4 <= A.N) {
+    if (A.wide >= 4 && n + 4 <= A.N) {
         *reinterpret_cast<vec<E, 4> *>(p) = v;
     } else {
 #pragma unroll
@@ -166,7 +166,8 @@ template <class E, int MI, int NI> __global__ __launch_bounds__(64 * FEW_WAVES) 
 // ------------------------------------------------------------ tiles
 // BM x BN outputs per workgroup, WM x WN waves, 128 k a step, two steps' operands in LDS: while one is multiplied, the
 // next comes from memory past the registers.  A row of a step is 128 bytes in eight pieces of 16; piece c of row r has
-// the place c ^ (r % 8), so that the eight rows that LDS serves together meet every bank once.
+// the place c ^ (r / 2 % 8), so that the sixteen lanes that LDS serves together, a piece of sixteen rows, meet each of
+// its 64 banks once.
 
 // 16 bytes per lane from memory to LDS, lane l's to p + 16 l.  In assembly, because the compiler would let every LDS
 // read behind it wait for its arrival; the barrier of a step waits for all of them.
@@ -204,11 +205,12 @@ template <class E, int BM, int BN, int WM, int WN> __global__ __launch_bounds__(
     const int n0 = tile.n * BN, full = A.K / 128, steps = (A.K + 127) / 128;
 
     const uint8_t *src[LOADS];   // row and piece of this lane in the wave's loads
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    static_assert(LOADS % 2 == 0, "a wave's loads begin at a multiple of sixteen rows");
+    auto piece = [&](int q) { return ((lane & 7) ^ (lane >> 4) ^ (q & 1) * 4) * 16; };
 #pragma unroll
     for (int q = 0; q < LOADS; ++q) {
         const int r = (wave * LOADS + q) * 8 + (lane >> 3);
-        src[q] = (r < BM ? A.a + min(m0 + r, A.M - 1) * A.a_rs : A.w + (long)min(n0 + r - BM, A.N - 1) * A.w_rs) + piece;
+        src[q] = (r < BM ? A.a + min(m0 + r, A.M - 1) * A.a_rs : A.w + (long)min(n0 + r - BM, A.N - 1) * A.w_rs) + piece(q);
     }
     auto fetch = [&](int step) {
         uint8_t *to = lds + (step & 1) * STAGE + wave * LOADS * 1024;
@@ -218,11 +220,11 @@ template <class E, int BM, int BN, int WM, int WN> __global__ __launch_bounds__(
         } else {   // the last step, where K ends within it
 #pragma unroll
             for (int q = 0; q < LOADS; ++q)
-                *reinterpret_cast<vec<uint32_t, 4> *>(to + q * 1024 + lane * 16) = row_piece(src[q] - piece, step * 128 + piece, A.K);
+                *reinterpret_cast<vec<uint32_t, 4> *>(to + q * 1024 + lane * 16) = row_piece(src[q] - piece(q), step * 128 + piece(q), A.K);
         }
     };
     const int wm = wave % WM * MI * 16, wn = wave / WM * NI * 16;
-    const int place = i * 128 + ((2 * g) ^ (i & 7)) * 16;   // of this lane's first piece among 16 rows; the second: place ^ 16
+    const int place = i * 128 + ((2 * g) ^ (i >> 1)) * 16;   // of this lane's first piece among 16 rows; the second: place ^ 16
     Acc s[MI][NI] = {};
     if (steps) fetch(0);
     for (int step = 0; step < steps; ++step) {
@@ -235,13 +237,48 @@ template <class E, int BM, int BN, int WM, int WN> __global__ __launch_bounds__(
         Operand<E> w[NI];
 #pragma unroll
         for (int y = 0; y < NI; ++y) w[y].set(piece32(lw + y * 2048));
+        Bytes32 next = piece32(la);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NI + 2, 0);
 #pragma unroll
-        for (int x = 0; x < MI; ++x) {
+        for (int x = 0; x < MI; ++x) {   // the next 16 rows are read behind the products of these
             Operand<E> a;
-            a.set(piece32(la + x * 2048));
+            a.set(next);
+            if (x + 1 < MI) next = piece32(la + (x + 1) * 2048);
 #pragma unroll
             for (int y = 0; y < NI; ++y) s[x][y] = mac(w[y], a, s[x][y]);
+            if (x + 1 < MI) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NI * (sizeof(E) == 2 ? 1 : 4), 0);
         }
+    }
+    // y in bf16, whole columns: a wave's 64 columns are a 128-byte line of a row.  Stored as the lanes hold them, 8 bytes of
+    // each of sixteen rows, they took 19 us of a tile of 8192 x 4096 outputs; through LDS, whose operands are done
+    // with, a lane stores 16 bytes and eight lanes a line.  Pieces of 16 bytes change places as the operands' do.
+    constexpr bool lines = sizeof(E) == 2 && NI == 4;
+    if (lines && A.wide == 8 && n0 + wn + 64 <= A.N) {
+        __syncthreads();
+        uint8_t *mine = lds + wave * (MI * 2048);
+#pragma unroll
+        for (int y = 0; y < NI; ++y) {
+            const int n = n0 + wn + 16 * y + 4 * g;
+            const Acc sw = four_of(A.w_scale, n, A.N), b = four_of(A.bias, n, A.N);
+#pragma unroll
+            for (int x = 0; x < MI; ++x) {
+                const float sa = A.a_scale[min(m0 + wm + 16 * x + i, A.M - 1)];
+                vec<bf16, 4> v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = (bf16)(s[x][y][j] * sa * sw[j] + b[j]);
+                *reinterpret_cast<vec<bf16, 4> *>(mine + x * 2048 + i * 128 + ((2 * y + g / 2) ^ (i >> 1)) * 16 + (g & 1) * 8) = v;
+            }
+        }
+        // the wave reads what it wrote itself: no barrier, the order of its own LDS accesses does
+#pragma unroll
+        for (int q = 0; q < 2 * MI; ++q) {
+            const int r = 8 * q + (lane >> 3), c = lane & 7;
+            const auto v = *reinterpret_cast<const vec<uint32_t, 4> *>(mine + r * 128 + (c ^ (r >> 1 & 7)) * 16);
+            const long m = m0 + wm + r;
+            if (m < A.M) *reinterpret_cast<vec<uint32_t, 4> *>((E *)A.y + m * A.y_rs + n0 + wn + 8 * c) = v;
+        }
+        return;
     }
 #pragma unroll
     for (int y = 0; y < NI; ++y) {

@@ -220,13 +220,20 @@ template <class E, int MI, int NI> bool launch_few(const seq::ProductArgs &A, hi
     seq::k_product_few<E, MI, NI><<<dim3((unsigned)tiles), 64 * seq::FEW_WAVES, 0, st>>>(A);
     return true;
 }
+// The largest tiles of which there are enough for the compute units; below that the outputs are few and K is shared.
+// Measured, us, bf16 y (M x N x K: 16 x 16 and 32 x 32 few outputs, tiles of 64, 128, 256):
+//   32 x 1024 x 512:     3.3   3.9   4.8   7.1  11.4      64 x 4096 x 4096:  17.1  10.3  13.0  23.9  48.2
+//   256 x 1024 x 1024:   6.3   4.8   6.3   9.6  17.4     128 x 4096 x 4096:  31.4  17.5  13.1  23.8  48.3
+//   2048 x 1024 x 512:  18.3  11.8   6.8   8.0  12.5    2048 x 2048 x 2048: 117    60.2  18.2  16.9  29.8
+//   8192 x 1024 x 512:  62.8  43.3  15.7  11.5  14.7    4096 x 4096 x 2048:     -     -  59.9  41.0  36.0
 template <class E> bool launch_product(const seq::ProductArgs &A, hipStream_t st)
 {
-    const int64_t tiles128 = (A.M + 127) / 128 * ((A.N + 127) / 128), tiles256 = (A.M + 255) / 256 * ((A.N + 255) / 256);
-    if (tiles256 >= 192) return launch_tile<E, 256, 256, 2, 4>(A, st);
-    if (A.M > 64 && tiles128 >= 64) return launch_tile<E, 128, 128, 2, 2>(A, st);
-    if (A.M <= 16) return launch_few<E, 1, 1>(A, st);
-    return launch_few<E, 2, 2>(A, st);
+    auto tiles = [&](int64_t n) { return (A.M + n - 1) / n * ((A.N + n - 1) / n); };
+    if (tiles(256) >= 192) return launch_tile<E, 256, 256, 2, 4>(A, st);
+    if (tiles(128) >= 192) return launch_tile<E, 128, 128, 2, 2>(A, st);
+    if (tiles(64) >= 128) return launch_tile<E, 64, 64, 2, 2>(A, st);
+    if (tiles(16) > 512) return launch_few<E, 2, 2>(A, st);
+    return launch_few<E, 1, 1>(A, st);
 }
 
 const char *check_tensors(const dqn_adamw_tensor *t, int32_t count, int32_t bits)
@@ -416,7 +423,7 @@ int32_t dqn_rows_product(const dqn_product_args *args, void *stream)
     if (!p.a_scale || !p.w_scale || !at(p.a_scale, 4) || !at(p.w_scale, 4) || !at(p.bias, 4)) return bad(call, "a scale is NULL or a pointer is not aligned to its elements");
     hipStream_t st = (hipStream_t)stream;
     const seq::ProductArgs A{p.a, p.w, p.a_rs, p.w_rs, p.a_scale, p.w_scale, p.bias, p.y, p.y_rs, p.M, p.N, p.K,
-                             p.y_rs % 4 == 0 && at(p.y, 4 * bytes_of(p.dtype))};
+                             p.dtype == DQN_BF16 && p.y_rs % 8 == 0 && at(p.y, 16) ? 8 : p.y_rs % 4 == 0 && at(p.y, 4 * bytes_of(p.dtype)) ? 4 : 1};
     const bool ok = p.dtype == DQN_F32 ? launch_product<float>(A, st) : launch_product<seq::bf16>(A, st);
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }

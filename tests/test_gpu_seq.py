@@ -277,7 +277,8 @@ def test_rows(seq, M, K, dtype):
 
 # ------------------------------------------------------------------ product
 PRODUCTS = [(1, 1, 1), (1, 16, 32), (2, 3, 7), (16, 16, 16), (17, 33, 100), (32, 1024, 512), (31, 100, 129), (1, 2048, 2048), (64, 64, 64), (100, 36, 513), (128, 128, 128),
-            (129, 257, 384), (200, 512, 1000), (256, 256, 2048), (300, 130, 4100), (3, 5, 8192), (1000, 18, 512), (513, 1100, 640)]
+            (129, 257, 384), (200, 512, 1000), (256, 256, 2048), (300, 130, 4100), (3, 5, 8192), (1000, 18, 512), (513, 1100, 640),
+            (1030, 1100, 640), (1024, 1024, 200), (1100, 1111, 16), (3333, 3700, 400), (4096, 3592, 256), (3600, 3601, 1025)]
 
 
 def small_rows(seed, n, K, pad=0x7F, high=3):
@@ -298,7 +299,10 @@ def test_product_of_whole_numbers(seq, M, N, K):
     one = lambda n: torch.ones(n, device="cuda")  # noqa: E731
     wide = torch.full((M, N + 3), 77.0, device="cuda")
     y = seq.product((a, one(M)), (w, one(N)), dtype=torch.float32, out=wide[:, 1:N + 1])
-    assert np.array_equal(host(y), (ha @ hw.T).astype(np.float64))
+    assert np.array_equal(host(y), ha.astype(np.float64) @ hw.T.astype(np.float64))
+    if N % 8 == 0:      # whole lines of y in bf16: whole numbers of up to 8 bits are exact in it too
+        y = seq.product((a, one(M)), (w, one(N)), dtype=torch.bfloat16)
+        assert torch.equal(y, torch.from_numpy(ha.astype(np.float64) @ hw.T.astype(np.float64)).to(torch.bfloat16).cuda())
     assert bool((wide[:, 0] == 77).all() and (wide[:, N + 1:] == 77).all())
 
 
