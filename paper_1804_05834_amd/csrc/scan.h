@@ -25,13 +25,10 @@ struct ScanArgs {
     float *h_last, *carry;
     long T;
     int B, C;
-    // Ranges: few sequences of few channels are cut over time, so that there are enough workgroups.  A first launch finds
-    // the map of every range but the last, a second one takes each range from the state that enters it on.
-    long range;      // steps of a range (a multiple of the tile)
-    int ranges;
-    float *totals;   // [B][ranges][2][C]: A (-1: an episode starts in the range) and H of each; the last A: a copy of h0,
-                     // which the last range may overwrite (h_last) before the first has read it
     long tiles;      // states per sequence in `carry`
+    long range;      // lines: steps of a range, ranges, and their maps (see there)
+    int ranges;
+    float *totals;
 };
 struct ScanGradArgs {
     const void *f, *x, *dh;
@@ -44,10 +41,10 @@ struct ScanGradArgs {
     float *dh0;
     long T;
     int B, C;
+    long tiles;
     long range;
     int ranges;
-    float *totals;   // A and P of every range but the first
-    long tiles;
+    float *totals;
 };
 
 constexpr int SCAN_RUN = 16;        // elements of a thread in a tile: 8 steps of 2 channels or 16 steps of one
@@ -199,14 +196,6 @@ template <int V> __device__ __forceinline__ void through(float (&s)[V], const fl
 #pragma unroll
     for (int k = 0; k < V; ++k) s[k] = through(s[k], a[k], h[k], cut);
 }
-// the same past a range of another workgroup
-template <int V> __device__ __forceinline__ void past_range(float (&s)[V], const float *p, int C)
-{
-    const auto a = load<V>(p), h = load<V>(p + C);
-#pragma unroll
-    for (int k = 0; k < V; ++k) s[k] = through(s[k], a[k], h[k], a[k] < 0.f);
-}
-
 // The runs of one wave: each lane's map in, the map of the whole wave out (in all lanes).  FORWARD: the lower half is
 // first, else the upper.  (fa, fh, fcut): the map of the half that is first, which what enters the wave goes through
 // on its way to the other half.  `cuts`: bit 0 the lower half, bit 1 the upper.
@@ -299,29 +288,23 @@ template <int V> __device__ __forceinline__ unsigned cuts_of(unsigned flags)
     return ((flags & run) != 0) | (flags >> Strip<V>::L != 0) << 1;
 }
 
-// TOTAL: nothing is written but the map of the range, for the launch that then takes the ranges from their states on.
-template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan(ScanArgs A)
+template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan(ScanArgs A)
 {
     constexpr int L = Strip<V>::L, G = Strip<V>::G, S = Strip<V>::S;
     __shared__ __attribute__((aligned(16))) float tot[2][2][SCAN_WAVES][SCAN_STRIP];
     __shared__ unsigned cuts[2][SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, g = lane % G, tile = W * S * L;
     const Lane<V> me(blockIdx.x * SCAN_STRIP + g * V, A.C);
-    const int z = blockIdx.z;
-    const long b = blockIdx.y, t0 = z * A.range, end = min(A.T, t0 + A.range), at = b * A.C + me.c;
-    float *totals = A.totals + b * A.ranges * 2 * A.C + me.c;   // (A, H) of range r at 2 r C and (2 r + 1) C
+    const long b = blockIdx.y, end = A.T, at = b * A.C + me.c;
     const E *f = (const E *)A.f + b * A.f_bs, *x = (const E *)A.x + b * A.x_bs;
     E *hs = (E *)A.h + b * A.h_bs;
     const uint8_t *reset = A.reset ? A.reset + b * A.r_bs : nullptr;
     const int wrow = wave * SCAN_RUN, half = lane / G * L;   // first step of the wave in a tile, of this thread's run in the wave
     auto place = [&](long ts) { return me.live ? (me.c + half * (int)ts) * (int)sizeof(E) : NOWHERE; };
     const int fplace = place(A.f_ts), xplace = place(A.x_ts), hplace = place(A.h_ts);
-    float *carry = A.carry ? A.carry + (b * A.tiles + t0 / tile) * A.C + me.c : nullptr;
+    float *carry = A.carry ? A.carry + b * A.tiles * A.C + me.c : nullptr;
 
-    float s[V] = {}, all[V];   // state entering the tile; TOTAL: the map so far is s -> all s + s
-    bool allcut = false;
-#pragma unroll
-    for (int k = 0; k < V; ++k) all[k] = 1.f;
+    float s[V] = {};   // state entering the tile
     Rows<E, V> fr, xr;
     Resets rs;
     auto fetch = [&](long t) {
@@ -329,15 +312,10 @@ template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAV
         xr.load_rows(Window<E>(x, A.x_ts, t + wrow, end, A.C), xplace, t + tile <= end);
         if (reset) rs.fetch(reset, A.r_ts, t + wrow, end);
     };
-    fetch(t0);
-    if constexpr (!TOTAL) {
-        if (A.ranges > 1) state<V>(totals + (long)(2 * A.ranges - 2) * A.C, s);
-        else if (A.h0) state<V>(A.h0 + at, s);
-#pragma unroll 8
-        for (int r = 0; r < z; ++r) past_range<V>(s, totals + 2l * r * A.C, A.C);
-    }
+    fetch(0);
+    if (A.h0) state<V>(A.h0 + at, s);
     int buf = 0;
-    for (long t = t0; t < end; t += tile, buf ^= 1) {
+    for (long t = 0; t < end; t += tile, buf ^= 1) {
         const unsigned flags = rs.flags(), r = flags >> half, mycuts = cuts_of<V>(flags);
         const bool edge = flags || t + tile > end;
         const int left = (int)min((long)L, end - t - wrow - half);   // steps of this thread that are in the range
@@ -377,94 +355,62 @@ template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAV
 #pragma unroll
                 for (int k = 0; k < V; ++k) in[k] = s[k];
             }
-            if constexpr (TOTAL) {
-                const auto m = load<V>(&tot[buf][0][w][g * V]);
-#pragma unroll
-                for (int k = 0; k < V; ++k) all[k] *= m[k];
-            }
             if (starts >> w & 1) through<V>(s, &tot[buf][0][w][g * V], &tot[buf][1][w][g * V], true);
             else through<V>(s, &tot[buf][0][w][g * V], &tot[buf][1][w][g * V], false);
         }
-        allcut |= starts != 0;
-        if constexpr (!TOTAL) {
-            if (carry) {
-                if (wave == 0 && lane < G && me.live) keep_state<V>(carry, in);
-                carry += A.C;
+        if (carry) {
+            if (wave == 0 && lane < G && me.live) keep_state<V>(carry, in);
+            carry += A.C;
+        }
+        up.enter(in);
+        const Window<E> hw(hs, A.h_ts, t + wrow, end, A.C);
+        auto steps = [&](auto e) {
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                const bool cut = e.value && r >> j & 1;
+#pragma unroll
+                for (int k = 0; k < V; ++k) in[k] = fmaf(ga[j][k], cut ? 0.f : in[k], gx[j][k]);
+                hw.template put<V, !e.value>(hplace, j, in);
             }
-            up.enter(in);
-            const Window<E> hw(hs, A.h_ts, t + wrow, end, A.C);
-            auto steps = [&](auto e) {
-#pragma unroll
-                for (int j = 0; j < L; ++j) {
-                    const bool cut = e.value && r >> j & 1;
-#pragma unroll
-                    for (int k = 0; k < V; ++k) in[k] = fmaf(ga[j][k], cut ? 0.f : in[k], gx[j][k]);
-                    hw.template put<V, !e.value>(hplace, j, in);
-                }
-            };
-            edge ? steps(Edge{}) : steps(Plain{});
-        }
+        };
+        edge ? steps(Edge{}) : steps(Plain{});
     }
-    if (wave || lane >= G || !me.live) return;
-    if constexpr (TOTAL) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) all[k] = allcut ? -1.f : all[k];
-        keep_state<V>(totals + 2l * z * A.C, all);
-        keep_state<V>(totals + (2l * z + 1) * A.C, s);
-        if (z == 0) {
-            float h0[V] = {};
-            if (A.h0) state<V>(A.h0 + at, h0);
-            keep_state<V>(totals + (long)(2 * A.ranges - 2) * A.C, h0);
-        }
-    } else if (A.h_last && end == A.T) {
-        keep_state<V>(A.h_last + at, s);
-    }
+    if (A.h_last && wave == 0 && lane < G && me.live) keep_state<V>(A.h_last + at, s);
 }
 
-template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_grad(ScanGradArgs A)
+template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_scan_grad(ScanGradArgs A)
 {
     constexpr int L = Strip<V>::L, G = Strip<V>::G, S = Strip<V>::S;
     __shared__ __attribute__((aligned(16))) float tot[2][3][SCAN_WAVES][SCAN_STRIP];   // A, P and H of the waves
     __shared__ unsigned cuts[2][SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, g = lane % G, tile = W * S * L;
     const Lane<V> me(blockIdx.x * SCAN_STRIP + g * V, A.C);
-    const int z = blockIdx.z + (TOTAL ? 1 : 0);
-    const long b = blockIdx.y, t0 = z * A.range, end = min(A.T, t0 + A.range), at = b * A.C + me.c;
-    float *totals = A.totals + b * A.ranges * 2 * A.C + me.c;
+    const long b = blockIdx.y, end = A.T, at = b * A.C + me.c;
     const E *f = (const E *)A.f + b * A.f_bs, *x = (const E *)A.x + b * A.x_bs, *dh = (const E *)A.dh + b * A.dh_bs;
     E *dfs = (E *)A.df + b * A.df_bs, *dxs = (E *)A.dx + b * A.dx_bs;
     const uint8_t *reset = A.reset ? A.reset + b * A.r_bs : nullptr;
     const int wrow = wave * SCAN_RUN, half = lane / G * L;
-    const long last = t0 + (end - t0 - 1) / tile * tile;
+    const long last = (A.tiles - 1) * tile;
     auto place = [&](long ts) { return me.live ? (me.c + half * (int)ts) * (int)sizeof(E) : NOWHERE; };
     const int fplace = place(A.f_ts), xplace = place(A.x_ts), gplace = place(A.dh_ts), dfplace = place(A.df_ts), dxplace = place(A.dx_ts);
-    const float *carry = A.carry + (b * A.tiles + last / tile) * A.C + me.c;
+    const float *carry = A.carry + ((b + 1) * A.tiles - 1) * A.C + me.c;
 
-    float mu[V] = {}, all[V];   // what comes from the right into the tile; TOTAL: the map so far is m -> all m + mu
-    bool allcut = false;
-#pragma unroll
-    for (int k = 0; k < V; ++k) all[k] = 1.f;
+    float mu[V] = {};   // what comes from the right into the tile
     Rows<E, V> fr, xr, gr;
     Resets rs;
     float first[V];   // state before the tile
     auto fetch = [&](long t) {
         fr.load_rows(Window<E>(f, A.f_ts, t + wrow, end, A.C), fplace, t + tile <= end);
-        if constexpr (!TOTAL) xr.load_rows(Window<E>(x, A.x_ts, t + wrow, end, A.C), xplace, t + tile <= end);
+        xr.load_rows(Window<E>(x, A.x_ts, t + wrow, end, A.C), xplace, t + tile <= end);
         gr.load_rows(Window<E>(dh, A.dh_ts, t + wrow, end, A.C), gplace, t + tile <= end);
-        if constexpr (!TOTAL) {
-            state<V>(carry, first);
-            carry -= A.C;
-        }
+        state<V>(carry, first);
+        carry -= A.C;
         if (reset) rs.fetch(reset, A.r_ts, t + wrow, end);
     };
     fetch(last);
-    if constexpr (!TOTAL) {
-        if (A.dlast) state<V>(A.dlast + at, mu);
-#pragma unroll 8
-        for (int r = A.ranges - 1; r > z; --r) past_range<V>(mu, totals + 2l * r * A.C, A.C);
-    }
+    if (A.dlast) state<V>(A.dlast + at, mu);
     int buf = 0;
-    for (long t = last; t >= t0; t -= tile, buf ^= 1) {
+    for (long t = last; t >= 0; t -= tile, buf ^= 1) {
         const unsigned flags = rs.flags(), r = flags >> half, mycuts = cuts_of<V>(flags);
         const bool edge = flags || t + tile > end;
         const int left = (int)min((long)L, end - t - wrow - half);
@@ -481,10 +427,8 @@ template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAV
                     gates((float)fr.v[j][k], ga[j][k], gi[j][k]);
                     gv[j][k] = (float)gr.v[j][k];
                     if (!in) { ga[j][k] = 1.f; gi[j][k] = gv[j][k] = 0.f; }
-                    if constexpr (!TOTAL) {
-                        xv[j][k] = in ? xr.v[j][k] : (E)0.f;
-                        h[k] = fmaf(ga[j][k], cut ? 0.f : h[k], gi[j][k] * (float)xv[j][k]);
-                    }
+                    xv[j][k] = in ? xr.v[j][k] : (E)0.f;
+                    h[k] = fmaf(ga[j][k], cut ? 0.f : h[k], gi[j][k] * (float)xv[j][k]);
                     a[k] = cut ? 0.f : a[k] * ga[j][k];
                 }
             }
@@ -494,22 +438,20 @@ template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAV
                 for (int k = 0; k < V; ++k) p[k] = e.value && r >> j & 1 ? 0.f : ga[j][k] * (gv[j][k] + p[k]);
         };
         edge ? maps(Edge{}) : maps(Plain{});
-        if constexpr (!TOTAL) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) s[k] = first[k];
-        }
-        if (t > t0) fetch(t - tile);
+        for (int k = 0; k < V; ++k) s[k] = first[k];
+        if (t > 0) fetch(t - tile);
         Across<V, true> up;
         Across<V, false> down;
         float aa[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) aa[k] = a[k];
-        if constexpr (!TOTAL) up.join(aa, h, mycuts);
+        up.join(aa, h, mycuts);
         down.join(a, p, mycuts);
         if (lane < G) {
             keep_state<V>(&tot[buf][0][wave][g * V], a);
             keep_state<V>(&tot[buf][1][wave][g * V], p);
-            if constexpr (!TOTAL) keep_state<V>(&tot[buf][2][wave][g * V], h);
+            keep_state<V>(&tot[buf][2][wave][g * V], h);
             if (lane == 0) cuts[buf][wave] = mycuts;
         }
         lds_barrier();
@@ -520,58 +462,401 @@ template <class E, int V, bool TOTAL> __global__ __launch_bounds__(64 * SCAN_WAV
 #pragma unroll
                 for (int k = 0; k < V; ++k) in[k] = mu[k];
             }
-            if constexpr (TOTAL) {
-                const auto m = load<V>(&tot[buf][0][w][g * V]);
-#pragma unroll
-                for (int k = 0; k < V; ++k) all[k] *= m[k];
-            }
             if (starts >> w & 1) through<V>(mu, &tot[buf][0][w][g * V], &tot[buf][1][w][g * V], true);
             else through<V>(mu, &tot[buf][0][w][g * V], &tot[buf][1][w][g * V], false);
         }
-        allcut |= starts != 0;
-        if constexpr (!TOTAL) {
-            for (int w = 0; w < wave; ++w) {
-                if (starts >> w & 1) through<V>(s, &tot[buf][0][w][g * V], &tot[buf][2][w][g * V], true);
-                else through<V>(s, &tot[buf][0][w][g * V], &tot[buf][2][w][g * V], false);
-            }
-            up.enter(s);
-            down.enter(in);
-            const Window<E> dfw(dfs, A.df_ts, t + wrow, end, A.C), dxw(dxs, A.dx_ts, t + wrow, end, A.C);
-            auto steps = [&](auto e) {
-                float before[L][V];
+        for (int w = 0; w < wave; ++w) {
+            if (starts >> w & 1) through<V>(s, &tot[buf][0][w][g * V], &tot[buf][2][w][g * V], true);
+            else through<V>(s, &tot[buf][0][w][g * V], &tot[buf][2][w][g * V], false);
+        }
+        up.enter(s);
+        down.enter(in);
+        const Window<E> dfw(dfs, A.df_ts, t + wrow, end, A.C), dxw(dxs, A.dx_ts, t + wrow, end, A.C);
+        auto steps = [&](auto e) {
+            float before[L][V];
 #pragma unroll
-                for (int j = 0; j < L; ++j)
+            for (int j = 0; j < L; ++j)
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        before[j][k] = e.value && r >> j & 1 ? 0.f : s[k];
-                        s[k] = fmaf(ga[j][k], before[j][k], gi[j][k] * (float)xv[j][k]);
-                    }
-#pragma unroll
-                for (int j = L - 1; j >= 0; --j) {
-                    float df[V], dx[V];
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const float l = gv[j][k] + in[k], m = ga[j][k] * l;
-                        dx[k] = gi[j][k] * l;
-                        df[k] = gi[j][k] * m * (before[j][k] - (float)xv[j][k]);
-                        in[k] = e.value && r >> j & 1 ? 0.f : m;
-                    }
-                    dfw.template put<V, !e.value>(dfplace, j, df);
-                    dxw.template put<V, !e.value>(dxplace, j, dx);
+                for (int k = 0; k < V; ++k) {
+                    before[j][k] = e.value && r >> j & 1 ? 0.f : s[k];
+                    s[k] = fmaf(ga[j][k], before[j][k], gi[j][k] * (float)xv[j][k]);
                 }
-            };
-            edge ? steps(Edge{}) : steps(Plain{});
+#pragma unroll
+            for (int j = L - 1; j >= 0; --j) {
+                float df[V], dx[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float l = gv[j][k] + in[k], m = ga[j][k] * l;
+                    dx[k] = gi[j][k] * l;
+                    df[k] = gi[j][k] * m * (before[j][k] - (float)xv[j][k]);
+                    in[k] = e.value && r >> j & 1 ? 0.f : m;
+                }
+                dfw.template put<V, !e.value>(dfplace, j, df);
+                dxw.template put<V, !e.value>(dxplace, j, dx);
+            }
+        };
+        edge ? steps(Edge{}) : steps(Plain{});
+    }
+    if (A.dh0 && wave == 0 && lane < G && me.live) keep_state<V>(A.dh0 + at, mu);
+}
+
+// ------------------------------------------------------------ lines
+// A wave goes through a range of steps of 64 V channels, step after step, LINE steps' loads ahead: no work but the
+// recurrence itself (fourteen vector instructions per element, where a strip takes twenty).  With enough sequences
+// and channels a wave takes a whole sequence.  Else time is cut into ranges, and the state that enters one is not known yet:
+// a first launch finds the map of every range, a second composes the maps of those before and then runs.  f and x
+// are read twice then, which long sequences of few channels have to: the other way would be to wait for the
+// workgroup before, a thousand times in turn.
+//
+// Eight waves, eight ranges of a sequence in turn, are a workgroup and a group: maps are kept of ranges and of groups, and
+// a workgroup composes the groups before it with all of its waves.
+constexpr int LINE = 8;         // steps between two states of `carry`, and of a wave's loads
+constexpr int LINE_WAVES = 8;   // waves of a workgroup
+
+// Maps in memory: [B][ranges + groups][2][C], A (-1: an episode starts there) and H of each range, then of each group.  A map
+// is made and composed in registers as (a, h).  The last range's map (forward; backward the first's) is not needed.
+// Forward, range 0 runs from h0 on and counts as the start of an episode, and a copy of h0 stands in place of the last
+// range's A: the last range may write h_last where h0 was before the first has read it.
+template <int V> struct Map {
+    float a[V], h[V];
+    bool cut = false;
+    __device__ __forceinline__ Map()
+    {
+#pragma unroll
+        for (int k = 0; k < V; ++k) { a[k] = 1.f; h[k] = 0.f; }
+    }
+    __device__ __forceinline__ void put(float *p, int C) const
+    {
+        float m[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) m[k] = cut ? -1.f : a[k];
+        keep_state<V>(p, m);
+        keep_state<V>(p + C, h);
+    }
+    // this map, then the one at p
+    __device__ __forceinline__ void then(const float *p, int C)
+    {
+        const auto pa = load<V>(p), ph = load<V>(p + C);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            h[k] = through(h[k], pa[k], ph[k], pa[k] < 0.f);
+            a[k] = pa[k] < 0.f || a[k] < 0.f ? -1.f : a[k] * pa[k];
         }
     }
-    if (wave || lane >= G || !me.live) return;
-    if constexpr (TOTAL) {
+    __device__ __forceinline__ void apply(float (&s)[V]) const
+    {
 #pragma unroll
-        for (int k = 0; k < V; ++k) all[k] = allcut ? -1.f : all[k];
-        keep_state<V>(totals + 2l * z * A.C, all);
-        keep_state<V>(totals + (2l * z + 1) * A.C, mu);
-    } else if (A.dh0 && z == 0) {
-        keep_state<V>(A.dh0 + at, mu);
+        for (int k = 0; k < V; ++k) s[k] = through(s[k], a[k], h[k], a[k] < 0.f);
     }
+};
+
+// Where a wave stands.
+template <int V> struct Line {
+    int strip, c, z, group, groups;
+    long b;
+    bool live, idle;   // idle: nothing to do, but the workgroup's barriers
+    __device__ __forceinline__ Line(int B, int C, int ranges)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strips = (C + 64 * V - 1) / (64 * V);
+        groups = (ranges + LINE_WAVES - 1) / LINE_WAVES;
+        if (ranges == 1) {   // a wave per strip
+            const long id = (long)blockIdx.x * LINE_WAVES + wave;
+            b = id / strips;
+            strip = (int)(id - b * strips);
+            z = group = 0;
+            idle = b >= B;
+        } else {             // a workgroup per strip and group
+            const unsigned id = blockIdx.x / strips;
+            strip = blockIdx.x - id * strips;
+            b = id / groups;
+            group = id - (unsigned)b * groups;
+            z = group * LINE_WAVES + wave;
+            idle = z >= ranges;
+        }
+        const int first = (strip * 64 + (threadIdx.x & 63)) * V;
+        live = first < C;
+        c = min(first, C - V);
+    }
+};
+
+// Rows t .. t + LINE - 1 of a tensor, and their reset flags
+template <class E, int V> struct LineRows {
+    vec<E, V> v[LINE];
+    __device__ __forceinline__ void fetch(const E *p, long ts, long t, long end, int C, int place)
+    {
+        const Window<E> w(p, ts, t, end, C);
+        if (t + LINE <= end) {
+#pragma unroll
+            for (int j = 0; j < LINE; ++j) v[j] = w.template get<V, true>(place, j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < LINE; ++j) v[j] = w.template get<V, false>(place, j);
+        }
+    }
+};
+
+// The state that enters a wave's range: every wave composes a share of the groups on the way to it (`before` of them, from
+// `from` on in steps of `way`), then the ranges of the waves before it in the workgroup.
+template <int V, bool FORWARD> __device__ __forceinline__ void enter_range(float (&s)[V], const Line<V> &me, const float *maps, int ranges, int C)
+{
+    __shared__ float sh[2 * LINE_WAVES][2][64 * V];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int before = FORWARD ? me.group : me.groups - 1 - me.group, order = FORWARD ? wave : LINE_WAVES - 1 - wave;
+    const int lo = before * order / LINE_WAVES, hi = before * (order + 1) / LINE_WAVES;
+    Map<V> m;
+#pragma unroll 8
+    for (int q = lo; q < hi; ++q) m.then(maps + (long)(ranges + (FORWARD ? q : me.groups - 1 - q)) * 2 * C, C);
+    Map<V> own;
+    const bool have = !me.idle && me.z != (FORWARD ? ranges - 1 : 0);
+    if (have) own.then(maps + (long)me.z * 2 * C, C);
+    keep_state<V>(&sh[order][0][lane * V], m.a);
+    keep_state<V>(&sh[order][1][lane * V], m.h);
+    keep_state<V>(&sh[LINE_WAVES + order][0][lane * V], own.a);
+    keep_state<V>(&sh[LINE_WAVES + order][1][lane * V], own.h);
+    __syncthreads();
+    for (int q = 0; q < LINE_WAVES + order; ++q) {
+        Map<V> step;
+        state<V>(&sh[q][0][lane * V], step.a);
+        state<V>(&sh[q][1][lane * V], step.h);
+        step.apply(s);
+    }
+}
+
+// the maps of a workgroup's ranges: each to its place, and all composed to the group's
+template <int V, bool FORWARD> __device__ __forceinline__ void leave_maps(const Map<V> &m, const Line<V> &me, float *maps, int ranges, int C)
+{
+    __shared__ float sh[LINE_WAVES][2][64 * V];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    m.put(&sh[FORWARD ? wave : LINE_WAVES - 1 - wave][0][lane * V], 64 * V);
+    if (!me.idle && me.live && me.z != (FORWARD ? ranges - 1 : 0)) m.put(maps + (long)me.z * 2 * C, C);
+    __syncthreads();
+    if (wave || !me.live) return;
+    Map<V> all;
+    for (int q = 0; q < LINE_WAVES; ++q) all.then(&sh[q][0][lane * V], 64 * V);
+    float *p = maps + (long)(ranges + me.group) * 2 * C;
+    keep_state<V>(p, all.a);
+    keep_state<V>(p + C, all.h);
+}
+
+template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_maps(ScanArgs A)
+{
+    const Line<V> me(A.B, A.C, A.ranges);
+    const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs;
+    const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
+    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    Map<V> m;
+    if (!me.idle && me.z < A.ranges - 1) {
+        LineRows<E, V> fr, xr;
+        Resets rs;
+        auto fetch = [&](long t) {
+            fr.fetch(f, A.f_ts, t, end, A.C, place);
+            xr.fetch(x, A.x_ts, t, end, A.C, place);
+            if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+        };
+        fetch(t0);
+        if (me.z == 0) {
+            m.cut = true;
+            if (A.h0) state<V>(A.h0 + me.b * A.C + me.c, m.h);
+        }
+        for (long t = t0; t < end; t += LINE) {   // a range that is not the last is whole: a multiple of LINE steps
+            const unsigned flags = rs.flags();
+            const LineRows<E, V> fv = fr, xv = xr;
+            if (t + LINE < end) fetch(t + LINE);
+            auto steps = [&](auto e) {
+#pragma unroll
+                for (int j = 0; j < LINE; ++j) {
+                    const bool cut = e.value && flags >> j & 1;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        float a, i;
+                        gates((float)fv.v[j][k], a, i);
+                        m.h[k] = fmaf(a, cut ? 0.f : m.h[k], i * (float)xv.v[j][k]);
+                        m.a[k] *= a;
+                    }
+                }
+            };
+            flags ? steps(Edge{}) : steps(Plain{});
+            m.cut |= flags != 0;
+        }
+    }
+    leave_maps<V, true>(m, me, maps, A.ranges, A.C);
+    if (me.z == A.ranges - 1 && me.live) {
+        float s[V] = {};
+        if (A.h0) state<V>(A.h0 + me.b * A.C + me.c, s);
+        keep_state<V>(maps + (long)(A.ranges - 1) * 2 * A.C, s);
+    }
+}
+
+template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_lines(ScanArgs A)
+{
+    const Line<V> me(A.B, A.C, A.ranges);
+    if (A.ranges == 1 && me.idle) return;
+    const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs;
+    E *h = (E *)A.h + me.b * A.h_bs;
+    const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
+    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    const long at = me.b * A.C + me.c, t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    LineRows<E, V> fr, xr;
+    Resets rs;
+    auto fetch = [&](long t) {
+        fr.fetch(f, A.f_ts, t, end, A.C, place);
+        xr.fetch(x, A.x_ts, t, end, A.C, place);
+        if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+    };
+    if (!me.idle) fetch(t0);
+    float s[V] = {};
+    if (A.ranges > 1) {
+        const float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
+        state<V>(maps + (long)(A.ranges - 1) * 2 * A.C, s);
+        enter_range<V, true>(s, me, maps, A.ranges, A.C);
+        if (me.idle) return;
+    } else if (A.h0) {
+        state<V>(A.h0 + at, s);
+    }
+    float *carry = A.carry ? A.carry + (me.b * A.tiles + t0 / LINE) * A.C + me.c : nullptr;
+    for (long t = t0; t < end; t += LINE) {
+        const unsigned flags = rs.flags();
+        const int left = (int)min((long)LINE, end - t);
+        const LineRows<E, V> fv = fr, xv = xr;
+        if (t + LINE < end) fetch(t + LINE);
+        if (carry) {
+            if (me.live) keep_state<V>(carry, s);
+            carry += A.C;
+        }
+        const Window<E> hw(h, A.h_ts, t, end, A.C);
+        auto steps = [&](auto e) {
+#pragma unroll
+            for (int j = 0; j < LINE; ++j) {
+                if (e.value && j >= left) break;
+                const bool cut = e.value && flags >> j & 1;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    float a, i;
+                    gates((float)fv.v[j][k], a, i);
+                    s[k] = fmaf(a, cut ? 0.f : s[k], i * (float)xv.v[j][k]);
+                }
+                hw.template put<V, !e.value>(place, j, s);
+            }
+        };
+        flags || left < LINE ? steps(Edge{}) : steps(Plain{});
+    }
+    if (A.h_last && end == A.T && me.live) keep_state<V>(A.h_last + at, s);
+}
+
+template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_grad_maps(ScanGradArgs A)
+{
+    const Line<V> me(A.B, A.C, A.ranges);
+    const E *f = (const E *)A.f + me.b * A.f_bs, *dh = (const E *)A.dh + me.b * A.dh_bs;
+    const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
+    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    Map<V> m;
+    if (!me.idle && me.z > 0) {
+        LineRows<E, V> fr, gr;
+        Resets rs;
+        auto fetch = [&](long t) {
+            fr.fetch(f, A.f_ts, t, end, A.C, place);
+            gr.fetch(dh, A.dh_ts, t, end, A.C, place);
+            if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+        };
+        const long last = t0 + (end - t0 - 1) / LINE * LINE;
+        fetch(last);
+        for (long t = last; t >= t0; t -= LINE) {
+            const unsigned flags = rs.flags();
+            const int left = (int)min((long)LINE, end - t);
+            const LineRows<E, V> fv = fr, gv = gr;
+            if (t > t0) fetch(t - LINE);
+            auto steps = [&](auto e) {
+#pragma unroll
+                for (int j = LINE - 1; j >= 0; --j) {
+                    if (e.value && j >= left) continue;
+                    const bool cut = e.value && flags >> j & 1;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        float a, i;
+                        gates((float)fv.v[j][k], a, i);
+                        m.h[k] = cut ? 0.f : a * ((float)gv.v[j][k] + m.h[k]);
+                        m.a[k] *= a;
+                    }
+                }
+            };
+            flags || left < LINE ? steps(Edge{}) : steps(Plain{});
+            m.cut |= flags != 0;
+        }
+    }
+    leave_maps<V, false>(m, me, maps, A.ranges, A.C);
+}
+
+template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_grad(ScanGradArgs A)
+{
+    const Line<V> me(A.B, A.C, A.ranges);
+    if (A.ranges == 1 && me.idle) return;
+    const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs, *dh = (const E *)A.dh + me.b * A.dh_bs;
+    E *df = (E *)A.df + me.b * A.df_bs, *dx = (E *)A.dx + me.b * A.dx_bs;
+    const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
+    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    const long at = me.b * A.C + me.c, t0 = me.z * A.range, end = min(A.T, t0 + A.range), last = t0 + (end - t0 - 1) / LINE * LINE;
+    const float *carry = A.carry + (me.b * A.tiles + last / LINE) * A.C + me.c;
+    LineRows<E, V> fr, xr, gr;
+    Resets rs;
+    float first[V];
+    auto fetch = [&](long t) {
+        fr.fetch(f, A.f_ts, t, end, A.C, place);
+        xr.fetch(x, A.x_ts, t, end, A.C, place);
+        gr.fetch(dh, A.dh_ts, t, end, A.C, place);
+        if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+        state<V>(carry, first);
+        carry -= A.C;
+    };
+    if (!me.idle) fetch(last);
+    float mu[V] = {};
+    if (A.dlast) state<V>(A.dlast + at, mu);
+    if (A.ranges > 1) {
+        enter_range<V, false>(mu, me, A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c, A.ranges, A.C);
+        if (me.idle) return;
+    }
+    for (long t = last; t >= t0; t -= LINE) {
+        const unsigned flags = rs.flags();
+        const int left = (int)min((long)LINE, end - t);
+        const LineRows<E, V> fv = fr, xv = xr, gv = gr;
+        float s[V], before[LINE][V], ga[LINE][V], gi[LINE][V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[k] = first[k];
+        if (t > t0) fetch(t - LINE);
+        const Window<E> dfw(df, A.df_ts, t, end, A.C), dxw(dx, A.dx_ts, t, end, A.C);
+        auto steps = [&](auto e) {
+#pragma unroll
+            for (int j = 0; j < LINE; ++j) {
+                const bool cut = e.value && flags >> j & 1;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    gates((float)fv.v[j][k], ga[j][k], gi[j][k]);
+                    before[j][k] = cut ? 0.f : s[k];
+                    s[k] = fmaf(ga[j][k], before[j][k], gi[j][k] * (float)xv.v[j][k]);
+                }
+            }
+#pragma unroll
+            for (int j = LINE - 1; j >= 0; --j) {
+                if (e.value && j >= left) continue;
+                const bool cut = e.value && flags >> j & 1;
+                float odf[V], odx[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float l = (float)gv.v[j][k] + mu[k], n = ga[j][k] * l;
+                    odx[k] = gi[j][k] * l;
+                    odf[k] = gi[j][k] * n * (before[j][k] - (float)xv.v[j][k]);
+                    mu[k] = cut ? 0.f : n;
+                }
+                dfw.template put<V, !e.value>(place, j, odf);
+                dxw.template put<V, !e.value>(place, j, odx);
+            }
+        };
+        flags || left < LINE ? steps(Edge{}) : steps(Plain{});
+    }
+    if (A.dh0 && me.z == 0 && me.live) keep_state<V>(A.dh0 + at, mu);
 }
 
 }  // namespace seq

@@ -34,6 +34,7 @@ int32_t launched(const char *call)
 bool dtype_ok(int32_t d) { return d == DQN_F32 || d == DQN_BF16; }
 size_t bytes_of(int32_t d) { return d == DQN_F32 ? 4 : 2; }
 bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
+constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
 constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
 
 bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && (!a || !b || a * b <= MOST) && (!a || !b || !c || a * b <= MOST / c); }
@@ -64,30 +65,32 @@ const char *check_scan(const dqn_scan_args &s)
 
 // How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
 struct ScanCut {
-    int waves, ranges;   // waves of a workgroup; ranges over time
-    long tile, tiles;    // steps of a tile, tiles of a sequence
-    long range;          // steps of a range
+    enum { SHORT, STRIPS, LINES } form;
+    int waves;         // of a workgroup of the strips
+    long tile, tiles;  // steps between two states of `carry`, states of a sequence
+    long range;        // lines: steps of a range
+    int ranges;
 };
 ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 {
-    ScanCut c{};
-    if (T <= seq::SCAN_SHORT) {
-        c = ScanCut{0, 1, seq::SCAN_SHORT, T ? 1 : 0, (long)T};
-        return c;
+    if (T <= seq::SCAN_SHORT) return ScanCut{ScanCut::SHORT, 0, seq::SCAN_SHORT, T ? 1 : 0, (long)T, 1};
+    const int64_t strips = (int64_t)B * ((C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), lines = (int64_t)B * ((C + 127) / 128);
+    if (lines < SCAN_LINES && strips >= SCAN_STRIPS) {
+        int waves = 1;
+        while (waves < seq::SCAN_WAVES && 16 * waves < T) waves *= 2;
+        const long tile = 16 * waves;
+        return ScanCut{ScanCut::STRIPS, waves, tile, (long)((T + tile - 1) / tile), (long)T, 1};
     }
-    c.waves = 1;
-    while (c.waves < seq::SCAN_WAVES && 16 * c.waves < T) c.waves *= 2;
-    c.tile = 16 * c.waves;
-    c.tiles = (T + c.tile - 1) / c.tile;
-    const int64_t strips = (int64_t)B * ((C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP);
-    // enough workgroups for two per compute unit, but ranges of four tiles at least
-    const int64_t want = std::min<int64_t>(std::min<int64_t>(256, strips ? (512 + strips - 1) / strips : 1), std::max<int64_t>(1, c.tiles / 4));
-    const long per = (c.tiles + want - 1) / want;
-    c.range = per * c.tile;
-    c.ranges = (int)((c.tiles + per - 1) / per);
-    return c;
+    const int64_t want = lines >= SCAN_LINES || !lines ? 1 : std::min<int64_t>((SCAN_WANT + lines - 1) / lines, (T + SCAN_LEAST - 1) / SCAN_LEAST);
+    const long per = (T + want - 1) / want, range = (per + seq::LINE - 1) / seq::LINE * seq::LINE;
+    return ScanCut{ScanCut::LINES, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), range, (int)((T + range - 1) / range)};
 }
-size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C) { return c.ranges > 1 ? ((size_t)B * c.ranges * 2 * C * 4 + 15) / 16 * 16 : 0; }
+size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C)
+{
+    if (c.ranges == 1) return 0;
+    const size_t maps = c.ranges + (c.ranges + seq::LINE_WAVES - 1) / seq::LINE_WAVES;
+    return ((size_t)B * maps * 2 * C * 4 + 15) / 16 * 16;
+}
 
 // whether `n` elements of every tensor can be taken at once
 bool together(int n, int32_t dtype, int32_t C, std::initializer_list<const void *> tensors, std::initializer_list<int64_t> strides, std::initializer_list<const void *> states)
@@ -110,23 +113,38 @@ template <class E, int V> void launch_short(const seq::ScanGradArgs &A, hipStrea
 {
     seq::k_scan_grad_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
 }
-template <class E, int V> void launch_scan(const seq::ScanArgs &A, const ScanCut &c, hipStream_t st)
+// a workgroup per strip and group of ranges, or eight lines
+template <int V> dim3 line_grid(int32_t B, int32_t C, int ranges)
 {
-    const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
-    if (c.ranges > 1) seq::k_scan<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
-    seq::k_scan<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
+    const int64_t strips = (C + 64 * V - 1) / (64 * V);
+    return dim3((unsigned)(ranges == 1 ? ((int64_t)B * strips + seq::LINE_WAVES - 1) / seq::LINE_WAVES : strips * B * ((ranges + seq::LINE_WAVES - 1) / seq::LINE_WAVES)));
 }
-template <class E, int V> void launch_scan(const seq::ScanGradArgs &A, const ScanCut &c, hipStream_t st)
+template <class E, int V> void launch_lines(const seq::ScanArgs &A, hipStream_t st)
 {
-    const unsigned strips = (unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), B = (unsigned)A.B;
-    if (c.ranges > 1) seq::k_scan_grad<E, V, true><<<dim3(strips, B, (unsigned)c.ranges - 1), 64 * c.waves, 0, st>>>(A);
-    seq::k_scan_grad<E, V, false><<<dim3(strips, B, (unsigned)c.ranges), 64 * c.waves, 0, st>>>(A);
+    const dim3 grid = line_grid<V>(A.B, A.C, A.ranges);
+    if (A.ranges > 1) seq::k_line_maps<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    seq::k_lines<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+}
+template <class E, int V> void launch_lines(const seq::ScanGradArgs &A, hipStream_t st)
+{
+    const dim3 grid = line_grid<V>(A.B, A.C, A.ranges);
+    if (A.ranges > 1) seq::k_line_grad_maps<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    seq::k_line_grad<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+}
+template <class E, int V> void launch_strips(const seq::ScanArgs &A, int waves, hipStream_t st)
+{
+    seq::k_scan<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
+}
+template <class E, int V> void launch_strips(const seq::ScanGradArgs &A, int waves, hipStream_t st)
+{
+    seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
 }
 // fits(n): whether n channels can be taken at once
 template <class E, class Args, class F> void launch_recurrence(const Args &A, const ScanCut &c, F &&fits, hipStream_t st)
 {
-    if (c.waves) fits(2) ? launch_scan<E, 2>(A, c, st) : launch_scan<E, 1>(A, c, st);
-    else fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
+    if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
+    else if (c.form == ScanCut::STRIPS) fits(2) ? launch_strips<E, 2>(A, c.waves, st) : launch_strips<E, 1>(A, c.waves, st);
+    else fits(2) ? launch_lines<E, 2>(A, st) : launch_lines<E, 1>(A, st);
 }
 
 const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
@@ -298,7 +316,7 @@ int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream)
     const ScanCut cut = scan_cut(s.B, s.T, s.C);
     if (scan_workspace(cut, s.B, s.C) && (!s.workspace || !at(s.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last,
-                          s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.range, cut.ranges, (float *)s.workspace, cut.tiles};
+                          s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.tiles, cut.range, cut.ranges, (float *)s.workspace};
     auto fits = [&](int n) { return together(n, s.dtype, s.C, {s.f, s.x, s.h}, {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts}, {s.h0, s.h_last, s.carry}); };
     s.dtype == DQN_F32 ? launch_recurrence<float>(A, cut, fits, st) : launch_recurrence<seq::bf16>(A, cut, fits, st);
     return launched(call);
@@ -325,7 +343,7 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream)
     const ScanCut cut = scan_cut(s.B, s.T, s.C);
     if (scan_workspace(cut, s.B, s.C) && (!g.workspace || !at(g.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanGradArgs A{g.f, g.x, g.dh, g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.carry, g.dlast, g.reset, g.reset_bs, g.reset_ts,
-                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.range, cut.ranges, (float *)g.workspace, cut.tiles};
+                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.tiles, cut.range, cut.ranges, (float *)g.workspace};
     auto fits = [&](int n) {
         return together(n, g.dtype, g.C, {g.f, g.x, g.dh, g.df, g.dx}, {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts},
                         {g.carry, g.dlast, g.dh0});

@@ -43,6 +43,9 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     (1, 257, 261, "plain", True, 0.01), (3, 300, 64, "broadcast", True, 0.01), (1, 1000, 512, "half", True, 0.003), (2, 777, 33, "odd", True, 0.0),
     (1, 5000, 64, "plain", True, 0.001), (1, 4097, 5, "plain", True, 0.0), (2, 2048, 72, "half", False, 1.0), (300, 3, 64, "half", True, 0.2),
     (70, 33, 192, "time", True, 0.05),
+    # many sequences: strips of channels in one workgroup, and whole sequences per wave
+    (300, 20, 64, "half", True, 0.05), (260, 150, 60, "plain", True, 0.02), (90, 300, 130, "odd", True, 0.01), (256, 129, 64, "time", False, 0.0), (64, 1030, 256, "half", True, 0.002),
+    (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
 
@@ -102,20 +105,20 @@ def test_scan_state_in_place_and_outputs_apart(seq):
         assert bool((wide[..., :4] == 5).all() and (wide[..., C + 4:] == 5).all())
 
 
-@pytest.mark.parametrize("T", [1, 5, 40, 600, 9000])
-def test_scan_a_reset_forgets_anything(seq, T):
+@pytest.mark.parametrize("B,T", [(2, 1), (2, 5), (2, 40), (2, 600), (2, 9000), (300, 20), (300, 300), (2100, 30)])
+def test_scan_a_reset_forgets_anything(seq, B, T):
     """A state that is NaN or infinite does not reach past an episode's start, forward or backward."""
-    B, C = 2, 64
+    C = 64
     f, x = rnd(1, B, T, C, at=1.0), rnd(2, B, T, C)
     cut = T // 2
     reset = torch.zeros(B, T, dtype=torch.uint8, device="cuda")
     reset[:, cut] = 1
     clean, cl, cc = seq.scan(f, x, reset=reset, save=True)
     h0 = torch.full((B, C), NAN, device="cuda")
-    h0[1] = INF
+    h0[1::2] = INF
     h, last, carry = seq.scan(f, x, h0=h0, reset=reset, save=True)
     assert torch.equal(h[:, cut:], clean[:, cut:]) and torch.equal(last, cl)
-    assert bool(torch.isnan(h[0, :cut]).all()) and not bool(torch.isfinite(h[1, :cut]).any())
+    assert bool(torch.isnan(h[::2, :cut]).all()) and not bool(torch.isfinite(h[1::2, :cut]).any())
     dh = rnd(3, B, T, C)
     ref_df, ref_dx, _ = seq.scan_backward(dh, f, x, cc, reset=reset)
     df, dx, dh0 = seq.scan_backward(dh, f, x, carry, reset=reset)
