@@ -34,7 +34,13 @@ int32_t launched(const char *call)
 bool dtype_ok(int32_t d) { return d == DQN_F32 || d == DQN_BF16; }
 size_t bytes_of(int32_t d) { return d == DQN_F32 ? 4 : 2; }
 bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
+// Which form a recurrence takes, by how many lines (sequences times strips of 128 channels) and strips (of 64) there are; us
+// forward / backward in bf16, C = 512, B x T:
+//   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
+//   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
+// below that ranges: as many waves as the card holds at four per SIMD, each with 32 steps at least.
 constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
+constexpr int64_t LAST_LEVEL = 256 << 20;   // bytes of the cache in front of memory
 constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
 
 bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && (!a || !b || a * b <= MOST) && (!a || !b || !c || a * b <= MOST / c); }
@@ -123,7 +129,8 @@ template <class E, int V> void launch_lines(const seq::ScanArgs &A, hipStream_t 
 {
     const dim3 grid = line_grid<V>(A.B, A.C, A.ranges);
     if (A.ranges > 1) seq::k_line_maps<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
-    seq::k_lines<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    if (V > 1 && 2 * (int64_t)sizeof(E) * A.B * A.T * A.C >= LAST_LEVEL) seq::k_lines<E, V, seq::STREAM><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    else seq::k_lines<E, V, 0><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
 }
 template <class E, int V> void launch_lines(const seq::ScanGradArgs &A, hipStream_t st)
 {
