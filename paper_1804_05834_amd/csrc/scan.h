@@ -865,4 +865,172 @@ template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_l
     if (A.dh0 && me.z == 0 && me.live) keep_state<V>(A.dh0 + at, mu);
 }
 
+// ------------------------------------------------------------ narrow sequences
+// Few channels: a wave of a strip or a line would have few lanes at work.  Here a thread takes one channel through a range of
+// steps, neighbouring threads the channels and then the ranges, and time is cut as far as it takes to have enough
+// threads.  Maps of ranges first, then one wave per channel of a sequence joins them into the states that enter the ranges
+// (in place of the maps' H), then the ranges.  `totals` is [2][B][ranges][C]: A (-1: an episode starts there), H.
+struct Thread {
+    long b;
+    int z, c;
+    bool none;
+    __device__ __forceinline__ Thread(int B, int ranges, int C)
+    {
+        const long id = (long)blockIdx.x * 256 + threadIdx.x;
+        const long q = id / C;
+        c = (int)(id - q * C);
+        b = q / ranges;
+        z = (int)(q - b * ranges);
+        none = b >= B;
+    }
+};
+template <class Args> __device__ __forceinline__ bool starts(const Args &A, long b, long t) { return A.reset && A.reset[b * A.r_bs + t * A.r_ts]; }
+
+template <class E> __global__ __launch_bounds__(256) void k_narrow_maps(ScanArgs A)
+{
+    const Thread me(A.B, A.ranges, A.C);
+    if (me.none) return;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c;
+    float pa = 1.f, ph = 0.f;
+    bool cut = false;
+#pragma unroll 8
+    for (long t = t0; t < end; ++t) {
+        const bool start = starts(A, me.b, t);
+        float a, i;
+        gates((float)f[t * A.f_ts], a, i);
+        ph = fmaf(a, start ? 0.f : ph, i * (float)x[t * A.x_ts]);
+        pa *= a;
+        cut |= start;
+    }
+    const long at = (me.b * A.ranges + me.z) * A.C + me.c;
+    A.totals[at] = cut ? -1.f : pa;
+    A.totals[(long)A.B * A.ranges * A.C + at] = ph;
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_narrow_grad_maps(ScanGradArgs A)
+{
+    const Thread me(A.B, A.ranges, A.C);
+    if (me.none) return;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
+    float pa = 1.f, pp = 0.f;
+    bool cut = false;
+#pragma unroll 8
+    for (long t = end - 1; t >= t0; --t) {
+        const bool start = starts(A, me.b, t);
+        float a, i;
+        gates((float)f[t * A.f_ts], a, i);
+        pp = start ? 0.f : a * ((float)dh[t * A.dh_ts] + pp);
+        pa *= a;
+        cut |= start;
+    }
+    const long at = (me.b * A.ranges + me.z) * A.C + me.c;
+    A.totals[at] = cut ? -1.f : pa;
+    A.totals[(long)A.B * A.ranges * A.C + at] = pp;
+}
+
+// One wave per channel of a sequence: lane l has the ranges from ranges l / 64 on (backward: from the other end).  `first`
+// ([B][C] or NULL): what enters the first of them.  In: maps; out: in place of H what enters each range.
+template <bool FORWARD> __global__ __launch_bounds__(64) void k_narrow_join(float *totals, const float *first, int B, int ranges, int C)
+{
+    const int lane = threadIdx.x, c = blockIdx.x % C;
+    const long b = blockIdx.x / C;
+    float *A = totals + b * ranges * C + c, *H = A + (long)B * ranges * C;
+    const int lo = (int)((long)ranges * lane / 64), hi = (int)((long)ranges * (lane + 1) / 64);
+    auto at = [&](int q) { return (long)(FORWARD ? q : ranges - 1 - q) * C; };
+    float a = 1.f, h = 0.f;      // the map of this lane's ranges
+#pragma unroll 4
+    for (int q = lo; q < hi; ++q) {
+        const float qa = A[at(q)], qh = H[at(q)];
+        h = through(h, qa, qh, qa < 0.f);
+        a = qa < 0.f || a < 0.f ? -1.f : a * qa;
+    }
+    for (int d = 1; d < 64; d *= 2) {   // of all up to this lane's
+        const float oa = __shfl_up(a, d), oh = __shfl_up(h, d);
+        if (lane >= d) {
+            h = through(oh, a, h, a < 0.f);
+            a = a < 0.f || oa < 0.f ? -1.f : a * oa;
+        }
+    }
+    const float ea = __shfl_up(a, 1), eh = __shfl_up(h, 1);
+    float s = first ? first[b * C + c] : 0.f;
+    if (lane) s = through(s, ea, eh, ea < 0.f);
+#pragma unroll 4
+    for (int q = lo; q < hi; ++q) {
+        const float qa = A[at(q)], qh = H[at(q)];
+        H[at(q)] = s;
+        s = through(s, qa, qh, qa < 0.f);
+    }
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_narrow(ScanArgs A)
+{
+    const Thread me(A.B, A.ranges, A.C);
+    if (me.none) return;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range), state = me.b * A.C + me.c;
+    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c;
+    E *h = (E *)A.h + me.b * A.h_bs + me.c;
+    float s = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.h0 ? A.h0[state] : 0.f;
+    float *carry = A.carry ? A.carry + (me.b * A.tiles + t0 / LINE) * A.C + me.c : nullptr;
+    for (long t = t0; t < end; t += LINE) {
+        if (carry) { *carry = s; carry += A.C; }
+        E fv[LINE], xv[LINE];
+        bool cut[LINE];
+#pragma unroll
+        for (int j = 0; j < LINE; ++j) {   // all loads before the first store
+            const long u = min(t + j, end - 1);
+            fv[j] = f[u * A.f_ts];
+            xv[j] = x[u * A.x_ts];
+            cut[j] = starts(A, me.b, u);
+        }
+#pragma unroll
+        for (int j = 0; j < LINE; ++j) {
+            if (t + j >= end) break;
+            float a, i;
+            gates((float)fv[j], a, i);
+            s = fmaf(a, cut[j] ? 0.f : s, i * (float)xv[j]);
+            h[(t + j) * A.h_ts] = (E)s;
+        }
+    }
+    if (A.h_last && end == A.T) A.h_last[state] = s;
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_narrow_grad(ScanGradArgs A)
+{
+    const Thread me(A.B, A.ranges, A.C);
+    if (me.none) return;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range), state = me.b * A.C + me.c;
+    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
+    E *df = (E *)A.df + me.b * A.df_bs + me.c, *dx = (E *)A.dx + me.b * A.dx_bs + me.c;
+    float mu = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.dlast ? A.dlast[state] : 0.f;
+    const long last = t0 + (end - t0 - 1) / LINE * LINE;
+    for (long t = last; t >= t0; t -= LINE) {
+        float s = A.carry[(me.b * A.tiles + t / LINE) * A.C + me.c], before[LINE], ga[LINE], gi[LINE], xv[LINE], gv[LINE];
+        bool cut[LINE];
+#pragma unroll
+        for (int j = 0; j < LINE; ++j) {
+            const long u = min(t + j, end - 1);
+            cut[j] = starts(A, me.b, u);
+            xv[j] = (float)x[u * A.x_ts];
+            gv[j] = (float)dh[u * A.dh_ts];
+            gates((float)f[u * A.f_ts], ga[j], gi[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < LINE; ++j) {
+            before[j] = cut[j] ? 0.f : s;
+            s = fmaf(ga[j], before[j], gi[j] * xv[j]);
+        }
+#pragma unroll
+        for (int j = LINE - 1; j >= 0; --j) {
+            if (t + j >= end) continue;
+            const float l = gv[j] + mu, n = ga[j] * l;
+            dx[(t + j) * A.dx_ts] = (E)(gi[j] * l);
+            df[(t + j) * A.df_ts] = (E)(gi[j] * n * (before[j] - xv[j]));
+            mu = cut[j] ? 0.f : n;
+        }
+    }
+    if (A.dh0 && me.z == 0) A.dh0[state] = mu;
+}
+
 }  // namespace seq

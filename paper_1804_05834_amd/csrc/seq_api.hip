@@ -39,6 +39,9 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
 // below that ranges: as many waves as the card holds at four per SIMD, each with 32 steps at least.
+// Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 117 / 285, 932 / 1229; 300 x 2000 x 8: 22 / 40, 78 / 122;
+// 574 x 2844 x 17: 101 / 210, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Up to 160 steps the two further launches of
+// ranges cost more than they give (2000 x 100 x 16: 29 / 51 in ranges, 16 / 26 without).
 constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
 constexpr int64_t LAST_LEVEL = 256 << 20;   // bytes of the cache in front of memory
 constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
@@ -71,7 +74,7 @@ const char *check_scan(const dqn_scan_args &s)
 
 // How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
 struct ScanCut {
-    enum { SHORT, STRIPS, LINES } form;
+    enum { SHORT, NARROW, STRIPS, LINES } form;
     int waves;         // of a workgroup of the strips
     long tile, tiles;  // steps between two states of `carry`, states of a sequence
     long range;        // lines: steps of a range
@@ -80,6 +83,11 @@ struct ScanCut {
 ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 {
     if (T <= seq::SCAN_SHORT) return ScanCut{ScanCut::SHORT, 0, seq::SCAN_SHORT, T ? 1 : 0, (long)T, 1};
+    if (C <= 16 || (C <= 32 && T > 1000)) {
+        const int64_t all = std::max<int64_t>(1, (int64_t)B * C), want = T <= 160 ? 1 : std::max<int64_t>(1, std::min<int64_t>(SCAN_WANT * 64 / all, T / SCAN_LEAST));
+        const long per = (T + want - 1) / want, range = (per + seq::LINE - 1) / seq::LINE * seq::LINE;
+        return ScanCut{ScanCut::NARROW, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), range, (int)((T + range - 1) / range)};
+    }
     const int64_t strips = (int64_t)B * ((C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), lines = (int64_t)B * ((C + 127) / 128);
     if (lines < SCAN_LINES && strips >= SCAN_STRIPS) {
         int waves = 1;
@@ -94,6 +102,7 @@ ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C)
 {
     if (c.ranges == 1) return 0;
+    if (c.form == ScanCut::NARROW) return ((size_t)B * c.ranges * 2 * C * 4 + 15) / 16 * 16;
     const size_t maps = c.ranges + (c.ranges + seq::LINE_WAVES - 1) / seq::LINE_WAVES;
     return ((size_t)B * maps * 2 * C * 4 + 15) / 16 * 16;
 }
@@ -146,10 +155,29 @@ template <class E, int V> void launch_strips(const seq::ScanGradArgs &A, int wav
 {
     seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
 }
+template <class E> void launch_narrow(const seq::ScanArgs &A, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
+    if (A.ranges > 1) {
+        seq::k_narrow_maps<E><<<grid, 256, 0, st>>>(A);
+        seq::k_narrow_join<true><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.h0, A.B, A.ranges, A.C);
+    }
+    seq::k_narrow<E><<<grid, 256, 0, st>>>(A);
+}
+template <class E> void launch_narrow(const seq::ScanGradArgs &A, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
+    if (A.ranges > 1) {
+        seq::k_narrow_grad_maps<E><<<grid, 256, 0, st>>>(A);
+        seq::k_narrow_join<false><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.dlast, A.B, A.ranges, A.C);
+    }
+    seq::k_narrow_grad<E><<<grid, 256, 0, st>>>(A);
+}
 // fits(n): whether n channels can be taken at once
 template <class E, class Args, class F> void launch_recurrence(const Args &A, const ScanCut &c, F &&fits, hipStream_t st)
 {
-    if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
+    if (c.form == ScanCut::NARROW) launch_narrow<E>(A, st);
+    else if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
     else if (c.form == ScanCut::STRIPS) fits(2) ? launch_strips<E, 2>(A, c.waves, st) : launch_strips<E, 1>(A, c.waves, st);
     else fits(2) ? launch_lines<E, 2>(A, st) : launch_lines<E, 1>(A, st);
 }

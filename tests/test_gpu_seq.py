@@ -45,6 +45,7 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     (70, 33, 192, "time", True, 0.05),
     # many sequences: strips of channels in one workgroup, and whole sequences per wave
     (300, 20, 64, "half", True, 0.05), (260, 150, 60, "plain", True, 0.02), (90, 300, 130, "odd", True, 0.01), (256, 129, 64, "time", False, 0.0), (64, 1030, 256, "half", True, 0.002),
+    (1, 20000, 1, "plain", True, 0.0005), (5, 3001, 2, "odd", True, 0.001), (40, 700, 16, "time", False, 0.01), (3, 2500, 31, "half", True, 0.002),
     (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
@@ -106,9 +107,9 @@ def test_scan_state_in_place_and_outputs_apart(seq):
 
 
 @pytest.mark.parametrize("B,T", [(2, 1), (2, 5), (2, 40), (2, 600), (2, 9000), (300, 20), (300, 300), (2100, 30)])
-def test_scan_a_reset_forgets_anything(seq, B, T):
+@pytest.mark.parametrize("C", [64, 3])
+def test_scan_a_reset_forgets_anything(seq, B, T, C):
     """A state that is NaN or infinite does not reach past an episode's start, forward or backward."""
-    C = 64
     f, x = rnd(1, B, T, C, at=1.0), rnd(2, B, T, C)
     cut = T // 2
     reset = torch.zeros(B, T, dtype=torch.uint8, device="cuda")
