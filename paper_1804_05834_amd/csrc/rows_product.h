@@ -250,33 +250,48 @@ template <class E, int BM, int BN, int WM, int WN> __global__ __launch_bounds__(
             __builtin_amdgcn_sched_group_barrier(0x008, NI * (sizeof(E) == 2 ? 1 : 4), 0);
         }
     }
-    // y in bf16, whole columns: a wave's 64 columns are a 128-byte line of a row.  Stored as the lanes hold them, 8 bytes of
-    // each of sixteen rows, they took 19 us of a tile of 8192 x 4096 outputs; through LDS, whose operands are done
-    // with, a lane stores 16 bytes and eight lanes a line.  Pieces of 16 bytes change places as the operands' do.
-    constexpr bool lines = sizeof(E) == 2 && NI == 4;
-    if (lines && A.wide == 8 && n0 + wn + 64 <= A.N) {
+    // 64 columns of a row are a line or two of memory.  Stored as the lanes hold them, 8 bytes of each of sixteen rows, they
+    // took 19 us of a tile of 8192 x 4096 outputs in bf16.  So they change places through LDS, whose operands are done
+    // with: rows of 64 columns, in pieces of 16 bytes with places as the operands' have.  Then a lane stores a piece; where
+    // y's rows are not aligned to pieces or end within the columns, a lane a column.
+    if constexpr (NI == 4) {
+        constexpr int ES = sizeof(E), ROW = 64 * ES, PIECES = ROW / 16, SHARE = 2 * STAGE / WAVES, XP = SHARE / (16 * ROW) < MI ? SHARE / (16 * ROW) : MI;
+        static_assert(MI % XP == 0, "passes of whole 16 rows");
+        auto swap = [](int r) { return ES == 2 ? r >> 1 & 7 : r & 15; };
+        uint8_t *mine = lds + wave * SHARE;
+        const bool whole = A.wide == 16 / ES && n0 + wn + 64 <= A.N;
         __syncthreads();
-        uint8_t *mine = lds + wave * (MI * 2048);
 #pragma unroll
-        for (int y = 0; y < NI; ++y) {
-            const int n = n0 + wn + 16 * y + 4 * g;
-            const Acc sw = four_of(A.w_scale, n, A.N), b = four_of(A.bias, n, A.N);
+        for (int pass = 0; pass < MI; pass += XP) {   // the wave reads what it wrote itself: its own LDS accesses are in order
 #pragma unroll
-            for (int x = 0; x < MI; ++x) {
-                const float sa = A.a_scale[min(m0 + wm + 16 * x + i, A.M - 1)];
-                vec<bf16, 4> v;
+            for (int y = 0; y < NI; ++y) {
+                const int n = n0 + wn + 16 * y + 4 * g;
+                const Acc sw = four_of(A.w_scale, n, A.N), b = four_of(A.bias, n, A.N);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = (bf16)(s[x][y][j] * sa * sw[j] + b[j]);
-                *reinterpret_cast<vec<bf16, 4> *>(mine + x * 2048 + i * 128 + ((2 * y + g / 2) ^ (i >> 1)) * 16 + (g & 1) * 8) = v;
+                for (int x = 0; x < XP; ++x) {
+                    const float sa = A.a_scale[min(m0 + wm + 16 * (pass + x) + i, A.M - 1)];
+                    vec<E, 4> v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = (E)(s[pass + x][y][j] * sa * sw[j] + b[j]);
+                    const int at = (16 * y + 4 * g) * ES;
+                    *reinterpret_cast<vec<E, 4> *>(mine + (16 * x + i) * ROW + ((at / 16) ^ swap(i)) * 16 + at % 16) = v;
+                }
             }
-        }
-        // the wave reads what it wrote itself: no barrier, the order of its own LDS accesses does
+            const long m1 = m0 + wm + 16 * pass;
+            E *out = (E *)A.y + m1 * A.y_rs + n0 + wn;
+            if (whole) {
 #pragma unroll
-        for (int q = 0; q < 2 * MI; ++q) {
-            const int r = 8 * q + (lane >> 3), c = lane & 7;
-            const auto v = *reinterpret_cast<const vec<uint32_t, 4> *>(mine + r * 128 + (c ^ (r >> 1 & 7)) * 16);
-            const long m = m0 + wm + r;
-            if (m < A.M) *reinterpret_cast<vec<uint32_t, 4> *>((E *)A.y + m * A.y_rs + n0 + wn + 8 * c) = v;
+                for (int q = 0; q < XP * 16 * PIECES / 64; ++q) {
+                    const int r = q * (64 / PIECES) + lane / PIECES, c = lane % PIECES;
+                    const auto v = *reinterpret_cast<const vec<uint32_t, 4> *>(mine + r * ROW + (c ^ swap(r)) * 16);
+                    if (m1 + r < A.M) *reinterpret_cast<vec<uint32_t, 4> *>(out + r * A.y_rs + c * (16 / ES)) = v;
+                }
+            } else if (n0 + wn + lane < A.N) {
+                const int left = (int)min((long)(16 * XP), A.M - m1);
+#pragma unroll 8
+                for (int r = 0; r < left; ++r)
+                    out[r * A.y_rs + lane] = *reinterpret_cast<const E *>(mine + r * ROW + ((lane * ES / 16) ^ swap(r)) * 16 + lane * ES % 16);
+            }
         }
         return;
     }

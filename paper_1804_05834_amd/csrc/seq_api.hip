@@ -195,11 +195,17 @@ const char *check_rows8(const void *p, int64_t rs, int64_t M, int64_t K)
     return M == 1 || rs >= K ? nullptr : "the stride of 8-bit rows is shorter than a row";
 }
 
-int norm_parts(int64_t M) { return (int)std::min<int64_t>(seq::NORM_PARTS, (M + seq::NORM_ROWS - 1) / seq::NORM_ROWS); }
+// Partial sums of the weight's gradient, a workgroup each: of 16 rows, or of fewer where there would not be one workgroup per
+// compute unit (241 rows of 6497: 16 workgroups 80 us, 241 workgroups 20 us).
+int norm_parts(int64_t M, int C)
+{
+    const int64_t least = std::min<int64_t>(256, C > 1024 ? M : (M + 3) / 4);
+    return (int)std::min<int64_t>(seq::NORM_PARTS, std::max<int64_t>((M + seq::NORM_ROWS - 1) / seq::NORM_ROWS, least));
+}
 
 // The smallest form of a norm kernel that holds a row of C elements (8-bit rows: up to the next multiple of 16), V being
-// 16 bytes' worth of elements or 1.  go(V, K, W, lanes) launches it.  A row is one wave's up to 32 (V = 1: 16) elements per
-// lane, four waves' up to four times that; a workgroup of sixteen waves takes longer ones.
+// 16 bytes' worth of elements or 1.  go(V, K, W, lanes) launches it.  A thread holds up to 16 elements (more cost so many
+// registers that few waves fit), a row is one wave's, four waves' or sixteen waves'.
 template <int N> using Int = std::integral_constant<int, N>;
 template <class E, class F> void norm_form(bool wide, int C, F &&go)
 {
@@ -212,14 +218,15 @@ template <class E, class F> void norm_form(bool wide, int C, F &&go)
     if (wide) {
         if (C <= 64 * V) go(Int<V>{}, Int<1>{}, Int<1>{}, lanes(V));
         else if (C <= 128 * V) go(Int<V>{}, Int<2>{}, Int<1>{}, 64);
-        else if (C <= 64 * 32) go(Int<V>{}, Int<32 / V>{}, Int<1>{}, 64);
-        else if (C <= 256 * 32) go(Int<V>{}, Int<32 / V>{}, Int<4>{}, 64);
+        else if (C <= 64 * 16) go(Int<V>{}, Int<16 / V>{}, Int<1>{}, 64);
+        else if (C <= 256 * 16) go(Int<V>{}, Int<16 / V>{}, Int<4>{}, 64);
         else go(Int<V>{}, Int<16 / V>{}, Int<16>{}, 64);
     } else {
         if (C <= 64) go(Int<1>{}, Int<1>{}, Int<1>{}, lanes(1));
         else if (C <= 256) go(Int<1>{}, Int<4>{}, Int<1>{}, 64);
         else if (C <= 1024) go(Int<1>{}, Int<16>{}, Int<1>{}, 64);
         else if (C <= 4096) go(Int<1>{}, Int<16>{}, Int<4>{}, 64);
+        else if (C <= 8192) go(Int<1>{}, Int<8>{}, Int<16>{}, 64);
         else go(Int<1>{}, Int<16>{}, Int<16>{}, 64);
     }
 }
@@ -393,7 +400,7 @@ int32_t dqn_norm_sizes(int64_t M, int32_t C, size_t *workspace)
     static const char *call = "dqn_norm_sizes";
     if (!workspace) return bad(call, "NULL argument");
     if (M < 0 || M > INT32_MAX || C < 1 || C > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, C in 1..DQN_NORM_MAX");
-    *workspace = (size_t)norm_parts(M) * C * 4;
+    *workspace = (size_t)norm_parts(M, C) * C * 4;
     return DQN_OK;
 }
 
@@ -429,7 +436,7 @@ int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream)
     if (n.M < 0 || n.M > INT32_MAX || n.C < 1 || n.C > DQN_NORM_MAX) return bad(call, "M must be in 0..2^31-1, C in 1..DQN_NORM_MAX");
     if (!n.dw || !at(n.dw, 4)) return bad(call, "dw is NULL or not aligned to its elements");
     hipStream_t st = (hipStream_t)stream;
-    const int parts = norm_parts(n.M);
+    const int parts = norm_parts(n.M, n.C);
     if (n.M) {
         if (!n.weight || !n.rstd || !at(n.weight, 4) || !at(n.rstd, 4)) return bad(call, "weight or rstd is NULL or not aligned to its elements");
         if (!n.workspace || !at(n.workspace, 16)) return bad(call, "workspace is NULL or not 16-byte aligned");
