@@ -33,7 +33,7 @@ struct NormGradArgs {
     int C, lanes;
 };
 
-constexpr int NORM_PARTS = 1024;   // most partial sums of the weight's gradient, one per workgroup
+constexpr int NORM_PARTS = 512;   // most partial sums of the weight's gradient, one per workgroup
 constexpr int NORM_ROWS = 16;      // rows that are worth a partial sum
 
 // The W waves of a row add up (or fold by f) a value; `sh` holds W floats and must not be written again before all have
@@ -223,6 +223,7 @@ __global__ __launch_bounds__(1024) void k_norm_grad_join(const float *part, int 
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     float s = 0.f;
     if (col < C)
+#pragma unroll 8
         for (int p = g; p < parts; p += 64) s += part[(long)p * C + col];
     sh[g][c] = s;
     for (int o = 32; o; o >>= 1) {

@@ -50,28 +50,28 @@ def _call(rc):
         raise DqnError(rc, (lib().dqn_last_error(None) or b"").decode())
 
 
-def _need(t, name, dtype, shape, device):
-    """t's address, after a look at what it is."""
+def _refuse(t, name, dtype, shape, device, why):
+    """Says what is wrong with a tensor that a look at it has found wanting."""
     if t.dtype is not dtype or t.shape != shape:
-        raise ValueError("%s: %s of shape %s expected, got %s of shape %s" % (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
-    if t.get_device() != device:
-        raise ValueError("%s: not on the current GPU" % name)
-    return t.data_ptr()
+        why = "%s of shape %s expected, got %s of shape %s" % (dtype, tuple(shape), t.dtype, tuple(t.shape))
+    elif t.get_device() != device:
+        why = "not on the current GPU"
+    raise ValueError("%s: %s" % (name, why))
 
 
 def _rows(t, name, dtype, shape, device):
     """(address, strides) of a tensor whose last dimension lies in one piece."""
-    p, st = _need(t, name, dtype, shape, device), t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
-        raise ValueError("%s: the last dimension must have stride 1" % name)
-    return p, st
+    st = t.stride()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and (st[-1] == 1 or shape[-1] <= 1):
+        return t.data_ptr(), st
+    _refuse(t, name, dtype, shape, device, "the last dimension must have stride 1")
 
 
 def _flat(t, name, dtype, shape, device):
     """The address of a tensor that must lie in one piece."""
-    if not t.is_contiguous():
-        raise ValueError("%s: must be contiguous" % name)
-    return _need(t, name, dtype, shape, device)
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, name, dtype, shape, device, "must be contiguous")
 
 
 def _kind(t, name):
@@ -119,10 +119,10 @@ def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
     fp, fs = _rows(f, "f", dt, shape, dev)
     xp, xs = _rows(x, "x", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
-    h = torch.empty(shape, dtype=dt, device=f.device) if out is None else out
+    h = torch.empty_like(f) if out is None else out
     hp, hs = _rows(h, "out", dt, shape, dev)
     if last is None:
-        last = torch.empty((B, Ch), dtype=torch.float32, device=f.device)
+        last = torch.empty_strided((B, Ch), (Ch, 1), dtype=torch.float32, device=f.device)
     carry = torch.empty(carry_n // 4, dtype=torch.float32, device=f.device) if save else None
     work, wp = _scratch(work_n, f.device)
     rp, rb, rt = _reset(reset, B, T, dev)
@@ -144,10 +144,10 @@ def scan_backward(dh, f, x, carry, reset=None, dlast=None, out=None):
     xp, xs = _rows(x, "x", dt, shape, dev)
     gp, gs = _rows(dh, "dh", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
-    df, dx = (torch.empty(shape, dtype=dt, device=f.device), torch.empty(shape, dtype=dt, device=f.device)) if out is None else out
+    df, dx = (torch.empty_like(f), torch.empty_like(x)) if out is None else out
     dfp, dfs = _rows(df, "df", dt, shape, dev)
     dxp, dxs = _rows(dx, "dx", dt, shape, dev)
-    dh0 = torch.empty((B, Ch), dtype=torch.float32, device=f.device)
+    dh0 = torch.empty_strided((B, Ch), (Ch, 1), dtype=torch.float32, device=f.device)
     work, wp = _scratch(work_n, f.device)
     rp, rb, rt = _reset(reset, B, T, dev)
     args = SCAN_GRAD_ARGS.pack(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1], _flat(carry, "carry", torch.float32, (carry_n // 4,), dev),
@@ -168,17 +168,17 @@ def _matrix(t, name):
 def _rows8(M, K, device):
     """8-bit rows as the library lays them out, their stride a multiple of 16: (the rows, that stride)"""
     st = (K + 15) & -16
-    q = torch.empty((M, st), dtype=torch.float8_e4m3fn, device=device)
+    q = torch.empty_strided((M, st), (st, 1), dtype=torch.float8_e4m3fn, device=device)
     return (q if st == K else q[:, :K]), st
 
 
 def _residual(x, residual, shape, dev):
-    """(address, stride, r to write, its address); nothing of it without a residual"""
+    """(address, stride, r to write, its address and stride); nothing of it without a residual"""
     if residual is None:
-        return 0, 0, x, 0
+        return 0, 0, x, 0, 0
     p, st = _rows(residual, "residual", x.dtype, shape, dev)
-    r = torch.empty(shape, dtype=x.dtype, device=x.device)
-    return p, st[0], r, r.data_ptr()
+    r = torch.empty_like(x)
+    return p, st[0], r, r.data_ptr(), r.stride()[0]
 
 
 def norm(x, weight, residual=None, eps=1e-6):
@@ -187,11 +187,11 @@ def norm(x, weight, residual=None, eps=1e-6):
     (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, Ch = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
-    sp, ss, r, rp = _residual(x, residual, shape, dev)
-    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    sp, ss, r, rp, rs = _residual(x, residual, shape, dev)
+    y = torch.empty_like(x)
     rstd = torch.empty(M, dtype=torch.float32, device=x.device)
-    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, Ch,
-                          y.data_ptr(), Ch, 0, 0, 0, rstd.data_ptr())
+    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, rs,
+                          y.data_ptr(), y.stride()[0], 0, 0, 0, rstd.data_ptr())
     _call(lib().dqn_norm_forward(args, _raw_stream(dev)))
     # in bf16 the backward pass forms the sum again from its two terms, since r is rounded
     return y, r, (rstd, x, residual) if kind == BF16 else (rstd, r, None)
@@ -202,10 +202,10 @@ def norm_rows(x, weight, residual=None, eps=1e-6):
     (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, Ch = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
-    sp, ss, r, rp = _residual(x, residual, shape, dev)
+    sp, ss, r, rp, rs = _residual(x, residual, shape, dev)
     q, qs = _rows8(M, Ch, x.device)
     scale = torch.empty(M, dtype=torch.float32, device=x.device)
-    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, Ch,
+    args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, rs,
                           0, 0, q.data_ptr(), qs, scale.data_ptr(), 0)
     _call(lib().dqn_norm_forward(args, _raw_stream(dev)))
     return q, scale, r
@@ -229,11 +229,11 @@ def norm_backward(dy, r, saved, weight, dr=None):
     xp, xs = _rows(x, "x", dt, shape, dev)
     sp, ss = (0, (0,)) if residual is None else _rows(residual, "residual", dt, shape, dev)
     rp, rs = (0, (0,)) if dr is None else _rows(dr, "dr", dt, shape, dev)
-    dx = torch.empty(shape, dtype=dt, device=r.device)
+    dx = torch.empty_like(r)
     dw = torch.empty(Ch, dtype=torch.float32, device=r.device)
     work, wp = _scratch(_norm_sizes(M, Ch), r.device)
     args = NORM_GRAD_ARGS.pack(kind, Ch, M, gp, xp, sp, rp, gs[0], xs[0], ss[0], rs[0], _flat(weight, "weight", torch.float32, (Ch,), dev),
-                               _flat(rstd, "rstd", torch.float32, (M,), dev), dx.data_ptr(), Ch, dw.data_ptr(), wp)
+                               _flat(rstd, "rstd", torch.float32, (M,), dev), dx.data_ptr(), dx.stride()[0], dw.data_ptr(), wp)
     _call(lib().dqn_norm_backward(args, _raw_stream(dev)))
     return dx, dw
 
@@ -260,7 +260,7 @@ def product(a, w, bias=None, dtype=torch.bfloat16, out=None):
     (M, K), N = qa.shape, qw.shape[0]
     ap, as_ = _rows(qa, "a", torch.float8_e4m3fn, (M, K), dev)
     wp, ws = _rows(qw, "w", torch.float8_e4m3fn, (N, K), dev)
-    y = torch.empty((M, N), dtype=dtype, device=qa.device) if out is None else out
+    y = torch.empty_strided((M, N), (N, 1), dtype=dtype, device=qa.device) if out is None else out
     yp, ys = _rows(y, "out", dtype, (M, N), dev)
     args = PRODUCT_ARGS.pack(kind, N, K, M, ap, wp, as_[0], ws[0], _flat(sa, "a's scale", torch.float32, (M,), dev),
                              _flat(sw, "w's scale", torch.float32, (N,), dev), 0 if bias is None else _flat(bias, "bias", torch.float32, (N,), dev),
