@@ -119,16 +119,23 @@ def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
     fp, fs = _rows(f, "f", dt, shape, dev)
     xp, xs = _rows(x, "x", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
-    h = torch.empty_like(f) if out is None else out
-    hp, hs = _rows(h, "out", dt, shape, dev)
+    if out is None:
+        h = torch.empty_like(f)
+        hp, hs = h.data_ptr(), h.stride()
+    else:
+        h = out
+        hp, hs = _rows(h, "out", dt, shape, dev)
     if last is None:
         last = torch.empty_strided((B, Ch), (Ch, 1), dtype=torch.float32, device=f.device)
+        lp = last.data_ptr()
+    else:
+        lp = _flat(last, "last", torch.float32, (B, Ch), dev)
     carry = torch.empty(carry_n // 4, dtype=torch.float32, device=f.device) if save else None
     work, wp = _scratch(work_n, f.device)
     rp, rb, rt = _reset(reset, B, T, dev)
     args = SCAN_ARGS.pack(kind, B, Ch, T, fp, xp, fs[0], fs[1], xs[0], xs[1],
                           0 if h0 is None else _flat(h0, "h0", torch.float32, (B, Ch), dev), rp, rb, rt, hp, hs[0], hs[1],
-                          _flat(last, "last", torch.float32, (B, Ch), dev), carry.data_ptr() if save else 0, wp)
+                          lp, carry.data_ptr() if save else 0, wp)
     _call(lib().dqn_scan_forward(args, _raw_stream(dev)))
     return (h, last, carry) if save else (h, last)
 
@@ -254,17 +261,21 @@ def product(a, w, bias=None, dtype=torch.bfloat16, out=None):
     """a = (q [M][K], scale [M]) and w = (q [N][K], scale [N]) as rows() and norm_rows() give them, bias [N] float32 or None
     -> y [M][N] of `dtype`."""
     (qa, sa), (qw, sw), dev = a, w, _current_device()
-    kind = _TYPES.get(dtype)
-    if kind is None or qa.ndim != 2 or qw.ndim != 2:
+    kind, shape, N = _TYPES.get(dtype), qa.shape, sw.shape[0] if sw.shape else 0
+    if kind is None or len(shape) != 2:
         raise ValueError("dtype: float32 or bfloat16 expected; rows: [M][K] and [N][K]")
-    (M, K), N = qa.shape, qw.shape[0]
+    M, K = shape
     ap, as_ = _rows(qa, "a", torch.float8_e4m3fn, (M, K), dev)
     wp, ws = _rows(qw, "w", torch.float8_e4m3fn, (N, K), dev)
-    y = torch.empty_strided((M, N), (N, 1), dtype=dtype, device=qa.device) if out is None else out
-    yp, ys = _rows(y, "out", dtype, (M, N), dev)
+    if out is None:
+        y = torch.empty_strided((M, N), (N, 1), dtype=dtype, device=qa.device)
+        yp, ys = y.data_ptr(), N
+    else:
+        y = out
+        yp, (ys, _) = _rows(y, "out", dtype, (M, N), dev)
     args = PRODUCT_ARGS.pack(kind, N, K, M, ap, wp, as_[0], ws[0], _flat(sa, "a's scale", torch.float32, (M,), dev),
                              _flat(sw, "w's scale", torch.float32, (N,), dev), 0 if bias is None else _flat(bias, "bias", torch.float32, (N,), dev),
-                             yp, ys[0])
+                             yp, ys)
     _call(lib().dqn_rows_product(args, _raw_stream(dev)))
     return y
 
