@@ -69,6 +69,10 @@ __device__ __forceinline__ float product(float a, float b)
 }
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN if one is a NaN
 
+// An address that comes from memory could be one in LDS for all that the compiler knows; these are not.
+template <class T> using Global = __attribute__((address_space(1))) T;
+template <class T> __device__ __forceinline__ Global<T> *global(T *p) { return (Global<T> *)(uintptr_t)p; }
+
 // What a lane holds of a block: four elements and their moments.
 template <class G, int BITS> struct AdamLane {
     using Word = std::conditional_t<BITS == 8, uint32_t, vec<float, 4>>;
@@ -86,13 +90,13 @@ template <class G, int BITS> struct AdamLane {
         count = min(4, max(0, ch.n - first));
         whole = ch.wide && ch.n >= base + ADAM_BLOCK;
         if (whole) {
-            p = load<4>(ch.param + first);
-            g = load<4>((const G *)ch.grad + first);
+            p = *reinterpret_cast<const Global<vec<float, 4>> *>(global(ch.param) + first);
+            g = *reinterpret_cast<const Global<vec<G, 4>> *>(global((const G *)ch.grad) + first);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                p[j] = j < count ? ch.param[first + j] : 0.f;
-                g[j] = j < count ? ((const G *)ch.grad)[first + j] : (G)0.f;
+                p[j] = j < count ? global(ch.param)[first + j] : 0.f;
+                g[j] = j < count ? global((const G *)ch.grad)[first + j] : (G)0.f;
             }
         }
         const long place = ch.at + first;     // the buffers of moments go on to the end of the block
@@ -122,14 +126,14 @@ template <class G, int BITS> struct AdamLane {
             p[j] = p[j] * keep - A.rate * mn[j] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(vn[j]), A.root, A.eps));
         }
         if (whole) {
-            store<4>(ch.param + first, p);
-            if (ch.copy) store<4>((bf16 *)ch.copy + first, __builtin_convertvector(p, vec<bf16, 4>));
+            *reinterpret_cast<Global<vec<float, 4>> *>(global(ch.param) + first) = p;
+            if (ch.copy) *reinterpret_cast<Global<vec<bf16, 4>> *>(global((bf16 *)ch.copy) + first) = __builtin_convertvector(p, vec<bf16, 4>);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (j < count) {
-                    ch.param[first + j] = p[j];
-                    if (ch.copy) ((bf16 *)ch.copy)[first + j] = (bf16)p[j];
+                    global(ch.param)[first + j] = p[j];
+                    if (ch.copy) global((bf16 *)ch.copy)[first + j] = (bf16)p[j];
                 } else {
                     mn[j] = vn[j] = 0.f;
                 }
@@ -143,11 +147,12 @@ template <class G, int BITS> struct AdamLane {
             mt = group_fold(mt, 64, larger);
             vt = group_fold(vt, 64, larger);
             const float mi = mt > 0.f ? product(1.f / mt, E4M3_MAX) : 0.f, vi = vt > 0.f ? product(1.f / vt, E5M2_MAX) : 0.f;
+            const uint64_t z0 = misc::mix64(A.seed, (uint64_t)place / 2), z1 = misc::mix64(A.seed, (uint64_t)place / 2 + 1);
             uint32_t mb[4], vb[4];
             float mq[4], vq[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint64_t z = misc::mix64(A.seed, (uint64_t)(place + j) >> 1);
+                const uint64_t z = j < 2 ? z0 : z1;
                 const uint32_t bits = (uint32_t)(j & 1 ? z >> 32 : z);
                 mb[j] = bits & 0xFFFF;
                 vb[j] = bits >> 16;
