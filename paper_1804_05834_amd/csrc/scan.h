@@ -85,7 +85,8 @@ __device__ __forceinline__ long sequence_of(long id, long all, int per)   // id 
 }
 
 // A thread takes V channels of a sequence through all of its at most SCAN_SHORT steps; all of its loads go out before
-// the first is used.  The step of an acting agent is T = 1.
+// the first is used.  The step of an acting agent is T = 1 (32 environments of 512 channels: 2.9 us, a launch and two trips
+// to memory).
 template <class E, int V> __global__ __launch_bounds__(256) void k_scan_short(ScanArgs A)
 {
     const long id = (long)blockIdx.x * 256 + threadIdx.x, all = (long)A.B * (A.C / V);
@@ -168,9 +169,10 @@ template <class E, int V> __global__ __launch_bounds__(256) void k_scan_grad_sho
 // and L = 16 / V steps: with V = 2 half a wave is a row of the strip and a wave holds two runs of eight steps, with
 // V = 1 (a size, a stride or an address that is not a multiple of two elements) a wave is one run of sixteen.
 //
-// Vector instructions cost as much as memory does here (about thirty per element, two of them exp and the reciprocal), so
-// the choices that few tiles need are kept out of the others' way: a tile that ends beyond the range or that holds
-// the start of an episode takes the careful form of the loops (EDGE), the rest the one without tests.
+// Vector instructions cost nearly as much as memory does here (about twenty per element, two of them exp and the
+// reciprocal), so the choices that few tiles need are kept out of the others' way: a tile that ends beyond the sequence or
+// that holds the start of an episode takes the careful form of the loops (Edge), the rest the one without tests.
+// Measured, 32 sequences of 512 steps of 512 channels in bf16: forward 14.1 us (3.6 TB/s), backward 21.0 (4.0).
 template <int V> struct Strip {
     static constexpr int L = SCAN_RUN / V, G = SCAN_STRIP / V, S = 64 / G;
 };
@@ -514,6 +516,9 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
 //
 // Eight waves, eight ranges of a sequence in turn, are a workgroup and a group: maps are kept of ranges and of groups, and
 // a workgroup composes the groups before it with all of its waves.
+//
+// Measured: 512 sequences of 64 steps of 512 channels in bf16, a wave each, 18 us forward (5.6 TB/s), 36 backward (4.7); one
+// sequence of 131072 steps of 512 channels, in ranges, 57 for the maps (4.7 TB/s) and 67 for the states (6.0).
 constexpr int LINE = 8;         // steps between two states of `carry`, and of a wave's loads
 constexpr int LINE_WAVES = 8;   // waves of a workgroup
 
@@ -868,7 +873,8 @@ template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_l
 // ------------------------------------------------------------ narrow sequences
 // Few channels: a wave of a strip or a line would have few lanes at work.  Here a thread takes one channel through a range of
 // steps, neighbouring threads the channels and then the ranges, and time is cut as far as it takes to have enough
-// threads.  Maps of ranges first, then one wave per channel of a sequence joins them into the states that enter the ranges
+// threads (83 sequences of 95456 steps of one channel in bf16: 117 us forward, 285 backward; a lane's steps lie in a row of
+// memory there, and a line is fetched again for every eight of them).  Maps of ranges first, then one wave per channel of a sequence joins them into the states that enter the ranges
 // (in place of the maps' H), then the ranges.  `totals` is [2][B][ranges][C]: A (-1: an episode starts there), H.
 struct Thread {
     long b;
