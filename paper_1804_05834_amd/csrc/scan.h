@@ -873,8 +873,8 @@ template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_l
 // ------------------------------------------------------------ narrow sequences
 // Few channels: a wave of a strip or a line would have few lanes at work.  Here a thread takes one channel through a range of
 // steps, neighbouring threads the channels and then the ranges, and time is cut as far as it takes to have enough
-// threads (83 sequences of 95456 steps of one channel in bf16: 117 us forward, 285 backward; a lane's steps lie in a row of
-// memory there, and a line is fetched again for every eight of them).  Maps of ranges first, then one wave per channel of a sequence joins them into the states that enter the ranges
+// threads (83 sequences of 95456 steps of one channel in bf16: 139 us forward, 179 backward, 0.4 TB/s: a load of a wave
+// touches 64 lines there).  Maps of ranges first, then one wave per channel of a sequence joins them into the states that enter the ranges
 // (in place of the maps' H), then the ranges.  `totals` is [2][B][ranges][C]: A (-1: an episode starts there), H.
 struct Thread {
     long b;
@@ -890,46 +890,90 @@ struct Thread {
         none = b >= B;
     }
 };
-template <class Args> __device__ __forceinline__ bool starts(const Args &A, long b, long t) { return A.reset && A.reset[b * A.r_bs + t * A.r_ts]; }
+// Steps t .. t + N - 1 of a thread, those from `end` on being the last one: what it loads of a tensor, and bit j of the
+// flags for step j.  N is 32 (16 backward) for many steps of one or two channels, so that a line of memory, which holds the steps one
+// after the other there, is used whole while it is in the first cache; else 8.
+template <int N, class E> __device__ __forceinline__ void steps_of(E (&v)[N], const E *p, long ts, long t, long end)
+{
+    if (t + N <= end) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = p[(t + j) * ts];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = p[min(t + j, end - 1) * ts];
+    }
+}
+template <int N, class Args> __device__ __forceinline__ unsigned flags_of(const Args &A, long b, long t, long end)
+{
+    unsigned m = 0;
+    if (!A.reset) return m;
+    const uint8_t *p = A.reset + b * A.r_bs;
+    if (A.r_ts == 1 && t + N <= end) {   // eight flags at a time, at any address
+#pragma unroll
+        for (int k = 0; k < N; k += 8) {
+            uint64_t v;
+            __builtin_memcpy(&v, p + t + k, 8);
+            if (!v) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m |= (unsigned)((v >> 8 * j & 255) != 0) << (k + j);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) m |= (unsigned)(t + j < end && p[min(t + j, end - 1) * A.r_ts] != 0) << j;
+    }
+    return m;
+}
 
-template <class E> __global__ __launch_bounds__(256) void k_narrow_maps(ScanArgs A)
+template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_maps(ScanArgs A)
 {
     const Thread me(A.B, A.ranges, A.C);
     if (me.none) return;
     const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
     const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c;
     float pa = 1.f, ph = 0.f;
-    bool cut = false;
-#pragma unroll 8
-    for (long t = t0; t < end; ++t) {
-        const bool start = starts(A, me.b, t);
-        float a, i;
-        gates((float)f[t * A.f_ts], a, i);
-        ph = fmaf(a, start ? 0.f : ph, i * (float)x[t * A.x_ts]);
-        pa *= a;
-        cut |= start;
+    unsigned cut = 0;
+    for (long t = t0; t < end; t += N) {
+        E fv[N], xv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(xv, x, A.x_ts, t, end);
+        const unsigned flags = flags_of<N>(A, me.b, t, end);
+        cut |= flags;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (t + j >= end) break;
+            float a, i;
+            gates((float)fv[j], a, i);
+            ph = fmaf(a, flags >> j & 1 ? 0.f : ph, i * (float)xv[j]);
+            pa *= a;
+        }
     }
     const long at = (me.b * A.ranges + me.z) * A.C + me.c;
     A.totals[at] = cut ? -1.f : pa;
     A.totals[(long)A.B * A.ranges * A.C + at] = ph;
 }
 
-template <class E> __global__ __launch_bounds__(256) void k_narrow_grad_maps(ScanGradArgs A)
+template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_grad_maps(ScanGradArgs A)
 {
     const Thread me(A.B, A.ranges, A.C);
     if (me.none) return;
     const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
     const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
     float pa = 1.f, pp = 0.f;
-    bool cut = false;
-#pragma unroll 8
-    for (long t = end - 1; t >= t0; --t) {
-        const bool start = starts(A, me.b, t);
-        float a, i;
-        gates((float)f[t * A.f_ts], a, i);
-        pp = start ? 0.f : a * ((float)dh[t * A.dh_ts] + pp);
-        pa *= a;
-        cut |= start;
+    unsigned cut = 0;
+    for (long t = t0 + (end - t0 - 1) / N * N; t >= t0; t -= N) {
+        E fv[N], gv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(gv, dh, A.dh_ts, t, end);
+        const unsigned flags = flags_of<N>(A, me.b, t, end);
+        cut |= flags;
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) {
+            if (t + j >= end) continue;
+            float a, i;
+            gates((float)fv[j], a, i);
+            pp = flags >> j & 1 ? 0.f : a * ((float)gv[j] + pp);
+            pa *= a;
+        }
     }
     const long at = (me.b * A.ranges + me.z) * A.C + me.c;
     A.totals[at] = cut ? -1.f : pa;
@@ -970,7 +1014,7 @@ template <bool FORWARD> __global__ __launch_bounds__(64) void k_narrow_join(floa
     }
 }
 
-template <class E> __global__ __launch_bounds__(256) void k_narrow(ScanArgs A)
+template <class E, int N> __global__ __launch_bounds__(256) void k_narrow(ScanArgs A)
 {
     const Thread me(A.B, A.ranges, A.C);
     if (me.none) return;
@@ -979,30 +1023,25 @@ template <class E> __global__ __launch_bounds__(256) void k_narrow(ScanArgs A)
     E *h = (E *)A.h + me.b * A.h_bs + me.c;
     float s = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.h0 ? A.h0[state] : 0.f;
     float *carry = A.carry ? A.carry + (me.b * A.tiles + t0 / LINE) * A.C + me.c : nullptr;
-    for (long t = t0; t < end; t += LINE) {
-        if (carry) { *carry = s; carry += A.C; }
-        E fv[LINE], xv[LINE];
-        bool cut[LINE];
+    for (long t = t0; t < end; t += N) {
+        E fv[N], xv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(xv, x, A.x_ts, t, end);
+        const unsigned flags = flags_of<N>(A, me.b, t, end);
 #pragma unroll
-        for (int j = 0; j < LINE; ++j) {   // all loads before the first store
-            const long u = min(t + j, end - 1);
-            fv[j] = f[u * A.f_ts];
-            xv[j] = x[u * A.x_ts];
-            cut[j] = starts(A, me.b, u);
-        }
-#pragma unroll
-        for (int j = 0; j < LINE; ++j) {
+        for (int j = 0; j < N; ++j) {
             if (t + j >= end) break;
+            if (j % LINE == 0 && carry) { *carry = s; carry += A.C; }
             float a, i;
             gates((float)fv[j], a, i);
-            s = fmaf(a, cut[j] ? 0.f : s, i * (float)xv[j]);
+            s = fmaf(a, flags >> j & 1 ? 0.f : s, i * (float)xv[j]);
             h[(t + j) * A.h_ts] = (E)s;
         }
     }
     if (A.h_last && end == A.T) A.h_last[state] = s;
 }
 
-template <class E> __global__ __launch_bounds__(256) void k_narrow_grad(ScanGradArgs A)
+template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_grad(ScanGradArgs A)
 {
     const Thread me(A.B, A.ranges, A.C);
     if (me.none) return;
@@ -1010,30 +1049,26 @@ template <class E> __global__ __launch_bounds__(256) void k_narrow_grad(ScanGrad
     const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
     E *df = (E *)A.df + me.b * A.df_bs + me.c, *dx = (E *)A.dx + me.b * A.dx_bs + me.c;
     float mu = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.dlast ? A.dlast[state] : 0.f;
-    const long last = t0 + (end - t0 - 1) / LINE * LINE;
-    for (long t = last; t >= t0; t -= LINE) {
-        float s = A.carry[(me.b * A.tiles + t / LINE) * A.C + me.c], before[LINE], ga[LINE], gi[LINE], xv[LINE], gv[LINE];
-        bool cut[LINE];
+    for (long t = t0 + (end - t0 - 1) / N * N; t >= t0; t -= N) {
+        float s = A.carry[(me.b * A.tiles + t / LINE) * A.C + me.c], before[N], ga[N], gi[N];
+        E fv[N], xv[N], gv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(xv, x, A.x_ts, t, end);
+        steps_of<N>(gv, dh, A.dh_ts, t, end);
+        const unsigned flags = flags_of<N>(A, me.b, t, end);
 #pragma unroll
-        for (int j = 0; j < LINE; ++j) {
-            const long u = min(t + j, end - 1);
-            cut[j] = starts(A, me.b, u);
-            xv[j] = (float)x[u * A.x_ts];
-            gv[j] = (float)dh[u * A.dh_ts];
-            gates((float)f[u * A.f_ts], ga[j], gi[j]);
+        for (int j = 0; j < N; ++j) {
+            gates((float)fv[j], ga[j], gi[j]);
+            before[j] = flags >> j & 1 ? 0.f : s;
+            s = fmaf(ga[j], before[j], gi[j] * (float)xv[j]);
         }
 #pragma unroll
-        for (int j = 0; j < LINE; ++j) {
-            before[j] = cut[j] ? 0.f : s;
-            s = fmaf(ga[j], before[j], gi[j] * xv[j]);
-        }
-#pragma unroll
-        for (int j = LINE - 1; j >= 0; --j) {
+        for (int j = N - 1; j >= 0; --j) {
             if (t + j >= end) continue;
-            const float l = gv[j] + mu, n = ga[j] * l;
+            const float l = (float)gv[j] + mu, n = ga[j] * l;
             dx[(t + j) * A.dx_ts] = (E)(gi[j] * l);
-            df[(t + j) * A.df_ts] = (E)(gi[j] * n * (before[j] - xv[j]));
-            mu = cut[j] ? 0.f : n;
+            df[(t + j) * A.df_ts] = (E)(gi[j] * n * (before[j] - (float)xv[j]));
+            mu = flags >> j & 1 ? 0.f : n;
         }
     }
     if (A.dh0 && me.z == 0) A.dh0[state] = mu;

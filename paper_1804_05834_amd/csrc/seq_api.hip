@@ -39,10 +39,13 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
 // below that ranges: as many waves as the card holds at four per SIMD, each with 32 steps at least.
-// Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 117 / 285, 932 / 1229; 300 x 2000 x 8: 22 / 40, 78 / 122;
-// 574 x 2844 x 17: 101 / 210, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Up to 160 steps the two further launches of
+// Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 139 / 179, 932 / 1229; 300 x 2000 x 8: 31 / 34, 78 / 122;
+// 574 x 2844 x 17: 125 / 160, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Up to 160 steps the two further launches of
 // ranges cost more than they give (2000 x 100 x 16: 29 / 51 in ranges, 16 / 26 without).
 constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
+// One or two channels: 32 steps of a thread at a time rather than 8 from this many elements on (83 x 95456 x 1: 139 / 179 us against
+// 166 / 400; 60 x 25811 x 1: 55 / 61 against 38 / 48).
+constexpr int64_t SCAN_LONG = 6 << 20;
 constexpr int64_t LAST_LEVEL = 256 << 20;   // bytes of the cache in front of memory
 constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
 
@@ -155,28 +158,28 @@ template <class E, int V> void launch_strips(const seq::ScanGradArgs &A, int wav
 {
     seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
 }
-template <class E> void launch_narrow(const seq::ScanArgs &A, hipStream_t st)
+template <class E, int N> void launch_narrow(const seq::ScanArgs &A, hipStream_t st)
 {
     const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
     if (A.ranges > 1) {
-        seq::k_narrow_maps<E><<<grid, 256, 0, st>>>(A);
+        seq::k_narrow_maps<E, N><<<grid, 256, 0, st>>>(A);
         seq::k_narrow_join<true><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.h0, A.B, A.ranges, A.C);
     }
-    seq::k_narrow<E><<<grid, 256, 0, st>>>(A);
+    seq::k_narrow<E, N><<<grid, 256, 0, st>>>(A);
 }
-template <class E> void launch_narrow(const seq::ScanGradArgs &A, hipStream_t st)
+template <class E, int N> void launch_narrow(const seq::ScanGradArgs &A, hipStream_t st)
 {
     const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
     if (A.ranges > 1) {
-        seq::k_narrow_grad_maps<E><<<grid, 256, 0, st>>>(A);
+        seq::k_narrow_grad_maps<E, N><<<grid, 256, 0, st>>>(A);
         seq::k_narrow_join<false><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.dlast, A.B, A.ranges, A.C);
     }
-    seq::k_narrow_grad<E><<<grid, 256, 0, st>>>(A);
+    seq::k_narrow_grad<E, N == 8 ? 8 : 16><<<grid, 256, 0, st>>>(A);
 }
 // fits(n): whether n channels can be taken at once
 template <class E, class Args, class F> void launch_recurrence(const Args &A, const ScanCut &c, F &&fits, hipStream_t st)
 {
-    if (c.form == ScanCut::NARROW) launch_narrow<E>(A, st);
+    if (c.form == ScanCut::NARROW) A.C <= 2 && A.T * A.B * A.C >= SCAN_LONG ? launch_narrow<E, 32>(A, st) : launch_narrow<E, 8>(A, st);
     else if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
     else if (c.form == ScanCut::STRIPS) fits(2) ? launch_strips<E, 2>(A, c.waves, st) : launch_strips<E, 1>(A, c.waves, st);
     else fits(2) ? launch_lines<E, 2>(A, st) : launch_lines<E, 1>(A, st);
