@@ -46,6 +46,7 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     # many sequences: strips of channels in one workgroup, and whole sequences per wave
     (300, 20, 64, "half", True, 0.05), (260, 150, 60, "plain", True, 0.02), (90, 300, 130, "odd", True, 0.01), (256, 129, 64, "time", False, 0.0), (64, 1030, 256, "half", True, 0.002),
     (1, 20000, 1, "plain", True, 0.0005), (5, 3001, 2, "odd", True, 0.001), (40, 700, 16, "time", False, 0.01), (3, 2500, 31, "half", True, 0.002),
+    (3000, 1100, 2, "half", True, 0.003), (6500, 1001, 1, "time", False, 0.003),      # more than six million elements of few channels
     (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
@@ -67,6 +68,8 @@ def scan_case(B, T, C, layout, state, chance, dtype, seed=0):
         f = f[:1].expand(B, T, C)
     h0 = rnd(seed + 2, B, C) if state else None
     reset = (torch.rand(B, T, generator=torch.Generator().manual_seed(seed + 3)) < chance).cuda() if chance else None
+    if layout == "time" and reset is not None:
+        reset = reset.t().contiguous().t()
     return f, x, h0, reset
 
 
