@@ -924,20 +924,19 @@ template <int N, class Args> __device__ __forceinline__ unsigned flags_of(const 
     return m;
 }
 
-template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_maps(ScanArgs A)
+// The map of steps t0 .. end - 1 of a channel, forward and backward.
+template <class E, int N> __device__ __forceinline__ void narrow_map(const ScanArgs &A, long b, int c, long t0, long end, float &pa, float &ph, bool &cut)
 {
-    const Thread me(A.B, A.ranges, A.C);
-    if (me.none) return;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
-    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c;
-    float pa = 1.f, ph = 0.f;
-    unsigned cut = 0;
+    const E *f = (const E *)A.f + b * A.f_bs + c, *x = (const E *)A.x + b * A.x_bs + c;
+    unsigned all = 0;
+    pa = 1.f;
+    ph = 0.f;
     for (long t = t0; t < end; t += N) {
         E fv[N], xv[N];
         steps_of<N>(fv, f, A.f_ts, t, end);
         steps_of<N>(xv, x, A.x_ts, t, end);
-        const unsigned flags = flags_of<N>(A, me.b, t, end);
-        cut |= flags;
+        const unsigned flags = flags_of<N>(A, b, t, end);
+        all |= flags;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             if (t + j >= end) break;
@@ -947,25 +946,20 @@ template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_maps(S
             pa *= a;
         }
     }
-    const long at = (me.b * A.ranges + me.z) * A.C + me.c;
-    A.totals[at] = cut ? -1.f : pa;
-    A.totals[(long)A.B * A.ranges * A.C + at] = ph;
+    cut = all;
 }
-
-template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_grad_maps(ScanGradArgs A)
+template <class E, int N> __device__ __forceinline__ void narrow_map(const ScanGradArgs &A, long b, int c, long t0, long end, float &pa, float &pp, bool &cut)
 {
-    const Thread me(A.B, A.ranges, A.C);
-    if (me.none) return;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
-    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
-    float pa = 1.f, pp = 0.f;
-    unsigned cut = 0;
+    const E *f = (const E *)A.f + b * A.f_bs + c, *dh = (const E *)A.dh + b * A.dh_bs + c;
+    unsigned all = 0;
+    pa = 1.f;
+    pp = 0.f;
     for (long t = t0 + (end - t0 - 1) / N * N; t >= t0; t -= N) {
         E fv[N], gv[N];
         steps_of<N>(fv, f, A.f_ts, t, end);
         steps_of<N>(gv, dh, A.dh_ts, t, end);
-        const unsigned flags = flags_of<N>(A, me.b, t, end);
-        cut |= flags;
+        const unsigned flags = flags_of<N>(A, b, t, end);
+        all |= flags;
 #pragma unroll
         for (int j = N - 1; j >= 0; --j) {
             if (t + j >= end) continue;
@@ -975,9 +969,113 @@ template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_grad_m
             pa *= a;
         }
     }
-    const long at = (me.b * A.ranges + me.z) * A.C + me.c;
-    A.totals[at] = cut ? -1.f : pa;
-    A.totals[(long)A.B * A.ranges * A.C + at] = pp;
+    cut = all;
+}
+
+// The steps themselves, from the state s that enters them; t0 is a multiple of LINE.  s: the state after them.
+template <class E, int N> __device__ __forceinline__ void narrow_run(const ScanArgs &A, long b, int c, long t0, long end, float &s)
+{
+    const E *f = (const E *)A.f + b * A.f_bs + c, *x = (const E *)A.x + b * A.x_bs + c;
+    E *h = (E *)A.h + b * A.h_bs + c;
+    float *carry = A.carry ? A.carry + (b * A.tiles + t0 / LINE) * A.C + c : nullptr;
+    for (long t = t0; t < end; t += N) {
+        E fv[N], xv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(xv, x, A.x_ts, t, end);
+        const unsigned flags = flags_of<N>(A, b, t, end);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (t + j >= end) break;
+            if (j % LINE == 0 && carry) { *carry = s; carry += A.C; }
+            float a, i;
+            gates((float)fv[j], a, i);
+            s = fmaf(a, flags >> j & 1 ? 0.f : s, i * (float)xv[j]);
+            h[(t + j) * A.h_ts] = (E)s;
+        }
+    }
+}
+template <class E, int N> __device__ __forceinline__ void narrow_run(const ScanGradArgs &A, long b, int c, long t0, long end, float &mu)
+{
+    const E *f = (const E *)A.f + b * A.f_bs + c, *x = (const E *)A.x + b * A.x_bs + c, *dh = (const E *)A.dh + b * A.dh_bs + c;
+    E *df = (E *)A.df + b * A.df_bs + c, *dx = (E *)A.dx + b * A.dx_bs + c;
+    for (long t = t0 + (end - t0 - 1) / N * N; t >= t0; t -= N) {
+        float s = A.carry[(b * A.tiles + t / LINE) * A.C + c], before[N], ga[N], gi[N];
+        E fv[N], xv[N], gv[N];
+        steps_of<N>(fv, f, A.f_ts, t, end);
+        steps_of<N>(xv, x, A.x_ts, t, end);
+        steps_of<N>(gv, dh, A.dh_ts, t, end);
+        const unsigned flags = flags_of<N>(A, b, t, end);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            gates((float)fv[j], ga[j], gi[j]);
+            before[j] = flags >> j & 1 ? 0.f : s;
+            s = fmaf(ga[j], before[j], gi[j] * (float)xv[j]);
+        }
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) {
+            if (t + j >= end) continue;
+            const float l = (float)gv[j] + mu, n = ga[j] * l;
+            dx[(t + j) * A.dx_ts] = (E)(gi[j] * l);
+            df[(t + j) * A.df_ts] = (E)(gi[j] * n * (before[j] - (float)xv[j]));
+            mu = flags >> j & 1 ? 0.f : n;
+        }
+    }
+}
+// what enters a sequence and where what leaves it goes
+__host__ __device__ __forceinline__ const float *entering(const ScanArgs &A) { return A.h0; }
+__host__ __device__ __forceinline__ const float *entering(const ScanGradArgs &A) { return A.dlast; }
+__device__ __forceinline__ float *leaving(const ScanArgs &A) { return A.h_last; }
+__device__ __forceinline__ float *leaving(const ScanGradArgs &A) { return A.dh0; }
+
+// A workgroup takes a sequence of up to NARROW_BLOCK elements: a thread a channel and a run of steps, maps joined in LDS, the
+// second reading from the caches.  One launch where ranges take three, and its lines are read by one unit.  us forward /
+// backward here against ranges, B x T x C in bf16: 32 x 333 x 3: 8 / 10, 25 / 31; 300 x 250 x 16: 11 / 19, 22 / 25; 300 x 4000 x 1: 21 / 33,
+// 34 / 45; past its limit one workgroup a sequence is too few: 32 x 16000 x 1: 39 / 62, 33 / 42; 32 x 4062 x 16: 37 / 67, 23 / 27.
+constexpr int NARROW_BLOCK = 8192;
+template <class Args> constexpr int BLOCK_THREADS = std::is_same<Args, ScanArgs>::value ? 1024 : 512;   // as many as have registers
+template <class E, class Args> __global__ __launch_bounds__(BLOCK_THREADS<Args>) void k_narrow_block(Args A)
+{
+    constexpr bool FORWARD = std::is_same<Args, ScanArgs>::value;
+    __shared__ float sa[BLOCK_THREADS<Args>], sh[BLOCK_THREADS<Args>];
+    const int c = threadIdx.x % A.C, runs = blockDim.x / A.C, run = threadIdx.x / A.C, order = FORWARD ? run : runs - 1 - run;
+    const long b = blockIdx.x, range = ((A.T + runs - 1) / runs + LINE - 1) / LINE * LINE, t0 = min(A.T, run * range), end = min(A.T, t0 + range);
+    const bool mine = run < runs;
+    const int at = order * A.C + c;   // place of this run's map among those of its channel
+    float a = 1.f, h = 0.f;
+    bool cut = false;
+    if (mine && t0 < end) narrow_map<E, 8>(A, b, c, t0, end, a, h, cut);
+    if (cut) a = -1.f;
+    for (int d = 1; d < runs; d *= 2) {   // maps of all runs up to this one
+        if (mine) { sa[at] = a; sh[at] = h; }
+        __syncthreads();
+        if (mine && order >= d) {
+            const float oa = sa[at - d * A.C], oh = sh[at - d * A.C];
+            h = through(oh, a, h, a < 0.f);
+            a = a < 0.f || oa < 0.f ? -1.f : a * oa;
+        }
+        __syncthreads();
+    }
+    if (mine) { sa[at] = a; sh[at] = h; }
+    __syncthreads();
+    if (!mine) return;
+    const float *first = entering(A);
+    float s = first ? first[b * A.C + c] : 0.f;
+    if (order) s = through(s, sa[at - A.C], sh[at - A.C], sa[at - A.C] < 0.f);
+    if (t0 < end) narrow_run<E, 8>(A, b, c, t0, end, s);
+    float *last = leaving(A);
+    if (last && order == runs - 1) last[b * A.C + c] = s;
+}
+
+template <class E, int N, class Args> __global__ __launch_bounds__(256) void k_narrow_maps(Args A)
+{
+    const Thread me(A.B, A.ranges, A.C);
+    if (me.none) return;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range), at = (me.b * A.ranges + me.z) * A.C + me.c;
+    float a, h;
+    bool cut;
+    narrow_map<E, N>(A, me.b, me.c, t0, end, a, h, cut);
+    A.totals[at] = cut ? -1.f : a;
+    A.totals[(long)A.B * A.ranges * A.C + at] = h;
 }
 
 // One wave per channel of a sequence: lane l has the ranges from ranges l / 64 on (backward: from the other end).  `first`
@@ -1014,64 +1112,17 @@ template <bool FORWARD> __global__ __launch_bounds__(64) void k_narrow_join(floa
     }
 }
 
-template <class E, int N> __global__ __launch_bounds__(256) void k_narrow(ScanArgs A)
+template <class E, int N, class Args> __global__ __launch_bounds__(256) void k_narrow(Args A)
 {
+    constexpr bool FORWARD = std::is_same<Args, ScanArgs>::value;
     const Thread me(A.B, A.ranges, A.C);
     if (me.none) return;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range), state = me.b * A.C + me.c;
-    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c;
-    E *h = (E *)A.h + me.b * A.h_bs + me.c;
-    float s = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.h0 ? A.h0[state] : 0.f;
-    float *carry = A.carry ? A.carry + (me.b * A.tiles + t0 / LINE) * A.C + me.c : nullptr;
-    for (long t = t0; t < end; t += N) {
-        E fv[N], xv[N];
-        steps_of<N>(fv, f, A.f_ts, t, end);
-        steps_of<N>(xv, x, A.x_ts, t, end);
-        const unsigned flags = flags_of<N>(A, me.b, t, end);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            if (t + j >= end) break;
-            if (j % LINE == 0 && carry) { *carry = s; carry += A.C; }
-            float a, i;
-            gates((float)fv[j], a, i);
-            s = fmaf(a, flags >> j & 1 ? 0.f : s, i * (float)xv[j]);
-            h[(t + j) * A.h_ts] = (E)s;
-        }
-    }
-    if (A.h_last && end == A.T) A.h_last[state] = s;
-}
-
-template <class E, int N> __global__ __launch_bounds__(256) void k_narrow_grad(ScanGradArgs A)
-{
-    const Thread me(A.B, A.ranges, A.C);
-    if (me.none) return;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range), state = me.b * A.C + me.c;
-    const E *f = (const E *)A.f + me.b * A.f_bs + me.c, *x = (const E *)A.x + me.b * A.x_bs + me.c, *dh = (const E *)A.dh + me.b * A.dh_bs + me.c;
-    E *df = (E *)A.df + me.b * A.df_bs + me.c, *dx = (E *)A.dx + me.b * A.dx_bs + me.c;
-    float mu = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : A.dlast ? A.dlast[state] : 0.f;
-    for (long t = t0 + (end - t0 - 1) / N * N; t >= t0; t -= N) {
-        float s = A.carry[(me.b * A.tiles + t / LINE) * A.C + me.c], before[N], ga[N], gi[N];
-        E fv[N], xv[N], gv[N];
-        steps_of<N>(fv, f, A.f_ts, t, end);
-        steps_of<N>(xv, x, A.x_ts, t, end);
-        steps_of<N>(gv, dh, A.dh_ts, t, end);
-        const unsigned flags = flags_of<N>(A, me.b, t, end);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            gates((float)fv[j], ga[j], gi[j]);
-            before[j] = flags >> j & 1 ? 0.f : s;
-            s = fmaf(ga[j], before[j], gi[j] * (float)xv[j]);
-        }
-#pragma unroll
-        for (int j = N - 1; j >= 0; --j) {
-            if (t + j >= end) continue;
-            const float l = (float)gv[j] + mu, n = ga[j] * l;
-            dx[(t + j) * A.dx_ts] = (E)(gi[j] * l);
-            df[(t + j) * A.df_ts] = (E)(gi[j] * n * (before[j] - (float)xv[j]));
-            mu = flags >> j & 1 ? 0.f : n;
-        }
-    }
-    if (A.dh0 && me.z == 0) A.dh0[state] = mu;
+    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
+    const float *first = entering(A);
+    float s = A.ranges > 1 ? A.totals[((long)A.B + me.b) * A.ranges * A.C + (long)me.z * A.C + me.c] : first ? first[me.b * A.C + me.c] : 0.f;
+    narrow_run<E, N>(A, me.b, me.c, t0, end, s);
+    float *last = leaving(A);
+    if (last && (FORWARD ? end == A.T : me.z == 0)) last[me.b * A.C + me.c] = s;
 }
 
 }  // namespace seq

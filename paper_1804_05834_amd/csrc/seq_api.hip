@@ -40,8 +40,7 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
 // below that ranges: as many waves as the card holds at four per SIMD, each with 32 steps at least.
 // Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 139 / 179, 932 / 1229; 300 x 2000 x 8: 31 / 34, 78 / 122;
-// 574 x 2844 x 17: 125 / 160, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Up to 160 steps the two further launches of
-// ranges cost more than they give (2000 x 100 x 16: 29 / 51 in ranges, 16 / 26 without).
+// 574 x 2844 x 17: 125 / 160, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Short ones of them a workgroup each (see there).
 constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
 // One or two channels: 32 steps of a thread at a time rather than 8 from this many elements on (83 x 95456 x 1: 139 / 179 us against
 // 166 / 400; 60 x 25811 x 1: 55 / 61 against 38 / 48).
@@ -77,7 +76,7 @@ const char *check_scan(const dqn_scan_args &s)
 
 // How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
 struct ScanCut {
-    enum { SHORT, NARROW, STRIPS, LINES } form;
+    enum { SHORT, BLOCK, NARROW, STRIPS, LINES } form;
     int waves;         // of a workgroup of the strips
     long tile, tiles;  // steps between two states of `carry`, states of a sequence
     long range;        // lines: steps of a range
@@ -87,7 +86,8 @@ ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 {
     if (T <= seq::SCAN_SHORT) return ScanCut{ScanCut::SHORT, 0, seq::SCAN_SHORT, T ? 1 : 0, (long)T, 1};
     if (C <= 16 || (C <= 32 && T > 1000)) {
-        const int64_t all = std::max<int64_t>(1, (int64_t)B * C), want = T <= 160 ? 1 : std::max<int64_t>(1, std::min<int64_t>(SCAN_WANT * 64 / all, T / SCAN_LEAST));
+        if (C && T * C <= seq::NARROW_BLOCK) return ScanCut{ScanCut::BLOCK, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), (long)T, 1};
+        const int64_t all = std::max<int64_t>(1, (int64_t)B * C), want = std::max<int64_t>(1, std::min<int64_t>(SCAN_WANT * 64 / all, T / SCAN_LEAST));
         const long per = (T + want - 1) / want, range = (per + seq::LINE - 1) / seq::LINE * seq::LINE;
         return ScanCut{ScanCut::NARROW, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), range, (int)((T + range - 1) / range)};
     }
@@ -158,28 +158,26 @@ template <class E, int V> void launch_strips(const seq::ScanGradArgs &A, int wav
 {
     seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
 }
-template <class E, int N> void launch_narrow(const seq::ScanArgs &A, hipStream_t st)
+template <class E, int N, class Args> void launch_narrow(const Args &A, hipStream_t st)
 {
+    constexpr bool FORWARD = std::is_same<Args, seq::ScanArgs>::value;
     const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
     if (A.ranges > 1) {
-        seq::k_narrow_maps<E, N><<<grid, 256, 0, st>>>(A);
-        seq::k_narrow_join<true><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.h0, A.B, A.ranges, A.C);
+        seq::k_narrow_maps<E, N, Args><<<grid, 256, 0, st>>>(A);
+        seq::k_narrow_join<FORWARD><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, seq::entering(A), A.B, A.ranges, A.C);
     }
-    seq::k_narrow<E, N><<<grid, 256, 0, st>>>(A);
+    seq::k_narrow<E, FORWARD ? N : std::min(N, 16), Args><<<grid, 256, 0, st>>>(A);
 }
-template <class E, int N> void launch_narrow(const seq::ScanGradArgs &A, hipStream_t st)
+template <class E, class Args> void launch_block(const Args &A, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((int64_t)A.B * A.ranges * A.C + 255) / 256));
-    if (A.ranges > 1) {
-        seq::k_narrow_grad_maps<E, N><<<grid, 256, 0, st>>>(A);
-        seq::k_narrow_join<false><<<dim3((unsigned)(A.B * A.C)), 64, 0, st>>>(A.totals, A.dlast, A.B, A.ranges, A.C);
-    }
-    seq::k_narrow_grad<E, N == 8 ? 8 : 16><<<grid, 256, 0, st>>>(A);
+    const int64_t threads = std::min<int64_t>(seq::BLOCK_THREADS<Args>, A.tiles * A.C);   // 8 steps each, or more
+    seq::k_narrow_block<E, Args><<<dim3((unsigned)A.B), (unsigned)((threads + 63) / 64 * 64), 0, st>>>(A);
 }
 // fits(n): whether n channels can be taken at once
 template <class E, class Args, class F> void launch_recurrence(const Args &A, const ScanCut &c, F &&fits, hipStream_t st)
 {
     if (c.form == ScanCut::NARROW) A.C <= 2 && A.T * A.B * A.C >= SCAN_LONG ? launch_narrow<E, 32>(A, st) : launch_narrow<E, 8>(A, st);
+    else if (c.form == ScanCut::BLOCK) launch_block<E>(A, st);
     else if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
     else if (c.form == ScanCut::STRIPS) fits(2) ? launch_strips<E, 2>(A, c.waves, st) : launch_strips<E, 1>(A, c.waves, st);
     else fits(2) ? launch_lines<E, 2>(A, st) : launch_lines<E, 1>(A, st);

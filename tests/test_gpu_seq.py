@@ -47,6 +47,9 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     (300, 20, 64, "half", True, 0.05), (260, 150, 60, "plain", True, 0.02), (90, 300, 130, "odd", True, 0.01), (256, 129, 64, "time", False, 0.0), (64, 1030, 256, "half", True, 0.002),
     (1, 20000, 1, "plain", True, 0.0005), (5, 3001, 2, "odd", True, 0.001), (40, 700, 16, "time", False, 0.01), (3, 2500, 31, "half", True, 0.002),
     (3000, 1100, 2, "half", True, 0.003), (6500, 1001, 1, "time", False, 0.003),      # more than six million elements of few channels
+    # few channels: more than six million elements in long sequences, whole sequences per thread, and either side of a workgroup each
+    (700, 9001, 1, "half", True, 0.001), (780, 4111, 2, "time", True, 0.003), (8200, 515, 16, "plain", True, 0.003),
+    (9, 512, 16, "odd", True, 0.01), (9, 513, 16, "half", True, 0.01), (30, 2730, 3, "time", True, 0.001), (4, 1025, 8, "broadcast", True, 0.5),
     (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
