@@ -353,7 +353,8 @@ enum { DQN_F32 = 0, DQN_BF16 = 1 };
  * step of an acting agent; h_last may be h0 then, and for any T. */
 typedef struct {
     int32_t dtype;                      /* DQN_F32 / DQN_BF16, of f, x, h           */
-    int32_t B, C;                       /* sequences 0..65535, channels 0..2^24     */
+    int32_t B, C;                       /* sequences 0..65535, channels 0..2^24, the
+                                           product of both at most 2^28             */
     int64_t T;                          /* steps, >= 0 (0: h_last = h0)             */
     const void *f, *x;                  /* [B][T][C]                                */
     int64_t f_bs, f_ts, x_bs, x_ts;     /* strides of a sequence and of a step; that

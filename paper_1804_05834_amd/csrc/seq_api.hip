@@ -67,7 +67,8 @@ const char *check_steps(const void *p, int64_t bs, int64_t ts, const dqn_scan_ar
 const char *check_scan(const dqn_scan_args &s)
 {
     if (!dtype_ok(s.dtype)) return "dtype must be DQN_F32 or DQN_BF16";
-    if (s.B < 0 || s.C < 0 || s.T < 0 || s.B > 65535 || s.C > 1 << 24 || !size_ok(s.B, s.T, s.C)) return "B must be in 0..65535, C in 0..2^24, T >= 0";
+    if (s.B < 0 || s.C < 0 || s.T < 0 || s.B > 65535 || s.C > 1 << 24 || (int64_t)s.B * s.C > 1 << 28 || !size_ok(s.B, s.T, s.C))
+        return "B must be in 0..65535, C in 0..2^24, B C in 0..2^28, T >= 0";
     if (!at(s.h0, 4) || !at(s.h_last, 4) || !at(s.carry, 4)) return "a state is not aligned to its elements";
     if (s.reset && (s.reset_bs < 0 || s.reset_ts < 0 || s.reset_bs > MOST || s.reset_ts > MOST ||
                     (s.reset_ts > 0 && s.T - 1 > MOST / s.reset_ts))) return "a stride of reset is negative or too large";

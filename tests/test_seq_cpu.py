@@ -177,3 +177,12 @@ def test_random_rounding_keeps_the_mean_and_the_draws_are_the_librarys():
     rest = np.arange(v.size) % 256 != 0
     assert abs((qm * np.repeat(sm, 256))[rest].mean() / 0.3 - 1) < 1e-3 and abs((qv * np.repeat(sv, 256))[rest].mean() / 0.3 - 1) < 1e-3
     assert (qm[~rest] == 448).all() and (qv[~rest] == 57344).all()
+
+
+def test_scan_refuses_more_states_than_a_launch_has_threads_for(lib):
+    a, b = C.c_size_t(), C.c_size_t()
+    for B, c in ((65535, 4097), (17, 1 << 24), (4097, 65536)):
+        for T in (1, 9, 100, 5000):
+            assert lib.dqn_scan_sizes(0, B, T, c, C.byref(a), C.byref(b)) == dqn.ERR_INVALID_ARG and "2^28" in said(lib)
+    for B, c in ((65535, 4096), (16, 1 << 24), (4096, 65536)):
+        assert lib.dqn_scan_sizes(0, B, 100, c, C.byref(a), C.byref(b)) == dqn.OK
