@@ -29,6 +29,8 @@ struct ScanArgs {
     long range;      // lines: steps of a range, ranges, and their maps (see there)
     int ranges;
     float *totals;
+    bool apart;      // lines: no wave may hold parts of two ranges
+    bool torn;       // rows are not aligned to the caches' lines
 };
 struct ScanGradArgs {
     const void *f, *x, *dh;
@@ -45,6 +47,8 @@ struct ScanGradArgs {
     long range;
     int ranges;
     float *totals;
+    bool apart;      // lines: no wave may hold parts of two ranges
+    bool torn;       // rows are not aligned to the caches' lines
 };
 
 constexpr int SCAN_RUN = 16;        // elements of a thread in a tile: 8 steps of 2 channels or 16 steps of one
@@ -70,13 +74,31 @@ template <int V> struct Lane {
     __device__ Lane(int first, int C) : c(min(first, C - V)), live(first < C) {}
 };
 
-template <int V> __device__ __forceinline__ void state(const float *p, float (&s)[V])
-{
-    const auto v = load<V>(p);
-#pragma unroll
-    for (int k = 0; k < V; ++k) s[k] = v[k];
-}
-template <int V> __device__ __forceinline__ void keep_state(float *p, const float (&s)[V]) { store<V>(p, narrow<float, V>(s)); }
+// a state of V channels, at any address of a float
+// Which of `all` items (a sequence or a group of ranges) and which strip of its channels a workgroup has.  Workgroups with the same
+// id modulo 8 share a cache.  Where rows are torn, that is where strips have lines of memory in common, those of an item
+// share a cache (7 x 4099 x 261 in fp32 with gradients: 101 -> 93 us); else they are dealt out in turn (131072 x 512 in bf16:
+// 127 -> 123 us).
+struct Dealt {
+    unsigned item;
+    int strip;
+    __device__ __forceinline__ Dealt(unsigned strips, unsigned all, bool torn)
+    {
+        const unsigned even = torn ? all / 8 * 8 : 0;   // the others do not make eight
+        if (blockIdx.x < even * strips) {
+            const unsigned k = blockIdx.x / 8;
+            item = k / strips * 8 + blockIdx.x % 8;
+            strip = k % strips;
+        } else {
+            const unsigned k = blockIdx.x - even * strips;
+            item = even + k / strips;
+            strip = k % strips;
+        }
+    }
+};
+
+template <int V> __device__ __forceinline__ void state(const float *p, float (&s)[V]) { __builtin_memcpy(s, p, sizeof(s)); }
+template <int V> __device__ __forceinline__ void keep_state(float *p, const float (&s)[V]) { __builtin_memcpy(p, s, sizeof(s)); }
 
 // ------------------------------------------------------------ short sequences
 __device__ __forceinline__ long sequence_of(long id, long all, int per)   // id / per; in 32 bits where that is enough
@@ -300,8 +322,9 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
     __shared__ __attribute__((aligned(16))) float tot[2][2][SCAN_WAVES][SCAN_STRIP];
     __shared__ unsigned cuts[2][SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, g = lane % G, tile = W * S * L;
-    const Lane<V> me(blockIdx.x * SCAN_STRIP + g * V, A.C);
-    const long b = blockIdx.y, end = A.T, at = b * A.C + me.c;
+    const Dealt to((A.C + SCAN_STRIP - 1) / SCAN_STRIP, A.B, A.torn);
+    const Lane<V> me(to.strip * SCAN_STRIP + g * V, A.C);
+    const long b = to.item, end = A.T, at = b * A.C + me.c;
     const E *f = (const E *)A.f + b * A.f_bs, *x = (const E *)A.x + b * A.x_bs;
     E *hs = (E *)A.h + b * A.h_bs;
     const uint8_t *reset = A.reset ? A.reset + b * A.r_bs : nullptr;
@@ -390,8 +413,9 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
     __shared__ __attribute__((aligned(16))) float tot[2][3][SCAN_WAVES][SCAN_STRIP];   // A, P and H of the waves
     __shared__ unsigned cuts[2][SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, g = lane % G, tile = W * S * L;
-    const Lane<V> me(blockIdx.x * SCAN_STRIP + g * V, A.C);
-    const long b = blockIdx.y, end = A.T, at = b * A.C + me.c;
+    const Dealt to((A.C + SCAN_STRIP - 1) / SCAN_STRIP, A.B, A.torn);
+    const Lane<V> me(to.strip * SCAN_STRIP + g * V, A.C);
+    const long b = to.item, end = A.T, at = b * A.C + me.c;
     const E *f = (const E *)A.f + b * A.f_bs, *x = (const E *)A.x + b * A.x_bs, *dh = (const E *)A.dh + b * A.dh_bs;
     E *dfs = (E *)A.df + b * A.df_bs, *dxs = (E *)A.dx + b * A.dx_bs;
     const uint8_t *reset = A.reset ? A.reset + b * A.r_bs : nullptr;
@@ -507,343 +531,442 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
 }
 
 // ------------------------------------------------------------ lines
-// A wave goes through a range of steps of 64 V channels, step after step, LINE steps' loads ahead: no work but the
+// A lane takes two channels through a range of steps, step after step, LINE steps' loads ahead: no work but the
 // recurrence itself (fourteen vector instructions per element, where a strip takes twenty).  With enough sequences
-// and channels a wave takes a whole sequence.  Else time is cut into ranges, and the state that enters one is not known yet:
+// and channels a wave takes whole sequences.  Else time is cut into ranges, and the state that enters one is not known yet:
 // a first launch finds the map of every range, a second composes the maps of those before and then runs.  f and x
 // are read twice then, which long sequences of few channels have to: the other way would be to wait for the
 // workgroup before, a thousand times in turn.
 //
-// Eight waves, eight ranges of a sequence in turn, are a workgroup and a group: maps are kept of ranges and of groups, and
-// a workgroup composes the groups before it with all of its waves.
+// LINE_GROUP ranges of a sequence in turn are a group: maps are kept of ranges and of groups, and a group's lanes compose the
+// groups before it among them.  A group's strip of 64 pairs of channels is a workgroup and a range of it a wave.  In a strip that is
+// half as wide, or less, the lanes of the group's ranges follow one another, so that a wave holds parts of several
+// (100 sequences of 900 steps of 64 channels in bf16: 18 us forward, 22 backward; a wave a range: 26 and 40).
+// Channels are taken in pairs at any alignment: what the first pair of a row begins with need not be aligned to two elements,
+// and of an odd number of channels the last lane has the last two but stores the last alone (`half`).
 //
 // Measured: 512 sequences of 64 steps of 512 channels in bf16, a wave each, 18 us forward (5.6 TB/s), 36 backward (4.7); one
 // sequence of 131072 steps of 512 channels, in ranges, 57 for the maps (4.7 TB/s) and 67 for the states (6.0).
 constexpr int LINE = 8;         // steps between two states of `carry`, and of a wave's loads
-constexpr int LINE_WAVES = 8;   // waves of a workgroup
+constexpr int LINE_GROUP = 8;   // ranges of a workgroup; waves of one whose waves take whole sequences
+
+// V values that lie at any address of a float
+__device__ __forceinline__ void pair(const float *p, float (&s)[2]) { __builtin_memcpy(s, p, 8); }
+__device__ __forceinline__ void keep_pair(float *p, const float (&s)[2], bool half)
+{
+    if (half) p[1] = s[1];
+    else __builtin_memcpy(p, s, 8);
+}
 
 // Maps in memory: [B][ranges + groups][2][C], A (-1: an episode starts there) and H of each range, then of each group.  A map
 // is made and composed in registers as (a, h).  The last range's map (forward; backward the first's) is not needed.
 // Forward, range 0 runs from h0 on and counts as the start of an episode, and a copy of h0 stands in place of the last
 // range's A: the last range may write h_last where h0 was before the first has read it.
-template <int V> struct Map {
-    float a[V], h[V];
+struct Map {
+    float a[2] = {1.f, 1.f}, h[2] = {};
     bool cut = false;
-    __device__ __forceinline__ Map()
+    __device__ __forceinline__ void put(float *p, int C, bool half) const
     {
-#pragma unroll
-        for (int k = 0; k < V; ++k) { a[k] = 1.f; h[k] = 0.f; }
+        const float m[2] = {cut ? -1.f : a[0], cut ? -1.f : a[1]};
+        keep_pair(p, m, half);
+        keep_pair(p + C, h, half);
     }
-    __device__ __forceinline__ void put(float *p, int C) const
+    // this map, then (pa, ph) if `there`
+    __device__ __forceinline__ void then(const float (&pa)[2], const float (&ph)[2], bool there)
     {
-        float m[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) m[k] = cut ? -1.f : a[k];
-        keep_state<V>(p, m);
-        keep_state<V>(p + C, h);
+        for (int k = 0; k < 2; ++k) {
+            const float nh = through(h[k], pa[k], ph[k], pa[k] < 0.f), na = pa[k] < 0.f || a[k] < 0.f ? -1.f : a[k] * pa[k];
+            h[k] = there ? nh : h[k];
+            a[k] = there ? na : a[k];
+        }
     }
     // this map, then the one at p
     __device__ __forceinline__ void then(const float *p, int C)
     {
-        const auto pa = load<V>(p), ph = load<V>(p + C);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            h[k] = through(h[k], pa[k], ph[k], pa[k] < 0.f);
-            a[k] = pa[k] < 0.f || a[k] < 0.f ? -1.f : a[k] * pa[k];
-        }
+        float pa[2], ph[2];
+        pair(p, pa);
+        pair(p + C, ph);
+        then(pa, ph, true);
     }
-    __device__ __forceinline__ void apply(float (&s)[V]) const
+    __device__ __forceinline__ void apply(float (&s)[2]) const
     {
 #pragma unroll
-        for (int k = 0; k < V; ++k) s[k] = through(s[k], a[k], h[k], a[k] < 0.f);
+        for (int k = 0; k < 2; ++k) s[k] = through(s[k], a[k], h[k], a[k] < 0.f);
     }
 };
 
-// Where a wave stands.
-template <int V> struct Line {
-    int strip, c, z, group, groups;
-    long b;
-    bool live, idle;   // idle: nothing to do, but the workgroup's barriers
-    __device__ __forceinline__ Line(int B, int C, int ranges)
+// lanes of a strip of so many pairs of channels: a power of two, so that the parts of rows that a wave has are not cut anew
+__host__ __device__ __forceinline__ int line_width(int pairs)
+{
+    int width = 64;
+    while (width / 2 >= pairs) width /= 2;
+    return width;
+}
+
+// Where a lane stands.
+struct Line {
+    int c, lane, q, z;          // its channels; in ranges: place in the strip, range in the group and in the sequence
+    int z0, z1, group, groups;  // first and last range of the wave, the workgroup's group, all groups
+    int width;                  // lanes of the strip
+    long b, range;
+    bool live, half, idle;      // idle: the wave has nothing to do, but the workgroup's barriers
+    bool halves;                // a lane of the wave is half
+    __device__ __forceinline__ Line(int B, int C, int ranges, long range, bool apart, bool torn) : range(range)
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), strips = (C + 64 * V - 1) / (64 * V);
-        groups = (ranges + LINE_WAVES - 1) / LINE_WAVES;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        groups = (ranges + LINE_GROUP - 1) / LINE_GROUP;
+        const int pairs = (C + 1) / 2, strips = (pairs + 63) / 64;
+        int first;
         if (ranges == 1) {   // a wave per strip
-            const long id = (long)blockIdx.x * LINE_WAVES + wave;
+            const long id = (long)blockIdx.x * LINE_GROUP + wave;
             b = id / strips;
-            strip = (int)(id - b * strips);
-            z = group = 0;
+            lane = threadIdx.x & 63;
+            first = ((int)(id - b * strips) * 64 + lane) * 2;
+            q = z = z0 = z1 = group = 0;
+            width = 64;
             idle = b >= B;
+            live = first < C && !idle;
         } else {             // a workgroup per strip and group
-            const unsigned id = blockIdx.x / strips;
-            strip = blockIdx.x - id * strips;
+            const Dealt to(strips, (unsigned)B * groups, torn);
+            const unsigned id = to.item;
+            const int strip = to.strip;
             b = id / groups;
             group = id - (unsigned)b * groups;
-            z = group * LINE_WAVES + wave;
-            idle = z >= ranges;
+            width = apart ? 64 : line_width(pairs - strip * 64);
+            q = threadIdx.x / (unsigned)width;
+            lane = threadIdx.x % (unsigned)width;
+            first = (strip * 64 + lane) * 2;
+            z = group * LINE_GROUP + q;
+            z0 = __builtin_amdgcn_readfirstlane(z);
+            const int last = min((group + 1) * LINE_GROUP, ranges) - 1;
+            z1 = min(__builtin_amdgcn_readlane(z, 63), last);
+            idle = z0 > last;
+            live = z <= last && first < C;
         }
-        const int first = (strip * 64 + (threadIdx.x & 63)) * V;
-        live = first < C;
-        c = min(first, C - V);
+        c = min(first, C - 2);
+        half = live && first > c;
+        halves = __ballot(half) != 0;
+    }
+    // the lane's step when the wave's first one is at `t`
+    __device__ __forceinline__ long step(long t) const { return t + (z - z0) * range; }
+    // Its bytes from the wave's first row on.  The host sees to it that they fit.
+    __device__ __forceinline__ int place(long ts, int size) const { return (int)(((z - z0) * range * ts + c) * size); }
+    // whether LINE steps from the wave's step t on are there in all of its lanes
+    __device__ __forceinline__ bool whole(long t, long T) const { return t + (z1 - z0) * range + LINE <= T; }
+    // batches of LINE steps
+    __device__ __forceinline__ long batches(int ranges, long T) const
+    {
+        return ((z0 < ranges - 1 ? range : T - z0 * range) + LINE - 1) / LINE;
     }
 };
 
-// Rows t .. t + LINE - 1 of a tensor, and their reset flags
-template <class E, int V, int LOAD = 0> struct LineRows {
-    vec<E, V> v[LINE];
-    __device__ __forceinline__ void fetch(const E *p, long ts, long t, long end, int C, int place)
+// Rows t .. t + LINE - 1 of a tensor
+template <class E, int LOAD = 0> struct LineRows {
+    vec<E, 2> v[LINE];
+    __device__ __forceinline__ void fetch(const E *p, long ts, long t, long T, int C, int place, bool whole)
     {
-        const Window<E> w(p, ts, t, end, C);
-        if (t + LINE <= end) {
+        const Window<E> w(p, ts, t, T, C);
+        if (whole) {
 #pragma unroll
-            for (int j = 0; j < LINE; ++j) v[j] = w.template get<V, true, LOAD>(place, j);
+            for (int j = 0; j < LINE; ++j) v[j] = w.template get<2, true, LOAD>(place, j);
         } else {
 #pragma unroll
-            for (int j = 0; j < LINE; ++j) v[j] = w.template get<V, false, LOAD>(place, j);
+            for (int j = 0; j < LINE; ++j) v[j] = w.template get<2, false, LOAD>(place, j);
         }
     }
 };
-
-// The state that enters a wave's range: every wave composes a share of the groups on the way to it (`before` of them, from
-// `from` on in steps of `way`), then the ranges of the waves before it in the workgroup.
-template <int V, bool FORWARD> __device__ __forceinline__ void enter_range(float (&s)[V], const Line<V> &me, const float *maps, int ranges, int C)
+// A row's results; `one`: the place of a lane's second channel where that is stored alone, if a lane of the wave has such.
+template <bool FULL, class E> __device__ __forceinline__ void put_line(const Window<E> &w, int place, int one, bool halves, int j, const float (&v)[2])
 {
-    __shared__ float sh[2 * LINE_WAVES][2][64 * V];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int before = FORWARD ? me.group : me.groups - 1 - me.group, order = FORWARD ? wave : LINE_WAVES - 1 - wave;
-    const int lo = before * order / LINE_WAVES, hi = before * (order + 1) / LINE_WAVES;
-    Map<V> m;
-#pragma unroll 8
-    for (int q = lo; q < hi; ++q) m.then(maps + (long)(ranges + (FORWARD ? q : me.groups - 1 - q)) * 2 * C, C);
-    Map<V> own;
-    const bool have = !me.idle && me.z != (FORWARD ? ranges - 1 : 0);
-    if (have) own.then(maps + (long)me.z * 2 * C, C);
-    keep_state<V>(&sh[order][0][lane * V], m.a);
-    keep_state<V>(&sh[order][1][lane * V], m.h);
-    keep_state<V>(&sh[LINE_WAVES + order][0][lane * V], own.a);
-    keep_state<V>(&sh[LINE_WAVES + order][1][lane * V], own.h);
+    w.template put<2, FULL>(place, j, v);
+    if (halves) w.template put<1, FULL>(one, j, {v[1]});
+}
+
+// The reset flags of a wave's next LINE steps, lane l having step l % 8 of range z0 + l / 8.
+struct LineResets {
+    uint8_t v = 0;
+    __device__ __forceinline__ void fetch(const uint8_t *reset, long r_ts, long t, long T, const Line &me)
+    {
+        const int lane = threadIdx.x & 63, z = lane / LINE;
+        const long row = t + z * me.range + lane % LINE;
+        v = z <= me.z1 - me.z0 && row < T ? reset[row * r_ts] : 0;
+    }
+    __device__ __forceinline__ uint64_t flags() const { return __ballot(v != 0); }
+};
+__device__ __forceinline__ unsigned of_lane(uint64_t flags, const Line &me) { return (unsigned)(flags >> ((me.z - me.z0) * LINE & 63)) & ((1u << LINE) - 1); }
+
+// The state that enters a lane's range: the lanes of every range of the group compose a share of the groups on the way to it,
+// then the ranges before theirs in the workgroup.
+template <bool FORWARD> __device__ __forceinline__ void enter_range(float (&s)[2], const Line &me, const float *maps, int ranges, int C)
+{
+    __shared__ float sh[2 * LINE_GROUP * 2 * 128];   // [2 LINE_GROUP][2][the strip's channels]
+    const int row = me.width * 2, before = FORWARD ? me.group : me.groups - 1 - me.group;
+    float *at = sh + me.lane * 2;
+    const int order = me.q >= LINE_GROUP ? 0 : FORWARD ? me.q : LINE_GROUP - 1 - me.q;   // (lanes beyond the last range: any)
+    if (me.q < LINE_GROUP) {
+        const int share = (before + LINE_GROUP - 1) / LINE_GROUP;
+        Map m;
+        for (int k = 0; k < share; k += 8) {   // eight maps' loads go out at once: one after the other they were 6 us of 14 at 256 groups
+            float a[8][2], h[8][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int q = min(order * share + k + j, me.groups - 1);
+                const float *p = maps + (long)(ranges + (FORWARD ? q : me.groups - 1 - q)) * 2 * C;
+                pair(p, a[j]);
+                pair(p + C, h[j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool mine = k + j < share && order * share + k + j < before;
+                m.then(a[j], h[j], mine);
+            }
+        }
+        Map own;
+        if (me.live && me.z != (FORWARD ? ranges - 1 : 0)) own.then(maps + (long)me.z * 2 * C, C);
+        m.put(at + order * 2 * row, row, false);
+        own.put(at + (LINE_GROUP + order) * 2 * row, row, false);
+    }
     __syncthreads();
-    for (int q = 0; q < LINE_WAVES + order; ++q) {
-        Map<V> step;
-        state<V>(&sh[q][0][lane * V], step.a);
-        state<V>(&sh[q][1][lane * V], step.h);
+    if (me.idle) return;
+    for (int q = 0; q < LINE_GROUP + order; ++q) {
+        Map step;
+        pair(at + q * 2 * row, step.a);
+        pair(at + q * 2 * row + row, step.h);
         step.apply(s);
     }
 }
 
 // the maps of a workgroup's ranges: each to its place, and all composed to the group's
-template <int V, bool FORWARD> __device__ __forceinline__ void leave_maps(const Map<V> &m, const Line<V> &me, float *maps, int ranges, int C)
+template <bool FORWARD> __device__ __forceinline__ void leave_maps(const Map &m, const Line &me, float *maps, int ranges, int C)
 {
-    __shared__ float sh[LINE_WAVES][2][64 * V];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    m.put(&sh[FORWARD ? wave : LINE_WAVES - 1 - wave][0][lane * V], 64 * V);
-    if (!me.idle && me.live && me.z != (FORWARD ? ranges - 1 : 0)) m.put(maps + (long)me.z * 2 * C, C);
+    __shared__ float sh[LINE_GROUP * 2 * 128];
+    const int row = me.width * 2;
+    float *at = sh + me.lane * 2;
+    if (me.q < LINE_GROUP) m.put(at + (FORWARD ? me.q : LINE_GROUP - 1 - me.q) * 2 * row, row, false);
+    if (me.live && me.z != (FORWARD ? ranges - 1 : 0)) m.put(maps + (long)me.z * 2 * C, C, me.half);
     __syncthreads();
-    if (wave || !me.live) return;
-    Map<V> all;
-    for (int q = 0; q < LINE_WAVES; ++q) all.then(&sh[q][0][lane * V], 64 * V);
+    if (me.q || !me.live) return;
+    Map all;
+    for (int q = 0; q < LINE_GROUP; ++q) all.then(at + q * 2 * row, row);
     float *p = maps + (long)(ranges + me.group) * 2 * C;
-    keep_state<V>(p, all.a);
-    keep_state<V>(p + C, all.h);
+    keep_pair(p, all.a, me.half);
+    keep_pair(p + C, all.h, me.half);
 }
 
-template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_maps(ScanArgs A)
+template <class E> __global__ __launch_bounds__(64 * LINE_GROUP) void k_line_maps(ScanArgs A)
 {
-    const Line<V> me(A.B, A.C, A.ranges);
+    const Line me(A.B, A.C, A.ranges, A.range, A.apart, A.torn);
     const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs;
     const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
-    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    const bool wanted = me.live && me.z < A.ranges - 1;   // a range that is not the last is whole: a multiple of LINE steps
+    const int fp = wanted ? me.place(A.f_ts, sizeof(E)) : NOWHERE, xp = wanted ? me.place(A.x_ts, sizeof(E)) : NOWHERE;
     float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
-    Map<V> m;
-    if (!me.idle && me.z < A.ranges - 1) {
-        LineRows<E, V> fr, xr;
-        Resets rs;
+    Map m;
+    if (!me.idle && me.z0 < A.ranges - 1) {
+        const long t0 = me.z0 * A.range, end = t0 + A.range;
+        LineRows<E> fr, xr;
+        LineResets rs;
         auto fetch = [&](long t) {
-            fr.fetch(f, A.f_ts, t, end, A.C, place);
-            xr.fetch(x, A.x_ts, t, end, A.C, place);
-            if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+            fr.fetch(f, A.f_ts, t, A.T, A.C, fp, true);
+            xr.fetch(x, A.x_ts, t, A.T, A.C, xp, true);
+            if (reset) rs.fetch(reset, A.r_ts, t, A.T, me);
         };
         fetch(t0);
         if (me.z == 0) {
             m.cut = true;
-            if (A.h0) state<V>(A.h0 + me.b * A.C + me.c, m.h);
+            if (A.h0) pair(A.h0 + me.b * A.C + me.c, m.h);
         }
-        for (long t = t0; t < end; t += LINE) {   // a range that is not the last is whole: a multiple of LINE steps
-            const unsigned flags = rs.flags();
-            const LineRows<E, V> fv = fr, xv = xr;
+        for (long t = t0; t < end; t += LINE) {
+            const uint64_t flags = rs.flags();
+            const LineRows<E> fv = fr, xv = xr;
             if (t + LINE < end) fetch(t + LINE);
             auto steps = [&](auto e) {
+                const unsigned mine = e.value ? of_lane(flags, me) : 0;
 #pragma unroll
                 for (int j = 0; j < LINE; ++j) {
-                    const bool cut = e.value && flags >> j & 1;
+                    const bool cut = e.value && mine >> j & 1;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         float a, i;
                         gates((float)fv.v[j][k], a, i);
                         m.h[k] = fmaf(a, cut ? 0.f : m.h[k], i * (float)xv.v[j][k]);
                         m.a[k] *= a;
                     }
                 }
+                if (e.value) m.cut |= mine != 0;
             };
             flags ? steps(Edge{}) : steps(Plain{});
-            m.cut |= flags != 0;
         }
+        if (!wanted) m = Map{};
     }
-    leave_maps<V, true>(m, me, maps, A.ranges, A.C);
+    leave_maps<true>(m, me, maps, A.ranges, A.C);
     if (me.z == A.ranges - 1 && me.live) {
-        float s[V] = {};
-        if (A.h0) state<V>(A.h0 + me.b * A.C + me.c, s);
-        keep_state<V>(maps + (long)(A.ranges - 1) * 2 * A.C, s);
+        float s[2] = {};
+        if (A.h0) pair(A.h0 + me.b * A.C + me.c, s);
+        keep_pair(maps + (long)(A.ranges - 1) * 2 * A.C, s, me.half);
     }
 }
 
 // LOAD = STREAM: f and x together are more than the last-level cache holds, so that the second reading finds nothing of the
 // first there any more, and does better not to look (131072 steps of 512 channels, 268 MB: 75 -> 63 us; below that it loses 10 %).
-template <class E, int V, int LOAD> __global__ __launch_bounds__(64 * LINE_WAVES) void k_lines(ScanArgs A)
+template <class E, int LOAD> __global__ __launch_bounds__(64 * LINE_GROUP) void k_lines(ScanArgs A)
 {
-    const Line<V> me(A.B, A.C, A.ranges);
+    const Line me(A.B, A.C, A.ranges, A.range, A.apart, A.torn);
     if (A.ranges == 1 && me.idle) return;
     const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs;
     E *h = (E *)A.h + me.b * A.h_bs;
     const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
-    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
-    const long at = me.b * A.C + me.c, t0 = me.z * A.range, end = min(A.T, t0 + A.range);
-    LineRows<E, V, LOAD> fr, xr;
-    Resets rs;
+    const int fp = me.live ? me.place(A.f_ts, sizeof(E)) : NOWHERE, xp = me.live ? me.place(A.x_ts, sizeof(E)) : NOWHERE;
+    const int out = me.live ? me.place(A.h_ts, sizeof(E)) : NOWHERE, hp = me.half ? NOWHERE : out, one = me.half ? out + (int)sizeof(E) : NOWHERE;
+    const long at = me.b * A.C + me.c, t0 = me.z0 * A.range, end = t0 + me.batches(A.ranges, A.T) * LINE, mine = min(A.T, (me.z + 1) * A.range);
+    LineRows<E, LOAD> fr, xr;
+    LineResets rs;
     auto fetch = [&](long t) {
-        fr.fetch(f, A.f_ts, t, end, A.C, place);
-        xr.fetch(x, A.x_ts, t, end, A.C, place);
-        if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+        const bool whole = me.whole(t, A.T);
+        fr.fetch(f, A.f_ts, t, A.T, A.C, fp, whole);
+        xr.fetch(x, A.x_ts, t, A.T, A.C, xp, whole);
+        if (reset) rs.fetch(reset, A.r_ts, t, A.T, me);
     };
     if (!me.idle) fetch(t0);
-    float s[V] = {};
+    float s[2] = {};
     if (A.ranges > 1) {
         const float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
-        state<V>(maps + (long)(A.ranges - 1) * 2 * A.C, s);
-        enter_range<V, true>(s, me, maps, A.ranges, A.C);
+        pair(maps + (long)(A.ranges - 1) * 2 * A.C, s);
+        enter_range<true>(s, me, maps, A.ranges, A.C);
         if (me.idle) return;
     } else if (A.h0) {
-        state<V>(A.h0 + at, s);
+        pair(A.h0 + at, s);
     }
-    float *carry = A.carry ? A.carry + (me.b * A.tiles + t0 / LINE) * A.C + me.c : nullptr;
+    float *carry = A.carry ? A.carry + (me.b * A.tiles + me.step(t0) / LINE) * A.C + me.c : nullptr;
     for (long t = t0; t < end; t += LINE) {
-        const unsigned flags = rs.flags();
-        const int left = (int)min((long)LINE, end - t);
-        const LineRows<E, V, LOAD> fv = fr, xv = xr;
+        const uint64_t flags = rs.flags();
+        const bool whole = me.whole(t, A.T);
+        const LineRows<E, LOAD> fv = fr, xv = xr;
         if (t + LINE < end) fetch(t + LINE);
         if (carry) {
-            if (me.live) keep_state<V>(carry, s);
+            if (me.live && (whole || me.step(t) < mine)) keep_pair(carry, s, me.half);
             carry += A.C;
         }
-        const Window<E> hw(h, A.h_ts, t, end, A.C);
+        const Window<E> hw(h, A.h_ts, t, A.T, A.C);
         auto steps = [&](auto e) {
+            const unsigned cuts = e.value ? of_lane(flags, me) : 0;
+            const long left = e.value ? mine - me.step(t) : LINE;
 #pragma unroll
             for (int j = 0; j < LINE; ++j) {
-                if (e.value && j >= left) break;
-                const bool cut = e.value && flags >> j & 1;
+                const bool cut = e.value && cuts >> j & 1, there = !e.value || j < left;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
+                for (int k = 0; k < 2; ++k) {
                     float a, i;
                     gates((float)fv.v[j][k], a, i);
-                    s[k] = fmaf(a, cut ? 0.f : s[k], i * (float)xv.v[j][k]);
+                    const float n = fmaf(a, cut ? 0.f : s[k], i * (float)xv.v[j][k]);
+                    s[k] = there ? n : s[k];
                 }
-                hw.template put<V, !e.value>(place, j, s);
+                put_line<!e.value>(hw, hp, one, me.halves, j, s);
             }
         };
-        flags || left < LINE ? steps(Edge{}) : steps(Plain{});
+        flags || !whole ? steps(Edge{}) : steps(Plain{});
     }
-    if (A.h_last && end == A.T && me.live) keep_state<V>(A.h_last + at, s);
+    if (A.h_last && me.z == A.ranges - 1 && me.live) keep_pair(A.h_last + at, s, me.half);
 }
 
-template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_grad_maps(ScanGradArgs A)
+template <class E> __global__ __launch_bounds__(64 * LINE_GROUP) void k_line_grad_maps(ScanGradArgs A)
 {
-    const Line<V> me(A.B, A.C, A.ranges);
+    const Line me(A.B, A.C, A.ranges, A.range, A.apart, A.torn);
     const E *f = (const E *)A.f + me.b * A.f_bs, *dh = (const E *)A.dh + me.b * A.dh_bs;
     const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
-    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
+    const bool wanted = me.live && me.z > 0;
+    const int fp = wanted ? me.place(A.f_ts, sizeof(E)) : NOWHERE, gp = wanted ? me.place(A.dh_ts, sizeof(E)) : NOWHERE;
     float *maps = A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c;
-    const long t0 = me.z * A.range, end = min(A.T, t0 + A.range);
-    Map<V> m;
-    if (!me.idle && me.z > 0) {
-        LineRows<E, V> fr, gr;
-        Resets rs;
+    Map m;
+    if (!me.idle && me.z1 > 0) {
+        LineRows<E> fr, gr;
+        LineResets rs;
         auto fetch = [&](long t) {
-            fr.fetch(f, A.f_ts, t, end, A.C, place);
-            gr.fetch(dh, A.dh_ts, t, end, A.C, place);
-            if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
+            const bool whole = me.whole(t, A.T);
+            fr.fetch(f, A.f_ts, t, A.T, A.C, fp, whole);
+            gr.fetch(dh, A.dh_ts, t, A.T, A.C, gp, whole);
+            if (reset) rs.fetch(reset, A.r_ts, t, A.T, me);
         };
-        const long last = t0 + (end - t0 - 1) / LINE * LINE;
+        const long t0 = me.z0 * A.range, last = t0 + (me.batches(A.ranges, A.T) - 1) * LINE, mine = min(A.T, (me.z + 1) * A.range);
         fetch(last);
         for (long t = last; t >= t0; t -= LINE) {
-            const unsigned flags = rs.flags();
-            const int left = (int)min((long)LINE, end - t);
-            const LineRows<E, V> fv = fr, gv = gr;
+            const uint64_t flags = rs.flags();
+            const bool whole = me.whole(t, A.T);
+            const LineRows<E> fv = fr, gv = gr;
             if (t > t0) fetch(t - LINE);
             auto steps = [&](auto e) {
+                const long left = e.value ? mine - me.step(t) : LINE;
+                const unsigned cuts = e.value ? of_lane(flags, me) : 0;
 #pragma unroll
                 for (int j = LINE - 1; j >= 0; --j) {
-                    if (e.value && j >= left) continue;
-                    const bool cut = e.value && flags >> j & 1;
+                    const bool cut = e.value && cuts >> j & 1, there = !e.value || j < left;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         float a, i;
                         gates((float)fv.v[j][k], a, i);
-                        m.h[k] = cut ? 0.f : a * ((float)gv.v[j][k] + m.h[k]);
-                        m.a[k] *= a;
+                        const float n = cut ? 0.f : a * ((float)gv.v[j][k] + m.h[k]);
+                        m.h[k] = there ? n : m.h[k];
+                        m.a[k] *= there ? a : 1.f;
                     }
                 }
+                if (e.value) m.cut |= cuts != 0;
             };
-            flags || left < LINE ? steps(Edge{}) : steps(Plain{});
-            m.cut |= flags != 0;
+            flags || !whole ? steps(Edge{}) : steps(Plain{});
         }
+        if (!wanted) m = Map{};
     }
-    leave_maps<V, false>(m, me, maps, A.ranges, A.C);
+    leave_maps<false>(m, me, maps, A.ranges, A.C);
 }
 
-template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_line_grad(ScanGradArgs A)
+template <class E> __global__ __launch_bounds__(64 * LINE_GROUP) void k_line_grad(ScanGradArgs A)
 {
-    const Line<V> me(A.B, A.C, A.ranges);
+    const Line me(A.B, A.C, A.ranges, A.range, A.apart, A.torn);
     if (A.ranges == 1 && me.idle) return;
     const E *f = (const E *)A.f + me.b * A.f_bs, *x = (const E *)A.x + me.b * A.x_bs, *dh = (const E *)A.dh + me.b * A.dh_bs;
     E *df = (E *)A.df + me.b * A.df_bs, *dx = (E *)A.dx + me.b * A.dx_bs;
     const uint8_t *reset = A.reset ? A.reset + me.b * A.r_bs : nullptr;
-    const int place = me.live ? me.c * (int)sizeof(E) : NOWHERE;
-    const long at = me.b * A.C + me.c, t0 = me.z * A.range, end = min(A.T, t0 + A.range), last = t0 + (end - t0 - 1) / LINE * LINE;
-    const float *carry = A.carry + (me.b * A.tiles + last / LINE) * A.C + me.c;
-    LineRows<E, V> fr, xr, gr;
-    Resets rs;
-    float first[V];
+    constexpr int size = sizeof(E);
+    const int fp = me.live ? me.place(A.f_ts, size) : NOWHERE, xp = me.live ? me.place(A.x_ts, size) : NOWHERE, gp = me.live ? me.place(A.dh_ts, size) : NOWHERE;
+    const int dfo = me.live ? me.place(A.df_ts, size) : NOWHERE, dfp = me.half ? NOWHERE : dfo, df1 = me.half ? dfo + size : NOWHERE;
+    const int dxo = me.live ? me.place(A.dx_ts, size) : NOWHERE, dxp = me.half ? NOWHERE : dxo, dx1 = me.half ? dxo + size : NOWHERE;
+    const long at = me.b * A.C + me.c, t0 = me.z0 * A.range, last = t0 + (me.batches(A.ranges, A.T) - 1) * LINE, mine = min(A.T, (me.z + 1) * A.range);
+    const float *final = A.carry + ((me.b + 1) * A.tiles - 1) * A.C + me.c, *carry = A.carry + (me.b * A.tiles + me.step(last) / LINE) * A.C + me.c;
+    LineRows<E> fr, xr, gr;
+    LineResets rs;
+    float first[2];
     auto fetch = [&](long t) {
-        fr.fetch(f, A.f_ts, t, end, A.C, place);
-        xr.fetch(x, A.x_ts, t, end, A.C, place);
-        gr.fetch(dh, A.dh_ts, t, end, A.C, place);
-        if (reset) rs.fetch(reset, A.r_ts, t, min(end, t + LINE));
-        state<V>(carry, first);
+        const bool whole = me.whole(t, A.T);
+        fr.fetch(f, A.f_ts, t, A.T, A.C, fp, whole);
+        xr.fetch(x, A.x_ts, t, A.T, A.C, xp, whole);
+        gr.fetch(dh, A.dh_ts, t, A.T, A.C, gp, whole);
+        if (reset) rs.fetch(reset, A.r_ts, t, A.T, me);
+        pair(whole || carry < final ? carry : final, first);   // a range that has ended reads what is there
         carry -= A.C;
     };
     if (!me.idle) fetch(last);
-    float mu[V] = {};
-    if (A.dlast) state<V>(A.dlast + at, mu);
+    float mu[2] = {};
+    if (A.dlast) pair(A.dlast + at, mu);
     if (A.ranges > 1) {
-        enter_range<V, false>(mu, me, A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c, A.ranges, A.C);
+        enter_range<false>(mu, me, A.totals + me.b * (A.ranges + me.groups) * 2 * A.C + me.c, A.ranges, A.C);
         if (me.idle) return;
     }
     for (long t = last; t >= t0; t -= LINE) {
-        const unsigned flags = rs.flags();
-        const int left = (int)min((long)LINE, end - t);
-        const LineRows<E, V> fv = fr, xv = xr, gv = gr;
-        float s[V], before[LINE][V], ga[LINE][V], gi[LINE][V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) s[k] = first[k];
+        const uint64_t flags = rs.flags();
+        const bool whole = me.whole(t, A.T);
+        const LineRows<E> fv = fr, xv = xr, gv = gr;
+        float s[2] = {first[0], first[1]}, before[LINE][2], ga[LINE][2], gi[LINE][2];
         if (t > t0) fetch(t - LINE);
-        const Window<E> dfw(df, A.df_ts, t, end, A.C), dxw(dx, A.dx_ts, t, end, A.C);
+        const Window<E> dfw(df, A.df_ts, t, A.T, A.C), dxw(dx, A.dx_ts, t, A.T, A.C);
         auto steps = [&](auto e) {
+            const unsigned cuts = e.value ? of_lane(flags, me) : 0;
+            const long left = e.value ? mine - me.step(t) : LINE;
 #pragma unroll
             for (int j = 0; j < LINE; ++j) {
-                const bool cut = e.value && flags >> j & 1;
+                const bool cut = e.value && cuts >> j & 1;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
+                for (int k = 0; k < 2; ++k) {
                     gates((float)fv.v[j][k], ga[j][k], gi[j][k]);
                     before[j][k] = cut ? 0.f : s[k];
                     s[k] = fmaf(ga[j][k], before[j][k], gi[j][k] * (float)xv.v[j][k]);
@@ -851,23 +974,22 @@ template <class E, int V> __global__ __launch_bounds__(64 * LINE_WAVES) void k_l
             }
 #pragma unroll
             for (int j = LINE - 1; j >= 0; --j) {
-                if (e.value && j >= left) continue;
-                const bool cut = e.value && flags >> j & 1;
-                float odf[V], odx[V];
+                const bool cut = e.value && cuts >> j & 1, there = !e.value || j < left;
+                float odf[2], odx[2];
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
+                for (int k = 0; k < 2; ++k) {
                     const float l = (float)gv.v[j][k] + mu[k], n = ga[j][k] * l;
                     odx[k] = gi[j][k] * l;
                     odf[k] = gi[j][k] * n * (before[j][k] - (float)xv.v[j][k]);
-                    mu[k] = cut ? 0.f : n;
+                    mu[k] = !there ? mu[k] : cut ? 0.f : n;
                 }
-                dfw.template put<V, !e.value>(place, j, odf);
-                dxw.template put<V, !e.value>(place, j, odx);
+                put_line<!e.value>(dfw, dfp, df1, e.value && me.halves, j, odf);
+                put_line<!e.value>(dxw, dxp, dx1, e.value && me.halves, j, odx);
             }
         };
-        flags || left < LINE ? steps(Edge{}) : steps(Plain{});
+        flags || !whole || me.halves ? steps(Edge{}) : steps(Plain{});
     }
-    if (A.dh0 && me.z == 0 && me.live) keep_state<V>(A.dh0 + at, mu);
+    if (A.dh0 && me.z == 0 && me.live) keep_pair(A.dh0 + at, mu, me.half);
 }
 
 // ------------------------------------------------------------ narrow sequences

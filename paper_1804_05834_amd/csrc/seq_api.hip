@@ -38,10 +38,20 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 // forward / backward in bf16, C = 512, B x T:
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
-// below that ranges: as many waves as the card holds at four per SIMD, each with 32 steps at least.
+// below that ranges, see SCAN_UNITS.
 // Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 139 / 179, 932 / 1229; 300 x 2000 x 8: 31 / 34, 78 / 122;
 // 574 x 2844 x 17: 125 / 160, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Short ones of them a workgroup each (see there).
 constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
+// Ranges of lines: the compute units hold one workgroup of eight waves each of the backward kernel, two of the others', and a
+// second turn of a few workgroups takes as long as the first.  So ranges are as short as leaves one workgroup for each unit, or two
+// if that is still 64 steps a range (131072 x 512 in bf16, forward: 122 us, 125 with one).  us forward / backward by the
+// steps of a range (workgroups), in bf16:
+//   7 x 4099 x 256:  16 (462) 21 / 30   24 (308) 24 / 35   32 (238) 20 / 26   48 (154) 24 / 31
+//   7 x 4099 x 320:  16 (693) 25 / 36   24 (462) 25 / 36   32 (357) 27 / 40   48 (231) 25 / 33
+// Every range composes the maps of all groups before it, so that more than 2048 cost more than they give (1 x 65536 x 64: 24 / 29 us
+// with 1024, 20 / 22 with 2048; before the loads went out in eights 27 / 29 with 2048, 34 / 34 with 4096).
+constexpr int64_t SCAN_UNITS = 256, SCAN_MOST = 2048;
+constexpr long SCAN_LONG_RANGE = 64;
 // One or two channels: 32 steps of a thread at a time rather than 8 from this many elements on (83 x 95456 x 1: 139 / 179 us against
 // 166 / 400; 60 x 25811 x 1: 55 / 61 against 38 / 48).
 constexpr int64_t SCAN_LONG = 6 << 20;
@@ -75,6 +85,9 @@ const char *check_scan(const dqn_scan_args &s)
     return nullptr;
 }
 
+// waves of a workgroup of lines in ranges
+int line_waves(int32_t C) { return C > 128 ? seq::LINE_GROUP : seq::line_width((C + 1) / 2) * seq::LINE_GROUP / 64; }
+
 // How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
 struct ScanCut {
     enum { SHORT, BLOCK, NARROW, STRIPS, LINES } form;
@@ -99,15 +112,23 @@ ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
         const long tile = 16 * waves;
         return ScanCut{ScanCut::STRIPS, waves, tile, (long)((T + tile - 1) / tile), (long)T, 1};
     }
-    const int64_t want = lines >= SCAN_LINES || !lines ? 1 : std::min<int64_t>((SCAN_WANT + lines - 1) / lines, (T + SCAN_LEAST - 1) / SCAN_LEAST);
-    const long per = (T + want - 1) / want, range = (per + seq::LINE - 1) / seq::LINE * seq::LINE;
+    long range = (T + seq::LINE - 1) / seq::LINE * seq::LINE;
+    if (lines && lines < SCAN_LINES) {
+        const int64_t groups = (int64_t)B * ((C + 127) / 128), slots = SCAN_UNITS * seq::LINE_GROUP / line_waves(C);
+        auto cut = [&](int64_t all) {
+            const int64_t n = std::min(std::max<int64_t>(1, all / groups) * seq::LINE_GROUP, SCAN_MOST);
+            return (long)(((T + n - 1) / n + seq::LINE - 1) / seq::LINE * seq::LINE);
+        };
+        range = cut(2 * slots);
+        if (range < SCAN_LONG_RANGE) range = cut(slots);
+    }
     return ScanCut{ScanCut::LINES, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), range, (int)((T + range - 1) / range)};
 }
 size_t scan_workspace(const ScanCut &c, int32_t B, int32_t C)
 {
     if (c.ranges == 1) return 0;
     if (c.form == ScanCut::NARROW) return ((size_t)B * c.ranges * 2 * C * 4 + 15) / 16 * 16;
-    const size_t maps = c.ranges + (c.ranges + seq::LINE_WAVES - 1) / seq::LINE_WAVES;
+    const size_t maps = c.ranges + (c.ranges + seq::LINE_GROUP - 1) / seq::LINE_GROUP;
     return ((size_t)B * maps * 2 * C * 4 + 15) / 16 * 16;
 }
 
@@ -132,32 +153,48 @@ template <class E, int V> void launch_short(const seq::ScanGradArgs &A, hipStrea
 {
     seq::k_scan_grad_short<E, V><<<dim3((unsigned)(((int64_t)A.B * (A.C / V) + 255) / 256)), 256, 0, st>>>(A);
 }
-// a workgroup per strip and group of ranges, or eight lines
-template <int V> dim3 line_grid(int32_t B, int32_t C, int ranges)
+dim3 line_grid(int32_t B, int32_t C, int ranges)
 {
-    const int64_t strips = (C + 64 * V - 1) / (64 * V);
-    return dim3((unsigned)(ranges == 1 ? ((int64_t)B * strips + seq::LINE_WAVES - 1) / seq::LINE_WAVES : strips * B * ((ranges + seq::LINE_WAVES - 1) / seq::LINE_WAVES)));
+    const int64_t strips = ((C + 1) / 2 + 63) / 64;
+    return dim3((unsigned)(ranges == 1 ? (B * strips + seq::LINE_GROUP - 1) / seq::LINE_GROUP : strips * B * ((ranges + seq::LINE_GROUP - 1) / seq::LINE_GROUP)));
 }
-template <class E, int V> void launch_lines(const seq::ScanArgs &A, hipStream_t st)
+// whether a group's ranges are too far from one another to count the distance in 32 bits: eight of them within 2^30 bytes
+bool far_ranges(int64_t range, std::initializer_list<int64_t> steps)
 {
-    const dim3 grid = line_grid<V>(A.B, A.C, A.ranges);
-    if (A.ranges > 1) seq::k_line_maps<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
-    if (V > 1 && 2 * (int64_t)sizeof(E) * A.B * A.T * A.C >= LAST_LEVEL) seq::k_lines<E, V, seq::STREAM><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
-    else seq::k_lines<E, V, 0><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    const int64_t most = std::max(steps);
+    return most && range > (1 << 25) / most;
 }
-template <class E, int V> void launch_lines(const seq::ScanGradArgs &A, hipStream_t st)
+// whether a row of a tensor begins within a line of the caches, of 128 bytes
+bool torn_rows(std::initializer_list<const void *> tensors, size_t size, std::initializer_list<int64_t> strides)
 {
-    const dim3 grid = line_grid<V>(A.B, A.C, A.ranges);
-    if (A.ranges > 1) seq::k_line_grad_maps<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
-    seq::k_line_grad<E, V><<<grid, 64 * seq::LINE_WAVES, 0, st>>>(A);
+    for (const void *p : tensors)
+        if (!at(p, 128)) return true;
+    for (int64_t s : strides)
+        if (s * (int64_t)size % 128) return true;
+    return false;
+}
+template <class E> void launch_lines(seq::ScanArgs A, hipStream_t st)
+{
+    A.apart = far_ranges(A.range, {A.f_ts, A.x_ts, A.h_ts});
+    const dim3 grid = line_grid(A.B, A.C, A.ranges), block(64 * (A.ranges == 1 || A.apart ? seq::LINE_GROUP : line_waves(A.C)));
+    if (A.ranges > 1) seq::k_line_maps<E><<<grid, block, 0, st>>>(A);
+    if (2 * (int64_t)sizeof(E) * A.B * A.T * A.C >= LAST_LEVEL) seq::k_lines<E, seq::STREAM><<<grid, block, 0, st>>>(A);
+    else seq::k_lines<E, 0><<<grid, block, 0, st>>>(A);
+}
+template <class E> void launch_lines(seq::ScanGradArgs A, hipStream_t st)
+{
+    A.apart = far_ranges(A.range, {A.f_ts, A.x_ts, A.dh_ts, A.df_ts, A.dx_ts});
+    const dim3 grid = line_grid(A.B, A.C, A.ranges), block(64 * (A.ranges == 1 || A.apart ? seq::LINE_GROUP : line_waves(A.C)));
+    if (A.ranges > 1) seq::k_line_grad_maps<E><<<grid, block, 0, st>>>(A);
+    seq::k_line_grad<E><<<grid, block, 0, st>>>(A);
 }
 template <class E, int V> void launch_strips(const seq::ScanArgs &A, int waves, hipStream_t st)
 {
-    seq::k_scan<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
+    seq::k_scan<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP * A.B)), 64 * waves, 0, st>>>(A);
 }
 template <class E, int V> void launch_strips(const seq::ScanGradArgs &A, int waves, hipStream_t st)
 {
-    seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), (unsigned)A.B), 64 * waves, 0, st>>>(A);
+    seq::k_scan_grad<E, V><<<dim3((unsigned)((A.C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP * A.B)), 64 * waves, 0, st>>>(A);
 }
 template <class E, int N, class Args> void launch_narrow(const Args &A, hipStream_t st)
 {
@@ -181,7 +218,7 @@ template <class E, class Args, class F> void launch_recurrence(const Args &A, co
     else if (c.form == ScanCut::BLOCK) launch_block<E>(A, st);
     else if (c.form == ScanCut::SHORT) fits(4) ? launch_short<E, 4>(A, st) : launch_short<E, 1>(A, st);
     else if (c.form == ScanCut::STRIPS) fits(2) ? launch_strips<E, 2>(A, c.waves, st) : launch_strips<E, 1>(A, c.waves, st);
-    else fits(2) ? launch_lines<E, 2>(A, st) : launch_lines<E, 1>(A, st);
+    else launch_lines<E>(A, st);
 }
 
 const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
@@ -360,7 +397,8 @@ int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream)
     const ScanCut cut = scan_cut(s.B, s.T, s.C);
     if (scan_workspace(cut, s.B, s.C) && (!s.workspace || !at(s.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanArgs A{s.f, s.x, s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h0, s.reset, s.reset_bs, s.reset_ts, s.h, s.h_bs, s.h_ts, s.h_last,
-                          s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.tiles, cut.range, cut.ranges, (float *)s.workspace};
+                          s.T ? s.carry : nullptr, s.T, s.B, s.C, cut.tiles, cut.range, cut.ranges, (float *)s.workspace, false,
+                          torn_rows({s.f, s.x, s.h}, bytes_of(s.dtype), {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts})};
     auto fits = [&](int n) { return together(n, s.dtype, s.C, {s.f, s.x, s.h}, {s.f_bs, s.f_ts, s.x_bs, s.x_ts, s.h_bs, s.h_ts}, {s.h0, s.h_last, s.carry}); };
     s.dtype == DQN_F32 ? launch_recurrence<float>(A, cut, fits, st) : launch_recurrence<seq::bf16>(A, cut, fits, st);
     return launched(call);
@@ -387,7 +425,9 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream)
     const ScanCut cut = scan_cut(s.B, s.T, s.C);
     if (scan_workspace(cut, s.B, s.C) && (!g.workspace || !at(g.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     const seq::ScanGradArgs A{g.f, g.x, g.dh, g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.carry, g.dlast, g.reset, g.reset_bs, g.reset_ts,
-                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.tiles, cut.range, cut.ranges, (float *)g.workspace};
+                              g.df, g.dx, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts, g.dh0, g.T, g.B, g.C, cut.tiles, cut.range, cut.ranges, (float *)g.workspace, false,
+                              torn_rows({g.f, g.x, g.dh, g.df, g.dx}, bytes_of(g.dtype),
+                                        {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts})};
     auto fits = [&](int n) {
         return together(n, g.dtype, g.C, {g.f, g.x, g.dh, g.df, g.dx}, {g.f_bs, g.f_ts, g.x_bs, g.x_ts, g.dh_bs, g.dh_ts, g.df_bs, g.df_ts, g.dx_bs, g.dx_ts},
                         {g.carry, g.dlast, g.dh0});
@@ -519,7 +559,7 @@ int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t
         if (!p || !at(p, 256)) return bad(call, "a buffer is NULL or not 256-byte aligned");
     for (int32_t i = 0; i < count; ++i)
         if (tensors[i].n && !at(tensors[i].grad, bytes_of(grad_dtype))) return bad(call, "a gradient is not aligned to its elements");
-    if (s.chunks > INT32_MAX) return bad(call, "too many elements");
+    if (s.chunks >= 1 << 24) return bad(call, "too many elements");   // a launch has 2^32 threads
     dqn_adamw *o = nullptr;
     try {
         std::vector<uint8_t> table(plan_bytes(s), 0);

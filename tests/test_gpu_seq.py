@@ -50,6 +50,9 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     # few channels: more than six million elements in long sequences, whole sequences per thread, and either side of a workgroup each
     (700, 9001, 1, "half", True, 0.001), (780, 4111, 2, "time", True, 0.003), (8200, 515, 16, "plain", True, 0.003),
     (9, 512, 16, "odd", True, 0.01), (9, 513, 16, "half", True, 0.01), (30, 2730, 3, "time", True, 0.001), (4, 1025, 8, "broadcast", True, 0.5),
+    # ranges whose lanes share waves, pairs of channels at any address, an odd last channel, rows far apart
+    (7, 1030, 261, "plain", True, 0.004), (2, 999, 17, "odd", True, 0.01), (1, 777, 19, "time", True, 0.05), (3, 2100, 64, "half", False, 0.002), (2, 641, 127, "odd", False, 0.0),
+    (1, 640, 129, "half", True, 0.3), (5, 333, 41, "broadcast", True, 0.02), (2, 40, 21, "far", True, 0.1), (1, 70, 100, "far", False, 0.0),
     (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
@@ -67,6 +70,9 @@ def scan_case(B, T, C, layout, state, chance, dtype, seed=0):
         z = torch.zeros(B, T, 2 * C + 3, dtype=t, device="cuda")
         z[..., 1:C + 1], z[..., C + 2:2 * C + 2] = f, x
         f, x = z[..., 1:C + 1], z[..., C + 2:2 * C + 2]
+    elif layout == "far":       # a step every million and a half elements
+        z = torch.empty(T * (1500001 + B) * 2, dtype=t, device="cuda")
+        f, x = (z[k * T * (1500001 + B):].as_strided((B, T, C), (C, 1500001, 1)).copy_(v) for k, v in enumerate((f, x)))
     elif layout == "broadcast":     # one sequence of gates for all
         f = f[:1].expand(B, T, C)
     h0 = rnd(seed + 2, B, C) if state else None
@@ -110,6 +116,25 @@ def test_scan_state_in_place_and_outputs_apart(seq):
         seq.scan(f, x, h0=s, reset=reset, out=wide[..., 4:C + 4], last=s)
         assert torch.equal(s, last) and torch.equal(wide[..., 4:C + 4], h)
         assert bool((wide[..., :4] == 5).all() and (wide[..., C + 4:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,T,C", [(1, 6000, 97), (3, 130, 67), (2, 800, 21), (2100, 20, 33), (300, 40, 65)])
+def test_scan_odd_channels_and_outputs_apart(seq, B, T, C, dtype):
+    """Nothing is written beside rows of an odd number of channels, forward and backward, nor beside the states."""
+    t = TYPES[dtype]
+    f, x, h0, reset = scan_case(B, T, C, "half", True, 0.01, dtype, 20)
+    h, last, carry = seq.scan(f, x, h0=h0, reset=reset, save=True)
+    wide, s = torch.full((B, T, C + 4), 5.0, dtype=t, device="cuda"), h0.clone()
+    seq.scan(f, x, h0=s, reset=reset, out=wide[..., 3:C + 3], last=s)
+    assert torch.equal(s, last) and torch.equal(wide[..., 3:C + 3], h)
+    assert bool((wide[..., :3] == 5).all() and (wide[..., C + 3:] == 5).all())
+    dh = rnd(7, B, T, C, dtype=t)
+    df, dx, dh0 = seq.scan_backward(dh, f, x, carry, reset=reset, dlast=h0)
+    wide = torch.full((B, T, 2 * C + 3), 5.0, dtype=t, device="cuda")
+    seq.scan_backward(dh, f, x, carry, reset=reset, dlast=h0, out=(wide[..., 1:C + 1], wide[..., C + 2:2 * C + 2]))
+    assert torch.equal(wide[..., 1:C + 1], df) and torch.equal(wide[..., C + 2:2 * C + 2], dx)
+    assert bool((wide[..., 0] == 5).all() and (wide[..., C + 1] == 5).all() and (wide[..., 2 * C + 2] == 5).all())
 
 
 @pytest.mark.parametrize("B,T", [(2, 1), (2, 5), (2, 40), (2, 600), (2, 9000), (300, 20), (300, 300), (2100, 30)])
