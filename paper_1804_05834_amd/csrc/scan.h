@@ -600,7 +600,7 @@ struct Map {
 __host__ __device__ __forceinline__ int line_width(int pairs)
 {
     int width = 64;
-    while (width / 2 >= pairs) width /= 2;
+    while (width > 1 && width / 2 >= pairs) width /= 2;
     return width;
 }
 
@@ -932,7 +932,7 @@ template <class E> __global__ __launch_bounds__(64 * LINE_GROUP) void k_line_gra
     const int dfo = me.live ? me.place(A.df_ts, size) : NOWHERE, dfp = me.half ? NOWHERE : dfo, df1 = me.half ? dfo + size : NOWHERE;
     const int dxo = me.live ? me.place(A.dx_ts, size) : NOWHERE, dxp = me.half ? NOWHERE : dxo, dx1 = me.half ? dxo + size : NOWHERE;
     const long at = me.b * A.C + me.c, t0 = me.z0 * A.range, last = t0 + (me.batches(A.ranges, A.T) - 1) * LINE, mine = min(A.T, (me.z + 1) * A.range);
-    const float *final = A.carry + ((me.b + 1) * A.tiles - 1) * A.C + me.c, *carry = A.carry + (me.b * A.tiles + me.step(last) / LINE) * A.C + me.c;
+    const float *final = A.carry + ((me.b + 1) * A.tiles - 1) * A.C + me.c, *carry = A.carry + (me.b * A.tiles + (me.live ? me.step(last) : last) / LINE) * A.C + me.c;   // a lane that is not live reads what the first does
     LineRows<E> fr, xr, gr;
     LineResets rs;
     float first[2];
