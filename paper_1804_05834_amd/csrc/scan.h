@@ -74,7 +74,6 @@ template <int V> struct Lane {
     __device__ Lane(int first, int C) : c(min(first, C - V)), live(first < C) {}
 };
 
-// a state of V channels, at any address of a float
 // Which of `all` items (a sequence or a group of ranges) and which strip of its channels a workgroup has.  Workgroups with the same
 // id modulo 8 share a cache.  Where rows are torn, that is where strips have lines of memory in common, those of an item
 // share a cache (7 x 4099 x 261 in fp32 with gradients: 101 -> 93 us); else they are dealt out in turn (131072 x 512 in bf16:
@@ -97,6 +96,7 @@ struct Dealt {
     }
 };
 
+// a state of V channels, at any address of a float
 template <int V> __device__ __forceinline__ void state(const float *p, float (&s)[V]) { __builtin_memcpy(s, p, sizeof(s)); }
 template <int V> __device__ __forceinline__ void keep_state(float *p, const float (&s)[V]) { __builtin_memcpy(p, s, sizeof(s)); }
 
@@ -546,7 +546,7 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
 // and of an odd number of channels the last lane has the last two but stores the last alone (`half`).
 //
 // Measured: 512 sequences of 64 steps of 512 channels in bf16, a wave each, 18 us forward (5.6 TB/s), 36 backward (4.7); one
-// sequence of 131072 steps of 512 channels, in ranges, 57 for the maps (4.7 TB/s) and 67 for the states (6.0).
+// sequence of 131072 steps of 512 channels, in ranges, 56 for the maps (4.8 TB/s) and 68 for the states (5.9).
 constexpr int LINE = 8;         // steps between two states of `carry`, and of a wave's loads
 constexpr int LINE_GROUP = 8;   // ranges of a workgroup; waves of one whose waves take whole sequences
 

@@ -39,9 +39,12 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
 // below that ranges, see SCAN_UNITS.
-// Narrow sequences (us, narrow against the other forms; B x T x C): 83 x 95456 x 1: 139 / 179, 932 / 1229; 300 x 2000 x 8: 31 / 34, 78 / 122;
-// 574 x 2844 x 17: 125 / 160, 189 / 307; 500 x 300 x 30: 25 / 51, 19 / 28.  Short ones of them a workgroup each (see there).
-constexpr int64_t SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
+// Narrow sequences: up to 16 channels, up to 32 of more than 1000 steps; us forward / backward, narrow against ranges of lines,
+// B x T x C in bf16: 2000 x 3000 x 8: 184 / 283, 240 / 298; 200 x 4000 x 5: 38 / 51, 48 / 70; 574 x 2844 x 17: 125 / 160, 150 / 189.  Ranges
+// of lines where a strip is filled for five eighths (100 x 3000 x 32: 42 / 52, 26 / 35; 2000 x 1000 x 16: 122 / 166, 89 / 120) or sequences and
+// steps are few (1 x 131072 x 2: 44 / 53, 25 / 31; 10 x 30000 x 3: 29 / 34, 22 / 26; 64 x 20000 x 4: 35 / 49, 56 / 79).  Short ones a
+// workgroup each (see there).
+constexpr int64_t SCAN_FEW = 1 << 18, SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
 // Ranges of lines: the compute units hold one workgroup of eight waves each of the backward kernel, two of the others', and a
 // second turn of a few workgroups takes as long as the first.  So ranges are as short as leaves one workgroup for each unit, or two
 // if that is still 64 steps a range (131072 x 512 in bf16, forward: 122 us, 125 with one).  us forward / backward by the
@@ -86,7 +89,7 @@ const char *check_scan(const dqn_scan_args &s)
 }
 
 // waves of a workgroup of lines in ranges
-int line_waves(int32_t C) { return C > 128 ? seq::LINE_GROUP : seq::line_width((C + 1) / 2) * seq::LINE_GROUP / 64; }
+int line_waves(int32_t C) { return C > 128 ? seq::LINE_GROUP : (seq::line_width((C + 1) / 2) * seq::LINE_GROUP + 63) / 64; }
 
 // How a recurrence of these sizes is cut: a function of the sizes alone, the same for both directions.
 struct ScanCut {
@@ -99,14 +102,17 @@ struct ScanCut {
 ScanCut scan_cut(int32_t B, int64_t T, int32_t C)
 {
     if (T <= seq::SCAN_SHORT) return ScanCut{ScanCut::SHORT, 0, seq::SCAN_SHORT, T ? 1 : 0, (long)T, 1};
-    if (C <= 16 || (C <= 32 && T > 1000)) {
+    const int pairs = (C + 1) / 2;
+    const bool narrow = C <= 16 || (C <= 32 && T > 1000), filled = C >= 16 && pairs * 8 >= seq::line_width(pairs) * 5;
+    const bool few = narrow && B < SCAN_LINES && (filled || (C >= 2 && B * T <= SCAN_FEW));   // ranges of lines all the same
+    if (narrow && (!few || T * C <= seq::NARROW_BLOCK)) {
         if (C && T * C <= seq::NARROW_BLOCK) return ScanCut{ScanCut::BLOCK, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), (long)T, 1};
         const int64_t all = std::max<int64_t>(1, (int64_t)B * C), want = std::max<int64_t>(1, std::min<int64_t>(SCAN_WANT * 64 / all, T / SCAN_LEAST));
         const long per = (T + want - 1) / want, range = (per + seq::LINE - 1) / seq::LINE * seq::LINE;
         return ScanCut{ScanCut::NARROW, 0, seq::LINE, (long)((T + seq::LINE - 1) / seq::LINE), range, (int)((T + range - 1) / range)};
     }
     const int64_t strips = (int64_t)B * ((C + seq::SCAN_STRIP - 1) / seq::SCAN_STRIP), lines = (int64_t)B * ((C + 127) / 128);
-    if (lines < SCAN_LINES && strips >= SCAN_STRIPS) {
+    if (!few && lines < SCAN_LINES && strips >= SCAN_STRIPS) {
         int waves = 1;
         while (waves < seq::SCAN_WAVES && 16 * waves < T) waves *= 2;
         const long tile = 16 * waves;

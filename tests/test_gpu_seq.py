@@ -53,6 +53,9 @@ SCANS = [  # B, T, C, layout, initial state, chance of a reset
     # ranges whose lanes share waves, pairs of channels at any address, an odd last channel, rows far apart
     (7, 1030, 261, "plain", True, 0.004), (2, 999, 17, "odd", True, 0.01), (1, 777, 19, "time", True, 0.05), (3, 2100, 64, "half", False, 0.002), (2, 641, 127, "odd", False, 0.0),
     (1, 640, 129, "half", True, 0.3), (5, 333, 41, "broadcast", True, 0.02), (2, 40, 21, "far", True, 0.1), (1, 70, 100, "far", False, 0.0),
+    # few channels in many ranges, of few sequences and of many
+    (3, 5000, 2, "odd", True, 0.001), (2, 4500, 3, "half", True, 0.01), (5, 3000, 4, "time", True, 0.0), (64, 2100, 5, "plain", False, 0.002), (66, 4000, 5, "half", True, 0.002), (140, 2100, 3, "plain", True, 0.001),
+    (1, 40000, 2, "half", True, 0.0002), (300, 1100, 20, "half", True, 0.003), (600, 1030, 17, "plain", True, 0.003), (2, 1003, 29, "odd", True, 0.5),
     (2100, 20, 12, "plain", True, 0.05), (2060, 17, 130, "half", True, 0.05), (2050, 24, 5, "odd", False, 0.1),
 ]
 
