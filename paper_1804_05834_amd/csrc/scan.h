@@ -57,13 +57,14 @@ constexpr int SCAN_WAVES = 8;       // most waves of a workgroup
 constexpr int SCAN_SHORT = 8;       // longest sequence that a thread goes through alone
 
 // sigmoid(f) = 1 / (1 + e) and 1 - sigmoid(f) = e / (1 + e) with e = exp(-f).  The second is not taken from the first: 1 - a
-// of an `a` near one, a memory that lasts, would keep few of its digits.  Where e is infinite, infinity times zero is
-// the one that it should be (fminf drops the NaN); a gate that is NaN has a = NaN.
+// of an `a` near one, a memory that lasts, would keep few of its digits.  Nor is it the product e a where e is large: the
+// instruction gives zero for a reciprocal below 2^-126, from f = -87.4 on, and infinity times zero is NaN.  From e = 2^24
+// on it is one to the last digit.  A gate that is NaN makes both NaN: no comparison with it holds.
 __device__ __forceinline__ void gates(float f, float &a, float &i)
 {
     const float e = __builtin_amdgcn_exp2f(-1.44269504088896341f * f);
     a = __builtin_amdgcn_rcpf(1.f + e);
-    i = fminf(e * a, 1.f);
+    i = e > 0x1p24f ? 1.f : e * a;
 }
 
 // What a thread works on: V channels from c on of sequence b, clamped to the tensor where c is beyond it (then `live` is

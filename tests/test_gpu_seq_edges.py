@@ -1,0 +1,63 @@
+"""Where the recurrent network's operators meet the ends of their types and of their launches, against their definitions in
+64 bits (tests/seq_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+import seq_ref as ref
+from test_gpu_seq import TYPES, close, host, rnd, scan_case, seq  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+# B, T, C: a thread per four channels and per channel; strips of pairs and of single channels; whole lines, ranges of lines, an odd
+# last channel; a workgroup per sequence; a thread per channel and range, 8 and 32 steps at a time
+FORMS = [(3, 5, 64), (2, 8, 3), (300, 20, 64), (260, 40, 65), (2100, 20, 64), (2, 700, 64), (1, 300, 67), (9, 300, 16), (3, 20000, 1), (700, 9001, 1)]
+SMALLEST = 2.0 ** -126      # of a normal number; a gate below it may count as zero
+
+
+def gates_case(B, T, C, dtype, values, seed):
+    g = torch.Generator().manual_seed(seed)
+    f = torch.tensor(values)[torch.randint(0, len(values), (B, T, C), generator=g)].to(TYPES[dtype]).cuda()
+    return f, rnd(seed + 1, B, T, C, dtype=TYPES[dtype]), rnd(seed + 2, B, C), rnd(seed + 3, B, T, C, dtype=TYPES[dtype]), rnd(seed + 4, B, C)
+
+
+def check_scan(seq, f, x, h0, reset, dh, dlast, bf):
+    """Forward and backward within the bounds of seq_ref and what gates below SMALLEST, taken as zero, would have let through."""
+    hf, hx, hh, hr = host(f), host(x), host(h0), None if reset is None else reset.cpu().numpy()
+    h, last, carry = seq.scan(f, x, h0=h0, reset=reset, save=True)
+    want, wl, _, eh, el, _ = ref.scan(hf, hx, hh, hr)
+    size = max(np.nanmax(np.abs(want)), np.abs(hx).max(), np.abs(hh).max())
+    lost = 2 * SMALLEST * f.shape[1] * size
+    close(h, want, ref.stored(eh, want, bf) + lost, "h")
+    close(last, wl, el + lost + 1e-37, "last")
+    df, dx, dh0 = seq.scan_backward(dh, f, x, carry, reset=reset, dlast=dlast)
+    wants, bounds = ref.scan_backward(host(dh), hf, hx, hh, hr, host(dlast))
+    sent = np.abs(host(dh)).sum(1).max() + np.abs(host(dlast)).max()      # no more than this comes from later steps
+    lost = 2 * SMALLEST * f.shape[1] * sent * (2 * size + 1)
+    close(df, wants[0], ref.stored(bounds[0], wants[0], bf) + lost, "df")
+    close(dx, wants[1], ref.stored(bounds[1], wants[1], bf) + lost, "dx")
+    close(dh0, wants[2], bounds[2] + lost + 1e-37, "dh0")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,T,C", FORMS)
+def test_scan_gates_whose_exponential_is_almost_infinite(seq, B, T, C, dtype):  # noqa: F811
+    """exp(88.7) is the largest exponential that is finite; from exp(87.4) on the gate itself is below the smallest normal number,
+    but the input still comes through whole."""
+    print("case gates", B, T, C, dtype, flush=True)
+    v = [87.0, 87.3, 87.4, 87.5, 88.0, 88.5, 88.7, 89.0, 103.0]
+    args = gates_case(B, T, C, dtype, [-u for u in v] + v[::2] + [0.0, 1.0, -1.0, 16.0, -16.0, -17.0], 400)
+    check_scan(seq, *args[:3], None, *args[3:], dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,T,C", FORMS)
+def test_scan_a_gate_that_is_not_a_number(seq, B, T, C, dtype):  # noqa: F811
+    """It spoils the state from its step to the next episode, and the gradients of its step and of those before it in its episode."""
+    f, x, h0, dh, dlast = gates_case(B, T, C, dtype, [0.0, 1.0, -1.0, 2.0], 420)
+    reset = (torch.rand(B, T, generator=torch.Generator().manual_seed(421)) < 4.0 / T).cuda()
+    f[0, T // 2, 0] = f[-1, T - 1, C - 1] = f[B // 2, 0, C // 2] = NAN
+    reset[0, T // 2] = False
+    check_scan(seq, f, x, h0, reset, dh, dlast, dtype == "bf16")
