@@ -343,7 +343,10 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
         if (reset) rs.fetch(reset, A.r_ts, t + wrow, end);
     };
     fetch(0);
-    if (A.h0) state<V>(A.h0 + at, s);
+    if (A.h0) {   // all waves read it, and the first may write h_last there behind the first barrier
+        state<V>(A.h0 + at, s);
+        arrived(s);
+    }
     int buf = 0;
     for (long t = 0; t < end; t += tile, buf ^= 1) {
         const unsigned flags = rs.flags(), r = flags >> half, mycuts = cuts_of<V>(flags);
@@ -1164,6 +1167,8 @@ template <class E, class Args> __global__ __launch_bounds__(BLOCK_THREADS<Args>)
     const long b = blockIdx.x, range = ((A.T + runs - 1) / runs + LINE - 1) / LINE * LINE, t0 = min(A.T, run * range), end = min(A.T, t0 + range);
     const bool mine = run < runs;
     const int at = order * A.C + c;   // place of this run's map among those of its channel
+    const float *first = entering(A);
+    float s = first ? first[b * A.C + c] : 0.f;   // every run reads it, and the last may write its own state there: before the joins
     float a = 1.f, h = 0.f;
     bool cut = false;
     if (mine && t0 < end) narrow_map<E, 8>(A, b, c, t0, end, a, h, cut);
@@ -1179,10 +1184,9 @@ template <class E, class Args> __global__ __launch_bounds__(BLOCK_THREADS<Args>)
         __syncthreads();
     }
     if (mine) { sa[at] = a; sh[at] = h; }
+    arrived(s);
     __syncthreads();
     if (!mine) return;
-    const float *first = entering(A);
-    float s = first ? first[b * A.C + c] : 0.f;
     if (order) s = through(s, sa[at - A.C], sh[at - A.C], sa[at - A.C] < 0.f);
     if (t0 < end) narrow_run<E, 8>(A, b, c, t0, end, s);
     float *last = leaving(A);

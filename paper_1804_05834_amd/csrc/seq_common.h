@@ -39,6 +39,14 @@ __device__ __forceinline__ void unpack_e5m2(uint32_t w, float (&o)[4])
 // Barrier that orders LDS traffic only: global loads and stores stay in flight across it.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Loaded values that have to be here before what follows, a barrier say: it need not wait for loads.
+__device__ __forceinline__ void arrived(float v) { asm volatile("" ::"v"(v) : "memory"); }
+template <int V> __device__ __forceinline__ void arrived(const float (&v)[V])
+{
+#pragma unroll
+    for (int k = 0; k < V; ++k) arrived(v[k]);
+}
+
 // the larger one, or a NaN if one is a NaN
 __device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : (b > a || b != b) ? b : a; }
 

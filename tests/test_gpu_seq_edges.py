@@ -61,3 +61,17 @@ def test_scan_a_gate_that_is_not_a_number(seq, B, T, C, dtype):  # noqa: F811
     f[0, T // 2, 0] = f[-1, T - 1, C - 1] = f[B // 2, 0, C // 2] = NAN
     reset[0, T // 2] = False
     check_scan(seq, f, x, h0, reset, dh, dlast, dtype == "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,T,C", [(9, 512, 16), (30, 300, 3), (32, 333, 3), (300, 250, 16), (32, 300, 16), (40, 13, 16), (5, 9, 1), (300, 4000, 1), (9, 513, 16), (3, 20000, 1), (300, 20, 64), (260, 40, 65)])
+def test_scan_state_in_place_of_every_form(seq, B, T, C, dtype):  # noqa: F811
+    """The final state may take the initial one's place where several waves begin from that."""
+    print("case in place", B, T, C, dtype, flush=True)
+    f, x, h0, reset = scan_case(B, T, C, "half", True, 0.5 / T, dtype, 430)
+    f = f - 2.0 + 4.0 * (T > 100)      # the initial state counts to the end
+    h, last, carry = seq.scan(f, x, h0=h0, reset=reset, save=True)
+    for _ in range(8):
+        s = h0.clone()
+        h1, last1, carry1 = seq.scan(f, x, h0=s, reset=reset, save=True, last=s)
+        assert last1 is s and torch.equal(s, last) and torch.equal(h1, h) and torch.equal(carry1, carry)
