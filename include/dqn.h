@@ -402,8 +402,9 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream);
  *   r = x + residual,  y = weight r rstd,  rstd = 1 / sqrt(mean(r^2) + eps)
  * y is taken of the fp32 sum, r is rounded once as it is stored.  Either y (in
  * dtype) or q and scale are written: 8-bit numbers (e4m3) with y ~ q scale and
- * scale = max |y| / 448 (a row of zeros has scale 0), the rows dqn_rows_product
- * reads.  A row that holds a NaN or an infinity has a NaN as scale. */
+ * scale = max(max |y|, 2^-117) / 448 (a row of zeros has scale 0), the rows
+ * dqn_rows_product reads.  A row that holds a NaN or an infinity has a NaN as
+ * scale. */
 typedef struct {
     int32_t dtype, C;                   /* 1 <= C <= DQN_NORM_MAX                   */
     int64_t M;                          /* rows, >= 0                               */
@@ -445,7 +446,8 @@ int32_t dqn_norm_sizes(int64_t M, int32_t C, size_t *workspace);
 int32_t dqn_norm_forward(const dqn_norm_args *args, void *stream);
 int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream);
 
-/* Rows [M][K] to 8 bits, as dqn_norm_forward writes them: scale = max |x| / 448 per row. */
+/* Rows [M][K] to 8 bits, 1 <= K <= DQN_NORM_MAX, as dqn_norm_forward writes them: scale = max(max |x|, 2^-117) / 448
+ * per row, 0 for a row of zeros. */
 int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, int64_t x_rs, uint8_t *q,
                           int64_t q_rs, float *scale, void *stream);
 

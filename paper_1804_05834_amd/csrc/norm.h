@@ -123,6 +123,7 @@ template <class E, int V, int K, int W, bool EIGHT> __global__ __launch_bounds__
                 for (int i = 0; i < V; ++i) top = nan_max(top, fabsf(r[k][i]));
             top = row_fold<W>(top, A.lanes, sh[turn + 1], nan_max);
             if (!(top <= 3.4028234e38f)) top = __builtin_nanf("");
+            if (top > 0.f) top = fmaxf(top, E4M3_LEAST);
             const float inv = top == 0.f ? 0.f : 1.f / top * E4M3_MAX;
             if (s.first == 0) A.scale[m] = top * (1.f / E4M3_MAX);
 #pragma unroll

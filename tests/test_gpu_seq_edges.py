@@ -75,3 +75,27 @@ def test_scan_state_in_place_of_every_form(seq, B, T, C, dtype):  # noqa: F811
         s = h0.clone()
         h1, last1, carry1 = seq.scan(f, x, h0=s, reset=reset, save=True, last=s)
         assert last1 is s and torch.equal(s, last) and torch.equal(h1, h) and torch.equal(carry1, carry)
+
+
+# ------------------------------------------------------------------ 8-bit rows
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("K", [40, 64, 200, 1500])
+def test_rows_of_small_numbers(seq, K, dtype):  # noqa: F811
+    """Rows whose largest number is near the smallest of the type, with zeros among them: q scale is the number to half a step of
+    e4m3 (2^-4 of it; 2^-10 scales below e4m3's normal numbers) and the rounding of the scale, and a zero is a zero."""
+    tops = [1e-30, 1e-35, 5e-36, 1.4e-36, 1e-36, 1e-37, 2e-38, 1e-38, 1e-40]
+    unit = rnd(440, len(tops), K).clamp(-3, 3)
+    unit[:, 1::3] = 0
+    unit[:, 0] = 3.0
+    x = (unit.double() * torch.tensor(tops).double().cuda()[:, None] / 3).to(TYPES[dtype])
+    for q, scale, name in ((*seq.rows(x), "rows"), (*seq.norm_rows(x, torch.ones(K, device="cuda"), eps=1.0)[:2], "norm")):
+        hx = host(x)      # the norm's mean square is nothing beside 1
+        hq, hs = host(q), host(scale)
+        assert (hs > 0).all(), name
+        assert (hq[hx == 0] == 0).all(), name
+        bound = np.maximum(np.abs(hx) * 2.0 ** -4, hs[:, None] * 2.0 ** -10) * 1.01 + 2.0 ** -148
+        off = np.abs(hq * hs[:, None] - hx)
+        assert (off <= bound).all(), (name, float((off / bound).max()))
+    zero = torch.zeros(2, K, dtype=TYPES[dtype], device="cuda")
+    q, scale = seq.rows(zero)
+    assert bool((q.float() == 0).all()) and bool((scale == 0).all())
