@@ -473,8 +473,9 @@ int32_t dqn_rows_product(const dqn_product_args *args, void *stream);
  * Parameters are fp32.  The moments of all tensors lie one behind the other, a
  * tensor beginning at a multiple of 256 elements (the places between hold the
  * caller's zeros).  bits = 32: fp32.  bits = 8: m as e4m3, v as e5m2, each with one fp32
- * scale per 256 elements, scale = largest / 448 and largest / 57344; the step is
- * computed in fp32 and p takes the moments before they are rounded.  They are rounded
+ * scale per 256 elements, scale = largest / 448 and largest / 57344 (a largest that is
+ * not zero counts as at least 2^-117 and 2^-110); the step is computed in fp32 and p
+ * takes the moments before they are rounded.  They are rounded
  * up or down at random, in proportion, since one step changes v by about 0.1 %,
  * far less than half the distance of two 8-bit numbers, and rounding to the nearest
  * would keep v where it is for ever; a v that is not zero stays so.  The random bits of

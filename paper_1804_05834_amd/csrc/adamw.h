@@ -147,6 +147,8 @@ template <class G, int BITS> struct AdamLane {
             for (int j = 0; j < 4; ++j) { mt = larger(mt, fabsf(mn[j])); vt = larger(vt, vn[j]); }
             mt = group_fold(mt, 64, larger);
             vt = group_fold(vt, 64, larger);
+            if (mt > 0.f) mt = fmaxf(mt, E4M3_LEAST);
+            if (vt > 0.f) vt = fmaxf(vt, E5M2_LEAST);
             const float mi = mt > 0.f ? product(1.f / mt, E4M3_MAX) : 0.f, vi = vt > 0.f ? product(1.f / vt, E5M2_MAX) : 0.f;
             const uint64_t z0 = misc::mix64(A.seed, (uint64_t)place / 2), z1 = misc::mix64(A.seed, (uint64_t)place / 2 + 1);
             uint32_t mb[4], vb[4];

@@ -14,7 +14,7 @@ template <class T, int N> using vec = T __attribute__((ext_vector_type(N)));
 constexpr float E4M3_MAX = 448.f, E5M2_MAX = 57344.f;
 // The least value that the largest of the numbers that share a scale counts as, unless all are zero.  Below it the scale would
 // lose its digits (it is 2^-125.8 there) and its inverse would be infinite, times zero a NaN.
-constexpr float E4M3_LEAST = 0x1p-117f;
+constexpr float E4M3_LEAST = 0x1p-117f, E5M2_LEAST = 0x1p-110f;
 
 // bytes a and b of a word as e4m3 / e5m2 numbers, and back.  The conversions to 8 bits are exact where the value is a
 // number of the type, else to the nearest, ties to even; nothing above the largest number is passed to them.

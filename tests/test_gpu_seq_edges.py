@@ -99,3 +99,27 @@ def test_rows_of_small_numbers(seq, K, dtype):  # noqa: F811
     zero = torch.zeros(2, K, dtype=TYPES[dtype], device="cuda")
     q, scale = seq.rows(zero)
     assert bool((q.float() == 0).all()) and bool((scale == 0).all())
+
+
+# ------------------------------------------------------------------ AdamW
+@pytest.mark.parametrize("size", [1e-12, 1e-16, 1e-17, 1e-18, 1e-20, 1e-37, 1e-39])
+def test_adamw_moments_of_small_gradients(seq, size):  # noqa: F811
+    """8-bit moments of gradients near the smallest numbers, with zeros among them: a zero stays zero, the others are within a step
+    of their type of the moment in 64 bits (a step is 2^-3 / 2^-2 of the number, or the smallest number of the type), and
+    a second moment that fp32 can hold does not become zero."""
+    n = 1024
+    unit = torch.exp(rnd(450, n).clamp(-2, 2)) * torch.where(rnd(451, n) > 0, 1.0, -1.0)
+    unit[::3] = 0
+    g = (unit.double() * size).float()
+    p = torch.zeros(n, device="cuda")
+    opt = seq.AdamW([p], [g], bits=8, lr=0.0)
+    opt.step(1, seed=9)
+    hg = host(g)
+    for got, scale, want, step, least in ((opt.m, opt.m_scale, 0.1 * hg, 2.0 ** -3, 2.0 ** -9), (opt.v, opt.v_scale, 0.001 * hg * hg, 2.0 ** -2, 2.0 ** -16)):
+        hs = np.repeat(host(scale), 256)
+        off = np.abs(host(got) * hs - want)
+        # squares and products below 2^-126 are multiples of 2^-149: two of them, rounded, and a scale's own rounding
+        bound = np.maximum(np.abs(want) * step, hs * least) * 1.01 + 2.0 ** -147
+        assert (host(got)[hg == 0] == 0).all()
+        assert (off <= bound).all(), float((off / bound).max())
+        assert (host(got)[np.abs(want) > 2.0 ** -126] != 0).all() or step == 2.0 ** -3
