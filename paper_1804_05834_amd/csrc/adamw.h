@@ -109,7 +109,7 @@ template <class G, int BITS> struct AdamLane {
         }
     }
 
-    __device__ __forceinline__ void step(const AdamArgs &A, const AdamChunk &ch, float keep, int lane)
+    __device__ __forceinline__ void step(const AdamArgs &A, const AdamChunk &ch, float decay, int lane)
     {
         float mn[4], vn[4];
         if constexpr (BITS == 8) {
@@ -124,7 +124,8 @@ template <class G, int BITS> struct AdamLane {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             moments(mn[j], vn[j], (float)g[j], A.b1, A.c1, A.b2, A.c2);
-            p[j] = p[j] * keep - A.rate * mn[j] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(vn[j]), A.root, A.eps));
+            // the whole change first: 1 - lr decay as one number would keep few digits of a small decay, or none
+            p[j] -= fmaf(decay, p[j], A.rate * mn[j] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(vn[j]), A.root, A.eps)));
         }
         if (whole) {
             *reinterpret_cast<Global<vec<float, 4>> *>(global(ch.param) + first) = p;
@@ -188,18 +189,18 @@ template <class G, int BITS> __global__ __launch_bounds__(256) void k_adamw(Adam
 {
     const AdamChunk ch = A.chunks[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const float keep = 1.f - A.lr * ch.decay;
+    const float decay = A.lr * ch.decay;
     const int first = wave * ADAM_DEEP, blocks = min(ADAM_DEEP, (ch.n + ADAM_BLOCK - 1) / ADAM_BLOCK - first);
     AdamLane<G, BITS> b[ADAM_DEEP];
     if (blocks == ADAM_DEEP) {
 #pragma unroll
         for (int k = 0; k < ADAM_DEEP; ++k) b[k].fetch(A, ch, first + k);
 #pragma unroll
-        for (int k = 0; k < ADAM_DEEP; ++k) b[k].step(A, ch, keep, lane);
+        for (int k = 0; k < ADAM_DEEP; ++k) b[k].step(A, ch, decay, lane);
     } else {
         for (int k = 0; k < blocks; ++k) {
             b[0].fetch(A, ch, first + k);
-            b[0].step(A, ch, keep, lane);
+            b[0].step(A, ch, decay, lane);
         }
     }
 }

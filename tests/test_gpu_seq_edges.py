@@ -123,3 +123,28 @@ def test_adamw_moments_of_small_gradients(seq, size):  # noqa: F811
         assert (host(got)[hg == 0] == 0).all()
         assert (off <= bound).all(), float((off / bound).max())
         assert (host(got)[np.abs(want) > 2.0 ** -126] != 0).all() or step == 2.0 ** -3
+
+
+@pytest.mark.parametrize("lr", [1e-5, 1e-6])
+def test_adamw_small_decay(seq, lr):  # noqa: F811
+    """A decay far below a parameter's rounding is not lost beside the gradient's part, and is as large as it should be.  A step is
+    5 roundings of the change's size and one of the parameter's off, which is at random over many parameters:
+    a mean over 65,536 of them, 200 steps each, is 2^-25 sqrt(200 / 65536) off (standard deviation at most), six of which are allowed."""
+    n, steps, decay = 65536, 200, 0.1
+    p0 = 1.0 + torch.rand(n, generator=torch.Generator().manual_seed(460)).cuda() * 0.9
+    p, g = p0.clone(), torch.zeros(n, device="cuda")
+    opt = seq.AdamW([p], [g], lr=lr, weight_decay=decay)
+    moved = seq.AdamW([q := p0.clone()], [g], lr=lr, weight_decay=0.0)
+    want, m, v = p0.double(), torch.zeros(n, dtype=torch.float64, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+    still = p0.double()
+    for t in range(1, steps + 1):
+        g.copy_(rnd(1000 + t, n))
+        opt.step(t)
+        moved.step(t)
+        m, v = 0.9 * m + 0.1 * g.double(), 0.999 * v + 0.001 * g.double() ** 2
+        change = lr / (1 - 0.9 ** t) * m / ((v / (1 - 0.999 ** t)).sqrt() + 1e-8)
+        want, still = want * (1 - lr * decay) - change, still - change
+    noise = 6 * 2.0 ** -24 * (steps / n) ** 0.5
+    for got, exact in ((p, want), (q, still)):
+        off = float((got.double() - exact).mean())
+        assert abs(off) < noise + 1e-3 * lr * decay * steps, (off, noise)
