@@ -70,6 +70,13 @@ __device__ __forceinline__ float product(float a, float b)
 }
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN if one is a NaN
 
+// sqrt(v) root + eps.  The instruction takes a v below 2^-126 for zero, and a small eps would be all that is left.
+__device__ __forceinline__ float root_plus(float v, float root, float eps)
+{
+    const bool small = v < 0x1p-96f;
+    return fmaf(__builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v), small ? root * 0x1p-32f : root, eps);
+}
+
 // An address that comes from memory could be one in LDS for all that the compiler knows; these are not.
 template <class T> using Global = __attribute__((address_space(1))) T;
 template <class T> __device__ __forceinline__ Global<T> *global(T *p) { return (Global<T> *)(uintptr_t)p; }
@@ -125,7 +132,7 @@ template <class G, int BITS> struct AdamLane {
         for (int j = 0; j < 4; ++j) {
             moments(mn[j], vn[j], (float)g[j], A.b1, A.c1, A.b2, A.c2);
             // the whole change first: 1 - lr decay as one number would keep few digits of a small decay, or none
-            p[j] -= fmaf(decay, p[j], A.rate * mn[j] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(vn[j]), A.root, A.eps)));
+            p[j] -= fmaf(decay, p[j], A.rate * mn[j] * __builtin_amdgcn_rcpf(root_plus(vn[j], A.root, A.eps)));
         }
         if (whole) {
             *reinterpret_cast<Global<vec<float, 4>> *>(global(ch.param) + first) = p;

@@ -148,3 +148,20 @@ def test_adamw_small_decay(seq, lr):  # noqa: F811
     for got, exact in ((p, want), (q, still)):
         off = float((got.double() - exact).mean())
         assert abs(off) < noise + 1e-3 * lr * decay * steps, (off, noise)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_second_moment_below_the_normal_numbers(seq, bits):  # noqa: F811
+    """With an eps that small the step is lr whatever the gradient's size, for a second moment below 2^-126 too.  There it is a
+    multiple of 2^-149, which its root is 2^-150 / v off by, and the bound has four times that."""
+    n = 512
+    g = torch.logspace(-18.5, -16, n, device="cuda")
+    p = torch.zeros(n, device="cuda")
+    opt = seq.AdamW([p], [g], bits=bits, lr=1.0, eps=1e-25, weight_decay=0.0)
+    opt.step(1, seed=1)
+    hg = host(g)
+    v = 0.001 * hg * hg
+    root = np.sqrt(v / 0.001) + 1e-25
+    want = -hg / root
+    bound = np.abs(want) * (24 * ref.U + 2.0 ** -148 / v)
+    assert (np.abs(host(p) - want) <= bound).all(), float((np.abs(host(p) - want) / bound).max())
