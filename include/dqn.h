@@ -358,7 +358,7 @@ typedef struct {
     int64_t T;                          /* steps, >= 0 (0: h_last = h0)             */
     const void *f, *x;                  /* [B][T][C]                                */
     int64_t f_bs, f_ts, x_bs, x_ts;     /* strides of a sequence and of a step; that
-                                           of a step at most 2^24                   */
+                                           of a step at most 2^24 (any with T = 1)  */
     const float *h0;                    /* [B][C], or NULL = zeros                  */
     const uint8_t *reset;               /* [B][T], or NULL = no episode starts      */
     int64_t reset_bs, reset_ts;

@@ -64,9 +64,11 @@ constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes bey
 bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && (!a || !b || a * b <= MOST) && (!a || !b || !c || a * b <= MOST / c); }
 
 // Called with elements present: a [B][T][C] tensor, its strides no shorter than what they step over, and apart for a
-// tensor that is written (no element twice).
+// tensor that is written (no element twice).  Where there is one step, or one sequence, its stride is not taken.
 const char *check_steps(const void *p, int64_t bs, int64_t ts, const dqn_scan_args &s, bool written)
 {
+    if (s.B == 1) bs = 0;
+    if (s.T == 1) ts = 0;
     if (!p || !at(p, bytes_of(s.dtype))) return "a tensor is NULL or not aligned to its elements";
     if (bs < 0 || ts < 0 || bs > MOST || ts > 1 << 24) return "a stride is negative or too large";   // 16 rows are within 2^30 bytes
     if (ts > 0 && s.T - 1 > MOST / ts) return "T times a stride is too large";

@@ -165,3 +165,16 @@ def test_adamw_second_moment_below_the_normal_numbers(seq, bits):  # noqa: F811
     want = -hg / root
     bound = np.abs(want) * (24 * ref.U + 2.0 ** -148 / v)
     assert (np.abs(host(p) - want) <= bound).all(), float((np.abs(host(p) - want) / bound).max())
+
+
+# ------------------------------------------------------------------ views
+def test_one_step_of_views_whose_steps_are_far_apart(seq):  # noqa: F811
+    """With one step there is no next one: its stride is whatever the tensor it was cut from has."""
+    B, C = 6, 40
+    f, x, dh = (rnd(470 + k, B, 1, C) for k in range(3))
+    far = [v.as_strided((B, 1, C), (C, 1 << 30, 1)) for v in (f, x, dh)]
+    h, last, carry = seq.scan(f, x, save=True)
+    h1, last1, carry1 = seq.scan(*far[:2], save=True, out=torch.empty_like(h).as_strided((B, 1, C), (C, 1 << 30, 1)))
+    assert torch.equal(h, h1) and torch.equal(last, last1)
+    for a, b in zip(seq.scan_backward(dh, f, x, carry), seq.scan_backward(far[2], *far[:2], carry1)):
+        assert torch.equal(a, b)
