@@ -89,6 +89,17 @@ def _scratch(n, device):
     return t, t.data_ptr()
 
 
+def _like(t):
+    """(an output of t's shape and type, its address, its strides): in t's order of dimensions, but for rows, which stay in one piece
+    (where t's rows lie on top of each other, a signal's windows say, its order may have them in columns)."""
+    o = torch.empty_like(t)
+    st = o.stride()
+    if st[-1] != 1:
+        o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        st = o.stride()
+    return o, o.data_ptr(), st
+
+
 # ------------------------------------------------------------------ gated linear recurrence
 @functools.lru_cache(maxsize=256)
 def _scan_sizes(kind, B, T, Ch):
@@ -120,8 +131,7 @@ def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
     xp, xs = _rows(x, "x", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
     if out is None:
-        h = torch.empty_like(f)
-        hp, hs = h.data_ptr(), h.stride()
+        h, hp, hs = _like(f)
     else:
         h = out
         hp, hs = _rows(h, "out", dt, shape, dev)
@@ -151,9 +161,12 @@ def scan_backward(dh, f, x, carry, reset=None, dlast=None, out=None):
     xp, xs = _rows(x, "x", dt, shape, dev)
     gp, gs = _rows(dh, "dh", dt, shape, dev)
     carry_n, work_n = _scan_sizes(kind, B, T, Ch)
-    df, dx = (torch.empty_like(f), torch.empty_like(x)) if out is None else out
-    dfp, dfs = _rows(df, "df", dt, shape, dev)
-    dxp, dxs = _rows(dx, "dx", dt, shape, dev)
+    if out is None:
+        (df, dfp, dfs), (dx, dxp, dxs) = _like(f), _like(x)
+    else:
+        df, dx = out
+        dfp, dfs = _rows(df, "df", dt, shape, dev)
+        dxp, dxs = _rows(dx, "dx", dt, shape, dev)
     dh0 = torch.empty_strided((B, Ch), (Ch, 1), dtype=torch.float32, device=f.device)
     work, wp = _scratch(work_n, f.device)
     rp, rb, rt = _reset(reset, B, T, dev)
@@ -184,8 +197,8 @@ def _residual(x, residual, shape, dev):
     if residual is None:
         return 0, 0, x, 0, 0
     p, st = _rows(residual, "residual", x.dtype, shape, dev)
-    r = torch.empty_like(x)
-    return p, st[0], r, r.data_ptr(), r.stride()[0]
+    r, rp, rs = _like(x)
+    return p, st[0], r, rp, rs[0]
 
 
 def norm(x, weight, residual=None, eps=1e-6):
@@ -195,10 +208,10 @@ def norm(x, weight, residual=None, eps=1e-6):
     M, Ch = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
     sp, ss, r, rp, rs = _residual(x, residual, shape, dev)
-    y = torch.empty_like(x)
+    y, yp, ys = _like(x)
     rstd = torch.empty(M, dtype=torch.float32, device=x.device)
     args = NORM_ARGS.pack(kind, Ch, M, xp, sp, xs[0], ss, _flat(weight, "weight", torch.float32, (Ch,), dev), eps, rp, rs,
-                          y.data_ptr(), y.stride()[0], 0, 0, 0, rstd.data_ptr())
+                          yp, ys[0], 0, 0, 0, rstd.data_ptr())
     _call(lib().dqn_norm_forward(args, _raw_stream(dev)))
     # in bf16 the backward pass forms the sum again from its two terms, since r is rounded
     return y, r, (rstd, x, residual) if kind == BF16 else (rstd, r, None)
@@ -236,11 +249,11 @@ def norm_backward(dy, r, saved, weight, dr=None):
     xp, xs = _rows(x, "x", dt, shape, dev)
     sp, ss = (0, (0,)) if residual is None else _rows(residual, "residual", dt, shape, dev)
     rp, rs = (0, (0,)) if dr is None else _rows(dr, "dr", dt, shape, dev)
-    dx = torch.empty_like(r)
+    dx, dxp, dxs = _like(r)
     dw = torch.empty(Ch, dtype=torch.float32, device=r.device)
     work, wp = _scratch(_norm_sizes(M, Ch), r.device)
     args = NORM_GRAD_ARGS.pack(kind, Ch, M, gp, xp, sp, rp, gs[0], xs[0], ss[0], rs[0], _flat(weight, "weight", torch.float32, (Ch,), dev),
-                               _flat(rstd, "rstd", torch.float32, (M,), dev), dx.data_ptr(), dx.stride()[0], dw.data_ptr(), wp)
+                               _flat(rstd, "rstd", torch.float32, (M,), dev), dxp, dxs[0], dw.data_ptr(), wp)
     _call(lib().dqn_norm_backward(args, _raw_stream(dev)))
     return dx, dw
 

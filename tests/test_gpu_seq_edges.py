@@ -178,3 +178,34 @@ def test_one_step_of_views_whose_steps_are_far_apart(seq):  # noqa: F811
     assert torch.equal(h, h1) and torch.equal(last, last1)
     for a, b in zip(seq.scan_backward(dh, f, x, carry), seq.scan_backward(far[2], *far[:2], carry1)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_windows_that_slide_over_a_signal(seq, dtype):  # noqa: F811
+    """Inputs whose rows lie on top of each other, a step of one element apart, fewer than a row has elements."""
+    bf = dtype == "bf16"
+    signal, w = rnd(480, 200, dtype=TYPES[dtype]), rnd(481, 48, scale=0.2, at=1.0)
+    x, res = signal.unfold(0, 48, 1)[:9], signal.unfold(0, 48, 1)[20:29]
+    y, r, saved = seq.norm(x, w, residual=res)
+    wr, wy, wrstd, er, ey, _ = ref.norm(host(x), host(w), host(res))
+    close(r, wr, ref.stored(er, wr, bf), "r")
+    close(y, wy, ref.stored(ey, wy, bf), "y")
+    dx, dw = seq.norm_backward(x, r, saved, w, dr=res)
+    (wdx, wdw), (edx, edw) = ref.norm_backward(host(x), wr, host(saved[0]), host(w), host(res))
+    close(dx, wdx, ref.stored(edx, wdx, bf), "dx")
+    close(dw, wdw, edw + 1e-37, "dw")
+    y, r, saved = seq.norm(x, w)
+    dx, dw = seq.norm_backward(res, x, saved, w)
+    wr, wy, wrstd, er, ey, _ = ref.norm(host(x), host(w))
+    (wdx, wdw), (edx, edw) = ref.norm_backward(host(res), wr, host(saved[0]), host(w))
+    close(y, wy, ref.stored(ey, wy, bf), "y")
+    close(dx, wdx, ref.stored(edx, wdx, bf), "dx")
+    q, scale, r8 = seq.norm_rows(x, w, residual=res)
+    assert q.shape == (9, 48) and r8.stride(1) == 1
+    f, v = (signal[k:].as_strided((5, 12, 48), (1, 2, 1)) for k in (0, 30))
+    h, last, carry = seq.scan(f, v, save=True)
+    want, wl, _, eh, el, _ = ref.scan(host(f), host(v))
+    close(h, want, ref.stored(eh, want, bf), "h")
+    wants, bounds = ref.scan_backward(host(v), host(f), host(v))
+    for got, a, b in zip(seq.scan_backward(v, f, v, carry), wants, bounds):
+        close(got, a, ref.stored(b, a, bf and got.ndim == 3), "gradient")
