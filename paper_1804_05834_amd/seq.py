@@ -331,10 +331,11 @@ class AdamW:
         _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, kind, C.byref(b), _raw_stream(dev)))
         self._h = h
 
-    def step(self, step, seed=0, lr=None):
-        """Step number `step` (from 1).  seed: of the random rounding of 8-bit moments, another one for each step."""
+    def step(self, step, seed=None, lr=None):
+        """Step number `step` (from 1).  seed: of the random rounding of 8-bit moments, another one for each step (None: the
+        step's number).  A step recorded into a graph repeats its number, rate and seed with every replay."""
         _call(lib().dqn_adamw_step(self._h, self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, step,
-                                   seed & 0xFFFFFFFFFFFFFFFF, _raw_stream(_current_device())))
+                                   (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, _raw_stream(_current_device())))
 
     def close(self):
         if getattr(self, "_h", None):

@@ -209,3 +209,16 @@ def test_windows_that_slide_over_a_signal(seq, dtype):  # noqa: F811
     wants, bounds = ref.scan_backward(host(v), host(f), host(v))
     for got, a, b in zip(seq.scan_backward(v, f, v, carry), wants, bounds):
         close(got, a, ref.stored(b, a, bf and got.ndim == 3), "gradient")
+
+
+def test_adamw_steps_without_a_seed_round_differently(seq):  # noqa: F811
+    """A step's own number is its seed: with the same bits at every step a second moment that was once rounded to itself always is."""
+    def run(seeds):
+        g = rnd(490, 4096)
+        opt = seq.AdamW([torch.zeros(4096, device="cuda")], [g], bits=8)
+        for t in range(1, 6):
+            opt.step(t, **({} if seeds is None else dict(seed=seeds[t - 1])))
+        return opt.v.view(torch.uint8).clone()
+
+    assert torch.equal(run(None), run([1, 2, 3, 4, 5]))
+    assert not torch.equal(run(None), run([0, 0, 0, 0, 0]))
