@@ -329,13 +329,16 @@ class AdamW:
         self.lr, self.betas, self.eps, self.bits = lr, betas, eps, bits
         h = C.c_void_p()
         _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, kind, C.byref(b), _raw_stream(dev)))
-        self._h = h
+        self._h, self._device = h, dev
 
     def step(self, step, seed=None, lr=None):
         """Step number `step` (from 1).  seed: of the random rounding of 8-bit moments, another one for each step (None: the
         step's number).  A step recorded into a graph repeats its number, rate and seed with every replay."""
+        dev = _current_device()
+        if dev != self._device:
+            raise ValueError("step: the optimizer's tensors are not on the current GPU")
         _call(lib().dqn_adamw_step(self._h, self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, step,
-                                   (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, _raw_stream(_current_device())))
+                                   (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, _raw_stream(dev)))
 
     def close(self):
         if getattr(self, "_h", None):

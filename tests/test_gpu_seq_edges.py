@@ -222,3 +222,16 @@ def test_adamw_steps_without_a_seed_round_differently(seq):  # noqa: F811
 
     assert torch.equal(run(None), run([1, 2, 3, 4, 5]))
     assert not torch.equal(run(None), run([0, 0, 0, 0, 0]))
+
+
+def test_adamw_steps_on_its_own_gpu_only(seq, monkeypatch):  # noqa: F811
+    """As with every other call, tensors of another GPU than the current one are refused, before anything is launched."""
+    p = torch.zeros(10, device="cuda")
+    opt = seq.AdamW([p], [torch.ones(10, device="cuda")])
+    monkeypatch.setattr(seq, "_current_device", lambda: p.get_device() + 1)
+    monkeypatch.setattr(seq, "_raw_stream", lambda device: pytest.fail("a launch was prepared"))
+    with pytest.raises(ValueError, match="current GPU"):
+        opt.step(1)
+    monkeypatch.undo()
+    opt.step(1)
+    assert bool((p != 0).all())
