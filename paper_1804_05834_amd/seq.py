@@ -9,11 +9,14 @@
 Argument marshalling only, as in dqn.py: the arithmetic runs in the HIP kernels of the library, on the
 current stream; torch allocates outputs.  Activations are float32 or bfloat16, states, weights of the norm
 and scales float32.  The last dimension of a tensor has stride 1, the others any (a half of a wider tensor is fine).
+Nothing is recorded for autograd: results are detached (a call that autograd would have recorded warns), and the
+*_backward calls give the gradients.
 A wrong shape, type or device raises ValueError; what the library refuses raises dqn.DqnError.
 """
 import ctypes as C
 import functools
 import struct
+import warnings
 
 import torch
 
@@ -81,6 +84,13 @@ def _kind(t, name):
     return k
 
 
+def _detached(call, backward):
+    """An input requires a gradient: says that the result will not, unless nobody expects it to."""
+    if torch.is_grad_enabled():
+        warnings.warn("%s records nothing for autograd: its results are detached from its inputs; %s, or call it under torch.no_grad()"
+                      % (call, "%s gives the gradients" % backward if backward else "it has no gradient"), stacklevel=3)
+
+
 def _scratch(n, device):
     """(a workspace of n bytes or None, its address or 0)"""
     if not n:
@@ -123,6 +133,8 @@ def scan(f, x, h0=None, reset=None, save=False, out=None, last=None):
     f, x: [B][T][C]; h0: [B][C] float32 or None (zeros); reset: [B][T] uint8 / bool or None.  out: a tensor for h;
     last: one for the final state, which may be h0 itself.  -> (h, final state [B][C] float32), and with save=True a
     third value that scan_backward needs."""
+    if f.requires_grad or x.requires_grad or (h0 is not None and h0.requires_grad):
+        _detached("scan", "scan_backward")
     kind, dt, shape, dev = _kind(f, "f"), f.dtype, f.shape, _current_device()
     if len(shape) != 3:
         raise ValueError("f: [B][T][C] expected")
@@ -204,6 +216,8 @@ def _residual(x, residual, shape, dev):
 def norm(x, weight, residual=None, eps=1e-6):
     """Per row of x [M][C]: r = x + residual, y = weight r / sqrt(mean r^2 + eps).  -> (y, r, what norm_backward needs);
     without a residual r is x."""
+    if x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad):
+        _detached("norm", "norm_backward")
     (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, Ch = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
@@ -219,6 +233,8 @@ def norm(x, weight, residual=None, eps=1e-6):
 
 def norm_rows(x, weight, residual=None, eps=1e-6):
     """The same with y in 8 bits: -> (q [M][C] e4m3, scale [M], r) with y ~ q scale[:, None]."""
+    if x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad):
+        _detached("norm_rows", None)
     (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, Ch = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
@@ -261,6 +277,8 @@ def norm_backward(dy, r, saved, weight, dr=None):
 # ------------------------------------------------------------------ 8-bit rows and their product
 def rows(x):
     """x [M][K] in 8 bits: -> (q [M][K] e4m3, scale [M]) with x ~ q scale[:, None]."""
+    if x.requires_grad:
+        _detached("rows", None)
     (kind, shape), dev = _matrix(x, "x"), _current_device()
     M, K = shape
     xp, xs = _rows(x, "x", x.dtype, shape, dev)
@@ -273,6 +291,8 @@ def rows(x):
 def product(a, w, bias=None, dtype=torch.bfloat16, out=None):
     """a = (q [M][K], scale [M]) and w = (q [N][K], scale [N]) as rows() and norm_rows() give them, bias [N] float32 or None
     -> y [M][N] of `dtype`."""
+    if bias is not None and bias.requires_grad:
+        _detached("product", None)
     (qa, sa), (qw, sw), dev = a, w, _current_device()
     kind, shape, N = _TYPES.get(dtype), qa.shape, sw.shape[0] if sw.shape else 0
     if kind is None or len(shape) != 2:

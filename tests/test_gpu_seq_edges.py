@@ -235,3 +235,29 @@ def test_adamw_steps_on_its_own_gpu_only(seq, monkeypatch):  # noqa: F811
     monkeypatch.undo()
     opt.step(1)
     assert bool((p != 0).all())
+
+
+# ------------------------------------------------------------------ autograd
+def test_a_gradient_that_nobody_records_is_not_lost_silently(seq):  # noqa: F811
+    """Calls on tensors that require a gradient warn while autograd records; their results are what they always are."""
+    import warnings
+    x, f, w, b = rnd(500, 2, 4, 16), rnd(501, 2, 4, 16), rnd(502, 16), rnd(503, 5)
+    w8 = seq.rows(rnd(504, 5, 16))
+    calls = {"scan": lambda x, w, b: seq.scan(f, x), "norm": lambda x, w, b: seq.norm(x.view(8, 16), w), "norm_rows": lambda x, w, b: seq.norm_rows(x.view(8, 16), w),
+             "rows": lambda x, w, b: seq.rows(x.view(8, 16)), "product": lambda x, w, b: (seq.product(seq.rows(f.view(8, 16)), w8, bias=b),)}
+    for name, call in calls.items():
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            want = call(x, w, b)
+            leaves = [t.clone().requires_grad_() for t in (x, w, b)]
+            with torch.no_grad():
+                call(*leaves)
+        with pytest.warns(UserWarning, match=name + " records nothing"):
+            got = call(*leaves)
+        # (the second output of norm is x itself where there is no residual)
+        assert torch.equal(got[0].view(torch.uint8), want[0].view(torch.uint8)) and not got[0].requires_grad, name
+    p = torch.nn.Parameter(torch.zeros(10, device="cuda"))
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        seq.AdamW([p], [torch.ones(10, device="cuda")]).step(1)      # an optimizer's tensors require gradients by their nature
+    assert bool((p != 0).all())
