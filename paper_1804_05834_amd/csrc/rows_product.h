@@ -101,7 +101,7 @@ __device__ __forceinline__ Acc four_of(const float *p, int n, int N)   // p[n ..
 // ------------------------------------------------------------ few outputs
 // A workgroup takes MI x 16 rows and NI x 16 columns; its waves share K, 128 bytes in turn, straight from memory into
 // registers, and add up in LDS.  For products that would not give every compute unit a tile of the kernel below: what
-// counts then is that much is in flight at once (32 x 1024 x 512: 3.4 us; 1 x 8192 x 8192, 64 MB of weights: 13 us).
+// counts then is that much is in flight at once (32 x 1024 x 512: 3.3 us; 1 x 4096 x 8192, 34 MB of weights: 7.4 us, 8.8 from memory).
 constexpr int FEW_WAVES = 8;
 template <class E, int MI, int NI> __global__ __launch_bounds__(64 * FEW_WAVES) void k_product_few(ProductArgs A)
 {
@@ -116,7 +116,6 @@ template <class E, int MI, int NI> __global__ __launch_bounds__(64 * FEW_WAVES) 
 #pragma unroll
     for (int x = 0; x < NI; ++x) w[x] = A.w + (long)min(n0 + 16 * x + i, A.N - 1) * A.w_rs;
     Acc s[MI][NI] = {};
-#pragma unroll 2
     for (int k = wave * 128; k < A.K; k += FEW_WAVES * 128) {
         const int at = k + 32 * g;
         vec<uint32_t, 4> va[MI][2], vw[NI][2];
