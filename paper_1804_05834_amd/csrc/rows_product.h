@@ -1,9 +1,11 @@
 // Product of 8-bit rows with 8-bit weights, y = (a w^T) a_scale w_scale + bias.
 //
-// The matrix instructions on e4m3 (16 x 16 outputs, 128 k) run at twice the rate of those on bf16, but they keep about 16
-// bits of a sum: measured 1.5e-5 off in the 2-norm at every K, where the same numbers as bf16, which holds them
-// exactly, are 5e-8 off.  An output that is rounded to bf16 loses a hundred times that anyway and takes them; an fp32
-// output takes the numbers as bf16.
+// The matrix instructions on e4m3 (16 x 16 outputs, 128 k) run at twice the rate of those on bf16, but they do not add up
+// in 32 bits: products are cut off 16 bits below the largest one's exponent (of products of 7.875 beside 256 x 256 and
+// its opposite each counted as 7: measured, 880 for 992).  So 128 of them are off by up to 2^-9 of the largest, which the
+// rounding of its operands to e4m3 has moved by up to 2^-4; over random numbers the sums are 1.5e-5 off in the 2-norm at every K,
+// where the same numbers as bf16, which holds them exactly, are 5e-8 off.  An output that is rounded to bf16 loses a hundred
+// times that anyway and takes them; an fp32 output, for which a caller may ask, takes the numbers as bf16.
 //
 // Operands are swapped, weights as the instruction's rows: a lane then has four neighbouring columns of a row of y and
 // stores them at once.  A lane holds 32 bytes of one row of either operand, lane l of row l % 16 bytes 32 (l / 16) and

@@ -261,3 +261,30 @@ def test_a_gradient_that_nobody_records_is_not_lost_silently(seq):  # noqa: F811
         warnings.simplefilter("error")
         seq.AdamW([p], [torch.ones(10, device="cuda")]).step(1)      # an optimizer's tensors require gradients by their nature
     assert bool((p != 0).all())
+
+
+# ------------------------------------------------------------------ product
+@pytest.mark.parametrize("big", [256.0, 288.0, 448.0])
+@pytest.mark.parametrize("M,N,K,at", [(9, 21, 128, 1), (9, 21, 128, 127), (50, 70, 400, 200), (300, 300, 1024, 1023), (1100, 1111, 640, 129), (40, 50, 8000, 7999)])
+def test_product_of_sums_that_cancel(seq, M, N, K, at, big):  # noqa: F811
+    """Two large products that cancel, among many of one size, at any distance.  fp32 outputs: sums in fp32.  bf16 outputs:
+    128 products at a time, each kept to 16 bits below the largest one's exponent, so a part is off by less than 128 2^-16 of its largest
+    product; the parts are added up in fp32."""
+    print("case cancel", M, N, K, at, big, flush=True)
+    g = torch.Generator().manual_seed(510)
+    size = lambda n: torch.exp2(torch.randint(-6, 8, (n, 1), generator=g).float()) * (1 + torch.randint(0, 8, (n, 1), generator=g) / 8)  # noqa: E731
+    a, w = size(M).expand(M, K).clone(), size(N).expand(N, K).clone()
+    a[:, 0], a[:, at], w[:, 0], w[:, at] = big, -big, big, big
+    pad = torch.zeros(M + N, (K + 15) // 16 * 16, dtype=torch.uint8)
+    pad[:, :K] = torch.cat([a, w]).to(torch.float8_e4m3fn).view(torch.uint8)
+    q = pad.cuda().view(torch.float8_e4m3fn)[:, :K]
+    one = torch.ones(M + N, device="cuda")
+    ha, hw = host(q)[:M], host(q)[M:]
+    assert np.array_equal(ha, a.numpy()) and np.array_equal(hw, w.numpy())      # numbers of e4m3
+    want, most = ha @ hw.T, np.abs(ha) @ np.abs(hw).T
+    parts = sum((np.abs(ha[:, None, k:k + 128]) * np.abs(hw[None, :, k:k + 128])).max(2) for k in range(0, K, 128))
+    sums = ref.U * (K / 32 + 40) * most
+    for dtype in (torch.float32, torch.bfloat16):
+        bf = dtype == torch.bfloat16
+        y = seq.product((q[:M], one[:M]), (q[M:], one[M:]), dtype=dtype)
+        close(y, want, ref.stored(sums + (2.0 ** -9 * parts if bf else 0.0), want, bf), "bf16" if bf else "fp32")
