@@ -340,7 +340,9 @@ int32_t dqn_destroy(dqn_ctx *ctx);
  * contiguous.  A stride may be larger than the row, so that a tensor can be a
  * part of a wider one.  Inputs and outputs of a call must not overlap except
  * where it says so.  Structs of arguments are host pointers, read during the
- * call.  Nothing is allocated; every call can be recorded into a HIP graph. */
+ * call.  Nothing is allocated.  Every call can be recorded into a HIP graph but
+ * dqn_adamw_init, which waits for its stream; a recorded dqn_adamw_step repeats its
+ * step number, rate and seed, and so its random bits, with every replay. */
 
 /* dtype of activations and their gradients: fp32, or bf16 with sums, states and
  * statistics in fp32. */
