@@ -102,11 +102,6 @@ template <int V> __device__ __forceinline__ void state(const float *p, float (&s
 template <int V> __device__ __forceinline__ void keep_state(float *p, const float (&s)[V]) { __builtin_memcpy(p, s, sizeof(s)); }
 
 // ------------------------------------------------------------ short sequences
-__device__ __forceinline__ long sequence_of(long id, long all, int per)   // id / per; in 32 bits where that is enough
-{
-    return all >> 32 ? id / per : (long)((unsigned)id / (unsigned)per);
-}
-
 // A thread takes V channels of a sequence through all of its at most SCAN_SHORT steps; all of its loads go out before
 // the first is used.  The step of an acting agent is T = 1 (32 environments of 512 channels: 2.9 us, a launch and two trips
 // to memory).
@@ -114,7 +109,7 @@ template <class E, int V> __global__ __launch_bounds__(256) void k_scan_short(Sc
 {
     const long id = (long)blockIdx.x * 256 + threadIdx.x, all = (long)A.B * (A.C / V);
     if (id >= all) return;
-    const long b = sequence_of(id, all, A.C / V);
+    const long b = (unsigned)id / (unsigned)(A.C / V);   // there are at most 2^28
     const int c = (int)(id - b * (A.C / V)) * V, T = (int)A.T;
     const E *f = (const E *)A.f + b * A.f_bs + c, *x = (const E *)A.x + b * A.x_bs + c;
     vec<E, V> fr[SCAN_SHORT], xr[SCAN_SHORT];
@@ -143,7 +138,7 @@ template <class E, int V> __global__ __launch_bounds__(256) void k_scan_grad_sho
 {
     const long id = (long)blockIdx.x * 256 + threadIdx.x, all = (long)A.B * (A.C / V);
     if (id >= all) return;
-    const long b = sequence_of(id, all, A.C / V);
+    const long b = (unsigned)id / (unsigned)(A.C / V);   // there are at most 2^28
     const int c = (int)(id - b * (A.C / V)) * V, T = (int)A.T;
     const E *f = (const E *)A.f + b * A.f_bs + c, *x = (const E *)A.x + b * A.x_bs + c, *dh = (const E *)A.dh + b * A.dh_bs + c;
     vec<E, V> fr[SCAN_SHORT], xr[SCAN_SHORT], gr[SCAN_SHORT];
