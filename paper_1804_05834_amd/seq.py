@@ -349,8 +349,9 @@ class AdamW:
         b.plan = self._plan.data_ptr()
         self.lr, self.betas, self.eps, self.bits = lr, betas, eps, bits
         h = C.c_void_p()
-        _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, kind, C.byref(b), _raw_stream(dev)))
-        self._h, self._device = h, dev
+        stream = _raw_stream(dev)
+        _call(lib().dqn_adamw_init(C.byref(h), table, n, bits, kind, C.byref(b), stream))
+        self._h, self._device, self._stream = h, dev, stream
 
     def step(self, step, seed=None, lr=None):
         """Step number `step` (from 1).  seed: of the random rounding of 8-bit moments, another one for each step (None: the
@@ -358,8 +359,13 @@ class AdamW:
         dev = _current_device()
         if dev != self._device:
             raise ValueError("step: the optimizer's tensors are not on the current GPU")
+        stream = _raw_stream(dev)
+        if stream != self._stream:      # what the optimizer holds must outlast this step, also if it is dropped before
+            for t in (self._plan, self.m, self.v, self.m_scale, self.v_scale):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream())
         _call(lib().dqn_adamw_step(self._h, self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, step,
-                                   (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, _raw_stream(dev)))
+                                   (step if seed is None else seed) & 0xFFFFFFFFFFFFFFFF, stream))
 
     def close(self):
         if getattr(self, "_h", None):

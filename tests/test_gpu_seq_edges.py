@@ -288,3 +288,27 @@ def test_product_of_sums_that_cancel(seq, M, N, K, at, big):  # noqa: F811
         bf = dtype == torch.bfloat16
         y = seq.product((q[:M], one[:M]), (q[M:], one[M:]), dtype=dtype)
         close(y, want, ref.stored(sums + (2.0 ** -9 * parts if bf else 0.0), want, bf), "bf16" if bf else "fp32")
+
+
+def test_adamw_dropped_while_another_stream_steps(seq):  # noqa: F811
+    """The table and the moments of an optimizer that is gone are not given to others before its last step has read them."""
+    n = 300000
+    p, g = rnd(520, n), rnd(521, n)
+    want = p.clone()
+    seq.AdamW([want], [g], bits=8).step(1)
+    a = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        q = p.clone()
+        opt = seq.AdamW([q], [g], bits=8)
+        held = [(t.data_ptr(), t.numel()) for t in (opt._plan, opt.m, opt.v)]
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                a @ a
+            opt.step(1)
+        del opt
+        others = [torch.zeros(k, dtype=torch.uint8, device="cuda") for _, k in held for _ in range(4)]
+        assert not {t.data_ptr() for t in others} & {at for at, _ in held}
+        torch.cuda.synchronize()
+        assert torch.equal(q, want)
