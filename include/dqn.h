@@ -351,7 +351,8 @@ enum { DQN_F32 = 0, DQN_BF16 = 1 };
 /* Gated linear recurrence over time, per channel, with a_t = sigmoid(f_t):
  *   h_t = a_t k_t h_{t-1} + (1 - a_t) x_t,   t = 0 .. T-1,   h_{-1} = h0
  * k_t = 0 where reset_t != 0 (step t is the first of an episode: whatever the
- * state was, a NaN too, is forgotten), else 1.  The state is fp32.  T = 1 is the
+ * state was, a NaN too, is forgotten; until then one that is not finite stays not
+ * finite, infinite or NaN), else 1.  The state is fp32.  T = 1 is the
  * step of an acting agent; h_last may be h0 then, and for any T. */
 typedef struct {
     int32_t dtype;                      /* DQN_F32 / DQN_BF16, of f, x, h           */

@@ -4,7 +4,7 @@
 // A wave takes blocks of 256 elements, four per lane: the elements that share a scale, so that the largest is found within
 // the wave.  A workgroup's share, a chunk, has a record of its own in the plan (addresses, length, decay): a look-up
 // of the chunk's tensor and then of the tensor would be two trips to memory before the first element is asked for.
-// Measured: 100M parameters in 150 tensors, 8 bits, bf16 gradients 259 us (5.4 TB/s); the Q-network's 1.7M in 32 bits 8.6.
+// Measured: 100M parameters in 150 tensors, 8 bits, bf16 gradients 263 us (5.3 TB/s); the Q-network's 1.7M in 32 bits 8.9.
 #pragma once
 #include "seq_common.h"
 #include "sumtree.h"

@@ -3,7 +3,7 @@
 // All of it is bound by memory: every element is read once and written once, a row being kept in registers between its
 // sums and its results.  A row belongs to W waves (1, 4 or 16), a lane holding K times V consecutive elements; V is 16
 // bytes' worth, or 1 where the size, a stride or an address does not allow that.  Short rows (K = 1) share a wave.
-// Measured: 16384 rows of 512 in bf16 with a residual 12.0 us forward (5.6 TB/s) and 16.1 backward (5.2); 30011 rows of
+// Measured: 16384 rows of 512 in bf16 with a residual 12.2 us forward (5.5 TB/s) and 16.7 backward (5.0); 30011 rows of
 // 1001 in fp32 81 us (5.9 TB/s) and 103 (5.8); a copy reaches 5.2.
 #pragma once
 #include "seq_common.h"

@@ -103,7 +103,7 @@ template <int V> __device__ __forceinline__ void keep_state(float *p, const floa
 
 // ------------------------------------------------------------ short sequences
 // A thread takes V channels of a sequence through all of its at most SCAN_SHORT steps; all of its loads go out before
-// the first is used.  The step of an acting agent is T = 1 (32 environments of 512 channels: 2.9 us, a launch and two trips
+// the first is used.  The step of an acting agent is T = 1 (32 environments of 512 channels: 3.1 us, a launch and two trips
 // to memory).
 template <class E, int V> __global__ __launch_bounds__(256) void k_scan_short(ScanArgs A)
 {
@@ -187,10 +187,10 @@ template <class E, int V> __global__ __launch_bounds__(256) void k_scan_grad_sho
 // and L = 16 / V steps: with V = 2 half a wave is a row of the strip and a wave holds two runs of eight steps, with
 // V = 1 (a size, a stride or an address that is not a multiple of two elements) a wave is one run of sixteen.
 //
-// Vector instructions cost nearly as much as memory does here (about twenty per element, two of them exp and the
+// Vector instructions cost nearly as much as memory does here (about twenty-one per element, two of them exp and the
 // reciprocal), so the choices that few tiles need are kept out of the others' way: a tile that ends beyond the sequence or
 // that holds the start of an episode takes the careful form of the loops (Edge), the rest the one without tests.
-// Measured, 32 sequences of 512 steps of 512 channels in bf16: forward 14.1 us (3.6 TB/s), backward 21.0 (4.0).
+// Measured, 32 sequences of 512 steps of 512 channels in bf16: forward 14.8 us (3.4 TB/s), backward 21.8 (3.8).
 template <int V> struct Strip {
     static constexpr int L = SCAN_RUN / V, G = SCAN_STRIP / V, S = 64 / G;
 };
@@ -531,7 +531,7 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
 
 // ------------------------------------------------------------ lines
 // A lane takes two channels through a range of steps, step after step, LINE steps' loads ahead: no work but the
-// recurrence itself (fourteen vector instructions per element, where a strip takes twenty).  With enough sequences
+// recurrence itself (fifteen vector instructions per element, where a strip takes twenty-one).  With enough sequences
 // and channels a wave takes whole sequences.  Else time is cut into ranges, and the state that enters one is not known yet:
 // a first launch finds the map of every range, a second composes the maps of those before and then runs.  f and x
 // are read twice then, which long sequences of few channels have to: the other way would be to wait for the
@@ -545,7 +545,7 @@ template <class E, int V> __global__ __launch_bounds__(64 * SCAN_WAVES) void k_s
 // and of an odd number of channels the last lane has the last two but stores the last alone (`half`).
 //
 // Measured: 512 sequences of 64 steps of 512 channels in bf16, a wave each, 18 us forward (5.6 TB/s), 36 backward (4.7); one
-// sequence of 131072 steps of 512 channels, in ranges, 56 for the maps (4.8 TB/s) and 68 for the states (5.9).
+// sequence of 131072 steps of 512 channels, in ranges, 58 for the maps (4.6 TB/s) and 70 for the states (5.8).
 constexpr int LINE = 8;         // steps between two states of `carry`, and of a wave's loads
 constexpr int LINE_GROUP = 8;   // ranges of a workgroup; waves of one whose waves take whole sequences
 

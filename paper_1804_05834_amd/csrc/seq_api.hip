@@ -38,14 +38,16 @@ bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 // forward / backward in bf16, C = 512, B x T:
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
 //   128 x 256, 512 lines:  strips 27 / 40, lines 44 / 73     32 x 512, 256 strips: strips 13 / 21, ranges 20 / 26
-// below that ranges, see SCAN_UNITS.
+// below that ranges, see SCAN_UNITS.  A compute unit holds one workgroup of a strip, so that strips go in turns of 256: B x 512, strips and
+// ranges, 31: 13 / 20, 19 / 27; 33: 23 / 35, 28 / 35; 63: 25 / 38, 33 / 43; 65: 35 / 53, 44 / 65; 100: 46 / 71, 50 / 71.  Below 256, and for
+// long sequences in a part of a turn (40 x 4000: 166 / 285, 145 / 240), the other form than the one taken is the faster.
 // Narrow sequences: up to 16 channels, up to 32 of more than 1000 steps; us forward / backward, narrow against ranges of lines,
 // B x T x C in bf16: 2000 x 3000 x 8: 184 / 283, 240 / 298; 200 x 4000 x 5: 38 / 51, 48 / 70; 574 x 2844 x 17: 125 / 160, 150 / 189.  Ranges
 // of lines where a strip is filled for five eighths (100 x 3000 x 32: 42 / 52, 26 / 35; 2000 x 1000 x 16: 122 / 166, 89 / 120) or sequences and
 // steps are few (1 x 131072 x 2: 44 / 53, 25 / 31; 10 x 30000 x 3: 29 / 34, 22 / 26; 64 x 20000 x 4: 35 / 49, 56 / 79).  Short ones a
 // workgroup each (see there).
 constexpr int64_t SCAN_FEW = 1 << 18, SCAN_LINES = 2048, SCAN_STRIPS = 256, SCAN_WANT = 4096, SCAN_LEAST = 32;
-// Ranges of lines: the compute units hold one workgroup of eight waves each of the backward kernel, two of the others', and a
+// Ranges of lines: the compute units hold one workgroup of eight waves each of the backward kernel, two of the lines' other kernels, and a
 // second turn of a few workgroups takes as long as the first.  So ranges are as short as leaves one workgroup for each unit, or two
 // if that is still 64 steps a range (131072 x 512 in bf16, forward: 122 us, 125 with one).  us forward / backward by the
 // steps of a range (workgroups), in bf16:
