@@ -401,6 +401,69 @@ int32_t dqn_scan_sizes(int32_t dtype, int32_t B, int64_t T, int32_t C, size_t *c
 int32_t dqn_scan_forward(const dqn_scan_args *args, void *stream);
 int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream);
 
+/* Gated delta rule: a memory of one matrix per head, S [Dk][Dv] in fp32, with
+ * a_t = sigmoid(f_t) and beta_t = sigmoid(b_t):
+ *   S_t = a_t (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T,   o_t = scale S_t^T q_t
+ * for t = 0 .. T-1, S_{-1} = s0.  The state is zero before a step whose reset flag is set
+ * (whatever it was, a NaN too).  A step that holds a NaN or an infinity spoils the
+ * outputs of its own episode from that step on (a q its own step's) and, in the backward call, the gradients
+ * of its own episode, nothing else.  Keys are taken as they are: the rule contracts the state for
+ * beta_t |k_t|^2 <= 2, beyond that it grows.  A stride of a head or of any other
+ * dimension of an input may be 0 (heads that share keys); the gradients are per head then as well.
+ * T = 1 is the step of an acting agent; s_last may be s0 then, and for any T. */
+#define DQN_DELTA_MAX 128
+typedef struct {
+    int32_t dtype;                      /* DQN_F32 / DQN_BF16, of q, k, v, f, b, o  */
+    int32_t B, H;                       /* sequences and heads, each 0..65535, the
+                                           product of both at most 2^20             */
+    int32_t Dk, Dv;                     /* 1..DQN_DELTA_MAX                         */
+    float scale;                        /* finite                                   */
+    int64_t T;                          /* steps, >= 0 (0: s_last = s0);
+                                           B H ceil(T / 64) at most 2^24            */
+    const void *q, *k, *v;              /* [B][T][H][Dk], the same, [B][T][H][Dv]   */
+    const void *f, *b;                  /* [B][T][H]                                */
+    int64_t q_s[3], k_s[3], v_s[3], f_s[3], b_s[3];
+                                        /* strides of a sequence, a step, a head    */
+    const float *s0;                    /* [B][H][Dk][Dv], or NULL = zeros          */
+    const uint8_t *reset;               /* [B][T], or NULL = no episode starts      */
+    int64_t reset_bs, reset_ts;
+    void *o;                            /* [B][T][H][Dv]                            */
+    int64_t o_s[3];
+    float *s_last;                      /* [B][H][Dk][Dv], or NULL                  */
+    float *carry;                       /* for dqn_delta_backward, or NULL: states at
+                                           some of the steps, bytes from
+                                           dqn_delta_sizes                          */
+    void *workspace;                    /* forward_workspace bytes from
+                                           dqn_delta_sizes, 16-byte aligned; free for
+                                           other use after the call                 */
+} dqn_delta_args;
+
+/* Gradients of the rule: of all five inputs and of s0, from the gradient of o and of s_last.
+ * The states are computed again from `carry` as the forward call left it. */
+typedef struct {
+    int32_t dtype, B, H, Dk, Dv;
+    float scale;
+    int64_t T;
+    const void *q, *k, *v, *f, *b;
+    int64_t q_s[3], k_s[3], v_s[3], f_s[3], b_s[3];
+    const float *carry;
+    const uint8_t *reset;
+    int64_t reset_bs, reset_ts;
+    const void *dout;                   /* [B][T][H][Dv]                            */
+    int64_t dout_s[3];
+    const float *dlast;                 /* [B][H][Dk][Dv], or NULL = zeros          */
+    void *dq, *dk, *dv, *df, *db;       /* as q, k, v, f, b                         */
+    int64_t dq_s[3], dk_s[3], dv_s[3], df_s[3], db_s[3];
+    float *ds0;                         /* [B][H][Dk][Dv], or NULL                  */
+    void *workspace;                    /* backward_workspace bytes                 */
+} dqn_delta_grad_args;
+
+/* Bytes of `carry` and of either call's workspace for these sizes. */
+int32_t dqn_delta_sizes(int32_t dtype, int32_t B, int64_t T, int32_t H, int32_t Dk, int32_t Dv, size_t *carry,
+                        size_t *forward_workspace, size_t *backward_workspace);
+int32_t dqn_delta_forward(const dqn_delta_args *args, void *stream);
+int32_t dqn_delta_backward(const dqn_delta_grad_args *args, void *stream);
+
 /* Root-mean-square norm with the residual's addition, per row of C elements:
  *   r = x + residual,  y = weight r rstd,  rstd = 1 / sqrt(mean(r^2) + eps)
  * y is taken of the fp32 sum, r is rounded once as it is stored.  Either y (in

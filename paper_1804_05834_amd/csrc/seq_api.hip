@@ -9,8 +9,8 @@
 #include <type_traits>
 #include <vector>
 
-#include "../../include/dqn.h"
 #include "adamw.h"
+#include "checks.h"
 #include "norm.h"
 #include "rows_product.h"
 #include "scan.h"
@@ -23,17 +23,6 @@ struct dqn_adamw {
 
 namespace {
 
-int32_t bad(const char *call, const char *why) { return dqn_seq_fail(DQN_ERR_INVALID_ARG, call, why); }
-
-int32_t launched(const char *call)
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? (int32_t)DQN_OK : dqn_seq_fail(DQN_ERR_HIP, call, hipGetErrorString(e));
-}
-
-bool dtype_ok(int32_t d) { return d == DQN_F32 || d == DQN_BF16; }
-size_t bytes_of(int32_t d) { return d == DQN_F32 ? 4 : 2; }
-bool at(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
 // Which form a recurrence takes, by how many lines (sequences times strips of 128 channels) and strips (of 64) there are; us
 // forward / backward in bf16, C = 512, B x T:
 //   512 x 64, 2048 lines:  whole lines 18 / 36              256 x 128, 1024 lines: strips 31 / 44, lines 24 / 46
@@ -61,9 +50,7 @@ constexpr long SCAN_LONG_RANGE = 64;
 // 166 / 400; 60 x 25811 x 1: 55 / 61 against 38 / 48).
 constexpr int64_t SCAN_LONG = 6 << 20;
 constexpr int64_t LAST_LEVEL = 256 << 20;   // bytes of the cache in front of memory
-constexpr int64_t MOST = 1ll << 48;   // no size, stride or product of sizes beyond this: byte offsets stay far below 2^63
 
-bool size_ok(int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && (!a || !b || a * b <= MOST) && (!a || !b || !c || a * b <= MOST / c); }
 
 // Called with elements present: a [B][T][C] tensor, its strides no shorter than what they step over, and apart for a
 // tensor that is written (no element twice).  Where there is one step, or one sequence, its stride is not taken.
@@ -231,13 +218,6 @@ template <class E, class Args, class F> void launch_recurrence(const Args &A, co
     else launch_lines<E>(A, st);
 }
 
-const char *check_rows(const void *p, int64_t rs, int64_t M, int32_t C, int32_t dtype, bool written)
-{
-    if (!p || !at(p, bytes_of(dtype))) return "a tensor is NULL or not aligned to its elements";
-    if (rs < 0 || rs > MOST || (rs > 0 && M - 1 > MOST / rs)) return "a stride is negative or too large";
-    return !written || M == 1 || rs >= C ? nullptr : "rows of an output lie on top of each other";
-}
-
 const char *check_rows8(const void *p, int64_t rs, int64_t M, int64_t K)
 {
     if (!p || !at(p, 16) || rs % 16 || rs < 0 || rs > MOST || (rs > 0 && M - 1 > MOST / rs)) return "8-bit rows must be 16-byte aligned, strides multiples of 16";
@@ -302,23 +282,12 @@ template <class E> void launch_norm_grad(seq::NormGradArgs A, int parts, hipStre
     });
 }
 
-// A tile kernel needs more LDS than a workgroup gets without asking; asked for once per kernel (and again by a racing thread, which does no harm).
 template <class E, int BM, int BN, int WM, int WN> bool launch_tile(const seq::ProductArgs &A, hipStream_t st)
 {
     constexpr int bytes = 2 * (BM + BN) * 128;
     auto kernel = seq::k_product_tile<E, BM, BN, WM, WN>;
-    if (bytes > 65536) {
-        static std::atomic<uint64_t> granted{0};   // a bit per device
-        int dev = 0;
-        if (hipGetDevice(&dev) != hipSuccess || dev > 63) return false;
-        if (!(granted.load(std::memory_order_relaxed) >> dev & 1)) {
-            if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
-                (void)hipGetLastError();
-                return false;
-            }
-            granted.fetch_or(1ull << dev, std::memory_order_relaxed);
-        }
-    }
+    static std::atomic<uint64_t> granted{0};
+    if (!lds_granted((const void *)kernel, bytes, granted)) return false;
     const int64_t tiles = (A.M + BM - 1) / BM * ((A.N + BN - 1) / BN);
     kernel<<<dim3((unsigned)tiles), 64 * WM * WN, bytes, st>>>(A);
     return true;

@@ -21,7 +21,8 @@ EXPORTS = ["dqn_query_sizes", "dqn_init", "dqn_act", "dqn_train_step", "per_samp
            "dqn_replay_store", "dqn_replay_state", "dqn_schedule_default", "dqn_schedule_at", "dqn_preprocess",
            "dqn_get_activations", "dqn_act_static", "dqn_selftest_fused_conv_schedule", "dqn_replay_store_envs",
            "dqn_scan_sizes", "dqn_scan_forward", "dqn_scan_backward", "dqn_norm_sizes", "dqn_norm_forward", "dqn_norm_backward",
-           "dqn_rows_quantize", "dqn_rows_product", "dqn_adamw_sizes", "dqn_adamw_init", "dqn_adamw_step", "dqn_adamw_destroy"]
+           "dqn_rows_quantize", "dqn_rows_product", "dqn_adamw_sizes", "dqn_adamw_init", "dqn_adamw_step", "dqn_adamw_destroy",
+           "dqn_delta_sizes", "dqn_delta_forward", "dqn_delta_backward"]
 
 
 class DqnConfig(C.Structure):
@@ -124,6 +125,9 @@ def lib():
             "dqn_scan_sizes": [i32, i32, i64, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
             "dqn_scan_forward": [C.c_char_p, vp],
             "dqn_scan_backward": [C.c_char_p, vp],
+            "dqn_delta_sizes": [i32, i32, i64, i32, i32, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "dqn_delta_forward": [C.c_char_p, vp],
+            "dqn_delta_backward": [C.c_char_p, vp],
             "dqn_norm_sizes": [i64, i32, C.POINTER(C.c_size_t)],
             "dqn_norm_forward": [C.c_char_p, vp],
             "dqn_norm_backward": [C.c_char_p, vp],

@@ -1,6 +1,7 @@
 """The operators of a recurrent Q-network (the second half of include/dqn.h) on torch tensors.
 
   scan, scan_backward       gated linear recurrence over time, per channel
+  delta, delta_backward     gated delta rule: a memory of one matrix per head
   norm, norm_backward       root-mean-square norm with the residual's addition
   norm_rows, rows           the same, or no norm, with the output in 8-bit rows
   product                   8-bit rows times 8-bit weights
@@ -30,6 +31,8 @@ _vp, _i64, _f32 = C.c_void_p, C.c_int64, C.c_float
 # filling a ctypes.Structure.  i: int32, q: int64, f: float, P: pointer, in C's own layout.
 SCAN_ARGS = struct.Struct("iiiqPPqqqqPPqqPqqPPP")
 SCAN_GRAD_ARGS = struct.Struct("iiiqPPqqqqPPqqPqqPPPqqqqPP")
+DELTA_ARGS = struct.Struct("iiiiifqPPPPPqqqqqqqqqqqqqqqPPqqPqqqPPP")
+DELTA_GRAD_ARGS = struct.Struct("iiiiifqPPPPPqqqqqqqqqqqqqqqPPqqPqqqPPPPPPqqqqqqqqqqqqqqqPP")
 NORM_ARGS = struct.Struct("iiqPPqqPfPqPqPqPP")
 NORM_GRAD_ARGS = struct.Struct("iiqPPPPqqqqPPPqPP")
 PRODUCT_ARGS = struct.Struct("iiiqPPqqPPPPq")
@@ -65,7 +68,7 @@ def _refuse(t, name, dtype, shape, device, why):
 def _rows(t, name, dtype, shape, device):
     """(address, strides) of a tensor whose last dimension lies in one piece."""
     st = t.stride()
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device and (st[-1] == 1 or shape[-1] <= 1):
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and (st[-1] == 1 or shape[-1] <= 1 or not t.numel()):
         return t.data_ptr(), st
     _refuse(t, name, dtype, shape, device, "the last dimension must have stride 1")
 
@@ -187,6 +190,94 @@ def scan_backward(dh, f, x, carry, reset=None, dlast=None, out=None):
                                dfp, dxp, dfs[0], dfs[1], dxs[0], dxs[1], dh0.data_ptr(), wp)
     _call(lib().dqn_scan_backward(args, _raw_stream(dev)))
     return df, dx, dh0
+
+
+# ------------------------------------------------------------------ gated delta rule
+@functools.lru_cache(maxsize=256)
+def _delta_sizes(kind, B, T, H, Dk, Dv):
+    carry, forward, backward = C.c_size_t(), C.c_size_t(), C.c_size_t()
+    _call(lib().dqn_delta_sizes(kind, B, T, H, Dk, Dv, C.byref(carry), C.byref(forward), C.byref(backward)))
+    return carry.value, forward.value, backward.value
+
+
+def _strided(t, name, dtype, shape, device):
+    """(address, strides) of a tensor [B][T][H], any strides."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        return t.data_ptr(), t.stride()
+    _refuse(t, name, dtype, shape, device, "")
+
+
+def _delta_inputs(q, k, v, f, b):
+    """-> (type, (B, T, H, Dk, Dv), device, addresses, strides) of what both directions read"""
+    kind, dt, dev = _kind(q, "q"), q.dtype, _current_device()
+    if len(q.shape) != 4 or len(v.shape) != 4:
+        raise ValueError("q and k: [B][T][H][Dk], v: [B][T][H][Dv] expected")
+    B, T, H, Dk = q.shape
+    Dv = v.shape[3]
+    qp, qs = _rows(q, "q", dt, (B, T, H, Dk), dev)
+    kp, ks = _rows(k, "k", dt, (B, T, H, Dk), dev)
+    vp, vs = _rows(v, "v", dt, (B, T, H, Dv), dev)
+    fp, fs = _strided(f, "f", dt, (B, T, H), dev)
+    bp, bs = _strided(b, "b", dt, (B, T, H), dev)
+    return kind, (B, T, H, Dk, Dv), dev, (qp, kp, vp, fp, bp), (*qs[:3], *ks[:3], *vs[:3], *fs, *bs)
+
+
+def delta(q, k, v, f, b, s0=None, reset=None, scale=1.0, save=False, out=None, last=None):
+    """S_t = a_t (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T, o_t = scale S_t^T q_t per head, with a = sigmoid(f) and
+    beta = sigmoid(b), the state zero before a step whose reset flag is set.
+
+    q, k: [B][T][H][Dk], v: [B][T][H][Dv], f, b: [B][T][H], all of one type; s0: [B][H][Dk][Dv] float32 or None (zeros);
+    reset: [B][T] uint8 / bool or None.  Keys are taken as they are (norm_heads makes them).  out: a tensor for o; last: one for the
+    final state, which may be s0 itself.  -> (o, final state [B][H][Dk][Dv] float32), and with save=True a third
+    value that delta_backward needs."""
+    if q.requires_grad or k.requires_grad or v.requires_grad or f.requires_grad or b.requires_grad or (s0 is not None and s0.requires_grad):
+        _detached("delta", "delta_backward")
+    kind, (B, T, H, Dk, Dv), dev, at, strides = _delta_inputs(q, k, v, f, b)
+    state = (B, H, Dk, Dv)
+    carry_n, work_n, _ = _delta_sizes(kind, B, T, H, Dk, Dv)
+    if out is None:
+        o, op, os_ = _like(v)
+    else:
+        o = out
+        op, os_ = _rows(o, "out", v.dtype, (B, T, H, Dv), dev)
+    if last is None:
+        last = torch.empty(state, dtype=torch.float32, device=q.device)
+        lp = last.data_ptr()
+    else:
+        lp = _flat(last, "last", torch.float32, state, dev)
+    carry = torch.empty(carry_n // 4, dtype=torch.float32, device=q.device) if save else None
+    rp, rb, rt = _reset(reset, B, T, dev)
+    work, wp = _scratch(work_n, q.device)
+    args = DELTA_ARGS.pack(kind, B, H, Dk, Dv, scale, T, *at, *strides, 0 if s0 is None else _flat(s0, "s0", torch.float32, state, dev),
+                           rp, rb, rt, op, *os_[:3], lp, carry.data_ptr() if save else 0, wp)
+    _call(lib().dqn_delta_forward(args, _raw_stream(dev)))
+    return (o, last, carry) if save else (o, last)
+
+
+def delta_backward(do, q, k, v, f, b, carry, reset=None, dlast=None, scale=1.0, out=None):
+    """Gradients of delta: do [B][T][H][Dv] of o, dlast [B][H][Dk][Dv] float32 of the final state (or None), the inputs, reset and
+    scale as they were, carry from delta(save=True).  out: (dq, dk, dv, df, db) to write into, None for what is to be allocated.
+    -> (dq, dk, dv, df, db, ds0 [B][H][Dk][Dv] float32)"""
+    kind, (B, T, H, Dk, Dv), dev, at, strides = _delta_inputs(q, k, v, f, b)
+    state, dt = (B, H, Dk, Dv), q.dtype
+    gp, gs = _rows(do, "do", dt, (B, T, H, Dv), dev)
+    carry_n, _, work_n = _delta_sizes(kind, B, T, H, Dk, Dv)
+    grads, gat, gstrides = [], [], []
+    for name, x, y in zip(("dq", "dk", "dv", "df", "db"), (q, k, v, f, b), out or (None,) * 5):
+        if y is None:
+            y = torch.empty(x.shape, dtype=dt, device=x.device)
+        p, st = (_rows if y.dim() == 4 else _strided)(y, name, dt, x.shape, dev)
+        grads.append(y)
+        gat.append(p)
+        gstrides += st[:3]
+    ds0 = torch.empty(state, dtype=torch.float32, device=q.device)
+    work, wp = _scratch(work_n, q.device)
+    rp, rb, rt = _reset(reset, B, T, dev)
+    args = DELTA_GRAD_ARGS.pack(kind, B, H, Dk, Dv, scale, T, *at, *strides, _flat(carry, "carry", torch.float32, (carry_n // 4,), dev), rp, rb, rt,
+                                gp, *gs[:3], 0 if dlast is None else _flat(dlast, "dlast", torch.float32, state, dev),
+                                *gat, *gstrides, ds0.data_ptr(), wp)
+    _call(lib().dqn_delta_backward(args, _raw_stream(dev)))
+    return (*grads, ds0)
 
 
 # ------------------------------------------------------------------ norm

@@ -1,0 +1,288 @@
+"""The matrix memory's operators on the GPU against their definitions in 64 bits (memory_ref.py), at the sizes, masks, strides and
+values where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import memory_ref as ref
+from paper_1804_05834_amd import dqn, seq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def to(x, dtype=torch.float32):
+    return torch.from_numpy(np.asarray(x)).to(dtype).to(DEV)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ------------------------------------------------------------------ gated delta rule
+class Delta:
+    """Inputs of the rule on the GPU and, as the numbers they hold there, in 64 bits."""
+
+    def __init__(self, seed, dtype, B, T, H, Dk, Dv, state=True, resets=0.05, lean=0.3):
+        r = np.random.RandomState(seed)
+        self.dt, self.size = TYPES[dtype], (B, T, H, Dk, Dv)
+        tilt = lean * r.randn(H, Dk)
+
+        def unit():      # a little below one: rounding to bf16 does not make a key longer than one
+            x = r.randn(B, T, H, Dk) + tilt
+            return 0.99 * x / np.sqrt((x * x).sum(3, keepdims=True))
+
+        self.q, self.k = to(unit(), self.dt), to(unit(), self.dt)
+        self.v, self.f, self.b = to(r.randn(B, T, H, Dv), self.dt), to(1.5 * r.randn(B, T, H) + 2, self.dt), to(r.randn(B, T, H), self.dt)
+        self.do = to(0.3 * r.randn(B, T, H, Dv), self.dt)
+        self.s0, self.dlast = (to(0.5 * r.randn(B, H, Dk, Dv)), to(0.3 * r.randn(B, H, Dk, Dv))) if state else (None, None)
+        self.reset = to(r.rand(B, T) < resets, torch.uint8) if resets else None
+        self.scale = Dk ** -0.5
+
+    def inputs(self):
+        return self.q, self.k, self.v, self.f, self.b
+
+    def exact(self):
+        h = [host(x) for x in self.inputs()]
+        s0, reset, dl = (None if x is None else host(x) for x in (self.s0, self.reset, self.dlast))
+        o, last, eo, el = ref.delta(*h, s0, reset, self.scale)[:4]
+        return (o, last), (eo, el), *ref.delta_backward(host(self.do), *h, s0, reset, dl, self.scale)
+
+    def run(self, **kw):
+        o, last, carry = seq.delta(*self.inputs(), s0=self.s0, reset=self.reset, scale=self.scale, save=True)
+        return o, last, seq.delta_backward(self.do, *self.inputs(), carry, reset=self.reset, dlast=self.dlast, scale=self.scale, **kw)
+
+    def check(self, o, last, grads):
+        out, bound, gwant, gbound = self.exact()
+        low = self.dt is torch.bfloat16
+        ref.within(host(o), out[0], bound[0], (3,), low, "o")
+        ref.within(host(last), out[1], bound[1], (2, 3), False, "last")
+        for name, got, want, most in zip(("dq", "dk", "dv", "df", "db"), grads, gwant, gbound):
+            ref.within(host(got), want, most, (3,) if got.dim() == 4 else (), low, name)
+        ref.within(host(grads[5]), gwant[5], gbound[5], (2, 3), False, "ds0")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 63, 64, 65, 130, 257])
+def test_delta_lengths(dtype, T):
+    c = Delta(T, dtype, 2, T, 3, 16, 24)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("Dk,Dv", [(1, 1), (3, 5), (31, 33), (32, 32), (33, 64), (64, 64), (64, 65), (65, 3), (100, 72), (128, 128), (7, 128)])
+def test_delta_widths(dtype, Dk, Dv):
+    c = Delta(Dk, dtype, 1, 70, 2, Dk, Dv)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("state,resets", [(False, 0), (True, 0), (False, 0.3), (True, 1.0)])
+def test_delta_states_and_episodes(dtype, state, resets):
+    c = Delta(5, dtype, 3, 100, 2, 12, 20, state=state, resets=resets)
+    o, last, grads = c.run()
+    c.check(o, last, grads)
+    if resets == 1.0:      # nothing passes a step
+        assert (grads[3] == 0).all() and (grads[5] == 0).all()
+    a, b, _ = c.run()
+    assert torch.equal(a, o) and torch.equal(b, last)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_delta_keys_that_repeat(dtype):
+    """The same key at every step and rates near one: N is full, what is written replaces what was."""
+    c = Delta(6, dtype, 1, 150, 2, 16, 16)
+    c.k[:] = c.k[:, :1].clone()
+    c.b[:] = 4.0
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_delta_gates_of_any_size(dtype):
+    """Gates that are shut, open and in between, side by side, and rates of exactly zero and one."""
+    c = Delta(7, dtype, 1, 130, 2, 16, 16, resets=0)
+    some = torch.tensor([-200.0, -90.0, -30.0, -5.0, 0.0, 5.0, 30.0, 200.0, float("inf"), float("-inf")], device=DEV)
+    c.f[:] = some[torch.arange(130, device=DEV)[:, None] * 7 % 10].to(c.dt)
+    c.b[:] = some[torch.arange(130, device=DEV)[:, None] * 3 % 10].to(c.dt)
+    got = c.run()
+    c.check(*got)
+    assert (got[2][3][c.f.float() < -150] == 0).all()
+
+
+def test_delta_a_gate_shut_long_ago_leaves_the_others_exact():
+    c = Delta(8, "fp32", 1, 64, 1, 8, 8, resets=0)
+    c.f[:, :40] = -100.0
+    c.check(*c.run())
+
+
+def part(x, front, back):
+    """x as a part of a wider tensor along its last dimension."""
+    wide = torch.full((*x.shape[:-1], front + x.shape[-1] + back), float("nan"), dtype=x.dtype, device=DEV)
+    wide[..., front:front + x.shape[-1]] = x
+    return wide[..., front:front + x.shape[-1]]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("Dk,Dv,front,back", [(16, 24, 1, 2), (64, 64, 8, 8), (64, 64, 3, 0), (40, 72, 4, 4)])
+def test_delta_views(dtype, Dk, Dv, front, back):
+    c = Delta(9, dtype, 2, 80, 3, Dk, Dv)
+    plain = c.run()
+    c.q, c.k, c.do = part(c.q, front, back), part(c.k.transpose(0, 1).contiguous(), back, front).transpose(0, 1), part(c.do, 0, back)
+    c.v = part(c.v.transpose(1, 2).contiguous(), front, 1).transpose(1, 2)
+    c.f, c.b = torch.stack([c.f, c.b], 3).unbind(3)
+    c.reset = torch.stack([c.reset, 1 - c.reset], 2)[..., 0]
+    outs = tuple(part(torch.zeros_like(x), front, back) for x in (c.q, c.k, c.v)) + tuple(torch.zeros(*c.f.shape, 3, dtype=c.dt, device=DEV)[..., 1] for _ in range(2))
+    other = c.run(out=outs)
+    c.check(*other)
+    for x, y in zip((plain[0], plain[1], *plain[2]), (other[0], other[1], *other[2])):
+        assert torch.equal(x, y)
+    for x in outs[:3]:
+        base = x._base
+        assert torch.isnan(base[..., :front]).all() and torch.isnan(base[..., front + x.shape[-1]:]).all()
+
+
+def test_delta_heads_that_share_keys():
+    c = Delta(10, "bf16", 2, 70, 4, 16, 16)
+    c.k = c.k[:, :, :1].expand(-1, -1, 4, -1)
+    c.q = c.q[:, :, :1].expand(-1, -1, 4, -1)
+    c.check(*c.run())
+
+
+def test_delta_in_pieces_is_the_whole():
+    c = Delta(11, "fp32", 2, 200, 2, 16, 16)
+    o, last = seq.delta(*c.inputs(), s0=c.s0, reset=c.reset, scale=c.scale)
+    state, got = c.s0.clone(), []
+    for a, b in ((0, 1), (1, 2), (2, 70), (70, 71), (71, 200)):
+        p, s = seq.delta(*(x[:, a:b] for x in c.inputs()), s0=state, reset=c.reset[:, a:b], scale=c.scale, last=state)
+        assert s is state
+        got.append(p)
+    out, bound = c.exact()[:2]
+    ref.within(host(torch.cat(got, 1)), out[0], bound[0], (3,), False, "o")
+    ref.within(host(state), out[1], bound[1], (2, 3), False, "last")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,Dk,Dv", [(200, 16, 20), (200, 64, 64), (5, 16, 20), (1, 64, 64)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_delta_what_is_not_finite_stays_in_its_episode(dtype, T, Dk, Dv, bad):
+    """A value, a key, a gate and a state that are not finite: outputs before them and of other episodes, gradients of other episodes
+    are what they are without them."""
+    clean = Delta(12, dtype, 4, T, 2, Dk, Dv, resets=0)
+    clean.reset = torch.zeros(4, T, dtype=torch.uint8, device=DEV)
+    starts, at = ((0, 0, 70, 130), (30, 66, 100, 131)) if T == 200 else ((0,) * 4, (0, 1 % T, 2 % T, T - 1))
+    ends = (64, 70, 128, 200) if T == 200 else (T,) * 4
+    for i in range(4):
+        clean.reset[i, starts[i]] = 1
+        if ends[i] < T:
+            clean.reset[i, ends[i]] = 1
+    want = clean.run()
+    c = Delta(12, dtype, 4, T, 2, Dk, Dv, resets=0)
+    c.reset = clean.reset
+    c.v[0, at[0], 1, 0] = bad
+    c.k[1, at[1], 0, 0] = bad
+    c.f[2, at[2], 0] = float("nan")
+    c.v[3, at[3]] = bad
+    c.s0[:, :, 0, 0] = bad       # forgotten at a first step's reset
+    got = c.run()
+    where = torch.zeros(4, T, 2, dtype=torch.bool, device=DEV)      # of outputs that may differ
+    gwhere = torch.zeros_like(where)
+    for i, heads in enumerate(((1,), (0,), (0,), (0, 1))):
+        for h in heads:
+            where[i, at[i]:ends[i], h] = True
+            gwhere[i, starts[i]:ends[i], h] = True
+    # sequences that do not start with a reset hold the state's NaN until the first
+    for i in range(4):
+        if starts[i] > 0:
+            where[i, :starts[i]] = gwhere[i, :starts[i]] = True
+    low = c.dt is torch.bfloat16
+
+    def alike(a, b, mask, what):
+        a, b = host(a), host(b)
+        keep = ~mask.cpu().numpy()
+        a, b = a[keep], b[keep]
+        assert np.isfinite(a).all(), what
+        # the tile is computed in another order: both within the same bounds of the definition, which are far below this
+        assert np.abs(a - b).max(initial=0.0) <= (2.0 ** -7 if low else 1e-4) * max(1.0, np.abs(b).max(initial=0.0)), what
+
+    alike(got[0], want[0], where, "o")
+    for name, x, y in zip(("dq", "dk", "dv", "df", "db"), got[2], want[2]):
+        alike(x, y, gwhere, name)
+    if T == 200:
+        assert torch.isfinite(got[1][:3]).all() and not torch.isfinite(got[1][3]).all()
+        assert not torch.isfinite(got[0][0, at[0], 1]).all() and not torch.isfinite(got[0][1, at[1], 0]).all()
+
+
+def test_delta_padding_behind_an_end_may_hold_anything():
+    c = Delta(13, "bf16", 2, 100, 2, 32, 32, resets=0)
+    c.reset = torch.zeros(2, 100, dtype=torch.bool, device=DEV)
+    c.reset[0, 61] = True
+    c.do[0, 61:] = 0
+    c.dlast = None
+    want = c.run()
+    for x in c.inputs():
+        x[0, 61:] = float("nan")
+    got = c.run()
+    assert torch.equal(got[0][0, :61], want[0][0, :61]) and torch.equal(got[0][1], want[0][1])
+    for x, y in zip(got[2][:5], want[2][:5]):
+        assert torch.allclose(x[0, :61].float(), y[0, :61].float(), rtol=2.0 ** -7, atol=2.0 ** -9) and torch.equal(x[1], y[1])
+    assert torch.allclose(got[2][5], want[2][5], rtol=1e-4, atol=1e-5)
+
+
+def test_delta_many_and_none():
+    for B, T, H in ((0, 5, 2), (2, 0, 2), (2, 5, 0)):
+        c = Delta(14, "fp32", B, T, H, 4, 4)
+        o, last, grads = c.run()
+        assert o.shape == (B, T, H, 4)
+        if T == 0:
+            assert torch.equal(last, c.s0) and torch.equal(grads[5], c.dlast)
+    c = Delta(15, "bf16", 300, 3, 5, 8, 8)
+    c.check(*c.run())
+
+
+def test_delta_on_another_stream_and_in_graphs():
+    c = Delta(16, "bf16", 2, 100, 2, 32, 32)
+    want = c.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = c.run()
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], want[0]) and all(torch.equal(x, y) for x, y in zip(got[2], want[2]))
+    graphs = []
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            graphs.append((g, c.run()))
+    for k in range(4):
+        c.v.copy_(torch.randn_like(c.v))
+        want = c.run()
+        for g, got in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, got in graphs:
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and all(torch.equal(x, y) for x, y in zip(got[2], want[2]))
+
+
+def test_delta_refuses():
+    c = Delta(17, "fp32", 2, 5, 2, 4, 6)
+    q, k, v, f, b = c.inputs()
+    for bad in ((q[0], k, v, f, b), (q, k[:, :4], v, f, b), (q, k, v.half(), f, b), (q, k.to(torch.bfloat16), v, f, b), (q, k, v, f[..., :1], b), (q, k, v, f, b.cpu()),
+                (q.transpose(2, 3).contiguous().transpose(2, 3), k, v, f, b), (q.half(), k, v, f, b)):
+        with pytest.raises(ValueError):
+            seq.delta(*bad)
+    with pytest.raises(ValueError):
+        seq.delta(*c.inputs(), s0=c.s0[:, :1])
+    with pytest.raises(ValueError):
+        seq.delta(*c.inputs(), reset=torch.zeros(2, 4, dtype=torch.uint8, device=DEV))
+    with pytest.raises(dqn.DqnError):
+        seq.delta(*c.inputs(), scale=float("nan"))
+    with pytest.raises(dqn.DqnError):
+        seq.delta(*(torch.zeros(1, 2, 1, 129, device=DEV) for _ in range(3)), *(torch.zeros(1, 2, 1, device=DEV) for _ in range(2)))
+    carry = seq.delta(*c.inputs(), save=True)[2]
+    with pytest.raises(ValueError):
+        seq.delta_backward(c.do, *c.inputs(), carry[:-1])
+    with pytest.raises(ValueError):
+        seq.delta_backward(c.do[..., :5], *c.inputs(), carry)
+    with pytest.warns(UserWarning, match="detached"):
+        seq.delta(q.clone().requires_grad_(), k, v, f, b)
