@@ -512,6 +512,51 @@ int32_t dqn_norm_sizes(int64_t M, int32_t C, size_t *workspace);
 int32_t dqn_norm_forward(const dqn_norm_args *args, void *stream);
 int32_t dqn_norm_backward(const dqn_norm_grad_args *args, void *stream);
 
+/* Queries and keys per head: per head of D elements a root-mean-square norm, and the rotation by
+ * position in the same pass,
+ *   z = weight x rstd,  rstd = 1 / sqrt(mean(x^2) + eps),
+ *   y_i = z_i cos t_i - z_{i+R/2} sin t_i,  y_{i+R/2} = z_{i+R/2} cos t_i + z_i sin t_i,  i < R/2,
+ *   t_i = 2 pi position turns_i,  y_i = z_i for i >= R.
+ * A weight of 1 / sqrt(D) makes keys of length one, as dqn_delta_forward wants them.  Angles are
+ * exact for any position: what counts of position times turns_i is its fraction, kept to
+ * 2^-32 of a full turn. */
+#define DQN_HEADS_MAX 256
+typedef struct {
+    int32_t dtype, Hq, Hk;              /* heads of queries and of keys, 0..65535   */
+    int32_t D, R;                       /* 1 <= D <= DQN_HEADS_MAX; R even, 0..D    */
+    float eps;                          /* >= 0                                     */
+    int64_t M;                          /* rows, 0..2^31-1                          */
+    const void *q, *k;                  /* [M][Hq][D], [M][Hk][D]                   */
+    int64_t q_rs, q_hs, k_rs, k_hs;     /* strides of a row and of a head           */
+    const float *q_weight, *k_weight;   /* [D]                                      */
+    const int32_t *position;            /* [M], not read if R = 0                   */
+    const double *turns;                /* HOST array [R/2], read during the call:
+                                           full turns per position, finite          */
+    void *yq, *yk;                      /* [M][Hq][D], [M][Hk][D]; may be q, k      */
+    int64_t yq_rs, yq_hs, yk_rs, yk_hs;
+    float *rstd;                        /* [M][Hq + Hk], or NULL                    */
+} dqn_heads_args;
+
+/* Gradients, from rstd and the same inputs: with dy turned back, g = weight dy and xh = x rstd,
+ *   dx = rstd (g - xh mean(g xh)),   dweight = sum over rows and heads of dy xh  (in a fixed order). */
+typedef struct {
+    int32_t dtype, Hq, Hk, D, R;
+    int64_t M;
+    const void *dyq, *dyk, *q, *k;
+    int64_t dyq_rs, dyq_hs, dyk_rs, dyk_hs, q_rs, q_hs, k_rs, k_hs;
+    const float *q_weight, *k_weight, *rstd;
+    const int32_t *position;
+    const double *turns;
+    void *dq, *dk;                      /* may be dyq, dyk                          */
+    int64_t dq_rs, dq_hs, dk_rs, dk_hs;
+    float *dq_weight, *dk_weight;       /* [D]; M = 0 gives zeros                   */
+    void *workspace;                    /* bytes from dqn_heads_sizes, 16-byte aligned */
+} dqn_heads_grad_args;
+
+int32_t dqn_heads_sizes(int64_t M, int32_t Hq, int32_t Hk, int32_t D, size_t *workspace);
+int32_t dqn_heads_forward(const dqn_heads_args *args, void *stream);
+int32_t dqn_heads_backward(const dqn_heads_grad_args *args, void *stream);
+
 /* Rows [M][K] to 8 bits, 1 <= K <= DQN_NORM_MAX, as dqn_norm_forward writes them: scale = max(max |x|, 2^-117) / 448
  * per row, 0 for a row of zeros. */
 int32_t dqn_rows_quantize(int32_t dtype, int64_t M, int32_t K, const void *x, int64_t x_rs, uint8_t *q,
@@ -586,6 +631,34 @@ int32_t dqn_adamw_init(dqn_adamw **out, const dqn_adamw_tensor *tensors, int32_t
 int32_t dqn_adamw_step(dqn_adamw *opt, double lr, double beta_m, double beta_v, double eps, int64_t step,
                        uint64_t seed, void *stream);
 int32_t dqn_adamw_destroy(dqn_adamw *opt);
+
+/* A step for matrices whose momentum is made orthogonal, for many of them at once:
+ *   m <- mu m + g,   u = g + mu m (nesterov) or m,   X = u / (|u| + eps), |u| the root of all squares' sum
+ *   `rounds` times:  A = X X^T,  X <- 3.4445 X + (-4.775 A + 2.0315 A^2) X   (of the transposed if rows > cols)
+ *   p <- p (1 - lr decay) - lr sqrt(max(1, rows / cols)) X
+ * Parameters and momentum are fp32.  Within the rounds numbers are kept to 16 bits (pairs of
+ * bf16), sums are fp32; five rounds take singular values between 1e-2 and 1 of |u| to 0.7 .. 1.2.  A gradient that is not finite
+ * spoils its own matrix alone.  Nothing but m is kept from step to step. */
+typedef struct {
+    float *param, *momentum;            /* [rows][cols]; the caller sets momentum (zeros at the start) */
+    const void *grad;                   /* [rows][cols], in the optimizer's grad_dtype */
+    uint16_t *copy;                     /* [rows][cols] bf16 copy of the new param, or NULL */
+    int64_t rows, cols;                 /* 0..2^20, the smaller at most 65536       */
+    float decay;                        /* finite, >= 0                             */
+} dqn_muon_matrix;
+
+typedef struct dqn_muon dqn_muon;
+
+/* `matrices`: host array of `count` descriptions, 1 <= count <= 65536; its device pointers must stay valid, as must plan and
+ * workspace (256-byte aligned, bytes from dqn_muon_sizes): a step uses both, so steps of one handle are not to overlap.
+ * The handle owns host-side bookkeeping only; the table is copied to `plan` on `stream` during dqn_muon_init, which
+ * waits for the copy and so cannot be recorded into a graph. */
+int32_t dqn_muon_sizes(const dqn_muon_matrix *matrices, int32_t count, size_t *plan, size_t *workspace);
+int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t count, int32_t grad_dtype, void *plan,
+                      void *workspace, void *stream);
+/* One step; 0 <= momentum < 1, 1 <= rounds <= 100. */
+int32_t dqn_muon_step(dqn_muon *opt, double lr, double momentum, int32_t nesterov, double eps, int32_t rounds, void *stream);
+int32_t dqn_muon_destroy(dqn_muon *opt);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,172 @@
+// C ABI of the steps for matrices (see include/dqn.h): checks of arguments and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "../../include/dqn.h"
+#include "checks.h"
+#include "muon.h"
+
+struct dqn_muon {
+    seq::MuonArgs args;
+    int64_t chunks, half, whole;       // workgroups of the launches
+    int grad_dtype;
+};
+
+namespace {
+
+constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
+
+const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
+{
+    if (!t || count < 1 || count > 65536) return "count must be in 1..65536, matrices not NULL";
+    for (int32_t i = 0; i < count; ++i) {
+        if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > LONGEST || t[i].cols > LONGEST || std::min(t[i].rows, t[i].cols) > 65536) return "a matrix's size is out of range";
+        if (t[i].rows && t[i].cols && (!t[i].param || !t[i].momentum || !t[i].grad || !at(t[i].param, 4) || !at(t[i].momentum, 4) || !at(t[i].copy, 2)))
+            return "a matrix's pointer is NULL or not aligned to its elements";
+        if (!(t[i].decay >= 0.f) || std::isinf(t[i].decay)) return "decay must be finite and >= 0";
+    }
+    return nullptr;
+}
+
+// Of one matrix: its padded sides and its parts of the workspace in bytes, in their order.
+struct Parts {
+    int64_t rp, cp, chunks, x, a, sums;
+    int64_t bytes() const { return 3 * x + 2 * a + sums; }
+};
+int64_t padded(int64_t n) { return (n + seq::MT - 1) / seq::MT * seq::MT; }
+Parts parts_of(const dqn_muon_matrix &t)
+{
+    Parts p{};
+    if (!t.rows || !t.cols) return p;
+    p.rp = padded(std::min(t.rows, t.cols));
+    p.cp = padded(std::max(t.rows, t.cols));
+    p.chunks = (t.rows * t.cols + seq::MUON_CHUNK - 1) / seq::MUON_CHUNK;
+    p.x = p.rp * p.cp * 4;
+    p.a = p.rp * p.rp * 4;
+    p.sums = (p.chunks * 8 + 255) / 256 * 256;
+    return p;
+}
+
+struct Total {
+    int64_t plan, workspace, chunks, half, whole;
+};
+Total total_of(const dqn_muon_matrix *t, int32_t count)
+{
+    Total s{((int64_t)count * (int64_t)sizeof(seq::MuonMatrix) + 255) / 256 * 256, 0, 0, 0, 0};
+    for (int32_t i = 0; i < count; ++i) {
+        const Parts p = parts_of(t[i]);
+        const int64_t down = p.rp / seq::MT, across = p.cp / seq::MT;
+        s.workspace += p.bytes();
+        s.chunks += p.chunks;
+        s.half += down * (down + 1) / 2;
+        s.whole += down * across;
+    }
+    return s;
+}
+
+template <class G> void launch_begin(const dqn_muon &o, hipStream_t st)
+{
+    seq::k_muon_momentum<G><<<dim3((unsigned)o.chunks), 256, 0, st>>>(o.args);
+    seq::k_muon_start<G><<<dim3((unsigned)o.whole), 256, 0, st>>>(o.args);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t dqn_muon_sizes(const dqn_muon_matrix *matrices, int32_t count, size_t *plan, size_t *workspace)
+{
+    static const char *call = "dqn_muon_sizes";
+    if (!plan || !workspace) return bad(call, "NULL argument");
+    if (const char *m = check_matrices(matrices, count)) return bad(call, m);
+    const Total s = total_of(matrices, count);
+    *plan = (size_t)s.plan;
+    *workspace = (size_t)std::max<int64_t>(s.workspace, 256);
+    return DQN_OK;
+}
+
+int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t count, int32_t grad_dtype, void *plan, void *workspace, void *stream)
+{
+    static const char *call = "dqn_muon_init";
+    if (!out) return bad(call, "NULL argument");
+    *out = nullptr;
+    if (const char *m = check_matrices(matrices, count)) return bad(call, m);
+    if (!dtype_ok(grad_dtype)) return bad(call, "grad_dtype must be DQN_F32 or DQN_BF16");
+    if (!plan || !workspace || !at(plan, 256) || !at(workspace, 256)) return bad(call, "plan or workspace is NULL or not 256-byte aligned");
+    for (int32_t i = 0; i < count; ++i)
+        if (!at(matrices[i].grad, bytes_of(grad_dtype))) return bad(call, "a gradient is not aligned to its elements");
+    const Total s = total_of(matrices, count);
+    if (s.chunks >= 1 << 24 || s.half >= 1 << 24 || s.whole >= 1 << 24) return bad(call, "too many elements");   // a launch has 2^32 threads
+    dqn_muon *o = nullptr;
+    try {
+        std::vector<seq::MuonMatrix> table;
+        table.reserve((size_t)count);
+        uint8_t *at = (uint8_t *)workspace;
+        int first_chunk = 0, first_half = 0, first_whole = 0;
+        for (int32_t i = 0; i < count; ++i) {
+            const dqn_muon_matrix &t = matrices[i];
+            if (!t.rows || !t.cols) continue;
+            const Parts p = parts_of(t);
+            seq::MuonMatrix m{};
+            m.p = t.param; m.m = t.momentum; m.g = t.grad; m.copy = t.copy;
+            m.x = (seq::bf16 *)at; m.xt[0] = (seq::bf16 *)(at + p.x); m.xt[1] = (seq::bf16 *)(at + 2 * p.x);
+            m.a = (seq::bf16 *)(at + 3 * p.x); m.b = (seq::bf16 *)(at + 3 * p.x + p.a); m.sums = (double *)(at + 3 * p.x + 2 * p.a);
+            at += p.bytes();
+            m.rows = (long)t.rows; m.cols = (long)t.cols; m.rp = (int)p.rp; m.cp = (int)p.cp; m.tall = t.rows > t.cols;
+            m.decay = t.decay; m.scale = (float)std::sqrt(std::max(1.0, (double)t.rows / (double)t.cols)); m.chunks = (int)p.chunks;
+            m.first_chunk = first_chunk; m.first_half = first_half; m.first_whole = first_whole;
+            const int down = m.rp / seq::MT;
+            first_chunk += m.chunks; first_half += down * (down + 1) / 2; first_whole += down * (m.cp / seq::MT);
+            table.push_back(m);
+        }
+        hipStream_t st = (hipStream_t)stream;
+        if (!table.empty() && (hipMemcpyAsync(plan, table.data(), table.size() * sizeof(table[0]), hipMemcpyHostToDevice, st) != hipSuccess || hipStreamSynchronize(st) != hipSuccess)) {
+            (void)hipGetLastError();
+            return dqn_seq_fail(DQN_ERR_HIP, call, "copying the table of matrices failed");
+        }
+        o = new dqn_muon{};
+        o->args.count = (int)table.size();
+    } catch (...) {
+        return dqn_seq_fail(DQN_ERR_OOM, call, "out of host memory");
+    }
+    o->args.matrices = (const seq::MuonMatrix *)plan;
+    o->chunks = s.chunks; o->half = s.half; o->whole = s.whole; o->grad_dtype = grad_dtype;
+    *out = o;
+    return DQN_OK;
+}
+
+int32_t dqn_muon_step(dqn_muon *opt, double lr, double momentum, int32_t nesterov, double eps, int32_t rounds, void *stream)
+{
+    static const char *call = "dqn_muon_step";
+    if (!opt) return bad(call, "NULL argument");
+    if (!(lr >= 0.0) || lr > 1e30 || !(eps >= 1e-30) || eps > 1e30) return bad(call, "lr in 0..1e30 and eps in 1e-30..1e30 required");
+    if (!(momentum >= 0.0 && momentum < 1.0)) return bad(call, "momentum must be in [0, 1)");
+    if (rounds < 1 || rounds > 100) return bad(call, "rounds must be in 1..100");
+    if (!opt->args.count) return DQN_OK;
+    seq::MuonArgs A = opt->args;
+    A.nesterov = nesterov != 0; A.mu = (float)momentum; A.eps = (float)eps; A.lr = (float)lr;
+    A.a = 3.4445f; A.b = -4.7750f; A.c = 2.0315f;
+    hipStream_t st = (hipStream_t)stream;
+    dqn_muon now = *opt;
+    now.args = A;
+    opt->grad_dtype == DQN_F32 ? launch_begin<float>(now, st) : launch_begin<seq::bf16>(now, st);
+    for (int32_t i = 0; i < rounds; ++i) {
+        seq::k_muon_gram<false><<<dim3((unsigned)opt->half), 256, 0, st>>>(A);
+        seq::k_muon_gram<true><<<dim3((unsigned)opt->half), 256, 0, st>>>(A);
+        if (i + 1 < rounds) seq::k_muon_apply<false><<<dim3((unsigned)opt->whole), 256, 0, st>>>(A, i & 1);
+        else seq::k_muon_apply<true><<<dim3((unsigned)opt->whole), 256, 0, st>>>(A, i & 1);
+    }
+    return launched(call);
+}
+
+int32_t dqn_muon_destroy(dqn_muon *opt)
+{
+    delete opt;
+    return DQN_OK;
+}
+
+}  // extern "C"

@@ -22,7 +22,9 @@ EXPORTS = ["dqn_query_sizes", "dqn_init", "dqn_act", "dqn_train_step", "per_samp
            "dqn_get_activations", "dqn_act_static", "dqn_selftest_fused_conv_schedule", "dqn_replay_store_envs",
            "dqn_scan_sizes", "dqn_scan_forward", "dqn_scan_backward", "dqn_norm_sizes", "dqn_norm_forward", "dqn_norm_backward",
            "dqn_rows_quantize", "dqn_rows_product", "dqn_adamw_sizes", "dqn_adamw_init", "dqn_adamw_step", "dqn_adamw_destroy",
-           "dqn_delta_sizes", "dqn_delta_forward", "dqn_delta_backward"]
+           "dqn_delta_sizes", "dqn_delta_forward", "dqn_delta_backward",
+           "dqn_heads_sizes", "dqn_heads_forward", "dqn_heads_backward",
+           "dqn_muon_sizes", "dqn_muon_init", "dqn_muon_step", "dqn_muon_destroy"]
 
 
 class DqnConfig(C.Structure):
@@ -128,6 +130,9 @@ def lib():
             "dqn_delta_sizes": [i32, i32, i64, i32, i32, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
             "dqn_delta_forward": [C.c_char_p, vp],
             "dqn_delta_backward": [C.c_char_p, vp],
+            "dqn_heads_sizes": [i64, i32, i32, i32, C.POINTER(C.c_size_t)],
+            "dqn_heads_forward": [C.c_char_p, vp],
+            "dqn_heads_backward": [C.c_char_p, vp],
             "dqn_norm_sizes": [i64, i32, C.POINTER(C.c_size_t)],
             "dqn_norm_forward": [C.c_char_p, vp],
             "dqn_norm_backward": [C.c_char_p, vp],
@@ -137,6 +142,10 @@ def lib():
             "dqn_adamw_init": [C.POINTER(vp), vp, i32, i32, i32, vp, vp],
             "dqn_adamw_step": [vp, C.c_double, C.c_double, C.c_double, C.c_double, i64, u64, vp],
             "dqn_adamw_destroy": [vp],
+            "dqn_muon_sizes": [vp, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "dqn_muon_init": [vp, vp, i32, i32, vp, vp, vp],
+            "dqn_muon_step": [vp, C.c_double, C.c_double, i32, C.c_double, i32, vp],
+            "dqn_muon_destroy": [vp],
         }
         for name, argtypes in sig.items():
             fn = getattr(L, name)

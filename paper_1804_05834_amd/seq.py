@@ -3,9 +3,11 @@
   scan, scan_backward       gated linear recurrence over time, per channel
   delta, delta_backward     gated delta rule: a memory of one matrix per head
   norm, norm_backward       root-mean-square norm with the residual's addition
+  norm_heads, .._backward   the norm of queries and keys per head, with the rotation by position
   norm_rows, rows           the same, or no norm, with the output in 8-bit rows
   product                   8-bit rows times 8-bit weights
   AdamW                     one step over many tensors, moments in 32 or 8 bits
+  Muon                      one step over many matrices, the momentum made orthogonal
 
 Argument marshalling only, as in dqn.py: the arithmetic runs in the HIP kernels of the library, on the
 current stream; torch allocates outputs.  Activations are float32 or bfloat16, states, weights of the norm
@@ -16,6 +18,7 @@ A wrong shape, type or device raises ValueError; what the library refuses raises
 """
 import ctypes as C
 import functools
+import math
 import struct
 import warnings
 
@@ -35,11 +38,17 @@ DELTA_ARGS = struct.Struct("iiiiifqPPPPPqqqqqqqqqqqqqqqPPqqPqqqPPP")
 DELTA_GRAD_ARGS = struct.Struct("iiiiifqPPPPPqqqqqqqqqqqqqqqPPqqPqqqPPPPPPqqqqqqqqqqqqqqqPP")
 NORM_ARGS = struct.Struct("iiqPPqqPfPqPqPqPP")
 NORM_GRAD_ARGS = struct.Struct("iiqPPPPqqqqPPPqPP")
+HEADS_ARGS = struct.Struct("iiiiifqPPqqqqPPPPPPqqqqP")
+HEADS_GRAD_ARGS = struct.Struct("iiiiiqPPPPqqqqqqqqPPPPPPPqqqqPPP")
 PRODUCT_ARGS = struct.Struct("iiiqPPqqPPPPq")
 
 
 class _AdamWTensor(C.Structure):
     _fields_ = [("param", _vp), ("grad", _vp), ("copy", _vp), ("n", _i64), ("decay", _f32)]
+
+
+class _MuonMatrix(C.Structure):
+    _fields_ = [("param", _vp), ("momentum", _vp), ("grad", _vp), ("copy", _vp), ("rows", _i64), ("cols", _i64), ("decay", _f32)]
 
 
 class _AdamWBytes(C.Structure):
@@ -365,6 +374,92 @@ def norm_backward(dy, r, saved, weight, dr=None):
     return dx, dw
 
 
+# ------------------------------------------------------------------ queries and keys per head
+class Rotation:
+    """Full turns per position of each pair of elements, as norm_heads takes them: a sequence of R/2 finite numbers."""
+
+    def __init__(self, turns):
+        self.R = 2 * len(turns)
+        self._turns = (C.c_double * max(1, len(turns)))(*turns)
+        self.address = C.addressof(self._turns)
+
+
+@functools.lru_cache(maxsize=64)
+def rotation(R, base=10000.0):
+    """Pair i of R/2 turns by base^(-2 i / R) radians a position."""
+    if R < 0 or R % 2 or not base > 0:
+        raise ValueError("rotation: an even R >= 0 and base > 0 expected")
+    return Rotation([base ** (-2.0 * i / R) / (2.0 * math.pi) for i in range(R // 2)])
+
+
+_STILL = Rotation(())
+
+
+def _heads_inputs(q, k, q_weight, k_weight, position, turns):
+    kind, dev = _kind(q, "q"), _current_device()
+    if len(q.shape) != 3 or len(k.shape) != 3:
+        raise ValueError("q and k: [M][H][D] expected")
+    (M, Hq, D), Hk = q.shape, k.shape[1]
+    qp, qs = _rows(q, "q", q.dtype, (M, Hq, D), dev)
+    kp, ks = _rows(k, "k", q.dtype, (M, Hk, D), dev)
+    turns = turns or _STILL
+    if turns.R and position is None:
+        raise ValueError("position: a rotation takes the positions of the rows")
+    pp = 0 if position is None else _flat(position, "position", torch.int32, (M,), dev)
+    return (kind, M, Hq, Hk, D, turns, dev, qp, kp, (*qs[:2], *ks[:2]), _flat(q_weight, "q_weight", torch.float32, (D,), dev),
+            _flat(k_weight, "k_weight", torch.float32, (D,), dev), pp)
+
+
+def norm_heads(q, k, q_weight, k_weight, position=None, turns=None, eps=1e-6, out=None):
+    """Queries q [M][Hq][D] and keys k [M][Hk][D]: per head weight x / sqrt(mean x^2 + eps), then elements i and i + R/2 as a point turned
+    by position turns_i of a full turn.  weights: [D] float32; position: [M] int32; turns: a Rotation, rotation(R) say, or None (no
+    turn).  out: (yq, yk) to write into, which may be q and k.  A weight of 1 / sqrt(D) makes vectors of length one.
+    -> (yq, yk, what norm_heads_backward needs)"""
+    if q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad:
+        _detached("norm_heads", "norm_heads_backward")
+    kind, M, Hq, Hk, D, turns, dev, qp, kp, strides, wq, wk, pp = _heads_inputs(q, k, q_weight, k_weight, position, turns)
+    if out is None:
+        (yq, yqp, yqs), (yk, ykp, yks) = _like(q), _like(k)
+    else:
+        yq, yk = out
+        yqp, yqs = _rows(yq, "out[0]", q.dtype, q.shape, dev)
+        ykp, yks = _rows(yk, "out[1]", q.dtype, k.shape, dev)
+    rstd = torch.empty((M, Hq + Hk), dtype=torch.float32, device=q.device)
+    args = HEADS_ARGS.pack(kind, Hq, Hk, D, turns.R, eps, M, qp, kp, *strides, wq, wk, pp, turns.address, yqp, ykp, *yqs[:2], *yks[:2], rstd.data_ptr())
+    _call(lib().dqn_heads_forward(args, _raw_stream(dev)))
+    return yq, yk, rstd
+
+
+@functools.lru_cache(maxsize=256)
+def _heads_sizes(M, Hq, Hk, D):
+    work = C.c_size_t()
+    _call(lib().dqn_heads_sizes(M, Hq, Hk, D, C.byref(work)))
+    return work.value
+
+
+def norm_heads_backward(dyq, dyk, q, k, rstd, q_weight, k_weight, position=None, turns=None, out=None):
+    """Gradients of norm_heads: dyq, dyk of its outputs, rstd from it, the rest as it was.  out: (dq, dk) to write into, which may be dyq and
+    dyk.  -> (dq, dk, dq_weight [D], dk_weight [D])"""
+    kind, M, Hq, Hk, D, turns, dev, qp, kp, strides, wq, wk, pp = _heads_inputs(q, k, q_weight, k_weight, position, turns)
+    gqp, gqs = _rows(dyq, "dyq", q.dtype, q.shape, dev)
+    gkp, gks = _rows(dyk, "dyk", q.dtype, k.shape, dev)
+    if out is None:
+        (dq, dqp, dqs), (dk, dkp, dks) = _like(q), _like(k)
+    else:
+        dq, dk = out
+        dqp, dqs = _rows(dq, "out[0]", q.dtype, q.shape, dev)
+        dkp, dks = _rows(dk, "out[1]", q.dtype, k.shape, dev)
+    dw = torch.empty((2, D), dtype=torch.float32, device=q.device)
+    if not Hq or not Hk:
+        dw.zero_()
+    work, wp = _scratch(_heads_sizes(M, Hq, Hk, D), q.device)
+    args = HEADS_GRAD_ARGS.pack(kind, Hq, Hk, D, turns.R, M, gqp, gkp, qp, kp, *gqs[:2], *gks[:2], *strides, wq, wk,
+                                _flat(rstd, "rstd", torch.float32, (M, Hq + Hk), dev), pp, turns.address, dqp, dkp, *dqs[:2], *dks[:2],
+                                dw.data_ptr(), dw.data_ptr() + 4 * D, wp)
+    _call(lib().dqn_heads_backward(args, _raw_stream(dev)))
+    return dq, dk, dw[0], dw[1]
+
+
 # ------------------------------------------------------------------ 8-bit rows and their product
 def rows(x):
     """x [M][K] in 8 bits: -> (q [M][K] e4m3, scale [M]) with x ~ q scale[:, None]."""
@@ -461,6 +556,63 @@ class AdamW:
     def close(self):
         if getattr(self, "_h", None):
             lib().dqn_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ------------------------------------------------------------------ steps for matrices
+class Muon:
+    """Steps for matrices `params` (contiguous float32 [rows][cols], updated in place) with gradients in the buffers `grads` (float32 or
+    bfloat16, one type for all), which the program fills before each step(): m <- momentum m + g, and what is subtracted is g +
+    momentum m (or m without nesterov) with all its singular values near one, by `rounds` products with itself, times lr sqrt(max(1,
+    rows / cols)).  Vectors, norms' weights and biases are AdamW's.  weight_decay: one number or one per matrix.  copies: bfloat16
+    tensors that receive the new parameters, or None.  state: the momentum, a float32 tensor like each parameter, of an earlier optimizer
+    of the same matrices; they become this one's."""
+
+    def __init__(self, params, grads, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.01, eps=1e-7, rounds=5, copies=None, state=None):
+        n = len(params)
+        decays = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        copies = list(copies) if copies is not None else [None] * n
+        if not n or len(grads) != n or len(decays) != n or len(copies) != n or (state is not None and len(state) != n):
+            raise ValueError("one gradient, weight decay, copy and momentum per parameter expected")
+        kind, gt, dev, device = _kind(grads[0], "grads"), grads[0].dtype, _current_device(), params[0].device
+        if any(p.dim() != 2 for p in params):
+            raise ValueError("params: matrices expected")
+        self.m = [torch.zeros_like(p) for p in params] if state is None else list(state)
+        table = (_MuonMatrix * n)()
+        for i, (p, m, g, d, c) in enumerate(zip(params, self.m, grads, decays, copies)):
+            table[i] = _MuonMatrix(_flat(p, "params", torch.float32, p.shape, dev), _flat(m, "state", torch.float32, p.shape, dev), _flat(g, "grads", gt, p.shape, dev),
+                                   None if c is None else _flat(c, "copies", torch.bfloat16, p.shape, dev), p.shape[0], p.shape[1], d)
+        plan, work = C.c_size_t(), C.c_size_t()
+        _call(lib().dqn_muon_sizes(table, n, C.byref(plan), C.byref(work)))
+        self._plan = torch.empty(plan.value, dtype=torch.uint8, device=device)
+        self._work = torch.empty(work.value, dtype=torch.uint8, device=device)
+        self._keep = (list(params), list(grads), copies)     # the table holds their addresses
+        self.lr, self.momentum, self.nesterov, self.eps, self.rounds = lr, momentum, nesterov, eps, rounds
+        h, stream = C.c_void_p(), _raw_stream(dev)
+        _call(lib().dqn_muon_init(C.byref(h), table, n, kind, self._plan.data_ptr(), self._work.data_ptr(), stream))
+        self._h, self._device, self._stream = h, dev, stream
+
+    def step(self, lr=None):
+        """One step.  Steps of one optimizer share a workspace: on several streams the program orders them.  A step recorded into a graph
+        repeats its rate with every replay."""
+        dev = _current_device()
+        if dev != self._device:
+            raise ValueError("step: the optimizer's matrices are not on the current GPU")
+        stream = _raw_stream(dev)
+        if stream != self._stream:      # what the optimizer holds must outlast this step, also if it is dropped before
+            for t in (self._plan, self._work, *self.m):
+                t.record_stream(torch.cuda.current_stream())
+        _call(lib().dqn_muon_step(self._h, self.lr if lr is None else lr, self.momentum, int(self.nesterov), self.eps, self.rounds, stream))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().dqn_muon_destroy(self._h)
             self._h = None
 
     def __del__(self):

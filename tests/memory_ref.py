@@ -104,6 +104,92 @@ def delta_backward(do, q, k, v, f, b, s0=None, reset=None, dlast=None, scale=1.0
     return (*out, D), (*err, e)
 
 
+# ------------------------------------------------------------------ queries and keys per head
+def _spin(position, turns):
+    """Cosines and sines [M][R/2]; the product in 64 bits of mantissa, so that its fraction is known for far positions too."""
+    t = np.asarray(position, np.longdouble)[:, None] * np.asarray(turns, np.longdouble)
+    t = (2 * np.pi * (t - np.floor(t))).astype(np.float64)
+    return np.cos(t)[:, None], np.sin(t)[:, None]
+
+
+def _turn(x, cos, sin):
+    h = cos.shape[-1]
+    lo, hi = x[..., :h], x[..., h:2 * h]
+    return np.concatenate([lo * cos - hi * sin, hi * cos + lo * sin, x[..., 2 * h:]], -1)
+
+
+def _partners(x, h):
+    """|x| + |what x is turned with|"""
+    lo, hi = np.abs(x[..., :h]), np.abs(x[..., h:2 * h])
+    return np.concatenate([lo + hi, lo + hi, np.abs(x[..., 2 * h:])], -1)
+
+
+def heads(x, weight, position, turns, eps):
+    """x [M][H][D] -> y, rstd, bounds of y and of rstd's relative error.  A sine or cosine is off by 2^-24 at most: by the angle's 2^-32 of a
+    turn and the series' end and rounding; a sum of D squares by D / 8 + 24 u."""
+    cos, sin = _spin(position, turns)
+    rstd = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    z = x * rstd * weight
+    erel = U * (x.shape[-1] / 8 + 24)
+    return _turn(z, cos, sin), rstd[..., 0], _partners(z, len(turns)) * (erel + 8 * U), erel
+
+
+def heads_backward(dy, x, weight, position, turns, eps):
+    """-> (dx, dweight), their bounds"""
+    cos, sin = _spin(position, turns)
+    M, H, D = x.shape
+    rstd = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    back, size = _turn(dy, cos, -sin), _partners(dy, len(turns))
+    xh, g, gs = x * rstd, back * weight, size * np.abs(weight)
+    mean, most = (g * xh).mean(-1, keepdims=True), (gs * np.abs(xh)).mean(-1, keepdims=True)
+    dx = rstd * (g - xh * mean)
+    return (dx, (back * xh).sum((0, 1))), (U * (D / 8 + 32) * rstd * (gs + np.abs(xh) * most), U * (M * H / 2 + 96 + D / 8) * (size * np.abs(xh)).sum((0, 1)))
+
+
+# ------------------------------------------------------------------ steps for matrices
+POLY = (3.4445, -4.7750, 2.0315)
+PAIR = 2.0 ** -18       # a number and its pair of bf16 differ by at most this, relatively: half a step of each of two times 8 bits
+
+
+def muon(p, g, m, lr, mu, nesterov=True, eps=1e-7, decay=0.0, rounds=5):
+    """-> p, m, the bound of the 2-norm of the error of p - that of rounding p itself left out.
+
+    Per round the errors of the products (each operand within PAIR, the product of both lower halves left out, another PAIR, sums of
+    K terms in fp32), all in 2-norms; an error that is there grows by the derivative of X -> a X + b X X^T X + c (X X^T)^2 X, whose factors at
+    singular values s, t are the quotients (f(s) - f(t)) / (s - t), (f(s) + f(t)) / (s + t) and f(s) / s."""
+    if not p.size:
+        return p, m, 0.0
+    a, b, c = POLY
+    m = mu * m + g
+    u = g + mu * m if nesterov else m
+    tall = u.shape[0] > u.shape[1]
+    x = (u.T if tall else u) / (np.sqrt((u * u).sum()) + eps)
+    r, k = x.shape
+    f = lambda s: a * s + b * s ** 3 + c * s ** 5  # noqa: E731
+    size = lambda y: np.sqrt((y * y).sum())  # noqa: E731
+    e = (PAIR + 8 * U) * size(x)
+    wide, square = 3 * PAIR + k * U / 2, 3 * PAIR + r * U / 2
+    for _ in range(rounds):
+        s = np.linalg.svd(x, compute_uv=False)
+        gram = x @ x.T
+        poly = b * gram + c * gram @ gram
+        ga, pa, sa = size(gram), size(poly), s.max()
+        ea = wide * size(x) * sa + PAIR * ga
+        eb = abs(b) * (ea + PAIR * ga) + abs(c) * (2 * sa ** 2 * ea + square * ga * sa ** 2) + PAIR * pa + 4 * U * (abs(b) + abs(c) * sa ** 2) * ga
+        new = a * x + poly @ x
+        top = np.linalg.svd(poly, compute_uv=False).max()
+        ex = eb * sa + square * min(pa * sa, top * size(x)) + PAIR * (size(new) + a * size(x)) + 4 * U * size(new)
+        si, sj = s[:, None], s[None]
+        with np.errstate(divide="ignore", invalid="ignore"):
+            slope = np.where(np.abs(si - sj) > 1e-9, (f(si) - f(sj)) / (si - sj), a + 3 * b * si ** 2 + 5 * c * si ** 4)
+            other = np.where(si + sj > 1e-9, (f(si) + f(sj)) / (si + sj), a)
+        e = max(np.abs(slope).max(), np.abs(other).max(), a if s.min() < 1e-6 else 0.0) * e + ex
+        x = new
+    x = x.T if tall else x
+    scale = np.sqrt(max(1.0, u.shape[0] / u.shape[1]))
+    return p - lr * decay * p - lr * scale * x, m, lr * scale * (e + 4 * U * size(x))
+
+
 def within(got, want, bound, axes, bf16, what):
     """2-norms of the error over `axes` against a bound of the fp32 result, the rounding to its type coming on top."""
     d = got.astype(np.float64) - want

@@ -286,3 +286,247 @@ def test_delta_refuses():
         seq.delta_backward(c.do[..., :5], *c.inputs(), carry)
     with pytest.warns(UserWarning, match="detached"):
         seq.delta(q.clone().requires_grad_(), k, v, f, b)
+
+
+# ------------------------------------------------------------------ queries and keys per head
+class Heads:
+    def __init__(self, seed, dtype, M, Hq, Hk, D, R, span=1000):
+        r = np.random.RandomState(seed)
+        self.dt, self.R = TYPES[dtype], R
+        self.q, self.k, self.dyq, self.dyk = (to(r.randn(M, h, D), self.dt) for h in (Hq, Hk, Hq, Hk))
+        self.wq, self.wk = to(r.randn(D)), to(r.randn(D))
+        self.position = to(r.randint(-span, span, M), torch.int32)
+        self.turns = seq.rotation(R)
+
+    def run(self, q=None, k=None, dyq=None, dyk=None, out=None, gout=None):
+        q, k, dyq, dyk = (y if y is not None else x for x, y in zip((self.q, self.k, self.dyq, self.dyk), (q, k, dyq, dyk)))
+        more = dict(position=self.position, turns=self.turns) if self.R else {}
+        yq, yk, rstd = seq.norm_heads(q, k, self.wq, self.wk, eps=1e-5, out=out, **more)
+        return (yq, yk, rstd), seq.norm_heads_backward(dyq, dyk, q, k, rstd, self.wq, self.wk, out=gout, **more)
+
+    def check(self, forward, grads):
+        low, turns, pos = self.dt is torch.bfloat16, np.array(self.turns._turns)[:self.R // 2], host(self.position)
+        for i, (x, w, dy) in enumerate(((self.q, self.wq, self.dyq), (self.k, self.wk, self.dyk))):
+            y, rstd, ey, er = ref.heads(host(x), host(w), pos, turns, 1e-5)
+            ref.within(host(forward[i]), y, ey, (), low, "y")
+            (dx, dw), (ex, ew) = ref.heads_backward(host(dy), host(x), host(w), pos, turns, 1e-5)
+            ref.within(host(grads[i]), dx, ex, (), low, "dx")
+            ref.within(host(grads[2 + i]), dw, ew, (), False, "dw")
+            Hq = self.q.shape[1]
+            got = host(forward[2])[:, :Hq] if i == 0 else host(forward[2])[:, Hq:]
+            ref.within(got, rstd, er * rstd, (), False, "rstd")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("D,R", [(1, 0), (2, 2), (3, 2), (7, 4), (8, 8), (16, 8), (24, 16), (40, 32), (64, 64), (64, 0), (100, 50), (127, 126), (128, 64), (200, 200), (255, 254), (256, 256), (256, 128)])
+def test_heads_widths(dtype, D, R):
+    c = Heads(D + R, dtype, 37, 3, 2, D, R)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,Hq,Hk", [(1, 1, 1), (1, 16, 16), (2, 5, 1), (33, 1, 7), (700, 8, 8), (5000, 2, 1), (3, 70, 33)])
+def test_heads_rows(dtype, M, Hq, Hk):
+    c = Heads(M, dtype, M, Hq, Hk, 64, 64)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_heads_far_positions(dtype):
+    c = Heads(1, dtype, 64, 2, 2, 64, 64)
+    far = torch.tensor([0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, -2 ** 24 - 1, 123456789], dtype=torch.int32, device=DEV)
+    c.position = far[torch.arange(64, device=DEV) % 8].contiguous()
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("front,back", [(0, 8), (8, 16), (1, 2), (3, 0)])
+def test_heads_views(dtype, front, back):
+    c = Heads(2, dtype, 50, 4, 2, 32, 32)
+    plain = c.run()
+    q, k, dyq, dyk = part(c.q, front, back), part(c.k.transpose(0, 1).contiguous(), front, back).transpose(0, 1), part(c.dyq, back, front), c.dyk[:, :1].expand(-1, 2, -1)
+    c.dyk = dyk
+    out, gout = (part(torch.zeros_like(c.q), front, back), torch.zeros_like(c.k)), (torch.zeros_like(c.q), part(torch.zeros_like(c.k), back, front))
+    got = c.run(q, k, dyq, dyk, out=out, gout=gout)
+    c.check(*got)
+    if front % 8 == 0 and back % 8 == 0:      # the same form: else rows are summed in another order
+        assert all(torch.equal(x, y) for x, y in zip(got[0], plain[0]))
+    base = out[0]._base
+    assert torch.isnan(base[..., :front]).all() and torch.isnan(base[..., front + 32:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_heads_in_place(dtype):
+    c = Heads(3, dtype, 40, 3, 3, 64, 32)
+    want, wgrad = c.run()
+    q, k, dyq, dyk = c.q.clone(), c.k.clone(), c.dyq.clone(), c.dyk.clone()
+    seq.norm_heads(q, k, c.wq, c.wk, position=c.position, turns=c.turns, eps=1e-5, out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    got = seq.norm_heads_backward(dyq, dyk, c.q, c.k, want[2], c.wq, c.wk, position=c.position, turns=c.turns, out=(dyq, dyk))
+    assert all(torch.equal(x, y) for x, y in zip(got, wgrad))
+
+
+def test_heads_what_is_not_finite_stays_in_its_head():
+    c = Heads(4, "bf16", 6, 2, 2, 24, 8)
+    (yq, yk, _), grads = c.run()
+    c.q[2, 1, 20], c.k[3, 0, 1] = float("nan"), float("inf")
+    (bq, bk, _), bad = c.run()
+    for x, y, at in ((yq, bq, (2, 1)), (yk, bk, (3, 0)), (grads[0], bad[0], (2, 1)), (grads[1], bad[1], (3, 0))):
+        same = torch.ones(6, 2, dtype=torch.bool)
+        same[at] = False
+        assert torch.equal(x[same.to(DEV)], y[same.to(DEV)]) and not torch.isfinite(y[at]).all()
+
+
+def test_heads_of_nothing_zeros_graphs_and_refusals():
+    c = Heads(5, "fp32", 0, 2, 1, 8, 4)
+    (yq, yk, rstd), grads = c.run()
+    assert yq.shape == (0, 2, 8) and (grads[2] == 0).all() and (grads[3] == 0).all()
+    c = Heads(6, "fp32", 5, 2, 0, 8, 4)
+    (yq, yk, rstd), grads = c.run()
+    assert yk.shape == (5, 0, 8) and (grads[3] == 0).all()
+    c = Heads(7, "bf16", 9, 2, 1, 16, 16)
+    c.q.zero_()
+    c.check(*c.run())
+    c = Heads(8, "bf16", 100, 4, 4, 64, 64)
+    g = torch.cuda.CUDAGraph()
+    c.run()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        got = c.run()
+    for _ in range(3):
+        c.q.copy_(torch.randn_like(c.q))
+        c.position.add_(3)
+        want = c.run()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b))
+    for kw in (dict(turns=c.turns), dict(position=c.position.long(), turns=c.turns), dict(position=c.position[:5], turns=c.turns)):
+        with pytest.raises(ValueError):
+            seq.norm_heads(c.q, c.k, c.wq, c.wk, **kw)
+    with pytest.raises(dqn.DqnError):
+        seq.norm_heads(c.q[..., :32], c.k[..., :32], c.wq[:32], c.wk[:32], position=c.position, turns=c.turns)
+    for bad in ((c.q[0], c.k), (c.q, c.k[:5]), (c.q, c.k.float()), (c.q[..., ::2], c.k)):
+        with pytest.raises(ValueError):
+            seq.norm_heads(*bad, c.wq, c.wk)
+    with pytest.warns(UserWarning, match="detached"):
+        seq.norm_heads(c.q, c.k, c.wq.clone().requires_grad_(), c.wk)
+
+
+# ------------------------------------------------------------------ steps for matrices
+class Steps:
+    def __init__(self, seed, shapes, grad="fp32", size=1e-3):
+        r = np.random.RandomState(seed)
+        self.p = [to(r.randn(*s) * 0.1) for s in shapes]
+        self.g = [to(size * (r.randn(*s) + r.randn(s[0], 1) * r.randn(1, s[1])), TYPES[grad]) for s in shapes]
+        self.m = [to(2 * size * r.randn(*s)) for s in shapes]
+        self.copies = [torch.zeros(s, dtype=torch.bfloat16, device=DEV) for s in shapes]
+        self.kw = dict(lr=0.5, momentum=0.9, weight_decay=[0.1 * i for i in range(len(shapes))])
+
+    def optimizer(self, **kw):
+        return seq.Muon(self.p, self.g, copies=self.copies, state=self.m, **{**self.kw, **kw})
+
+    def expected(self, **kw):
+        kw = {**self.kw, **kw}
+        decay = kw.pop("weight_decay")
+        mu = kw.pop("momentum")
+        return [ref.muon(host(p), host(g), host(m), mu=mu, decay=d, **kw) for p, g, m, d in zip(self.p, self.g, self.m, decay)]
+
+    def check(self, want):
+        for p, m, c, (wp, wm, bound) in zip(self.p, self.m, self.copies, want):
+            if not p.numel():
+                continue
+            # p itself is rounded as it is stored, m by two roundings
+            ref.within(host(p), wp, bound + 2 * ref.U * np.sqrt((wp * wp).sum()), (0, 1), False, "p")
+            assert np.abs(host(m) - wm).max() <= 2 * ref.U * np.abs(wm).max()
+            assert torch.equal(c, p.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("grad", ["fp32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(1, 1)], [(1, 300)], [(300, 1)], [(2, 3), (63, 65), (64, 64), (65, 64)], [(18, 512), (100, 37), (0, 5), (37, 100), (130, 129)], [(257, 600), (600, 257)]])
+def test_muon_shapes(grad, shapes):
+    c = Steps(len(shapes), shapes, grad)
+    want = c.expected()
+    c.optimizer().step()
+    c.check(want)
+
+
+@pytest.mark.parametrize("kw", [dict(nesterov=False), dict(rounds=1), dict(rounds=2), dict(rounds=7), dict(momentum=0.0), dict(lr=0.0), dict(eps=1e-3)])
+def test_muon_settings(kw):
+    c = Steps(3, [(40, 90), (90, 40)])
+    want = c.expected(**kw)
+    c.optimizer(**kw).step()
+    c.check(want)
+
+
+@pytest.mark.parametrize("size", [0.0, 1e-30, 1e-20, 1e15])
+def test_muon_gradients_of_any_size(size):
+    c = Steps(4, [(40, 90), (90, 40)], size=size)
+    want = c.expected(eps=1e-25)
+    c.optimizer(eps=1e-25).step()
+    c.check(want)
+
+
+def test_muon_steps_one_after_another_and_a_matrix_that_is_not_finite():
+    c = Steps(5, [(40, 90), (33, 20), (64, 64)], "bf16")
+    opt = c.optimizer()
+    for k in range(3):
+        for g in c.g:
+            g.copy_(torch.randn_like(g))
+        want = c.expected(lr=0.1 * k)
+        opt.step(lr=0.1 * k)
+        c.check(want)
+    want = c.expected()
+    c.g[1][3, 4] = float("nan")
+    opt.step()
+    assert torch.isnan(c.p[1]).all()
+    for k in (0, 2):
+        ref.within(host(c.p[k]), want[k][0], want[k][2] + 2 * ref.U * np.sqrt((want[k][0] ** 2).sum()), (0, 1), False, "p")
+    opt.close()
+    opt.close()
+
+
+def test_muon_repeats_in_graphs_and_on_other_streams():
+    shapes = [(40, 90), (200, 130)]
+    runs = []
+    for kind in ("eager", "again", "graph", "stream"):
+        c = Steps(6, shapes)
+        opt = c.optimizer()
+        if kind == "graph":
+            side = torch.cuda.CUDAGraph()
+            keep = [x.clone() for x in c.p + c.m]
+            opt.step()
+            for x, y in zip(c.p + c.m, keep):
+                x.copy_(y)
+            torch.cuda.synchronize()
+            with torch.cuda.graph(side):
+                opt.step()
+        for k in range(4):
+            for g in c.g:
+                g.copy_(torch.full_like(g, 1e-3 * (k + 1)) + torch.arange(g.numel(), device=DEV).view(g.shape) % 7 * 1e-3)
+            if kind == "graph":
+                side.replay()
+            elif kind == "stream":
+                s = torch.cuda.Stream()
+                s.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(s):
+                    opt.step()
+                torch.cuda.current_stream().wait_stream(s)
+            else:
+                opt.step()
+            torch.cuda.synchronize()
+        runs.append(c.p + c.m)
+    for other in runs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(runs[0], other))
+
+
+def test_muon_refuses():
+    c = Steps(7, [(8, 9)])
+    for params, grads, kw in (([], [], {}), (c.p, [], {}), ([c.p[0][0]], [c.g[0][0]], dict(state=None)), ([c.p[0].t()], [c.g[0].t()], {}), (c.p, [c.g[0].half()], {}), (c.p, [c.g[0][:4]], {}),
+                              (c.p, c.g, dict(weight_decay=[0.1, 0.2])), (c.p, c.g, dict(copies=[c.p[0]])), (c.p, c.g, dict(state=[c.m[0][:, :3]])), (c.p, c.g, dict(state=c.m * 2))):
+        with pytest.raises(ValueError):
+            seq.Muon(params, grads, **kw)
+    with pytest.raises(dqn.DqnError):
+        seq.Muon(c.p, c.g, weight_decay=-1.0)
+    for kw in (dict(lr=-1.0), dict(lr=float("nan")), dict(momentum=1.0), dict(eps=0.0), dict(rounds=0), dict(rounds=101)):
+        with pytest.raises(dqn.DqnError):
+            c.optimizer(**kw).step()
