@@ -419,7 +419,7 @@ typedef struct {
     int32_t Dk, Dv;                     /* 1..DQN_DELTA_MAX                         */
     float scale;                        /* finite                                   */
     int64_t T;                          /* steps, >= 0 (0: s_last = s0);
-                                           B H ceil(T / 64) at most 2^24            */
+                                           B H ceil(T / 32) at most 2^24            */
     const void *q, *k, *v;              /* [B][T][H][Dk], the same, [B][T][H][Dv]   */
     const void *f, *b;                  /* [B][T][H]                                */
     int64_t q_s[3], k_s[3], v_s[3], f_s[3], b_s[3];
@@ -431,11 +431,13 @@ typedef struct {
     int64_t o_s[3];
     float *s_last;                      /* [B][H][Dk][Dv], or NULL                  */
     float *carry;                       /* for dqn_delta_backward, or NULL: states at
-                                           some of the steps, bytes from
-                                           dqn_delta_sizes                          */
+                                           some of the steps and what lies between
+                                           them, bytes from dqn_delta_sizes, 16-byte
+                                           aligned                                  */
     void *workspace;                    /* forward_workspace bytes from
                                            dqn_delta_sizes, 16-byte aligned; free for
-                                           other use after the call                 */
+                                           other use after the call; not used with
+                                           carry                                    */
 } dqn_delta_args;
 
 /* Gradients of the rule: of all five inputs and of s0, from the gradient of o and of s_last.

@@ -3,118 +3,231 @@
 // Per head, with a_t = sigmoid(f_t), beta_t = sigmoid(b_t) and the state S [Dk][Dv] (zero before a step that starts an episode):
 //   S_t = a_t (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T,  o_t = scale S_t^T q_t.
 // Over a tile of CH steps that the state S enters, with g_i = a_1 .. a_i and G_ij = g_i / g_j (0 where an episode starts in between):
-//   S_i = g_i S + sum_{j <= i} G_ij k_j u_j^T,   (I + N) U = R,   N_ij = beta_i G_ij k_i.k_j (j < i),   R_i = beta_i (v_i - g_i S^T k_i)
+//   S_i = g_i S + sum_{j <= i} G_ij k_j u_j^T,   U = T R,   T = (I + N)^-1,   N_ij = beta_i G_ij k_i.k_j (j < i),   R_i = beta_i (v_i - g_i S^T k_i)
 //   O = scale g Q S + P U,   P_ij = scale G_ij q_i.k_j (j <= i),   S' = g_C S + (G_C. K)^T U.
 // Backward, from dO and the gradient D of the state that leaves:
-//   dU = P^T dO + (G_C. K) D,   (I + N)^T Y = dU,   dS = g_C D + (scale g Q)^T dO - (beta g K)^T Y,   dv = beta Y,   db = (1 - beta) Y.u
-//   dP = dO U^T, dN = -Y U^T:   dq = scale (g S do + (dP G) k),   dk = scale (dP G)^T q + G_C. D u - beta g S y + (dN beta G) k + (dN beta G)^T k
+//   dU = P^T dO + (G_C. K) D,   Y = T^T dU,   dS = g_C D + (scale g Q)^T dO - (beta g K)^T Y,   dv = beta Y,   db = (1 - beta) Y.u
+//   dP = dO U^T, dN = -Y U^T:   dq = scale g S do + (dP scale G) k,   dk = (dP scale G)^T q + G_C. D u - beta g S y + (dN beta G) k + (dN beta G)^T k
 // and, since o_i grows with a_t for every i >= t of the episode while what v_i writes does not shrink with it,
 //   d log a_t = sum_{i >= t} (do_i.o_i - dv_i.v_i) + <D, S'>   (the sum ends with the episode, the last term counts if it lives on),  df = (1 - a) d log a,
 // with do_i.o_i = q_i.dq_i and <D, S'> = g_C <D, S> + sum_j G_Cj u_j.(D^T k_j).
 //
-// All of this is independent per column of S.  A wave owns 16 columns and keeps its part of the state, of R, U, O, Y in registers in
-// the layout in which the matrix instructions leave their results, which is the one in which they take their right operand; the
-// left operands, K, Q, N, P, are the same for all waves and lie in LDS.  So the chain from state to state has no barrier.
+// Three kinds of launch: what a tile needs that no state has part in (T, P, the gates), all tiles at once, a wave each; the chain from state to
+// state, forward or backward, a wave per 16 columns of the state; and the gradients, all tiles at once, a workgroup each.
+//
+// Everything but T and P is independent per column of the state.  A wave of the chain keeps its 16 columns of S, R, U, O in registers in the
+// layout in which the matrix instructions leave their results; with the rows of a pair of 16 x 16 results dealt out so that a lane's eight
+// numbers are eight neighbours (row 8 (l / 16) + 4 (half) + r), that is also the layout in which they take a right operand 32 deep.  So nothing is
+// exchanged between lanes from state to state, and left operands (rows of K, Q, T, P in LDS) are read as they lie, 16 bytes a lane.
+//
+// bf16 inputs are exact operands of the bf16 instructions; a state or a U, which is fp32, is taken apart into three bf16 that are
+// exactly its 24 bits, one instruction for each, where it feeds a state, into two (16 bits) where it only feeds results that are rounded to bf16.
+// fp32 inputs go through the fp32 instructions, of a sixteenth of the rate.
 #pragma once
 #include "seq_common.h"
 
 namespace seq {
 
-constexpr int CH = 64;                 // steps of a tile
-constexpr int CB = CH / 16;
+constexpr int CH = 32;                 // steps of a tile
 constexpr int COLS = 64;               // columns of the state of a workgroup, 16 of each wave
 constexpr float LOG_LEAST = -150.f;    // exp of it is 0 in fp32: a gate that closes further counts as this, so that differences of sums stay finite
 
 using f4 = vec<float, 4>;
+using f8 = vec<float, 8>;
+using b8 = vec<bf16, 8>;
 
 struct Strides {
     long bs, ts, hs;                   // of a sequence, a step, a head
 };
 
-struct DeltaArgs {
+struct DeltaIn {
     const void *q, *k, *v, *f, *b;
     Strides sq, sk, sv, sf, sb;
-    const float *s0;
     const uint8_t *reset;
     long reset_bs, reset_ts;
-    void *o;
-    Strides so;
-    float *last, *carry;               // carry: the state that enters each tile, [B][H][tiles][Dk][Dv]
     long T, tiles;
     int B, H, Dk, Dv;
     float scale;
+    int wide;                          // rows of q and k can be read 16 bytes at a time
 };
-
-struct DeltaGradArgs {
-    const void *q, *k, *v, *f, *b, *dout;
-    Strides sq, sk, sv, sf, sb, sdo;
-    const float *carry, *dlast;
-    const uint8_t *reset;
-    long reset_bs, reset_ts;
+struct DeltaArgs : DeltaIn {
+    const float *s0;
+    void *o;
+    Strides so;
+    float *last, *states, *records;    // states: the one that enters each tile, [B][H][tiles][Dk][Dv], or NULL
+};
+struct DeltaGradArgs : DeltaIn {
+    const void *dout;
+    Strides sdo;
+    const float *states, *records, *dlast;
     void *dq, *dk, *dv, *df, *db;
     Strides sdq, sdk, sdv, sdf, sdb;
     float *ds0;
-    float *into;                       // workspace: the gradient of the state that leaves each tile, as carry
-    long T, tiles;
-    int B, H, Dk, Dv;
-    float scale;
+    float *into;                       // the gradient of the state that leaves each tile, as states
 };
 
-__device__ __forceinline__ f4 mm4(f4 a, f4 b, f4 c)
-{
-#pragma unroll
-    for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
-    return c;
-}
-// 16 x 16 of a matrix in LDS as left operand: rows m0.., columns k0..; its transposed: rows m0.. are columns of the stored one
-template <int LD> __device__ __forceinline__ f4 rows_of(const float *p, int m0, int k0, int lane)
-{
-    return *reinterpret_cast<const f4 *>(p + (m0 + (lane & 15)) * LD + k0 + 4 * (lane >> 4));
-}
-template <int LD> __device__ __forceinline__ f4 cols_of(const float *p, int m0, int k0, int lane)
-{
-    const float *a = p + (k0 + 4 * (lane >> 4)) * LD + m0 + (lane & 15);
-    return f4{a[0], a[LD], a[2 * LD], a[3 * LD]};
-}
-
-// What the waves share of a tile.  Rows outside [lo, hi) are steps that do nothing: keys, queries and rates zero, gates one.
-template <int DK> struct DeltaTile {
-    static constexpr int LD = DK + 4, LC = CH + 4;
-    float q[CH * LD], k[CH * LD];
-    float n[CH * LC];                  // -N below the blocks of the diagonal, on which (I + N)^-1 of the block
-    float p[CH * LC];                  // P; upper blocks are not written
-    float run_hi[CH], run_lo[CH];      // sum of log a up to each step, as a multiple of 2^-10 and the rest
+// What the first launch leaves of a tile.
+struct DeltaRecord {
+    float t[CH * CH], p[CH * CH];
+    float since[CH], until[CH], beta[CH];   // g_i, 0 behind an episode's start; G_Ci, 0 before one
     float gate[CH];                    // a
-    float since[CH], until[CH], beta[CH];   // g_i; G_Ci, 0 where the episode ends in the tile
+    float run_hi[CH], run_lo[CH];      // sum of log a up to each step, as a multiple of 2^-10 and the rest
     int cut[CH];                       // episodes that have started up to each step
 };
+static_assert(sizeof(DeltaRecord) % 16 == 0, "records are copied 16 bytes at a time");
 
-// The factor from step j to step i >= j: differences of the multiples of 2^-10 are exact, so that a gate that closed long before leaves
-// no rounding in later ones.
-template <class Tile> __device__ __forceinline__ float between(const Tile &s, int i, int j)
+// ---------------------------------------------------------------- operands, 8 numbers deep a lane
+// a, b of a word as their upper halves
+__device__ __forceinline__ uint32_t uppers(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// N bf16 whose sum is the number, exactly for N = 3 (each takes eight bits off); the last of two is rounded.
+template <int N> struct Planes {
+    b8 p[N];
+};
+template <int N> __device__ __forceinline__ Planes<N> planes(const float (&v)[8])
 {
-    return s.cut[i] == s.cut[j] ? __expf((s.run_hi[i] - s.run_hi[j]) + (s.run_lo[i] - s.run_lo[j])) : 0.f;
+    vec<uint32_t, 4> w[N];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float x = v[i], y = v[i + 1];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+            if (N == 2 && n == 1) a += 0x8000u, b += 0x8000u;
+            w[n][i / 2] = uppers(a, b);
+            if (n + 1 < N) {
+                x -= __uint_as_float(a & 0xFFFF0000u);
+                y -= __uint_as_float(b & 0xFFFF0000u);
+            }
+        }
+    }
+    Planes<N> o;
+#pragma unroll
+    for (int n = 0; n < N; ++n) o.p[n] = __builtin_bit_cast(b8, w[n]);
+    return o;
 }
 
-// Fills the tile from step t0 on; rows outside [lo, hi) stay out of it.  Every thread of 256 takes part; the barrier before it is the caller's.
-template <class E, int DK, class Args> __device__ void delta_tile(const Args &A, DeltaTile<DK> &s, int bi, int h, long t0, int lo, int hi)
+__device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma(f8 a, f8 b, f4 c)
 {
-    using Tile = DeltaTile<DK>;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const E *q = (const E *)A.q + bi * A.sq.bs + t0 * A.sq.ts + h * A.sq.hs;
-    const E *k = (const E *)A.k + bi * A.sk.bs + t0 * A.sk.ts + h * A.sk.hs;
-    for (int e = tid; e < CH * DK; e += 256) {
-        const int r = e / DK, c = e % DK;
-        const bool in = r >= lo && r < hi && c < A.Dk;
-        s.q[r * Tile::LD + c] = in ? (float)q[r * A.sq.ts + c] : 0.f;
-        s.k[r * Tile::LD + c] = in ? (float)k[r * A.sk.ts + c] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// Operands for inputs of type E.  Exact: of the inputs themselves; Split<N>: of fp32 numbers.
+template <class E> struct Operand;
+template <> struct Operand<bf16> {
+    using Exact = b8;
+    template <int N> using Split = Planes<N>;
+    template <int N> static __device__ __forceinline__ Planes<N> split(const float (&v)[8]) { return planes<N>(v); }
+    template <int N> static __device__ __forceinline__ f4 mul(b8 a, const Planes<N> &b, f4 c)
+    {
+#pragma unroll
+        for (int n = N - 1; n >= 0; --n) c = mfma(a, b.p[n], c);
+        return c;
     }
-    if (w == 0) {
-        const bool in = lane >= lo && lane < hi;
-        const long t = t0 + lane;
+    template <int N> static __device__ __forceinline__ f4 mul(const Planes<N> &a, b8 b, f4 c)
+    {
+#pragma unroll
+        for (int n = N - 1; n >= 0; --n) c = mfma(a.p[n], b, c);
+        return c;
+    }
+    static __device__ __forceinline__ f4 mul(const Planes<2> &a, const Planes<2> &b, f4 c)
+    {
+        c = mfma(a.p[1], b.p[0], c);
+        c = mfma(a.p[0], b.p[1], c);
+        return mfma(a.p[0], b.p[0], c);
+    }
+    static __device__ __forceinline__ f4 mul(b8 a, b8 b, f4 c) { return mfma(a, b, c); }
+};
+template <> struct Operand<float> {
+    using Exact = f8;
+    template <int N> using Split = f8;
+    template <int N> static __device__ __forceinline__ f8 split(const float (&v)[8])
+    {
+        f8 o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = v[i];
+        return o;
+    }
+    static __device__ __forceinline__ f4 mul(f8 a, f8 b, f4 c) { return mfma(a, b, c); }
+    template <int N> static __device__ __forceinline__ f4 mul(f8 a, f8 b, f4 c) { return mfma(a, b, c); }
+};
+
+__device__ __forceinline__ f8 both(f4 a, f4 b) { return f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+template <class E, int N> __device__ __forceinline__ typename Operand<E>::template Split<N> split(f4 a, f4 b)
+{
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return Operand<E>::template split<N>(v);
+}
+template <class E, int N> __device__ __forceinline__ f4 mul(typename Operand<E>::Exact a, const typename Operand<E>::template Split<N> &b, f4 c)
+{
+    if constexpr (std::is_same<E, float>::value) return mfma(a, b, c);
+    else return Operand<bf16>::template mul<N>(a, b, c);
+}
+
+// The step of a tile that row `rho` of result `half` of a pair stands for, and the row of the state in 32 of them.
+__device__ __forceinline__ int dealt(int half, int rho) { return 8 * (rho >> 2) + 4 * half + (rho & 3); }
+
+// 8 numbers of a row from column c on, zeros from D on
+template <class E> __device__ __forceinline__ vec<E, 8> load8(const E *p, int c, int D, bool real, int wide)
+{
+    vec<E, 8> v = vec<E, 8>(0.f);
+    if (!real) return v;
+    if (wide) {
+        constexpr int V = 16 / (int)sizeof(E);
+#pragma unroll
+        for (int i = 0; i < 8; i += V)
+            if (c + i < D) {
+                const vec<E, V> x = load<V>(p + c + i);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[i + e] = x[e];
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < D) v[i] = p[c + i];
+    }
+    return v;
+}
+
+__device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// ---------------------------------------------------------------- T, P and the gates of every tile
+template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(DeltaIn A, DeltaRecord *records)
+{
+    constexpr int LN = CH + 4, KS = DK / 32;
+    struct Own {
+        float n[CH * LN];
+        float run_hi[CH], run_lo[CH], beta[CH];
+        int cut[CH];
+    };
+    __shared__ __align__(16) Own all[4];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const long id = (long)blockIdx.x * 4 + w;
+    if (id >= (long)A.B * A.H * A.tiles) return;      // whole waves, and no barrier follows
+    Own &s = all[w];
+    const long head = id / A.tiles, tile = id % A.tiles, t0 = tile * CH;
+    const int bi = (int)(head / A.H), h = (int)(head % A.H), rows = (int)min((long)CH, A.T - t0);
+    DeltaRecord &out = records[id];
+    const E *q = (const E *)A.q + bi * A.sq.bs + t0 * A.sq.ts + h * A.sq.hs, *k = (const E *)A.k + bi * A.sk.bs + t0 * A.sk.ts + h * A.sk.hs;
+    vec<E, 8> kf[2][KS], qf[2][KS];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int r = 16 * m + col;
+            kf[m][ks] = load8<E>(k + r * A.sk.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
+            qf[m][ks] = load8<E>(q + r * A.sq.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
+        }
+    {   // both halves of the wave do the same
+        const int i = lane & 31;
+        const bool in = i < rows;
         float la = 0.f, beta = 0.f;
         int cut = 0;
         if (in) {
+            const long t = t0 + i;
             const float f = (float)((const E *)A.f)[bi * A.sf.bs + t * A.sf.ts + h * A.sf.hs];
             const float b = (float)((const E *)A.b)[bi * A.sb.bs + t * A.sb.ts + h * A.sb.hs];
             la = (f < 0.f ? f : 0.f) - log1pf(expf(-fabsf(f)));
@@ -122,92 +235,203 @@ template <class E, int DK, class Args> __device__ void delta_tile(const Args &A,
             beta = 1.f / (1.f + expf(-b));
             cut = A.reset && A.reset[bi * A.reset_bs + t * A.reset_ts];
         }
-        s.gate[lane] = expf(la);
         double run = la;
         int cuts = cut;
 #pragma unroll
         for (int d = 1; d < CH; d *= 2) {
-            const double o = __shfl_up(run, d);
-            const int oc = __shfl_up(cuts, d);
-            if (lane >= d) run += o, cuts += oc;
+            const double o = __shfl_up(run, d, 32);
+            const int oc = __shfl_up(cuts, d, 32);
+            if (i >= d) run += o, cuts += oc;
         }
-        const double whole = rint(run * 1024.0) * (1.0 / 1024.0);
-        s.run_hi[lane] = (float)whole;
-        s.run_lo[lane] = (float)(run - whole);
-        s.cut[lane] = cuts;
-        s.beta[lane] = beta;
-        s.since[lane] = cuts ? 0.f : expf((float)run);
-        const double end = __shfl(run, CH - 1);
-        const int last = __shfl(cuts, CH - 1);
-        s.until[lane] = in && cuts == last ? expf((float)(end - run)) : 0.f;
-    }
-    __syncthreads();
-    const int col = lane & 15, row = 4 * (lane >> 4);
-#pragma unroll
-    for (int n = 0; n < CB; ++n) {
-        if (n > w) break;
-        f4 kk = {}, qk = {};
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) {
-            const f4 b = rows_of<Tile::LD>(s.k, 16 * n, 16 * kb, lane);
-            kk = mm4(rows_of<Tile::LD>(s.k, 16 * w, 16 * kb, lane), b, kk);
-            qk = mm4(rows_of<Tile::LD>(s.q, 16 * w, 16 * kb, lane), b, qk);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + row + r, j = 16 * n + col;
-            const float g = j <= i ? between(s, i, j) : 0.f;
-            s.n[i * Tile::LC + j] = j < i && g != 0.f ? -s.beta[i] * g * kk[r] : 0.f;
-            s.p[i * Tile::LC + j] = g != 0.f ? A.scale * g * qk[r] : 0.f;
+        const double whole = rint(run * 1024.0) * (1.0 / 1024.0), end = __shfl(run, CH - 1, 32);
+        const int last = __shfl(cuts, CH - 1, 32);
+        if (lane < CH) {
+            s.run_hi[i] = out.run_hi[i] = (float)whole;
+            s.run_lo[i] = out.run_lo[i] = (float)(run - whole);
+            s.cut[i] = out.cut[i] = cuts;
+            s.beta[i] = out.beta[i] = beta;
+            out.gate[i] = expf(la);
+            out.since[i] = cuts ? 0.f : expf((float)run);
+            out.until[i] = in && cuts == last ? expf((float)(end - run)) : 0.f;
         }
     }
-    __syncthreads();
-    // (I + N)^-1 of the blocks on the diagonal by forward substitution, a column per lane
-    if (w == 0) {
-        float *blk = s.n + (16 * (lane >> 4)) * (Tile::LC + 1);
+    wave_sync();
+    // The factor from step j to step i >= j: differences of the multiples of 2^-10 are exact, so that a gate that closed long before
+    // leaves no rounding in later ones.
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            f4 kk = {}, qk = {};
+            if (n <= m)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    kk = mfma(kf[m][ks], kf[n][ks], kk);
+                    qk = mfma(qf[m][ks], kf[n][ks], qk);
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * m + 4 * g + r, j = 16 * n + col;
+                const float b = j <= i && s.cut[i] == s.cut[j] ? expf((s.run_hi[i] - s.run_hi[j]) + (s.run_lo[i] - s.run_lo[j])) : 0.f;
+                if (n <= m) s.n[i * LN + j] = j < i && b != 0.f ? -s.beta[i] * b * kk[r] : 0.f;
+                out.p[i * CH + j] = b != 0.f ? A.scale * b * qk[r] : 0.f;
+            }
+        }
+    wave_sync();
+    // (I + N)^-1 of the two blocks on the diagonal by forward substitution, a column per lane, in their places
+    if (lane < 32) {
+        float *blk = s.n + 16 * g * (LN + 1);
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             float v = i == col ? 1.f : 0.f;
 #pragma unroll
-            for (int j = 0; j < i; ++j) v = fmaf(blk[i * Tile::LC + j], x[j], v);
+            for (int j = 0; j < i; ++j) v = fmaf(blk[i * LN + j], x[j], v);
             x[i] = v;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) blk[i * Tile::LC + col] = x[i];
+        for (int i = 0; i < 16; ++i) blk[i * LN + col] = x[i];
     }
-    __syncthreads();
+    wave_sync();
+    // below them T11 (-N10) T00: a result's layout is that of the next right operand, 16 deep
+    f4 x = {}, y = {};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(s.n[(16 + col) * LN + 4 * g + e], s.n[(4 * g + e) * LN + col], x, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(s.n[(16 + col) * LN + 16 + 4 * g + e], x[e], y, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = 4 * g + r;
+        out.t[i * CH + col] = s.n[i * LN + col];
+        out.t[i * CH + 16 + col] = 0.f;
+        out.t[(16 + i) * CH + col] = y[r];
+        out.t[(16 + i) * CH + 16 + col] = s.n[(16 + i) * LN + 16 + col];
+    }
 }
 
-template <class Tile> __device__ __forceinline__ f4 four(const float *p, int m0, int lane) { return *reinterpret_cast<const f4 *>(p + m0 + 4 * (lane >> 4)); }
+// ---------------------------------------------------------------- what a workgroup holds of a tile in LDS
+template <class E, int DK> struct DeltaTile {
+    static constexpr int LD = DK + 16 / (int)sizeof(E), LC = CH + 4;
+    E q[CH * LD], k[CH * LD];
+    float t[CH * LC], p[CH * LC];
+    float vectors[7 * CH];             // as in the record
+    __device__ __forceinline__ const float *since() const { return vectors; }
+    __device__ __forceinline__ const float *until() const { return vectors + CH; }
+    __device__ __forceinline__ const float *beta() const { return vectors + 2 * CH; }
+    __device__ __forceinline__ const float *gate() const { return vectors + 3 * CH; }
+    __device__ __forceinline__ const float *run_hi() const { return vectors + 4 * CH; }
+    __device__ __forceinline__ const float *run_lo() const { return vectors + 5 * CH; }
+    __device__ __forceinline__ const int *cut() const { return reinterpret_cast<const int *>(vectors + 6 * CH); }
+    __device__ __forceinline__ float between(int i, int j) const
+    {
+        return cut()[i] == cut()[j] ? expf((run_hi()[i] - run_hi()[j]) + (run_lo()[i] - run_lo()[j])) : 0.f;
+    }
+};
 
-// R of a wave's columns, then U in its place.  state: the state that enters, or its part of 0 where none does.
-template <class E, int DK, class Args>
-__device__ __forceinline__ void delta_u(const Args &A, const DeltaTile<DK> &s, const f4 (&state)[DK / 16], int bi, int h, long t0, int lo, int hi, int c, f4 (&u)[CB], f4 (*val)[CB] = nullptr)
-{
-    using Tile = DeltaTile<DK>;
-    const int lane = threadIdx.x & 63, row = 4 * (lane >> 4);
-    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs + c;
+// The part of a tile that a thread of 256 brings from memory: into registers first, so that it can arrive while the tile before is worked on.
+template <class E, int DK> struct DeltaFetch {
+    static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + 255) / 256;
+    vec<E, V> q[N], k[N];
+    f4 t, p, vectors;
+    __device__ __forceinline__ void load(const DeltaIn &A, const DeltaRecord *records, long head, long tile)
+    {
+        const long t0 = tile * CH;
+        const int bi = (int)(head / A.H), h = (int)(head % A.H), rows = (int)min((long)CH, A.T - t0);
+        const E *qp = (const E *)A.q + bi * A.sq.bs + t0 * A.sq.ts + h * A.sq.hs, *kp = (const E *)A.k + bi * A.sk.bs + t0 * A.sk.ts + h * A.sk.hs;
 #pragma unroll
-    for (int m = 0; m < CB; ++m) {
-        f4 ks = {};
+        for (int n = 0; n < N; ++n) {
+            const int e = threadIdx.x + 256 * n, r = e / PER, c = e % PER * V;
+            vec<E, V> a = vec<E, V>(0.f), b = vec<E, V>(0.f);
+            if (r < rows && c < A.Dk) {
+                if (A.wide) {
+                    a = seq::load<V>(qp + r * A.sq.ts + c);
+                    b = seq::load<V>(kp + r * A.sk.ts + c);
+                } else {
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) ks = mm4(rows_of<Tile::LD>(s.k, 16 * m, 16 * kb, lane), state[kb], ks);
-        f4 r = {};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 16 * m + row + e;
-            if (i >= lo && i < hi) {
-                const float x = c < A.Dv ? (float)v[i * A.sv.ts] : 0.f;
-                if (val) (*val)[m][e] = x;
-                r[e] = s.beta[i] * (x - (s.cut[i] ? 0.f : s.since[i] * ks[e]));
-            } else if (val) (*val)[m][e] = 0.f;
+                    for (int i = 0; i < V; ++i)
+                        if (c + i < A.Dk) {
+                            a[i] = qp[r * A.sq.ts + c + i];
+                            b[i] = kp[r * A.sk.ts + c + i];
+                        }
+                }
+            }
+            q[n] = a;
+            k[n] = b;
         }
+        const DeltaRecord &rec = records[head * A.tiles + tile];
+        t = seq::load<4>(rec.t + 4 * threadIdx.x);
+        p = seq::load<4>(rec.p + 4 * threadIdx.x);
+        if (threadIdx.x < 7 * CH / 4) vectors = seq::load<4>(rec.since + 4 * threadIdx.x);
+    }
+    __device__ __forceinline__ void put(DeltaTile<E, DK> &s) const
+    {
+        using Tile = DeltaTile<E, DK>;
 #pragma unroll
-        for (int kb = 0; kb < m; ++kb) r = mm4(rows_of<Tile::LC>(s.n, 16 * m, 16 * kb, lane), u[kb], r);
-        u[m] = mm4(rows_of<Tile::LC>(s.n, 16 * m, 16 * m, lane), r, f4{});
+        for (int n = 0; n < N; ++n) {
+            const int e = threadIdx.x + 256 * n, r = e / PER, c = e % PER * V;
+            if (r < CH) {
+                seq::store<V>(s.q + r * Tile::LD + c, q[n]);
+                seq::store<V>(s.k + r * Tile::LD + c, k[n]);
+            }
+        }
+        const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+        seq::store<4>(s.t + r * Tile::LC + c, t);
+        seq::store<4>(s.p + r * Tile::LC + c, p);
+        if (threadIdx.x < 7 * CH / 4) seq::store<4>(s.vectors + 4 * threadIdx.x, vectors);
+    }
+};
+static_assert(offsetof(DeltaRecord, cut) - offsetof(DeltaRecord, since) == 6 * CH * 4, "the vectors lie one behind the other");
+
+template <class T> __device__ __forceinline__ vec<T, 8> eight(const T *p)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    vec<T, 8> v;
+#pragma unroll
+    for (int i = 0; i < 8; i += V) {
+        const vec<T, V> x = load<V>(p + i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[i + e] = x[e];
+    }
+    return v;
+}
+
+// Rows of a matrix of steps (K, Q) as left operand for half a pair: dealt rows, columns 32 p..
+template <class E, int LD> __device__ __forceinline__ vec<E, 8> rows_of(const E *m, int half, int p, int lane)
+{
+    return eight(m + dealt(half, lane & 15) * LD + 32 * p + 8 * (lane >> 4));
+}
+// Its transposed, the rows being the dealt columns of 32 p.., 32 steps deep.  In bf16 by the transposing LDS read: of four rows that a group of 16 lanes
+// points at, four lanes a row, each lane gets one column.
+template <class E, int LD> __device__ __forceinline__ vec<E, 8> columns_of(const E *m, int half, int p, int lane)
+{
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (std::is_same<E, float>::value) {
+        const float *a = m + 8 * g * LD + 32 * p + dealt(half, i);
+        f8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = a[e * LD];
+        return v;
+    } else {
+        using s4 = vec<short, 4>;
+        const bf16 *a = m + (8 * g + (i >> 2)) * LD + 32 * p + 8 * (i & 3) + 4 * half;
+        typedef __attribute__((address_space(3))) s4 *At;
+        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)a), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(a + 4 * LD));
+        vec<short, 8> v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        return __builtin_bit_cast(b8, v);
     }
 }
+// Rows of T or P (fp32) as left operand, and of their transposed
+template <int LC> __device__ __forceinline__ f8 square_rows(const float *m, int half, int lane) { return eight(m + dealt(half, lane & 15) * LC + 8 * (lane >> 4)); }
+template <int LC> __device__ __forceinline__ f8 square_columns(const float *m, int half, int lane)
+{
+    const float *a = m + 8 * (lane >> 4) * LC + dealt(half, lane & 15);
+    f8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = a[e * LC];
+    return v;
+}
+// Numbers of a step each, of the dealt steps of half a pair that a lane holds
+__device__ __forceinline__ f4 of_steps(const float *p, int half, int lane) { return load<4>(p + 8 * (lane >> 4) + 4 * half); }
 
 template <int N> __device__ __forceinline__ bool finite(const f4 (&v)[N])
 {
@@ -218,445 +442,624 @@ template <int N> __device__ __forceinline__ bool finite(const f4 (&v)[N])
         for (int e = 0; e < 4; ++e) ok &= fabsf(v[i][e]) < INFINITY;
     return ok;
 }
+__device__ __forceinline__ f4 where(f4 factor, f4 v)      // factor v, 0 where factor is 0, whatever v is
+{
+    f4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = factor[e] != 0.f ? factor[e] * v[e] : 0.f;
+    return o;
+}
+__device__ __forceinline__ f4 where(float factor, f4 v) { return where(f4(factor), v); }
 
-// A workgroup per head and COLS columns, tile after tile.  A tile whose result holds a number that is not finite is taken again step by step,
-// where nothing is multiplied by the zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
+// the sum over the four groups of 16 lanes, in all of them
+__device__ __forceinline__ float groups_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(x), __float_as_int(x), false, false);
+    x = __int_as_float((int)r[0]) + __int_as_float((int)r[1]);
+    float lo, hi;
+    halves(x, lo, hi);
+    return lo + hi;
+}
+
+// A wave's columns of a state: state[2 p + half][r] is row 32 p + 8 (l / 16) + 4 half + r, column c.
+template <int DK> struct Columns {
+    f4 s[DK / 16];
+    __device__ __forceinline__ void get(const float *from, int Dk, int Dv, int c, int lane)
+    {
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
+                s[n][e] = from && c < Dv && d < Dk ? from[(long)d * Dv + c] : 0.f;
+            }
+    }
+    __device__ __forceinline__ void put(float *to, int Dk, int Dv, int c, int lane) const
+    {
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
+                if (c < Dv && d < Dk) to[(long)d * Dv + c] = s[n][e];
+            }
+    }
+    // sum over rows of x_d S_dc, x a step's row of K or Q in LDS
+    template <class E> __device__ __forceinline__ float dot(const E *x, int lane) const
+    {
+        float sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf((float)x[32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e], s[n][e], sum);
+        return groups_sum(sum);
+    }
+    template <class E> __device__ __forceinline__ void add(const E *x, float y, int lane)
+    {
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = fmaf((float)x[32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e], y, s[n][e]);
+    }
+    __device__ __forceinline__ void scaled(float a)
+    {
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) s[n] *= a;
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) s[n] = f4{};
+    }
+};
+
+template <class Tile> __device__ __forceinline__ bool starts(const Tile &s, int i) { return s.cut()[i] != (i ? s.cut()[i - 1] : 0); }
+
+// One step as its definition has it; the state after it.  -> what is written, beta (v - S^T k)
+template <class E, int DK> __device__ __forceinline__ float delta_step(const DeltaTile<E, DK> &s, Columns<DK> &S, int i, float v, int lane)
+{
+    using Tile = DeltaTile<E, DK>;
+    if (starts(s, i)) S.clear();
+    S.scaled(s.gate()[i]);
+    const float u = s.beta()[i] * (v - S.dot(s.k + i * Tile::LD, lane));
+    S.add(s.k + i * Tile::LD, u, lane);
+    return u;
+}
+// and the gradient of the state before step i from that after it, do and q being the step's.  -> the gradient of v
+template <class E, int DK> __device__ __forceinline__ float delta_step_back(const DeltaTile<E, DK> &s, Columns<DK> &D, int i, float dout, float scale, int lane)
+{
+    using Tile = DeltaTile<E, DK>;
+    D.add(s.q + i * Tile::LD, scale * dout, lane);
+    const float dv = s.beta()[i] * D.dot(s.k + i * Tile::LD, lane);
+    D.add(s.k + i * Tile::LD, -dv, lane);
+    return dv;
+}
+template <class E, int DK> __device__ __forceinline__ void delta_pass_back(const DeltaTile<E, DK> &s, Columns<DK> &D, int i)
+{
+    if (starts(s, i)) D.clear();
+    else D.scaled(s.gate()[i]);
+}
+
+// A lane's numbers of column c of a tensor of steps [..][Dv] (V, dO), and storing them
+template <class E> __device__ __forceinline__ void get_steps(const E *p, long ts, bool mine, int rows, int lane, f4 (&v)[2])
+{
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 8 * (lane >> 4) + 4 * m + e;
+            v[m][e] = mine && i < rows ? (float)p[i * ts] : 0.f;
+        }
+}
+template <class E> __device__ __forceinline__ void put_steps(E *p, long ts, bool mine, int rows, int lane, const f4 (&v)[2])
+{
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 8 * (lane >> 4) + 4 * m + e;
+            if (mine && i < rows) p[i * ts] = (E)v[m][e];
+        }
+}
+
+// U of a wave's columns from the state that enters and V.
+template <class E, int DK, int N> __device__ __forceinline__ void delta_u(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&S)[DK / 32], const f4 (&v)[2], int rows, int lane, f4 (&u)[2])
+{
+    using Tile = DeltaTile<E, DK>;
+    f4 r[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        f4 ks = {};
+#pragma unroll
+        for (int p = 0; p < DK / 32; ++p) ks = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), S[p], ks);
+        const f4 old = where(of_steps(s.since(), m, lane), ks), beta = of_steps(s.beta(), m, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[m][e] = 8 * (lane >> 4) + 4 * m + e < rows ? beta[e] * (v[m][e] - old[e]) : 0.f;
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) u[m] = mfma(square_rows<Tile::LC>(s.t, m, lane), both(r[0], r[1]), f4{});
+}
+
+// ---------------------------------------------------------------- from state to state
+// A workgroup per head and COLS columns.  A tile whose results hold a number that is not finite is taken again step by step as the definition
+// has it, where nothing is multiplied by the zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta(DeltaArgs A)
 {
-    using Tile = DeltaTile<DK>;
+    using Tile = DeltaTile<E, DK>;
     extern __shared__ __align__(16) unsigned char lds[];
-    Tile &s = *reinterpret_cast<Tile *>(lds);
-    const int lane = threadIdx.x & 63, row = 4 * (lane >> 4);
+    Tile *tiles = reinterpret_cast<Tile *>(lds);
+    const int lane = threadIdx.x & 63;
     const int slices = (A.Dv + COLS - 1) / COLS, slice = blockIdx.x % slices;
     const long head = blockIdx.x / slices;
     const int bi = (int)(head / A.H), h = (int)(head % A.H), c = COLS * slice + 16 * (threadIdx.x >> 6) + (lane & 15);
     const bool mine = c < A.Dv;
-    f4 state[DK / 16];
-#pragma unroll
-    for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int d = 16 * kb + row + e;
-            state[kb][e] = A.s0 && mine && d < A.Dk ? A.s0[(head * A.Dk + d) * A.Dv + c] : 0.f;
-        }
-    auto put = [&](float *to) {
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 16 * kb + row + e;
-                if (mine && d < A.Dk) to[(long)d * A.Dv + c] = state[kb][e];
-            }
-    };
+    const E *v = (const E *)A.v + bi * A.sv.bs + h * A.sv.hs + c;
+    E *o = (E *)A.o + bi * A.so.bs + h * A.so.hs + c;
+    const DeltaRecord *records = (const DeltaRecord *)A.records;
+    Columns<DK> S;
+    S.get(A.s0 ? A.s0 + head * A.Dk * A.Dv : nullptr, A.Dk, A.Dv, c, lane);
+    DeltaFetch<E, DK> fetch;
+    f4 val[2], next_val[2];
+    if (A.tiles) {
+        fetch.load(A, records, head, 0);
+        get_steps(v, A.sv.ts, mine, (int)min((long)CH, A.T), lane, next_val);
+        fetch.put(tiles[0]);
+    }
+    __syncthreads();
     for (long tile = 0; tile < A.tiles; ++tile) {
+        const Tile &s = tiles[tile & 1];
         const long t0 = tile * CH;
         const int rows = (int)min((long)CH, A.T - t0);
-        if (A.carry) put(A.carry + (head * A.tiles + tile) * A.Dk * A.Dv);
-        E *o = (E *)A.o + bi * A.so.bs + t0 * A.so.ts + h * A.so.hs + c;
-        for (int lo = 0, hi = rows; lo < rows;) {
-            delta_tile<E, DK>(A, s, bi, h, t0, lo, hi);
-            f4 u[CB], out[CB], next[DK / 16];
-            delta_u<E, DK>(A, s, state, bi, h, t0, lo, hi, c, u);
-#pragma unroll
-            for (int m = 0; m < CB; ++m) {
-                f4 qs = {};
-#pragma unroll
-                for (int kb = 0; kb < DK / 16; ++kb) qs = mm4(rows_of<Tile::LD>(s.q, 16 * m, 16 * kb, lane), state[kb], qs);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    qs[e] = s.cut[i] ? 0.f : A.scale * s.since[i] * qs[e];
-                }
-#pragma unroll
-                for (int kb = 0; kb <= m; ++kb) qs = mm4(rows_of<Tile::LC>(s.p, 16 * m, 16 * kb, lane), u[kb], qs);
-                out[m] = qs;
-            }
-#pragma unroll
-            for (int m = 0; m < CB; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float left = s.until[16 * m + row + e];
-                    u[m][e] = left != 0.f ? left * u[m][e] : 0.f;
-                }
-            const bool lives = !s.cut[CH - 1];
-            const float left = s.since[CH - 1];
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                f4 n;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) n[e] = lives ? left * state[d][e] : 0.f;
-#pragma unroll
-                for (int kb = 0; kb < CB; ++kb) n = mm4(cols_of<Tile::LD>(s.k, 16 * d, 16 * kb, lane), u[kb], n);
-                next[d] = n;
-            }
-            const bool ok = finite(out) && finite(next);
-            const bool again = __syncthreads_or(!ok) && hi - lo > 1;
-            if (again) {
-                hi = lo + 1;
-                continue;
-            }
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) state[d] = next[d];
-#pragma unroll
-            for (int m = 0; m < CB; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    if (mine && i >= lo && i < hi) o[i * A.so.ts] = (E)out[m][e];
-                }
-            lo = hi++;
+        val[0] = next_val[0];
+        val[1] = next_val[1];
+        const bool more = tile + 1 < A.tiles;
+        if (more) {
+            fetch.load(A, records, head, tile + 1);
+            get_steps(v + (t0 + CH) * A.sv.ts, A.sv.ts, mine, (int)min((long)CH, A.T - t0 - CH), lane, next_val);
         }
+        if (A.states) S.put(A.states + (head * A.tiles + tile) * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
+        typename Operand<E>::template Split<3> sp[DK / 32];
+#pragma unroll
+        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(S.s[2 * p], S.s[2 * p + 1]);
+        f4 u[2], out[2];
+        delta_u<E, DK, 3>(s, sp, val, rows, lane, u);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            f4 qs = {};
+#pragma unroll
+            for (int p = 0; p < DK / 32; ++p) {
+                const auto a = rows_of<E, Tile::LD>(s.q, m, p, lane);
+                if constexpr (std::is_same<E, float>::value) qs = mfma(a, sp[p], qs);
+                else qs = mfma(a, sp[p].p[0], mfma(a, sp[p].p[1], qs));     // o is rounded to bf16: 16 bits of the state do
+            }
+            qs = where(of_steps(s.since(), m, lane), A.scale * qs);
+            out[m] = mfma(square_rows<Tile::LC>(s.p, m, lane), both(u[0], u[1]), qs);
+        }
+        const auto up = split<E, 3>(where(of_steps(s.until(), 0, lane), u[0]), where(of_steps(s.until(), 1, lane), u[1]));
+        f4 next[DK / 16];
+        const float left = s.since()[CH - 1];
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.k, n & 1, n >> 1, lane), up, where(left, S.s[n]));
+        if (__any(!(finite(out) && finite(next)))) {
+            for (int i = 0; i < rows; ++i) {
+                delta_step<E, DK>(s, S, i, mine ? (float)v[(t0 + i) * A.sv.ts] : 0.f, lane);
+                const float x = A.scale * S.dot(s.q + i * Tile::LD, lane);
+                if (mine && lane < 16) o[(t0 + i) * A.so.ts] = (E)x;
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < DK / 16; ++n) S.s[n] = next[n];
+            put_steps(o + t0 * A.so.ts, A.so.ts, mine, rows, lane, out);
+        }
+        if (more) fetch.put(tiles[(tile + 1) & 1]);
+        lds_barrier();
     }
-    if (A.last) put(A.last + head * A.Dk * A.Dv);
+    if (A.last) S.put(A.last + head * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
 }
 
-// The end of the episode that step lo begins or continues, at most `rows`: for tiles that are taken again episode by episode.
-template <class Args> __device__ __forceinline__ int episode_end(const Args &A, int bi, long t0, int lo, int rows)
+// kd = (G_C. K) D, then Y = T^T (P^T dO + kd) of a wave's columns.
+template <class E, int DK, int N>
+__device__ __forceinline__ void delta_y(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&D)[DK / 32], const f4 (&dout)[2], int lane, f4 (&kd)[2], f4 (&y)[2])
 {
-    int hi = lo + 1;
-    while (hi < rows && !(A.reset && A.reset[bi * A.reset_bs + (t0 + hi) * A.reset_ts])) ++hi;
-    return hi;
-}
-// Its beginning, for an end `hi`.
-template <class Args> __device__ __forceinline__ int episode_begin(const Args &A, int bi, long t0, int hi)
-{
-    int lo = hi - 1;
-    while (lo > 0 && !(A.reset && A.reset[bi * A.reset_bs + (t0 + lo) * A.reset_ts])) --lo;
-    return lo;
-}
-
-// dU, then Y in its place: (I + N)^T Y = dU from the last rows up.  out: dO of the wave's columns; D: the state's gradient or zeros.
-template <int DK> __device__ __forceinline__ void delta_y(const DeltaTile<DK> &s, const f4 (&out)[CB], const f4 (&D)[DK / 16], f4 (&y)[CB], f4 (*kd)[CB] = nullptr)
-{
-    using Tile = DeltaTile<DK>;
-    const int lane = threadIdx.x & 63, row = 4 * (lane >> 4);
+    using Tile = DeltaTile<E, DK>;
+    f4 du[2];
 #pragma unroll
-    for (int m = CB - 1; m >= 0; --m) {
-        f4 t = {};
+    for (int m = 0; m < 2; ++m) {
+        kd[m] = f4{};
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) t = mm4(rows_of<Tile::LD>(s.k, 16 * m, 16 * kb, lane), D[kb], t);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float left = s.until[16 * m + row + e];
-            t[e] = left != 0.f ? left * t[e] : 0.f;
-        }
-        if (kd) (*kd)[m] = t;
-#pragma unroll
-        for (int kb = m; kb < CB; ++kb) t = mm4(cols_of<Tile::LC>(s.p, 16 * m, 16 * kb, lane), out[kb], t);
-#pragma unroll
-        for (int kb = m + 1; kb < CB; ++kb) t = mm4(cols_of<Tile::LC>(s.n, 16 * m, 16 * kb, lane), y[kb], t);
-        y[m] = mm4(cols_of<Tile::LC>(s.n, 16 * m, 16 * m, lane), t, f4{});
+        for (int p = 0; p < DK / 32; ++p) kd[m] = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), D[p], kd[m]);
+        kd[m] = where(of_steps(s.until(), m, lane), kd[m]);
+        du[m] = mfma(square_columns<Tile::LC>(s.p, m, lane), both(dout[0], dout[1]), kd[m]);
     }
-}
-
-template <class E> __device__ __forceinline__ void delta_dout(const DeltaGradArgs &A, int bi, int h, long t0, int lo, int hi, int c, f4 (&d)[CB])
-{
-    const int lane = threadIdx.x & 63, row = 4 * (lane >> 4);
-    const E *p = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs + c;
 #pragma unroll
-    for (int m = 0; m < CB; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 16 * m + row + e;
-            d[m][e] = c < A.Dv && i >= lo && i < hi ? (float)p[i * A.sdo.ts] : 0.f;
-        }
+    for (int m = 0; m < 2; ++m) y[m] = mfma(square_columns<Tile::LC>(s.t, m, lane), both(du[0], du[1]), f4{});
 }
 
 // The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_back(DeltaGradArgs A)
 {
-    using Tile = DeltaTile<DK>;
+    using Tile = DeltaTile<E, DK>;
     extern __shared__ __align__(16) unsigned char lds[];
-    Tile &s = *reinterpret_cast<Tile *>(lds);
-    const int lane = threadIdx.x & 63, row = 4 * (lane >> 4);
+    Tile *tiles = reinterpret_cast<Tile *>(lds);
+    const int lane = threadIdx.x & 63;
     const int slices = (A.Dv + COLS - 1) / COLS, slice = blockIdx.x % slices;
     const long head = blockIdx.x / slices;
     const int bi = (int)(head / A.H), h = (int)(head % A.H), c = COLS * slice + 16 * (threadIdx.x >> 6) + (lane & 15);
     const bool mine = c < A.Dv;
-    f4 D[DK / 16];
-#pragma unroll
-    for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int d = 16 * kb + row + e;
-            D[kb][e] = A.dlast && mine && d < A.Dk ? A.dlast[(head * A.Dk + d) * A.Dv + c] : 0.f;
-        }
-    auto put = [&](float *to) {
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 16 * kb + row + e;
-                if (mine && d < A.Dk) to[(long)d * A.Dv + c] = D[kb][e];
-            }
+    const E *dout = (const E *)A.dout + bi * A.sdo.bs + h * A.sdo.hs + c;
+    const DeltaRecord *records = (const DeltaRecord *)A.records;
+    Columns<DK> D;
+    D.get(A.dlast ? A.dlast + head * A.Dk * A.Dv : nullptr, A.Dk, A.Dv, c, lane);
+    DeltaFetch<E, DK> fetch;
+    f4 out[2], next_out[2];
+    auto get = [&](long tile) {
+        fetch.load(A, records, head, tile);
+        get_steps(dout + tile * CH * A.sdo.ts, A.sdo.ts, mine, (int)min((long)CH, A.T - tile * CH), lane, next_out);
     };
+    if (A.tiles) {
+        get(A.tiles - 1);
+        fetch.put(tiles[(A.tiles - 1) & 1]);
+    }
+    __syncthreads();
     for (long tile = A.tiles - 1; tile >= 0; --tile) {
+        const Tile &s = tiles[tile & 1];
         const long t0 = tile * CH;
         const int rows = (int)min((long)CH, A.T - t0);
-        put(A.into + (head * A.tiles + tile) * A.Dk * A.Dv);
-        for (int lo = 0, hi = rows; hi > 0;) {
-            delta_tile<E, DK>(A, s, bi, h, t0, lo, hi);
-            f4 out[CB], y[CB], next[DK / 16];
-            delta_dout<E>(A, bi, h, t0, lo, hi, c, out);
-            delta_y<DK>(s, out, D, y);
+        out[0] = next_out[0];
+        out[1] = next_out[1];
+        if (tile) get(tile - 1);
+        D.put(A.into + (head * A.tiles + tile) * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
+        typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
-            for (int m = 0; m < CB; ++m)
+        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(D.s[2 * p], D.s[2 * p + 1]);
+        f4 kd[2], y[2];
+        delta_y<E, DK, 3>(s, sp, out, lane, kd, y);
+        f4 x[2], z[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    const bool live = !s.cut[i];
-                    out[m][e] = live ? A.scale * s.since[i] * out[m][e] : 0.f;
-                    y[m][e] = live && i >= lo && i < hi ? -s.beta[i] * s.since[i] * y[m][e] : 0.f;
-                }
-            const bool lives = !s.cut[CH - 1];
-            const float left = s.since[CH - 1];
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                f4 n;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) n[e] = lives ? left * D[d][e] : 0.f;
-#pragma unroll
-                for (int kb = 0; kb < CB; ++kb) {
-                    n = mm4(cols_of<Tile::LD>(s.q, 16 * d, 16 * kb, lane), out[kb], n);
-                    n = mm4(cols_of<Tile::LD>(s.k, 16 * d, 16 * kb, lane), y[kb], n);
-                }
-                // where the first step starts an episode nothing passes it, no NaN of theirs either
-                next[d] = s.cut[lo] ? f4{} : n;
-            }
-            const bool again = __syncthreads_or(!finite(next)) && (lo == 0 && hi == rows);
-            if (again) {
-                const int first = episode_begin(A, bi, t0, hi);
-                if (first > 0) {
-                    lo = first;
-                    continue;
-                }
-            }
-#pragma unroll
-            for (int d = 0; d < DK / 16; ++d) D[d] = next[d];
-            hi = lo;
-            if (hi > 0) lo = episode_begin(A, bi, t0, hi);
+        for (int m = 0; m < 2; ++m) {
+            const f4 since = of_steps(s.since(), m, lane);
+            x[m] = where(since, A.scale * out[m]);
+            z[m] = where(since, -of_steps(s.beta(), m, lane) * y[m]);
         }
+        const auto xp = split<E, 3>(x[0], x[1]), zp = split<E, 3>(z[0], z[1]);
+        const float left = s.since()[CH - 1];
+        f4 next[DK / 16];
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) {
+            next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.q, n & 1, n >> 1, lane), xp, where(left, D.s[n]));
+            next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.k, n & 1, n >> 1, lane), zp, next[n]);
+        }
+        if (__any(!finite(next))) {
+            for (int i = rows - 1; i >= 0; --i) {
+                delta_step_back<E, DK>(s, D, i, mine ? (float)dout[(t0 + i) * A.sdo.ts] : 0.f, A.scale, lane);
+                delta_pass_back<E, DK>(s, D, i);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < DK / 16; ++n) D.s[n] = next[n];
+        }
+        if (tile) fetch.put(tiles[(tile - 1) & 1]);
+        lds_barrier();
     }
-    if (A.ds0) put(A.ds0 + head * A.Dk * A.Dv);
+    if (A.ds0) D.put(A.ds0 + head * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
 }
 
-template <int DK> struct DeltaGradTile {
-    static constexpr int LU = COLS + 4;
-    DeltaTile<DK> s;
-    float dout[CH * LU], u[CH * LU], y[CH * LU];
-    float sums[3][4][CH];              // of each wave and row: q.dq, Y.u, dv.v
-    float ends[4];                     // of each wave: <D, S'>
+// ---------------------------------------------------------------- gradients
+// Two numbers to a place: for bf16 a matrix of fp32 numbers as two planes of bf16, which hold 16 bits; for fp32 the matrix.
+template <class E, int R, int C> struct Matrix;
+template <int R, int C> struct Matrix<float, R, C> {
+    static constexpr int LD = C + 4;
+    float m[R * LD];
+    __device__ __forceinline__ void put(int i, int j, float v) { m[i * LD + j] = v; }
+    __device__ __forceinline__ f8 get(int i, int j) const { return eight(m + i * LD + j); }
+};
+template <int R, int C> struct Matrix<bf16, R, C> {
+    static constexpr int LD = C + 8;
+    bf16 m[2][R * LD];
+    __device__ __forceinline__ void put(int i, int j, float v)
+    {
+        const uint32_t a = __float_as_uint(v), b = __float_as_uint(v - __uint_as_float(a & 0xFFFF0000u)) + 0x8000u;
+        m[0][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(a >> 16));
+        m[1][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(b >> 16));
+    }
+    __device__ __forceinline__ Planes<2> get(int i, int j) const { return Planes<2>{{eight(m[0] + i * LD + j), eight(m[1] + i * LD + j)}}; }
+};
+template <class E, int DK> struct DeltaGradTile {
+    static constexpr int LO = COLS + 16 / (int)sizeof(E);
+    DeltaTile<E, DK> s;
+    E dout[CH * LO];
+    Matrix<E, CH, COLS> u, y;
+    Matrix<E, CH, CH> dp, dn, dpt, dnt;     // of P's and N's products, and transposed
+    float sums[3][4][CH];                   // of each wave and row: q.dq, Y.u, dv.v
+    float ends[4];                          // of each wave: <D, S'>
+    float rows[2][4][DK];                   // step by step: of each wave, dq and dk of a step
 };
 
-// Sums of x over the 16 lanes that share rows, in lane 0 of them
-__device__ __forceinline__ float lanes16(float x)
+// 8 numbers of a state's row d, columns c.., as right operand
+template <class E> __device__ __forceinline__ typename Operand<E>::template Split<2> state_row(const float *S, int d, int c, int Dk, int Dv, bool real)
 {
-    return group_fold(x, 16, add);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = real && d < Dk && c + e < Dv ? S[(long)d * Dv + c + e] : 0.f;
+    return Operand<E>::template split<2>(v);
 }
 
-// Everything else: a workgroup per tile and head.
+// The gradients of a tile's steps one by one, as the definition has them: every state is formed again from the first, which takes as many
+// passes as there are steps.  For tiles with numbers that are not finite.
+template <class E, int DK> __device__ __noinline__ void delta_grad_steps(const DeltaGradArgs &A, DeltaGradTile<E, DK> &g, long head, long tile, const float *S0, const float *D0)
+{
+    using Tile = DeltaTile<E, DK>;
+    Tile &s = g.s;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bi = (int)(head / A.H), h = (int)(head % A.H);
+    const long t0 = tile * CH;
+    const int rows = (int)min((long)CH, A.T - t0);
+    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs, *dout = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs;
+    for (int t = rows - 1; t >= 0; --t) {
+        float dq[DK / 16][4] = {}, dk[DK / 16][4] = {}, rate = 0.f, gate = 0.f;
+        for (int c0 = 0; c0 < A.Dv; c0 += COLS) {
+            const int c = c0 + 16 * w + (lane & 15);
+            const bool mine = c < A.Dv;
+            Columns<DK> S, D;
+            S.get(S0, A.Dk, A.Dv, c, lane);
+            for (int i = 0; i < t; ++i) delta_step<E, DK>(s, S, i, mine ? (float)v[i * A.sv.ts + c] : 0.f, lane);
+            D.get(D0, A.Dk, A.Dv, c, lane);
+            for (int i = rows - 1; i > t; --i) {
+                delta_step_back<E, DK>(s, D, i, mine ? (float)dout[i * A.sdo.ts + c] : 0.f, A.scale, lane);
+                delta_pass_back<E, DK>(s, D, i);
+            }
+            if (starts(s, t)) S.clear();
+            const Columns<DK> before = S;
+            S.scaled(s.gate()[t]);
+            const Columns<DK> held = S;
+            const float d = mine ? (float)dout[t * A.sdo.ts + c] : 0.f, gap = (mine ? (float)v[t * A.sv.ts + c] : 0.f) - S.dot(s.k + t * Tile::LD, lane);
+            S.add(s.k + t * Tile::LD, s.beta()[t] * gap, lane);
+            Columns<DK> full = D;
+            full.add(s.q + t * Tile::LD, A.scale * d, lane);
+            const float dv = delta_step_back<E, DK>(s, D, t, d, A.scale, lane);
+            if (mine) {
+                float toward = full.dot(s.k + t * Tile::LD, lane) * gap, kept = 0.f;
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        dq[n][e] += A.scale * S.s[n][e] * d;
+                        dk[n][e] += s.beta()[t] * full.s[n][e] * gap - held.s[n][e] * dv;
+                        kept += D.s[n][e] * before.s[n][e];
+                    }
+                if (lane < 16) {
+                    rate += toward;
+                    ((E *)A.dv)[bi * A.sdv.bs + (t0 + t) * A.sdv.ts + h * A.sdv.hs + c] = (E)dv;
+                }
+                gate += kept;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = group_fold(dq[n][e], 16, seq::add), y = group_fold(dk[n][e], 16, seq::add);
+                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
+                if ((lane & 15) == 0) g.rows[0][w][d] = x, g.rows[1][w][d] = y;
+            }
+        const float r = group_fold(rate, 64, seq::add), a = group_fold(gate, 64, seq::add);
+        if (lane == 0) g.sums[0][w][0] = r, g.sums[1][w][0] = a;
+        __syncthreads();
+        if (tid < A.Dk) {
+            const int d = tid;
+            ((E *)A.dq)[bi * A.sdq.bs + (t0 + t) * A.sdq.ts + h * A.sdq.hs + d] = (E)((g.rows[0][0][d] + g.rows[0][1][d]) + (g.rows[0][2][d] + g.rows[0][3][d]));
+            ((E *)A.dk)[bi * A.sdk.bs + (t0 + t) * A.sdk.ts + h * A.sdk.hs + d] = (E)((g.rows[1][0][d] + g.rows[1][1][d]) + (g.rows[1][2][d] + g.rows[1][3][d]));
+        }
+        if (tid == 0) {
+            const float gt = s.gate()[t], bt = s.beta()[t];
+            const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + t) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + t) * A.sb.ts + h * A.sb.hs];
+            const float sr = (g.sums[0][0][0] + g.sums[0][1][0]) + (g.sums[0][2][0] + g.sums[0][3][0]), sa = (g.sums[1][0][0] + g.sums[1][1][0]) + (g.sums[1][2][0] + g.sums[1][3][0]);
+            ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, t) || gt == 0.f ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
+            ((E *)A.db)[bi * A.sdb.bs + (t0 + t) * A.sdb.ts + h * A.sdb.hs] = (E)(bt * (1.f / (1.f + expf(b))) * sr);
+        }
+        __syncthreads();
+    }
+}
+
+// All gradients but the state's: a workgroup per tile and head.
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad(DeltaGradArgs A)
 {
-    using Tile = DeltaTile<DK>;
-    using Grad = DeltaGradTile<DK>;
-    constexpr int LU = Grad::LU, ND = (DK + 63) / 64;      // tiles of 16 of a wave's columns of dq and dk
+    using Op = Operand<E>;
+    using Tile = DeltaTile<E, DK>;
+    using Grad = DeltaGradTile<E, DK>;
+    constexpr int LO = Grad::LO, ND = (DK + 63) / 64;      // tiles of 16 of a wave's columns of dq and dk
     extern __shared__ __align__(16) unsigned char lds[];
     Grad &g = *reinterpret_cast<Grad *>(lds);
     Tile &s = g.s;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, row = 4 * (lane >> 4), col = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, grp = lane >> 4, col = lane & 15;
     const long tile = blockIdx.x % A.tiles, head = blockIdx.x / A.tiles;
     const int bi = (int)(head / A.H), h = (int)(head % A.H);
     const long t0 = tile * CH;
     const int rows = (int)min((long)CH, A.T - t0);
-    const float *S = A.carry + (head * A.tiles + tile) * A.Dk * A.Dv, *Dn = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
-    for (int lo = 0, hi = rows; lo < rows;) {
-        delta_tile<E, DK>(A, s, bi, h, t0, lo, hi);
-        // the state enters the rows from 0 on, unless the first step starts an episode; its gradient those up to the last
-        const bool enters = lo == 0 && !s.cut[0], leaves = hi == rows;
-        f4 dp[CB] = {}, dn[CB] = {}, os[ND][CB] = {}, ys[ND][CB] = {}, ud[ND][CB] = {};
-        f4 yu[CB] = {}, vv[CB] = {};
-        float end = 0.f;
-        bool ok = true;
-        for (int sl = 0; sl < A.Dv; sl += COLS) {
-            const int c = sl + 16 * w + col;
-            f4 out[CB], u[CB], y[CB], val[CB], kd[CB];
-            {
-                f4 st[DK / 16], D[DK / 16];
+    const float *S = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *Dn = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
+    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs, *dout = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs;
+    {
+        DeltaFetch<E, DK> fetch;
+        fetch.load(A, (const DeltaRecord *)A.records, head, tile);
+        fetch.put(s);
+    }
+    __syncthreads();
+    const float left = s.since()[CH - 1];
+    // dP and dN: wave 0 has rows and columns 0.., wave 1 rows 16.. of columns 0.., wave 2 rows and columns 16..
+    const int ti = w ? 16 : 0, tj = w == 2 ? 16 : 0;
+    f4 dp = {}, dn = {}, os[ND][2] = {}, ys[ND][2] = {}, ud[ND][2] = {}, yu[2] = {}, vv[2] = {};
+    float end = 0.f;
+    bool ok = true;
+    for (int sl = 0; sl < A.Dv; sl += COLS) {
+        const int c = sl + 16 * w + col;
+        const bool mine = c < A.Dv;
+        f4 out[2], u[2], y[2], val[2], kd[2];
+        get_steps(v + c, A.sv.ts, mine, rows, lane, val);
+        get_steps(dout + c, A.sdo.ts, mine, rows, lane, out);
+        {
+            Columns<DK> st, D;
+            st.get(S, A.Dk, A.Dv, c, lane);
+            D.get(Dn, A.Dk, A.Dv, c, lane);
+            typename Op::template Split<2> sp[DK / 32], dp2[DK / 32];
 #pragma unroll
-                for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int d = 16 * kb + row + e;
-                        const bool in = c < A.Dv && d < A.Dk;
-                        st[kb][e] = in && enters ? S[(long)d * A.Dv + c] : 0.f;
-                        D[kb][e] = in && leaves ? Dn[(long)d * A.Dv + c] : 0.f;
-                    }
-                delta_u<E, DK>(A, s, st, bi, h, t0, lo, hi, c, u, &val);
-                delta_dout<E>(A, bi, h, t0, lo, hi, c, out);
-                delta_y<DK>(s, out, D, y, &kd);
-                if (enters && leaves && !s.cut[CH - 1])
-#pragma unroll
-                    for (int kb = 0; kb < DK / 16; ++kb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) end = fmaf(s.since[CH - 1] * st[kb][e], D[kb][e], end);
+            for (int p = 0; p < DK / 32; ++p) {
+                sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
+                dp2[p] = split<E, 2>(D.s[2 * p], D.s[2 * p + 1]);
             }
+            delta_u<E, DK, 2>(s, sp, val, rows, lane, u);
+            delta_y<E, DK, 2>(s, dp2, out, lane, kd, y);
+            if (left != 0.f)
 #pragma unroll
-            for (int m = 0; m < CB; ++m)
+                for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    const bool in = i >= lo && i < hi;
-                    const float dv = s.beta[i] * y[m][e];
-                    if (in) {
-                        ok &= fabsf(dv) < INFINITY;
-                        yu[m][e] = fmaf(y[m][e], u[m][e], yu[m][e]);
-                        vv[m][e] = fmaf(dv, val[m][e], vv[m][e]);
-                        end = fmaf(kd[m][e], u[m][e], end);
-                        if (c < A.Dv) ((E *)A.dv)[bi * A.sdv.bs + (t0 + i) * A.sdv.ts + h * A.sdv.hs + c] = (E)dv;
-                    }
-                    g.dout[i * LU + 16 * w + col] = in ? out[m][e] : 0.f;
-                    g.u[i * LU + 16 * w + col] = in ? u[m][e] : 0.f;
-                    g.y[i * LU + 16 * w + col] = in ? y[m][e] : 0.f;
-                }
-            __syncthreads();
-            // rows 16 w.. of dO U^T and of -Y U^T, up to the diagonal
-#pragma unroll
-            for (int kb = 0; kb < COLS / 16; ++kb) {
-                const f4 ao = rows_of<LU>(g.dout, 16 * w, 16 * kb, lane), ay = -rows_of<LU>(g.y, 16 * w, 16 * kb, lane);
-#pragma unroll
-                for (int n = 0; n < CB; ++n) {
-                    if (n > w) break;
-                    const f4 b = rows_of<LU>(g.u, 16 * n, 16 * kb, lane);
-                    dp[n] = mm4(ao, b, dp[n]);
-                    dn[n] = mm4(ay, b, dn[n]);
-                }
-            }
-            // columns 16 (w + 4 d).. of dO S^T, Y S^T and U D^T
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                const int dk = 16 * (w + 4 * d) + col;
-                if (16 * (w + 4 * d) >= DK) break;
-#pragma unroll
-                for (int kb = 0; kb < COLS / 16; ++kb) {
-                    f4 st, D;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int cc = sl + 16 * kb + row + e;
-                        const bool in = cc < A.Dv && dk < A.Dk;
-                        st[e] = in && enters ? S[(long)dk * A.Dv + cc] : 0.f;
-                        D[e] = in && leaves ? Dn[(long)dk * A.Dv + cc] : 0.f;
-                    }
-#pragma unroll
-                    for (int m = 0; m < CB; ++m) {
-                        os[d][m] = mm4(rows_of<LU>(g.dout, 16 * m, 16 * kb, lane), st, os[d][m]);
-                        ys[d][m] = mm4(rows_of<LU>(g.y, 16 * m, 16 * kb, lane), st, ys[d][m]);
-                        ud[d][m] = mm4(rows_of<LU>(g.u, 16 * m, 16 * kb, lane), D, ud[d][m]);
-                    }
-                }
-            }
-            __syncthreads();
+                    for (int e = 0; e < 4; ++e) end = fmaf(left * st.s[n][e], D.s[n][e], end);
         }
-        // the gradients of P's and N's products, in their places
+        f4 dv[2];
 #pragma unroll
-        for (int n = 0; n < CB; ++n) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + row + r, j = 16 * n + col;
-                const float b = n <= w && j <= i ? between(s, i, j) : 0.f;
-                s.p[i * Tile::LC + j] = b != 0.f ? A.scale * b * dp[n][r] : 0.f;
-                s.n[i * Tile::LC + j] = b != 0.f && j < i ? s.beta[i] * b * dn[n][r] : 0.f;
-            }
-        }
-        __syncthreads();
-        f4 qd[CB] = {};
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            if (16 * (w + 4 * d) >= DK) break;
-            const int dk = 16 * (w + 4 * d) + col;
-#pragma unroll
-            for (int m = 0; m < CB; ++m) {
-                f4 dq, dkk, add_q = {}, add_k = {};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    const bool live = !s.cut[i] && i >= lo && i < hi;
-                    dq[e] = live ? A.scale * s.since[i] * os[d][m][e] : 0.f;
-                    dkk[e] = (live ? -s.beta[i] * s.since[i] * ys[d][m][e] : 0.f) + (s.until[i] != 0.f ? s.until[i] * ud[d][m][e] : 0.f);
-                }
-#pragma unroll
-                for (int kb = 0; kb < CB; ++kb) {
-                    const f4 kr = cols_of<Tile::LD>(s.k, 16 * (w + 4 * d), 16 * kb, lane);
-                    if (kb <= m) {
-                        add_q = mm4(rows_of<Tile::LC>(s.p, 16 * m, 16 * kb, lane), kr, add_q);
-                        add_k = mm4(rows_of<Tile::LC>(s.n, 16 * m, 16 * kb, lane), kr, add_k);
-                    }
-                    if (kb >= m) {
-                        add_k = mm4(cols_of<Tile::LC>(s.p, 16 * m, 16 * kb, lane), cols_of<Tile::LD>(s.q, 16 * (w + 4 * d), 16 * kb, lane), add_k);
-                        add_k = mm4(cols_of<Tile::LC>(s.n, 16 * m, 16 * kb, lane), kr, add_k);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + row + e;
-                    if (i < lo || i >= hi) continue;
-                    const float x = dq[e] + add_q[e], z = dkk[e] + add_k[e];
-                    ok &= fabsf(x) < INFINITY && fabsf(z) < INFINITY;
-                    qd[m][e] = fmaf(x, s.q[i * Tile::LD + 16 * (w + 4 * d) + col], qd[m][e]);
-                    if (dk < A.Dk) {
-                        ((E *)A.dq)[bi * A.sdq.bs + (t0 + i) * A.sdq.ts + h * A.sdq.hs + dk] = (E)x;
-                        ((E *)A.dk)[bi * A.sdk.bs + (t0 + i) * A.sdk.ts + h * A.sdk.hs + dk] = (E)z;
-                    }
-                }
-            }
-        }
-        if (__syncthreads_or(!ok) && lo == 0 && hi == rows) {
-            const int first = episode_end(A, bi, t0, 0, rows);
-            if (first < rows) {       // written again, episode by episode
-                hi = first;
-                continue;
-            }
-        }
-#pragma unroll
-        for (int m = 0; m < CB; ++m)
+        for (int m = 0; m < 2; ++m) {
+            dv[m] = of_steps(s.beta(), m, lane) * y[m];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float a = lanes16(qd[m][e]), b = lanes16(yu[m][e]), d = lanes16(vv[m][e]);
-                if (col == 0) {
-                    const int i = 16 * m + row + e;
-                    g.sums[0][w][i] = a;
-                    g.sums[1][w][i] = b;
-                    g.sums[2][w][i] = d;
-                }
-            }
-        end = group_fold(end, 64, add);
-        if (lane == 0) g.ends[w] = end;
-        __syncthreads();
-        if (w == 0) {
-            const int i = lane;
-            auto all = [&](int k) { return (g.sums[k][0][i] + g.sums[k][1][i]) + (g.sums[k][2][i] + g.sums[k][3][i]); };
-            const bool in = i >= lo && i < hi;
-            float x = in ? all(0) - all(2) : 0.f;
-            if (i == hi - 1 && leaves) x += (g.ends[0] + g.ends[1]) + (g.ends[2] + g.ends[3]);
-            const int cut = s.cut[i];
-#pragma unroll
-            for (int d = 1; d < CH; d *= 2) {
-                const float o = __shfl_down(x, d);
-                const int oc = __shfl_down(cut, d);
-                if (i + d < CH && oc == cut) x += o;
-            }
-            if (in) {
-                const bool starts = A.reset && A.reset[bi * A.reset_bs + (t0 + i) * A.reset_ts];
-                const float a = s.gate[i], f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs];
-                const float df = starts || a == 0.f ? 0.f : x * (1.f / (1.f + expf(f)));
-                const float bb = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
-                ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)df;
-                ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(all(1) * (1.f / (1.f + expf(bb))));
+                const int i = 8 * grp + 4 * m + e;
+                ok &= fabsf(dv[m][e]) < INFINITY && fabsf(u[m][e]) < INFINITY;
+                yu[m][e] = fmaf(y[m][e], u[m][e], yu[m][e]);
+                vv[m][e] = fmaf(dv[m][e], val[m][e], vv[m][e]);
+                end = fmaf(kd[m][e], u[m][e], end);
+                g.dout[i * LO + 16 * w + col] = (E)out[m][e];
+                g.u.put(i, 16 * w + col, u[m][e]);
+                g.y.put(i, 16 * w + col, y[m][e]);
             }
         }
-        if (hi >= rows) break;
+        put_steps((E *)A.dv + bi * A.sdv.bs + t0 * A.sdv.ts + h * A.sdv.hs + c, A.sdv.ts, mine, rows, lane, dv);
         __syncthreads();
-        lo = hi;
-        hi = episode_end(A, bi, t0, lo, rows);
+        if (w < 3) {
+#pragma unroll
+            for (int kb = 0; kb < COLS; kb += 32) {
+                const auto b = g.u.get(tj + col, kb + 8 * grp);
+                dp = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, dp);
+                dn = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, dn);
+            }
+        }
+        // columns 16 (w + 4 d).. of dO S^T, Y S^T and U D^T
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const int dk = 16 * (w + 4 * d) + col;
+            if (16 * (w + 4 * d) >= DK) break;
+#pragma unroll
+            for (int kb = 0; kb < COLS; kb += 32) {
+                const auto st = state_row<E>(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, true), D = state_row<E>(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, true);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    os[d][m] = Op::mul(eight(g.dout + (16 * m + col) * LO + kb + 8 * grp), st, os[d][m]);
+                    ys[d][m] = Op::mul(g.y.get(16 * m + col, kb + 8 * grp), st, ys[d][m]);
+                    ud[d][m] = Op::mul(g.u.get(16 * m + col, kb + 8 * grp), D, ud[d][m]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (w < 3) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = ti + 4 * grp + r, j = tj + col;
+            const float b = j <= i ? s.between(i, j) : 0.f;
+            const float x = b != 0.f ? A.scale * b * dp[r] : 0.f, z = b != 0.f && j < i ? -s.beta()[i] * b * dn[r] : 0.f;
+            g.dp.put(i, j, x);
+            g.dpt.put(j, i, x);
+            g.dn.put(i, j, z);
+            g.dnt.put(j, i, z);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * grp + r, j = 16 + col;      // above the diagonal
+            g.dp.put(i, j, 0.f);
+            g.dpt.put(j, i, 0.f);
+            g.dn.put(i, j, 0.f);
+            g.dnt.put(j, i, 0.f);
+        }
+    }
+    __syncthreads();
+    f4 qd[2] = {};
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        if (16 * (w + 4 * d) >= DK) break;
+        // columns of K and Q, 32 steps deep, a natural column per lane: column 16 t + i of 32 p.. is dealt as half (i / 4) % 2
+        typename Op::Exact kc, qc;
+        {
+            const int n = w + 4 * d;
+            if constexpr (std::is_same<E, float>::value) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    kc[e] = s.k[(8 * grp + e) * Tile::LD + 16 * n + col];
+                    qc[e] = s.q[(8 * grp + e) * Tile::LD + 16 * n + col];
+                }
+            } else {
+                using s4 = vec<short, 4>;
+                typedef __attribute__((address_space(3))) s4 *At;
+                const int at = (8 * grp + (col >> 2)) * Tile::LD + 16 * n + 4 * (col & 3);
+                const s4 k0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.k + at)), k1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.k + at + 4 * Tile::LD));
+                const s4 q0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.q + at)), q1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.q + at + 4 * Tile::LD));
+                kc = __builtin_bit_cast(b8, (vec<short, 8>){k0[0], k0[1], k0[2], k0[3], k1[0], k1[1], k1[2], k1[3]});
+                qc = __builtin_bit_cast(b8, (vec<short, 8>){q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]});
+            }
+        }
+        const int dk = 16 * (w + 4 * d) + col;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f4 since = load<4>(s.since() + 16 * m + 4 * grp), beta = load<4>(s.beta() + 16 * m + 4 * grp), until = load<4>(s.until() + 16 * m + 4 * grp);
+            f4 x = where(since, A.scale * os[d][m]), z = where(since, -beta * ys[d][m]) + where(until, ud[d][m]);
+            x = Op::mul(g.dp.get(16 * m + col, 8 * grp), kc, x);
+            z = Op::mul(g.dpt.get(16 * m + col, 8 * grp), qc, z);
+            z = Op::mul(g.dn.get(16 * m + col, 8 * grp), kc, z);
+            z = Op::mul(g.dnt.get(16 * m + col, 8 * grp), kc, z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * m + 4 * grp + e;
+                ok &= fabsf(x[e]) < INFINITY && fabsf(z[e]) < INFINITY;
+                qd[m][e] = fmaf(x[e], (float)s.q[i * Tile::LD + dk], qd[m][e]);
+                if (dk < A.Dk && i < rows) {
+                    ((E *)A.dq)[bi * A.sdq.bs + (t0 + i) * A.sdq.ts + h * A.sdq.hs + dk] = (E)x[e];
+                    ((E *)A.dk)[bi * A.sdk.bs + (t0 + i) * A.sdk.ts + h * A.sdk.hs + dk] = (E)z[e];
+                }
+            }
+        }
+    }
+    ok &= fabsf(end) < INFINITY;
+    if (__syncthreads_or(!ok)) {
+        delta_grad_steps<E, DK>(A, g, head, tile, S, Dn);
+        return;
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = group_fold(qd[m][e], 16, add), b = group_fold(yu[m][e], 16, add), d = group_fold(vv[m][e], 16, add);
+            if (col == 0) {
+                g.sums[0][w][16 * m + 4 * grp + e] = a;
+                g.sums[1][w][8 * grp + 4 * m + e] = b;
+                g.sums[2][w][8 * grp + 4 * m + e] = d;
+            }
+        }
+    end = group_fold(end, 64, add);
+    if (lane == 0) g.ends[w] = end;
+    __syncthreads();
+    if (tid < CH) {
+        const int i = tid, cut = s.cut()[i];
+        auto all = [&](int k) { return (g.sums[k][0][i] + g.sums[k][1][i]) + (g.sums[k][2][i] + g.sums[k][3][i]); };
+        float x = i < rows ? all(0) - all(2) : 0.f;
+        if (i == rows - 1) x += (g.ends[0] + g.ends[1]) + (g.ends[2] + g.ends[3]);
+#pragma unroll
+        for (int d = 1; d < CH; d *= 2) {
+            const float o = __shfl_down(x, d, CH);
+            const int oc = __shfl_down(cut, d, CH);
+            if (i + d < CH && oc == cut) x += o;
+        }
+        if (i < rows) {
+            const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
+            ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, i) || s.gate()[i] == 0.f ? 0.f : x * (1.f / (1.f + expf(f))));
+            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(all(1) * (1.f / (1.f + expf(b))));
+        }
     }
 }
 

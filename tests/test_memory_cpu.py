@@ -41,7 +41,7 @@ GATE = (16, 4, 1)
 
 def delta_args(**kw):
     return packed(seq.DELTA_ARGS, dict(dtype=0, B=2, H=4, Dk=8, Dv=8, scale=1.0, T=4, q=P, k=P, v=P, f=P, b=P, q_s=IN, k_s=IN, v_s=IN, f_s=GATE, b_s=GATE,
-                                       s0=0, reset=0, reset_bs=0, reset_ts=0, o=P, o_s=IN, s_last=0, carry=0, workspace=0), kw)
+                                       s0=0, reset=0, reset_bs=0, reset_ts=0, o=P, o_s=IN, s_last=0, carry=0, workspace=P), kw)
 
 
 def delta_grad_args(**kw):
@@ -51,13 +51,13 @@ def delta_grad_args(**kw):
 
 
 BOTH = [dict(dtype=2), dict(B=-1), dict(B=65536), dict(H=-1), dict(H=65536), dict(B=2000, H=2000), dict(Dk=0), dict(Dk=129), dict(Dv=0), dict(Dv=129), dict(T=-1),
-        dict(T=1 << 40), dict(B=65535, H=16, T=2000), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(k=P + 2), dict(v=None), dict(f=P + 1), dict(b=None),
+        dict(T=1 << 40), dict(B=65535, H=16, T=1000), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(k=P + 2), dict(v=None), dict(f=P + 1), dict(b=None),
         dict(q_s=(-1, 32, 8)), dict(k_s=(128, 1 << 60, 8)), dict(v_s=(128, 32, -8)), dict(f_s=(16, -4, 1)), dict(b_s=(1 << 60, 4, 1)),
         dict(reset=P, reset_ts=-1), dict(reset=P, reset_bs=1 << 60)]
 
 
 @pytest.mark.parametrize("kw", BOTH + [dict(o=None), dict(o=P + 2), dict(o_s=(128, 32, 7)), dict(o_s=(128, 31, 8)), dict(o_s=(127, 32, 8)), dict(o_s=(0, 32, 8)), dict(o_s=(8, 32, 16)),
-                                       dict(s0=P + 2), dict(s_last=P + 1), dict(carry=P + 2)])
+                                       dict(s0=P + 2), dict(s_last=P + 1), dict(carry=P + 4), dict(workspace=None), dict(workspace=P + 8)])
 def test_delta_refuses(lib, kw):
     assert lib.dqn_delta_forward(delta_args(**kw), None) == dqn.ERR_INVALID_ARG and "dqn_delta_forward" in said(lib)
 
