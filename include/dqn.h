@@ -423,7 +423,9 @@ typedef struct {
     const void *q, *k, *v;              /* [B][T][H][Dk], the same, [B][T][H][Dv]   */
     const void *f, *b;                  /* [B][T][H]                                */
     int64_t q_s[3], k_s[3], v_s[3], f_s[3], b_s[3];
-                                        /* strides of a sequence, a step, a head    */
+                                        /* strides of a sequence, a step, a head;
+                                           that of a step at most 2^24 (any with
+                                           T = 1)                                   */
     const float *s0;                    /* [B][H][Dk][Dv], or NULL = zeros          */
     const uint8_t *reset;               /* [B][T], or NULL = no episode starts      */
     int64_t reset_bs, reset_ts;

@@ -64,6 +64,7 @@ struct DeltaGradArgs : DeltaIn {
     Strides sdq, sdk, sdv, sdf, sdb;
     float *ds0;
     float *into;                       // the gradient of the state that leaves each tile, as states
+    int *again;                        // of each tile: whether its gradients hold a number that is not finite
 };
 
 // What the first launch leaves of a tile.
@@ -167,27 +168,27 @@ template <class E, int N> __device__ __forceinline__ f4 mul(typename Operand<E>:
     else return Operand<bf16>::template mul<N>(a, b, c);
 }
 
-// The step of a tile that row `rho` of result `half` of a pair stands for, and the row of the state in 32 of them.
-__device__ __forceinline__ int dealt(int half, int rho) { return 8 * (rho >> 2) + 4 * half + (rho & 3); }
+// Loads take addresses that are always there, the last step's or column's in place of those beyond, and zeros are put in afterwards: a branch
+// around each of them would wait for one before it asks for the next.
 
-// 8 numbers of a row from column c on, zeros from D on
+// 8 numbers of a row from column c on, zeros from D on and where the row is not real
 template <class E> __device__ __forceinline__ vec<E, 8> load8(const E *p, int c, int D, bool real, int wide)
 {
-    vec<E, 8> v = vec<E, 8>(0.f);
-    if (!real) return v;
-    if (wide) {
+    vec<E, 8> v;
+    if (wide) {      // D is a multiple of V
         constexpr int V = 16 / (int)sizeof(E);
 #pragma unroll
-        for (int i = 0; i < 8; i += V)
-            if (c + i < D) {
-                const vec<E, V> x = load<V>(p + c + i);
+        for (int i = 0; i < 8; i += V) {
+            const vec<E, V> x = load<V>(p + min(c + i, D - V));
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[i + e] = x[e];
-            }
+            for (int e = 0; e < V; ++e) v[i + e] = real && c + i < D ? x[e] : (E)0.f;
+        }
     } else {
+        E x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < D) v[i] = p[c + i];
+        for (int i = 0; i < 8; ++i) x[i] = p[min(c + i, D - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = real && c + i < D ? x[i] : (E)0.f;
     }
     return v;
 }
@@ -218,8 +219,8 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int r = 16 * m + col;
-            kf[m][ks] = load8<E>(k + r * A.sk.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
-            qf[m][ks] = load8<E>(q + r * A.sq.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
+            kf[m][ks] = load8<E>(k + min(r, rows - 1) * A.sk.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
+            qf[m][ks] = load8<E>(q + min(r, rows - 1) * A.sq.ts, 32 * ks + 8 * g, A.Dk, r < rows, A.wide);
         }
     {   // both halves of the wave do the same
         const int i = lane & 31;
@@ -328,56 +329,99 @@ template <class E, int DK> struct DeltaTile {
     }
 };
 
-// The part of a tile that a thread of 256 brings from memory: into registers first, so that it can arrive while the tile before is worked on.
-template <class E, int DK> struct DeltaFetch {
-    static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + 255) / 256;
+// Where a head's tensors begin, for all lanes alike, and 32-bit offsets from there: a stride from step to step is at most 2^24 elements.
+template <class E> __device__ __forceinline__ const E *head_of(const void *p, const Strides &s, int bi, int h) { return (const E *)p + bi * s.bs + h * s.hs; }
+template <class E> __device__ __forceinline__ E *head_of(void *p, const Strides &s, int bi, int h) { return (E *)p + bi * s.bs + h * s.hs; }
+template <class T> __device__ __forceinline__ T *plus(T *p, uint32_t bytes) { return (T *)((char *)p + bytes); }
+template <class T> __device__ __forceinline__ const T *plus(const T *p, uint32_t bytes) { return (const T *)((const char *)p + bytes); }
+
+// The part of a tile that a thread of THREADS brings from memory: into registers first, so that it can arrive while another tile is worked on.
+template <class E, int DK, int THREADS> struct DeltaFetch {
+    static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + THREADS - 1) / THREADS, NR = CH * CH / 4 / THREADS;
+    static_assert(7 * CH / 4 <= THREADS, "a thread brings one piece of the vectors");
+    const E *qh, *kh;
+    const DeltaRecord *records;
+    int tid, rows;
+    uint32_t qo[N], ko[N];
     vec<E, V> q[N], k[N];
-    f4 t, p, vectors;
-    __device__ __forceinline__ void load(const DeltaIn &A, const DeltaRecord *records, long head, long tile)
+    f4 t[NR], p[NR], vectors;
+    __device__ __forceinline__ void offsets(const DeltaIn &A, int n_rows)
+    {
+        rows = n_rows;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int e = tid + THREADS * n, r = min(e / PER, n_rows - 1), c = min(e % PER * V, A.wide ? A.Dk - V : A.Dk - 1);
+            qo[n] = (uint32_t)(r * (int)A.sq.ts + c) * (uint32_t)sizeof(E);
+            ko[n] = (uint32_t)(r * (int)A.sk.ts + c) * (uint32_t)sizeof(E);
+        }
+    }
+    __device__ __forceinline__ void begin(const DeltaIn &A, const DeltaRecord *all, long head, int bi, int h, int thread)
+    {
+        qh = head_of<E>(A.q, A.sq, bi, h);
+        kh = head_of<E>(A.k, A.sk, bi, h);
+        records = all + head * A.tiles;
+        tid = thread;
+        offsets(A, CH);
+    }
+    __device__ __forceinline__ void load(const DeltaIn &A, long tile)
     {
         const long t0 = tile * CH;
-        const int bi = (int)(head / A.H), h = (int)(head % A.H), rows = (int)min((long)CH, A.T - t0);
-        const E *qp = (const E *)A.q + bi * A.sq.bs + t0 * A.sq.ts + h * A.sq.hs, *kp = (const E *)A.k + bi * A.sk.bs + t0 * A.sk.ts + h * A.sk.hs;
+        const int now = (int)min((long)CH, A.T - t0);
+        if (now != rows) offsets(A, now);
+        const E *qp = qh + t0 * A.sq.ts, *kp = kh + t0 * A.sk.ts;
+        if (A.wide) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int e = threadIdx.x + 256 * n, r = e / PER, c = e % PER * V;
-            vec<E, V> a = vec<E, V>(0.f), b = vec<E, V>(0.f);
-            if (r < rows && c < A.Dk) {
-                if (A.wide) {
-                    a = seq::load<V>(qp + r * A.sq.ts + c);
-                    b = seq::load<V>(kp + r * A.sk.ts + c);
-                } else {
+            for (int n = 0; n < N; ++n) {
+                q[n] = seq::load<V>(plus(qp, qo[n]));
+                k[n] = seq::load<V>(plus(kp, ko[n]));
+            }
+        } else {
 #pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (c + i < A.Dk) {
-                            a[i] = qp[r * A.sq.ts + c + i];
-                            b[i] = kp[r * A.sk.ts + c + i];
-                        }
+            for (int n = 0; n < N; ++n) {
+                const int c = (tid + THREADS * n) % PER * V;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int more = max(0, min(i, A.Dk - 1 - c));
+                    q[n][i] = plus(qp, qo[n])[more];
+                    k[n][i] = plus(kp, ko[n])[more];
                 }
             }
-            q[n] = a;
-            k[n] = b;
         }
-        const DeltaRecord &rec = records[head * A.tiles + tile];
-        t = seq::load<4>(rec.t + 4 * threadIdx.x);
-        p = seq::load<4>(rec.p + 4 * threadIdx.x);
-        if (threadIdx.x < 7 * CH / 4) vectors = seq::load<4>(rec.since + 4 * threadIdx.x);
+        const DeltaRecord *rec = records + tile;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            t[n] = seq::load<4>(rec->t + 4 * (tid + THREADS * n));
+            p[n] = seq::load<4>(rec->p + 4 * (tid + THREADS * n));
+        }
+        vectors = seq::load<4>(rec->since + 4 * min(tid, 7 * CH / 4 - 1));
     }
-    __device__ __forceinline__ void put(DeltaTile<E, DK> &s) const
+    __device__ __forceinline__ void put(DeltaTile<E, DK> &s, int Dk) const
     {
         using Tile = DeltaTile<E, DK>;
+        const bool whole = rows == CH && Dk == DK;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int e = threadIdx.x + 256 * n, r = e / PER, c = e % PER * V;
-            if (r < CH) {
-                seq::store<V>(s.q + r * Tile::LD + c, q[n]);
-                seq::store<V>(s.k + r * Tile::LD + c, k[n]);
+            const int e = tid + THREADS * n, r = e / PER, c = e % PER * V;
+            vec<E, V> x = q[n], y = k[n];
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const bool in = r < rows && c + i < Dk;
+                    x[i] = in ? x[i] : (E)0.f;
+                    y[i] = in ? y[i] : (E)0.f;
+                }
+            if (CH * PER % THREADS == 0 || r < CH) {
+                seq::store<V>(s.q + r * Tile::LD + c, x);
+                seq::store<V>(s.k + r * Tile::LD + c, y);
             }
         }
-        const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4;
-        seq::store<4>(s.t + r * Tile::LC + c, t);
-        seq::store<4>(s.p + r * Tile::LC + c, p);
-        if (threadIdx.x < 7 * CH / 4) seq::store<4>(s.vectors + 4 * threadIdx.x, vectors);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const int e = tid + THREADS * n, r = e / 8, c = e % 8 * 4;
+            seq::store<4>(s.t + r * Tile::LC + c, t[n]);
+            seq::store<4>(s.p + r * Tile::LC + c, p[n]);
+        }
+        if (tid < 7 * CH / 4) seq::store<4>(s.vectors + 4 * tid, vectors);
     }
 };
 static_assert(offsetof(DeltaRecord, cut) - offsetof(DeltaRecord, since) == 6 * CH * 4, "the vectors lie one behind the other");
@@ -395,52 +439,63 @@ template <class T> __device__ __forceinline__ vec<T, 8> eight(const T *p)
     return v;
 }
 
-// Rows of a matrix of steps (K, Q) as left operand for half a pair: dealt rows, columns 32 p..
-template <class E, int LD> __device__ __forceinline__ vec<E, 8> rows_of(const E *m, int half, int p, int lane)
+// Rows of a matrix of steps (K, Q) as left operand: steps 16 m.., columns 32 p..
+template <class E, int LD> __device__ __forceinline__ vec<E, 8> rows_of(const E *x, int m, int p, int lane)
 {
-    return eight(m + dealt(half, lane & 15) * LD + 32 * p + 8 * (lane >> 4));
+    return eight(x + (16 * m + (lane & 15)) * LD + 32 * p + 8 * (lane >> 4));
 }
-// Its transposed, the rows being the dealt columns of 32 p.., 32 steps deep.  In bf16 by the transposing LDS read: of four rows that a group of 16 lanes
-// points at, four lanes a row, each lane gets one column.
-template <class E, int LD> __device__ __forceinline__ vec<E, 8> columns_of(const E *m, int half, int p, int lane)
+// Columns of one as left operand, 32 steps deep in the order of a pair of results: a lane has steps 4 (l / 16).. and 16 + 4 (l / 16)... Column `i` of 16 is
+// element 4 (i / 4) STRIDE + i % 4 from x on.  In bf16 by the transposing LDS read: of four rows that a group of 16 lanes points at, four lanes a row,
+// each lane gets one column.
+template <int STRIDE, int LD> __device__ __forceinline__ f8 columns_of(const float *x, int lane)
 {
-    const int g = lane >> 4, i = lane & 15;
-    if constexpr (std::is_same<E, float>::value) {
-        const float *a = m + 8 * g * LD + 32 * p + dealt(half, i);
-        f8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = a[e * LD];
-        return v;
-    } else {
-        using s4 = vec<short, 4>;
-        const bf16 *a = m + (8 * g + (i >> 2)) * LD + 32 * p + 8 * (i & 3) + 4 * half;
-        typedef __attribute__((address_space(3))) s4 *At;
-        const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)a), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(a + 4 * LD));
-        vec<short, 8> v = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-        return __builtin_bit_cast(b8, v);
-    }
+    const float *a = x + 4 * (lane >> 4) * LD + 4 * STRIDE * ((lane & 15) >> 2) + (lane & 3);
+    return f8{a[0], a[LD], a[2 * LD], a[3 * LD], a[16 * LD], a[17 * LD], a[18 * LD], a[19 * LD]};
 }
-// Rows of T or P (fp32) as left operand, and of their transposed
-template <int LC> __device__ __forceinline__ f8 square_rows(const float *m, int half, int lane) { return eight(m + dealt(half, lane & 15) * LC + 8 * (lane >> 4)); }
-template <int LC> __device__ __forceinline__ f8 square_columns(const float *m, int half, int lane)
+template <int STRIDE, int LD> __device__ __forceinline__ b8 columns_of(const bf16 *x, int lane)
 {
-    const float *a = m + 8 * (lane >> 4) * LC + dealt(half, lane & 15);
-    f8 v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = a[e * LC];
-    return v;
+    using s4 = vec<short, 4>;
+    typedef __attribute__((address_space(3))) s4 *At;
+    const bf16 *a = x + (4 * (lane >> 4) + ((lane & 15) >> 2)) * LD + 4 * STRIDE * (lane & 3);
+    const s4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)a), v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(a + 16 * LD));
+    return __builtin_bit_cast(b8, (vec<short, 8>){u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]});
 }
-// Numbers of a step each, of the dealt steps of half a pair that a lane holds
-__device__ __forceinline__ f4 of_steps(const float *p, int half, int lane) { return load<4>(p + 8 * (lane >> 4) + 4 * half); }
+// The columns that result n of a state's results stands for: dealt, every second four of 32
+template <class E, int LD> __device__ __forceinline__ vec<E, 8> state_columns(const E *x, int n, int lane) { return columns_of<2, LD>(x + 32 * (n >> 1) + 4 * (n & 1), lane); }
 
-template <int N> __device__ __forceinline__ bool finite(const f4 (&v)[N])
+__device__ __forceinline__ f4 mm4(f4 a, f4 b, f4 c)
 {
-    bool ok = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+// X r and X^T r for lower triangular X (T, P) of fp32 in LDS, r a pair of results
+template <int LC> __device__ __forceinline__ void lower(const float *x, const f4 (&r)[2], int lane, f4 (&out)[2])
+{
+    const float *a = x + (lane & 15) * LC + 4 * (lane >> 4);
+    out[1] = mm4(load<4>(a + 16 * LC), r[0], out[1]);
+    out[0] = mm4(load<4>(a), r[0], out[0]);
+    out[1] = mm4(load<4>(a + 16 * LC + 16), r[1], out[1]);
+}
+template <int LC> __device__ __forceinline__ void upper(const float *x, const f4 (&r)[2], int lane, f4 (&out)[2])
+{
+    const float *a = x + 4 * (lane >> 4) * LC + (lane & 15), *b = a + 16 * LC;
+    out[0] = mm4(f4{b[0], b[LC], b[2 * LC], b[3 * LC]}, r[1], out[0]);
+    out[1] = mm4(f4{b[16], b[16 + LC], b[16 + 2 * LC], b[16 + 3 * LC]}, r[1], out[1]);
+    out[0] = mm4(f4{a[0], a[LC], a[2 * LC], a[3 * LC]}, r[0], out[0]);
+}
+// Numbers of a step each, of the steps that a lane holds of result m
+__device__ __forceinline__ f4 of_steps(const float *p, int m, int lane) { return load<4>(p + 16 * m + 4 * (lane >> 4)); }
+
+// 0, or NaN if a number is not finite
+template <int N> __device__ __forceinline__ float nothing(const f4 (&v)[N])
+{
+    f4 sum = {};
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ok &= fabsf(v[i][e]) < INFINITY;
-    return ok;
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(v[i][e], 0.f, sum[e]);
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 __device__ __forceinline__ f4 where(f4 factor, f4 v)      // factor v, 0 where factor is 0, whatever v is
 {
@@ -466,23 +521,38 @@ template <int DK> struct Columns {
     f4 s[DK / 16];
     __device__ __forceinline__ void get(const float *from, int Dk, int Dv, int c, int lane)
     {
+        if (!from) return clear();
+        const int g = lane >> 4;
+        const bool mine = c < Dv;
+        from += mine ? c : Dv - 1;
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
-                s[n][e] = from && c < Dv && d < Dk ? from[(long)d * Dv + c] : 0.f;
+                const int d = 32 * (n >> 1) + 8 * g + 4 * (n & 1) + e;
+                const float x = from[(long)min(d, Dk - 1) * Dv];
+                s[n][e] = mine && d < Dk ? x : 0.f;
             }
     }
     __device__ __forceinline__ void put(float *to, int Dk, int Dv, int c, int lane) const
     {
+        if (c >= Dv) return;
+        const int g = lane >> 4;
+        to += (long)(8 * g) * Dv + c;
+        if (Dk == DK) {
 #pragma unroll
-        for (int n = 0; n < DK / 16; ++n)
+            for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
-                if (c < Dv && d < Dk) to[(long)d * Dv + c] = s[n][e];
-            }
+                for (int e = 0; e < 4; ++e) to[(long)(32 * (n >> 1) + 4 * (n & 1) + e) * Dv] = s[n][e];
+        } else {
+#pragma unroll
+            for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int d = 32 * (n >> 1) + 4 * (n & 1) + e;
+                    if (8 * g + d < Dk) to[(long)d * Dv] = s[n][e];
+                }
+        }
     }
     // sum over rows of x_d S_dc, x a step's row of K or Q in LDS
     template <class E> __device__ __forceinline__ float dot(const E *x, int lane) const
@@ -540,208 +610,288 @@ template <class E, int DK> __device__ __forceinline__ void delta_pass_back(const
     else D.scaled(s.gate()[i]);
 }
 
-// A lane's numbers of column c of a tensor of steps [..][Dv] (V, dO), and storing them
-template <class E> __device__ __forceinline__ void get_steps(const E *p, long ts, bool mine, int rows, int lane, f4 (&v)[2])
+// A lane's numbers of a column of a tensor of steps [..][Dv] (V, dO, O): where they lie, and as they are loaded
+template <class E> struct Steps {
+    uint32_t at[8];
+    int rows;
+    E x[8];
+    __device__ __forceinline__ void offsets(int ts, int c, int Dv, int n_rows, int lane)
+    {
+        rows = n_rows;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) at[i] = (uint32_t)(min(16 * (i >> 2) + 4 * (lane >> 4) + (i & 3), n_rows - 1) * ts + min(c, Dv - 1)) * (uint32_t)sizeof(E);
+    }
+    __device__ __forceinline__ void load(const E *tile, int ts, int c, int Dv, int n_rows, int lane)
+    {
+        if (n_rows != rows) offsets(ts, c, Dv, n_rows, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = *plus(tile, at[i]);
+    }
+    __device__ __forceinline__ void get(bool mine, int lane, f4 (&v)[2]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = mine && 16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) < rows ? (float)x[i] : 0.f;
+    }
+};
+template <class E> __device__ __forceinline__ void put_steps(E *tile, const Steps<E> &s, bool mine, int rows, int lane, const f4 (&v)[2])
 {
+    if (!mine) return;
+    if (rows == CH) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+        for (int i = 0; i < 8; ++i) *plus(tile, s.at[i]) = (E)v[i >> 2][i & 3];
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 8 * (lane >> 4) + 4 * m + e;
-            v[m][e] = mine && i < rows ? (float)p[i * ts] : 0.f;
-        }
-}
-template <class E> __device__ __forceinline__ void put_steps(E *p, long ts, bool mine, int rows, int lane, const f4 (&v)[2])
-{
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 8 * (lane >> 4) + 4 * m + e;
-            if (mine && i < rows) p[i * ts] = (E)v[m][e];
-        }
+        for (int i = 0; i < 8; ++i)
+            if (16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) < rows) *plus(tile, s.at[i]) = (E)v[i >> 2][i & 3];
+    }
 }
 
 // U of a wave's columns from the state that enters and V.
 template <class E, int DK, int N> __device__ __forceinline__ void delta_u(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&S)[DK / 32], const f4 (&v)[2], int rows, int lane, f4 (&u)[2])
 {
     using Tile = DeltaTile<E, DK>;
-    f4 r[2];
+    f4 r[2], ks[2] = {};
+#pragma unroll
+    for (int p = 0; p < DK / 32; ++p)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) ks[m] = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), S[p], ks[m]);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        f4 ks = {};
+        const f4 old = where(of_steps(s.since(), m, lane), ks[m]), beta = of_steps(s.beta(), m, lane);
 #pragma unroll
-        for (int p = 0; p < DK / 32; ++p) ks = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), S[p], ks);
-        const f4 old = where(of_steps(s.since(), m, lane), ks), beta = of_steps(s.beta(), m, lane);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[m][e] = 8 * (lane >> 4) + 4 * m + e < rows ? beta[e] * (v[m][e] - old[e]) : 0.f;
+        for (int e = 0; e < 4; ++e) r[m][e] = 16 * m + 4 * (lane >> 4) + e < rows ? beta[e] * (v[m][e] - old[e]) : 0.f;
+        u[m] = f4{};
     }
-#pragma unroll
-    for (int m = 0; m < 2; ++m) u[m] = mfma(square_rows<Tile::LC>(s.t, m, lane), both(r[0], r[1]), f4{});
+    lower<Tile::LC>(s.t, r, lane, u);
 }
-
-// ---------------------------------------------------------------- from state to state
-// A workgroup per head and COLS columns.  A tile whose results hold a number that is not finite is taken again step by step as the definition
-// has it, where nothing is multiplied by the zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
-template <class E, int DK> __global__ __launch_bounds__(256) void k_delta(DeltaArgs A)
-{
-    using Tile = DeltaTile<E, DK>;
-    extern __shared__ __align__(16) unsigned char lds[];
-    Tile *tiles = reinterpret_cast<Tile *>(lds);
-    const int lane = threadIdx.x & 63;
-    const int slices = (A.Dv + COLS - 1) / COLS, slice = blockIdx.x % slices;
-    const long head = blockIdx.x / slices;
-    const int bi = (int)(head / A.H), h = (int)(head % A.H), c = COLS * slice + 16 * (threadIdx.x >> 6) + (lane & 15);
-    const bool mine = c < A.Dv;
-    const E *v = (const E *)A.v + bi * A.sv.bs + h * A.sv.hs + c;
-    E *o = (E *)A.o + bi * A.so.bs + h * A.so.hs + c;
-    const DeltaRecord *records = (const DeltaRecord *)A.records;
-    Columns<DK> S;
-    S.get(A.s0 ? A.s0 + head * A.Dk * A.Dv : nullptr, A.Dk, A.Dv, c, lane);
-    DeltaFetch<E, DK> fetch;
-    f4 val[2], next_val[2];
-    if (A.tiles) {
-        fetch.load(A, records, head, 0);
-        get_steps(v, A.sv.ts, mine, (int)min((long)CH, A.T), lane, next_val);
-        fetch.put(tiles[0]);
-    }
-    __syncthreads();
-    for (long tile = 0; tile < A.tiles; ++tile) {
-        const Tile &s = tiles[tile & 1];
-        const long t0 = tile * CH;
-        const int rows = (int)min((long)CH, A.T - t0);
-        val[0] = next_val[0];
-        val[1] = next_val[1];
-        const bool more = tile + 1 < A.tiles;
-        if (more) {
-            fetch.load(A, records, head, tile + 1);
-            get_steps(v + (t0 + CH) * A.sv.ts, A.sv.ts, mine, (int)min((long)CH, A.T - t0 - CH), lane, next_val);
-        }
-        if (A.states) S.put(A.states + (head * A.tiles + tile) * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
-        typename Operand<E>::template Split<3> sp[DK / 32];
-#pragma unroll
-        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(S.s[2 * p], S.s[2 * p + 1]);
-        f4 u[2], out[2];
-        delta_u<E, DK, 3>(s, sp, val, rows, lane, u);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            f4 qs = {};
-#pragma unroll
-            for (int p = 0; p < DK / 32; ++p) {
-                const auto a = rows_of<E, Tile::LD>(s.q, m, p, lane);
-                if constexpr (std::is_same<E, float>::value) qs = mfma(a, sp[p], qs);
-                else qs = mfma(a, sp[p].p[0], mfma(a, sp[p].p[1], qs));     // o is rounded to bf16: 16 bits of the state do
-            }
-            qs = where(of_steps(s.since(), m, lane), A.scale * qs);
-            out[m] = mfma(square_rows<Tile::LC>(s.p, m, lane), both(u[0], u[1]), qs);
-        }
-        const auto up = split<E, 3>(where(of_steps(s.until(), 0, lane), u[0]), where(of_steps(s.until(), 1, lane), u[1]));
-        f4 next[DK / 16];
-        const float left = s.since()[CH - 1];
-#pragma unroll
-        for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.k, n & 1, n >> 1, lane), up, where(left, S.s[n]));
-        if (__any(!(finite(out) && finite(next)))) {
-            for (int i = 0; i < rows; ++i) {
-                delta_step<E, DK>(s, S, i, mine ? (float)v[(t0 + i) * A.sv.ts] : 0.f, lane);
-                const float x = A.scale * S.dot(s.q + i * Tile::LD, lane);
-                if (mine && lane < 16) o[(t0 + i) * A.so.ts] = (E)x;
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < DK / 16; ++n) S.s[n] = next[n];
-            put_steps(o + t0 * A.so.ts, A.so.ts, mine, rows, lane, out);
-        }
-        if (more) fetch.put(tiles[(tile + 1) & 1]);
-        lds_barrier();
-    }
-    if (A.last) S.put(A.last + head * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
-}
-
-// kd = (G_C. K) D, then Y = T^T (P^T dO + kd) of a wave's columns.
+// kd = (G_C. K) D, then Y = T^T (pd + kd) of a wave's columns, pd = P^T dO.
 template <class E, int DK, int N>
-__device__ __forceinline__ void delta_y(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&D)[DK / 32], const f4 (&dout)[2], int lane, f4 (&kd)[2], f4 (&y)[2])
+__device__ __forceinline__ void delta_y(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&D)[DK / 32], const f4 (&pd)[2], int lane, f4 (&kd)[2], f4 (&y)[2])
 {
     using Tile = DeltaTile<E, DK>;
     f4 du[2];
+    kd[0] = kd[1] = f4{};
+#pragma unroll
+    for (int p = 0; p < DK / 32; ++p)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) kd[m] = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), D[p], kd[m]);
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        kd[m] = f4{};
-#pragma unroll
-        for (int p = 0; p < DK / 32; ++p) kd[m] = mul<E, N>(rows_of<E, Tile::LD>(s.k, m, p, lane), D[p], kd[m]);
         kd[m] = where(of_steps(s.until(), m, lane), kd[m]);
-        du[m] = mfma(square_columns<Tile::LC>(s.p, m, lane), both(dout[0], dout[1]), kd[m]);
+        du[m] = kd[m] + pd[m];
+        y[m] = f4{};
     }
+    upper<Tile::LC>(s.t, du, lane, y);
+}
+
+// ---------------------------------------------------------------- from state to state
+// A workgroup per head and 16 columns of each of WAVES pairs of waves.  One wave of a pair takes the state from tile to tile and nothing else; the
+// other brings tiles into LDS and does, a tile apart, what the chain does not wait for: the outputs, or in the backward direction what dO alone
+// gives.  They hand each other registers as they are, through LDS, with one barrier a tile.
+// A tile whose results hold a number that is not finite is taken again step by step as the definition has it, where nothing is multiplied by the
+// zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
+template <class E, int DK> struct DeltaPairs {
+    static constexpr int tile = (int)sizeof(DeltaTile<E, DK>), pair = 2 * 64 * (DK / 16 + 2) * 16, room = 160 * 1024;
+    static constexpr int waves = 3 * tile + 4 * pair <= room ? 4 : 3 * tile + 2 * pair <= room ? 2 : 1;
+};
+template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>::waves;
+template <class E, int DK> struct DeltaChain {
+    static constexpr int WAVES = DeltaPairs<E, DK>::waves;
+    DeltaTile<E, DK> tiles[3];
+    f4 state[2][WAVES][DK / 16][64];      // forward: the state that enters; backward: (scale g Q)^T dO
+    f4 steps[2][WAVES][2][64];            // U; P^T dO
+};
+template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta(DeltaArgs A)
+{
+    using Tile = DeltaTile<E, DK>;
+    using Chain = DeltaChain<E, DK>;
+    constexpr int WAVES = Chain::WAVES;
+    extern __shared__ __align__(16) unsigned char lds[];
+    Chain &L = *reinterpret_cast<Chain *>(lds);
+    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
+    const bool chain = threadIdx.x < 64 * WAVES;
+    const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
+    const unsigned head = blockIdx.x / slices;
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), c = 16 * (WAVES * slice + w) + (lane & 15);
+    const bool mine = c < A.Dv;
+    const long size = (long)A.Dk * A.Dv;
+    const E *v = head_of<E>(A.v, A.sv, bi, h);
+    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - tile * CH); };
+    if (chain) {
+        Columns<DK> S;
+        S.get(A.s0 ? A.s0 + head * size : nullptr, A.Dk, A.Dv, c, lane);
+        Steps<E> vs;
+        vs.rows = 0;
+        if (A.tiles) vs.load(v, (int)A.sv.ts, c, A.Dv, rows_in(0), lane);
+        __syncthreads();
+        for (long i = 0; i <= A.tiles; ++i) {
+            if (i < A.tiles) {
+                const Tile &s = L.tiles[i % 3];
+                const int rows = rows_in(i);
+                f4 val[2], u[2], next[DK / 16];
+                vs.get(mine, lane, val);
+                if (i + 1 < A.tiles) vs.load(v + (i + 1) * CH * A.sv.ts, (int)A.sv.ts, c, A.Dv, rows_in(i + 1), lane);
 #pragma unroll
-    for (int m = 0; m < 2; ++m) y[m] = mfma(square_columns<Tile::LC>(s.t, m, lane), both(du[0], du[1]), f4{});
+                for (int n = 0; n < DK / 16; ++n) L.state[i & 1][w][n][lane] = S.s[n];
+                typename Operand<E>::template Split<3> sp[DK / 32];
+#pragma unroll
+                for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(S.s[2 * p], S.s[2 * p + 1]);
+                delta_u<E, DK, 3>(s, sp, val, rows, lane, u);
+                L.steps[i & 1][w][0][lane] = u[0];
+                L.steps[i & 1][w][1][lane] = u[1];
+                const auto up = split<E, 3>(where(of_steps(s.until(), 0, lane), u[0]), where(of_steps(s.until(), 1, lane), u[1]));
+                const float left = s.since()[CH - 1];
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), up, where(left, S.s[n]));
+                if (__any(nothing(next) != 0.f)) {
+                    for (int t = 0; t < rows; ++t) delta_step<E, DK>(s, S, t, mine ? (float)v[(i * CH + t) * A.sv.ts + c] : 0.f, lane);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < DK / 16; ++n) S.s[n] = next[n];
+                }
+            }
+            lds_barrier();
+        }
+        if (A.last) S.put(A.last + head * size, A.Dk, A.Dv, c, lane);
+    } else {
+        DeltaFetch<E, DK, 64 * WAVES> fetch;
+        E *o = head_of<E>(A.o, A.so, bi, h);
+        Steps<E> os;
+        os.offsets((int)A.so.ts, c, A.Dv, CH, lane);
+        if (A.tiles) {
+            fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, threadIdx.x - 64 * WAVES);
+            fetch.load(A, 0);
+            fetch.put(L.tiles[0], A.Dk);
+            if (A.tiles > 1) fetch.load(A, 1);
+        }
+        __syncthreads();
+        for (long i = 0; i <= A.tiles; ++i) {
+            if (i + 1 < A.tiles) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
+            if (i + 2 < A.tiles) fetch.load(A, i + 2);
+            if (i > 0) {
+                const long tile = i - 1;
+                const Tile &s = L.tiles[tile % 3];
+                const int rows = rows_in(tile);
+                Columns<DK> S;
+                f4 u[2], out[2];
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) S.s[n] = L.state[tile & 1][w][n][lane];
+                u[0] = L.steps[tile & 1][w][0][lane];
+                u[1] = L.steps[tile & 1][w][1][lane];
+                if (A.states) S.put(A.states + (head * A.tiles + tile) * size, A.Dk, A.Dv, c, lane);
+                typename Operand<E>::template Split<2> sp[DK / 32];      // o is rounded to bf16: 16 bits of the state do
+#pragma unroll
+                for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(S.s[2 * p], S.s[2 * p + 1]);
+                out[0] = out[1] = f4{};
+#pragma unroll
+                for (int p = 0; p < DK / 32; ++p)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) out[m] = mul<E, 2>(rows_of<E, Tile::LD>(s.q, m, p, lane), sp[p], out[m]);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) out[m] = where(of_steps(s.since(), m, lane), A.scale * out[m]);
+                lower<Tile::LC>(s.p, u, lane, out);
+                E *to = o + tile * CH * A.so.ts;
+                if (__any(nothing(out) != 0.f)) {
+                    for (int t = 0; t < rows; ++t) {
+                        delta_step<E, DK>(s, S, t, mine ? (float)v[(tile * CH + t) * A.sv.ts + c] : 0.f, lane);
+                        const float x = A.scale * S.dot(s.q + t * Tile::LD, lane);
+                        if (mine && lane < 16) to[t * A.so.ts + c] = (E)x;
+                    }
+                } else put_steps(to, os, mine, rows, lane, out);
+            }
+            lds_barrier();
+        }
+    }
 }
 
 // The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.
-template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_back(DeltaGradArgs A)
+template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta_back(DeltaGradArgs A)
 {
     using Tile = DeltaTile<E, DK>;
+    using Chain = DeltaChain<E, DK>;
+    constexpr int WAVES = Chain::WAVES;
     extern __shared__ __align__(16) unsigned char lds[];
-    Tile *tiles = reinterpret_cast<Tile *>(lds);
-    const int lane = threadIdx.x & 63;
-    const int slices = (A.Dv + COLS - 1) / COLS, slice = blockIdx.x % slices;
-    const long head = blockIdx.x / slices;
-    const int bi = (int)(head / A.H), h = (int)(head % A.H), c = COLS * slice + 16 * (threadIdx.x >> 6) + (lane & 15);
+    Chain &L = *reinterpret_cast<Chain *>(lds);
+    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
+    const bool chain = threadIdx.x < 64 * WAVES;
+    const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
+    const unsigned head = blockIdx.x / slices;
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), c = 16 * (WAVES * slice + w) + (lane & 15);
     const bool mine = c < A.Dv;
-    const E *dout = (const E *)A.dout + bi * A.sdo.bs + h * A.sdo.hs + c;
-    const DeltaRecord *records = (const DeltaRecord *)A.records;
-    Columns<DK> D;
-    D.get(A.dlast ? A.dlast + head * A.Dk * A.Dv : nullptr, A.Dk, A.Dv, c, lane);
-    DeltaFetch<E, DK> fetch;
-    f4 out[2], next_out[2];
-    auto get = [&](long tile) {
-        fetch.load(A, records, head, tile);
-        get_steps(dout + tile * CH * A.sdo.ts, A.sdo.ts, mine, (int)min((long)CH, A.T - tile * CH), lane, next_out);
-    };
-    if (A.tiles) {
-        get(A.tiles - 1);
-        fetch.put(tiles[(A.tiles - 1) & 1]);
-    }
-    __syncthreads();
-    for (long tile = A.tiles - 1; tile >= 0; --tile) {
-        const Tile &s = tiles[tile & 1];
-        const long t0 = tile * CH;
-        const int rows = (int)min((long)CH, A.T - t0);
-        out[0] = next_out[0];
-        out[1] = next_out[1];
-        if (tile) get(tile - 1);
-        D.put(A.into + (head * A.tiles + tile) * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
-        typename Operand<E>::template Split<3> sp[DK / 32];
+    const long size = (long)A.Dk * A.Dv;
+    const E *dout = head_of<E>(A.dout, A.sdo, bi, h);
+    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - tile * CH); };
+    // turn i of the pair that brings and prepares is for tile `tiles - 1 - i`, of the chain for the one before
+    if (chain) {
+        Columns<DK> D;
+        D.get(A.dlast ? A.dlast + head * size : nullptr, A.Dk, A.Dv, c, lane);
+        __syncthreads();
+        for (long i = 0; i <= A.tiles; ++i) {
+            if (i > 0) {
+                const long tile = A.tiles - i;
+                const Tile &s = L.tiles[tile % 3];
+                D.put(A.into + (head * A.tiles + tile) * size, A.Dk, A.Dv, c, lane);
+                typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
-        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(D.s[2 * p], D.s[2 * p + 1]);
-        f4 kd[2], y[2];
-        delta_y<E, DK, 3>(s, sp, out, lane, kd, y);
-        f4 x[2], z[2];
+                for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(D.s[2 * p], D.s[2 * p + 1]);
+                const f4 pd[2] = {L.steps[tile & 1][w][0][lane], L.steps[tile & 1][w][1][lane]};
+                f4 kd[2], y[2], next[DK / 16];
+                delta_y<E, DK, 3>(s, sp, pd, lane, kd, y);
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f4 since = of_steps(s.since(), m, lane);
-            x[m] = where(since, A.scale * out[m]);
-            z[m] = where(since, -of_steps(s.beta(), m, lane) * y[m]);
-        }
-        const auto xp = split<E, 3>(x[0], x[1]), zp = split<E, 3>(z[0], z[1]);
-        const float left = s.since()[CH - 1];
-        f4 next[DK / 16];
+                for (int m = 0; m < 2; ++m) y[m] = where(of_steps(s.since(), m, lane), -of_steps(s.beta(), m, lane) * y[m]);
+                const auto yp = split<E, 3>(y[0], y[1]);
+                const float left = s.since()[CH - 1];
 #pragma unroll
-        for (int n = 0; n < DK / 16; ++n) {
-            next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.q, n & 1, n >> 1, lane), xp, where(left, D.s[n]));
-            next[n] = mul<E, 3>(columns_of<E, Tile::LD>(s.k, n & 1, n >> 1, lane), zp, next[n]);
-        }
-        if (__any(!finite(next))) {
-            for (int i = rows - 1; i >= 0; --i) {
-                delta_step_back<E, DK>(s, D, i, mine ? (float)dout[(t0 + i) * A.sdo.ts] : 0.f, A.scale, lane);
-                delta_pass_back<E, DK>(s, D, i);
+                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), yp, where(left, D.s[n]) + L.state[tile & 1][w][n][lane]);
+                if (__any(nothing(next) != 0.f)) {
+                    for (int t = rows_in(tile) - 1; t >= 0; --t) {
+                        delta_step_back<E, DK>(s, D, t, mine ? (float)dout[(tile * CH + t) * A.sdo.ts + c] : 0.f, A.scale, lane);
+                        delta_pass_back<E, DK>(s, D, t);
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < DK / 16; ++n) D.s[n] = next[n];
+                }
             }
-        } else {
-#pragma unroll
-            for (int n = 0; n < DK / 16; ++n) D.s[n] = next[n];
+            lds_barrier();
         }
-        if (tile) fetch.put(tiles[(tile - 1) & 1]);
-        lds_barrier();
+        if (A.ds0) D.put(A.ds0 + head * size, A.Dk, A.Dv, c, lane);
+    } else {
+        DeltaFetch<E, DK, 64 * WAVES> fetch;
+        Steps<E> ds;
+        ds.rows = 0;
+        auto get = [&](long tile) { ds.load(dout + tile * CH * A.sdo.ts, (int)A.sdo.ts, c, A.Dv, rows_in(tile), lane); };
+        if (A.tiles) {
+            fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, threadIdx.x - 64 * WAVES);
+            fetch.load(A, A.tiles - 1);
+            get(A.tiles - 1);
+            fetch.put(L.tiles[(A.tiles - 1) % 3], A.Dk);
+            if (A.tiles > 1) fetch.load(A, A.tiles - 2);
+        }
+        __syncthreads();
+        for (long i = 0; i <= A.tiles; ++i) {
+            const long tile = A.tiles - 1 - i;
+            if (tile >= 0) {
+                f4 out[2], pd[2] = {}, x[2];
+                ds.get(mine, lane, out);
+                if (tile > 0) {
+                    fetch.put(L.tiles[(tile - 1) % 3], A.Dk);
+                    get(tile - 1);
+                }
+                if (tile > 1) fetch.load(A, tile - 2);
+                const Tile &s = L.tiles[tile % 3];
+                upper<Tile::LC>(s.p, out, lane, pd);
+                L.steps[tile & 1][w][0][lane] = pd[0];
+                L.steps[tile & 1][w][1][lane] = pd[1];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) x[m] = where(of_steps(s.since(), m, lane), A.scale * out[m]);
+                const auto xp = split<E, 3>(x[0], x[1]);
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) L.state[tile & 1][w][n][lane] = mul<E, 3>(state_columns<E, Tile::LD>(s.q, n, lane), xp, f4{});
+            }
+            lds_barrier();
+        }
     }
-    if (A.ds0) D.put(A.ds0 + head * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
 }
 
 // ---------------------------------------------------------------- gradients
@@ -752,6 +902,8 @@ template <int R, int C> struct Matrix<float, R, C> {
     float m[R * LD];
     __device__ __forceinline__ void put(int i, int j, float v) { m[i * LD + j] = v; }
     __device__ __forceinline__ f8 get(int i, int j) const { return eight(m + i * LD + j); }
+    // columns j.. and 16 + j..
+    __device__ __forceinline__ f8 pair(int i, int j) const { return both(load<4>(m + i * LD + j), load<4>(m + i * LD + j + 16)); }
 };
 template <int R, int C> struct Matrix<bf16, R, C> {
     static constexpr int LD = C + 8;
@@ -763,6 +915,16 @@ template <int R, int C> struct Matrix<bf16, R, C> {
         m[1][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(b >> 16));
     }
     __device__ __forceinline__ Planes<2> get(int i, int j) const { return Planes<2>{{eight(m[0] + i * LD + j), eight(m[1] + i * LD + j)}}; }
+    __device__ __forceinline__ Planes<2> pair(int i, int j) const
+    {
+        Planes<2> o;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const vec<bf16, 4> a = load<4>(m[n] + i * LD + j), b = load<4>(m[n] + i * LD + j + 16);
+            o.p[n] = b8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        }
+        return o;
+    }
 };
 template <class E, int DK> struct DeltaGradTile {
     static constexpr int LO = COLS + 16 / (int)sizeof(E);
@@ -772,23 +934,235 @@ template <class E, int DK> struct DeltaGradTile {
     Matrix<E, CH, CH> dp, dn, dpt, dnt;     // of P's and N's products, and transposed
     float sums[3][4][CH];                   // of each wave and row: q.dq, Y.u, dv.v
     float ends[4];                          // of each wave: <D, S'>
-    float rows[2][4][DK];                   // step by step: of each wave, dq and dk of a step
 };
 
-// 8 numbers of a state's row d, columns c.., as right operand
-template <class E> __device__ __forceinline__ typename Operand<E>::template Split<2> state_row(const float *S, int d, int c, int Dk, int Dv, bool real)
+// 8 numbers of a state's row d, columns c.., as right operand; quads: Dv is a multiple of 4
+template <class E> __device__ __forceinline__ typename Operand<E>::template Split<2> state_row(const float *S, int d, int c, int Dk, int Dv, bool quads)
 {
     float v[8];
+    const float *p = S + (long)min(d, Dk - 1) * Dv;
+    if (quads) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = real && d < Dk && c + e < Dv ? S[(long)d * Dv + c + e] : 0.f;
+        for (int e = 0; e < 8; e += 4) {
+            const f4 x = load<4>(p + min(c + e, Dv - 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[e + i] = d < Dk && c + e < Dv ? x[i] : 0.f;
+        }
+    } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p[min(c + e, Dv - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = d < Dk && c + e < Dv ? x[e] : 0.f;
+    }
     return Operand<E>::template split<2>(v);
 }
 
+// All gradients but the state's: a workgroup per tile and head.
+template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad(DeltaGradArgs A)
+{
+    using Op = Operand<E>;
+    using Tile = DeltaTile<E, DK>;
+    using Grad = DeltaGradTile<E, DK>;
+    constexpr int LO = Grad::LO, ND = (DK + 63) / 64;      // tiles of 16 of a wave's columns of dq and dk
+    extern __shared__ __align__(16) unsigned char lds[];
+    Grad &g = *reinterpret_cast<Grad *>(lds);
+    Tile &s = g.s;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, grp = lane >> 4, col = lane & 15;
+    const long tile = blockIdx.x % A.tiles, head = blockIdx.x / A.tiles;
+    const int bi = (int)(head / A.H), h = (int)(head % A.H);
+    const long t0 = tile * CH;
+    const int rows = (int)min((long)CH, A.T - t0);
+    const float *S = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *Dn = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
+    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs, *dout = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs;
+    {
+        DeltaFetch<E, DK, 256> fetch;
+        fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, tid);
+        fetch.load(A, tile);
+        fetch.put(s, A.Dk);
+    }
+    __syncthreads();
+    const float left = s.since()[CH - 1];
+    const bool quads = A.Dv % 4 == 0;      // states are 16-byte aligned then
+    // dP and dN: wave 0 has rows and columns 0.., wave 1 rows 16.. of columns 0.., wave 2 rows and columns 16..
+    const int ti = w ? 16 : 0, tj = w == 2 ? 16 : 0;
+    f4 dp = {}, dn = {}, os[ND][2] = {}, ys[ND][2] = {}, ud[ND][2] = {}, yu[2] = {}, vv[2] = {};
+    float end = 0.f;
+    bool ok = true;
+    for (int sl = 0; sl < A.Dv; sl += COLS) {
+        const int c = sl + 16 * w + col;
+        const bool mine = c < A.Dv;
+        f4 out[2], u[2], y[2], val[2], kd[2], pd[2] = {};
+        {
+            Steps<E> vs, ds;
+            vs.rows = ds.rows = 0;
+            vs.load(v, (int)A.sv.ts, c, A.Dv, rows, lane);
+            ds.load(dout, (int)A.sdo.ts, c, A.Dv, rows, lane);
+            Columns<DK> st, D;
+            st.get(S, A.Dk, A.Dv, c, lane);
+            D.get(Dn, A.Dk, A.Dv, c, lane);
+            vs.get(mine, lane, val);
+            ds.get(mine, lane, out);
+            typename Op::template Split<2> sp[DK / 32], dp2[DK / 32];
+#pragma unroll
+            for (int p = 0; p < DK / 32; ++p) {
+                sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
+                dp2[p] = split<E, 2>(D.s[2 * p], D.s[2 * p + 1]);
+            }
+            delta_u<E, DK, 2>(s, sp, val, rows, lane, u);
+            upper<Tile::LC>(s.p, out, lane, pd);
+            delta_y<E, DK, 2>(s, dp2, pd, lane, kd, y);
+            if (left != 0.f)
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) end = fmaf(left * st.s[n][e], D.s[n][e], end);
+        }
+        f4 dv[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            dv[m] = of_steps(s.beta(), m, lane) * y[m];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * m + 4 * grp + e;
+                ok &= fabsf(dv[m][e]) < INFINITY && fabsf(u[m][e]) < INFINITY;
+                yu[m][e] = fmaf(y[m][e], u[m][e], yu[m][e]);
+                vv[m][e] = fmaf(dv[m][e], val[m][e], vv[m][e]);
+                end = fmaf(kd[m][e], u[m][e], end);
+                g.dout[i * LO + 16 * w + col] = (E)out[m][e];
+                g.u.put(i, 16 * w + col, u[m][e]);
+                g.y.put(i, 16 * w + col, y[m][e]);
+            }
+        }
+        {
+            Steps<E> to;
+            to.offsets((int)A.sdv.ts, c, A.Dv, CH, lane);
+            put_steps(head_of<E>(A.dv, A.sdv, bi, h) + t0 * A.sdv.ts, to, mine, rows, lane, dv);
+        }
+        __syncthreads();
+        if (w < 3) {
+#pragma unroll
+            for (int kb = 0; kb < COLS; kb += 32) {
+                const auto b = g.u.get(tj + col, kb + 8 * grp);
+                dp = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, dp);
+                dn = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, dn);
+            }
+        }
+        // columns 16 (w + 4 d).. of dO S^T, Y S^T and U D^T
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const int dk = 16 * (w + 4 * d) + col;
+            if (16 * (w + 4 * d) >= DK) break;
+#pragma unroll
+            for (int kb = 0; kb < COLS; kb += 32) {
+                const auto st = state_row<E>(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads), D = state_row<E>(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    os[d][m] = Op::mul(eight(g.dout + (16 * m + col) * LO + kb + 8 * grp), st, os[d][m]);
+                    ys[d][m] = Op::mul(g.y.get(16 * m + col, kb + 8 * grp), st, ys[d][m]);
+                    ud[d][m] = Op::mul(g.u.get(16 * m + col, kb + 8 * grp), D, ud[d][m]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (w < 3) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = ti + 4 * grp + r, j = tj + col;
+            const float b = j <= i ? s.between(i, j) : 0.f;
+            const float x = b != 0.f ? A.scale * b * dp[r] : 0.f, z = b != 0.f && j < i ? -s.beta()[i] * b * dn[r] : 0.f;
+            g.dp.put(i, j, x);
+            g.dpt.put(j, i, x);
+            g.dn.put(i, j, z);
+            g.dnt.put(j, i, z);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * grp + r, j = 16 + col;      // above the diagonal
+            g.dp.put(i, j, 0.f);
+            g.dpt.put(j, i, 0.f);
+            g.dn.put(i, j, 0.f);
+            g.dnt.put(j, i, 0.f);
+        }
+    }
+    __syncthreads();
+    f4 qd[2] = {};
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        if (16 * (w + 4 * d) >= DK) break;
+        const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * (w + 4 * d), lane), qc = columns_of<1, Tile::LD>(s.q + 16 * (w + 4 * d), lane);
+        const int dk = 16 * (w + 4 * d) + col;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f4 since = load<4>(s.since() + 16 * m + 4 * grp), beta = load<4>(s.beta() + 16 * m + 4 * grp), until = load<4>(s.until() + 16 * m + 4 * grp);
+            f4 x = where(since, A.scale * os[d][m]), z = where(since, -beta * ys[d][m]) + where(until, ud[d][m]);
+            x = Op::mul(g.dp.pair(16 * m + col, 4 * grp), kc, x);
+            z = Op::mul(g.dpt.pair(16 * m + col, 4 * grp), qc, z);
+            z = Op::mul(g.dn.pair(16 * m + col, 4 * grp), kc, z);
+            z = Op::mul(g.dnt.pair(16 * m + col, 4 * grp), kc, z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * m + 4 * grp + e;
+                ok &= fabsf(x[e]) < INFINITY && fabsf(z[e]) < INFINITY;
+                qd[m][e] = fmaf(x[e], (float)s.q[i * Tile::LD + dk], qd[m][e]);
+                if (dk < A.Dk && i < rows) {
+                    ((E *)A.dq)[bi * A.sdq.bs + (t0 + i) * A.sdq.ts + h * A.sdq.hs + dk] = (E)x[e];
+                    ((E *)A.dk)[bi * A.sdk.bs + (t0 + i) * A.sdk.ts + h * A.sdk.hs + dk] = (E)z[e];
+                }
+            }
+        }
+    }
+    ok &= fabsf(end) < INFINITY;
+    const bool again = __syncthreads_or(!ok);
+    if (tid == 0) A.again[head * A.tiles + tile] = again;
+    if (again) return;                  // k_delta_grad_steps's
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = group_fold(qd[m][e], 16, add), b = group_fold(yu[m][e], 16, add), d = group_fold(vv[m][e], 16, add);
+            if (col == 0) {
+                g.sums[0][w][16 * m + 4 * grp + e] = a;
+                g.sums[1][w][16 * m + 4 * grp + e] = b;
+                g.sums[2][w][16 * m + 4 * grp + e] = d;
+            }
+        }
+    end = group_fold(end, 64, add);
+    if (lane == 0) g.ends[w] = end;
+    __syncthreads();
+    if (tid < CH) {
+        const int i = tid, cut = s.cut()[i];
+        auto all = [&](int k) { return (g.sums[k][0][i] + g.sums[k][1][i]) + (g.sums[k][2][i] + g.sums[k][3][i]); };
+        float x = i < rows ? all(0) - all(2) : 0.f;
+        if (i == rows - 1) x += (g.ends[0] + g.ends[1]) + (g.ends[2] + g.ends[3]);
+#pragma unroll
+        for (int d = 1; d < CH; d *= 2) {
+            const float o = __shfl_down(x, d, CH);
+            const int oc = __shfl_down(cut, d, CH);
+            if (i + d < CH && oc == cut) x += o;
+        }
+        if (i < rows) {
+            const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
+            ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, i) || s.gate()[i] == 0.f ? 0.f : x * (1.f / (1.f + expf(f))));
+            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(all(1) * (1.f / (1.f + expf(b))));
+        }
+    }
+}
+
 // The gradients of a tile's steps one by one, as the definition has them: every state is formed again from the first, which takes as many
-// passes as there are steps.  For tiles with numbers that are not finite.
-template <class E, int DK> __device__ __noinline__ void delta_grad_steps(const DeltaGradArgs &A, DeltaGradTile<E, DK> &g, long head, long tile, const float *S0, const float *D0)
+// passes as there are steps.  For tiles with numbers that are not finite, which k_delta_grad has left: a workgroup looks at AGAIN tiles.
+constexpr int AGAIN = 64;
+template <class E, int DK> struct DeltaSteps {
+    DeltaTile<E, DK> s;
+    float sums[2][4];
+    float rows[2][4][DK];               // of each wave, dq and dk of a step
+};
+template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs &A, DeltaSteps<E, DK> &g, long head, long tile)
 {
     using Tile = DeltaTile<E, DK>;
+    const float *S0 = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *D0 = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
     Tile &s = g.s;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bi = (int)(head / A.H), h = (int)(head % A.H);
     const long t0 = tile * CH;
@@ -843,7 +1217,7 @@ template <class E, int DK> __device__ __noinline__ void delta_grad_steps(const D
                 if ((lane & 15) == 0) g.rows[0][w][d] = x, g.rows[1][w][d] = y;
             }
         const float r = group_fold(rate, 64, seq::add), a = group_fold(gate, 64, seq::add);
-        if (lane == 0) g.sums[0][w][0] = r, g.sums[1][w][0] = a;
+        if (lane == 0) g.sums[0][w] = r, g.sums[1][w] = a;
         __syncthreads();
         if (tid < A.Dk) {
             const int d = tid;
@@ -853,213 +1227,28 @@ template <class E, int DK> __device__ __noinline__ void delta_grad_steps(const D
         if (tid == 0) {
             const float gt = s.gate()[t], bt = s.beta()[t];
             const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + t) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + t) * A.sb.ts + h * A.sb.hs];
-            const float sr = (g.sums[0][0][0] + g.sums[0][1][0]) + (g.sums[0][2][0] + g.sums[0][3][0]), sa = (g.sums[1][0][0] + g.sums[1][1][0]) + (g.sums[1][2][0] + g.sums[1][3][0]);
+            const float sr = (g.sums[0][0] + g.sums[0][1]) + (g.sums[0][2] + g.sums[0][3]), sa = (g.sums[1][0] + g.sums[1][1]) + (g.sums[1][2] + g.sums[1][3]);
             ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, t) || gt == 0.f ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
             ((E *)A.db)[bi * A.sdb.bs + (t0 + t) * A.sdb.ts + h * A.sdb.hs] = (E)(bt * (1.f / (1.f + expf(b))) * sr);
         }
         __syncthreads();
     }
 }
-
-// All gradients but the state's: a workgroup per tile and head.
-template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad(DeltaGradArgs A)
+template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad_steps(DeltaGradArgs A)
 {
-    using Op = Operand<E>;
-    using Tile = DeltaTile<E, DK>;
-    using Grad = DeltaGradTile<E, DK>;
-    constexpr int LO = Grad::LO, ND = (DK + 63) / 64;      // tiles of 16 of a wave's columns of dq and dk
     extern __shared__ __align__(16) unsigned char lds[];
-    Grad &g = *reinterpret_cast<Grad *>(lds);
-    Tile &s = g.s;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, grp = lane >> 4, col = lane & 15;
-    const long tile = blockIdx.x % A.tiles, head = blockIdx.x / A.tiles;
-    const int bi = (int)(head / A.H), h = (int)(head % A.H);
-    const long t0 = tile * CH;
-    const int rows = (int)min((long)CH, A.T - t0);
-    const float *S = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *Dn = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
-    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs, *dout = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs;
-    {
-        DeltaFetch<E, DK> fetch;
-        fetch.load(A, (const DeltaRecord *)A.records, head, tile);
-        fetch.put(s);
-    }
-    __syncthreads();
-    const float left = s.since()[CH - 1];
-    // dP and dN: wave 0 has rows and columns 0.., wave 1 rows 16.. of columns 0.., wave 2 rows and columns 16..
-    const int ti = w ? 16 : 0, tj = w == 2 ? 16 : 0;
-    f4 dp = {}, dn = {}, os[ND][2] = {}, ys[ND][2] = {}, ud[ND][2] = {}, yu[2] = {}, vv[2] = {};
-    float end = 0.f;
-    bool ok = true;
-    for (int sl = 0; sl < A.Dv; sl += COLS) {
-        const int c = sl + 16 * w + col;
-        const bool mine = c < A.Dv;
-        f4 out[2], u[2], y[2], val[2], kd[2];
-        get_steps(v + c, A.sv.ts, mine, rows, lane, val);
-        get_steps(dout + c, A.sdo.ts, mine, rows, lane, out);
-        {
-            Columns<DK> st, D;
-            st.get(S, A.Dk, A.Dv, c, lane);
-            D.get(Dn, A.Dk, A.Dv, c, lane);
-            typename Op::template Split<2> sp[DK / 32], dp2[DK / 32];
-#pragma unroll
-            for (int p = 0; p < DK / 32; ++p) {
-                sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
-                dp2[p] = split<E, 2>(D.s[2 * p], D.s[2 * p + 1]);
-            }
-            delta_u<E, DK, 2>(s, sp, val, rows, lane, u);
-            delta_y<E, DK, 2>(s, dp2, out, lane, kd, y);
-            if (left != 0.f)
-#pragma unroll
-                for (int n = 0; n < DK / 16; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) end = fmaf(left * st.s[n][e], D.s[n][e], end);
-        }
-        f4 dv[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            dv[m] = of_steps(s.beta(), m, lane) * y[m];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 8 * grp + 4 * m + e;
-                ok &= fabsf(dv[m][e]) < INFINITY && fabsf(u[m][e]) < INFINITY;
-                yu[m][e] = fmaf(y[m][e], u[m][e], yu[m][e]);
-                vv[m][e] = fmaf(dv[m][e], val[m][e], vv[m][e]);
-                end = fmaf(kd[m][e], u[m][e], end);
-                g.dout[i * LO + 16 * w + col] = (E)out[m][e];
-                g.u.put(i, 16 * w + col, u[m][e]);
-                g.y.put(i, 16 * w + col, y[m][e]);
-            }
-        }
-        put_steps((E *)A.dv + bi * A.sdv.bs + t0 * A.sdv.ts + h * A.sdv.hs + c, A.sdv.ts, mine, rows, lane, dv);
+    DeltaSteps<E, DK> &g = *reinterpret_cast<DeltaSteps<E, DK> *>(lds);
+    const long all = (long)A.B * A.H * A.tiles, first = (long)blockIdx.x * AGAIN, mine = first + (threadIdx.x & 63);
+    uint64_t left = __ballot(mine < all && A.again[min(mine, all - 1)]);      // the same for all waves
+    for (; left; left &= left - 1) {
+        const long id = first + __ffsll((unsigned long long)left) - 1, head = id / A.tiles, tile = id % A.tiles;
+        DeltaFetch<E, DK, 256> fetch;
+        fetch.begin(A, (const DeltaRecord *)A.records, head, (int)(head / A.H), (int)(head % A.H), threadIdx.x);
+        fetch.load(A, tile);
         __syncthreads();
-        if (w < 3) {
-#pragma unroll
-            for (int kb = 0; kb < COLS; kb += 32) {
-                const auto b = g.u.get(tj + col, kb + 8 * grp);
-                dp = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, dp);
-                dn = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, dn);
-            }
-        }
-        // columns 16 (w + 4 d).. of dO S^T, Y S^T and U D^T
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            const int dk = 16 * (w + 4 * d) + col;
-            if (16 * (w + 4 * d) >= DK) break;
-#pragma unroll
-            for (int kb = 0; kb < COLS; kb += 32) {
-                const auto st = state_row<E>(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, true), D = state_row<E>(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, true);
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    os[d][m] = Op::mul(eight(g.dout + (16 * m + col) * LO + kb + 8 * grp), st, os[d][m]);
-                    ys[d][m] = Op::mul(g.y.get(16 * m + col, kb + 8 * grp), st, ys[d][m]);
-                    ud[d][m] = Op::mul(g.u.get(16 * m + col, kb + 8 * grp), D, ud[d][m]);
-                }
-            }
-        }
+        fetch.put(g.s, A.Dk);
         __syncthreads();
-    }
-    if (w < 3) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = ti + 4 * grp + r, j = tj + col;
-            const float b = j <= i ? s.between(i, j) : 0.f;
-            const float x = b != 0.f ? A.scale * b * dp[r] : 0.f, z = b != 0.f && j < i ? -s.beta()[i] * b * dn[r] : 0.f;
-            g.dp.put(i, j, x);
-            g.dpt.put(j, i, x);
-            g.dn.put(i, j, z);
-            g.dnt.put(j, i, z);
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 4 * grp + r, j = 16 + col;      // above the diagonal
-            g.dp.put(i, j, 0.f);
-            g.dpt.put(j, i, 0.f);
-            g.dn.put(i, j, 0.f);
-            g.dnt.put(j, i, 0.f);
-        }
-    }
-    __syncthreads();
-    f4 qd[2] = {};
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-        if (16 * (w + 4 * d) >= DK) break;
-        // columns of K and Q, 32 steps deep, a natural column per lane: column 16 t + i of 32 p.. is dealt as half (i / 4) % 2
-        typename Op::Exact kc, qc;
-        {
-            const int n = w + 4 * d;
-            if constexpr (std::is_same<E, float>::value) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    kc[e] = s.k[(8 * grp + e) * Tile::LD + 16 * n + col];
-                    qc[e] = s.q[(8 * grp + e) * Tile::LD + 16 * n + col];
-                }
-            } else {
-                using s4 = vec<short, 4>;
-                typedef __attribute__((address_space(3))) s4 *At;
-                const int at = (8 * grp + (col >> 2)) * Tile::LD + 16 * n + 4 * (col & 3);
-                const s4 k0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.k + at)), k1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.k + at + 4 * Tile::LD));
-                const s4 q0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.q + at)), q1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(s.q + at + 4 * Tile::LD));
-                kc = __builtin_bit_cast(b8, (vec<short, 8>){k0[0], k0[1], k0[2], k0[3], k1[0], k1[1], k1[2], k1[3]});
-                qc = __builtin_bit_cast(b8, (vec<short, 8>){q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]});
-            }
-        }
-        const int dk = 16 * (w + 4 * d) + col;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f4 since = load<4>(s.since() + 16 * m + 4 * grp), beta = load<4>(s.beta() + 16 * m + 4 * grp), until = load<4>(s.until() + 16 * m + 4 * grp);
-            f4 x = where(since, A.scale * os[d][m]), z = where(since, -beta * ys[d][m]) + where(until, ud[d][m]);
-            x = Op::mul(g.dp.get(16 * m + col, 8 * grp), kc, x);
-            z = Op::mul(g.dpt.get(16 * m + col, 8 * grp), qc, z);
-            z = Op::mul(g.dn.get(16 * m + col, 8 * grp), kc, z);
-            z = Op::mul(g.dnt.get(16 * m + col, 8 * grp), kc, z);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 16 * m + 4 * grp + e;
-                ok &= fabsf(x[e]) < INFINITY && fabsf(z[e]) < INFINITY;
-                qd[m][e] = fmaf(x[e], (float)s.q[i * Tile::LD + dk], qd[m][e]);
-                if (dk < A.Dk && i < rows) {
-                    ((E *)A.dq)[bi * A.sdq.bs + (t0 + i) * A.sdq.ts + h * A.sdq.hs + dk] = (E)x[e];
-                    ((E *)A.dk)[bi * A.sdk.bs + (t0 + i) * A.sdk.ts + h * A.sdk.hs + dk] = (E)z[e];
-                }
-            }
-        }
-    }
-    ok &= fabsf(end) < INFINITY;
-    if (__syncthreads_or(!ok)) {
-        delta_grad_steps<E, DK>(A, g, head, tile, S, Dn);
-        return;
-    }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = group_fold(qd[m][e], 16, add), b = group_fold(yu[m][e], 16, add), d = group_fold(vv[m][e], 16, add);
-            if (col == 0) {
-                g.sums[0][w][16 * m + 4 * grp + e] = a;
-                g.sums[1][w][8 * grp + 4 * m + e] = b;
-                g.sums[2][w][8 * grp + 4 * m + e] = d;
-            }
-        }
-    end = group_fold(end, 64, add);
-    if (lane == 0) g.ends[w] = end;
-    __syncthreads();
-    if (tid < CH) {
-        const int i = tid, cut = s.cut()[i];
-        auto all = [&](int k) { return (g.sums[k][0][i] + g.sums[k][1][i]) + (g.sums[k][2][i] + g.sums[k][3][i]); };
-        float x = i < rows ? all(0) - all(2) : 0.f;
-        if (i == rows - 1) x += (g.ends[0] + g.ends[1]) + (g.ends[2] + g.ends[3]);
-#pragma unroll
-        for (int d = 1; d < CH; d *= 2) {
-            const float o = __shfl_down(x, d, CH);
-            const int oc = __shfl_down(cut, d, CH);
-            if (i + d < CH && oc == cut) x += o;
-        }
-        if (i < rows) {
-            const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
-            ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, i) || s.gate()[i] == 0.f ? 0.f : x * (1.f / (1.f + expf(f))));
-            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(all(1) * (1.f / (1.f + expf(b))));
-        }
+        delta_grad_steps<E, DK>(A, g, head, tile);
     }
 }
 

@@ -23,6 +23,7 @@ const char *check_heads(const void *p, const int64_t (&stride)[3], int64_t B, in
         if (d.second == 1) d.first = 0;
         else if (d.first < 0 || d.first > MOST || (d.first > 0 && d.second - 1 > MOST / d.first)) return "a stride is negative or too large";
     }
+    if (by[1].first > 1 << 24) return "a stride from step to step is above 2^24";      // 32 steps are within 2^32 bytes
     if (!written) return nullptr;
     std::sort(by, by + 3);
     int64_t extent = D;
@@ -87,19 +88,23 @@ template <class E, int DK> void launch_tiles(const seq::DeltaIn &A, float *recor
 template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, hipStream_t st)
 {
     static std::atomic<uint64_t> granted{0};
-    constexpr int bytes = 2 * sizeof(seq::DeltaTile<E, DK>);
+    constexpr int bytes = sizeof(seq::DeltaChain<E, DK>), waves = seq::DeltaChain<E, DK>::WAVES;
+    static_assert(bytes <= 160 * 1024, "within a compute unit's LDS");
     if (!lds_granted((const void *)seq::k_delta<E, DK>, bytes, granted)) return false;
     launch_tiles<E, DK>(A, A.records, st);
-    seq::k_delta<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + seq::COLS - 1) / seq::COLS))), 256, bytes, st>>>(A);
+    seq::k_delta<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, bytes, st>>>(A);
     return true;
 }
 template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, hipStream_t st)
 {
     static std::atomic<uint64_t> back_granted{0}, granted{0};
-    constexpr int back = 2 * sizeof(seq::DeltaTile<E, DK>), bytes = sizeof(seq::DeltaGradTile<E, DK>);
+    constexpr int back = sizeof(seq::DeltaChain<E, DK>), waves = seq::DeltaChain<E, DK>::WAVES, bytes = sizeof(seq::DeltaGradTile<E, DK>);
     if (!lds_granted((const void *)seq::k_delta_back<E, DK>, back, back_granted) || !lds_granted((const void *)seq::k_delta_grad<E, DK>, bytes, granted)) return false;
-    seq::k_delta_back<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + seq::COLS - 1) / seq::COLS))), 256, back, st>>>(A);
-    if (A.tiles) seq::k_delta_grad<E, DK><<<dim3((unsigned)(heads_of(A) * A.tiles)), 256, bytes, st>>>(A);
+    seq::k_delta_back<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, back, st>>>(A);
+    if (!A.tiles) return true;
+    static_assert(sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup gets");
+    seq::k_delta_grad<E, DK><<<dim3((unsigned)(heads_of(A) * A.tiles)), 256, bytes, st>>>(A);
+    seq::k_delta_grad_steps<E, DK><<<dim3((unsigned)((heads_of(A) * A.tiles + seq::AGAIN - 1) / seq::AGAIN)), 256, sizeof(seq::DeltaSteps<E, DK>), st>>>(A);
     return true;
 }
 size_t record_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * sizeof(seq::DeltaRecord); }
@@ -118,7 +123,7 @@ int32_t dqn_delta_sizes(int32_t dtype, int32_t B, int64_t T, int32_t H, int32_t 
     if (const char *m = check_sizes(s)) return bad(call, m);
     *carry = state_bytes(s) + record_bytes(s);
     *forward_workspace = record_bytes(s);
-    *backward_workspace = state_bytes(s);
+    *backward_workspace = state_bytes(s) + (size_t)B * H * tiles_of(T) * 4;
     return DQN_OK;
 }
 
@@ -175,7 +180,7 @@ int32_t dqn_delta_backward(const dqn_delta_grad_args *args, void *stream)
     A.dout = d.dout; A.sdo = strides(d.dout_s); A.states = d.carry; A.records = (const float *)((const uint8_t *)d.carry + state_bytes(s)); A.dlast = d.dlast;
     A.dq = d.dq; A.dk = d.dk; A.dv = d.dv; A.df = d.df; A.db = d.db;
     A.sdq = strides(d.dq_s); A.sdk = strides(d.dk_s); A.sdv = strides(d.dv_s); A.sdf = strides(d.df_s); A.sdb = strides(d.db_s);
-    A.ds0 = d.ds0; A.into = (float *)d.workspace;
+    A.ds0 = d.ds0; A.into = (float *)d.workspace; A.again = (int *)((uint8_t *)d.workspace + state_bytes(s));
     hipStream_t st = (hipStream_t)stream;
     const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta_grad<decltype(e), dk.value>(A, st); });
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");

@@ -52,7 +52,7 @@ def delta_grad_args(**kw):
 
 BOTH = [dict(dtype=2), dict(B=-1), dict(B=65536), dict(H=-1), dict(H=65536), dict(B=2000, H=2000), dict(Dk=0), dict(Dk=129), dict(Dv=0), dict(Dv=129), dict(T=-1),
         dict(T=1 << 40), dict(B=65535, H=16, T=1000), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(k=P + 2), dict(v=None), dict(f=P + 1), dict(b=None),
-        dict(q_s=(-1, 32, 8)), dict(k_s=(128, 1 << 60, 8)), dict(v_s=(128, 32, -8)), dict(f_s=(16, -4, 1)), dict(b_s=(1 << 60, 4, 1)),
+        dict(q_s=(-1, 32, 8)), dict(k_s=(128, 1 << 60, 8)), dict(v_s=(128, (1 << 24) + 1, 8)), dict(v_s=(128, 32, -8)), dict(f_s=(16, -4, 1)), dict(b_s=(1 << 60, 4, 1)),
         dict(reset=P, reset_ts=-1), dict(reset=P, reset_bs=1 << 60)]
 
 
