@@ -337,7 +337,7 @@ template <class T> __device__ __forceinline__ const T *plus(const T *p, uint32_t
 
 // The part of a tile that a thread of THREADS brings from memory: into registers first, so that it can arrive while another tile is worked on.
 template <class E, int DK, int THREADS> struct DeltaFetch {
-    static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + THREADS - 1) / THREADS, NR = CH * CH / 4 / THREADS;
+    static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + THREADS - 1) / THREADS, NR = (CH * CH / 4 + THREADS - 1) / THREADS;
     static_assert(7 * CH / 4 <= THREADS, "a thread brings one piece of the vectors");
     const E *qh, *kh;
     const DeltaRecord *records;
@@ -390,8 +390,9 @@ template <class E, int DK, int THREADS> struct DeltaFetch {
         const DeltaRecord *rec = records + tile;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            t[n] = seq::load<4>(rec->t + 4 * (tid + THREADS * n));
-            p[n] = seq::load<4>(rec->p + 4 * (tid + THREADS * n));
+            const int e = min(tid + THREADS * n, CH * CH / 4 - 1);
+            t[n] = seq::load<4>(rec->t + 4 * e);
+            p[n] = seq::load<4>(rec->p + 4 * e);
         }
         vectors = seq::load<4>(rec->since + 4 * min(tid, 7 * CH / 4 - 1));
     }
@@ -418,8 +419,10 @@ template <class E, int DK, int THREADS> struct DeltaFetch {
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             const int e = tid + THREADS * n, r = e / 8, c = e % 8 * 4;
-            seq::store<4>(s.t + r * Tile::LC + c, t[n]);
-            seq::store<4>(s.p + r * Tile::LC + c, p[n]);
+            if (CH * CH / 4 % THREADS == 0 || r < CH) {
+                seq::store<4>(s.t + r * Tile::LC + c, t[n]);
+                seq::store<4>(s.p + r * Tile::LC + c, p[n]);
+            }
         }
         if (tid < 7 * CH / 4) seq::store<4>(s.vectors + 4 * tid, vectors);
     }
@@ -524,33 +527,33 @@ template <int DK> struct Columns {
         if (!from) return clear();
         const int g = lane >> 4;
         const bool mine = c < Dv;
-        from += mine ? c : Dv - 1;
+        float x[DK / 16][4];
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 32 * (n >> 1) + 8 * g + 4 * (n & 1) + e;
-                const float x = from[(long)min(d, Dk - 1) * Dv];
-                s[n][e] = mine && d < Dk ? x : 0.f;
-            }
+            for (int e = 0; e < 4; ++e) x[n][e] = from[(uint32_t)(min(32 * (n >> 1) + 8 * g + 4 * (n & 1) + e, Dk - 1) * Dv + min(c, Dv - 1))];
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = mine && 32 * (n >> 1) + 8 * g + 4 * (n & 1) + e < Dk ? x[n][e] : 0.f;
     }
     __device__ __forceinline__ void put(float *to, int Dk, int Dv, int c, int lane) const
     {
         if (c >= Dv) return;
         const int g = lane >> 4;
-        to += (long)(8 * g) * Dv + c;
+        const uint32_t at = (uint32_t)(8 * g * Dv + c);
         if (Dk == DK) {
 #pragma unroll
             for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) to[(long)(32 * (n >> 1) + 4 * (n & 1) + e) * Dv] = s[n][e];
+                for (int e = 0; e < 4; ++e) (to + (32 * (n >> 1) + 4 * (n & 1) + e) * Dv)[at] = s[n][e];
         } else {
 #pragma unroll
             for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int d = 32 * (n >> 1) + 4 * (n & 1) + e;
-                    if (8 * g + d < Dk) to[(long)d * Dv] = s[n][e];
+                    if (8 * g + d < Dk) (to + d * Dv)[at] = s[n][e];
                 }
         }
     }
@@ -902,6 +905,7 @@ template <int R, int C> struct Matrix<float, R, C> {
     float m[R * LD];
     __device__ __forceinline__ void put(int i, int j, float v) { m[i * LD + j] = v; }
     __device__ __forceinline__ f8 get(int i, int j) const { return eight(m + i * LD + j); }
+    __device__ __forceinline__ float at(int i, int j) const { return m[i * LD + j]; }
     // columns j.. and 16 + j..
     __device__ __forceinline__ f8 pair(int i, int j) const { return both(load<4>(m + i * LD + j), load<4>(m + i * LD + j + 16)); }
 };
@@ -915,6 +919,7 @@ template <int R, int C> struct Matrix<bf16, R, C> {
         m[1][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(b >> 16));
     }
     __device__ __forceinline__ Planes<2> get(int i, int j) const { return Planes<2>{{eight(m[0] + i * LD + j), eight(m[1] + i * LD + j)}}; }
+    __device__ __forceinline__ float at(int i, int j) const { return (float)m[0][i * LD + j] + (float)m[1][i * LD + j]; }
     __device__ __forceinline__ Planes<2> pair(int i, int j) const
     {
         Planes<2> o;
@@ -932,15 +937,14 @@ template <class E, int DK> struct DeltaGradTile {
     E dout[CH * LO];
     Matrix<E, CH, COLS> u, y;
     Matrix<E, CH, CH> dp, dn, dpt, dnt;     // of P's and N's products, and transposed
-    float sums[3][4][CH];                   // of each wave and row: q.dq, Y.u, dv.v
-    float ends[4];                          // of each wave: <D, S'>
+    float qdq[DK / 16][CH], yu[4][CH], vdv[4][CH];      // sums over 16 columns each of q.dq, Y.u, dv.v
+    float ends[8];                          // of each wave: <D, S'>
 };
 
-// 8 numbers of a state's row d, columns c.., as right operand; quads: Dv is a multiple of 4
-template <class E> __device__ __forceinline__ typename Operand<E>::template Split<2> state_row(const float *S, int d, int c, int Dk, int Dv, bool quads)
+// 8 numbers of a state's row d, columns c..; quads: Dv is a multiple of 4
+__device__ __forceinline__ void state_row(const float *S, int d, int c, int Dk, int Dv, bool quads, float (&v)[8])
 {
-    float v[8];
-    const float *p = S + (long)min(d, Dk - 1) * Dv;
+    const float *p = S + (uint32_t)(min(d, Dk - 1) * Dv);
     if (quads) {
 #pragma unroll
         for (int e = 0; e < 8; e += 4) {
@@ -955,198 +959,197 @@ template <class E> __device__ __forceinline__ typename Operand<E>::template Spli
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = d < Dk && c + e < Dv ? x[e] : 0.f;
     }
-    return Operand<E>::template split<2>(v);
 }
 
-// All gradients but the state's: a workgroup per tile and head.
-template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad(DeltaGradArgs A)
+// All gradients but the state's: a workgroup of eight waves per tile and head.  Of each 64 columns of the state four waves form U, four Y; then
+// dP and dN; then the products over all columns, a wave having 16 of the columns of dq and dk for half of the steps (DK = 128: for all).
+template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs A)
 {
     using Op = Operand<E>;
     using Tile = DeltaTile<E, DK>;
     using Grad = DeltaGradTile<E, DK>;
-    constexpr int LO = Grad::LO, ND = (DK + 63) / 64;      // tiles of 16 of a wave's columns of dq and dk
+    constexpr int LO = Grad::LO, NM = DK == 128 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char lds[];
     Grad &g = *reinterpret_cast<Grad *>(lds);
     Tile &s = g.s;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, grp = lane >> 4, col = lane & 15;
-    const long tile = blockIdx.x % A.tiles, head = blockIdx.x / A.tiles;
-    const int bi = (int)(head / A.H), h = (int)(head % A.H);
-    const long t0 = tile * CH;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wc = w & 3, grp = lane >> 4, col = lane & 15;
+    const bool for_y = w >= 4;
+    const unsigned tile = blockIdx.x % (unsigned)A.tiles, head = blockIdx.x / (unsigned)A.tiles;
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H);
+    const long t0 = (long)tile * CH, size = (long)A.Dk * A.Dv;
     const int rows = (int)min((long)CH, A.T - t0);
-    const float *S = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *Dn = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
-    const E *v = (const E *)A.v + bi * A.sv.bs + t0 * A.sv.ts + h * A.sv.hs, *dout = (const E *)A.dout + bi * A.sdo.bs + t0 * A.sdo.ts + h * A.sdo.hs;
-    {
-        DeltaFetch<E, DK, 256> fetch;
-        fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, tid);
-        fetch.load(A, tile);
-        fetch.put(s, A.Dk);
-    }
-    __syncthreads();
-    const float left = s.since()[CH - 1];
-    const bool quads = A.Dv % 4 == 0;      // states are 16-byte aligned then
-    // dP and dN: wave 0 has rows and columns 0.., wave 1 rows 16.. of columns 0.., wave 2 rows and columns 16..
-    const int ti = w ? 16 : 0, tj = w == 2 ? 16 : 0;
-    f4 dp = {}, dn = {}, os[ND][2] = {}, ys[ND][2] = {}, ud[ND][2] = {}, yu[2] = {}, vv[2] = {};
-    float end = 0.f;
-    bool ok = true;
+    const float *S = A.states + ((long)head * A.tiles + tile) * size, *Dn = A.into + ((long)head * A.tiles + tile) * size;
+    const E *v = head_of<E>(A.v, A.sv, bi, h) + t0 * A.sv.ts, *dout = head_of<E>(A.dout, A.sdo, bi, h) + t0 * A.sdo.ts;
+    // the part of dP (waves 0..2) or dN (4..6): rows ti.., columns tj.., up to the diagonal
+    const int ti = wc ? 16 : 0, tj = wc == 2 ? 16 : 0;
+    // and of dq and dk: columns 16 d.., steps 16 m..
+    const int d = w % (DK / 16), m0 = NM == 2 ? 0 : w / (DK / 16), dk = 16 * d + col;
+    const bool has = m0 < 2, quads = A.Dv % 4 == 0;        // states are 16-byte aligned then
+    f4 part = {}, os[NM] = {}, ys[NM] = {}, ud[NM] = {};
+    float end = 0.f, wrong = 0.f;
+    DeltaFetch<E, DK, 512> fetch;
+    fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, tid);
+    fetch.load(A, tile);
     for (int sl = 0; sl < A.Dv; sl += COLS) {
-        const int c = sl + 16 * w + col;
+        const int c = sl + 16 * wc + col;
         const bool mine = c < A.Dv;
-        f4 out[2], u[2], y[2], val[2], kd[2], pd[2] = {};
-        {
-            Steps<E> vs, ds;
-            vs.rows = ds.rows = 0;
-            vs.load(v, (int)A.sv.ts, c, A.Dv, rows, lane);
-            ds.load(dout, (int)A.sdo.ts, c, A.Dv, rows, lane);
-            Columns<DK> st, D;
-            st.get(S, A.Dk, A.Dv, c, lane);
-            D.get(Dn, A.Dk, A.Dv, c, lane);
-            vs.get(mine, lane, val);
-            ds.get(mine, lane, out);
-            typename Op::template Split<2> sp[DK / 32], dp2[DK / 32];
+        Steps<E> vs, ds;
+        vs.rows = ds.rows = 0;
+        Columns<DK> st;
+        f4 val[2], kd[2], dv[2];
+        vs.load(v, (int)A.sv.ts, c, A.Dv, rows, lane);
+        if (for_y) ds.load(dout, (int)A.sdo.ts, c, A.Dv, rows, lane);
+        st.get(for_y ? Dn : S, A.Dk, A.Dv, c, lane);
+        if (sl == 0) fetch.put(s, A.Dk);
+        __syncthreads();        // and of the slice before all has been read
+        typename Op::template Split<2> sp[DK / 32];
 #pragma unroll
-            for (int p = 0; p < DK / 32; ++p) {
-                sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
-                dp2[p] = split<E, 2>(D.s[2 * p], D.s[2 * p + 1]);
-            }
+        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
+        vs.get(mine, lane, val);
+        if (!for_y) {
+            f4 u[2];
             delta_u<E, DK, 2>(s, sp, val, rows, lane, u);
+            wrong += nothing(u);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g.u.put(16 * m + 4 * grp + e, 16 * wc + col, u[m][e]);
+        } else {
+            f4 out[2], y[2], pd[2] = {};
+            ds.get(mine, lane, out);
             upper<Tile::LC>(s.p, out, lane, pd);
-            delta_y<E, DK, 2>(s, dp2, pd, lane, kd, y);
-            if (left != 0.f)
+            delta_y<E, DK, 2>(s, sp, pd, lane, kd, y);
 #pragma unroll
-                for (int n = 0; n < DK / 16; ++n)
+            for (int m = 0; m < 2; ++m) {
+                dv[m] = of_steps(s.beta(), m, lane) * y[m];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) end = fmaf(left * st.s[n][e], D.s[n][e], end);
-        }
-        f4 dv[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            dv[m] = of_steps(s.beta(), m, lane) * y[m];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 16 * m + 4 * grp + e;
-                ok &= fabsf(dv[m][e]) < INFINITY && fabsf(u[m][e]) < INFINITY;
-                yu[m][e] = fmaf(y[m][e], u[m][e], yu[m][e]);
-                vv[m][e] = fmaf(dv[m][e], val[m][e], vv[m][e]);
-                end = fmaf(kd[m][e], u[m][e], end);
-                g.dout[i * LO + 16 * w + col] = (E)out[m][e];
-                g.u.put(i, 16 * w + col, u[m][e]);
-                g.y.put(i, 16 * w + col, y[m][e]);
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * m + 4 * grp + e;
+                    g.dout[i * LO + 16 * wc + col] = (E)out[m][e];
+                    g.y.put(i, 16 * wc + col, y[m][e]);
+                }
             }
-        }
-        {
+            wrong += nothing(dv);
             Steps<E> to;
             to.offsets((int)A.sdv.ts, c, A.Dv, CH, lane);
             put_steps(head_of<E>(A.dv, A.sdv, bi, h) + t0 * A.sdv.ts, to, mine, rows, lane, dv);
         }
         __syncthreads();
-        if (w < 3) {
+        if (for_y) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * m + 4 * grp + e;
+                    const float u = g.u.at(i, 16 * wc + col);
+                    const float a = group_fold(g.y.at(i, 16 * wc + col) * u, 16, add), b = group_fold(dv[m][e] * val[m][e], 16, add);
+                    end = fmaf(kd[m][e], u, end);
+                    if (col == 0) {
+                        g.yu[wc][i] = sl ? g.yu[wc][i] + a : a;
+                        g.vdv[wc][i] = sl ? g.vdv[wc][i] + b : b;
+                    }
+                }
+        }
+        if (wc < 3) {
 #pragma unroll
             for (int kb = 0; kb < COLS; kb += 32) {
                 const auto b = g.u.get(tj + col, kb + 8 * grp);
-                dp = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, dp);
-                dn = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, dn);
+                if (!for_y) part = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, part);
+                else part = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, part);
             }
         }
-        // columns 16 (w + 4 d).. of dO S^T, Y S^T and U D^T
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            const int dk = 16 * (w + 4 * d) + col;
-            if (16 * (w + 4 * d) >= DK) break;
+        // columns 16 d.. of dO S^T, Y S^T and U D^T
+        if (has) {
 #pragma unroll
             for (int kb = 0; kb < COLS; kb += 32) {
-                const auto st = state_row<E>(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads), D = state_row<E>(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads);
+                float x[8], z[8];
+                state_row(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads, x);
+                state_row(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads, z);
+                if (m0 == 0 && s.since()[CH - 1] != 0.f)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    os[d][m] = Op::mul(eight(g.dout + (16 * m + col) * LO + kb + 8 * grp), st, os[d][m]);
-                    ys[d][m] = Op::mul(g.y.get(16 * m + col, kb + 8 * grp), st, ys[d][m]);
-                    ud[d][m] = Op::mul(g.u.get(16 * m + col, kb + 8 * grp), D, ud[d][m]);
+                    for (int e = 0; e < 8; ++e) end = fmaf(s.since()[CH - 1] * x[e], z[e], end);
+                const auto sr = Op::template split<2>(x), dr = Op::template split<2>(z);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) {
+                    const int i = 16 * (m0 + m) + col;
+                    os[m] = Op::mul(eight(g.dout + i * LO + kb + 8 * grp), sr, os[m]);
+                    ys[m] = Op::mul(g.y.get(i, kb + 8 * grp), sr, ys[m]);
+                    ud[m] = Op::mul(g.u.get(i, kb + 8 * grp), dr, ud[m]);
                 }
             }
         }
-        __syncthreads();
+        if (sl + COLS < A.Dv) __syncthreads();
     }
-    if (w < 3) {
+    if (wc < 3) {
+        auto &to = for_y ? g.dn : g.dp;
+        auto &tr = for_y ? g.dnt : g.dpt;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = ti + 4 * grp + r, j = tj + col;
             const float b = j <= i ? s.between(i, j) : 0.f;
-            const float x = b != 0.f ? A.scale * b * dp[r] : 0.f, z = b != 0.f && j < i ? -s.beta()[i] * b * dn[r] : 0.f;
-            g.dp.put(i, j, x);
-            g.dpt.put(j, i, x);
-            g.dn.put(i, j, z);
-            g.dnt.put(j, i, z);
+            const float x = b == 0.f ? 0.f : !for_y ? A.scale * b * part[r] : j < i ? -s.beta()[i] * b * part[r] : 0.f;
+            to.put(i, j, x);
+            tr.put(j, i, x);
         }
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 4 * grp + r, j = 16 + col;      // above the diagonal
-            g.dp.put(i, j, 0.f);
-            g.dpt.put(j, i, 0.f);
-            g.dn.put(i, j, 0.f);
-            g.dnt.put(j, i, 0.f);
+        for (int r = 0; r < 4; ++r) {       // above the diagonal
+            (for_y ? g.dn : g.dp).put(4 * grp + r, 16 + col, 0.f);
+            (for_y ? g.dnt : g.dpt).put(16 + col, 4 * grp + r, 0.f);
         }
     }
     __syncthreads();
-    f4 qd[2] = {};
+    if (has) {
+        const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * d, lane), qc = columns_of<1, Tile::LD>(s.q + 16 * d, lane);
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-        if (16 * (w + 4 * d) >= DK) break;
-        const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * (w + 4 * d), lane), qc = columns_of<1, Tile::LD>(s.q + 16 * (w + 4 * d), lane);
-        const int dk = 16 * (w + 4 * d) + col;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f4 since = load<4>(s.since() + 16 * m + 4 * grp), beta = load<4>(s.beta() + 16 * m + 4 * grp), until = load<4>(s.until() + 16 * m + 4 * grp);
-            f4 x = where(since, A.scale * os[d][m]), z = where(since, -beta * ys[d][m]) + where(until, ud[d][m]);
-            x = Op::mul(g.dp.pair(16 * m + col, 4 * grp), kc, x);
-            z = Op::mul(g.dpt.pair(16 * m + col, 4 * grp), qc, z);
-            z = Op::mul(g.dn.pair(16 * m + col, 4 * grp), kc, z);
-            z = Op::mul(g.dnt.pair(16 * m + col, 4 * grp), kc, z);
+        for (int n = 0; n < NM; ++n) {
+            const int m = m0 + n, i0 = 16 * m + col;
+            const f4 since = of_steps(s.since(), m, lane), beta = of_steps(s.beta(), m, lane), until = of_steps(s.until(), m, lane);
+            f4 x[2] = {where(since, A.scale * os[n]), where(since, -beta * ys[n]) + where(until, ud[n])};
+            x[0] = Op::mul(g.dp.pair(i0, 4 * grp), kc, x[0]);
+            x[1] = Op::mul(g.dpt.pair(i0, 4 * grp), qc, x[1]);
+            x[1] = Op::mul(g.dn.pair(i0, 4 * grp), kc, x[1]);
+            x[1] = Op::mul(g.dnt.pair(i0, 4 * grp), kc, x[1]);
+            wrong += nothing(x);
+            E *dq = head_of<E>(A.dq, A.sdq, bi, h) + t0 * A.sdq.ts, *dkp = head_of<E>(A.dk, A.sdk, bi, h) + t0 * A.sdk.ts;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = 16 * m + 4 * grp + e;
-                ok &= fabsf(x[e]) < INFINITY && fabsf(z[e]) < INFINITY;
-                qd[m][e] = fmaf(x[e], (float)s.q[i * Tile::LD + dk], qd[m][e]);
                 if (dk < A.Dk && i < rows) {
-                    ((E *)A.dq)[bi * A.sdq.bs + (t0 + i) * A.sdq.ts + h * A.sdq.hs + dk] = (E)x[e];
-                    ((E *)A.dk)[bi * A.sdk.bs + (t0 + i) * A.sdk.ts + h * A.sdk.hs + dk] = (E)z[e];
+                    dq[(uint32_t)(i * (int)A.sdq.ts + dk)] = (E)x[0][e];
+                    dkp[(uint32_t)(i * (int)A.sdk.ts + dk)] = (E)x[1][e];
                 }
+                const float sum = group_fold(x[0][e] * (float)s.q[i * Tile::LD + dk], 16, add);
+                if (col == 0) g.qdq[d][i] = sum;
             }
         }
     }
-    ok &= fabsf(end) < INFINITY;
-    const bool again = __syncthreads_or(!ok);
-    if (tid == 0) A.again[head * A.tiles + tile] = again;
-    if (again) return;                  // k_delta_grad_steps's
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = group_fold(qd[m][e], 16, add), b = group_fold(yu[m][e], 16, add), d = group_fold(vv[m][e], 16, add);
-            if (col == 0) {
-                g.sums[0][w][16 * m + 4 * grp + e] = a;
-                g.sums[1][w][16 * m + 4 * grp + e] = b;
-                g.sums[2][w][16 * m + 4 * grp + e] = d;
-            }
-        }
     end = group_fold(end, 64, add);
+    wrong = wrong + end * 0.f;
     if (lane == 0) g.ends[w] = end;
-    __syncthreads();
+    const bool again = __syncthreads_or(wrong != 0.f);
+    if (tid == 0) A.again[(long)head * A.tiles + tile] = again;
+    if (again) return;                  // k_delta_grad_steps's
     if (tid < CH) {
         const int i = tid, cut = s.cut()[i];
-        auto all = [&](int k) { return (g.sums[k][0][i] + g.sums[k][1][i]) + (g.sums[k][2][i] + g.sums[k][3][i]); };
-        float x = i < rows ? all(0) - all(2) : 0.f;
-        if (i == rows - 1) x += (g.ends[0] + g.ends[1]) + (g.ends[2] + g.ends[3]);
+        float x = 0.f;
 #pragma unroll
-        for (int d = 1; d < CH; d *= 2) {
-            const float o = __shfl_down(x, d, CH);
-            const int oc = __shfl_down(cut, d, CH);
-            if (i + d < CH && oc == cut) x += o;
+        for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][i];
+        x = i < rows ? x - ((g.vdv[0][i] + g.vdv[1][i]) + (g.vdv[2][i] + g.vdv[3][i])) : 0.f;
+        if (i == rows - 1)
+#pragma unroll
+            for (int n = 0; n < 8; ++n) x += g.ends[n];
+#pragma unroll
+        for (int n = 1; n < CH; n *= 2) {
+            const float o = __shfl_down(x, n, CH);
+            const int oc = __shfl_down(cut, n, CH);
+            if (i + n < CH && oc == cut) x += o;
         }
         if (i < rows) {
             const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
+            const float rate = (g.yu[0][i] + g.yu[1][i]) + (g.yu[2][i] + g.yu[3][i]);
             ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, i) || s.gate()[i] == 0.f ? 0.f : x * (1.f / (1.f + expf(f))));
-            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(all(1) * (1.f / (1.f + expf(b))));
+            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(rate * (1.f / (1.f + expf(b))));
         }
     }
 }

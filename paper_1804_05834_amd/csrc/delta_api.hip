@@ -103,7 +103,7 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, h
     seq::k_delta_back<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, back, st>>>(A);
     if (!A.tiles) return true;
     static_assert(sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup gets");
-    seq::k_delta_grad<E, DK><<<dim3((unsigned)(heads_of(A) * A.tiles)), 256, bytes, st>>>(A);
+    seq::k_delta_grad<E, DK><<<dim3((unsigned)(heads_of(A) * A.tiles)), 512, bytes, st>>>(A);
     seq::k_delta_grad_steps<E, DK><<<dim3((unsigned)((heads_of(A) * A.tiles + seq::AGAIN - 1) / seq::AGAIN)), 256, sizeof(seq::DeltaSteps<E, DK>), st>>>(A);
     return true;
 }
