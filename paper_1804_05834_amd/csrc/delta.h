@@ -30,7 +30,7 @@ namespace seq {
 
 constexpr int CH = 32;                 // steps of a tile
 constexpr int COLS = 64;               // columns of the state of a workgroup, 16 of each wave
-constexpr float LOG_LEAST = -150.f;    // exp of it is 0 in fp32: a gate that closes further counts as this, so that differences of sums stay finite
+constexpr float LOG_LEAST = -216.f;    // of a gate, base 2; 2 to it is 0 in fp32: a gate that closes further counts as this, so that differences of sums stay finite
 
 using f4 = vec<float, 4>;
 using f8 = vec<float, 8>;
@@ -54,7 +54,7 @@ struct DeltaArgs : DeltaIn {
     const float *s0;
     void *o;
     Strides so;
-    float *last, *states, *records;    // states: the one that enters each tile, [B][H][tiles][Dk][Dv], or NULL
+    float *last, *states, *records;    // states: the one that enters each tile, as waves hold it (Columns), or NULL
 };
 struct DeltaGradArgs : DeltaIn {
     const void *dout;
@@ -72,7 +72,7 @@ struct DeltaRecord {
     float t[CH * CH], p[CH * CH];
     float since[CH], until[CH], beta[CH];   // g_i, 0 behind an episode's start; G_Ci, 0 before one
     float gate[CH];                    // a
-    float run_hi[CH], run_lo[CH];      // sum of log a up to each step, as a multiple of 2^-10 and the rest
+    float run_hi[CH], run_lo[CH];      // sum of log a, base 2, up to each step, as a multiple of 2^-10 and the rest
     int cut[CH];                       // episodes that have started up to each step
 };
 static_assert(sizeof(DeltaRecord) % 16 == 0, "records are copied 16 bytes at a time");
@@ -195,6 +195,11 @@ template <class E> __device__ __forceinline__ vec<E, 8> load8(const E *p, int c,
 
 __device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
+__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
+// The factor from step j to step i >= j of an episode: differences of the multiples of 2^-10 are exact, so that a gate that closed long before
+// leaves no rounding in later ones.
+__device__ __forceinline__ float between(float hi_i, float lo_i, float hi_j, float lo_j) { return power((hi_i - hi_j) + (lo_i - lo_j)); }
+
 // ---------------------------------------------------------------- T, P and the gates of every tile
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(DeltaIn A, DeltaRecord *records)
 {
@@ -225,17 +230,15 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
     {   // both halves of the wave do the same
         const int i = lane & 31;
         const bool in = i < rows;
-        float la = 0.f, beta = 0.f;
-        int cut = 0;
-        if (in) {
-            const long t = t0 + i;
-            const float f = (float)((const E *)A.f)[bi * A.sf.bs + t * A.sf.ts + h * A.sf.hs];
-            const float b = (float)((const E *)A.b)[bi * A.sb.bs + t * A.sb.ts + h * A.sb.hs];
-            la = (f < 0.f ? f : 0.f) - log1pf(expf(-fabsf(f)));
-            la = la < LOG_LEAST ? LOG_LEAST : la;
-            beta = 1.f / (1.f + expf(-b));
-            cut = A.reset && A.reset[bi * A.reset_bs + t * A.reset_ts];
-        }
+        const long t = t0 + min(i, rows - 1);
+        const float f = (float)((const E *)A.f)[bi * A.sf.bs + t * A.sf.ts + h * A.sf.hs];
+        const float b = (float)((const E *)A.b)[bi * A.sb.bs + t * A.sb.ts + h * A.sb.hs];
+        const int start = A.reset ? A.reset[bi * A.reset_bs + t * A.reset_ts] : 0;
+        double la = ((double)(f < 0.f ? f : 0.f) - (double)log1pf(expf(-fabsf(f)))) * 1.4426950408889634;
+        la = la < LOG_LEAST ? LOG_LEAST : la;
+        la = in ? la : 0.0;
+        const float beta = in ? 1.f / (1.f + expf(-b)) : 0.f;
+        const int cut = in && start ? 1 : 0;
         double run = la;
         int cuts = cut;
 #pragma unroll
@@ -251,16 +254,21 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
             s.run_lo[i] = out.run_lo[i] = (float)(run - whole);
             s.cut[i] = out.cut[i] = cuts;
             s.beta[i] = out.beta[i] = beta;
-            out.gate[i] = expf(la);
-            out.since[i] = cuts ? 0.f : expf((float)run);
-            out.until[i] = in && cuts == last ? expf((float)(end - run)) : 0.f;
+            out.gate[i] = power((float)la);
+            out.since[i] = cuts ? 0.f : power((float)run);
+            out.until[i] = in && cuts == last ? power((float)(end - run)) : 0.f;
         }
     }
     wave_sync();
-    // The factor from step j to step i >= j: differences of the multiples of 2^-10 are exact, so that a gate that closed long before
-    // leaves no rounding in later ones.
+    int cut_j[2];
+    float hi_j[2], lo_j[2];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int n = 0; n < 2; ++n) cut_j[n] = s.cut[16 * n + col], hi_j[n] = s.run_hi[16 * n + col], lo_j[n] = s.run_lo[16 * n + col];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const vec<int, 4> cut_i = load<4>(s.cut + 16 * m + 4 * g);
+        const f4 hi_i = load<4>(s.run_hi + 16 * m + 4 * g), lo_i = load<4>(s.run_lo + 16 * m + 4 * g), beta = load<4>(s.beta + 16 * m + 4 * g);
+        float *p = out.p + (16 * m + 4 * g) * CH + col;
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             f4 kk = {}, qk = {};
@@ -273,11 +281,12 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = 16 * m + 4 * g + r, j = 16 * n + col;
-                const float b = j <= i && s.cut[i] == s.cut[j] ? expf((s.run_hi[i] - s.run_hi[j]) + (s.run_lo[i] - s.run_lo[j])) : 0.f;
-                if (n <= m) s.n[i * LN + j] = j < i && b != 0.f ? -s.beta[i] * b * kk[r] : 0.f;
-                out.p[i * CH + j] = b != 0.f ? A.scale * b * qk[r] : 0.f;
+                const float b = n > m || j > i || cut_i[r] != cut_j[n] ? 0.f : between(hi_i[r], lo_i[r], hi_j[n], lo_j[n]);
+                if (n <= m) s.n[i * LN + j] = j < i && b != 0.f ? -beta[r] * b * kk[r] : 0.f;
+                p[r * CH + 16 * n] = b != 0.f ? A.scale * b * qk[r] : 0.f;
             }
         }
+    }
     wave_sync();
     // (I + N)^-1 of the two blocks on the diagonal by forward substitution, a column per lane, in their places
     if (lane < 32) {
@@ -323,10 +332,6 @@ template <class E, int DK> struct DeltaTile {
     __device__ __forceinline__ const float *run_hi() const { return vectors + 4 * CH; }
     __device__ __forceinline__ const float *run_lo() const { return vectors + 5 * CH; }
     __device__ __forceinline__ const int *cut() const { return reinterpret_cast<const int *>(vectors + 6 * CH); }
-    __device__ __forceinline__ float between(int i, int j) const
-    {
-        return cut()[i] == cut()[j] ? expf((run_hi()[i] - run_hi()[j]) + (run_lo()[i] - run_lo()[j])) : 0.f;
-    }
 };
 
 // Where a head's tensors begin, for all lanes alike, and 32-bit offsets from there: a stride from step to step is at most 2^24 elements.
@@ -519,43 +524,44 @@ __device__ __forceinline__ float groups_sum(float x)
     return lo + hi;
 }
 
-// A wave's columns of a state: state[2 p + half][r] is row 32 p + 8 (l / 16) + 4 half + r, column c.
+__device__ __forceinline__ int blocks_of(int Dv) { return (Dv + 15) / 16; }
+// A wave's 16 columns of a state: s[2 p + half][r] is row 32 p + 8 (l / 16) + 4 half + r, column l % 16; zeros from Dk and Dv on.
 template <int DK> struct Columns {
     f4 s[DK / 16];
+    // from and to a caller's state [Dk][Dv]
     __device__ __forceinline__ void get(const float *from, int Dk, int Dv, int c, int lane)
     {
         if (!from) return clear();
-        const int g = lane >> 4;
-        const bool mine = c < Dv;
         float x[DK / 16][4];
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[n][e] = from[(uint32_t)(min(32 * (n >> 1) + 8 * g + 4 * (n & 1) + e, Dk - 1) * Dv + min(c, Dv - 1))];
+            for (int e = 0; e < 4; ++e) x[n][e] = from[(uint32_t)(min(32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e, Dk - 1) * Dv + min(c, Dv - 1))];
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = mine && 32 * (n >> 1) + 8 * g + 4 * (n & 1) + e < Dk ? x[n][e] : 0.f;
+            for (int e = 0; e < 4; ++e) s[n][e] = c < Dv && 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e < Dk ? x[n][e] : 0.f;
     }
     __device__ __forceinline__ void put(float *to, int Dk, int Dv, int c, int lane) const
     {
-        if (c >= Dv) return;
-        const int g = lane >> 4;
-        const uint32_t at = (uint32_t)(8 * g * Dv + c);
-        if (Dk == DK) {
 #pragma unroll
-            for (int n = 0; n < DK / 16; ++n)
+        for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) (to + (32 * (n >> 1) + 4 * (n & 1) + e) * Dv)[at] = s[n][e];
-        } else {
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e;
+                if (c < Dv && d < Dk) to[(uint32_t)(d * Dv + c)] = s[n][e];
+            }
+    }
+    // from and to a state of the kernels' own: block after block of 16 columns, 16 bytes a lane
+    __device__ __forceinline__ void load(const float *block, int lane)
+    {
 #pragma unroll
-            for (int n = 0; n < DK / 16; ++n)
+        for (int n = 0; n < DK / 16; ++n) s[n] = seq::load<4>(block + 256 * n + 4 * lane);
+    }
+    __device__ __forceinline__ void store(float *block, int lane) const
+    {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = 32 * (n >> 1) + 4 * (n & 1) + e;
-                    if (8 * g + d < Dk) (to + d * Dv)[at] = s[n][e];
-                }
-        }
+        for (int n = 0; n < DK / 16; ++n) seq::store<4>(block + 256 * n + 4 * lane, s[n]);
     }
     // sum over rows of x_d S_dc, x a step's row of K or Q in LDS
     template <class E> __device__ __forceinline__ float dot(const E *x, int lane) const
@@ -613,7 +619,7 @@ template <class E, int DK> __device__ __forceinline__ void delta_pass_back(const
     else D.scaled(s.gate()[i]);
 }
 
-// A lane's numbers of a column of a tensor of steps [..][Dv] (V, dO, O): where they lie, and as they are loaded
+// A lane's numbers of a column of a tensor of steps [..][Dv] (V, dO): where they lie, and as they are loaded
 template <class E> struct Steps {
     uint32_t at[8];
     int rows;
@@ -636,16 +642,17 @@ template <class E> struct Steps {
         for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = mine && 16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) < rows ? (float)x[i] : 0.f;
     }
 };
-template <class E> __device__ __forceinline__ void put_steps(E *tile, const Steps<E> &s, bool mine, int rows, int lane, const f4 (&v)[2])
+template <class E> __device__ __forceinline__ void put_steps(E *tile, int ts, int c, bool mine, int rows, int lane, const f4 (&v)[2])
 {
     if (!mine) return;
+    const uint32_t at = (uint32_t)(4 * (lane >> 4) * ts + c);
     if (rows == CH) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *plus(tile, s.at[i]) = (E)v[i >> 2][i & 3];
+        for (int i = 0; i < 8; ++i) (tile + (16 * (i >> 2) + (i & 3)) * (long)ts)[at] = (E)v[i >> 2][i & 3];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) < rows) *plus(tile, s.at[i]) = (E)v[i >> 2][i & 3];
+            if (16 * (i >> 2) + 4 * (lane >> 4) + (i & 3) < rows) (tile + (16 * (i >> 2) + (i & 3)) * (long)ts)[at] = (E)v[i >> 2][i & 3];
     }
 }
 
@@ -715,7 +722,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
     const bool chain = threadIdx.x < 64 * WAVES;
     const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
     const unsigned head = blockIdx.x / slices;
-    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), c = 16 * (WAVES * slice + w) + (lane & 15);
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), block = WAVES * slice + w, blocks = blocks_of(A.Dv), c = 16 * block + (lane & 15);
     const bool mine = c < A.Dv;
     const long size = (long)A.Dk * A.Dv;
     const E *v = head_of<E>(A.v, A.sv, bi, h);
@@ -759,8 +766,6 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
     } else {
         DeltaFetch<E, DK, 64 * WAVES> fetch;
         E *o = head_of<E>(A.o, A.so, bi, h);
-        Steps<E> os;
-        os.offsets((int)A.so.ts, c, A.Dv, CH, lane);
         if (A.tiles) {
             fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, threadIdx.x - 64 * WAVES);
             fetch.load(A, 0);
@@ -781,7 +786,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
                 for (int n = 0; n < DK / 16; ++n) S.s[n] = L.state[tile & 1][w][n][lane];
                 u[0] = L.steps[tile & 1][w][0][lane];
                 u[1] = L.steps[tile & 1][w][1][lane];
-                if (A.states) S.put(A.states + (head * A.tiles + tile) * size, A.Dk, A.Dv, c, lane);
+                if (A.states && block < blocks) S.store(A.states + ((head * A.tiles + tile) * blocks + block) * 16 * DK, lane);
                 typename Operand<E>::template Split<2> sp[DK / 32];      // o is rounded to bf16: 16 bits of the state do
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(S.s[2 * p], S.s[2 * p + 1]);
@@ -800,7 +805,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
                         const float x = A.scale * S.dot(s.q + t * Tile::LD, lane);
                         if (mine && lane < 16) to[t * A.so.ts + c] = (E)x;
                     }
-                } else put_steps(to, os, mine, rows, lane, out);
+                } else put_steps(to, (int)A.so.ts, c, mine, rows, lane, out);
             }
             lds_barrier();
         }
@@ -819,7 +824,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
     const bool chain = threadIdx.x < 64 * WAVES;
     const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
     const unsigned head = blockIdx.x / slices;
-    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), c = 16 * (WAVES * slice + w) + (lane & 15);
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), block = WAVES * slice + w, blocks = blocks_of(A.Dv), c = 16 * block + (lane & 15);
     const bool mine = c < A.Dv;
     const long size = (long)A.Dk * A.Dv;
     const E *dout = head_of<E>(A.dout, A.sdo, bi, h);
@@ -833,7 +838,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
             if (i > 0) {
                 const long tile = A.tiles - i;
                 const Tile &s = L.tiles[tile % 3];
-                D.put(A.into + (head * A.tiles + tile) * size, A.Dk, A.Dv, c, lane);
+                if (block < blocks) D.store(A.into + ((head * A.tiles + tile) * blocks + block) * 16 * DK, lane);
                 typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(D.s[2 * p], D.s[2 * p + 1]);
@@ -936,34 +941,17 @@ template <class E, int DK> struct DeltaGradTile {
     DeltaTile<E, DK> s;
     E dout[CH * LO];
     Matrix<E, CH, COLS> u, y;
+    Matrix<E, DK, COLS> state, back;        // the state that enters, the gradient of the one that leaves
     Matrix<E, CH, CH> dp, dn, dpt, dnt;     // of P's and N's products, and transposed
     float qdq[DK / 16][CH], yu[4][CH], vdv[4][CH];      // sums over 16 columns each of q.dq, Y.u, dv.v
     float ends[8];                          // of each wave: <D, S'>
+    int wrong[8];                           // whether it has met a number that is not finite
 };
 
-// 8 numbers of a state's row d, columns c..; quads: Dv is a multiple of 4
-__device__ __forceinline__ void state_row(const float *S, int d, int c, int Dk, int Dv, bool quads, float (&v)[8])
-{
-    const float *p = S + (uint32_t)(min(d, Dk - 1) * Dv);
-    if (quads) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-            const f4 x = load<4>(p + min(c + e, Dv - 4));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[e + i] = d < Dk && c + e < Dv ? x[i] : 0.f;
-        }
-    } else {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = p[min(c + e, Dv - 1)];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = d < Dk && c + e < Dv ? x[e] : 0.f;
-    }
-}
-
-// All gradients but the state's: a workgroup of eight waves per tile and head.  Of each 64 columns of the state four waves form U, four Y; then
-// dP and dN; then the products over all columns, a wave having 16 of the columns of dq and dk for half of the steps (DK = 128: for all).
-template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs A)
+// All gradients but the state's: workgroups of eight waves, `per` tiles each, one after the other, a tile's loads under way while the one before
+// is worked on.  Of each 64 columns of the state four waves form U, four Y; then dP and dN; then the products over all columns, a wave having 16 of
+// the columns of dq and dk for half of the steps (DK = 128: for all).
+template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs A, int per)
 {
     using Op = Operand<E>;
     using Tile = DeltaTile<E, DK>;
@@ -974,182 +962,231 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
     Tile &s = g.s;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wc = w & 3, grp = lane >> 4, col = lane & 15;
     const bool for_y = w >= 4;
-    const unsigned tile = blockIdx.x % (unsigned)A.tiles, head = blockIdx.x / (unsigned)A.tiles;
-    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H);
-    const long t0 = (long)tile * CH, size = (long)A.Dk * A.Dv;
-    const int rows = (int)min((long)CH, A.T - t0);
-    const float *S = A.states + ((long)head * A.tiles + tile) * size, *Dn = A.into + ((long)head * A.tiles + tile) * size;
-    const E *v = head_of<E>(A.v, A.sv, bi, h) + t0 * A.sv.ts, *dout = head_of<E>(A.dout, A.sdo, bi, h) + t0 * A.sdo.ts;
+    const unsigned all = (unsigned)(A.B * A.H * A.tiles), tiles = (unsigned)A.tiles;
+    unsigned id = blockIdx.x * (unsigned)per;
+    const unsigned stop = min(all, id + (unsigned)per);
+    const int blocks = blocks_of(A.Dv);
     // the part of dP (waves 0..2) or dN (4..6): rows ti.., columns tj.., up to the diagonal
     const int ti = wc ? 16 : 0, tj = wc == 2 ? 16 : 0;
     // and of dq and dk: columns 16 d.., steps 16 m..
     const int d = w % (DK / 16), m0 = NM == 2 ? 0 : w / (DK / 16), dk = 16 * d + col;
-    const bool has = m0 < 2, quads = A.Dv % 4 == 0;        // states are 16-byte aligned then
-    f4 part = {}, os[NM] = {}, ys[NM] = {}, ud[NM] = {};
-    float end = 0.f, wrong = 0.f;
+    const bool has = m0 < 2;
+    // what is under way: a tile, and of 64 columns V and the state that enters, or dO and the gradient of the one that leaves
     DeltaFetch<E, DK, 512> fetch;
-    fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, tid);
-    fetch.load(A, tile);
-    for (int sl = 0; sl < A.Dv; sl += COLS) {
-        const int c = sl + 16 * wc + col;
-        const bool mine = c < A.Dv;
-        Steps<E> vs, ds;
-        vs.rows = ds.rows = 0;
-        Columns<DK> st;
-        f4 val[2], kd[2], dv[2];
-        vs.load(v, (int)A.sv.ts, c, A.Dv, rows, lane);
-        if (for_y) ds.load(dout, (int)A.sdo.ts, c, A.Dv, rows, lane);
-        st.get(for_y ? Dn : S, A.Dk, A.Dv, c, lane);
-        if (sl == 0) fetch.put(s, A.Dk);
-        __syncthreads();        // and of the slice before all has been read
-        typename Op::template Split<2> sp[DK / 32];
-#pragma unroll
-        for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
-        vs.get(mine, lane, val);
-        if (!for_y) {
-            f4 u[2];
-            delta_u<E, DK, 2>(s, sp, val, rows, lane, u);
-            wrong += nothing(u);
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) g.u.put(16 * m + 4 * grp + e, 16 * wc + col, u[m][e]);
-        } else {
-            f4 out[2], y[2], pd[2] = {};
-            ds.get(mine, lane, out);
-            upper<Tile::LC>(s.p, out, lane, pd);
-            delta_y<E, DK, 2>(s, sp, pd, lane, kd, y);
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                dv[m] = of_steps(s.beta(), m, lane) * y[m];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + 4 * grp + e;
-                    g.dout[i * LO + 16 * wc + col] = (E)out[m][e];
-                    g.y.put(i, 16 * wc + col, y[m][e]);
-                }
-            }
-            wrong += nothing(dv);
-            Steps<E> to;
-            to.offsets((int)A.sdv.ts, c, A.Dv, CH, lane);
-            put_steps(head_of<E>(A.dv, A.sdv, bi, h) + t0 * A.sdv.ts, to, mine, rows, lane, dv);
+    Steps<E> in;
+    Columns<DK> st;
+    const E *steps = nullptr;
+    const long ts = for_y ? A.sdo.ts : A.sv.ts;
+    const float *states = for_y ? A.into : A.states;
+    in.rows = 0;
+    auto get = [&](unsigned which, int sl, bool new_head) {
+        const unsigned head = which / tiles, tile = which % tiles;
+        const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), rows = (int)min((long)CH, A.T - (long)tile * CH), c = sl + 16 * wc + col;
+        if (new_head) {
+            fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, tid);
+            steps = for_y ? head_of<E>(A.dout, A.sdo, bi, h) : head_of<E>(A.v, A.sv, bi, h);
         }
-        __syncthreads();
-        if (for_y) {
+        if (sl == 0) fetch.load(A, tile);
+        if (A.Dv > COLS) in.rows = 0;      // other columns
+        in.load(steps + (long)tile * CH * ts, (int)ts, c, A.Dv, rows, lane);
+        st.load(states + ((long)which * blocks + min(sl / 16 + wc, blocks - 1)) * 16 * DK, lane);
+    };
+    if (id < stop) get(id, 0, true);
+    for (; id < stop; ++id) {
+        const unsigned head = id / tiles, tile = id % tiles;
+        const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H);
+        const long t0 = (long)tile * CH;
+        const int rows = (int)min((long)CH, A.T - t0);
+        f4 part = {}, os[NM] = {}, ys[NM] = {}, ud[NM] = {};
+        float end = 0.f, wrong = 0.f;
+        for (int sl = 0; sl < A.Dv; sl += COLS) {
+            const int c = sl + 16 * wc + col;
+            const bool mine = c < A.Dv;
+            f4 val[2], res[2];         // V and U, or dO and kd
+            if (sl) lds_barrier();     // of the columns before all has been read
+            if (sl == 0) fetch.put(s, A.Dk);
+            in.get(mine, lane, val);
+            if (sl / 16 + wc >= blocks) st.clear();
+            {
+                auto &to = for_y ? g.back : g.state;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int n = 0; n < DK / 16; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * m + 4 * grp + e;
-                    const float u = g.u.at(i, 16 * wc + col);
-                    const float a = group_fold(g.y.at(i, 16 * wc + col) * u, 16, add), b = group_fold(dv[m][e] * val[m][e], 16, add);
-                    end = fmaf(kd[m][e], u, end);
-                    if (col == 0) {
-                        g.yu[wc][i] = sl ? g.yu[wc][i] + a : a;
-                        g.vdv[wc][i] = sl ? g.vdv[wc][i] + b : b;
+                    for (int e = 0; e < 4; ++e) to.put(32 * (n >> 1) + 8 * grp + 4 * (n & 1) + e, 16 * wc + col, st.s[n][e]);
+            }
+            typename Op::template Split<2> sp[DK / 32];
+#pragma unroll
+            for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
+            lds_barrier();
+            if (!for_y) {
+                delta_u<E, DK, 2>(s, sp, val, rows, lane, res);
+                wrong += nothing(res);
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) g.u.put(16 * m + 4 * grp + e, 16 * wc + col, res[m][e]);
+            } else {
+                f4 y[2], dv[2], pd[2] = {};
+                upper<Tile::LC>(s.p, val, lane, pd);
+                delta_y<E, DK, 2>(s, sp, pd, lane, res, y);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    dv[m] = of_steps(s.beta(), m, lane) * y[m];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 16 * m + 4 * grp + e;
+                        g.dout[i * LO + 16 * wc + col] = (E)val[m][e];
+                        g.y.put(i, 16 * wc + col, y[m][e]);
                     }
                 }
+                wrong += nothing(dv);
+                put_steps(head_of<E>(A.dv, A.sdv, bi, h) + t0 * A.sdv.ts, (int)A.sdv.ts, c, mine, rows, lane, dv);
+            }
+            lds_barrier();
+            if (!for_y) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const f4 beta = of_steps(s.beta(), m, lane);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = 16 * m + 4 * grp + e;
+                        const float y = g.y.at(i, 16 * wc + col);
+                        const float a = group_fold(y * res[m][e], 16, add), b = group_fold(beta[e] * y * val[m][e], 16, add);
+                        if (col == 0) {
+                            g.yu[wc][i] = sl ? g.yu[wc][i] + a : a;
+                            g.vdv[wc][i] = sl ? g.vdv[wc][i] + b : b;
+                        }
+                    }
+                }
+            } else {
+                const float left = s.since()[CH - 1];
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) end = fmaf(res[m][e], g.u.at(16 * m + 4 * grp + e, 16 * wc + col), end);
+                if (left != 0.f)
+#pragma unroll
+                    for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) end = fmaf(left * g.state.at(32 * (n >> 1) + 8 * grp + 4 * (n & 1) + e, 16 * wc + col), st.s[n][e], end);
+            }
+            const bool same = sl + COLS < A.Dv;
+            if (same || id + 1 < stop) get(same ? id : id + 1, same ? sl + COLS : 0, !same && tile + 1 == tiles);
+            if (wc < 3) {
+#pragma unroll
+                for (int kb = 0; kb < COLS; kb += 32) {
+                    const auto b = g.u.get(tj + col, kb + 8 * grp);
+                    if (!for_y) part = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, part);
+                    else part = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, part);
+                }
+            }
+            // columns 16 d.. of dO S^T, Y S^T and U D^T
+            if (has) {
+#pragma unroll
+                for (int kb = 0; kb < COLS; kb += 32) {
+                    const auto sr = g.state.get(dk, kb + 8 * grp), dr = g.back.get(dk, kb + 8 * grp);
+#pragma unroll
+                    for (int m = 0; m < NM; ++m) {
+                        const int i = 16 * (m0 + m) + col, k = kb + 8 * grp;
+                        os[m] = Op::mul(eight(g.dout + i * LO + k), sr, os[m]);
+                        ys[m] = Op::mul(g.y.get(i, k), sr, ys[m]);
+                        ud[m] = Op::mul(g.u.get(i, k), dr, ud[m]);
+                    }
+                }
+            }
         }
         if (wc < 3) {
+            auto &to = for_y ? g.dn : g.dp;
+            auto &tr = for_y ? g.dnt : g.dpt;
+            const int i0 = ti + 4 * grp, j = tj + col, cut_j = s.cut()[j];
+            const vec<int, 4> cut_i = load<4>(s.cut() + i0);
+            const f4 hi_i = load<4>(s.run_hi() + i0), lo_i = load<4>(s.run_lo() + i0), beta = load<4>(s.beta() + i0);
+            const float hi_j = s.run_hi()[j], lo_j = s.run_lo()[j];
 #pragma unroll
-            for (int kb = 0; kb < COLS; kb += 32) {
-                const auto b = g.u.get(tj + col, kb + 8 * grp);
-                if (!for_y) part = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, part);
-                else part = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, part);
+            for (int r = 0; r < 4; ++r) {
+                const int i = i0 + r;
+                const float b = j > i || (for_y && j == i) || cut_i[r] != cut_j ? 0.f : between(hi_i[r], lo_i[r], hi_j, lo_j);
+                const float q = b == 0.f ? 0.f : (for_y ? -beta[r] : A.scale) * b * part[r];
+                to.put(i, j, q);
+                tr.put(j, i, q);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {       // above the diagonal
+                (for_y ? g.dn : g.dp).put(4 * grp + r, 16 + col, 0.f);
+                (for_y ? g.dnt : g.dpt).put(16 + col, 4 * grp + r, 0.f);
             }
         }
-        // columns 16 d.. of dO S^T, Y S^T and U D^T
+        lds_barrier();
         if (has) {
-#pragma unroll
-            for (int kb = 0; kb < COLS; kb += 32) {
-                float x[8], z[8];
-                state_row(S, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads, x);
-                state_row(Dn, dk, sl + kb + 8 * grp, A.Dk, A.Dv, quads, z);
-                if (m0 == 0 && s.since()[CH - 1] != 0.f)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) end = fmaf(s.since()[CH - 1] * x[e], z[e], end);
-                const auto sr = Op::template split<2>(x), dr = Op::template split<2>(z);
-#pragma unroll
-                for (int m = 0; m < NM; ++m) {
-                    const int i = 16 * (m0 + m) + col;
-                    os[m] = Op::mul(eight(g.dout + i * LO + kb + 8 * grp), sr, os[m]);
-                    ys[m] = Op::mul(g.y.get(i, kb + 8 * grp), sr, ys[m]);
-                    ud[m] = Op::mul(g.u.get(i, kb + 8 * grp), dr, ud[m]);
-                }
-            }
-        }
-        if (sl + COLS < A.Dv) __syncthreads();
-    }
-    if (wc < 3) {
-        auto &to = for_y ? g.dn : g.dp;
-        auto &tr = for_y ? g.dnt : g.dpt;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = ti + 4 * grp + r, j = tj + col;
-            const float b = j <= i ? s.between(i, j) : 0.f;
-            const float x = b == 0.f ? 0.f : !for_y ? A.scale * b * part[r] : j < i ? -s.beta()[i] * b * part[r] : 0.f;
-            to.put(i, j, x);
-            tr.put(j, i, x);
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {       // above the diagonal
-            (for_y ? g.dn : g.dp).put(4 * grp + r, 16 + col, 0.f);
-            (for_y ? g.dnt : g.dpt).put(16 + col, 4 * grp + r, 0.f);
-        }
-    }
-    __syncthreads();
-    if (has) {
-        const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * d, lane), qc = columns_of<1, Tile::LD>(s.q + 16 * d, lane);
-#pragma unroll
-        for (int n = 0; n < NM; ++n) {
-            const int m = m0 + n, i0 = 16 * m + col;
-            const f4 since = of_steps(s.since(), m, lane), beta = of_steps(s.beta(), m, lane), until = of_steps(s.until(), m, lane);
-            f4 x[2] = {where(since, A.scale * os[n]), where(since, -beta * ys[n]) + where(until, ud[n])};
-            x[0] = Op::mul(g.dp.pair(i0, 4 * grp), kc, x[0]);
-            x[1] = Op::mul(g.dpt.pair(i0, 4 * grp), qc, x[1]);
-            x[1] = Op::mul(g.dn.pair(i0, 4 * grp), kc, x[1]);
-            x[1] = Op::mul(g.dnt.pair(i0, 4 * grp), kc, x[1]);
-            wrong += nothing(x);
+            const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * d, lane), qc = columns_of<1, Tile::LD>(s.q + 16 * d, lane);
             E *dq = head_of<E>(A.dq, A.sdq, bi, h) + t0 * A.sdq.ts, *dkp = head_of<E>(A.dk, A.sdk, bi, h) + t0 * A.sdk.ts;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 16 * m + 4 * grp + e;
-                if (dk < A.Dk && i < rows) {
-                    dq[(uint32_t)(i * (int)A.sdq.ts + dk)] = (E)x[0][e];
-                    dkp[(uint32_t)(i * (int)A.sdk.ts + dk)] = (E)x[1][e];
+            for (int n = 0; n < NM; ++n) {
+                const int m = m0 + n, i0 = 16 * m + col;
+                const f4 since = of_steps(s.since(), m, lane), beta = of_steps(s.beta(), m, lane), until = of_steps(s.until(), m, lane);
+                f4 r[2] = {where(since, A.scale * os[n]), where(since, -beta * ys[n]) + where(until, ud[n])};
+                r[0] = Op::mul(g.dp.pair(i0, 4 * grp), kc, r[0]);
+                r[1] = Op::mul(g.dpt.pair(i0, 4 * grp), qc, r[1]);
+                r[1] = Op::mul(g.dn.pair(i0, 4 * grp), kc, r[1]);
+                r[1] = Op::mul(g.dnt.pair(i0, 4 * grp), kc, r[1]);
+                wrong += nothing(r);
+                const int i = 16 * m + 4 * grp;
+                const uint32_t qa = (uint32_t)(i * (int)A.sdq.ts + dk), ka = (uint32_t)(i * (int)A.sdk.ts + dk);
+                if (rows == CH && A.Dk == DK) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        (dq + e * A.sdq.ts)[qa] = (E)r[0][e];
+                        (dkp + e * A.sdk.ts)[ka] = (E)r[1][e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (dk < A.Dk && i + e < rows) {
+                            (dq + e * A.sdq.ts)[qa] = (E)r[0][e];
+                            (dkp + e * A.sdk.ts)[ka] = (E)r[1][e];
+                        }
                 }
-                const float sum = group_fold(x[0][e] * (float)s.q[i * Tile::LD + dk], 16, add);
-                if (col == 0) g.qdq[d][i] = sum;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float sum = group_fold(r[0][e] * (float)s.q[(i + e) * Tile::LD + dk], 16, add);
+                    if (col == 0) g.qdq[d][i + e] = sum;
+                }
             }
         }
-    }
-    end = group_fold(end, 64, add);
-    wrong = wrong + end * 0.f;
-    if (lane == 0) g.ends[w] = end;
-    const bool again = __syncthreads_or(wrong != 0.f);
-    if (tid == 0) A.again[(long)head * A.tiles + tile] = again;
-    if (again) return;                  // k_delta_grad_steps's
-    if (tid < CH) {
-        const int i = tid, cut = s.cut()[i];
-        float x = 0.f;
+        end = group_fold(end, 64, add);
+        wrong = wrong + end * 0.f;
+        if (lane == 0) g.ends[w] = end;
+        const int step = lane & 31, cut = s.cut()[step];      // before the next tile takes their place
+        const bool still = starts(s, step) || s.gate()[step] == 0.f;
+        if (__any(wrong != 0.f) && lane == 0) g.wrong[w] = 1;
+        else if (lane == 0) g.wrong[w] = 0;
+        lds_barrier();
+        if (w == 0) {
+            int again = 0;
 #pragma unroll
-        for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][i];
-        x = i < rows ? x - ((g.vdv[0][i] + g.vdv[1][i]) + (g.vdv[2][i] + g.vdv[3][i])) : 0.f;
-        if (i == rows - 1)
+            for (int n = 0; n < 8; ++n) again |= g.wrong[n];
+            if (lane == 0) A.again[id] = again;
+            const int i = step;
+            float x = 0.f;
 #pragma unroll
-            for (int n = 0; n < 8; ++n) x += g.ends[n];
+            for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][i];
+            x = i < rows ? x - ((g.vdv[0][i] + g.vdv[1][i]) + (g.vdv[2][i] + g.vdv[3][i])) : 0.f;
+            if (i == rows - 1)
 #pragma unroll
-        for (int n = 1; n < CH; n *= 2) {
-            const float o = __shfl_down(x, n, CH);
-            const int oc = __shfl_down(cut, n, CH);
-            if (i + n < CH && oc == cut) x += o;
-        }
-        if (i < rows) {
-            const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
-            const float rate = (g.yu[0][i] + g.yu[1][i]) + (g.yu[2][i] + g.yu[3][i]);
-            ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, i) || s.gate()[i] == 0.f ? 0.f : x * (1.f / (1.f + expf(f))));
-            ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(rate * (1.f / (1.f + expf(b))));
+                for (int n = 0; n < 8; ++n) x += g.ends[n];
+#pragma unroll
+            for (int n = 1; n < CH; n *= 2) {
+                const float o = __shfl_down(x, n, CH);
+                const int oc = __shfl_down(cut, n, CH);
+                if (i + n < CH && oc == cut) x += o;
+            }
+            if (lane < rows && !again) {      // else k_delta_grad_steps's
+                const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
+                const float rate = (g.yu[0][i] + g.yu[1][i]) + (g.yu[2][i] + g.yu[3][i]);
+                ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(still ? 0.f : x * (1.f / (1.f + expf(f))));
+                ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(rate * (1.f / (1.f + expf(b))));
+            }
         }
     }
 }
@@ -1165,7 +1202,7 @@ template <class E, int DK> struct DeltaSteps {
 template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs &A, DeltaSteps<E, DK> &g, long head, long tile)
 {
     using Tile = DeltaTile<E, DK>;
-    const float *S0 = A.states + (head * A.tiles + tile) * A.Dk * A.Dv, *D0 = A.into + (head * A.tiles + tile) * A.Dk * A.Dv;
+    const int blocks = blocks_of(A.Dv);
     Tile &s = g.s;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bi = (int)(head / A.H), h = (int)(head % A.H);
     const long t0 = tile * CH;
@@ -1177,9 +1214,12 @@ template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs 
             const int c = c0 + 16 * w + (lane & 15);
             const bool mine = c < A.Dv;
             Columns<DK> S, D;
-            S.get(S0, A.Dk, A.Dv, c, lane);
+            const long at = ((head * A.tiles + tile) * blocks + min(c0 / 16 + w, blocks - 1)) * 16 * DK;
+            S.load(A.states + at, lane);
+            if (c0 / 16 + w >= blocks) S.clear();
             for (int i = 0; i < t; ++i) delta_step<E, DK>(s, S, i, mine ? (float)v[i * A.sv.ts + c] : 0.f, lane);
-            D.get(D0, A.Dk, A.Dv, c, lane);
+            D.load(A.into + at, lane);
+            if (c0 / 16 + w >= blocks) D.clear();
             for (int i = rows - 1; i > t; --i) {
                 delta_step_back<E, DK>(s, D, i, mine ? (float)dout[i * A.sdo.ts + c] : 0.f, A.scale, lane);
                 delta_pass_back<E, DK>(s, D, i);

@@ -40,7 +40,7 @@ struct DeltaSizes {
     int64_t T;
 };
 int64_t tiles_of(int64_t T) { return (T + seq::CH - 1) / seq::CH; }
-int64_t states_of(const DeltaSizes &s) { return (int64_t)s.B * s.H * s.Dk * s.Dv; }
+int width_of(int32_t Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
 
 const char *check_sizes(const DeltaSizes &s)
 {
@@ -77,7 +77,7 @@ template <class Args> seq::DeltaIn inputs(const Args &d)      // what both direc
 template <int N> using Int = std::integral_constant<int, N>;
 template <class F> bool delta_form(int32_t dtype, int32_t Dk, F &&go)
 {
-    auto wide = [&](auto e) { return Dk <= 32 ? go(e, Int<32>{}) : Dk <= 64 ? go(e, Int<64>{}) : go(e, Int<128>{}); };
+    auto wide = [&](auto e) { return width_of(Dk) == 32 ? go(e, Int<32>{}) : width_of(Dk) == 64 ? go(e, Int<64>{}) : go(e, Int<128>{}); };
     return dtype == DQN_F32 ? wide(float{}) : wide(seq::bf16{});
 }
 int64_t heads_of(const seq::DeltaIn &A) { return (int64_t)A.B * A.H; }
@@ -95,6 +95,7 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, hipStream_
     seq::k_delta<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, bytes, st>>>(A);
     return true;
 }
+constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit
 template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, hipStream_t st)
 {
     static std::atomic<uint64_t> back_granted{0}, granted{0};
@@ -103,12 +104,14 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, h
     seq::k_delta_back<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, back, st>>>(A);
     if (!A.tiles) return true;
     static_assert(sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup gets");
-    seq::k_delta_grad<E, DK><<<dim3((unsigned)(heads_of(A) * A.tiles)), 512, bytes, st>>>(A);
+    const int64_t all = heads_of(A) * A.tiles, per = std::max<int64_t>(1, (all + GRAD_GROUPS - 1) / GRAD_GROUPS);
+    seq::k_delta_grad<E, DK><<<dim3((unsigned)((all + per - 1) / per)), 512, bytes, st>>>(A, (int)per);
     seq::k_delta_grad_steps<E, DK><<<dim3((unsigned)((heads_of(A) * A.tiles + seq::AGAIN - 1) / seq::AGAIN)), 256, sizeof(seq::DeltaSteps<E, DK>), st>>>(A);
     return true;
 }
 size_t record_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * sizeof(seq::DeltaRecord); }
-size_t state_bytes(const DeltaSizes &s) { return ((size_t)states_of(s) * tiles_of(s.T) * 4 + 15) / 16 * 16; }
+// a state for each tile, padded as the kernels hold them
+size_t state_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * width_of(s.Dk) * ((s.Dv + 15) / 16 * 16) * 4; }
 
 }  // namespace
 
