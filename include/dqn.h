@@ -438,8 +438,7 @@ typedef struct {
                                            aligned                                  */
     void *workspace;                    /* forward_workspace bytes from
                                            dqn_delta_sizes, 16-byte aligned; free for
-                                           other use after the call; not used with
-                                           carry                                    */
+                                           other use after the call                 */
 } dqn_delta_args;
 
 /* Gradients of the rule: of all five inputs and of s0, from the gradient of o and of s_last.

@@ -320,11 +320,11 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
 }
 
 // ---------------------------------------------------------------- what a workgroup holds of a tile in LDS
-template <class E, int DK> struct DeltaTile {
+template <class E, int DK, int VECTORS> struct DeltaTile {      // VECTORS: how many of the record's, from `since` on
     static constexpr int LD = DK + 16 / (int)sizeof(E), LC = CH + 4;
     E q[CH * LD], k[CH * LD];
     float t[CH * LC], p[CH * LC];
-    float vectors[7 * CH];             // as in the record
+    float vectors[VECTORS * CH];
     __device__ __forceinline__ const float *since() const { return vectors; }
     __device__ __forceinline__ const float *until() const { return vectors + CH; }
     __device__ __forceinline__ const float *beta() const { return vectors + 2 * CH; }
@@ -341,9 +341,9 @@ template <class T> __device__ __forceinline__ T *plus(T *p, uint32_t bytes) { re
 template <class T> __device__ __forceinline__ const T *plus(const T *p, uint32_t bytes) { return (const T *)((const char *)p + bytes); }
 
 // The part of a tile that a thread of THREADS brings from memory: into registers first, so that it can arrive while another tile is worked on.
-template <class E, int DK, int THREADS> struct DeltaFetch {
+template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
     static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + THREADS - 1) / THREADS, NR = (CH * CH / 4 + THREADS - 1) / THREADS;
-    static_assert(7 * CH / 4 <= THREADS, "a thread brings one piece of the vectors");
+    static_assert(VECTORS * CH / 4 <= THREADS, "a thread brings one piece of the vectors");
     const E *qh, *kh;
     const DeltaRecord *records;
     int tid, rows;
@@ -399,11 +399,11 @@ template <class E, int DK, int THREADS> struct DeltaFetch {
             t[n] = seq::load<4>(rec->t + 4 * e);
             p[n] = seq::load<4>(rec->p + 4 * e);
         }
-        vectors = seq::load<4>(rec->since + 4 * min(tid, 7 * CH / 4 - 1));
+        vectors = seq::load<4>(rec->since + 4 * min(tid, VECTORS * CH / 4 - 1));
     }
-    __device__ __forceinline__ void put(DeltaTile<E, DK> &s, int Dk) const
+    __device__ __forceinline__ void put(DeltaTile<E, DK, VECTORS> &s, int Dk) const
     {
-        using Tile = DeltaTile<E, DK>;
+        using Tile = DeltaTile<E, DK, VECTORS>;
         const bool whole = rows == CH && Dk == DK;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -429,7 +429,7 @@ template <class E, int DK, int THREADS> struct DeltaFetch {
                 seq::store<4>(s.p + r * Tile::LC + c, p[n]);
             }
         }
-        if (tid < 7 * CH / 4) seq::store<4>(s.vectors + 4 * tid, vectors);
+        if (tid < VECTORS * CH / 4) seq::store<4>(s.vectors + 4 * tid, vectors);
     }
 };
 static_assert(offsetof(DeltaRecord, cut) - offsetof(DeltaRecord, since) == 6 * CH * 4, "the vectors lie one behind the other");
@@ -592,31 +592,29 @@ template <int DK> struct Columns {
     }
 };
 
-template <class Tile> __device__ __forceinline__ bool starts(const Tile &s, int i) { return s.cut()[i] != (i ? s.cut()[i - 1] : 0); }
+__device__ __forceinline__ bool starts(const int *cut, int i) { return cut[i] != (i ? cut[i - 1] : 0); }
 
 // One step as its definition has it; the state after it.  -> what is written, beta (v - S^T k)
-template <class E, int DK> __device__ __forceinline__ float delta_step(const DeltaTile<E, DK> &s, Columns<DK> &S, int i, float v, int lane)
+template <class Tile, int DK> __device__ __forceinline__ float delta_step(const Tile &s, const DeltaRecord &rec, Columns<DK> &S, int i, float v, int lane)
 {
-    using Tile = DeltaTile<E, DK>;
-    if (starts(s, i)) S.clear();
-    S.scaled(s.gate()[i]);
+    if (starts(rec.cut, i)) S.clear();
+    S.scaled(rec.gate[i]);
     const float u = s.beta()[i] * (v - S.dot(s.k + i * Tile::LD, lane));
     S.add(s.k + i * Tile::LD, u, lane);
     return u;
 }
 // and the gradient of the state before step i from that after it, do and q being the step's.  -> the gradient of v
-template <class E, int DK> __device__ __forceinline__ float delta_step_back(const DeltaTile<E, DK> &s, Columns<DK> &D, int i, float dout, float scale, int lane)
+template <class Tile, int DK> __device__ __forceinline__ float delta_step_back(const Tile &s, Columns<DK> &D, int i, float dout, float scale, int lane)
 {
-    using Tile = DeltaTile<E, DK>;
     D.add(s.q + i * Tile::LD, scale * dout, lane);
     const float dv = s.beta()[i] * D.dot(s.k + i * Tile::LD, lane);
     D.add(s.k + i * Tile::LD, -dv, lane);
     return dv;
 }
-template <class E, int DK> __device__ __forceinline__ void delta_pass_back(const DeltaTile<E, DK> &s, Columns<DK> &D, int i)
+template <int DK> __device__ __forceinline__ void delta_pass_back(const DeltaRecord &rec, Columns<DK> &D, int i)
 {
-    if (starts(s, i)) D.clear();
-    else D.scaled(s.gate()[i]);
+    if (starts(rec.cut, i)) D.clear();
+    else D.scaled(rec.gate[i]);
 }
 
 // A lane's numbers of a column of a tensor of steps [..][Dv] (V, dO): where they lie, and as they are loaded
@@ -657,9 +655,8 @@ template <class E> __device__ __forceinline__ void put_steps(E *tile, int ts, in
 }
 
 // U of a wave's columns from the state that enters and V.
-template <class E, int DK, int N> __device__ __forceinline__ void delta_u(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&S)[DK / 32], const f4 (&v)[2], int rows, int lane, f4 (&u)[2])
+template <class E, int DK, int N, class Tile> __device__ __forceinline__ void delta_u(const Tile &s, const typename Operand<E>::template Split<N> (&S)[DK / 32], const f4 (&v)[2], int rows, int lane, f4 (&u)[2])
 {
-    using Tile = DeltaTile<E, DK>;
     f4 r[2], ks[2] = {};
 #pragma unroll
     for (int p = 0; p < DK / 32; ++p)
@@ -675,10 +672,9 @@ template <class E, int DK, int N> __device__ __forceinline__ void delta_u(const 
     lower<Tile::LC>(s.t, r, lane, u);
 }
 // kd = (G_C. K) D, then Y = T^T (pd + kd) of a wave's columns, pd = P^T dO.
-template <class E, int DK, int N>
-__device__ __forceinline__ void delta_y(const DeltaTile<E, DK> &s, const typename Operand<E>::template Split<N> (&D)[DK / 32], const f4 (&pd)[2], int lane, f4 (&kd)[2], f4 (&y)[2])
+template <class E, int DK, int N, class Tile>
+__device__ __forceinline__ void delta_y(const Tile &s, const typename Operand<E>::template Split<N> (&D)[DK / 32], const f4 (&pd)[2], int lane, f4 (&kd)[2], f4 (&y)[2])
 {
-    using Tile = DeltaTile<E, DK>;
     f4 du[2];
     kd[0] = kd[1] = f4{};
 #pragma unroll
@@ -695,66 +691,121 @@ __device__ __forceinline__ void delta_y(const DeltaTile<E, DK> &s, const typenam
 }
 
 // ---------------------------------------------------------------- from state to state
-// A workgroup per head and 16 columns of each of WAVES pairs of waves.  One wave of a pair takes the state from tile to tile and nothing else; the
-// other brings tiles into LDS and does, a tile apart, what the chain does not wait for: the outputs, or in the backward direction what dO alone
-// gives.  They hand each other registers as they are, through LDS, with one barrier a tile.
+// A workgroup per head, range of tiles and 16 columns of each of WAVES pairs of waves.  One wave of a pair takes the state from tile to tile and
+// nothing else; the other brings tiles into LDS and does, a tile apart, what the chain does not wait for: the outputs, or in the backward
+// direction what dO alone gives.  They hand each other registers as they are, through LDS, with one barrier a tile.
+// Where heads are few, a head's tiles are cut into ranges.  What a range does to the state is a linear map and an addition, S -> M S + B; a first
+// launch (MAPS) finds both, M by the same chain from the unit matrix's columns, a second goes from range to range, and the last has all
+// ranges' first states.
 // A tile whose results hold a number that is not finite is taken again step by step as the definition has it, where nothing is multiplied by the
 // zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
 template <class E, int DK> struct DeltaPairs {
-    static constexpr int tile = (int)sizeof(DeltaTile<E, DK>), pair = 2 * 64 * (DK / 16 + 2) * 16, room = 160 * 1024;
+    static constexpr int tile = (int)sizeof(DeltaTile<E, DK, 3>), pair = 2 * 64 * (DK / 16 + 2) * 16, room = 160 * 1024;
     static constexpr int waves = 3 * tile + 4 * pair <= room ? 4 : 3 * tile + 2 * pair <= room ? 2 : 1;
 };
 template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>::waves;
 template <class E, int DK> struct DeltaChain {
     static constexpr int WAVES = DeltaPairs<E, DK>::waves;
-    DeltaTile<E, DK> tiles[3];
+    DeltaTile<E, DK, 3> tiles[3];
     f4 state[2][WAVES][DK / 16][64];      // forward: the state that enters; backward: (scale g Q)^T dO
     f4 steps[2][WAVES][2][64];            // U; P^T dO
 };
-template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta(DeltaArgs A)
+// How tiles are cut into ranges, and what is kept of each: M [DK][DK], B and the state it begins with [Dk][Dv]
+struct DeltaRanges {
+    int ranges;
+    long per;                             // tiles of a range, but for the last
+    float *m, *b, *first;                 // [heads][ranges][..]
+};
+// A wave's place: head, range and block of 16 columns; with MAPS the blocks behind those of the state are M's.
+template <class E, int DK, bool MAPS> struct ChainPlace {
+    unsigned head;
+    int range, block, blocks, bi, h, c;
+    long tile0, n;                        // the range's first tile, how many it has
+    bool mine, unit;                      // whether the column is one of the state's; whether the block is one of M's
+    __device__ __forceinline__ ChainPlace(const DeltaIn &A, const DeltaRanges &R, int w, int lane)
+    {
+        constexpr int WAVES = DeltaPairs<E, DK>::waves;
+        blocks = blocks_of(A.Dv);
+        const unsigned groups = (unsigned)((blocks + (MAPS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x / groups;
+        block = (int)(blockIdx.x % groups) * WAVES + w;
+        head = which / (unsigned)R.ranges;
+        range = (int)(which % (unsigned)R.ranges);
+        bi = (int)(head / (unsigned)A.H);
+        h = (int)(head % (unsigned)A.H);
+        c = 16 * block + (lane & 15);
+        mine = c < A.Dv;
+        unit = MAPS && block >= blocks;
+        tile0 = range * R.per;
+        n = min(R.per, A.tiles - tile0);
+    }
+    // the columns that the chain begins with
+    __device__ __forceinline__ void begin(const DeltaIn &A, const DeltaRanges &R, const float *given, Columns<DK> &S, int lane) const
+    {
+        if (MAPS) {
+            S.clear();
+            if (unit)
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S.s[n][e] = 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1) + e == c - 16 * blocks ? 1.f : 0.f;
+        } else {
+            const float *from = R.ranges > 1 ? R.first + (long)range * A.Dk * A.Dv + (long)head * R.ranges * A.Dk * A.Dv : given ? given + (long)head * A.Dk * A.Dv : nullptr;
+            S.get(from, A.Dk, A.Dv, c, lane);
+        }
+    }
+    // and ends with, in a launch that finds maps
+    __device__ __forceinline__ void end(const DeltaIn &A, const DeltaRanges &R, const Columns<DK> &S, int lane) const
+    {
+        const long at = (long)head * R.ranges + range;
+        if (!unit) S.put(R.b + at * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
+        else S.put(R.m + at * DK * DK, DK, DK, c - 16 * blocks, lane);
+    }
+};
+
+template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta(DeltaArgs A, DeltaRanges R)
 {
-    using Tile = DeltaTile<E, DK>;
+    using Tile = DeltaTile<E, DK, 3>;
     using Chain = DeltaChain<E, DK>;
     constexpr int WAVES = Chain::WAVES;
     extern __shared__ __align__(16) unsigned char lds[];
     Chain &L = *reinterpret_cast<Chain *>(lds);
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
     const bool chain = threadIdx.x < 64 * WAVES;
-    const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
-    const unsigned head = blockIdx.x / slices;
-    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), block = WAVES * slice + w, blocks = blocks_of(A.Dv), c = 16 * block + (lane & 15);
-    const bool mine = c < A.Dv;
-    const long size = (long)A.Dk * A.Dv;
-    const E *v = head_of<E>(A.v, A.sv, bi, h);
-    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - tile * CH); };
+    const ChainPlace<E, DK, MAPS> at(A, R, w, lane);
+    const E *v = head_of<E>(A.v, A.sv, at.bi, at.h) + at.tile0 * CH * A.sv.ts;
+    const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
+    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
     if (chain) {
         Columns<DK> S;
-        S.get(A.s0 ? A.s0 + head * size : nullptr, A.Dk, A.Dv, c, lane);
+        at.begin(A, R, A.s0, S, lane);
         Steps<E> vs;
         vs.rows = 0;
-        if (A.tiles) vs.load(v, (int)A.sv.ts, c, A.Dv, rows_in(0), lane);
+        if (at.n > 0) vs.load(v, (int)A.sv.ts, at.c, A.Dv, rows_in(0), lane);
         __syncthreads();
-        for (long i = 0; i <= A.tiles; ++i) {
-            if (i < A.tiles) {
+        for (long i = 0; i <= at.n; ++i) {
+            if (i < at.n) {
                 const Tile &s = L.tiles[i % 3];
                 const int rows = rows_in(i);
                 f4 val[2], u[2], next[DK / 16];
-                vs.get(mine, lane, val);
-                if (i + 1 < A.tiles) vs.load(v + (i + 1) * CH * A.sv.ts, (int)A.sv.ts, c, A.Dv, rows_in(i + 1), lane);
+                vs.get(at.mine, lane, val);
+                if (i + 1 < at.n) vs.load(v + (i + 1) * CH * A.sv.ts, (int)A.sv.ts, at.c, A.Dv, rows_in(i + 1), lane);
+                if (!MAPS)
 #pragma unroll
-                for (int n = 0; n < DK / 16; ++n) L.state[i & 1][w][n][lane] = S.s[n];
+                    for (int n = 0; n < DK / 16; ++n) L.state[i & 1][w][n][lane] = S.s[n];
                 typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(S.s[2 * p], S.s[2 * p + 1]);
                 delta_u<E, DK, 3>(s, sp, val, rows, lane, u);
-                L.steps[i & 1][w][0][lane] = u[0];
-                L.steps[i & 1][w][1][lane] = u[1];
+                if (!MAPS) {
+                    L.steps[i & 1][w][0][lane] = u[0];
+                    L.steps[i & 1][w][1][lane] = u[1];
+                }
                 const auto up = split<E, 3>(where(of_steps(s.until(), 0, lane), u[0]), where(of_steps(s.until(), 1, lane), u[1]));
                 const float left = s.since()[CH - 1];
 #pragma unroll
                 for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), up, where(left, S.s[n]));
                 if (__any(nothing(next) != 0.f)) {
-                    for (int t = 0; t < rows; ++t) delta_step<E, DK>(s, S, t, mine ? (float)v[(i * CH + t) * A.sv.ts + c] : 0.f, lane);
+                    for (int t = 0; t < rows; ++t) delta_step(s, records[i], S, t, at.mine ? (float)v[(i * CH + t) * A.sv.ts + at.c] : 0.f, lane);
                 } else {
 #pragma unroll
                     for (int n = 0; n < DK / 16; ++n) S.s[n] = next[n];
@@ -762,21 +813,22 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
             }
             lds_barrier();
         }
-        if (A.last) S.put(A.last + head * size, A.Dk, A.Dv, c, lane);
+        if (MAPS) at.end(A, R, S, lane);
+        else if (A.last && at.tile0 + at.n >= A.tiles) S.put(A.last + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
     } else {
-        DeltaFetch<E, DK, 64 * WAVES> fetch;
-        E *o = head_of<E>(A.o, A.so, bi, h);
-        if (A.tiles) {
-            fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, threadIdx.x - 64 * WAVES);
-            fetch.load(A, 0);
+        DeltaFetch<E, DK, 64 * WAVES, 3> fetch;
+        E *o = head_of<E>(A.o, A.so, at.bi, at.h) + at.tile0 * CH * A.so.ts;
+        if (at.n > 0) {
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x - 64 * WAVES);
+            fetch.load(A, at.tile0);
             fetch.put(L.tiles[0], A.Dk);
-            if (A.tiles > 1) fetch.load(A, 1);
+            if (at.n > 1) fetch.load(A, at.tile0 + 1);
         }
         __syncthreads();
-        for (long i = 0; i <= A.tiles; ++i) {
-            if (i + 1 < A.tiles) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
-            if (i + 2 < A.tiles) fetch.load(A, i + 2);
-            if (i > 0) {
+        for (long i = 0; i <= at.n; ++i) {
+            if (i + 1 < at.n) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
+            if (i + 2 < at.n) fetch.load(A, at.tile0 + i + 2);
+            if (!MAPS && i > 0) {
                 const long tile = i - 1;
                 const Tile &s = L.tiles[tile % 3];
                 const int rows = rows_in(tile);
@@ -786,7 +838,7 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
                 for (int n = 0; n < DK / 16; ++n) S.s[n] = L.state[tile & 1][w][n][lane];
                 u[0] = L.steps[tile & 1][w][0][lane];
                 u[1] = L.steps[tile & 1][w][1][lane];
-                if (A.states && block < blocks) S.store(A.states + ((head * A.tiles + tile) * blocks + block) * 16 * DK, lane);
+                if (A.states && at.block < at.blocks) S.store(A.states + ((at.head * A.tiles + at.tile0 + tile) * at.blocks + at.block) * 16 * DK, lane);
                 typename Operand<E>::template Split<2> sp[DK / 32];      // o is rounded to bf16: 16 bits of the state do
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(S.s[2 * p], S.s[2 * p + 1]);
@@ -801,44 +853,42 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
                 E *to = o + tile * CH * A.so.ts;
                 if (__any(nothing(out) != 0.f)) {
                     for (int t = 0; t < rows; ++t) {
-                        delta_step<E, DK>(s, S, t, mine ? (float)v[(tile * CH + t) * A.sv.ts + c] : 0.f, lane);
+                        delta_step(s, records[tile], S, t, at.mine ? (float)v[(tile * CH + t) * A.sv.ts + at.c] : 0.f, lane);
                         const float x = A.scale * S.dot(s.q + t * Tile::LD, lane);
-                        if (mine && lane < 16) to[t * A.so.ts + c] = (E)x;
+                        if (at.mine && lane < 16) to[t * A.so.ts + at.c] = (E)x;
                     }
-                } else put_steps(to, (int)A.so.ts, c, mine, rows, lane, out);
+                } else put_steps(to, (int)A.so.ts, at.c, at.mine, rows, lane, out);
             }
             lds_barrier();
         }
     }
 }
 
-// The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.
-template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta_back(DeltaGradArgs A)
+// The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.  A range's map is the transposed
+// of its map in the other direction, found from the unit matrix in the same way.
+template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta_back(DeltaGradArgs A, DeltaRanges R)
 {
-    using Tile = DeltaTile<E, DK>;
+    using Tile = DeltaTile<E, DK, 3>;
     using Chain = DeltaChain<E, DK>;
     constexpr int WAVES = Chain::WAVES;
     extern __shared__ __align__(16) unsigned char lds[];
     Chain &L = *reinterpret_cast<Chain *>(lds);
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
     const bool chain = threadIdx.x < 64 * WAVES;
-    const int slices = (A.Dv + 16 * WAVES - 1) / (16 * WAVES), slice = blockIdx.x % slices;
-    const unsigned head = blockIdx.x / slices;
-    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), block = WAVES * slice + w, blocks = blocks_of(A.Dv), c = 16 * block + (lane & 15);
-    const bool mine = c < A.Dv;
-    const long size = (long)A.Dk * A.Dv;
-    const E *dout = head_of<E>(A.dout, A.sdo, bi, h);
-    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - tile * CH); };
-    // turn i of the pair that brings and prepares is for tile `tiles - 1 - i`, of the chain for the one before
+    const ChainPlace<E, DK, MAPS> at(A, R, w, lane);
+    const E *dout = head_of<E>(A.dout, A.sdo, at.bi, at.h) + at.tile0 * CH * A.sdo.ts;
+    const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
+    auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
+    // turn i of the wave that brings and prepares is for tile n - 1 - i, of the chain for the one before that
     if (chain) {
         Columns<DK> D;
-        D.get(A.dlast ? A.dlast + head * size : nullptr, A.Dk, A.Dv, c, lane);
+        at.begin(A, R, A.dlast, D, lane);
         __syncthreads();
-        for (long i = 0; i <= A.tiles; ++i) {
+        for (long i = 0; i <= at.n; ++i) {
             if (i > 0) {
-                const long tile = A.tiles - i;
+                const long tile = at.n - i;
                 const Tile &s = L.tiles[tile % 3];
-                if (block < blocks) D.store(A.into + ((head * A.tiles + tile) * blocks + block) * 16 * DK, lane);
+                if (!MAPS && at.block < at.blocks) D.store(A.into + ((at.head * A.tiles + at.tile0 + tile) * at.blocks + at.block) * 16 * DK, lane);
                 typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(D.s[2 * p], D.s[2 * p + 1]);
@@ -853,8 +903,8 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
                 for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), yp, where(left, D.s[n]) + L.state[tile & 1][w][n][lane]);
                 if (__any(nothing(next) != 0.f)) {
                     for (int t = rows_in(tile) - 1; t >= 0; --t) {
-                        delta_step_back<E, DK>(s, D, t, mine ? (float)dout[(tile * CH + t) * A.sdo.ts + c] : 0.f, A.scale, lane);
-                        delta_pass_back<E, DK>(s, D, t);
+                        delta_step_back(s, D, t, at.mine ? (float)dout[(tile * CH + t) * A.sdo.ts + at.c] : 0.f, A.scale, lane);
+                        delta_pass_back(records[tile], D, t);
                     }
                 } else {
 #pragma unroll
@@ -863,30 +913,31 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
             }
             lds_barrier();
         }
-        if (A.ds0) D.put(A.ds0 + head * size, A.Dk, A.Dv, c, lane);
+        if (MAPS) at.end(A, R, D, lane);
+        else if (A.ds0 && at.range == 0) D.put(A.ds0 + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
     } else {
-        DeltaFetch<E, DK, 64 * WAVES> fetch;
+        DeltaFetch<E, DK, 64 * WAVES, 3> fetch;
         Steps<E> ds;
         ds.rows = 0;
-        auto get = [&](long tile) { ds.load(dout + tile * CH * A.sdo.ts, (int)A.sdo.ts, c, A.Dv, rows_in(tile), lane); };
-        if (A.tiles) {
-            fetch.begin(A, (const DeltaRecord *)A.records, head, bi, h, threadIdx.x - 64 * WAVES);
-            fetch.load(A, A.tiles - 1);
-            get(A.tiles - 1);
-            fetch.put(L.tiles[(A.tiles - 1) % 3], A.Dk);
-            if (A.tiles > 1) fetch.load(A, A.tiles - 2);
+        auto get = [&](long tile) { ds.load(dout + tile * CH * A.sdo.ts, (int)A.sdo.ts, at.c, A.Dv, rows_in(tile), lane); };
+        if (at.n > 0) {
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x - 64 * WAVES);
+            fetch.load(A, at.tile0 + at.n - 1);
+            get(at.n - 1);
+            fetch.put(L.tiles[(at.n - 1) % 3], A.Dk);
+            if (at.n > 1) fetch.load(A, at.tile0 + at.n - 2);
         }
         __syncthreads();
-        for (long i = 0; i <= A.tiles; ++i) {
-            const long tile = A.tiles - 1 - i;
+        for (long i = 0; i <= at.n; ++i) {
+            const long tile = at.n - 1 - i;
             if (tile >= 0) {
                 f4 out[2], pd[2] = {}, x[2];
-                ds.get(mine, lane, out);
+                ds.get(at.mine, lane, out);
                 if (tile > 0) {
                     fetch.put(L.tiles[(tile - 1) % 3], A.Dk);
                     get(tile - 1);
                 }
-                if (tile > 1) fetch.load(A, tile - 2);
+                if (tile > 1) fetch.load(A, at.tile0 + tile - 2);
                 const Tile &s = L.tiles[tile % 3];
                 upper<Tile::LC>(s.p, out, lane, pd);
                 L.steps[tile & 1][w][0][lane] = pd[0];
@@ -899,6 +950,48 @@ template <class E, int DK> __global__ __launch_bounds__((chain_threads<E, DK>)) 
             }
             lds_barrier();
         }
+    }
+}
+
+// From range to range: the state each begins with, forward from s0 or backward from dlast.  A workgroup per head and 16 columns, a wave per 16 rows;
+// a result of 16 x 16 is the next right operand as it is, in its place in LDS.  What enters a range with an episode's start leaves nothing,
+// whatever it is.
+template <int DK, bool BACK> __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaRanges R, const float *given, const DeltaRecord *records, long tiles, int Dk, int Dv)
+{
+    __shared__ f4 state[2][DK / 16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4;
+    const unsigned blocks = (unsigned)blocks_of(Dv), head = blockIdx.x / blocks;
+    const int c = 16 * (int)(blockIdx.x % blocks) + (lane & 15), row = 16 * w + 4 * g;
+    const long size = (long)Dk * Dv, base = (long)head * R.ranges;
+    auto in = [&](int e) { return c < Dv && row + e < Dk; };
+    f4 S = {};
+    if (given)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (in(e)) S[e] = given[head * size + (row + e) * Dv + c];
+    for (int i = 0; i < R.ranges; ++i) {
+        const int r = BACK ? R.ranges - 1 - i : i;
+        float *first = R.first + (base + r) * size;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (in(e)) first[(row + e) * Dv + c] = S[e];
+        if (i + 1 == R.ranges) break;
+        const float *m = R.m + (base + r) * DK * DK + (16 * w + (lane & 15)) * DK + 4 * g, *b = R.b + (base + r) * size;
+        f4 a[DK / 16], next = {};
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) a[kb] = load<4>(m + 16 * kb);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (in(e)) next[e] = b[(row + e) * Dv + c];
+        int cut = 0;
+        for (long t = r * R.per + threadIdx.x; t < min(tiles, (r + 1) * R.per); t += 4 * DK) cut |= records[head * tiles + t].cut[CH - 1];
+        state[i & 1][w][lane] = S;
+        const bool forgets = __syncthreads_or(cut);
+        if (!forgets) {
+#pragma unroll
+            for (int kb = 0; kb < DK / 16; ++kb) next = mm4(a[kb], state[i & 1][kb][lane], next);
+        }
+        S = next;
     }
 }
 
@@ -938,7 +1031,7 @@ template <int R, int C> struct Matrix<bf16, R, C> {
 };
 template <class E, int DK> struct DeltaGradTile {
     static constexpr int LO = COLS + 16 / (int)sizeof(E);
-    DeltaTile<E, DK> s;
+    DeltaTile<E, DK, 7> s;
     E dout[CH * LO];
     Matrix<E, CH, COLS> u, y;
     Matrix<E, DK, COLS> state, back;        // the state that enters, the gradient of the one that leaves
@@ -954,7 +1047,7 @@ template <class E, int DK> struct DeltaGradTile {
 template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs A, int per)
 {
     using Op = Operand<E>;
-    using Tile = DeltaTile<E, DK>;
+    using Tile = DeltaTile<E, DK, 7>;
     using Grad = DeltaGradTile<E, DK>;
     constexpr int LO = Grad::LO, NM = DK == 128 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -972,7 +1065,7 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
     const int d = w % (DK / 16), m0 = NM == 2 ? 0 : w / (DK / 16), dk = 16 * d + col;
     const bool has = m0 < 2;
     // what is under way: a tile, and of 64 columns V and the state that enters, or dO and the gradient of the one that leaves
-    DeltaFetch<E, DK, 512> fetch;
+    DeltaFetch<E, DK, 512, 7> fetch;
     Steps<E> in;
     Columns<DK> st;
     const E *steps = nullptr;
@@ -1158,7 +1251,7 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
         wrong = wrong + end * 0.f;
         if (lane == 0) g.ends[w] = end;
         const int step = lane & 31, cut = s.cut()[step];      // before the next tile takes their place
-        const bool still = starts(s, step) || s.gate()[step] == 0.f;
+        const bool still = starts(s.cut(), step) || s.gate()[step] == 0.f;
         if (__any(wrong != 0.f) && lane == 0) g.wrong[w] = 1;
         else if (lane == 0) g.wrong[w] = 0;
         lds_barrier();
@@ -1195,14 +1288,15 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
 // passes as there are steps.  For tiles with numbers that are not finite, which k_delta_grad has left: a workgroup looks at AGAIN tiles.
 constexpr int AGAIN = 64;
 template <class E, int DK> struct DeltaSteps {
-    DeltaTile<E, DK> s;
+    DeltaTile<E, DK, 7> s;
     float sums[2][4];
     float rows[2][4][DK];               // of each wave, dq and dk of a step
 };
 template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs &A, DeltaSteps<E, DK> &g, long head, long tile)
 {
-    using Tile = DeltaTile<E, DK>;
+    using Tile = DeltaTile<E, DK, 7>;
     const int blocks = blocks_of(A.Dv);
+    const DeltaRecord &rec = ((const DeltaRecord *)A.records)[head * A.tiles + tile];
     Tile &s = g.s;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bi = (int)(head / A.H), h = (int)(head % A.H);
     const long t0 = tile * CH;
@@ -1217,14 +1311,14 @@ template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs 
             const long at = ((head * A.tiles + tile) * blocks + min(c0 / 16 + w, blocks - 1)) * 16 * DK;
             S.load(A.states + at, lane);
             if (c0 / 16 + w >= blocks) S.clear();
-            for (int i = 0; i < t; ++i) delta_step<E, DK>(s, S, i, mine ? (float)v[i * A.sv.ts + c] : 0.f, lane);
+            for (int i = 0; i < t; ++i) delta_step(s, rec, S, i, mine ? (float)v[i * A.sv.ts + c] : 0.f, lane);
             D.load(A.into + at, lane);
             if (c0 / 16 + w >= blocks) D.clear();
             for (int i = rows - 1; i > t; --i) {
-                delta_step_back<E, DK>(s, D, i, mine ? (float)dout[i * A.sdo.ts + c] : 0.f, A.scale, lane);
-                delta_pass_back<E, DK>(s, D, i);
+                delta_step_back(s, D, i, mine ? (float)dout[i * A.sdo.ts + c] : 0.f, A.scale, lane);
+                delta_pass_back(rec, D, i);
             }
-            if (starts(s, t)) S.clear();
+            if (starts(rec.cut, t)) S.clear();
             const Columns<DK> before = S;
             S.scaled(s.gate()[t]);
             const Columns<DK> held = S;
@@ -1232,7 +1326,7 @@ template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs 
             S.add(s.k + t * Tile::LD, s.beta()[t] * gap, lane);
             Columns<DK> full = D;
             full.add(s.q + t * Tile::LD, A.scale * d, lane);
-            const float dv = delta_step_back<E, DK>(s, D, t, d, A.scale, lane);
+            const float dv = delta_step_back(s, D, t, d, A.scale, lane);
             if (mine) {
                 float toward = full.dot(s.k + t * Tile::LD, lane) * gap, kept = 0.f;
 #pragma unroll
@@ -1271,7 +1365,7 @@ template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs 
             const float gt = s.gate()[t], bt = s.beta()[t];
             const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + t) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + t) * A.sb.ts + h * A.sb.hs];
             const float sr = (g.sums[0][0] + g.sums[0][1]) + (g.sums[0][2] + g.sums[0][3]), sa = (g.sums[1][0] + g.sums[1][1]) + (g.sums[1][2] + g.sums[1][3]);
-            ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(s, t) || gt == 0.f ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
+            ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(rec.cut, t) || gt == 0.f ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
             ((E *)A.db)[bi * A.sdb.bs + (t0 + t) * A.sdb.ts + h * A.sdb.hs] = (E)(bt * (1.f / (1.f + expf(b))) * sr);
         }
         __syncthreads();
@@ -1285,7 +1379,7 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_grad_s
     uint64_t left = __ballot(mine < all && A.again[min(mine, all - 1)]);      // the same for all waves
     for (; left; left &= left - 1) {
         const long id = first + __ffsll((unsigned long long)left) - 1, head = id / A.tiles, tile = id % A.tiles;
-        DeltaFetch<E, DK, 256> fetch;
+        DeltaFetch<E, DK, 256, 7> fetch;
         fetch.begin(A, (const DeltaRecord *)A.records, head, (int)(head / A.H), (int)(head % A.H), threadIdx.x);
         fetch.load(A, tile);
         __syncthreads();

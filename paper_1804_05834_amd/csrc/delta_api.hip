@@ -80,38 +80,86 @@ template <class F> bool delta_form(int32_t dtype, int32_t Dk, F &&go)
     auto wide = [&](auto e) { return width_of(Dk) == 32 ? go(e, Int<32>{}) : width_of(Dk) == 64 ? go(e, Int<64>{}) : go(e, Int<128>{}); };
     return dtype == DQN_F32 ? wide(float{}) : wide(seq::bf16{});
 }
-int64_t heads_of(const seq::DeltaIn &A) { return (int64_t)A.B * A.H; }
-template <class E, int DK> void launch_tiles(const seq::DeltaIn &A, float *records, hipStream_t st)
-{
-    if (A.tiles) seq::k_delta_tiles<E, DK><<<dim3((unsigned)((heads_of(A) * A.tiles + 3) / 4)), 256, 0, st>>>(A, (seq::DeltaRecord *)records);
-}
-template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, hipStream_t st)
-{
-    static std::atomic<uint64_t> granted{0};
-    constexpr int bytes = sizeof(seq::DeltaChain<E, DK>), waves = seq::DeltaChain<E, DK>::WAVES;
-    static_assert(bytes <= 160 * 1024, "within a compute unit's LDS");
-    if (!lds_granted((const void *)seq::k_delta<E, DK>, bytes, granted)) return false;
-    launch_tiles<E, DK>(A, A.records, st);
-    seq::k_delta<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, bytes, st>>>(A);
-    return true;
-}
-constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit
-template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, hipStream_t st)
-{
-    static std::atomic<uint64_t> back_granted{0}, granted{0};
-    constexpr int back = sizeof(seq::DeltaChain<E, DK>), waves = seq::DeltaChain<E, DK>::WAVES, bytes = sizeof(seq::DeltaGradTile<E, DK>);
-    if (!lds_granted((const void *)seq::k_delta_back<E, DK>, back, back_granted) || !lds_granted((const void *)seq::k_delta_grad<E, DK>, bytes, granted)) return false;
-    seq::k_delta_back<E, DK><<<dim3((unsigned)(heads_of(A) * ((A.Dv + 16 * waves - 1) / (16 * waves)))), 128 * waves, back, st>>>(A);
-    if (!A.tiles) return true;
-    static_assert(sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup gets");
-    const int64_t all = heads_of(A) * A.tiles, per = std::max<int64_t>(1, (all + GRAD_GROUPS - 1) / GRAD_GROUPS);
-    seq::k_delta_grad<E, DK><<<dim3((unsigned)((all + per - 1) / per)), 512, bytes, st>>>(A, (int)per);
-    seq::k_delta_grad_steps<E, DK><<<dim3((unsigned)((heads_of(A) * A.tiles + seq::AGAIN - 1) / seq::AGAIN)), 256, sizeof(seq::DeltaSteps<E, DK>), st>>>(A);
-    return true;
-}
 size_t record_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * sizeof(seq::DeltaRecord); }
 // a state for each tile, padded as the kernels hold them
 size_t state_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * width_of(s.Dk) * ((s.Dv + 15) / 16 * 16) * 4; }
+
+// Ranges of a head's tiles, where there are fewer workgroups of a chain than compute units.  All of its tiles are gone through three times then
+// (the maps take as many columns again), so that fewer than four ranges would not pay.
+constexpr int64_t UNITS = 256, LEAST_TILES = 4, LEAST_RANGES = 4, MOST_RANGES = 64;
+template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t tiles, int Dv)
+{
+    constexpr int waves = seq::DeltaChain<E, DK>::WAVES;
+    const int64_t groups = heads * (((Dv + 15) / 16 + waves - 1) / waves);
+    const int64_t n = groups ? std::min({UNITS / groups, tiles / LEAST_TILES, MOST_RANGES}) : 1;
+    seq::DeltaRanges R{1, (long)tiles, nullptr, nullptr, nullptr};
+    if (n < LEAST_RANGES) return R;
+    R.per = (long)((tiles + n - 1) / n);
+    R.ranges = (int)((tiles + R.per - 1) / R.per);
+    return R;
+}
+size_t range_bytes(const seq::DeltaRanges &R, const DeltaSizes &s)
+{
+    if (R.ranges == 1) return 0;
+    return ((size_t)s.B * s.H * R.ranges * ((size_t)width_of(s.Dk) * width_of(s.Dk) + 2 * (size_t)s.Dk * s.Dv) * 4 + 15) / 16 * 16;
+}
+size_t ranges_workspace(const DeltaSizes &s)
+{
+    size_t n = 0;
+    delta_form(s.dtype, s.Dk, [&](auto e, auto dk) { return n = range_bytes(ranges_of<decltype(e), dk.value>((int64_t)s.B * s.H, tiles_of(s.T), s.Dv), s), true; });
+    return n;
+}
+template <class E, int DK> seq::DeltaRanges ranges_at(const seq::DeltaIn &A, void *workspace)
+{
+    seq::DeltaRanges R = ranges_of<E, DK>((int64_t)A.B * A.H, A.tiles, A.Dv);
+    const int64_t n = (int64_t)A.B * A.H * R.ranges, size = (int64_t)A.Dk * A.Dv;
+    R.m = (float *)workspace;
+    R.b = R.m + n * DK * DK;
+    R.first = R.b + n * size;
+    return R;
+}
+template <class E, int DK> unsigned chain_groups(const seq::DeltaIn &A, const seq::DeltaRanges &R, bool maps)
+{
+    constexpr int waves = seq::DeltaChain<E, DK>::WAVES;
+    return (unsigned)((int64_t)A.B * A.H * R.ranges * (((A.Dv + 15) / 16 + (maps ? DK / 16 : 0) + waves - 1) / waves));
+}
+template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *workspace, hipStream_t st)
+{
+    static std::atomic<uint64_t> granted{0}, maps_granted{0};
+    constexpr int bytes = sizeof(seq::DeltaChain<E, DK>), threads = seq::chain_threads<E, DK>;
+    static_assert(bytes <= 160 * 1024, "within a compute unit's LDS");
+    if (!lds_granted((const void *)seq::k_delta<E, DK, false>, bytes, granted) || !lds_granted((const void *)seq::k_delta<E, DK, true>, bytes, maps_granted)) return false;
+    const int64_t heads = (int64_t)A.B * A.H;
+    if (A.tiles) seq::k_delta_tiles<E, DK><<<dim3((unsigned)((heads * A.tiles + 3) / 4)), 256, 0, st>>>(A, (seq::DeltaRecord *)A.records);
+    const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
+    if (R.ranges > 1) {
+        seq::k_delta<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, bytes, st>>>(A, R);
+        seq::k_delta_join<DK, false><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 4 * DK, 0, st>>>(R, A.s0, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+    }
+    seq::k_delta<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, bytes, st>>>(A, R);
+    return true;
+}
+constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit
+template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, void *workspace, hipStream_t st)
+{
+    static std::atomic<uint64_t> back_granted{0}, maps_granted{0}, granted{0};
+    constexpr int back = sizeof(seq::DeltaChain<E, DK>), threads = seq::chain_threads<E, DK>, bytes = sizeof(seq::DeltaGradTile<E, DK>);
+    static_assert(bytes <= 160 * 1024 && sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup can have");
+    if (!lds_granted((const void *)seq::k_delta_back<E, DK, false>, back, back_granted) || !lds_granted((const void *)seq::k_delta_back<E, DK, true>, back, maps_granted) ||
+        !lds_granted((const void *)seq::k_delta_grad<E, DK>, bytes, granted)) return false;
+    const int64_t heads = (int64_t)A.B * A.H;
+    const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
+    if (R.ranges > 1) {
+        seq::k_delta_back<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, back, st>>>(A, R);
+        seq::k_delta_join<DK, true><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 4 * DK, 0, st>>>(R, A.dlast, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+    }
+    seq::k_delta_back<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, back, st>>>(A, R);
+    if (!A.tiles) return true;
+    const int64_t all = heads * A.tiles, per = std::max<int64_t>(1, (all + GRAD_GROUPS - 1) / GRAD_GROUPS);
+    seq::k_delta_grad<E, DK><<<dim3((unsigned)((all + per - 1) / per)), 512, bytes, st>>>(A, (int)per);
+    seq::k_delta_grad_steps<E, DK><<<dim3((unsigned)((all + seq::AGAIN - 1) / seq::AGAIN)), 256, sizeof(seq::DeltaSteps<E, DK>), st>>>(A);
+    return true;
+}
 
 }  // namespace
 
@@ -125,8 +173,8 @@ int32_t dqn_delta_sizes(int32_t dtype, int32_t B, int64_t T, int32_t H, int32_t 
     if (!carry || !forward_workspace || !backward_workspace) return bad(call, "NULL argument");
     if (const char *m = check_sizes(s)) return bad(call, m);
     *carry = state_bytes(s) + record_bytes(s);
-    *forward_workspace = record_bytes(s);
-    *backward_workspace = state_bytes(s) + (size_t)B * H * tiles_of(T) * 4;
+    *forward_workspace = ranges_workspace(s) + record_bytes(s);      // the records lie in `carry` if there is one
+    *backward_workspace = ranges_workspace(s) + state_bytes(s) + (size_t)B * H * tiles_of(T) * 4;
     return DQN_OK;
 }
 
@@ -141,18 +189,18 @@ int32_t dqn_delta_forward(const dqn_delta_args *args, void *stream)
     if (!at(d.s0, 4) || !at(d.s_last, 4) || !at(d.carry, 16)) return bad(call, "a state is not aligned to its elements, or carry to 16 bytes");
     if (!std::isfinite(d.scale)) return bad(call, "scale must be finite");
     if (!d.B || !d.H) return DQN_OK;
-    if (d.T && !d.carry && (!d.workspace || !at(d.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
+    if (d.T && (!d.workspace || !at(d.workspace, 16))) return bad(call, "workspace is NULL or not 16-byte aligned");
     if (d.T)
         for (const char *m : {check_heads(d.q, d.q_s, d.B, d.T, d.H, d.Dk, d.dtype, false), check_heads(d.k, d.k_s, d.B, d.T, d.H, d.Dk, d.dtype, false),
                               check_heads(d.v, d.v_s, d.B, d.T, d.H, d.Dv, d.dtype, false), check_heads(d.f, d.f_s, d.B, d.T, d.H, 1, d.dtype, false),
                               check_heads(d.b, d.b_s, d.B, d.T, d.H, 1, d.dtype, false), check_heads(d.o, d.o_s, d.B, d.T, d.H, d.Dv, d.dtype, true)})
             if (m) return bad(call, m);
-    float *records = (float *)(d.carry ? (uint8_t *)d.carry + state_bytes(s) : (uint8_t *)d.workspace);
+    float *records = (float *)(d.carry ? (uint8_t *)d.carry + state_bytes(s) : (uint8_t *)d.workspace + ranges_workspace(s));
     seq::DeltaArgs A{};
     static_cast<seq::DeltaIn &>(A) = inputs(d);
     A.s0 = d.s0; A.o = d.o; A.so = strides(d.o_s); A.last = d.s_last; A.states = d.carry; A.records = records;
     hipStream_t st = (hipStream_t)stream;
-    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta<decltype(e), dk.value>(A, st); });
+    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta<decltype(e), dk.value>(A, d.workspace, st); });
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }
 
@@ -183,9 +231,9 @@ int32_t dqn_delta_backward(const dqn_delta_grad_args *args, void *stream)
     A.dout = d.dout; A.sdo = strides(d.dout_s); A.states = d.carry; A.records = (const float *)((const uint8_t *)d.carry + state_bytes(s)); A.dlast = d.dlast;
     A.dq = d.dq; A.dk = d.dk; A.dv = d.dv; A.df = d.df; A.db = d.db;
     A.sdq = strides(d.dq_s); A.sdk = strides(d.dk_s); A.sdv = strides(d.dv_s); A.sdf = strides(d.df_s); A.sdb = strides(d.db_s);
-    A.ds0 = d.ds0; A.into = (float *)d.workspace; A.again = (int *)((uint8_t *)d.workspace + state_bytes(s));
+    A.ds0 = d.ds0; A.into = (float *)((uint8_t *)d.workspace + ranges_workspace(s)); A.again = (int *)((uint8_t *)A.into + state_bytes(s));
     hipStream_t st = (hipStream_t)stream;
-    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta_grad<decltype(e), dk.value>(A, st); });
+    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta_grad<decltype(e), dk.value>(A, d.workspace, st); });
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }
 

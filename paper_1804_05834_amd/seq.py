@@ -256,7 +256,7 @@ def delta(q, k, v, f, b, s0=None, reset=None, scale=1.0, save=False, out=None, l
         lp = _flat(last, "last", torch.float32, state, dev)
     carry = torch.empty(carry_n // 4, dtype=torch.float32, device=q.device) if save else None
     rp, rb, rt = _reset(reset, B, T, dev)
-    work, wp = _scratch(0 if save else work_n, q.device)
+    work, wp = _scratch(work_n, q.device)
     args = DELTA_ARGS.pack(kind, B, H, Dk, Dv, scale, T, *at, *strides, 0 if s0 is None else _flat(s0, "s0", torch.float32, state, dev),
                            rp, rb, rt, op, *os_[:3], lp, carry.data_ptr() if save else 0, wp)
     _call(lib().dqn_delta_forward(args, _raw_stream(dev)))

@@ -78,6 +78,31 @@ def test_delta_widths(dtype, Dk, Dv):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv,resets", [(512, 1, 1, 16, 16, 0), (611, 1, 2, 24, 40, 0.01), (2049, 1, 1, 64, 64, 0.002), (1100, 3, 2, 33, 20, 0.01), (700, 1, 1, 128, 128, 0), (999, 2, 1, 100, 72, 0.003)])
+def test_delta_few_heads_and_many_steps(dtype, T, B, H, Dk, Dv, resets):
+    """Tiles in ranges, each from the state that the maps of those before it give."""
+    c = Delta(T, dtype, B, T, H, Dk, Dv, resets=resets)
+    c.check(*c.run())
+
+
+def test_delta_ranges_and_what_is_not_finite():
+    """A NaN in one range: gone with the next episode, there till then; a state that is NaN at the start ends at the first reset."""
+    clean, c = (Delta(3, "bf16", 1, 1024, 2, 32, 32, resets=0) for _ in range(2))
+    for x in (clean, c):
+        x.reset = torch.zeros(1, 1024, dtype=torch.uint8, device=DEV)
+        x.reset[0, [300, 700]] = 1
+    want = clean.run()
+    c.s0[:] = float("nan")
+    c.v[0, 400, 0, 3] = float("inf")
+    got = c.run()
+    assert not torch.isfinite(got[0][0, :300]).any()
+    assert torch.isfinite(got[0][0, 300:400]).all() and torch.isfinite(got[0][0, 300:, 1]).all() and torch.isfinite(got[0][0, 700:]).all() and torch.isfinite(got[1]).all()
+    assert not torch.isfinite(got[0][0, 400:700, 0, 3]).any() and torch.isfinite(got[0][0, 400:700, 0, :3]).all()
+    for x, y in zip(got[2][:5], want[2][:5]):       # half a step of bf16 off the definition, each
+        assert torch.allclose(x[0, 700:].float(), y[0, 700:].float(), rtol=2.0 ** -7, atol=2.0 ** -8) and torch.allclose(x[0, 300:, 1].float(), y[0, 300:, 1].float(), rtol=2.0 ** -7, atol=2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("state,resets", [(False, 0), (True, 0), (False, 0.3), (True, 1.0)])
 def test_delta_states_and_episodes(dtype, state, resets):
     c = Delta(5, dtype, 3, 100, 2, 12, 20, state=state, resets=resets)
