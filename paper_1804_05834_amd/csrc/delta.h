@@ -711,6 +711,7 @@ template <class E, int DK> struct DeltaChain {
     f4 steps[2][WAVES][2][64];            // U; P^T dO
 };
 // How tiles are cut into ranges, and what is kept of each: M [DK][DK], B and the state it begins with [Dk][Dv]
+constexpr int MOST_RANGES = 64;
 struct DeltaRanges {
     int ranges;
     long per;                             // tiles of a range, but for the last
@@ -954,45 +955,110 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
 }
 
 // From range to range: the state each begins with, forward from s0 or backward from dlast.  A workgroup per head and 16 columns, a wave per 16 rows;
-// a result of 16 x 16 is the next right operand as it is, in its place in LDS.  What enters a range with an episode's start leaves nothing,
-// whatever it is.
-template <int DK, bool BACK> __global__ __launch_bounds__(4 * DK) void k_delta_join(DeltaRanges R, const float *given, const DeltaRecord *records, long tiles, int Dk, int Dv)
+// a result of 16 x 16 is the next right operand as it is, in its place in LDS.  As many waves more take it from there to memory: a wave that loads
+// maps would wait for its own stores (32 ranges of 128 x 128: 79 us against 69; what is left is bringing 64 KB a range to each of few compute
+// units, and two ranges ahead it is slower).  What enters a range with an episode's start leaves nothing, whatever it is.
+template <int DK, bool BACK> __global__ __launch_bounds__(8 * DK) void k_delta_join(DeltaRanges R, const float *given, const DeltaRecord *records, long tiles, int Dk, int Dv)
 {
     __shared__ f4 state[2][DK / 16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4;
+    __shared__ int forgets[MOST_RANGES];      // whether an episode starts in a range
+    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % (DK / 16), g = lane >> 4;
+    const bool stores = threadIdx.x >= 4 * DK;
     const unsigned blocks = (unsigned)blocks_of(Dv), head = blockIdx.x / blocks;
     const int c = 16 * (int)(blockIdx.x % blocks) + (lane & 15), row = 16 * w + 4 * g;
     const long size = (long)Dk * Dv, base = (long)head * R.ranges;
     auto in = [&](int e) { return c < Dv && row + e < Dk; };
-    f4 S = {};
+    auto range = [&](int i) { return BACK ? R.ranges - 1 - i : i; };
+    for (int r = threadIdx.x; r < R.ranges; r += 8 * DK) forgets[r] = 0;
+    __syncthreads();
+    for (long t = threadIdx.x; t < tiles; t += 8 * DK)
+        if (records[head * tiles + t].cut[CH - 1]) forgets[t / R.per] = 1;
+    if (stores) {
+        for (int i = 0; i < R.ranges; ++i) {
+            lds_barrier();
+            const f4 S = state[i & 1][w][lane];
+            float *first = R.first + (base + range(i)) * size;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (in(e)) first[(row + e) * Dv + c] = S[e];
+        }
+        return;
+    }
+    f4 S = {}, a[DK / 16], add;
     if (given)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (in(e)) S[e] = given[head * size + (row + e) * Dv + c];
-    for (int i = 0; i < R.ranges; ++i) {
-        const int r = BACK ? R.ranges - 1 - i : i;
-        float *first = R.first + (base + r) * size;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (in(e)) first[(row + e) * Dv + c] = S[e];
-        if (i + 1 == R.ranges) break;
-        const float *m = R.m + (base + r) * DK * DK + (16 * w + (lane & 15)) * DK + 4 * g, *b = R.b + (base + r) * size;
-        f4 a[DK / 16], next = {};
+    // a range's map is under way while the one before is applied
+    auto get = [&](int i) {
+        const float *m = R.m + (base + range(i)) * DK * DK + (16 * w + (lane & 15)) * DK + 4 * g, *b = R.b + (base + range(i)) * size;
 #pragma unroll
         for (int kb = 0; kb < DK / 16; ++kb) a[kb] = load<4>(m + 16 * kb);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (in(e)) next[e] = b[(row + e) * Dv + c];
-        int cut = 0;
-        for (long t = r * R.per + threadIdx.x; t < min(tiles, (r + 1) * R.per); t += 4 * DK) cut |= records[head * tiles + t].cut[CH - 1];
+        for (int e = 0; e < 4; ++e) add[e] = b[min(row + e, Dk - 1) * Dv + min(c, Dv - 1)];
+    };
+    get(0);
+    for (int i = 0; i < R.ranges; ++i) {
         state[i & 1][w][lane] = S;
-        const bool forgets = __syncthreads_or(cut);
-        if (!forgets) {
+        lds_barrier();
+        if (i + 1 == R.ranges) break;
+        f4 next, other = {};
 #pragma unroll
-            for (int kb = 0; kb < DK / 16; ++kb) next = mm4(a[kb], state[i & 1][kb][lane], next);
+        for (int e = 0; e < 4; ++e) next[e] = in(e) ? add[e] : 0.f;
+        if (!forgets[range(i)]) {
+#pragma unroll
+            for (int kb = 0; kb < DK / 16; kb += 2) {
+                next = mm4(a[kb], state[i & 1][kb][lane], next);
+                other = mm4(a[kb + 1], state[i & 1][kb + 1][lane], other);
+            }
+            next += other;
         }
+        get(i + 1);      // of the last range, whose map nobody needs, too
         S = next;
     }
+}
+
+// Few steps, of an acting agent say: the definition, step by step, a wave per 16 columns of a head's state.
+constexpr long STEPS_MOST = 8;
+template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_few(DeltaArgs A)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4, blocks = blocks_of(A.Dv);
+    const unsigned at = blockIdx.x * 4 + (threadIdx.x >> 6), head = at / (unsigned)blocks;
+    if (head >= (unsigned)(A.B * A.H)) return;
+    const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), c = 16 * (int)(at % (unsigned)blocks) + (lane & 15);
+    const bool mine = c < A.Dv;
+    const E *q = head_of<E>(A.q, A.sq, bi, h), *k = head_of<E>(A.k, A.sk, bi, h), *v = head_of<E>(A.v, A.sv, bi, h), *f = head_of<E>(A.f, A.sf, bi, h), *b = head_of<E>(A.b, A.sb, bi, h);
+    E *o = head_of<E>(A.o, A.so, bi, h);
+    const long size = (long)A.Dk * A.Dv;
+    Columns<DK> S;
+    S.get(A.s0 ? A.s0 + head * size : nullptr, A.Dk, A.Dv, c, lane);
+    for (long t = 0; t < A.T; ++t) {
+        vec<E, 8> kt[DK / 32], qt[DK / 32];
+#pragma unroll
+        for (int p = 0; p < DK / 32; ++p) {
+            kt[p] = load8<E>(k + t * A.sk.ts, 32 * p + 8 * g, A.Dk, true, A.wide);
+            qt[p] = load8<E>(q + t * A.sq.ts, 32 * p + 8 * g, A.Dk, true, A.wide);
+        }
+        const float x = (float)v[t * A.sv.ts + min(c, A.Dv - 1)], gate = 1.f / (1.f + expf(-(float)f[t * A.sf.ts])), rate = 1.f / (1.f + expf(-(float)b[t * A.sb.ts]));
+        if (A.reset && A.reset[bi * A.reset_bs + t * A.reset_ts]) S.clear();
+        S.scaled(gate);
+        float held = 0.f, out = 0.f;
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) held = fmaf((float)kt[n >> 1][4 * (n & 1) + e], S.s[n][e], held);
+        const float u = rate * ((mine ? x : 0.f) - groups_sum(held));
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                S.s[n][e] = fmaf((float)kt[n >> 1][4 * (n & 1) + e], u, S.s[n][e]);
+                out = fmaf((float)qt[n >> 1][4 * (n & 1) + e], S.s[n][e], out);
+            }
+        out = groups_sum(out);
+        if (mine && g == 0) o[t * A.so.ts + c] = (E)(A.scale * out);
+    }
+    if (A.last) S.put(A.last + head * size, A.Dk, A.Dv, c, lane);
 }
 
 // ---------------------------------------------------------------- gradients

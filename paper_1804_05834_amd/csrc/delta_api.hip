@@ -86,12 +86,12 @@ size_t state_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.
 
 // Ranges of a head's tiles, where there are fewer workgroups of a chain than compute units.  All of its tiles are gone through three times then
 // (the maps take as many columns again), so that fewer than four ranges would not pay.
-constexpr int64_t UNITS = 256, LEAST_TILES = 4, LEAST_RANGES = 4, MOST_RANGES = 64;
+constexpr int64_t UNITS = 256, LEAST_TILES = 4, LEAST_RANGES = 4;
 template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t tiles, int Dv)
 {
     constexpr int waves = seq::DeltaChain<E, DK>::WAVES;
     const int64_t groups = heads * (((Dv + 15) / 16 + waves - 1) / waves);
-    const int64_t n = groups ? std::min({UNITS / groups, tiles / LEAST_TILES, MOST_RANGES}) : 1;
+    const int64_t n = groups ? std::min({UNITS / groups, tiles / LEAST_TILES, (int64_t)seq::MOST_RANGES}) : 1;
     seq::DeltaRanges R{1, (long)tiles, nullptr, nullptr, nullptr};
     if (n < LEAST_RANGES) return R;
     R.per = (long)((tiles + n - 1) / n);
@@ -130,11 +130,15 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
     static_assert(bytes <= 160 * 1024, "within a compute unit's LDS");
     if (!lds_granted((const void *)seq::k_delta<E, DK, false>, bytes, granted) || !lds_granted((const void *)seq::k_delta<E, DK, true>, bytes, maps_granted)) return false;
     const int64_t heads = (int64_t)A.B * A.H;
+    if (A.T <= seq::STEPS_MOST && !A.states) {
+        seq::k_delta_few<E, DK><<<dim3((unsigned)((heads * ((A.Dv + 15) / 16) + 3) / 4)), 256, 0, st>>>(A);
+        return true;
+    }
     if (A.tiles) seq::k_delta_tiles<E, DK><<<dim3((unsigned)((heads * A.tiles + 3) / 4)), 256, 0, st>>>(A, (seq::DeltaRecord *)A.records);
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
         seq::k_delta<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, bytes, st>>>(A, R);
-        seq::k_delta_join<DK, false><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 4 * DK, 0, st>>>(R, A.s0, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+        seq::k_delta_join<DK, false><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.s0, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
     }
     seq::k_delta<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, bytes, st>>>(A, R);
     return true;
@@ -151,7 +155,7 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, v
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
         seq::k_delta_back<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, back, st>>>(A, R);
-        seq::k_delta_join<DK, true><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 4 * DK, 0, st>>>(R, A.dlast, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+        seq::k_delta_join<DK, true><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.dlast, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
     }
     seq::k_delta_back<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, back, st>>>(A, R);
     if (!A.tiles) return true;

@@ -115,6 +115,20 @@ def test_delta_states_and_episodes(dtype, state, resets):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,Dk,Dv", [(1, 64, 64), (1, 33, 20), (3, 128, 128), (8, 16, 5), (9, 16, 5)])
+def test_delta_few_steps(dtype, T, Dk, Dv):
+    """Without what a backward pass needs: step by step up to eight steps, also with the state in place."""
+    c = Delta(T + Dk, dtype, 5, T, 3, Dk, Dv, resets=0.2)
+    out, bound = c.exact()[:2]
+    state = c.s0.clone()
+    o, last = seq.delta(*c.inputs(), s0=state, reset=c.reset, scale=c.scale, last=state)
+    ref.within(host(o), out[0], bound[0], (3,), c.dt is torch.bfloat16, "o")
+    ref.within(host(last), out[1], bound[1], (2, 3), False, "last")
+    o2, last2 = seq.delta(*c.inputs(), s0=c.s0, reset=c.reset, scale=c.scale)
+    assert torch.equal(o, o2) and torch.equal(last, last2)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_delta_keys_that_repeat(dtype):
     """The same key at every step and rates near one: N is full, what is written replaces what was."""
     c = Delta(6, dtype, 1, 150, 2, 16, 16)
