@@ -6,42 +6,48 @@
 // The products are the cost, 2 r^2 c + 2 r^3 + 2 r^2 c operations a round, a fourth less with A and A^2 formed on one side of their
 // diagonal.  Operands are pairs of bf16, hi + lo, which hold 16 bits of a number, and a product takes three matrix instructions,
 // hi hi + hi lo + lo hi: rounding X or A to one bf16 would put the result 2^-9 off at every round, pairs are 2^-17 off, and fp32
-// instructions have a sixteenth of the rate.  Sums are fp32.  All operands lie with their inner dimension in one piece: A and B are
-// symmetric, and X is kept as its transposed as well.  Sizes are padded with zeros to multiples of TILE, so that no product looks at bounds.
+// instructions have a sixteenth of the rate.  Sums are fp32.
+//
+// X is kept as its transposed Y [c][r] alone.  B X has rows of B and rows of Y as operands, whose inner dimension lies in one piece; what a lane
+// holds of a result is four neighbours of a row of the new Y.  X X^T has columns of Y on both sides, which the transposing LDS reads take.
+// A row lies in memory as 32 numbers' hi, the same numbers' lo, the next 32 numbers: 128 bytes, a line, for 32 of the inner dimension.
+// Sizes are padded with zeros to multiples of PAD, so that no product looks at bounds of the inner dimension.
 #pragma once
 #include "seq_common.h"
 
 namespace seq {
 
-constexpr int MT = 64;                  // rows and columns of a tile of a product
+constexpr int PAD = 64;
 constexpr int MUON_CHUNK = 4096;        // elements of a partial sum of squares
+constexpr int TILES[3] = {64, 128, 256};       // rows and columns of a workgroup's part of a product
 
 struct MuonMatrix {
     float *p, *m;
     const void *g;
     uint16_t *copy;
-    bf16 *x, *xt[2], *a, *b;            // planes: all hi, then all lo
+    bf16 *y[2], *a, *b;
     double *sums;
     long rows, cols;
     int rp, cp;                         // the shorter and the longer side, padded
-    int tall;                           // more rows than columns: x is the transposed
+    int tall;                           // more rows than columns: y is the matrix, else its transposed
     float decay, scale;
     int chunks;                         // of its elements
-    int first_chunk, first_half, first_whole;   // its first workgroup in a launch over chunks, tiles on and below the diagonal of A, tiles of X
+    int first_chunk, first_start;       // its first workgroup in a launch over chunks, over parts of 64 x 64,
+    int first_half[3], first_whole[3];  // over parts of A on and below the diagonal, over parts of X, by their size
 };
 struct MuonArgs {
     const MuonMatrix *matrices;
-    int count, nesterov;
+    int count, nesterov, from;          // from: which Y holds X
     float mu, eps, lr, a, b, c;
 };
 
 // The matrix that workgroup `i` of a launch belongs to.
-template <int MuonMatrix::*FIRST> __device__ __forceinline__ const MuonMatrix &matrix_of(const MuonArgs &A, int i)
+template <class F> __device__ __forceinline__ const MuonMatrix &matrix_of(const MuonArgs &A, int i, F &&first)
 {
     int lo = 0, hi = A.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        (A.matrices[mid].*FIRST <= i ? lo : hi) = mid;
+        (first(A.matrices[mid]) <= i ? lo : hi) = mid;
     }
     return A.matrices[lo];
 }
@@ -49,7 +55,7 @@ template <int MuonMatrix::*FIRST> __device__ __forceinline__ const MuonMatrix &m
 template <class G> __global__ __launch_bounds__(256) void k_muon_momentum(MuonArgs A)
 {
     __shared__ double sh[4];
-    const MuonMatrix &M = matrix_of<&MuonMatrix::first_chunk>(A, blockIdx.x);
+    const MuonMatrix &M = matrix_of(A, blockIdx.x, [](const MuonMatrix &m) { return m.first_chunk; });
     const int chunk = blockIdx.x - M.first_chunk;
     const long first = (long)chunk * MUON_CHUNK, n = min((long)MUON_CHUNK, M.rows * M.cols - first);
     double sum = 0.0;
@@ -71,13 +77,16 @@ __device__ __forceinline__ void halves_of(float v, bf16 &hi, bf16 &lo)
     lo = (bf16)(v - (float)hi);
 }
 
-// X and its transposed, a tile of 64 x 64 per workgroup.
+// where the hi of number (row, col) of a matrix `width` wide lies; its lo is 32 further
+__device__ __forceinline__ long hi_at(long row, int col, int width) { return row * 2 * width + (col >> 5) * 64 + (col & 31); }
+
+// Y, 64 x 64 of it per workgroup.
 template <class G> __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A)
 {
-    __shared__ float t[MT][MT + 1];
+    __shared__ float t[64][65];
     __shared__ double sh[4];
-    const MuonMatrix &M = matrix_of<&MuonMatrix::first_whole>(A, blockIdx.x);
-    const int tile = blockIdx.x - M.first_whole, across = M.cp / MT, ti = tile / across, tj = tile % across;
+    const MuonMatrix &M = matrix_of(A, blockIdx.x, [](const MuonMatrix &m) { return m.first_start; });
+    const int tile = blockIdx.x - M.first_start, across = M.rp / 64, ti = tile / across, tj = tile % across;      // rows of Y 64 ti.., columns 64 tj..
     double sum = 0.0;
     for (int i = threadIdx.x; i < M.chunks; i += 256) sum += M.sums[i];
 #pragma unroll
@@ -86,154 +95,201 @@ template <class G> __global__ __launch_bounds__(256) void k_muon_start(MuonArgs 
     __syncthreads();
     const float inv = 1.f / ((float)sqrt((sh[0] + sh[1]) + (sh[2] + sh[3])) + A.eps);
     const int c = threadIdx.x & 63;
-    for (int r = threadIdx.x >> 6; r < MT; r += 4) {
-        // row and column as they lie in memory; in t as they lie in x
-        const long row = (long)(M.tall ? tj : ti) * MT + r, col = (long)(M.tall ? ti : tj) * MT + c;
+    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
+        const long row = (long)(M.tall ? ti : tj) * 64 + r, col = (long)(M.tall ? tj : ti) * 64 + c;      // as they lie in memory
         float v = 0.f;
         if (row < M.rows && col < M.cols) {
             const long at = row * M.cols + col;
             const float m = M.m[at];
             v = (A.nesterov ? fmaf(A.mu, m, (float)((const G *)M.g)[at]) : m) * inv;
         }
-        (M.tall ? t[c][r] : t[r][c]) = v;
+        (M.tall ? t[r][c] : t[c][r]) = v;
     }
     __syncthreads();
-    const long plane = (long)M.rp * M.cp;
-    for (int r = threadIdx.x >> 6; r < MT; r += 4) {
-        bf16 hi, lo;
-        halves_of(t[r][c], hi, lo);
-        bf16 *x = M.x + (long)(ti * MT + r) * M.cp + tj * MT + c;
-        x[0] = hi;
-        x[plane] = lo;
-        halves_of(t[c][r], hi, lo);
-        x = M.xt[0] + (long)(tj * MT + r) * M.rp + ti * MT + c;
-        x[0] = hi;
-        x[plane] = lo;
+    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
+        bf16 *y = M.y[0] + hi_at(ti * 64 + r, tj * 64 + c, M.rp);
+        halves_of(t[r][c], y[0], y[32]);
     }
 }
 
 using f4 = vec<float, 4>;
-
-// Rows i0.. of L times rows j0.. of R, both [.][K] in planes, inner dimension in one piece: 32 x 32 of each wave's, lane l holding rows
-// 4 (l / 16).. of column l % 16 of each of four 16 x 16.
-constexpr int MK = 64, MLD = MK + 8;    // inner dimension of a step, and its rows' distance in LDS
-struct MuonTiles {
-    bf16 l[2][MT * MLD], r[2][MT * MLD];
-};
-__device__ __forceinline__ void muon_product(MuonTiles &s, const bf16 *L, long lplane, int i0, const bf16 *R, long rplane, int j0, int K, f4 (&acc)[2][2])
+using b4 = vec<bf16, 4>;
+using b8 = vec<bf16, 8>;
+__device__ __forceinline__ f4 whole_of(const bf16 *hi)
 {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wi = 32 * (w >> 1), wj = 32 * (w & 1);
-    for (int k0 = 0; k0 < K; k0 += MK) {
-        __syncthreads();
-        for (int e = tid; e < MT * MK / 8; e += 256) {
-            const int r = e / (MK / 8), c = e % (MK / 8) * 8;
+    const b4 a = load<4>(hi), b = load<4>(hi + 32);
+    return f4{(float)a[0] + (float)b[0], (float)a[1] + (float)b[1], (float)a[2] + (float)b[2], (float)a[3] + (float)b[3]};
+}
+__device__ __forceinline__ void put_halves(bf16 *hi, f4 v)
+{
+    b4 a, b;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                *reinterpret_cast<vec<bf16, 8> *>(s.l[h] + r * MLD + c) = *reinterpret_cast<const vec<bf16, 8> *>(L + h * lplane + (long)(i0 + r) * K + k0 + c);
-                *reinterpret_cast<vec<bf16, 8> *>(s.r[h] + r * MLD + c) = *reinterpret_cast<const vec<bf16, 8> *>(R + h * rplane + (long)(j0 + r) * K + k0 + c);
+    for (int e = 0; e < 4; ++e) {
+        a[e] = (bf16)v[e];
+        b[e] = (bf16)(v[e] - (float)a[e]);
+    }
+    store<4>(hi, a);
+    store<4>(hi + 32, b);
+}
+
+// N x N numbers of L R^T (COLUMNS false: rows i0.. of L, j0.. of R, both K wide) or of L^T R (COLUMNS: columns i0.., j0.. of the same matrix of K rows,
+// `width` wide), by WM x WN waves, a wave having MI x NI results of 16 x 16, a lane rows 4 (l / 16).. of column l % 16 of each.  32 of K a step, two
+// steps' operands in LDS: while one is multiplied, the next comes from memory past the registers.
+// LDS, rows: a row's 128 bytes in eight pieces of 16, four of hi and four of lo; piece c of row r has the place c ^ (r / 2 % 8).  Columns: a row has 4 N
+// bytes in pieces of 32, sixteen columns' hi or lo; piece c of row r has the place c ^ (r % 8).  So the lanes that LDS serves together meet each of
+// its banks once.
+template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
+    static constexpr int WAVES = WM * WN, MI = N / WM / 16, NI = N / WN / 16, SIDE = N * 128, STAGE = 2 * SIDE, LOADS = STAGE / 1024 / WAVES;
+    static_assert(STAGE % (1024 * WAVES) == 0 && LOADS >= 1, "whole loads of a wave");
+    f4 acc[MI][NI];
+    __device__ __forceinline__ void run(uint8_t *lds, const bf16 *L, const bf16 *R, int i0, int j0, int rows_l, int rows_r, int width, int K)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+        const uint8_t *src[LOADS];
+        const long pitch = COLUMNS ? 4l * width : 4l * K, step_bytes = COLUMNS ? 32 * pitch : 128;
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            const int at = (wave * LOADS + q) * 1024 + lane * 16, side = at / SIDE, in = at % SIDE;
+            const bf16 *from = side ? R : L;
+            const int first = side ? j0 : i0, last = side ? rows_r : rows_l;
+            if (COLUMNS) {
+                const int r = in / (4 * N), piece = in % (4 * N) / 32 ^ (r & 7);
+                const int block = min(first / 32 + piece / 4, width / 32 - 1);        // beyond the last columns: numbers that nobody keeps
+                src[q] = (const uint8_t *)from + r * pitch + block * 128 + (piece & 3) * 32 + (in & 16);
+            } else {
+                const int r = in / 128, piece = in % 128 / 16 ^ (r >> 1 & 7);
+                src[q] = (const uint8_t *)from + min(first + r, last - 1) * pitch + piece * 16;
             }
         }
-        __syncthreads();
+        auto fetch = [&](int step) {
+            uint8_t *to = lds + (step & 1) * STAGE + wave * LOADS * 1024;
 #pragma unroll
-        for (int kk = 0; kk < MK; kk += 32) {
-            vec<bf16, 8> a[2][2], b[2][2];
+            for (int q = 0; q < LOADS; ++q) to_lds(src[q] + step * step_bytes, to + q * 1024);
+        };
+        // 16 rows (columns) from `first` on as an operand, its hi and its lo
+        auto operand = [&](const uint8_t *side, int first, b8 (&v)[2]) {
+            if constexpr (COLUMNS) {
+                using s4 = vec<short, 4>;
+                typedef __attribute__((address_space(3))) s4 *At;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    a[h][n] = *reinterpret_cast<const vec<bf16, 8> *>(s.l[h] + (wi + 16 * n + (lane & 15)) * MLD + kk + 8 * (lane >> 4));
-                    b[h][n] = *reinterpret_cast<const vec<bf16, 8> *>(s.r[h] + (wj + 16 * n + (lane & 15)) * MLD + kk + 8 * (lane >> 4));
+                for (int h = 0; h < 2; ++h) {
+                    const int piece = first / 32 * 4 + 2 * h + (first >> 4 & 1), r = 8 * g + (i >> 2);
+                    const uint8_t *a = side + r * (4 * N) + (piece ^ (i >> 2)) * 32 + (i & 3) * 8;
+                    const uint8_t *b = side + (r + 4) * (4 * N) + (piece ^ ((i >> 2) + 4)) * 32 + (i & 3) * 8;
+                    const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)a), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)b);
+                    v[h] = __builtin_bit_cast(b8, (vec<short, 8>){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
                 }
+            } else {
+                const int place = (first + i) * 128 + (g ^ (i >> 1)) * 16;
+                v[0] = *reinterpret_cast<const b8 *>(side + place);
+                v[1] = *reinterpret_cast<const b8 *>(side + (place ^ 64));
+            }
+        };
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+        for (int x = 0; x < MI; ++x)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][i], b[0][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0][i], b[1][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
-                }
+            for (int y = 0; y < NI; ++y) acc[x][y] = f4{};
+        const int wm = wave % WM * MI * 16, wn = wave / WM * NI * 16, steps = K / 32;
+        fetch(0);
+        for (int step = 0; step < steps; ++step) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (step + 1 < steps) fetch(step + 1);
+            const uint8_t *l = lds + (step & 1) * STAGE, *r = l + SIDE;
+            b8 b[NI][2];
+#pragma unroll
+            for (int y = 0; y < NI; ++y) operand(r, wn + 16 * y, b[y]);
+#pragma unroll
+            for (int x = 0; x < MI; ++x) {
+                b8 a[2];
+                operand(l, wm + 16 * x, a);
+#pragma unroll
+                for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b[y][0], acc[x][y], 0, 0, 0);
+#pragma unroll
+                for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[y][1], acc[x][y], 0, 0, 0);
+#pragma unroll
+                for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[y][0], acc[x][y], 0, 0, 0);
+            }
         }
     }
+    // f(row, column, the four numbers of rows row.. and that column)
+    template <class F> __device__ __forceinline__ void each(F &&f)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % WM * MI * 16, wn = wave / WM * NI * 16;
+#pragma unroll
+        for (int x = 0; x < MI; ++x)
+#pragma unroll
+            for (int y = 0; y < NI; ++y) f(wm + 16 * x + 4 * (lane >> 4), wn + 16 * y + (lane & 15), acc[x][y]);
+    }
+};
+constexpr int muon_wn(int n) { return n == 256 ? 4 : 2; }
+constexpr int muon_threads(int n) { return 128 * muon_wn(n); }
+
+// Neighbouring parts on the same XCD (workgroups go round the eight), whose L2 holds what they read together.
+__device__ __forceinline__ int muon_part()
+{
+    const int all = gridDim.x, x = blockIdx.x & 7, q = all / 8, r = all % 8;
+    return x * q + min(x, r) + (int)(blockIdx.x >> 3);
 }
 
-// SQUARE: B = b A + c A A, else A = X X^T; a tile on or below the diagonal and its mirror.
-template <bool SQUARE> __global__ __launch_bounds__(256) void k_muon_gram(MuonArgs A)
+// SQUARE: B = b A + c A A, else A = X X^T; a part on or below the diagonal and its mirror.
+template <bool SQUARE, int T> __global__ __launch_bounds__(muon_threads(TILES[T])) void k_muon_gram(MuonArgs A)
 {
-    __shared__ __align__(16) MuonTiles s;
-    const MuonMatrix &M = matrix_of<&MuonMatrix::first_half>(A, blockIdx.x);
-    const int tile = blockIdx.x - M.first_half;
-    int ti = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
-    while (ti * (ti + 1) / 2 > tile) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
-    const int tj = tile - ti * (ti + 1) / 2, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const long plane = (long)M.rp * M.rp;
-    f4 acc[2][2] = {};
-    if (SQUARE) muon_product(s, M.a, plane, ti * MT, M.a, plane, tj * MT, M.rp, acc);
-    else muon_product(s, M.x, (long)M.rp * M.cp, ti * MT, M.x, (long)M.rp * M.cp, tj * MT, M.cp, acc);
+    constexpr int N = TILES[T];
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int which = muon_part();
+    const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_half[T]; });
+    const int part = which - M.first_half[T], rp = M.rp;
+    int ti = (int)((sqrtf(8.f * part + 1.f) - 1.f) * 0.5f);
+    while (ti * (ti + 1) / 2 > part) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= part) ++ti;
+    const int tj = part - ti * (ti + 1) / 2, i0 = ti * N, j0 = tj * N;
+    MuonProduct<N, 2, muon_wn(N), !SQUARE> P;
+    if (SQUARE) P.run(lds, M.a, M.a, i0, j0, rp, rp, rp, rp);
+    else P.run(lds, M.y[A.from], M.y[A.from], i0, j0, rp, rp, rp, M.cp);
     bf16 *out = SQUARE ? M.b : M.a;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const long row = ti * MT + 32 * (w >> 1) + 16 * i + 4 * (lane >> 4), col = tj * MT + 32 * (w & 1) + 16 * j + (lane & 15);
-            vec<bf16, 4> hi, lo;
+    P.each([&](int r, int c, f4 v) {
+        const int row = i0 + r, col = j0 + c;
+        if (row >= rp || col >= rp) return;
+        const long mirror = hi_at(col, row, rp);
+        if (SQUARE) v = A.b * whole_of(M.a + mirror) + A.c * v;
+        put_halves(out + mirror, v);
+        if (ti != tj)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const long at = (row + e) * M.rp + col;
-                float v = acc[i][j][e];
-                if (SQUARE) v = A.b * ((float)M.a[at] + (float)M.a[at + plane]) + A.c * v;
-                bf16 h, l;
-                halves_of(v, h, l);
-                out[at] = hi[e] = h;
-                out[at + plane] = lo[e] = l;
+                bf16 *p = out + hi_at(row + e, col, rp);
+                halves_of(v[e], p[0], p[32]);
             }
-            if (ti != tj) {
-                *reinterpret_cast<vec<bf16, 4> *>(out + col * M.rp + row) = hi;
-                *reinterpret_cast<vec<bf16, 4> *>(out + col * M.rp + row + plane) = lo;
-            }
-        }
+    });
 }
 
-// X <- a X + B X, from the transposed number `from` into the other; the last time into the parameters.
-template <bool LAST> __global__ __launch_bounds__(256) void k_muon_apply(MuonArgs A, int from)
+// X <- a X + B X, into the other Y; the last time into the parameters.
+template <bool LAST, int T> __global__ __launch_bounds__(muon_threads(TILES[T])) void k_muon_apply(MuonArgs A)
 {
-    __shared__ __align__(16) MuonTiles s;
-    const MuonMatrix &M = matrix_of<&MuonMatrix::first_whole>(A, blockIdx.x);
-    const int tile = blockIdx.x - M.first_whole, across = M.cp / MT, ti = tile / across, tj = tile % across, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const long plane = (long)M.rp * M.cp;
-    f4 acc[2][2] = {};
-    muon_product(s, M.b, (long)M.rp * M.rp, ti * MT, M.xt[from], plane, tj * MT, M.rp, acc);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const long row = ti * MT + 32 * (w >> 1) + 16 * i + 4 * (lane >> 4), col = tj * MT + 32 * (w & 1) + 16 * j + (lane & 15);
-            vec<bf16, 4> hi, lo;
+    constexpr int N = TILES[T];
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int which = muon_part();
+    const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_whole[T]; });
+    const int part = which - M.first_whole[T], down = (M.rp + N - 1) / N, i0 = part % down * N, j0 = part / down * N;
+    MuonProduct<N, 2, muon_wn(N), false> P;
+    P.run(lds, M.b, M.y[A.from], i0, j0, M.rp, M.cp, M.rp, M.rp);
+    P.each([&](int r, int c, f4 v) {
+        const int row = i0 + r, col = j0 + c;       // of X
+        if (row >= M.rp || col >= M.cp) return;
+        const long at = hi_at(col, row, M.rp);
+        v = A.a * whole_of(M.y[A.from] + at) + v;
+        if (!LAST) put_halves(M.y[A.from ^ 1] + at, v);
+        else
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const long at = (row + e) * M.cp + col;
-                const float v = A.a * ((float)M.x[at] + (float)M.x[at + plane]) + acc[i][j][e];
-                if (LAST) {
-                    const long r = M.tall ? col : row + e, c = M.tall ? row + e : col;
-                    if (r < M.rows && c < M.cols) {
-                        const long to = r * M.cols + c;
-                        const float p = M.p[to], n = p - A.lr * (M.decay * p + M.scale * v);
-                        M.p[to] = n;
-                        if (M.copy) M.copy[to] = __builtin_bit_cast(uint16_t, (bf16)n);
-                    }
-                } else {
-                    bf16 h, l;
-                    halves_of(v, h, l);
-                    M.x[at] = hi[e] = h;
-                    M.x[at + plane] = lo[e] = l;
+                const long pr = M.tall ? col : row + e, pc = M.tall ? row + e : col;
+                if (pr < M.rows && pc < M.cols) {
+                    const long to = pr * M.cols + pc;
+                    const float p = M.p[to], n = p - A.lr * (M.decay * p + M.scale * v[e]);
+                    M.p[to] = n;
+                    if (M.copy) M.copy[to] = __builtin_bit_cast(uint16_t, (bf16)n);
                 }
             }
-            if (!LAST) {
-                bf16 *to = M.xt[from ^ 1] + col * M.rp + row;
-                *reinterpret_cast<vec<bf16, 4> *>(to) = hi;
-                *reinterpret_cast<vec<bf16, 4> *>(to + plane) = lo;
-            }
-        }
+    });
 }
 
 }  // namespace seq

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/dqn.h"
@@ -12,13 +13,14 @@
 
 struct dqn_muon {
     seq::MuonArgs args;
-    int64_t chunks, half, whole;       // workgroups of the launches
+    int64_t chunks, start, half[3], whole[3];       // workgroups of the launches, by the size of their parts
     int grad_dtype;
 };
 
 namespace {
 
 constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
+constexpr int64_t ENOUGH = 192;         // parts of a product for 256 compute units
 
 const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
 {
@@ -35,9 +37,9 @@ const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
 // Of one matrix: its padded sides and its parts of the workspace in bytes, in their order.
 struct Parts {
     int64_t rp, cp, chunks, x, a, sums;
-    int64_t bytes() const { return 3 * x + 2 * a + sums; }
+    int64_t bytes() const { return 2 * x + 2 * a + sums; }
 };
-int64_t padded(int64_t n) { return (n + seq::MT - 1) / seq::MT * seq::MT; }
+int64_t padded(int64_t n) { return (n + seq::PAD - 1) / seq::PAD * seq::PAD; }
 Parts parts_of(const dqn_muon_matrix &t)
 {
     Parts p{};
@@ -52,26 +54,46 @@ Parts parts_of(const dqn_muon_matrix &t)
 }
 
 struct Total {
-    int64_t plan, workspace, chunks, half, whole;
+    int64_t plan, workspace, chunks, start, half[3], whole[3];
+    void add(const Parts &p)
+    {
+        workspace += p.bytes();
+        chunks += p.chunks;
+        start += p.rp / 64 * (p.cp / 64);
+        for (int t = 0; t < 3; ++t) {
+            const int64_t n = seq::TILES[t], down = (p.rp + n - 1) / n;
+            half[t] += down * (down + 1) / 2;
+            whole[t] += down * ((p.cp + n - 1) / n);
+        }
+    }
 };
 Total total_of(const dqn_muon_matrix *t, int32_t count)
 {
-    Total s{((int64_t)count * (int64_t)sizeof(seq::MuonMatrix) + 255) / 256 * 256, 0, 0, 0, 0};
-    for (int32_t i = 0; i < count; ++i) {
-        const Parts p = parts_of(t[i]);
-        const int64_t down = p.rp / seq::MT, across = p.cp / seq::MT;
-        s.workspace += p.bytes();
-        s.chunks += p.chunks;
-        s.half += down * (down + 1) / 2;
-        s.whole += down * across;
-    }
+    Total s{((int64_t)count * (int64_t)sizeof(seq::MuonMatrix) + 255) / 256 * 256, 0, 0, 0, {}, {}};
+    for (int32_t i = 0; i < count; ++i) s.add(parts_of(t[i]));
     return s;
+}
+
+// The largest parts of which there is enough for the compute units.
+int part_of(const int64_t (&n)[3]) { return n[2] >= ENOUGH ? 2 : n[1] >= ENOUGH ? 1 : 0; }
+template <int T> bool granted_lds()
+{
+    static std::atomic<uint64_t> a{0}, b{0}, c{0}, d{0};
+    constexpr int bytes = 512 * seq::TILES[T];
+    return lds_granted((const void *)seq::k_muon_gram<false, T>, bytes, a) && lds_granted((const void *)seq::k_muon_gram<true, T>, bytes, b) &&
+           lds_granted((const void *)seq::k_muon_apply<false, T>, bytes, c) && lds_granted((const void *)seq::k_muon_apply<true, T>, bytes, d);
+}
+template <class F> void with_part(int t, F &&go)
+{
+    if (t == 2) go(std::integral_constant<int, 2>{});
+    else if (t == 1) go(std::integral_constant<int, 1>{});
+    else go(std::integral_constant<int, 0>{});
 }
 
 template <class G> void launch_begin(const dqn_muon &o, hipStream_t st)
 {
     seq::k_muon_momentum<G><<<dim3((unsigned)o.chunks), 256, 0, st>>>(o.args);
-    seq::k_muon_start<G><<<dim3((unsigned)o.whole), 256, 0, st>>>(o.args);
+    seq::k_muon_start<G><<<dim3((unsigned)o.start), 256, 0, st>>>(o.args);
 }
 
 }  // namespace
@@ -100,27 +122,27 @@ int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t c
     for (int32_t i = 0; i < count; ++i)
         if (!at(matrices[i].grad, bytes_of(grad_dtype))) return bad(call, "a gradient is not aligned to its elements");
     const Total s = total_of(matrices, count);
-    if (s.chunks >= 1 << 24 || s.half >= 1 << 24 || s.whole >= 1 << 24) return bad(call, "too many elements");   // a launch has 2^32 threads
+    if (s.chunks >= 1 << 24 || s.start >= 1 << 24 || s.half[0] >= 1 << 24 || s.whole[0] >= 1 << 24) return bad(call, "too many elements");   // a launch has 2^32 threads
     dqn_muon *o = nullptr;
     try {
         std::vector<seq::MuonMatrix> table;
         table.reserve((size_t)count);
         uint8_t *at = (uint8_t *)workspace;
-        int first_chunk = 0, first_half = 0, first_whole = 0;
+        Total before{};
         for (int32_t i = 0; i < count; ++i) {
             const dqn_muon_matrix &t = matrices[i];
             if (!t.rows || !t.cols) continue;
             const Parts p = parts_of(t);
             seq::MuonMatrix m{};
             m.p = t.param; m.m = t.momentum; m.g = t.grad; m.copy = t.copy;
-            m.x = (seq::bf16 *)at; m.xt[0] = (seq::bf16 *)(at + p.x); m.xt[1] = (seq::bf16 *)(at + 2 * p.x);
-            m.a = (seq::bf16 *)(at + 3 * p.x); m.b = (seq::bf16 *)(at + 3 * p.x + p.a); m.sums = (double *)(at + 3 * p.x + 2 * p.a);
+            m.y[0] = (seq::bf16 *)at; m.y[1] = (seq::bf16 *)(at + p.x);
+            m.a = (seq::bf16 *)(at + 2 * p.x); m.b = (seq::bf16 *)(at + 2 * p.x + p.a); m.sums = (double *)(at + 2 * p.x + 2 * p.a);
             at += p.bytes();
             m.rows = (long)t.rows; m.cols = (long)t.cols; m.rp = (int)p.rp; m.cp = (int)p.cp; m.tall = t.rows > t.cols;
             m.decay = t.decay; m.scale = (float)std::sqrt(std::max(1.0, (double)t.rows / (double)t.cols)); m.chunks = (int)p.chunks;
-            m.first_chunk = first_chunk; m.first_half = first_half; m.first_whole = first_whole;
-            const int down = m.rp / seq::MT;
-            first_chunk += m.chunks; first_half += down * (down + 1) / 2; first_whole += down * (m.cp / seq::MT);
+            m.first_chunk = (int)before.chunks; m.first_start = (int)before.start;
+            for (int k = 0; k < 3; ++k) m.first_half[k] = (int)before.half[k], m.first_whole[k] = (int)before.whole[k];
+            before.add(p);
             table.push_back(m);
         }
         hipStream_t st = (hipStream_t)stream;
@@ -134,7 +156,9 @@ int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t c
         return dqn_seq_fail(DQN_ERR_OOM, call, "out of host memory");
     }
     o->args.matrices = (const seq::MuonMatrix *)plan;
-    o->chunks = s.chunks; o->half = s.half; o->whole = s.whole; o->grad_dtype = grad_dtype;
+    o->chunks = s.chunks; o->start = s.start; o->grad_dtype = grad_dtype;
+    std::copy(s.half, s.half + 3, o->half);
+    std::copy(s.whole, s.whole + 3, o->whole);
     *out = o;
     return DQN_OK;
 }
@@ -153,12 +177,25 @@ int32_t dqn_muon_step(dqn_muon *opt, double lr, double momentum, int32_t nestero
     hipStream_t st = (hipStream_t)stream;
     dqn_muon now = *opt;
     now.args = A;
+    const int half = part_of(opt->half), whole = part_of(opt->whole);
+    bool ok = true;
+    with_part(half, [&](auto t) { ok = ok && granted_lds<t.value>(); });
+    with_part(whole, [&](auto t) { ok = ok && granted_lds<t.value>(); });
+    if (!ok) return dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a part was not granted");
     opt->grad_dtype == DQN_F32 ? launch_begin<float>(now, st) : launch_begin<seq::bf16>(now, st);
     for (int32_t i = 0; i < rounds; ++i) {
-        seq::k_muon_gram<false><<<dim3((unsigned)opt->half), 256, 0, st>>>(A);
-        seq::k_muon_gram<true><<<dim3((unsigned)opt->half), 256, 0, st>>>(A);
-        if (i + 1 < rounds) seq::k_muon_apply<false><<<dim3((unsigned)opt->whole), 256, 0, st>>>(A, i & 1);
-        else seq::k_muon_apply<true><<<dim3((unsigned)opt->whole), 256, 0, st>>>(A, i & 1);
+        A.from = i & 1;
+        with_part(half, [&](auto t) {
+            constexpr int n = seq::TILES[t.value];
+            seq::k_muon_gram<false, t.value><<<dim3((unsigned)opt->half[t.value]), seq::muon_threads(n), 512 * n, st>>>(A);
+            seq::k_muon_gram<true, t.value><<<dim3((unsigned)opt->half[t.value]), seq::muon_threads(n), 512 * n, st>>>(A);
+        });
+        with_part(whole, [&](auto t) {
+            constexpr int n = seq::TILES[t.value];
+            const dim3 grid((unsigned)opt->whole[t.value]);
+            if (i + 1 < rounds) seq::k_muon_apply<false, t.value><<<grid, seq::muon_threads(n), 512 * n, st>>>(A);
+            else seq::k_muon_apply<true, t.value><<<grid, seq::muon_threads(n), 512 * n, st>>>(A);
+        });
     }
     return launched(call);
 }

@@ -171,16 +171,6 @@ template <class E, int MI, int NI> __global__ __launch_bounds__(64 * FEW_WAVES) 
 // the place c ^ (r / 2 % 8), so that the sixteen lanes that LDS serves together, a piece of sixteen rows, meet each of
 // its 64 banks once.
 
-// 16 bytes per lane from memory to LDS, lane l's to p + 16 l.  In assembly, because the compiler would let every LDS
-// read behind it wait for its arrival; the barrier of a step waits for all of them.
-__device__ __forceinline__ void to_lds(const uint8_t *g, uint8_t *p)
-{
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
-    uint32_t m0;   // left as it was
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-                 : "=&s"(m0) : "s"(at), "v"(g) : "memory");
-}
-
 // Which tile a workgroup takes: neighbouring ones on the same XCD (workgroups go round the eight), eight tiles high
 // bands of them, so that an XCD's L2 holds what its workgroups read together.
 struct Tile {

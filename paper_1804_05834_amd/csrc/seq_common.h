@@ -50,6 +50,16 @@ template <int V> __device__ __forceinline__ void arrived(const float (&v)[V])
     for (int k = 0; k < V; ++k) arrived(v[k]);
 }
 
+// 16 bytes per lane from memory to LDS, lane l's to p + 16 l.  In assembly, because the compiler would let every LDS
+// read behind it wait for its arrival; the barrier of a step waits for all of them.
+__device__ __forceinline__ void to_lds(const uint8_t *g, uint8_t *p)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)p);
+    uint32_t m0;   // left as it was
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(at), "v"(g) : "memory");
+}
+
 // the larger one, or a NaN if one is a NaN
 __device__ __forceinline__ float nan_max(float a, float b) { return a != a ? a : (b > a || b != b) ? b : a; }
 
