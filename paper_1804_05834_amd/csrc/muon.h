@@ -115,11 +115,14 @@ template <class G> __global__ __launch_bounds__(256) void k_muon_start(MuonArgs 
 using f4 = vec<float, 4>;
 using b4 = vec<bf16, 4>;
 using b8 = vec<bf16, 8>;
-__device__ __forceinline__ f4 whole_of(const bf16 *hi)
-{
-    const b4 a = load<4>(hi), b = load<4>(hi + 32);
-    return f4{(float)a[0] + (float)b[0], (float)a[1] + (float)b[1], (float)a[2] + (float)b[2], (float)a[3] + (float)b[3]};
-}
+struct Pair4 {
+    b4 hi, lo;
+    __device__ __forceinline__ f4 whole() const
+    {
+        return f4{(float)hi[0] + (float)lo[0], (float)hi[1] + (float)lo[1], (float)hi[2] + (float)lo[2], (float)hi[3] + (float)lo[3]};
+    }
+};
+__device__ __forceinline__ Pair4 pair_at(const bf16 *hi) { return Pair4{load<4>(hi), load<4>(hi + 32)}; }
 __device__ __forceinline__ void put_halves(bf16 *hi, f4 v)
 {
     b4 a, b;
@@ -133,16 +136,26 @@ __device__ __forceinline__ void put_halves(bf16 *hi, f4 v)
 }
 
 // N x N numbers of L R^T (COLUMNS false: rows i0.. of L, j0.. of R, both K wide) or of L^T R (COLUMNS: columns i0.., j0.. of the same matrix of K rows,
-// `width` wide), by WM x WN waves, a wave having MI x NI results of 16 x 16, a lane rows 4 (l / 16).. of column l % 16 of each.  32 of K a step, two
-// steps' operands in LDS: while one is multiplied, the next comes from memory past the registers.
+// `width` wide), `steps` steps of 32 of K from k0 on, by WM x WN waves, a wave having MI x NI results of 16 x 16, a lane rows 4 (l / 16).. of column l % 16 of each.  32 of K a step,
+// STAGES steps' operands in LDS: while one is multiplied, the next ones come from memory past the registers (four stages of 64 x 64, which are often
+// few and wait for memory: a step 0.49 us with two, 0.36 with four).
 // LDS, rows: a row's 128 bytes in eight pieces of 16, four of hi and four of lo; piece c of row r has the place c ^ (r / 2 % 8).  Columns: a row has 4 N
 // bytes in pieces of 32, sixteen columns' hi or lo; piece c of row r has the place c ^ (r % 8).  So the lanes that LDS serves together meet each of
 // its banks once.
+constexpr int muon_stages(int n) { return n == 64 ? 4 : 2; }
+constexpr int muon_lds(int n) { return muon_stages(n) * 256 * n; }
 template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
-    static constexpr int WAVES = WM * WN, MI = N / WM / 16, NI = N / WN / 16, SIDE = N * 128, STAGE = 2 * SIDE, LOADS = STAGE / 1024 / WAVES;
+    static constexpr int WAVES = WM * WN, MI = N / WM / 16, NI = N / WN / 16, SIDE = N * 128, STAGE = 2 * SIDE, LOADS = STAGE / 1024 / WAVES, STAGES = muon_stages(N);
     static_assert(STAGE % (1024 * WAVES) == 0 && LOADS >= 1, "whole loads of a wave");
     f4 acc[MI][NI];
-    __device__ __forceinline__ void run(uint8_t *lds, const bf16 *L, const bf16 *R, int i0, int j0, int rows_l, int rows_r, int width, int K)
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int x = 0; x < MI; ++x)
+#pragma unroll
+            for (int y = 0; y < NI; ++y) acc[x][y] = f4{};
+    }
+    __device__ __forceinline__ void run(uint8_t *lds, const bf16 *L, const bf16 *R, int i0, int j0, int rows_l, int rows_r, int width, int K, int k0, int steps)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
         const uint8_t *src[LOADS];
@@ -162,9 +175,10 @@ template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
             }
         }
         auto fetch = [&](int step) {
-            uint8_t *to = lds + (step & 1) * STAGE + wave * LOADS * 1024;
+            uint8_t *to = lds + step % STAGES * STAGE + wave * LOADS * 1024;
+            const long from = (k0 / 32 + min(step, steps - 1)) * step_bytes;      // behind the last step it again, so that the same number is under way always
 #pragma unroll
-            for (int q = 0; q < LOADS; ++q) to_lds(src[q] + step * step_bytes, to + q * 1024);
+            for (int q = 0; q < LOADS; ++q) to_lds(src[q] + from, to + q * 1024);
         };
         // 16 rows (columns) from `first` on as an operand, its hi and its lo
         auto operand = [&](const uint8_t *side, int first, b8 (&v)[2]) {
@@ -185,16 +199,14 @@ template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
                 v[1] = *reinterpret_cast<const b8 *>(side + (place ^ 64));
             }
         };
+        clear();
+        const int wm = wave % WM * MI * 16, wn = wave / WM * NI * 16;
 #pragma unroll
-        for (int x = 0; x < MI; ++x)
-#pragma unroll
-            for (int y = 0; y < NI; ++y) acc[x][y] = f4{};
-        const int wm = wave % WM * MI * 16, wn = wave / WM * NI * 16, steps = K / 32;
-        fetch(0);
+        for (int n = 0; n + 1 < STAGES; ++n) fetch(n);
         for (int step = 0; step < steps; ++step) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (step + 1 < steps) fetch(step + 1);
-            const uint8_t *l = lds + (step & 1) * STAGE, *r = l + SIDE;
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
+            fetch(step + STAGES - 1);
+            const uint8_t *l = lds + step % STAGES * STAGE, *r = l + SIDE;
             b8 b[NI][2];
 #pragma unroll
             for (int y = 0; y < NI; ++y) operand(r, wn + 16 * y, b[y]);
@@ -210,15 +222,20 @@ template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
                 for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[y][0], acc[x][y], 0, 0, 0);
             }
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS that another workgroup has by then
     }
-    // f(row, column, the four numbers of rows row.. and that column)
-    template <class F> __device__ __forceinline__ void each(F &&f)
+    // f(row, column, the four numbers of rows row.. and that column, get(row, column)); what several get() read is asked for before the first is waited for
+    template <class G, class F> __device__ __forceinline__ void each(G &&get, F &&f)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % WM * MI * 16, wn = wave / WM * NI * 16;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % WM * MI * 16 + 4 * (lane >> 4), wn = wave / WM * NI * 16 + (lane & 15);
 #pragma unroll
-        for (int x = 0; x < MI; ++x)
+        for (int x = 0; x < MI; ++x) {
+            decltype(get(0, 0)) old[NI];
 #pragma unroll
-            for (int y = 0; y < NI; ++y) f(wm + 16 * x + 4 * (lane >> 4), wn + 16 * y + (lane & 15), acc[x][y]);
+            for (int y = 0; y < NI; ++y) old[y] = get(wm + 16 * x, wn + 16 * y);
+#pragma unroll
+            for (int y = 0; y < NI; ++y) f(wm + 16 * x, wn + 16 * y, acc[x][y], old[y]);
+        }
     }
 };
 constexpr int muon_wn(int n) { return n == 256 ? 4 : 2; }
@@ -231,27 +248,49 @@ __device__ __forceinline__ int muon_part()
     return x * q + min(x, r) + (int)(blockIdx.x >> 3);
 }
 
-// SQUARE: B = b A + c A A, else A = X X^T; a part on or below the diagonal and its mirror.
-template <bool SQUARE, int T> __global__ __launch_bounds__(muon_threads(TILES[T])) void k_muon_gram(MuonArgs A)
+// SQUARE: B = b A + c A A, else A = X X^T; a part on or below the diagonal and its mirror.  Where parts are few and K is long, it is cut: SPLIT leaves `cuts` sums of
+// each part, JOIN adds them up in their order.
+enum Gram { WHOLE, SQUARE, SPLIT, JOIN };
+template <Gram G, int T> __global__ __launch_bounds__(muon_threads(TILES[T])) void k_muon_gram(MuonArgs A, f4 *sums, int cuts)
 {
-    constexpr int N = TILES[T];
+    constexpr int N = TILES[T], THREADS = muon_threads(N);
     extern __shared__ __align__(16) uint8_t lds[];
-    const int which = muon_part();
+    const int group = G == JOIN ? (int)blockIdx.x : muon_part(), which = G == SPLIT ? group / cuts : group;
     const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_half[T]; });
     const int part = which - M.first_half[T], rp = M.rp;
     int ti = (int)((sqrtf(8.f * part + 1.f) - 1.f) * 0.5f);
     while (ti * (ti + 1) / 2 > part) --ti;
     while ((ti + 1) * (ti + 2) / 2 <= part) ++ti;
     const int tj = part - ti * (ti + 1) / 2, i0 = ti * N, j0 = tj * N;
-    MuonProduct<N, 2, muon_wn(N), !SQUARE> P;
-    if (SQUARE) P.run(lds, M.a, M.a, i0, j0, rp, rp, rp, rp);
-    else P.run(lds, M.y[A.from], M.y[A.from], i0, j0, rp, rp, rp, M.cp);
-    bf16 *out = SQUARE ? M.b : M.a;
-    P.each([&](int r, int c, f4 v) {
+    MuonProduct<N, 2, muon_wn(N), G != SQUARE> P;
+    constexpr int MI = decltype(P)::MI, NI = decltype(P)::NI;
+    if (G == SQUARE) P.run(lds, M.a, M.a, i0, j0, rp, rp, rp, rp, 0, rp / 32);
+    if (G == WHOLE) P.run(lds, M.y[A.from], M.y[A.from], i0, j0, rp, rp, rp, M.cp, 0, M.cp / 32);
+    if (G == SPLIT) {
+        const int steps = M.cp / 32, per = (steps + cuts - 1) / cuts, first = min(group % cuts * per, steps), n = min(per, steps - first);
+        if (n > 0) P.run(lds, M.y[A.from], M.y[A.from], i0, j0, rp, rp, rp, M.cp, 32 * first, n);
+        else P.clear();
+#pragma unroll
+        for (int x = 0; x < MI; ++x)
+#pragma unroll
+            for (int y = 0; y < NI; ++y) sums[((long)group * MI * NI + x * NI + y) * THREADS + threadIdx.x] = P.acc[x][y];
+        return;
+    }
+    if (G == JOIN) {
+        P.clear();
+        for (int k = 0; k < cuts; ++k)
+#pragma unroll
+            for (int x = 0; x < MI; ++x)
+#pragma unroll
+                for (int y = 0; y < NI; ++y) P.acc[x][y] += sums[(((long)which * cuts + k) * MI * NI + x * NI + y) * THREADS + threadIdx.x];
+    }
+    bf16 *out = G == SQUARE ? M.b : M.a;
+    P.each([&](int r, int c) { return G == SQUARE ? pair_at(M.a + hi_at(min(j0 + c, rp - 1), min(i0 + r, rp - 4), rp)) : Pair4{}; },
+           [&](int r, int c, f4 v, const Pair4 &old) {
         const int row = i0 + r, col = j0 + c;
         if (row >= rp || col >= rp) return;
         const long mirror = hi_at(col, row, rp);
-        if (SQUARE) v = A.b * whole_of(M.a + mirror) + A.c * v;
+        if (G == SQUARE) v = A.b * old.whole() + A.c * v;
         put_halves(out + mirror, v);
         if (ti != tj)
 #pragma unroll
@@ -271,23 +310,39 @@ template <bool LAST, int T> __global__ __launch_bounds__(muon_threads(TILES[T]))
     const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_whole[T]; });
     const int part = which - M.first_whole[T], down = (M.rp + N - 1) / N, i0 = part % down * N, j0 = part / down * N;
     MuonProduct<N, 2, muon_wn(N), false> P;
-    P.run(lds, M.b, M.y[A.from], i0, j0, M.rp, M.cp, M.rp, M.rp);
-    P.each([&](int r, int c, f4 v) {
-        const int row = i0 + r, col = j0 + c;       // of X
-        if (row >= M.rp || col >= M.cp) return;
-        const long at = hi_at(col, row, M.rp);
-        v = A.a * whole_of(M.y[A.from] + at) + v;
-        if (!LAST) put_halves(M.y[A.from ^ 1] + at, v);
-        else
+    P.run(lds, M.b, M.y[A.from], i0, j0, M.rp, M.cp, M.rp, M.rp, 0, M.rp / 32);
+    if (!LAST) {
+        P.each([&](int r, int c) { return pair_at(M.y[A.from] + hi_at(min(j0 + c, M.cp - 1), min(i0 + r, M.rp - 4), M.rp)); },
+               [&](int r, int c, f4 v, const Pair4 &old) {
+            const int row = i0 + r, col = j0 + c;       // of X
+            if (row < M.rp && col < M.cp) put_halves(M.y[A.from ^ 1] + hi_at(col, row, M.rp), A.a * old.whole() + v);
+        });
+        return;
+    }
+    struct Old {
+        Pair4 x;
+        float p[4];
+    };
+    const long down_p = M.tall ? 1 : M.cols, across_p = M.tall ? M.cols : 1;       // from row to row, column to column of X in the parameters
+    const int r_end = (int)(M.tall ? M.cols : M.rows), c_end = (int)(M.tall ? M.rows : M.cols);
+    P.each([&](int r, int c) {
+               const int row = i0 + r, col = j0 + c;
+               Old o;
+               o.x = pair_at(M.y[A.from] + hi_at(min(col, M.cp - 1), min(row, M.rp - 4), M.rp));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const long pr = M.tall ? col : row + e, pc = M.tall ? row + e : col;
-                if (pr < M.rows && pc < M.cols) {
-                    const long to = pr * M.cols + pc;
-                    const float p = M.p[to], n = p - A.lr * (M.decay * p + M.scale * v[e]);
-                    M.p[to] = n;
-                    if (M.copy) M.copy[to] = __builtin_bit_cast(uint16_t, (bf16)n);
-                }
+               for (int e = 0; e < 4; ++e) o.p[e] = M.p[min(row + e, r_end - 1) * down_p + min(col, c_end - 1) * across_p];
+               return o;
+           },
+           [&](int r, int c, f4 v, const Old &old) {
+        const int row = i0 + r, col = j0 + c;
+        v = A.a * old.x.whole() + v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (row + e < r_end && col < c_end) {
+                const long to = (row + e) * down_p + col * across_p;
+                const float n = old.p[e] - A.lr * (M.decay * old.p[e] + M.scale * v[e]);
+                M.p[to] = n;
+                if (M.copy) M.copy[to] = __builtin_bit_cast(uint16_t, (bf16)n);
             }
     });
 }

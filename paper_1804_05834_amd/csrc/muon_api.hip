@@ -15,12 +15,14 @@ struct dqn_muon {
     seq::MuonArgs args;
     int64_t chunks, start, half[3], whole[3];       // workgroups of the launches, by the size of their parts
     int grad_dtype;
+    seq::f4 *sums;
 };
 
 namespace {
 
 constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
-constexpr int64_t ENOUGH = 192;         // parts of a product for 256 compute units
+constexpr int64_t ENOUGH[3] = {0, 256, 192};         // parts of a product for 256 compute units, by their size
+constexpr int64_t MOST_CUTS = 8;
 
 const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
 {
@@ -75,12 +77,15 @@ Total total_of(const dqn_muon_matrix *t, int32_t count)
 }
 
 // The largest parts of which there is enough for the compute units.
-int part_of(const int64_t (&n)[3]) { return n[2] >= ENOUGH ? 2 : n[1] >= ENOUGH ? 1 : 0; }
+int part_of(const int64_t (&n)[3]) { return n[2] >= ENOUGH[2] ? 2 : n[1] >= ENOUGH[1] ? 1 : 0; }
+// Sums that X X^T is cut into where it has few parts (of 64 x 64): as many as leave a workgroup for each compute unit.
+int cuts_of(int64_t parts) { return parts ? (int)std::max<int64_t>(1, std::min<int64_t>(MOST_CUTS, 256 / parts)) : 1; }
+size_t sums_bytes(int64_t parts) { return cuts_of(parts) > 1 ? (size_t)parts * cuts_of(parts) * 64 * 64 * 4 : 0; }
 template <int T> bool granted_lds()
 {
     static std::atomic<uint64_t> a{0}, b{0}, c{0}, d{0};
-    constexpr int bytes = 512 * seq::TILES[T];
-    return lds_granted((const void *)seq::k_muon_gram<false, T>, bytes, a) && lds_granted((const void *)seq::k_muon_gram<true, T>, bytes, b) &&
+    constexpr int bytes = seq::muon_lds(seq::TILES[T]);
+    return lds_granted((const void *)seq::k_muon_gram<seq::WHOLE, T>, bytes, a) && lds_granted((const void *)seq::k_muon_gram<seq::SQUARE, T>, bytes, b) &&
            lds_granted((const void *)seq::k_muon_apply<false, T>, bytes, c) && lds_granted((const void *)seq::k_muon_apply<true, T>, bytes, d);
 }
 template <class F> void with_part(int t, F &&go)
@@ -107,7 +112,7 @@ int32_t dqn_muon_sizes(const dqn_muon_matrix *matrices, int32_t count, size_t *p
     if (const char *m = check_matrices(matrices, count)) return bad(call, m);
     const Total s = total_of(matrices, count);
     *plan = (size_t)s.plan;
-    *workspace = (size_t)std::max<int64_t>(s.workspace, 256);
+    *workspace = std::max<size_t>((size_t)s.workspace + sums_bytes(s.half[0]), 256);
     return DQN_OK;
 }
 
@@ -157,6 +162,7 @@ int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t c
     }
     o->args.matrices = (const seq::MuonMatrix *)plan;
     o->chunks = s.chunks; o->start = s.start; o->grad_dtype = grad_dtype;
+    o->sums = (seq::f4 *)((uint8_t *)workspace + s.workspace);
     std::copy(s.half, s.half + 3, o->half);
     std::copy(s.whole, s.whole + 3, o->whole);
     *out = o;
@@ -177,7 +183,7 @@ int32_t dqn_muon_step(dqn_muon *opt, double lr, double momentum, int32_t nestero
     hipStream_t st = (hipStream_t)stream;
     dqn_muon now = *opt;
     now.args = A;
-    const int half = part_of(opt->half), whole = part_of(opt->whole);
+    const int half = part_of(opt->half), whole = part_of(opt->whole), cuts = cuts_of(opt->half[0]);
     bool ok = true;
     with_part(half, [&](auto t) { ok = ok && granted_lds<t.value>(); });
     with_part(whole, [&](auto t) { ok = ok && granted_lds<t.value>(); });
@@ -187,14 +193,18 @@ int32_t dqn_muon_step(dqn_muon *opt, double lr, double momentum, int32_t nestero
         A.from = i & 1;
         with_part(half, [&](auto t) {
             constexpr int n = seq::TILES[t.value];
-            seq::k_muon_gram<false, t.value><<<dim3((unsigned)opt->half[t.value]), seq::muon_threads(n), 512 * n, st>>>(A);
-            seq::k_muon_gram<true, t.value><<<dim3((unsigned)opt->half[t.value]), seq::muon_threads(n), 512 * n, st>>>(A);
+            const dim3 grid((unsigned)opt->half[t.value]);
+            if (t.value == 0 && cuts > 1) {
+                seq::k_muon_gram<seq::SPLIT, 0><<<dim3((unsigned)(opt->half[0] * cuts)), seq::muon_threads(64), seq::muon_lds(64), st>>>(A, opt->sums, cuts);
+                seq::k_muon_gram<seq::JOIN, 0><<<grid, seq::muon_threads(64), 0, st>>>(A, opt->sums, cuts);
+            } else seq::k_muon_gram<seq::WHOLE, t.value><<<grid, seq::muon_threads(n), seq::muon_lds(n), st>>>(A, nullptr, 1);
+            seq::k_muon_gram<seq::SQUARE, t.value><<<grid, seq::muon_threads(n), seq::muon_lds(n), st>>>(A, nullptr, 1);
         });
         with_part(whole, [&](auto t) {
             constexpr int n = seq::TILES[t.value];
             const dim3 grid((unsigned)opt->whole[t.value]);
-            if (i + 1 < rounds) seq::k_muon_apply<false, t.value><<<grid, seq::muon_threads(n), 512 * n, st>>>(A);
-            else seq::k_muon_apply<true, t.value><<<grid, seq::muon_threads(n), 512 * n, st>>>(A);
+            if (i + 1 < rounds) seq::k_muon_apply<false, t.value><<<grid, seq::muon_threads(n), seq::muon_lds(n), st>>>(A);
+            else seq::k_muon_apply<true, t.value><<<grid, seq::muon_threads(n), seq::muon_lds(n), st>>>(A);
         });
     }
     return launched(call);
