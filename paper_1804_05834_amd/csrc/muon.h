@@ -207,19 +207,24 @@ template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
             fetch(step + STAGES - 1);
             const uint8_t *l = lds + step % STAGES * STAGE, *r = l + SIDE;
-            b8 b[NI][2];
+            constexpr int READS = COLUMNS ? 4 : 2;      // of LDS for an operand
+            b8 b[NI][2], next[2];
 #pragma unroll
             for (int y = 0; y < NI; ++y) operand(r, wn + 16 * y, b[y]);
+            operand(l, wm, next);
+            __builtin_amdgcn_sched_group_barrier(0x100, READS * (NI + 1), 0);
 #pragma unroll
-            for (int x = 0; x < MI; ++x) {
-                b8 a[2];
-                operand(l, wm + 16 * x, a);
+            for (int x = 0; x < MI; ++x) {      // the next 16 rows are read behind the products of these
+                const b8 a[2] = {next[0], next[1]};
+                if (x + 1 < MI) operand(l, wm + 16 * (x + 1), next);
 #pragma unroll
                 for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b[y][0], acc[x][y], 0, 0, 0);
 #pragma unroll
                 for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[y][1], acc[x][y], 0, 0, 0);
 #pragma unroll
                 for (int y = 0; y < NI; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b[y][0], acc[x][y], 0, 0, 0);
+                if (x + 1 < MI) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 3 * NI, 0);
             }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may arrive in LDS that another workgroup has by then
@@ -241,11 +246,13 @@ template <int N, int WM, int WN, bool COLUMNS> struct MuonProduct {
 constexpr int muon_wn(int n) { return n == 256 ? 4 : 2; }
 constexpr int muon_threads(int n) { return 128 * muon_wn(n); }
 
-// Neighbouring parts on the same XCD (workgroups go round the eight), whose L2 holds what they read together.
-__device__ __forceinline__ int muon_part()
+// The part of a matrix that workgroup `i` of its `n` takes: neighbouring parts on the same XCD (workgroups go round the eight), whose L2 holds what
+// they read together, and every matrix, its inner dimension being its own, spread over all of them (twelve of two kinds: 537 us for B X where the
+// eight took an eighth of all parts each, 424 so).
+__device__ __forceinline__ int muon_part(int i, int n)
 {
-    const int all = gridDim.x, x = blockIdx.x & 7, q = all / 8, r = all % 8;
-    return x * q + min(x, r) + (int)(blockIdx.x >> 3);
+    const int x = i & 7, q = n / 8, r = n % 8;
+    return x * q + min(x, r) + (i >> 3);
 }
 
 // SQUARE: B = b A + c A A, else A = X X^T; a part on or below the diagonal and its mirror.  Where parts are few and K is long, it is cut: SPLIT leaves `cuts` sums of
@@ -255,9 +262,9 @@ template <Gram G, int T> __global__ __launch_bounds__(muon_threads(TILES[T])) vo
 {
     constexpr int N = TILES[T], THREADS = muon_threads(N);
     extern __shared__ __align__(16) uint8_t lds[];
-    const int group = G == JOIN ? (int)blockIdx.x : muon_part(), which = G == SPLIT ? group / cuts : group;
+    const int group = blockIdx.x, which = G == SPLIT ? group / cuts : group;
     const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_half[T]; });
-    const int part = which - M.first_half[T], rp = M.rp;
+    const int rp = M.rp, down = (rp + N - 1) / N, part = G == SPLIT || G == JOIN ? which - M.first_half[T] : muon_part(which - M.first_half[T], down * (down + 1) / 2);
     int ti = (int)((sqrtf(8.f * part + 1.f) - 1.f) * 0.5f);
     while (ti * (ti + 1) / 2 > part) --ti;
     while ((ti + 1) * (ti + 2) / 2 <= part) ++ti;
@@ -306,9 +313,8 @@ template <bool LAST, int T> __global__ __launch_bounds__(muon_threads(TILES[T]))
 {
     constexpr int N = TILES[T];
     extern __shared__ __align__(16) uint8_t lds[];
-    const int which = muon_part();
-    const MuonMatrix &M = matrix_of(A, which, [](const MuonMatrix &m) { return m.first_whole[T]; });
-    const int part = which - M.first_whole[T], down = (M.rp + N - 1) / N, i0 = part % down * N, j0 = part / down * N;
+    const MuonMatrix &M = matrix_of(A, blockIdx.x, [](const MuonMatrix &m) { return m.first_whole[T]; });
+    const int down = (M.rp + N - 1) / N, part = muon_part((int)blockIdx.x - M.first_whole[T], down * ((M.cp + N - 1) / N)), i0 = part % down * N, j0 = part / down * N;
     MuonProduct<N, 2, muon_wn(N), false> P;
     P.run(lds, M.b, M.y[A.from], i0, j0, M.rp, M.cp, M.rp, M.rp, 0, M.rp / 32);
     if (!LAST) {

@@ -21,7 +21,9 @@ struct dqn_muon {
 namespace {
 
 constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
-constexpr int64_t ENOUGH[3] = {0, 256, 192};         // parts of a product for 256 compute units, by their size
+// Parts of a product that are enough for 256 compute units, by their size.  us a launch in parts of 64, 128, 256: B X of twelve matrices of 1024 x 4096 and
+// 2048 x 2048 (768 parts of 256) 822, 582, 424, their X X^T (224) 434, 307, 311; of a block of 512 channels (196 parts of 128) 22, 26, 64.
+constexpr int64_t ENOUGH[3] = {0, 256, 192};
 constexpr int64_t MOST_CUTS = 8;
 
 const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
@@ -134,9 +136,16 @@ int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t c
         table.reserve((size_t)count);
         uint8_t *at = (uint8_t *)workspace;
         Total before{};
-        for (int32_t i = 0; i < count; ++i) {
+        // those whose parts take longest first
+        std::vector<int32_t> order;
+        for (int32_t i = 0; i < count; ++i)
+            if (matrices[i].rows && matrices[i].cols) order.push_back(i);
+        std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) {
+            const Parts p = parts_of(matrices[x]), q = parts_of(matrices[y]);
+            return p.rp != q.rp ? p.rp > q.rp : p.cp > q.cp;
+        });
+        for (int32_t i : order) {
             const dqn_muon_matrix &t = matrices[i];
-            if (!t.rows || !t.cols) continue;
             const Parts p = parts_of(t);
             seq::MuonMatrix m{};
             m.p = t.param; m.m = t.momentum; m.g = t.grad; m.copy = t.copy;
