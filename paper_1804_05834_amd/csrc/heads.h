@@ -12,7 +12,7 @@
 namespace seq {
 
 constexpr int HEADS_MAX = 256;
-constexpr int HEADS_PARTS = 512;       // most partial sums of the weights' gradients, one per workgroup
+constexpr int HEADS_PARTS = 1024;      // most partial sums of the weights' gradients, one per workgroup; of wide rows half of them
 
 struct HeadsShape {
     long M;
@@ -239,8 +239,8 @@ template <class E, int V, int K> __global__ __launch_bounds__(256) void k_heads_
         Angles<V, K> a;
         if (s.half) a.set(u, t, row ? A.position[m] : 0);
         const float *rstd = A.rstd + m * (s.Hq + s.Hk);
-        heads_backward<E, V, K, 2>((const E *)A.dyq + m * A.dyq_rs, A.dyq_hs, (const E *)A.q + m * A.q_rs, A.q_hs, (E *)A.dq + m * A.dq_rs, A.dq_hs, s.Hq, ql, qh, dq[0], dq[1], u, a, s, sub, row, rstd);
-        heads_backward<E, V, K, 2>((const E *)A.dyk + m * A.dyk_rs, A.dyk_hs, (const E *)A.k + m * A.k_rs, A.k_hs, (E *)A.dk + m * A.dk_rs, A.dk_hs, s.Hk, kl, kh, dk[0], dk[1], u, a, s, sub, row, rstd + s.Hq);
+        heads_backward<E, V, K, V == 1 ? 4 : 2>((const E *)A.dyq + m * A.dyq_rs, A.dyq_hs, (const E *)A.q + m * A.q_rs, A.q_hs, (E *)A.dq + m * A.dq_rs, A.dq_hs, s.Hq, ql, qh, dq[0], dq[1], u, a, s, sub, row, rstd);
+        heads_backward<E, V, K, V == 1 ? 4 : 2>((const E *)A.dyk + m * A.dyk_rs, A.dyk_hs, (const E *)A.k + m * A.k_rs, A.k_hs, (E *)A.dk + m * A.dk_rs, A.dk_hs, s.Hk, kl, kh, dk[0], dk[1], u, a, s, sub, row, rstd + s.Hq);
     }
     // the groups' sums, four numbers per lane at a time, in the order of the groups
     float *part = A.part + (long)blockIdx.x * 2 * s.D;

@@ -152,8 +152,9 @@ int32_t dqn_heads_backward(const dqn_heads_grad_args *args, void *stream)
             const bool w = wide(16 / (int)sizeof(E), n.dtype, A.s,
                                 {n.Hq ? n.dyq : nullptr, n.Hk ? n.dyk : nullptr, n.Hq ? n.q : nullptr, n.Hk ? n.k : nullptr, n.Hq ? n.dq : nullptr, n.Hk ? n.dk : nullptr},
                                 {n.dyq_rs, n.dyq_hs, n.dyk_rs, n.dyk_hs, n.q_rs, n.q_hs, n.k_rs, n.k_hs, n.dq_rs, n.dq_hs, n.dk_rs, n.dk_hs});
-            heads_form<E>(w, A.s, 4 * seq::HEADS_PARTS, [&](auto V, auto K) {
-                parts = std::min<int64_t>(groups_of_rows(A.s), seq::HEADS_PARTS);
+            const int64_t most = w ? seq::HEADS_PARTS / 2 : seq::HEADS_PARTS;
+            heads_form<E>(w, A.s, 4 * most, [&](auto V, auto K) {
+                parts = std::min<int64_t>(groups_of_rows(A.s), most);
                 seq::k_heads_grad<E, V.value, K.value><<<dim3((unsigned)parts), 256, 0, st>>>(A);
             });
         };
