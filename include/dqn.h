@@ -341,8 +341,10 @@ int32_t dqn_destroy(dqn_ctx *ctx);
  * part of a wider one.  Inputs and outputs of a call must not overlap except
  * where it says so.  Structs of arguments are host pointers, read during the
  * call.  Nothing is allocated.  Every call can be recorded into a HIP graph but
- * dqn_adamw_init, which waits for its stream; a recorded dqn_adamw_step repeats its
- * step number, rate and seed, and so its random bits, with every replay. */
+ * dqn_adamw_init and dqn_muon_init, which wait for their stream; a recorded dqn_adamw_step repeats its
+ * step number, rate and seed, and so its random bits, with every replay, a recorded dqn_muon_step
+ * its rate.  A call's workspace is its own until it has run: graphs that may run at the same
+ * time, or calls on several streams, take one each. */
 
 /* dtype of activations and their gradients: fp32, or bf16 with sums, states and
  * statistics in fp32. */
