@@ -1062,60 +1062,113 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_few(De
 }
 
 // ---------------------------------------------------------------- gradients
-// Two numbers to a place: for bf16 a matrix of fp32 numbers as two planes of bf16, which hold 16 bits; for fp32 the matrix.
-template <class E, int R, int C> struct Matrix;
-template <int R, int C> struct Matrix<float, R, C> {
-    static constexpr int LD = C + 4;
-    float m[R * LD];
-    __device__ __forceinline__ void put(int i, int j, float v) { m[i * LD + j] = v; }
-    __device__ __forceinline__ f8 get(int i, int j) const { return eight(m + i * LD + j); }
-    __device__ __forceinline__ float at(int i, int j) const { return m[i * LD + j]; }
-    // columns j.. and 16 + j..
-    __device__ __forceinline__ f8 pair(int i, int j) const { return both(load<4>(m + i * LD + j), load<4>(m + i * LD + j + 16)); }
-};
-template <int R, int C> struct Matrix<bf16, R, C> {
-    static constexpr int LD = C + 8;
-    bf16 m[2][R * LD];
-    __device__ __forceinline__ void put(int i, int j, float v)
+// Matrices of the gradients' products, in LDS: results are put in four rows of a column at a time and read again as operands, both ways round.
+// bf16 lies by columns, so that four rows are one store, and the transposing read makes rows of it; fp32, which has none, by rows.  Rounded holds fp32
+// numbers, in bf16 as two planes with 16 bits together, Given an input's.
+template <int R, int C> struct Plane {
+    static constexpr int LD = R + 8;
+    alignas(16) bf16 m[C * LD];
+    using s4 = vec<short, 4>;
+    // four rows, those of a group's lanes 4 x c.. to c.. + 3, of the 16 columns from i0 on: each lane gets a row of the matrix
+    __device__ __forceinline__ s4 turned(int i0, int j, int lane) const
     {
-        const uint32_t a = __float_as_uint(v), b = __float_as_uint(v - __uint_as_float(a & 0xFFFF0000u)) + 0x8000u;
-        m[0][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(a >> 16));
-        m[1][i * LD + j] = __builtin_bit_cast(bf16, (uint16_t)(b >> 16));
+        typedef __attribute__((address_space(3))) s4 *At;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(m + (j + ((lane & 15) >> 2)) * LD + i0 + 4 * (lane & 3)));
     }
-    __device__ __forceinline__ Planes<2> get(int i, int j) const { return Planes<2>{{eight(m[0] + i * LD + j), eight(m[1] + i * LD + j)}}; }
-    __device__ __forceinline__ float at(int i, int j) const { return (float)m[0][i * LD + j] + (float)m[1][i * LD + j]; }
-    __device__ __forceinline__ Planes<2> pair(int i, int j) const
+    static __device__ __forceinline__ b8 joined(s4 a, s4 b) { return __builtin_bit_cast(b8, (vec<short, 8>){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}); }
+    __device__ __forceinline__ void put(int i, int j, uint32_t ab, uint32_t cd) { *reinterpret_cast<vec<uint32_t, 2> *>(m + j * LD + i) = vec<uint32_t, 2>{ab, cd}; }
+    __device__ __forceinline__ s4 column(int i, int j) const { return load<4>(reinterpret_cast<const short *>(m) + j * LD + i); }
+    __device__ __forceinline__ b8 rows(int i0, int j, int lane) const { return joined(turned(i0, j + 8 * (lane >> 4), lane), turned(i0, j + 8 * (lane >> 4) + 4, lane)); }
+    __device__ __forceinline__ b8 pair(int i0, int lane) const { return joined(turned(i0, 4 * (lane >> 4), lane), turned(i0, 16 + 4 * (lane >> 4), lane)); }
+    __device__ __forceinline__ b8 pair_of_columns(int j0, int lane) const { return joined(column(4 * (lane >> 4), j0 + (lane & 15)), column(16 + 4 * (lane >> 4), j0 + (lane & 15))); }
+};
+template <class E, int R, int C> struct Rounded;
+template <int R, int C> struct Rounded<float, R, C> {
+    static constexpr int LD = C + 4;
+    alignas(16) float m[R * LD];
+    // rows i.. to i + 3 of column j
+    __device__ __forceinline__ void put(int i, int j, f4 v)
     {
-        Planes<2> o;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const vec<bf16, 4> a = load<4>(m[n] + i * LD + j), b = load<4>(m[n] + i * LD + j + 16);
-            o.p[n] = b8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        }
+        for (int e = 0; e < 4; ++e) m[(i + e) * LD + j] = v[e];
+    }
+    __device__ __forceinline__ f4 column(int i, int j) const { const float *a = m + i * LD + j; return f4{a[0], a[LD], a[2 * LD], a[3 * LD]}; }
+    // left or right operands: row i0 + lane % 16, columns j + 8 (lane / 16)..
+    __device__ __forceinline__ f8 rows(int i0, int j, int lane) const { return eight(m + (i0 + (lane & 15)) * LD + j + 8 * (lane >> 4)); }
+    // that row's columns 4 (lane / 16).. and 16 + 4 (lane / 16)..
+    __device__ __forceinline__ f8 pair(int i0, int lane) const
+    {
+        const float *a = m + (i0 + (lane & 15)) * LD + 4 * (lane >> 4);
+        return both(load<4>(a), load<4>(a + 16));
+    }
+    // the same of the transposed matrix
+    __device__ __forceinline__ f8 pair_of_columns(int j0, int lane) const { return both(column(4 * (lane >> 4), j0 + (lane & 15)), column(16 + 4 * (lane >> 4), j0 + (lane & 15))); }
+};
+template <int R, int C> struct Rounded<bf16, R, C> {
+    Plane<R, C> p[2];
+    __device__ __forceinline__ void put(int i, int j, f4 v)
+    {
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = __float_as_uint(v[e]), b[e] = __float_as_uint(v[e] - __uint_as_float(a[e] & 0xFFFF0000u)) + 0x8000u;
+        p[0].put(i, j, upper_halves(a[0], a[1]), upper_halves(a[2], a[3]));
+        p[1].put(i, j, upper_halves(b[0], b[1]), upper_halves(b[2], b[3]));
+    }
+    static __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+    __device__ __forceinline__ f4 column(int i, int j) const
+    {
+        const vec<short, 4> a = p[0].column(i, j), b = p[1].column(i, j);
+        f4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16) + __uint_as_float((uint32_t)(uint16_t)b[e] << 16);
         return o;
+    }
+    __device__ __forceinline__ Planes<2> rows(int i0, int j, int lane) const { return Planes<2>{{p[0].rows(i0, j, lane), p[1].rows(i0, j, lane)}}; }
+    __device__ __forceinline__ Planes<2> pair(int i0, int lane) const { return Planes<2>{{p[0].pair(i0, lane), p[1].pair(i0, lane)}}; }
+    __device__ __forceinline__ Planes<2> pair_of_columns(int j0, int lane) const { return Planes<2>{{p[0].pair_of_columns(j0, lane), p[1].pair_of_columns(j0, lane)}}; }
+};
+template <class E, int R, int C> struct Given : Rounded<float, R, C> {};
+template <int R, int C> struct Given<bf16, R, C> : Plane<R, C> {
+    __device__ __forceinline__ void put(int i, int j, f4 v)
+    {
+        Plane<R, C>::put(i, j, Rounded<bf16, R, C>::upper_halves(__float_as_uint(v[0]), __float_as_uint(v[1])), Rounded<bf16, R, C>::upper_halves(__float_as_uint(v[2]), __float_as_uint(v[3])));
     }
 };
 template <class E, int DK> struct DeltaGradTile {
-    static constexpr int LO = COLS + 16 / (int)sizeof(E);
     DeltaTile<E, DK, 7> s;
-    E dout[CH * LO];
-    Matrix<E, CH, COLS> u, y;
-    Matrix<E, DK, COLS> state, back;        // the state that enters, the gradient of the one that leaves
-    Matrix<E, CH, CH> dp, dn, dpt, dnt;     // of P's and N's products, and transposed
-    float qdq[DK / 16][CH], yu[4][CH], vdv[4][CH];      // sums over 16 columns each of q.dq, Y.u, dv.v
+    Given<E, CH, COLS> dout;
+    Rounded<E, CH, COLS> u, y;
+    Rounded<E, DK, COLS> state, back;       // the state that enters, the gradient of the one that leaves
+    Rounded<E, CH, CH> dp, dn;              // of P's and N's products
+    float qdq[DK / 16][CH], yu[2][4][CH], vdv[2][4][CH];      // sums over 16 columns each of q.dq; for even and odd tiles of Y.u, dv.v
     float ends[8];                          // of each wave: <D, S'>
     int wrong[8];                           // whether it has met a number that is not finite
 };
 
+// x of the step N later, 0 where that is in another episode or row of 16
+template <int N> __device__ __forceinline__ float after(float x, int cut)
+{
+    const float o = __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x100 + N, 0xF, 0xF, false));
+    return __builtin_amdgcn_update_dpp(-1, cut, 0x100 + N, 0xF, 0xF, false) == cut ? o : 0.f;
+}
+
 // All gradients but the state's: workgroups of eight waves, `per` tiles each, one after the other, a tile's loads under way while the one before
 // is worked on.  Of each 64 columns of the state four waves form U, four Y; then dP and dN; then the products over all columns, a wave having 16 of
 // the columns of dq and dk for half of the steps (DK = 128: for all).
-template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs A, int per)
+template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs given, int per)
 {
     using Op = Operand<E>;
     using Tile = DeltaTile<E, DK, 7>;
     using Grad = DeltaGradTile<E, DK>;
-    constexpr int LO = Grad::LO, NM = DK == 128 ? 2 : 1;
+    constexpr int NM = DK == 128 ? 2 : 1;
+    // The arguments are more than scalar registers hold.  Each part reads them anew: kept over all of them they would be moved to vector registers' lanes
+    // and back.
+    auto arguments = []() -> const DeltaGradArgs & {
+        auto *p = (const __attribute__((address_space(4))) DeltaGradArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(p));
+        return *(const DeltaGradArgs *)p;
+    };
+    const DeltaGradArgs &A = arguments();
     extern __shared__ __align__(16) unsigned char lds[];
     Grad &g = *reinterpret_cast<Grad *>(lds);
     Tile &s = g.s;
@@ -1139,6 +1192,7 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
     const float *states = for_y ? A.into : A.states;
     in.rows = 0;
     auto get = [&](unsigned which, int sl, bool new_head) {
+        const DeltaGradArgs &A = arguments();
         const unsigned head = which / tiles, tile = which % tiles;
         const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H), rows = (int)min((long)CH, A.T - (long)tile * CH), c = sl + 16 * wc + col;
         if (new_head) {
@@ -1150,8 +1204,53 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
         in.load(steps + (long)tile * CH * ts, (int)ts, c, A.Dv, rows, lane);
         st.load(states + ((long)which * blocks + min(sl / 16 + wc, blocks - 1)) * 16 * DK, lane);
     };
+    // The gradients of gates and rates are formed from the sums of all waves, a step per lane, by the last wave, one tile late, while the others have
+    // dP and dN.  What that takes of the tile is kept meanwhile.
+    const unsigned first = id;
+    const int step = lane & 31;
+    struct Gates {
+        E f, b;             // the inputs, as they are: a conversion would wait for them, and with them for all that was asked for before
+        E *df, *db;
+        int rows;
+    };
+    Gates last{};
+    float f_in = 0.f, b_in = 0.f;
+    int cut = 0;
+    bool still = false;
+    auto take = [&]() {         // after the wait for later loads
+        f_in = (float)last.f, b_in = (float)last.b;
+        asm volatile("" : "+v"(f_in), "+v"(b_in));      // here, not where they are used
+    };
+    auto finish = [&]() {
+        const DeltaGradArgs &A = arguments();
+        int again = 0;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) again |= g.wrong[n];
+        const float (&vdv)[4][CH] = g.vdv[(id - 1) & 1], (&yu)[4][CH] = g.yu[(id - 1) & 1];
+        if (lane == 0) A.again[id - 1] = again;
+        float x = 0.f;
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][step];
+        x = step < last.rows ? x - ((vdv[0][step] + vdv[1][step]) + (vdv[2][step] + vdv[3][step])) : 0.f;
+        float end = 0.f;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) end += g.ends[n];
+        x += step == last.rows - 1 ? end : 0.f;
+        x += after<1>(x, cut);      // sums to the episode's end, of 16 steps, then of 32
+        x += after<2>(x, cut);
+        x += after<4>(x, cut);
+        x += after<8>(x, cut);
+        const float half = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 16));
+        x += step < 16 && cut == __builtin_amdgcn_readlane(cut, 16) ? half : 0.f;
+        if (lane < last.rows && !again) {      // else k_delta_grad_steps's
+            const float rate = (yu[0][step] + yu[1][step]) + (yu[2][step] + yu[3][step]);
+            *last.df = (E)(still ? 0.f : x * (1.f / (1.f + expf(f_in))));
+            *last.db = (E)(rate * (1.f / (1.f + expf(b_in))));
+        }
+    };
     if (id < stop) get(id, 0, true);
     for (; id < stop; ++id) {
+        const DeltaGradArgs &A = arguments();
         const unsigned head = id / tiles, tile = id % tiles;
         const int bi = (int)(head / (unsigned)A.H), h = (int)(head % (unsigned)A.H);
         const long t0 = (long)tile * CH;
@@ -1169,21 +1268,18 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
             {
                 auto &to = for_y ? g.back : g.state;
 #pragma unroll
-                for (int n = 0; n < DK / 16; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) to.put(32 * (n >> 1) + 8 * grp + 4 * (n & 1) + e, 16 * wc + col, st.s[n][e]);
+                for (int n = 0; n < DK / 16; ++n) to.put(32 * (n >> 1) + 8 * grp + 4 * (n & 1), 16 * wc + col, st.s[n]);
             }
             typename Op::template Split<2> sp[DK / 32];
 #pragma unroll
             for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 2>(st.s[2 * p], st.s[2 * p + 1]);
+            if (w == 7 && sl == 0) take();
             lds_barrier();
             if (!for_y) {
                 delta_u<E, DK, 2>(s, sp, val, rows, lane, res);
                 wrong += nothing(res);
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) g.u.put(16 * m + 4 * grp + e, 16 * wc + col, res[m][e]);
+                for (int m = 0; m < 2; ++m) g.u.put(16 * m + 4 * grp, 16 * wc + col, res[m]);
             } else {
                 f4 y[2], dv[2], pd[2] = {};
                 upper<Tile::LC>(s.p, val, lane, pd);
@@ -1191,12 +1287,8 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     dv[m] = of_steps(s.beta(), m, lane) * y[m];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 16 * m + 4 * grp + e;
-                        g.dout[i * LO + 16 * wc + col] = (E)val[m][e];
-                        g.y.put(i, 16 * wc + col, y[m][e]);
-                    }
+                    g.dout.put(16 * m + 4 * grp, 16 * wc + col, val[m]);
+                    g.y.put(16 * m + 4 * grp, 16 * wc + col, y[m]);
                 }
                 wrong += nothing(dv);
                 put_steps(head_of<E>(A.dv, A.sdv, bi, h) + t0 * A.sdv.ts, (int)A.sdv.ts, c, mine, rows, lane, dv);
@@ -1205,90 +1297,97 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
             if (!for_y) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    const f4 beta = of_steps(s.beta(), m, lane);
+                    const f4 beta = of_steps(s.beta(), m, lane), y = g.y.column(16 * m + 4 * grp, 16 * wc + col);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int i = 16 * m + 4 * grp + e;
-                        const float y = g.y.at(i, 16 * wc + col);
-                        const float a = group_fold(y * res[m][e], 16, add), b = group_fold(beta[e] * y * val[m][e], 16, add);
+                        const float a = group_fold(y[e] * res[m][e], 16, add), b = group_fold(beta[e] * y[e] * val[m][e], 16, add);
                         if (col == 0) {
-                            g.yu[wc][i] = sl ? g.yu[wc][i] + a : a;
-                            g.vdv[wc][i] = sl ? g.vdv[wc][i] + b : b;
+                            float &yu = g.yu[id & 1][wc][i], &vdv = g.vdv[id & 1][wc][i];
+                            yu = sl ? yu + a : a;
+                            vdv = sl ? vdv + b : b;
                         }
                     }
                 }
             } else {
                 const float left = s.since()[CH - 1];
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m) {
+                    const f4 u = g.u.column(16 * m + 4 * grp, 16 * wc + col);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) end = fmaf(res[m][e], g.u.at(16 * m + 4 * grp + e, 16 * wc + col), end);
+                    for (int e = 0; e < 4; ++e) end = fmaf(res[m][e], u[e], end);
+                }
                 if (left != 0.f)
 #pragma unroll
-                    for (int n = 0; n < DK / 16; ++n)
+                    for (int n = 0; n < DK / 16; ++n) {
+                        const f4 entered = g.state.column(32 * (n >> 1) + 8 * grp + 4 * (n & 1), 16 * wc + col);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) end = fmaf(left * g.state.at(32 * (n >> 1) + 8 * grp + 4 * (n & 1) + e, 16 * wc + col), st.s[n][e], end);
+                        for (int e = 0; e < 4; ++e) end = fmaf(left * entered[e], st.s[n][e], end);
+                    }
             }
             const bool same = sl + COLS < A.Dv;
             if (same || id + 1 < stop) get(same ? id : id + 1, same ? sl + COLS : 0, !same && tile + 1 == tiles);
             if (wc < 3) {
 #pragma unroll
                 for (int kb = 0; kb < COLS; kb += 32) {
-                    const auto b = g.u.get(tj + col, kb + 8 * grp);
-                    if (!for_y) part = Op::mul(eight(g.dout + (ti + col) * LO + kb + 8 * grp), b, part);
-                    else part = Op::mul(g.y.get(ti + col, kb + 8 * grp), b, part);
+                    const auto b = g.u.rows(tj, kb, lane);
+                    if (!for_y) part = Op::mul(g.dout.rows(ti, kb, lane), b, part);
+                    else part = Op::mul(g.y.rows(ti, kb, lane), b, part);
                 }
             }
             // columns 16 d.. of dO S^T, Y S^T and U D^T
             if (has) {
 #pragma unroll
                 for (int kb = 0; kb < COLS; kb += 32) {
-                    const auto sr = g.state.get(dk, kb + 8 * grp), dr = g.back.get(dk, kb + 8 * grp);
+                    const auto sr = g.state.rows(16 * d, kb, lane), dr = g.back.rows(16 * d, kb, lane);
 #pragma unroll
                     for (int m = 0; m < NM; ++m) {
-                        const int i = 16 * (m0 + m) + col, k = kb + 8 * grp;
-                        os[m] = Op::mul(eight(g.dout + i * LO + k), sr, os[m]);
-                        ys[m] = Op::mul(g.y.get(i, k), sr, ys[m]);
-                        ud[m] = Op::mul(g.u.get(i, k), dr, ud[m]);
+                        const int i = 16 * (m0 + m);
+                        os[m] = Op::mul(g.dout.rows(i, kb, lane), sr, os[m]);
+                        ys[m] = Op::mul(g.y.rows(i, kb, lane), sr, ys[m]);
+                        ud[m] = Op::mul(g.u.rows(i, kb, lane), dr, ud[m]);
                     }
                 }
             }
         }
         if (wc < 3) {
             auto &to = for_y ? g.dn : g.dp;
-            auto &tr = for_y ? g.dnt : g.dpt;
             const int i0 = ti + 4 * grp, j = tj + col, cut_j = s.cut()[j];
             const vec<int, 4> cut_i = load<4>(s.cut() + i0);
             const f4 hi_i = load<4>(s.run_hi() + i0), lo_i = load<4>(s.run_lo() + i0), beta = load<4>(s.beta() + i0);
             const float hi_j = s.run_hi()[j], lo_j = s.run_lo()[j];
+            f4 q;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = i0 + r;
                 const float b = j > i || (for_y && j == i) || cut_i[r] != cut_j ? 0.f : between(hi_i[r], lo_i[r], hi_j, lo_j);
-                const float q = b == 0.f ? 0.f : (for_y ? -beta[r] : A.scale) * b * part[r];
-                to.put(i, j, q);
-                tr.put(j, i, q);
+                q[r] = b == 0.f ? 0.f : (for_y ? -beta[r] : A.scale) * b * part[r];
             }
+            to.put(i0, j, q);
         } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {       // above the diagonal
-                (for_y ? g.dn : g.dp).put(4 * grp + r, 16 + col, 0.f);
-                (for_y ? g.dnt : g.dpt).put(16 + col, 4 * grp + r, 0.f);
+            (for_y ? g.dn : g.dp).put(4 * grp, 16 + col, f4{});     // above the diagonal
+            if (for_y) {
+                if (id > first) finish();
+                const DeltaGradArgs &A = arguments();
+                const long t = min(t0 + step, A.T - 1);
+                last = Gates{((const E *)A.f)[bi * A.sf.bs + t * A.sf.ts + h * A.sf.hs], ((const E *)A.b)[bi * A.sb.bs + t * A.sb.ts + h * A.sb.hs],
+                             (E *)A.df + bi * A.sdf.bs + t * A.sdf.ts + h * A.sdf.hs, (E *)A.db + bi * A.sdb.bs + t * A.sdb.ts + h * A.sdb.hs, rows};
             }
         }
         lds_barrier();
         if (has) {
+            const DeltaGradArgs &A = arguments();
             const typename Op::Exact kc = columns_of<1, Tile::LD>(s.k + 16 * d, lane), qc = columns_of<1, Tile::LD>(s.q + 16 * d, lane);
             E *dq = head_of<E>(A.dq, A.sdq, bi, h) + t0 * A.sdq.ts, *dkp = head_of<E>(A.dk, A.sdk, bi, h) + t0 * A.sdk.ts;
 #pragma unroll
             for (int n = 0; n < NM; ++n) {
-                const int m = m0 + n, i0 = 16 * m + col;
+                const int m = m0 + n, i0 = 16 * m;
                 const f4 since = of_steps(s.since(), m, lane), beta = of_steps(s.beta(), m, lane), until = of_steps(s.until(), m, lane);
                 f4 r[2] = {where(since, A.scale * os[n]), where(since, -beta * ys[n]) + where(until, ud[n])};
-                r[0] = Op::mul(g.dp.pair(i0, 4 * grp), kc, r[0]);
-                r[1] = Op::mul(g.dpt.pair(i0, 4 * grp), qc, r[1]);
-                r[1] = Op::mul(g.dn.pair(i0, 4 * grp), kc, r[1]);
-                r[1] = Op::mul(g.dnt.pair(i0, 4 * grp), kc, r[1]);
+                r[0] = Op::mul(g.dp.pair(i0, lane), kc, r[0]);
+                r[1] = Op::mul(g.dp.pair_of_columns(i0, lane), qc, r[1]);
+                r[1] = Op::mul(g.dn.pair(i0, lane), kc, r[1]);
+                r[1] = Op::mul(g.dn.pair_of_columns(i0, lane), kc, r[1]);
                 wrong += nothing(r);
                 const int i = 16 * m + 4 * grp;
                 const uint32_t qa = (uint32_t)(i * (int)A.sdq.ts + dk), ka = (uint32_t)(i * (int)A.sdk.ts + dk);
@@ -1316,37 +1415,17 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
         end = group_fold(end, 64, add);
         wrong = wrong + end * 0.f;
         if (lane == 0) g.ends[w] = end;
-        const int step = lane & 31, cut = s.cut()[step];      // before the next tile takes their place
-        const bool still = starts(s.cut(), step) || s.gate()[step] == 0.f;
+        if (w == 7) {
+            cut = s.cut()[step];
+            still = starts(s.cut(), step) || s.gate()[step] == 0.f;
+        }
         if (__any(wrong != 0.f) && lane == 0) g.wrong[w] = 1;
         else if (lane == 0) g.wrong[w] = 0;
         lds_barrier();
-        if (w == 0) {
-            int again = 0;
-#pragma unroll
-            for (int n = 0; n < 8; ++n) again |= g.wrong[n];
-            if (lane == 0) A.again[id] = again;
-            const int i = step;
-            float x = 0.f;
-#pragma unroll
-            for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][i];
-            x = i < rows ? x - ((g.vdv[0][i] + g.vdv[1][i]) + (g.vdv[2][i] + g.vdv[3][i])) : 0.f;
-            if (i == rows - 1)
-#pragma unroll
-                for (int n = 0; n < 8; ++n) x += g.ends[n];
-#pragma unroll
-            for (int n = 1; n < CH; n *= 2) {
-                const float o = __shfl_down(x, n, CH);
-                const int oc = __shfl_down(cut, n, CH);
-                if (i + n < CH && oc == cut) x += o;
-            }
-            if (lane < rows && !again) {      // else k_delta_grad_steps's
-                const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + i) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + i) * A.sb.ts + h * A.sb.hs];
-                const float rate = (g.yu[0][i] + g.yu[1][i]) + (g.yu[2][i] + g.yu[3][i]);
-                ((E *)A.df)[bi * A.sdf.bs + (t0 + i) * A.sdf.ts + h * A.sdf.hs] = (E)(still ? 0.f : x * (1.f / (1.f + expf(f))));
-                ((E *)A.db)[bi * A.sdb.bs + (t0 + i) * A.sdb.ts + h * A.sdb.hs] = (E)(rate * (1.f / (1.f + expf(b))));
-            }
-        }
+    }
+    if (w == 7 && id > first) {
+        take();
+        finish();
     }
 }
 
