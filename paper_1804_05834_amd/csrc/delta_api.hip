@@ -85,7 +85,9 @@ size_t record_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s
 size_t state_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.T) * width_of(s.Dk) * ((s.Dv + 15) / 16 * 16) * 4; }
 
 // Ranges of a head's tiles, where there are fewer workgroups of a chain than compute units.  All of its tiles are gone through three times then
-// (the maps take as many columns again), so that fewer than four ranges would not pay.
+// (the maps take as many columns again), so that fewer than four ranges would not pay.  Measured (bf16, 64 x 64, forward / backward): 4 ranges
+// (64 heads of 4096 steps) 207 / 414 us, one 286 / 457; 3 (85 heads) 276 / 557, one 305 / 534; 2 (128 heads) 413 / 809, one 346 / 668.  Ranges of
+// 4 tiles (4 heads of 1024 steps) 37 / 44 us, of 8 47 / 56, one 71 / 72; of 2 tiles, which makes 64 of them at 4096 steps, 80 / 95 for 57 / 72.
 constexpr int64_t UNITS = 256, LEAST_TILES = 4, LEAST_RANGES = 4;
 template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t tiles, int Dv)
 {
@@ -143,7 +145,7 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
     seq::k_delta<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, bytes, st>>>(A, R);
     return true;
 }
-constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit
+constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit, which is all that fits; 512 in two turns: 4 % slower
 template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, void *workspace, hipStream_t st)
 {
     static std::atomic<uint64_t> back_granted{0}, maps_granted{0}, granted{0};

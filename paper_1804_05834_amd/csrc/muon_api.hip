@@ -24,7 +24,7 @@ constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
 // Parts of a product that are enough for 256 compute units, by their size.  us a launch in parts of 64, 128, 256: B X of twelve matrices of 1024 x 4096 and
 // 2048 x 2048 (768 parts of 256) 822, 582, 424, their X X^T (224) 434, 307, 311; of a block of 512 channels (196 parts of 128) 22, 26, 64.
 constexpr int64_t ENOUGH[3] = {0, 256, 192};
-constexpr int64_t MOST_CUTS = 8;
+constexpr int64_t MOST_CUTS = 6;
 
 const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
 {
@@ -80,8 +80,9 @@ Total total_of(const dqn_muon_matrix *t, int32_t count)
 
 // The largest parts of which there is enough for the compute units.
 int part_of(const int64_t (&n)[3]) { return n[2] >= ENOUGH[2] ? 2 : n[1] >= ENOUGH[1] ? 1 : 0; }
-// Sums that X X^T is cut into where it has few parts (of 64 x 64): as many as leave a workgroup for each compute unit.
-int cuts_of(int64_t parts) { return parts ? (int)std::max<int64_t>(1, std::min<int64_t>(MOST_CUTS, 256 / parts)) : 1; }
+// Sums that X X^T is cut into where it has few parts (of 64 x 64), for one to two workgroups per compute unit, two being what LDS has place for.  A step with
+// 144 parts: uncut 329 us, in two 299, in three 314; with 40 parts: in six 204, in eight 211, in twelve 234.
+int cuts_of(int64_t parts) { return parts ? (int)std::max<int64_t>(1, std::min<int64_t>(MOST_CUTS, 384 / parts)) : 1; }
 size_t sums_bytes(int64_t parts) { return cuts_of(parts) > 1 ? (size_t)parts * cuts_of(parts) * 64 * 64 * 4 : 0; }
 template <int T> bool granted_lds()
 {
