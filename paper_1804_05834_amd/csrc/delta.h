@@ -201,6 +201,9 @@ __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float between(float hi_i, float lo_i, float hi_j, float lo_j) { return power((hi_i - hi_j) + (lo_i - lo_j)); }
 
 // ---------------------------------------------------------------- T, P and the gates of every tile
+// A wave per tile.  K K^T and Q K^T are a few matrix instructions; the time goes into what waits step after step: the sums of the gates' logarithms
+// (in 64 bits), and the substitution that forms T's blocks on the diagonal, 16 rows one after the other.  32 x 512 x 8 x 64 in bf16, 4096 tiles: 18 us;
+// 4096 of 128 columns 23.
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(DeltaIn A, DeltaRecord *records)
 {
     constexpr int LN = CH + 4, KS = DK / 32;
@@ -697,6 +700,10 @@ __device__ __forceinline__ void delta_y(const Tile &s, const typename Operand<E>
 // Where heads are few, a head's tiles are cut into ranges.  What a range does to the state is a linear map and an addition, S -> M S + B; a first
 // launch (MAPS) finds both, M by the same chain from the unit matrix's columns, a second goes from range to range, and the last has all
 // ranges' first states.
+// Bound by what follows upon what within a tile: state into planes, S^T k, T, K^T u, each a few matrix instructions deep, and two barriers' worth of waiting
+// for LDS: 2.8 us a tile of 64 x 64 in bf16 (256 heads of 16 tiles, forward 46 us, backward 43), 3.1 of 128 x 128 (a head of 1024 tiles in 32 ranges: 100 us, the
+// maps, which are as many columns again on the same compute units, 148).  With
+// one wave for both parts of a pair: 72 and 62 us for 46 and 43.
 // A tile whose results hold a number that is not finite is taken again step by step as the definition has it, where nothing is multiplied by the
 // zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
 template <class E, int DK> struct DeltaPairs {
@@ -1018,7 +1025,9 @@ template <int DK, bool BACK> __global__ __launch_bounds__(8 * DK) void k_delta_j
     }
 }
 
-// Few steps, of an acting agent say: the definition, step by step, a wave per 16 columns of a head's state.
+// Few steps, of an acting agent say: the definition, step by step, a wave per 16 columns of a head's state.  Read and written once, the state is the
+// traffic: 32 x 8 x 64 x 64 and one step 6 us, most of it a launch's way to memory and back; 2048 x 8 heads 120 us, 540 MB at 4.5 TB/s.  Up to 8 steps: 2048 x 8 x 64
+// x 64 take 413 us with 8, the other way 443 with 9, 32 x 8 x 64 x 64 13 and 14; at 32 x 4 x 128 x 128 the other way would be quicker from 6 steps on (8: 21 us, 9: 17).
 constexpr long STEPS_MOST = 8;
 template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_few(DeltaArgs A)
 {
@@ -1155,6 +1164,9 @@ template <int N> __device__ __forceinline__ float after(float x, int cut)
 // All gradients but the state's: workgroups of eight waves, `per` tiles each, one after the other, a tile's loads under way while the one before
 // is worked on.  Of each 64 columns of the state four waves form U, four Y; then dP and dN; then the products over all columns, a wave having 16 of
 // the columns of dq and dk for half of the steps (DK = 128: for all).
+// 32 x 512 x 8 x 64 in bf16: 111 us, 16 tiles of 64 KB a compute unit, 2.4 TB/s.  What bounds it is the way through a tile, 15000 cycles in four parts between
+// barriers, in which two waves a SIMD share the vector instructions.  Both directions together: with four waves a workgroup
+// 461 us, with eight 313, with the next tile's loads under way and states as the waves hold them 252, with matrices by columns and arguments read anew 216.
 template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs given, int per)
 {
     using Op = Operand<E>;

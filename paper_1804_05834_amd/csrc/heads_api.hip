@@ -77,7 +77,7 @@ template <class E, class F> void heads_form(bool wide, seq::HeadsShape &s, int64
     else if (units <= 64) go(Int<1>{}, Int<1>{});
     else go(Int<1>{}, Int<2>{});
 }
-constexpr int64_t WAVES = 4096;
+constexpr int64_t WAVES = 4096;     // four per SIMD
 int64_t groups_of_rows(const seq::HeadsShape &s) { return (s.M + 256 / s.lanes / s.per_row - 1) / (256 / s.lanes / s.per_row); }
 
 }  // namespace
