@@ -657,7 +657,8 @@ typedef struct dqn_muon dqn_muon;
 /* `matrices`: host array of `count` descriptions, 1 <= count <= 65536; its device pointers must stay valid, as must plan and
  * workspace (256-byte aligned, bytes from dqn_muon_sizes): a step uses both, so steps of one handle are not to overlap.
  * The handle owns host-side bookkeeping only; the table is copied to `plan` on `stream` during dqn_muon_init, which
- * waits for the copy and so cannot be recorded into a graph. */
+ * waits for the copy and so cannot be recorded into a graph.  No param, momentum or copy may lie on another buffer (gradients may
+ * lie on each other). */
 int32_t dqn_muon_sizes(const dqn_muon_matrix *matrices, int32_t count, size_t *plan, size_t *workspace);
 int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t count, int32_t grad_dtype, void *plan,
                       void *workspace, void *stream);

@@ -38,6 +38,33 @@ const char *check_matrices(const dqn_muon_matrix *t, int32_t count)
     return nullptr;
 }
 
+// Whether a buffer that a step writes (parameters, momentum, copy) lies on any other, a gradient's too: the same matrix twice, say.
+bool overlapping(const dqn_muon_matrix *t, int32_t count, size_t grad_bytes)
+{
+    struct Range {
+        uintptr_t begin, end;
+        bool written;
+    };
+    std::vector<Range> ranges;
+    auto add = [&](const void *p, size_t bytes, bool written) { ranges.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written}); };
+    for (int32_t i = 0; i < count; ++i) {
+        const size_t n = (size_t)t[i].rows * (size_t)t[i].cols;
+        if (!n) continue;
+        add(t[i].param, 4 * n, true);
+        add(t[i].momentum, 4 * n, true);
+        add(t[i].grad, grad_bytes * n, false);
+        if (t[i].copy) add(t[i].copy, 2 * n, true);
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range &x, const Range &y) { return x.begin < y.begin; });
+    uintptr_t any = 0, written = 0;
+    for (const Range &r : ranges) {
+        if (r.begin < (r.written ? any : written)) return true;
+        any = std::max(any, r.end);
+        if (r.written) written = std::max(written, r.end);
+    }
+    return false;
+}
+
 // Of one matrix: its padded sides and its parts of the workspace in bytes, in their order.
 struct Parts {
     int64_t rp, cp, chunks, x, a, sums;
@@ -133,6 +160,7 @@ int32_t dqn_muon_init(dqn_muon **out, const dqn_muon_matrix *matrices, int32_t c
     if (s.chunks >= 1 << 24 || s.start >= 1 << 24 || s.half[0] >= 1 << 24 || s.whole[0] >= 1 << 24) return bad(call, "too many elements");   // a launch has 2^32 threads
     dqn_muon *o = nullptr;
     try {
+        if (overlapping(matrices, count, bytes_of(grad_dtype))) return bad(call, "a matrix's parameters, momentum or copy lie on another buffer");
         std::vector<seq::MuonMatrix> table;
         table.reserve((size_t)count);
         uint8_t *at = (uint8_t *)workspace;

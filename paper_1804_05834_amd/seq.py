@@ -272,7 +272,10 @@ def delta_backward(do, q, k, v, f, b, carry, reset=None, dlast=None, scale=1.0, 
     gp, gs = _rows(do, "do", dt, (B, T, H, Dv), dev)
     carry_n, _, work_n = _delta_sizes(kind, B, T, H, Dk, Dv)
     grads, gat, gstrides = [], [], []
-    for name, x, y in zip(("dq", "dk", "dv", "df", "db"), (q, k, v, f, b), out or (None,) * 5):
+    out = (None,) * 5 if out is None else tuple(out)
+    if len(out) != 5:
+        raise ValueError("out: (dq, dk, dv, df, db) expected")
+    for name, x, y in zip(("dq", "dk", "dv", "df", "db"), (q, k, v, f, b), out):
         if y is None:
             y = torch.empty(x.shape, dtype=dt, device=x.device)
         p, st = (_rows if y.dim() == 4 else _strided)(y, name, dt, x.shape, dev)

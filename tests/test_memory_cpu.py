@@ -192,6 +192,18 @@ def test_muon_refuses(lib):
     assert lib.dqn_muon_destroy(None) == dqn.OK
 
 
+def test_muon_refuses_buffers_that_lie_on_each_other(lib):
+    """The same matrix twice would be written by two workgroups at once."""
+    h, n = C.c_void_p(), 30 * 70
+    apart = [P + 4096 * 1024 * i for i in range(8)]
+    for which, what in ((("param", "param"), 0), (("momentum", "momentum"), 0), (("param", "momentum"), 4 * n - 4), (("copy", "copy"), 2 * n - 2), (("grad", "param"), 0), (("momentum", "grad"), 4 * n - 4),
+                        (("param", "grad"), 2 * n)):
+        t = (seq._MuonMatrix * 2)(*(seq._MuonMatrix(*apart[4 * i:4 * i + 4], 30, 70, 0.0) for i in range(2)))
+        setattr(t[1], which[1], getattr(t[0], which[0]) + what)
+        assert lib.dqn_muon_init(C.byref(h), t, 2, 0, P, P, None) == dqn.ERR_INVALID_ARG and not h.value, which
+        assert b"another buffer" in lib.dqn_last_error(None)
+
+
 def test_the_rounds_take_singular_values_near_one():
     r = np.random.RandomState(3)
     for n, m in ((5, 40), (40, 5), (8, 8)):
