@@ -323,10 +323,11 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
 }
 
 // ---------------------------------------------------------------- what a workgroup holds of a tile in LDS
-template <class E, int DK, int VECTORS> struct DeltaTile {      // VECTORS: how many of the record's, from `since` on
+template <class E, int DK, int VECTORS> struct DeltaKeys {      // VECTORS: how many of the record's, from `since` on
     static constexpr int LD = DK + 16 / (int)sizeof(E), LC = CH + 4;
-    E q[CH * LD], k[CH * LD];
-    float t[CH * LC], p[CH * LC];
+    static constexpr bool QUERIES = false;
+    alignas(16) E k[CH * LD];
+    float t[CH * LC];
     float vectors[VECTORS * CH];
     __device__ __forceinline__ const float *since() const { return vectors; }
     __device__ __forceinline__ const float *until() const { return vectors + CH; }
@@ -336,6 +337,12 @@ template <class E, int DK, int VECTORS> struct DeltaTile {      // VECTORS: how 
     __device__ __forceinline__ const float *run_lo() const { return vectors + 5 * CH; }
     __device__ __forceinline__ const int *cut() const { return reinterpret_cast<const int *>(vectors + 6 * CH); }
 };
+template <class E, int DK, int VECTORS> struct DeltaTile : DeltaKeys<E, DK, VECTORS> {
+    using Keys = DeltaKeys<E, DK, VECTORS>;
+    static constexpr bool QUERIES = true;
+    alignas(16) E q[CH * Keys::LD];
+    float p[CH * Keys::LC];
+};
 
 // Where a head's tensors begin, for all lanes alike, and 32-bit offsets from there: a stride from step to step is at most 2^24 elements.
 template <class E> __device__ __forceinline__ const E *head_of(const void *p, const Strides &s, int bi, int h) { return (const E *)p + bi * s.bs + h * s.hs; }
@@ -344,7 +351,7 @@ template <class T> __device__ __forceinline__ T *plus(T *p, uint32_t bytes) { re
 template <class T> __device__ __forceinline__ const T *plus(const T *p, uint32_t bytes) { return (const T *)((const char *)p + bytes); }
 
 // The part of a tile that a thread of THREADS brings from memory: into registers first, so that it can arrive while another tile is worked on.
-template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
+template <class E, int DK, int THREADS, int VECTORS, class Tile = DeltaTile<E, DK, VECTORS>> struct DeltaFetch {
     static constexpr int V = 16 / (int)sizeof(E), PER = DK / V, N = (CH * PER + THREADS - 1) / THREADS, NR = (CH * CH / 4 + THREADS - 1) / THREADS;
     static_assert(VECTORS * CH / 4 <= THREADS, "a thread brings one piece of the vectors");
     const E *qh, *kh;
@@ -380,7 +387,7 @@ template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
         if (A.wide) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                q[n] = seq::load<V>(plus(qp, qo[n]));
+                if (Tile::QUERIES) q[n] = seq::load<V>(plus(qp, qo[n]));
                 k[n] = seq::load<V>(plus(kp, ko[n]));
             }
         } else {
@@ -390,7 +397,7 @@ template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const int more = max(0, min(i, A.Dk - 1 - c));
-                    q[n][i] = plus(qp, qo[n])[more];
+                    if (Tile::QUERIES) q[n][i] = plus(qp, qo[n])[more];
                     k[n][i] = plus(kp, ko[n])[more];
                 }
             }
@@ -400,18 +407,18 @@ template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
         for (int n = 0; n < NR; ++n) {
             const int e = min(tid + THREADS * n, CH * CH / 4 - 1);
             t[n] = seq::load<4>(rec->t + 4 * e);
-            p[n] = seq::load<4>(rec->p + 4 * e);
+            if (Tile::QUERIES) p[n] = seq::load<4>(rec->p + 4 * e);
         }
         vectors = seq::load<4>(rec->since + 4 * min(tid, VECTORS * CH / 4 - 1));
     }
-    __device__ __forceinline__ void put(DeltaTile<E, DK, VECTORS> &s, int Dk) const
+    __device__ __forceinline__ void put(Tile &s, int Dk) const
     {
-        using Tile = DeltaTile<E, DK, VECTORS>;
         const bool whole = rows == CH && Dk == DK;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int e = tid + THREADS * n, r = e / PER, c = e % PER * V;
-            vec<E, V> x = q[n], y = k[n];
+            vec<E, V> x{}, y = k[n];
+            if (Tile::QUERIES) x = q[n];
             if (!whole)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -420,7 +427,7 @@ template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
                     y[i] = in ? y[i] : (E)0.f;
                 }
             if (CH * PER % THREADS == 0 || r < CH) {
-                seq::store<V>(s.q + r * Tile::LD + c, x);
+                if constexpr (Tile::QUERIES) seq::store<V>(s.q + r * Tile::LD + c, x);
                 seq::store<V>(s.k + r * Tile::LD + c, y);
             }
         }
@@ -429,7 +436,7 @@ template <class E, int DK, int THREADS, int VECTORS> struct DeltaFetch {
             const int e = tid + THREADS * n, r = e / 8, c = e % 8 * 4;
             if (CH * CH / 4 % THREADS == 0 || r < CH) {
                 seq::store<4>(s.t + r * Tile::LC + c, t[n]);
-                seq::store<4>(s.p + r * Tile::LC + c, p[n]);
+                if constexpr (Tile::QUERIES) seq::store<4>(s.p + r * Tile::LC + c, p[n]);
             }
         }
         if (tid < VECTORS * CH / 4) seq::store<4>(s.vectors + 4 * tid, vectors);
@@ -515,7 +522,8 @@ __device__ __forceinline__ f4 where(f4 factor, f4 v)      // factor v, 0 where f
     for (int e = 0; e < 4; ++e) o[e] = factor[e] != 0.f ? factor[e] * v[e] : 0.f;
     return o;
 }
-__device__ __forceinline__ f4 where(float factor, f4 v) { return where(f4(factor), v); }
+// for a number that is the same in all lanes
+__device__ __forceinline__ bool is_zero(float x) { return (__builtin_amdgcn_readfirstlane(__float_as_uint(x)) & 0x7FFFFFFFu) == 0; }
 
 // the sum over the four groups of 16 lanes, in all of them
 __device__ __forceinline__ float groups_sum(float x)
@@ -701,9 +709,8 @@ __device__ __forceinline__ void delta_y(const Tile &s, const typename Operand<E>
 // launch (MAPS) finds both, M by the same chain from the unit matrix's columns, a second goes from range to range, and the last has all
 // ranges' first states.
 // Bound by what follows upon what within a tile: state into planes, S^T k, T, K^T u, each a few matrix instructions deep, and two barriers' worth of waiting
-// for LDS: 2.8 us a tile of 64 x 64 in bf16 (256 heads of 16 tiles, forward 46 us, backward 43), 3.1 of 128 x 128 (a head of 1024 tiles in 32 ranges: 100 us, the
-// maps, which are as many columns again on the same compute units, 148).  With
-// one wave for both parts of a pair: 72 and 62 us for 46 and 43.
+// for LDS: 2.8 us a tile of 64 x 64 in bf16 (256 heads of 16 tiles, forward 46 us, backward 43), 3.1 of 128 x 128 (a head of 1024 tiles in 32 ranges:
+// 98 us).  With one wave for both parts of a pair: 72 and 62 us for 46 and 43.
 // A tile whose results hold a number that is not finite is taken again step by step as the definition has it, where nothing is multiplied by the
 // zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
 template <class E, int DK> struct DeltaPairs {
@@ -711,7 +718,17 @@ template <class E, int DK> struct DeltaPairs {
     static constexpr int waves = 3 * tile + 4 * pair <= room ? 4 : 3 * tile + 2 * pair <= room ? 2 : 1;
 };
 template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>::waves;
+// A launch that finds the maps of the forward direction has no outputs: keys alone, and four waves of a chain that bring their tiles themselves.  So two
+// workgroups fit into a compute unit, and one has what the other waits for: the same head's maps, twice the state's columns, 110 us; in pairs of waves 147.
+constexpr int MAPS_WAVES = 4;
+template <class E, int DK> struct DeltaMaps {
+    static constexpr int WAVES = MAPS_WAVES, OTHERS = 0, PER_SIMD = 2;
+    using Tile = DeltaKeys<E, DK, 3>;
+    Tile tiles[3];
+};
 template <class E, int DK> struct DeltaChain {
+    using Tile = DeltaTile<E, DK, 3>;
+    static constexpr int OTHERS = DeltaPairs<E, DK>::waves, PER_SIMD = 1;
     static constexpr int WAVES = DeltaPairs<E, DK>::waves;
     DeltaTile<E, DK, 3> tiles[3];
     f4 state[2][WAVES][DK / 16][64];      // forward: the state that enters; backward: (scale g Q)^T dO
@@ -725,14 +742,13 @@ struct DeltaRanges {
     float *m, *b, *first;                 // [heads][ranges][..]
 };
 // A wave's place: head, range and block of 16 columns; with MAPS the blocks behind those of the state are M's.
-template <class E, int DK, bool MAPS> struct ChainPlace {
+template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> struct ChainPlace {
     unsigned head;
     int range, block, blocks, bi, h, c;
     long tile0, n;                        // the range's first tile, how many it has
     bool mine, unit;                      // whether the column is one of the state's; whether the block is one of M's
     __device__ __forceinline__ ChainPlace(const DeltaIn &A, const DeltaRanges &R, int w, int lane)
     {
-        constexpr int WAVES = DeltaPairs<E, DK>::waves;
         blocks = blocks_of(A.Dv);
         const unsigned groups = (unsigned)((blocks + (MAPS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x / groups;
         block = (int)(blockIdx.x % groups) * WAVES + w;
@@ -770,48 +786,67 @@ template <class E, int DK, bool MAPS> struct ChainPlace {
     }
 };
 
-template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta(DeltaArgs A, DeltaRanges R)
+template <class E, int DK, bool MAPS> using ForwardChain = std::conditional_t<MAPS, DeltaMaps<E, DK>, DeltaChain<E, DK>>;
+template <class Chain> constexpr int threads_of = 64 * (Chain::WAVES + Chain::OTHERS);
+template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<ForwardChain<E, DK, MAPS>>), (ForwardChain<E, DK, MAPS>::PER_SIMD)) void k_delta(DeltaArgs A, DeltaRanges R)
 {
-    using Tile = DeltaTile<E, DK, 3>;
-    using Chain = DeltaChain<E, DK>;
+    using Chain = ForwardChain<E, DK, MAPS>;
+    using Tile = typename Chain::Tile;
     constexpr int WAVES = Chain::WAVES;
     extern __shared__ __align__(16) unsigned char lds[];
     Chain &L = *reinterpret_cast<Chain *>(lds);
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
     const bool chain = threadIdx.x < 64 * WAVES;
-    const ChainPlace<E, DK, MAPS> at(A, R, w, lane);
+    const ChainPlace<E, DK, MAPS, WAVES> at(A, R, w, lane);
     const E *v = head_of<E>(A.v, A.sv, at.bi, at.h) + at.tile0 * CH * A.sv.ts;
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
+    // what is brought in turn i, while tile i is worked on: tile i + 1 into LDS, i + 2 on its way
+    auto bring = [&](auto &fetch, long i) {
+        if (i < 0 && at.n > 0) {
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x % (64 * WAVES));
+            fetch.load(A, at.tile0);
+        }
+        if (i + 1 < at.n) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
+        if (i + 2 < at.n) fetch.load(A, at.tile0 + i + 2);
+    };
     if (chain) {
         Columns<DK> S;
         at.begin(A, R, A.s0, S, lane);
         Steps<E> vs;
         vs.rows = 0;
         if (at.n > 0) vs.load(v, (int)A.sv.ts, at.c, A.Dv, rows_in(0), lane);
+        DeltaFetch<E, DK, 64 * WAVES, 3, Tile> fetch;
+        if (MAPS) bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
+            if (MAPS) bring(fetch, i);
             if (i < at.n) {
                 const Tile &s = L.tiles[i % 3];
                 const int rows = rows_in(i);
                 f4 val[2], u[2], next[DK / 16];
                 vs.get(at.mine, lane, val);
                 if (i + 1 < at.n) vs.load(v + (i + 1) * CH * A.sv.ts, (int)A.sv.ts, at.c, A.Dv, rows_in(i + 1), lane);
-                if (!MAPS)
+                if constexpr (!MAPS)
 #pragma unroll
                     for (int n = 0; n < DK / 16; ++n) L.state[i & 1][w][n][lane] = S.s[n];
                 typename Operand<E>::template Split<3> sp[DK / 32];
 #pragma unroll
                 for (int p = 0; p < DK / 32; ++p) sp[p] = split<E, 3>(S.s[2 * p], S.s[2 * p + 1]);
                 delta_u<E, DK, 3>(s, sp, val, rows, lane, u);
-                if (!MAPS) {
+                if constexpr (!MAPS) {
                     L.steps[i & 1][w][0][lane] = u[0];
                     L.steps[i & 1][w][1][lane] = u[1];
                 }
                 const auto up = split<E, 3>(where(of_steps(s.until(), 0, lane), u[0]), where(of_steps(s.until(), 1, lane), u[1]));
                 const float left = s.since()[CH - 1];
 #pragma unroll
-                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), up, where(left, S.s[n]));
+                for (int n = 0; n < DK / 16; ++n) next[n] = left * S.s[n];
+                if (is_zero(left))      // whatever it was
+#pragma unroll
+                    for (int n = 0; n < DK / 16; ++n) next[n] = f4{};
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), up, next[n]);
                 if (__any(nothing(next) != 0.f)) {
                     for (int t = 0; t < rows; ++t) delta_step(s, records[i], S, t, at.mine ? (float)v[(i * CH + t) * A.sv.ts + at.c] : 0.f, lane);
                 } else {
@@ -823,20 +858,14 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
         }
         if (MAPS) at.end(A, R, S, lane);
         else if (A.last && at.tile0 + at.n >= A.tiles) S.put(A.last + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
-    } else {
-        DeltaFetch<E, DK, 64 * WAVES, 3> fetch;
+    } else if constexpr (!MAPS) {
+        DeltaFetch<E, DK, 64 * WAVES, 3, Tile> fetch;
         E *o = head_of<E>(A.o, A.so, at.bi, at.h) + at.tile0 * CH * A.so.ts;
-        if (at.n > 0) {
-            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x - 64 * WAVES);
-            fetch.load(A, at.tile0);
-            fetch.put(L.tiles[0], A.Dk);
-            if (at.n > 1) fetch.load(A, at.tile0 + 1);
-        }
+        bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
-            if (i + 1 < at.n) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
-            if (i + 2 < at.n) fetch.load(A, at.tile0 + i + 2);
-            if (!MAPS && i > 0) {
+            bring(fetch, i);
+            if (i > 0) {
                 const long tile = i - 1;
                 const Tile &s = L.tiles[tile % 3];
                 const int rows = rows_in(tile);
@@ -908,7 +937,12 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
                 const auto yp = split<E, 3>(y[0], y[1]);
                 const float left = s.since()[CH - 1];
 #pragma unroll
-                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), yp, where(left, D.s[n]) + L.state[tile & 1][w][n][lane]);
+                for (int n = 0; n < DK / 16; ++n) next[n] = L.state[tile & 1][w][n][lane] + left * D.s[n];
+                if (is_zero(left))      // whatever it was
+#pragma unroll
+                    for (int n = 0; n < DK / 16; ++n) next[n] = L.state[tile & 1][w][n][lane];
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) next[n] = mul<E, 3>(state_columns<E, Tile::LD>(s.k, n, lane), yp, next[n]);
                 if (__any(nothing(next) != 0.f)) {
                     for (int t = rows_in(tile) - 1; t >= 0; --t) {
                         delta_step_back(s, D, t, at.mine ? (float)dout[(tile * CH + t) * A.sdo.ts + at.c] : 0.f, A.scale, lane);

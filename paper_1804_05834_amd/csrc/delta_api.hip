@@ -120,17 +120,19 @@ template <class E, int DK> seq::DeltaRanges ranges_at(const seq::DeltaIn &A, voi
     R.first = R.b + n * size;
     return R;
 }
-template <class E, int DK> unsigned chain_groups(const seq::DeltaIn &A, const seq::DeltaRanges &R, bool maps)
+template <class Chain, int DK> unsigned chain_groups(const seq::DeltaIn &A, const seq::DeltaRanges &R, bool maps)
 {
-    constexpr int waves = seq::DeltaChain<E, DK>::WAVES;
+    constexpr int waves = Chain::WAVES;
     return (unsigned)((int64_t)A.B * A.H * R.ranges * (((A.Dv + 15) / 16 + (maps ? DK / 16 : 0) + waves - 1) / waves));
 }
 template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *workspace, hipStream_t st)
 {
     static std::atomic<uint64_t> granted{0}, maps_granted{0};
-    constexpr int bytes = sizeof(seq::DeltaChain<E, DK>), threads = seq::chain_threads<E, DK>;
-    static_assert(bytes <= 160 * 1024, "within a compute unit's LDS");
-    if (!lds_granted((const void *)seq::k_delta<E, DK, false>, bytes, granted) || !lds_granted((const void *)seq::k_delta<E, DK, true>, bytes, maps_granted)) return false;
+    using Chain = seq::DeltaChain<E, DK>;
+    using Maps = seq::DeltaMaps<E, DK>;
+    constexpr int bytes = sizeof(Chain), maps_bytes = sizeof(Maps);
+    static_assert(bytes <= 160 * 1024 && maps_bytes <= 80 * 1024, "one and two within a compute unit's LDS");
+    if (!lds_granted((const void *)seq::k_delta<E, DK, false>, bytes, granted) || !lds_granted((const void *)seq::k_delta<E, DK, true>, maps_bytes, maps_granted)) return false;
     const int64_t heads = (int64_t)A.B * A.H;
     if (A.T <= seq::STEPS_MOST && !A.states) {
         seq::k_delta_few<E, DK><<<dim3((unsigned)((heads * ((A.Dv + 15) / 16) + 3) / 4)), 256, 0, st>>>(A);
@@ -139,10 +141,10 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
     if (A.tiles) seq::k_delta_tiles<E, DK><<<dim3((unsigned)((heads * A.tiles + 3) / 4)), 256, 0, st>>>(A, (seq::DeltaRecord *)A.records);
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
-        seq::k_delta<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, bytes, st>>>(A, R);
+        seq::k_delta<E, DK, true><<<dim3(chain_groups<Maps, DK>(A, R, true)), seq::threads_of<Maps>, maps_bytes, st>>>(A, R);
         seq::k_delta_join<DK, false><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.s0, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
     }
-    seq::k_delta<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, bytes, st>>>(A, R);
+    seq::k_delta<E, DK, false><<<dim3(chain_groups<Chain, DK>(A, R, false)), seq::threads_of<Chain>, bytes, st>>>(A, R);
     return true;
 }
 constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit, which is all that fits; 512 in two turns: 4 % slower
@@ -156,10 +158,10 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, v
     const int64_t heads = (int64_t)A.B * A.H;
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
-        seq::k_delta_back<E, DK, true><<<dim3(chain_groups<E, DK>(A, R, true)), threads, back, st>>>(A, R);
+        seq::k_delta_back<E, DK, true><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, true)), threads, back, st>>>(A, R);
         seq::k_delta_join<DK, true><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.dlast, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
     }
-    seq::k_delta_back<E, DK, false><<<dim3(chain_groups<E, DK>(A, R, false)), threads, back, st>>>(A, R);
+    seq::k_delta_back<E, DK, false><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, false)), threads, back, st>>>(A, R);
     if (!A.tiles) return true;
     const int64_t all = heads * A.tiles, per = std::max<int64_t>(1, (all + GRAD_GROUPS - 1) / GRAD_GROUPS);
     seq::k_delta_grad<E, DK><<<dim3((unsigned)((all + per - 1) / per)), 512, bytes, st>>>(A, (int)per);
