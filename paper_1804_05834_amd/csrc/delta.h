@@ -750,8 +750,9 @@ template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> stru
     __device__ __forceinline__ ChainPlace(const DeltaIn &A, const DeltaRanges &R, int w, int lane)
     {
         blocks = blocks_of(A.Dv);
-        const unsigned groups = (unsigned)((blocks + (MAPS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x / groups;
-        block = (int)(blockIdx.x % groups) * WAVES + w;
+        // workgroups of the same tiles on the same XCD, where there are heads and ranges for that
+        const unsigned all = gridDim.x / (unsigned)((blocks + (MAPS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x % all;
+        block = (int)(blockIdx.x / all) * WAVES + w;
         head = which / (unsigned)R.ranges;
         range = (int)(which % (unsigned)R.ranges);
         bi = (int)(head / (unsigned)A.H);
@@ -997,39 +998,50 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
 
 // From range to range: the state each begins with, forward from s0 or backward from dlast.  A workgroup per head and 16 columns, a wave per 16 rows;
 // a result of 16 x 16 is the next right operand as it is, in its place in LDS.  As many waves more take it from there to memory: a wave that loads
-// maps would wait for its own stores (32 ranges of 128 x 128: 79 us against 69; what is left is bringing 64 KB a range to each of few compute
-// units, and two ranges ahead it is slower).  What enters a range with an episode's start leaves nothing, whatever it is.
-template <int DK, bool BACK> __global__ __launch_bounds__(8 * DK) void k_delta_join(DeltaRanges R, const float *given, const DeltaRecord *records, long tiles, int Dk, int Dv)
+// maps would wait for its own stores.  What enters a range with an episode's start leaves nothing, whatever it is.
+// Many ranges go in groups of `span`: COMPOSE finds each group's map and addition, 16 columns of either a workgroup, from the unit matrix and zeros; then from
+// group to group; then within all groups at once, `given` being what enters each.  Bound by bringing 64 KB a range (of 128 x 128) to each compute unit: 32 ranges
+// of four heads one after the other 69 us, in groups of 8 18 + 31.
+template <int DK, bool BACK, bool COMPOSE>
+__global__ __launch_bounds__((COMPOSE ? 4 : 8) * DK) void k_delta_join(DeltaRanges R, int span, const float *given, DeltaRanges to, const DeltaRecord *records, long tiles, int Dk, int Dv)
 {
+    constexpr int THREADS = (COMPOSE ? 4 : 8) * DK;
     __shared__ f4 state[2][DK / 16][64];
     __shared__ int forgets[MOST_RANGES];      // whether an episode starts in a range
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % (DK / 16), g = lane >> 4;
     const bool stores = threadIdx.x >= 4 * DK;
-    const unsigned blocks = (unsigned)blocks_of(Dv), head = blockIdx.x / blocks;
-    const int c = 16 * (int)(blockIdx.x % blocks) + (lane & 15), row = 16 * w + 4 * g;
-    const long size = (long)Dk * Dv, base = (long)head * R.ranges;
+    const unsigned mine = (unsigned)blocks_of(Dv), blocks = COMPOSE ? mine + DK / 16 : mine, groups = (unsigned)((R.ranges + span - 1) / span);
+    // which: head and group; its workgroups, which read the same maps, on the same XCD
+    const unsigned all = gridDim.x / blocks, block = blockIdx.x / all, which = blockIdx.x % all, head = which / groups;
+    const int first = (int)(which % groups) * span, n = min(span, R.ranges - first);
+    const bool unit = COMPOSE && block >= mine;      // 16 columns of the map
+    const int c = 16 * (int)(unit ? block - mine : block) + (lane & 15), row = 16 * w + 4 * g;
+    const long size = (long)Dk * Dv, base = (long)head * R.ranges + first;
     auto in = [&](int e) { return c < Dv && row + e < Dk; };
-    auto range = [&](int i) { return BACK ? R.ranges - 1 - i : i; };
-    for (int r = threadIdx.x; r < R.ranges; r += 8 * DK) forgets[r] = 0;
+    auto range = [&](int i) { return BACK ? n - 1 - i : i; };
+    for (int r = threadIdx.x; r < n; r += THREADS) forgets[r] = 0;
     __syncthreads();
-    for (long t = threadIdx.x; t < tiles; t += 8 * DK)
-        if (records[head * tiles + t].cut[CH - 1]) forgets[t / R.per] = 1;
+    for (long t = first * R.per + threadIdx.x; t < min(tiles, (first + n) * R.per); t += THREADS)
+        if (records[head * tiles + t].cut[CH - 1]) forgets[t / R.per - first] = 1;
     if (stores) {
-        for (int i = 0; i < R.ranges; ++i) {
+        for (int i = 0; i < n; ++i) {
             lds_barrier();
             const f4 S = state[i & 1][w][lane];
-            float *first = R.first + (base + range(i)) * size;
+            float *out = R.first + (base + range(i)) * size;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (in(e)) first[(row + e) * Dv + c] = S[e];
+                if (in(e)) out[(row + e) * Dv + c] = S[e];
         }
         return;
     }
     f4 S = {}, a[DK / 16], add;
-    if (given)
+    if (!COMPOSE && given)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (in(e)) S[e] = given[head * size + (row + e) * Dv + c];
+            if (in(e)) S[e] = given[which * size + (row + e) * Dv + c];
+    if (unit)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[e] = row + e == c ? 1.f : 0.f;
     // a range's map is under way while the one before is applied
     auto get = [&](int i) {
         const float *m = R.m + (base + range(i)) * DK * DK + (16 * w + (lane & 15)) * DK + 4 * g, *b = R.b + (base + range(i)) * size;
@@ -1039,13 +1051,13 @@ template <int DK, bool BACK> __global__ __launch_bounds__(8 * DK) void k_delta_j
         for (int e = 0; e < 4; ++e) add[e] = b[min(row + e, Dk - 1) * Dv + min(c, Dv - 1)];
     };
     get(0);
-    for (int i = 0; i < R.ranges; ++i) {
+    for (int i = 0; i < n; ++i) {
         state[i & 1][w][lane] = S;
         lds_barrier();
-        if (i + 1 == R.ranges) break;
+        if (!COMPOSE && i + 1 == n) break;
         f4 next, other = {};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) next[e] = in(e) ? add[e] : 0.f;
+        for (int e = 0; e < 4; ++e) next[e] = !unit && in(e) ? add[e] : 0.f;
         if (!forgets[range(i)]) {
 #pragma unroll
             for (int kb = 0; kb < DK / 16; kb += 2) {
@@ -1054,8 +1066,14 @@ template <int DK, bool BACK> __global__ __launch_bounds__(8 * DK) void k_delta_j
             }
             next += other;
         }
-        get(i + 1);      // of the last range, whose map nobody needs, too
+        get(min(i + 1, n - 1));      // of the last range, whose map nobody needs, too
         S = next;
+    }
+    if (COMPOSE) {
+        float *out = unit ? to.m + (long)which * DK * DK + row * DK + c : to.b + which * size + (long)row * Dv + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (unit || in(e)) out[(long)e * (unit ? DK : Dv)] = S[e];
     }
 }
 

@@ -100,25 +100,57 @@ template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t til
     R.ranges = (int)((tiles + R.per - 1) / R.per);
     return R;
 }
-size_t range_bytes(const seq::DeltaRanges &R, const DeltaSizes &s)
+// Ranges are joined in groups of 8 where there are many, which takes two launches more: 64 of them (8192 steps, one head of 64 in fp32) 86 / 97 us at once,
+// 62 / 72 so; 32 (4096 steps, four heads of 128 in bf16) 124 / 168 and 97 / 142; 20 (2560 steps, two of 64) 46 / 53 and 47 / 54; 16 are slower in groups.
+constexpr int LEAST_JOINED = 24, JOINED = 8;
+int span_of(int ranges) { return ranges < LEAST_JOINED ? ranges : JOINED; }
+seq::DeltaRanges groups_of(const seq::DeltaRanges &R)
 {
-    if (R.ranges == 1) return 0;
-    return ((size_t)s.B * s.H * R.ranges * ((size_t)width_of(s.Dk) * width_of(s.Dk) + 2 * (size_t)s.Dk * s.Dv) * 4 + 15) / 16 * 16;
+    const int span = span_of(R.ranges);
+    return seq::DeltaRanges{(R.ranges + span - 1) / span, R.per * span, nullptr, nullptr, nullptr};
+}
+size_t range_bytes(const seq::DeltaRanges &R, int64_t heads, int width, int64_t size)
+{
+    return R.ranges == 1 ? 0 : ((size_t)heads * R.ranges * ((size_t)width * width + 2 * (size_t)size) * 4 + 15) / 16 * 16;
 }
 size_t ranges_workspace(const DeltaSizes &s)
 {
     size_t n = 0;
-    delta_form(s.dtype, s.Dk, [&](auto e, auto dk) { return n = range_bytes(ranges_of<decltype(e), dk.value>((int64_t)s.B * s.H, tiles_of(s.T), s.Dv), s), true; });
+    delta_form(s.dtype, s.Dk, [&](auto e, auto dk) { const int64_t heads = (int64_t)s.B * s.H, size = (int64_t)s.Dk * s.Dv;
+        const seq::DeltaRanges R = ranges_of<decltype(e), dk.value>(heads, tiles_of(s.T), s.Dv);
+        n = range_bytes(R, heads, dk.value, size) + range_bytes(groups_of(R), heads, dk.value, size);
+        return true;
+    });
     return n;
 }
-template <class E, int DK> seq::DeltaRanges ranges_at(const seq::DeltaIn &A, void *workspace)
+template <int DK> void place(seq::DeltaRanges &R, const seq::DeltaIn &A, void *workspace)
 {
-    seq::DeltaRanges R = ranges_of<E, DK>((int64_t)A.B * A.H, A.tiles, A.Dv);
     const int64_t n = (int64_t)A.B * A.H * R.ranges, size = (int64_t)A.Dk * A.Dv;
     R.m = (float *)workspace;
     R.b = R.m + n * DK * DK;
     R.first = R.b + n * size;
+}
+template <class E, int DK> seq::DeltaRanges ranges_at(const seq::DeltaIn &A, void *workspace)
+{
+    seq::DeltaRanges R = ranges_of<E, DK>((int64_t)A.B * A.H, A.tiles, A.Dv);
+    place<DK>(R, A, workspace);
     return R;
+}
+// The states that ranges begin with, from their maps.
+template <int DK, bool BACK> void launch_join(const seq::DeltaRanges &R, const seq::DeltaIn &A, const float *given, const seq::DeltaRecord *records, void *workspace, hipStream_t st)
+{
+    const int64_t heads = (int64_t)A.B * A.H;
+    const unsigned blocks = (unsigned)((A.Dv + 15) / 16);
+    const int span = span_of(R.ranges);
+    auto join = [&](const seq::DeltaRanges &r, int n, const float *from) {
+        seq::k_delta_join<DK, BACK, false><<<dim3((unsigned)heads * ((r.ranges + n - 1) / n) * blocks), 8 * DK, 0, st>>>(r, n, from, r, records, A.tiles, A.Dk, A.Dv);
+    };
+    if (span == R.ranges) return join(R, span, given);
+    seq::DeltaRanges G = groups_of(R);
+    place<DK>(G, A, (uint8_t *)workspace + range_bytes(R, heads, DK, (int64_t)A.Dk * A.Dv));
+    seq::k_delta_join<DK, BACK, true><<<dim3((unsigned)heads * G.ranges * (blocks + DK / 16)), 4 * DK, 0, st>>>(R, span, nullptr, G, records, A.tiles, A.Dk, A.Dv);
+    join(G, G.ranges, given);
+    join(R, span, G.first);
 }
 template <class Chain, int DK> unsigned chain_groups(const seq::DeltaIn &A, const seq::DeltaRanges &R, bool maps)
 {
@@ -142,7 +174,7 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
         seq::k_delta<E, DK, true><<<dim3(chain_groups<Maps, DK>(A, R, true)), seq::threads_of<Maps>, maps_bytes, st>>>(A, R);
-        seq::k_delta_join<DK, false><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.s0, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+        launch_join<DK, false>(R, A, A.s0, (const seq::DeltaRecord *)A.records, workspace, st);
     }
     seq::k_delta<E, DK, false><<<dim3(chain_groups<Chain, DK>(A, R, false)), seq::threads_of<Chain>, bytes, st>>>(A, R);
     return true;
@@ -159,7 +191,7 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, v
     const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
         seq::k_delta_back<E, DK, true><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, true)), threads, back, st>>>(A, R);
-        seq::k_delta_join<DK, true><<<dim3((unsigned)(heads * ((A.Dv + 15) / 16))), 8 * DK, 0, st>>>(R, A.dlast, (const seq::DeltaRecord *)A.records, A.tiles, A.Dk, A.Dv);
+        launch_join<DK, true>(R, A, A.dlast, (const seq::DeltaRecord *)A.records, workspace, st);
     }
     seq::k_delta_back<E, DK, false><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, false)), threads, back, st>>>(A, R);
     if (!A.tiles) return true;

@@ -1,4 +1,4 @@
-"""The matrix memory's operators on tensors whose elements lie further apart than 32 bits reach."""
+"""The matrix memory's operators where there is much: elements further apart than 32 bits reach, more tiles than compute units, many ranges."""
 import pytest
 import torch
 
@@ -86,3 +86,35 @@ def test_delta_many_sequences_are_what_a_few_are(dtype, Dk, Dv, bad):
             y = y[at:at + 26]
             assert torch.equal(x.nan_to_num(7.0, 8.0, 9.0), y.nan_to_num(7.0, 8.0, 9.0)) and torch.equal(x.isnan(), y.isnan())
     assert bad == bool(want[2][2].isnan().any())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv,resets", [(3300, 1, 1, 64, 64, 0), (3300, 1, 2, 33, 20, 0.001), (4100, 2, 1, 20, 72, 0.002), (3109, 1, 1, 128, 128, 0.001), (8200, 1, 1, 16, 17, 0.0005)])
+def test_delta_ranges_in_groups(dtype, T, B, H, Dk, Dv, resets):
+    """So many ranges that they are joined in groups, the last one smaller; some with an episode's start."""
+    c = Delta(T, dtype, B, T, H, Dk, Dv, resets=resets)
+    c.check(*c.run())
+
+
+def test_delta_groups_and_what_is_not_finite():
+    """A state that is NaN and a value that is infinite end with their episodes, whatever is joined."""
+    clean, c = (Delta(5, "bf16", 1, 4096, 2, 32, 32, resets=0) for _ in range(2))
+    for x in (clean, c):
+        x.reset = torch.zeros(1, 4096, dtype=torch.uint8, device=DEV)
+        x.reset[0, [1000, 1700, 3000]] = 1
+    want = clean.run()
+    c.s0[:] = float("nan")
+    c.dlast[0, 1] = float("nan")
+    c.v[0, 2000, 0, 3] = float("inf")
+    got = c.run()
+    assert not torch.isfinite(got[0][0, :1000]).any() and not torch.isfinite(got[0][0, 2000:3000, 0, 3]).any() and torch.isfinite(got[1]).all()
+    # A tile with such a number is formed step by step, the clean run's by its products, which take 16 bits of the state: with |q| < 1, columns of the
+    # state below 8 and the scale 32^-1/2 those are 2^-17 * 8 / 5.7 < 2^-16 off, fp32 roundings of either far less.  Rounded by half a step each, the two
+    # are one step of bf16 (2^-7) and 2^-16 apart at most.
+    for part in (slice(1000, 2000), slice(3000, 4096)):
+        assert torch.allclose(got[0][0, part].float(), want[0][0, part].float(), rtol=2.0 ** -7, atol=2.0 ** -16)
+    for x, y in zip(got[2][:5], want[2][:5]):
+        assert torch.isfinite(x[0, 1000:1700]).all() and torch.isfinite(x[0, 3000:, 0]).all()
+        # another tile's way of forming it: a step of bf16
+        assert torch.allclose(x[0, 1000:1700].float(), y[0, 1000:1700].float(), rtol=2.0 ** -7, atol=2.0 ** -8)
+    assert not torch.isfinite(got[2][2][0, 3000:, 1]).all()
