@@ -719,7 +719,7 @@ template <class E, int DK> struct DeltaPairs {
 };
 template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>::waves;
 // A launch that finds the maps of the forward direction has no outputs: keys alone, and four waves of a chain that bring their tiles themselves.  So two
-// workgroups fit into a compute unit, and one has what the other waits for: the same head's maps, twice the state's columns, 110 us; in pairs of waves 147.
+// workgroups fit into a compute unit, and one has what the other waits for: the same head's maps, twice the state's columns, 103 us; in pairs of waves 147.
 constexpr int MAPS_WAVES = 4;
 template <class E, int DK> struct DeltaMaps {
     static constexpr int WAVES = MAPS_WAVES, OTHERS = 0, PER_SIMD = 2;
