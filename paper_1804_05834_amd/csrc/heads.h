@@ -107,7 +107,7 @@ template <int V, int K> __device__ __forceinline__ void load_turns(const uint64_
 }
 
 // HB heads of a group at a time, their loads ahead of everything else (an element at a time, 30011 x 7 x 100 in fp32: 4 heads 46 us, 8, with fewer waves on a
-// compute unit, 55)
+// compute unit, 55).  With the next batch's loads under way as well registers leave fewer waves, and it is no faster (50; backward, 16384 x 16 x 64 in bf16, 47 for 31).
 template <class E, int V, int K, int HB> __device__ __forceinline__ void heads_forward(const E *x, long hs, E *y, long yhs, int H, const float (&wl)[K][V], const float (&wh)[K][V],
                                                                                       const Units<V, K> &u, const Angles<V, K> &a, const HeadsShape &s, int sub, bool row, float eps, float *rstd)
 {
@@ -172,8 +172,8 @@ template <class E, int V, int K> __global__ __launch_bounds__(256) void k_heads(
         Angles<V, K> a;
         if (s.half) a.set(u, t, row ? A.position[m] : 0);
         float *rstd = A.rstd ? A.rstd + m * (s.Hq + s.Hk) : nullptr;
-        heads_forward<E, V, K, 4>((const E *)A.q + m * A.q_rs, A.q_hs, (E *)A.yq + m * A.yq_rs, A.yq_hs, s.Hq, ql, qh, u, a, s, sub, row, A.eps, rstd);
-        heads_forward<E, V, K, 4>((const E *)A.k + m * A.k_rs, A.k_hs, (E *)A.yk + m * A.yk_rs, A.yk_hs, s.Hk, kl, kh, u, a, s, sub, row, A.eps, rstd ? rstd + s.Hq : nullptr);
+        heads_forward<E, V, K, V == 1 ? 4 : 2>((const E *)A.q + m * A.q_rs, A.q_hs, (E *)A.yq + m * A.yq_rs, A.yq_hs, s.Hq, ql, qh, u, a, s, sub, row, A.eps, rstd);
+        heads_forward<E, V, K, V == 1 ? 4 : 2>((const E *)A.k + m * A.k_rs, A.k_hs, (E *)A.yk + m * A.yk_rs, A.yk_hs, s.Hk, kl, kh, u, a, s, sub, row, A.eps, rstd ? rstd + s.Hq : nullptr);
     }
 }
 
@@ -229,7 +229,7 @@ __device__ __forceinline__ void heads_backward(const E *dy, long dhs, const E *x
 
 template <class E, int V, int K> __global__ __launch_bounds__(256) void k_heads_grad(HeadsGradArgs A)
 {
-    __shared__ float sh[4][256];
+    __shared__ float sh[4][4][HEADS_MAX / 2];
     const HeadsShape &s = A.s;
     const Units<V, K> u(s);
     const int group = threadIdx.x / s.lanes, groups = 256 / s.lanes, sub = group & (s.per_row - 1), rows = groups / s.per_row;
@@ -247,29 +247,29 @@ template <class E, int V, int K> __global__ __launch_bounds__(256) void k_heads_
         heads_backward<E, V, K, V == 1 ? 4 : 2>((const E *)A.dyq + m * A.dyq_rs, A.dyq_hs, (const E *)A.q + m * A.q_rs, A.q_hs, (E *)A.dq + m * A.dq_rs, A.dq_hs, s.Hq, ql, qh, dq[0], dq[1], u, a, s, sub, row, rstd);
         heads_backward<E, V, K, V == 1 ? 4 : 2>((const E *)A.dyk + m * A.dyk_rs, A.dyk_hs, (const E *)A.k + m * A.k_rs, A.k_hs, (E *)A.dk + m * A.dk_rs, A.dk_hs, s.Hk, kl, kh, dk[0], dk[1], u, a, s, sub, row, rstd + s.Hq);
     }
-    // the groups' sums, four numbers per lane at a time, in the order of the groups
+    // the groups' sums, of a wave's groups lane by lane, then of the four waves
     float *part = A.part + (long)blockIdx.x * 2 * s.D;
-    const int lane = threadIdx.x & (s.lanes - 1);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
     for (int j = 0; j < K; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            sh[0][threadIdx.x] = dq[0][j][i];
-            sh[1][threadIdx.x] = dq[1][j][i];
-            sh[2][threadIdx.x] = dk[0][j][i];
-            sh[3][threadIdx.x] = dk[1][j][i];
-            __syncthreads();
-            for (int e = threadIdx.x; e < 4 * s.lanes; e += 256) {
-                const int which = e / s.lanes;
-                const int pairs = (s.half + V - 1) / V, unit = lane + j * s.lanes;      // 256 is a multiple of lanes: e's lane is the thread's
-                const int lo = unit < pairs ? unit * V : 2 * s.half + 2 * (unit - pairs) * V, hi = unit < pairs ? s.half + unit * V : lo + V;
-                float sum = 0.f;
-                for (int g = 0; g < groups; ++g) sum += sh[which][g * s.lanes + lane];
-                const int c = (which & 1 ? hi : lo) + i;
-                if (c < s.D) part[(which >> 1) * s.D + c] = sum;
-            }
-            __syncthreads();
+            float v[4] = {dq[0][j][i], dq[1][j][i], dk[0][j][i], dk[1][j][i]};
+            for (int d = s.lanes; d < 64; d *= 2)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) v[n] += __shfl_xor(v[n], d);
+            if (lane < s.lanes)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) sh[w][n][(j * V + i) * s.lanes + lane] = v[n];
         }
+    __syncthreads();
+    const int count = K * V * s.lanes, pairs = (s.half + V - 1) / V;
+    for (int e = threadIdx.x; e < 4 * count; e += 256) {
+        const int which = e / count, at = e % count, i = at / s.lanes % V, unit = at / s.lanes / V * s.lanes + at % s.lanes;
+        const int lo = unit < pairs ? unit * V : 2 * s.half + 2 * (unit - pairs) * V, hi = unit < pairs ? s.half + unit * V : lo + V;
+        const int c = (which & 1 ? hi : lo) + i;
+        if (c < s.D) part[(which >> 1) * s.D + c] = (sh[0][which][at] + sh[1][which][at]) + (sh[2][which][at] + sh[3][which][at]);
+    }
 }
 
 // The sum of the workgroups' parts, 16 columns a workgroup, in a fixed order.
