@@ -6,7 +6,7 @@
 // exchange, and the angles of a row, 25 instructions a pair, serve all heads that a group takes.
 // An angle is exact before its sine is taken: position times turns_i in 64-bit fixed point, whose upper 32 bits are the fraction of
 // a full turn.  Sine and cosine of the rest of an eighth are their series, off by 2^-25 at most.
-// 16384 rows of 8 + 8 heads of 64 in bf16: forward 19 us (67 MB, 3.5 TB/s), gradients 31 + 4 (101 MB, 3.3 TB/s); 30011 rows of 5 + 2 heads of 100 in fp32, 50
+// 16384 rows of 8 + 8 heads of 64 in bf16: forward 19 us (67 MB, 3.6 TB/s), gradients 25 + 4 (101 MB, 4.0 TB/s); 30011 rows of 5 + 2 heads of 100 in fp32, 50
 // of them turned, an element at a time because no partners 25 elements apart lie at multiples of 16 bytes both: 46 (168 MB, 3.7 TB/s) and 66 + 7 (252 MB, 3.8 TB/s).  A large copy reaches 5.1.
 #pragma once
 #include "seq_common.h"
@@ -15,7 +15,7 @@ namespace seq {
 
 constexpr int HEADS_MAX = 256;
 // Most partial sums of the weights' gradients, one per workgroup.  Wide rows take half of them: what a workgroup begins and ends with counts for more there
-// (16384 x 16 x 64 in bf16: 512 31 us, 1024 43).
+// (16384 x 16 x 64 in bf16: 512 25 + 4 us, 1024 32 + 6).
 constexpr int HEADS_PARTS = 1024;
 
 struct HeadsShape {
@@ -107,7 +107,7 @@ template <int V, int K> __device__ __forceinline__ void load_turns(const uint64_
 }
 
 // HB heads of a group at a time, their loads ahead of everything else (an element at a time, 30011 x 7 x 100 in fp32: 4 heads 46 us, 8, with fewer waves on a
-// compute unit, 55).  With the next batch's loads under way as well registers leave fewer waves, and it is no faster (50; backward, 16384 x 16 x 64 in bf16, 47 for 31).
+// compute unit, 55).  With the next batch's loads under way as well registers leave fewer waves, and it is no faster (50; backward, 16384 x 16 x 64 in bf16, 47 where this took 31).
 template <class E, int V, int K, int HB> __device__ __forceinline__ void heads_forward(const E *x, long hs, E *y, long yhs, int H, const float (&wl)[K][V], const float (&wh)[K][V],
                                                                                       const Units<V, K> &u, const Angles<V, K> &a, const HeadsShape &s, int sub, bool row, float eps, float *rstd)
 {
