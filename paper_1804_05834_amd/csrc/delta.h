@@ -722,14 +722,15 @@ template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>
 // workgroups fit into a compute unit, and one has what the other waits for: the same head's maps, twice the state's columns, 103 us; in pairs of waves 147.
 constexpr int MAPS_WAVES = 4;
 template <class E, int DK> struct DeltaMaps {
-    static constexpr int WAVES = MAPS_WAVES, OTHERS = 0, PER_SIMD = 2;
+    static constexpr int WAVES = MAPS_WAVES, BRING = 0, OTHERS = 0, PER_SIMD = 2;
     using Tile = DeltaKeys<E, DK, 3>;
     Tile tiles[3];
 };
 template <class E, int DK> struct DeltaChain {
     using Tile = DeltaTile<E, DK, 3>;
-    static constexpr int OTHERS = DeltaPairs<E, DK>::waves, PER_SIMD = 1;
     static constexpr int WAVES = DeltaPairs<E, DK>::waves;
+    static constexpr int BRING = DK == 128 ? 0 : 2;      // waves that do nothing but bring tiles: of 128 columns registers leave no place for them
+    static constexpr int OTHERS = WAVES + BRING, PER_SIMD = 1;
     DeltaTile<E, DK, 3> tiles[3];
     f4 state[2][WAVES][DK / 16][64];      // forward: the state that enters; backward: (scale g Q)^T dO
     f4 steps[2][WAVES][2][64];            // U; P^T dO
@@ -803,9 +804,10 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
     // what is brought in turn i, while tile i is worked on: tile i + 1 into LDS, i + 2 on its way
+    constexpr int BRINGING = Chain::BRING ? Chain::BRING : WAVES;
     auto bring = [&](auto &fetch, long i) {
         if (i < 0 && at.n > 0) {
-            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x % (64 * WAVES));
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, Chain::BRING ? threadIdx.x - 128 * WAVES : threadIdx.x % (64 * WAVES));
             fetch.load(A, at.tile0);
         }
         if (i + 1 < at.n) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
@@ -817,7 +819,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
         Steps<E> vs;
         vs.rows = 0;
         if (at.n > 0) vs.load(v, (int)A.sv.ts, at.c, A.Dv, rows_in(0), lane);
-        DeltaFetch<E, DK, 64 * WAVES, 3, Tile> fetch;
+        DeltaFetch<E, DK, 64 * BRINGING, 3, Tile> fetch;
         if (MAPS) bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
@@ -859,13 +861,21 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
         }
         if (MAPS) at.end(A, R, S, lane);
         else if (A.last && at.tile0 + at.n >= A.tiles) S.put(A.last + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
-    } else if constexpr (!MAPS) {
-        DeltaFetch<E, DK, 64 * WAVES, 3, Tile> fetch;
-        E *o = head_of<E>(A.o, A.so, at.bi, at.h) + at.tile0 * CH * A.so.ts;
+    } else if (Chain::BRING && threadIdx.x >= 128 * WAVES) {
+        DeltaFetch<E, DK, 64 * BRINGING, 3, Tile> fetch;
         bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
             bring(fetch, i);
+            lds_barrier();
+        }
+    } else if constexpr (!MAPS) {
+        DeltaFetch<E, DK, 64 * BRINGING, 3, Tile> fetch;
+        E *o = head_of<E>(A.o, A.so, at.bi, at.h) + at.tile0 * CH * A.so.ts;
+        if (!Chain::BRING) bring(fetch, -1);
+        __syncthreads();
+        for (long i = 0; i <= at.n; ++i) {
+            if (!Chain::BRING) bring(fetch, i);
             if (i > 0) {
                 const long tile = i - 1;
                 const Tile &s = L.tiles[tile % 3];
