@@ -717,7 +717,6 @@ template <class E, int DK> struct DeltaPairs {
     static constexpr int tile = (int)sizeof(DeltaTile<E, DK, 3>), pair = 2 * 64 * (DK / 16 + 2) * 16, room = 160 * 1024;
     static constexpr int waves = 3 * tile + 4 * pair <= room ? 4 : 3 * tile + 2 * pair <= room ? 2 : 1;
 };
-template <class E, int DK> constexpr int chain_threads = 128 * DeltaPairs<E, DK>::waves;
 // A launch that finds the maps of the forward direction has no outputs: keys alone, and four waves of a chain that bring their tiles themselves.  So two
 // workgroups fit into a compute unit, and one has what the other waits for: the same head's maps, twice the state's columns, 103 us; in pairs of waves 147.
 constexpr int MAPS_WAVES = 4;
@@ -914,7 +913,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
 
 // The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.  A range's map is the transposed
 // of its map in the other direction, found from the unit matrix in the same way.
-template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_threads<E, DK>)) void k_delta_back(DeltaGradArgs A, DeltaRanges R)
+template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<DeltaChain<E, DK>>)) void k_delta_back(DeltaGradArgs A, DeltaRanges R)
 {
     using Tile = DeltaTile<E, DK, 3>;
     using Chain = DeltaChain<E, DK>;
@@ -927,8 +926,27 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
     const E *dout = head_of<E>(A.dout, A.sdo, at.bi, at.h) + at.tile0 * CH * A.sdo.ts;
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
-    // turn i of the wave that brings and prepares is for tile n - 1 - i, of the chain for the one before that
-    if (chain) {
+    // turn i of the wave that prepares is for tile n - 1 - i, of the chain for the one before that; meanwhile the one after it comes into LDS
+    constexpr int BRINGING = Chain::BRING ? Chain::BRING : WAVES;
+    using Fetch = DeltaFetch<E, DK, 64 * BRINGING, 3>;
+    auto bring = [&](Fetch &fetch, long i) {
+        if (i < 0 && at.n > 0) {
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, Chain::BRING ? threadIdx.x - 128 * WAVES : threadIdx.x % (64 * WAVES));
+            fetch.load(A, at.tile0 + at.n - 1);
+        }
+        const long tile = at.n - 2 - i;
+        if (tile >= 0) fetch.put(L.tiles[tile % 3], A.Dk);
+        if (tile >= 1) fetch.load(A, at.tile0 + tile - 1);
+    };
+    if (Chain::BRING && threadIdx.x >= 128 * WAVES) {
+        Fetch fetch;
+        bring(fetch, -1);
+        __syncthreads();
+        for (long i = 0; i <= at.n; ++i) {
+            bring(fetch, i);
+            lds_barrier();
+        }
+    } else if (chain) {
         Columns<DK> D;
         at.begin(A, R, A.dlast, D, lane);
         __syncthreads();
@@ -969,28 +987,20 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((chain_thread
         if (MAPS) at.end(A, R, D, lane);
         else if (A.ds0 && at.range == 0) D.put(A.ds0 + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
     } else {
-        DeltaFetch<E, DK, 64 * WAVES, 3> fetch;
+        Fetch fetch;
         Steps<E> ds;
         ds.rows = 0;
         auto get = [&](long tile) { ds.load(dout + tile * CH * A.sdo.ts, (int)A.sdo.ts, at.c, A.Dv, rows_in(tile), lane); };
-        if (at.n > 0) {
-            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x - 64 * WAVES);
-            fetch.load(A, at.tile0 + at.n - 1);
-            get(at.n - 1);
-            fetch.put(L.tiles[(at.n - 1) % 3], A.Dk);
-            if (at.n > 1) fetch.load(A, at.tile0 + at.n - 2);
-        }
+        if (at.n > 0) get(at.n - 1);
+        if (!Chain::BRING) bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
             const long tile = at.n - 1 - i;
             if (tile >= 0) {
                 f4 out[2], pd[2] = {}, x[2];
                 ds.get(at.mine, lane, out);
-                if (tile > 0) {
-                    fetch.put(L.tiles[(tile - 1) % 3], A.Dk);
-                    get(tile - 1);
-                }
-                if (tile > 1) fetch.load(A, at.tile0 + tile - 2);
+                if (tile > 0) get(tile - 1);
+                if (!Chain::BRING) bring(fetch, i);
                 const Tile &s = L.tiles[tile % 3];
                 upper<Tile::LC>(s.p, out, lane, pd);
                 L.steps[tile & 1][w][0][lane] = pd[0];

@@ -183,7 +183,7 @@ constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per com
 template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, void *workspace, hipStream_t st)
 {
     static std::atomic<uint64_t> back_granted{0}, maps_granted{0}, granted{0};
-    constexpr int back = sizeof(seq::DeltaChain<E, DK>), threads = seq::chain_threads<E, DK>, bytes = sizeof(seq::DeltaGradTile<E, DK>);
+    constexpr int back = sizeof(seq::DeltaChain<E, DK>), threads = seq::threads_of<seq::DeltaChain<E, DK>>, bytes = sizeof(seq::DeltaGradTile<E, DK>);
     static_assert(bytes <= 160 * 1024 && sizeof(seq::DeltaSteps<E, DK>) <= 65536, "within what a workgroup can have");
     if (!lds_granted((const void *)seq::k_delta_back<E, DK, false>, back, back_granted) || !lds_granted((const void *)seq::k_delta_back<E, DK, true>, back, maps_granted) ||
         !lds_granted((const void *)seq::k_delta_grad<E, DK>, bytes, granted)) return false;
