@@ -703,14 +703,14 @@ __device__ __forceinline__ void delta_y(const Tile &s, const typename Operand<E>
 
 // ---------------------------------------------------------------- from state to state
 // A workgroup per head, range of tiles and 16 columns of each of WAVES pairs of waves.  One wave of a pair takes the state from tile to tile and
-// nothing else; the other brings tiles into LDS and does, a tile apart, what the chain does not wait for: the outputs, or in the backward
-// direction what dO alone gives.  They hand each other registers as they are, through LDS, with one barrier a tile.
+// nothing else; the other does, a tile apart, what the chain does not wait for: the outputs, or in the backward
+// direction what dO alone gives.  They hand each other registers as they are, through LDS, with one barrier a tile.  Two more waves bring tiles into LDS.
 // Where heads are few, a head's tiles are cut into ranges.  What a range does to the state is a linear map and an addition, S -> M S + B; a first
 // launch (MAPS) finds both, M by the same chain from the unit matrix's columns, a second goes from range to range, and the last has all
 // ranges' first states.
-// Bound by what follows upon what within a tile: state into planes, S^T k, T, K^T u, each a few matrix instructions deep, and two barriers' worth of waiting
-// for LDS: 2.8 us a tile of 64 x 64 in bf16 (256 heads of 16 tiles, forward 46 us, backward 43), 3.1 of 128 x 128 (a head of 1024 tiles in 32 ranges:
-// 98 us).  With one wave for both parts of a pair: 72 and 62 us for 46 and 43.
+// Bound by what follows upon what within a tile: state into planes, S^T k, T, K^T u, each a few matrix instructions deep, and waiting
+// for LDS: 2.6 us a tile of 64 x 64 in bf16 (256 heads of 16 tiles: forward 42 us, backward 37), 2.9 of 128 x 128 (a head of 1024 tiles in 32 ranges:
+// 89 us).  With one wave for both parts of a pair 72 and 62 us; with the second waves of the pairs, which then took longer than the first, bringing the tiles 46 and 43.
 // A tile whose results hold a number that is not finite is taken again step by step as the definition has it, where nothing is multiplied by the
 // zeros of other steps: a NaN reaches what comes after it in its episode and nothing else.
 template <class E, int DK> struct DeltaPairs {
@@ -728,7 +728,7 @@ template <class E, int DK> struct DeltaMaps {
 template <class E, int DK> struct DeltaChain {
     using Tile = DeltaTile<E, DK, 3>;
     static constexpr int WAVES = DeltaPairs<E, DK>::waves;
-    static constexpr int BRING = DK == 128 ? 0 : 2;      // waves that do nothing but bring tiles: of 128 columns registers leave no place for them
+    static constexpr int BRING = 2;      // waves that do nothing but bring tiles
     static constexpr int OTHERS = WAVES + BRING, PER_SIMD = 1;
     DeltaTile<E, DK, 3> tiles[3];
     f4 state[2][WAVES][DK / 16][64];      // forward: the state that enters; backward: (scale g Q)^T dO
@@ -803,10 +803,10 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
     // what is brought in turn i, while tile i is worked on: tile i + 1 into LDS, i + 2 on its way
-    constexpr int BRINGING = Chain::BRING ? Chain::BRING : WAVES;
+    constexpr int BRINGING = MAPS ? WAVES : Chain::BRING;
     auto bring = [&](auto &fetch, long i) {
         if (i < 0 && at.n > 0) {
-            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, Chain::BRING ? threadIdx.x - 128 * WAVES : threadIdx.x % (64 * WAVES));
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x % (128 * WAVES));
             fetch.load(A, at.tile0);
         }
         if (i + 1 < at.n) fetch.put(L.tiles[(i + 1) % 3], A.Dk);
@@ -860,7 +860,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
         }
         if (MAPS) at.end(A, R, S, lane);
         else if (A.last && at.tile0 + at.n >= A.tiles) S.put(A.last + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
-    } else if (Chain::BRING && threadIdx.x >= 128 * WAVES) {
+    } else if (threadIdx.x >= 128 * WAVES) {
         DeltaFetch<E, DK, 64 * BRINGING, 3, Tile> fetch;
         bring(fetch, -1);
         __syncthreads();
@@ -869,12 +869,9 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
             lds_barrier();
         }
     } else if constexpr (!MAPS) {
-        DeltaFetch<E, DK, 64 * BRINGING, 3, Tile> fetch;
         E *o = head_of<E>(A.o, A.so, at.bi, at.h) + at.tile0 * CH * A.so.ts;
-        if (!Chain::BRING) bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
-            if (!Chain::BRING) bring(fetch, i);
             if (i > 0) {
                 const long tile = i - 1;
                 const Tile &s = L.tiles[tile % 3];
@@ -927,18 +924,17 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<D
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
     // turn i of the wave that prepares is for tile n - 1 - i, of the chain for the one before that; meanwhile the one after it comes into LDS
-    constexpr int BRINGING = Chain::BRING ? Chain::BRING : WAVES;
-    using Fetch = DeltaFetch<E, DK, 64 * BRINGING, 3>;
+    using Fetch = DeltaFetch<E, DK, 64 * Chain::BRING, 3>;
     auto bring = [&](Fetch &fetch, long i) {
         if (i < 0 && at.n > 0) {
-            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, Chain::BRING ? threadIdx.x - 128 * WAVES : threadIdx.x % (64 * WAVES));
+            fetch.begin(A, (const DeltaRecord *)A.records, at.head, at.bi, at.h, threadIdx.x % (128 * WAVES));
             fetch.load(A, at.tile0 + at.n - 1);
         }
         const long tile = at.n - 2 - i;
         if (tile >= 0) fetch.put(L.tiles[tile % 3], A.Dk);
         if (tile >= 1) fetch.load(A, at.tile0 + tile - 1);
     };
-    if (Chain::BRING && threadIdx.x >= 128 * WAVES) {
+    if (threadIdx.x >= 128 * WAVES) {
         Fetch fetch;
         bring(fetch, -1);
         __syncthreads();
@@ -987,12 +983,10 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<D
         if (MAPS) at.end(A, R, D, lane);
         else if (A.ds0 && at.range == 0) D.put(A.ds0 + (long)at.head * A.Dk * A.Dv, A.Dk, A.Dv, at.c, lane);
     } else {
-        Fetch fetch;
         Steps<E> ds;
         ds.rows = 0;
         auto get = [&](long tile) { ds.load(dout + tile * CH * A.sdo.ts, (int)A.sdo.ts, at.c, A.Dv, rows_in(tile), lane); };
         if (at.n > 0) get(at.n - 1);
-        if (!Chain::BRING) bring(fetch, -1);
         __syncthreads();
         for (long i = 0; i <= at.n; ++i) {
             const long tile = at.n - 1 - i;
@@ -1000,7 +994,6 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<D
                 f4 out[2], pd[2] = {}, x[2];
                 ds.get(at.mine, lane, out);
                 if (tile > 0) get(tile - 1);
-                if (!Chain::BRING) bring(fetch, i);
                 const Tile &s = L.tiles[tile % 3];
                 upper<Tile::LC>(s.p, out, lane, pd);
                 L.steps[tile & 1][w][0][lane] = pd[0];
