@@ -86,8 +86,8 @@ size_t state_bytes(const DeltaSizes &s) { return (size_t)s.B * s.H * tiles_of(s.
 
 // Ranges of a head's tiles, where there are fewer workgroups of a chain than compute units.  All of its tiles are gone through three times then
 // (the maps take as many columns again), so that fewer than four ranges would not pay.  Measured (bf16, 64 x 64, forward / backward): 4 ranges
-// (64 heads of 4096 steps) 207 / 414 us, one 286 / 457; 3 (85 heads) 276 / 557, one 305 / 534; 2 (128 heads) 413 / 809, one 346 / 668.  Ranges of
-// 4 tiles (4 heads of 1024 steps) 37 / 44 us, of 8 47 / 56, one 71 / 72; of 2 tiles, which makes 64 of them at 4096 steps, 80 / 95 for 57 / 72.
+// (64 heads of 4096 steps) 171 / 376 us, one 257 / 403; 3 (85 heads) 227 / 502, one 268 / 478; 2 (128 heads) 339 / 727, one 302 / 615.  Ranges of
+// 4 tiles (4 heads of 1024 steps) 38 / 44 us, of 8 49 / 52, one 68 / 65; of 2 tiles, which makes 64 of them at 4096 steps, 55 / 71 for 53 / 67.
 constexpr int64_t UNITS = 256, LEAST_TILES = 4, LEAST_RANGES = 4;
 template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t tiles, int Dv)
 {
