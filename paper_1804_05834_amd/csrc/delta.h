@@ -740,9 +740,10 @@ struct DeltaRanges {
     int ranges;
     long per;                             // tiles of a range, but for the last
     float *m, *b, *first;                 // [heads][ranges][..]
+    float *turned;                        // M^T, the backward direction's M, for a backward call to come; or NULL
 };
-// A wave's place: head, range and block of 16 columns; with MAPS the blocks behind those of the state are M's.
-template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> struct ChainPlace {
+// A wave's place: head, range and block of 16 columns; with MAPS, forward, the blocks behind those of the state are M's.
+template <class E, int DK, bool MAPS, int WAVES, bool UNITS> struct ChainPlace {
     unsigned head;
     int range, block, blocks, bi, h, c;
     long tile0, n;                        // the range's first tile, how many it has
@@ -751,7 +752,7 @@ template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> stru
     {
         blocks = blocks_of(A.Dv);
         // workgroups of the same tiles on the same XCD, where there are heads and ranges for that
-        const unsigned all = gridDim.x / (unsigned)((blocks + (MAPS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x % all;
+        const unsigned all = gridDim.x / (unsigned)((blocks + (UNITS ? DK / 16 : 0) + WAVES - 1) / WAVES), which = blockIdx.x % all;
         block = (int)(blockIdx.x / all) * WAVES + w;
         head = which / (unsigned)R.ranges;
         range = (int)(which % (unsigned)R.ranges);
@@ -759,7 +760,7 @@ template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> stru
         h = (int)(head % (unsigned)A.H);
         c = 16 * block + (lane & 15);
         mine = c < A.Dv;
-        unit = MAPS && block >= blocks;
+        unit = UNITS && block >= blocks;
         tile0 = range * R.per;
         n = min(R.per, A.tiles - tile0);
     }
@@ -783,7 +784,13 @@ template <class E, int DK, bool MAPS, int WAVES = DeltaPairs<E, DK>::waves> stru
     {
         const long at = (long)head * R.ranges + range;
         if (!unit) S.put(R.b + at * A.Dk * A.Dv, A.Dk, A.Dv, c, lane);
-        else S.put(R.m + at * DK * DK, DK, DK, c - 16 * blocks, lane);
+        else {
+            const int column = c - 16 * blocks;
+            S.put(R.m + at * DK * DK, DK, DK, column, lane);
+            if (R.turned && column < DK)
+#pragma unroll
+                for (int n = 0; n < DK / 16; ++n) store<4>(R.turned + at * DK * DK + column * DK + 32 * (n >> 1) + 8 * (lane >> 4) + 4 * (n & 1), S.s[n]);
+        }
     }
 };
 
@@ -798,7 +805,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
     Chain &L = *reinterpret_cast<Chain *>(lds);
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
     const bool chain = threadIdx.x < 64 * WAVES;
-    const ChainPlace<E, DK, MAPS, WAVES> at(A, R, w, lane);
+    const ChainPlace<E, DK, MAPS, WAVES, MAPS> at(A, R, w, lane);
     const E *v = head_of<E>(A.v, A.sv, at.bi, at.h) + at.tile0 * CH * A.sv.ts;
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };
@@ -909,7 +916,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
 }
 
 // The gradient of the state, from the last tile to the first: what leaves each tile is kept, for k_delta_grad.  A range's map is the transposed
-// of its map in the other direction, found from the unit matrix in the same way.
+// of its map in the other direction, which the forward call has kept; MAPS finds the additions alone.
 template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<DeltaChain<E, DK>>)) void k_delta_back(DeltaGradArgs A, DeltaRanges R)
 {
     using Tile = DeltaTile<E, DK, 3>;
@@ -919,7 +926,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<D
     Chain &L = *reinterpret_cast<Chain *>(lds);
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) % WAVES;
     const bool chain = threadIdx.x < 64 * WAVES;
-    const ChainPlace<E, DK, MAPS> at(A, R, w, lane);
+    const ChainPlace<E, DK, MAPS, WAVES, false> at(A, R, w, lane);
     const E *dout = head_of<E>(A.dout, A.sdo, at.bi, at.h) + at.tile0 * CH * A.sdo.ts;
     const DeltaRecord *records = (const DeltaRecord *)A.records + at.head * A.tiles + at.tile0;
     auto rows_in = [&](long tile) { return (int)min((long)CH, A.T - (at.tile0 + tile) * CH); };

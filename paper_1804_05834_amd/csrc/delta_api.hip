@@ -94,7 +94,7 @@ template <class E, int DK> seq::DeltaRanges ranges_of(int64_t heads, int64_t til
     constexpr int waves = seq::DeltaChain<E, DK>::WAVES;
     const int64_t groups = heads * (((Dv + 15) / 16 + waves - 1) / waves);
     const int64_t n = groups ? std::min({UNITS / groups, tiles / LEAST_TILES, (int64_t)seq::MOST_RANGES}) : 1;
-    seq::DeltaRanges R{1, (long)tiles, nullptr, nullptr, nullptr};
+    seq::DeltaRanges R{1, (long)tiles, nullptr, nullptr, nullptr, nullptr};
     if (n < LEAST_RANGES) return R;
     R.per = (long)((tiles + n - 1) / n);
     R.ranges = (int)((tiles + R.per - 1) / R.per);
@@ -107,7 +107,7 @@ int span_of(int ranges) { return ranges < LEAST_JOINED ? ranges : JOINED; }
 seq::DeltaRanges groups_of(const seq::DeltaRanges &R)
 {
     const int span = span_of(R.ranges);
-    return seq::DeltaRanges{(R.ranges + span - 1) / span, R.per * span, nullptr, nullptr, nullptr};
+    return seq::DeltaRanges{(R.ranges + span - 1) / span, R.per * span, nullptr, nullptr, nullptr, nullptr};
 }
 size_t range_bytes(const seq::DeltaRanges &R, int64_t heads, int width, int64_t size)
 {
@@ -119,6 +119,17 @@ size_t ranges_workspace(const DeltaSizes &s)
     delta_form(s.dtype, s.Dk, [&](auto e, auto dk) { const int64_t heads = (int64_t)s.B * s.H, size = (int64_t)s.Dk * s.Dv;
         const seq::DeltaRanges R = ranges_of<decltype(e), dk.value>(heads, tiles_of(s.T), s.Dv);
         n = range_bytes(R, heads, dk.value, size) + range_bytes(groups_of(R), heads, dk.value, size);
+        return true;
+    });
+    return n;
+}
+// What a forward call keeps of the ranges' maps for a backward call.
+size_t map_bytes(const DeltaSizes &s)
+{
+    size_t n = 0;
+    delta_form(s.dtype, s.Dk, [&](auto e, auto dk) {
+        const int ranges = ranges_of<decltype(e), dk.value>((int64_t)s.B * s.H, tiles_of(s.T), s.Dv).ranges;
+        n = ranges == 1 ? 0 : (size_t)s.B * s.H * ranges * dk.value * dk.value * 4;
         return true;
     });
     return n;
@@ -157,7 +168,7 @@ template <class Chain, int DK> unsigned chain_groups(const seq::DeltaIn &A, cons
     constexpr int waves = Chain::WAVES;
     return (unsigned)((int64_t)A.B * A.H * R.ranges * (((A.Dv + 15) / 16 + (maps ? DK / 16 : 0) + waves - 1) / waves));
 }
-template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *workspace, hipStream_t st)
+template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *workspace, float *maps, hipStream_t st)
 {
     static std::atomic<uint64_t> granted{0}, maps_granted{0};
     using Chain = seq::DeltaChain<E, DK>;
@@ -171,7 +182,8 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
         return true;
     }
     if (A.tiles) seq::k_delta_tiles<E, DK><<<dim3((unsigned)((heads * A.tiles + 3) / 4)), 256, 0, st>>>(A, (seq::DeltaRecord *)A.records);
-    const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
+    seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
+    R.turned = maps;
     if (R.ranges > 1) {
         seq::k_delta<E, DK, true><<<dim3(chain_groups<Maps, DK>(A, R, true)), seq::threads_of<Maps>, maps_bytes, st>>>(A, R);
         launch_join<DK, false>(R, A, A.s0, (const seq::DeltaRecord *)A.records, workspace, st);
@@ -180,7 +192,7 @@ template <class E, int DK> bool launch_delta(const seq::DeltaArgs &A, void *work
     return true;
 }
 constexpr int64_t GRAD_GROUPS = 256;     // a workgroup of the gradients per compute unit, which is all that fits; 512 in two turns: 4 % slower
-template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, void *workspace, hipStream_t st)
+template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, void *workspace, const float *maps, hipStream_t st)
 {
     static std::atomic<uint64_t> back_granted{0}, maps_granted{0}, granted{0};
     constexpr int back = sizeof(seq::DeltaChain<E, DK>), threads = seq::threads_of<seq::DeltaChain<E, DK>>, bytes = sizeof(seq::DeltaGradTile<E, DK>);
@@ -188,9 +200,10 @@ template <class E, int DK> bool launch_delta_grad(const seq::DeltaGradArgs &A, v
     if (!lds_granted((const void *)seq::k_delta_back<E, DK, false>, back, back_granted) || !lds_granted((const void *)seq::k_delta_back<E, DK, true>, back, maps_granted) ||
         !lds_granted((const void *)seq::k_delta_grad<E, DK>, bytes, granted)) return false;
     const int64_t heads = (int64_t)A.B * A.H;
-    const seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
+    seq::DeltaRanges R = ranges_at<E, DK>(A, workspace);
     if (R.ranges > 1) {
-        seq::k_delta_back<E, DK, true><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, true)), threads, back, st>>>(A, R);
+        R.m = const_cast<float *>(maps);      // read only
+        seq::k_delta_back<E, DK, true><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, false)), threads, back, st>>>(A, R);
         launch_join<DK, true>(R, A, A.dlast, (const seq::DeltaRecord *)A.records, workspace, st);
     }
     seq::k_delta_back<E, DK, false><<<dim3(chain_groups<seq::DeltaChain<E, DK>, DK>(A, R, false)), threads, back, st>>>(A, R);
@@ -212,7 +225,7 @@ int32_t dqn_delta_sizes(int32_t dtype, int32_t B, int64_t T, int32_t H, int32_t 
     const DeltaSizes s{dtype, B, H, Dk, Dv, T};
     if (!carry || !forward_workspace || !backward_workspace) return bad(call, "NULL argument");
     if (const char *m = check_sizes(s)) return bad(call, m);
-    *carry = state_bytes(s) + record_bytes(s);
+    *carry = state_bytes(s) + record_bytes(s) + map_bytes(s);
     *forward_workspace = ranges_workspace(s) + record_bytes(s);      // the records lie in `carry` if there is one
     *backward_workspace = ranges_workspace(s) + state_bytes(s) + (size_t)B * H * tiles_of(T) * 4;
     return DQN_OK;
@@ -236,11 +249,12 @@ int32_t dqn_delta_forward(const dqn_delta_args *args, void *stream)
                               check_heads(d.b, d.b_s, d.B, d.T, d.H, 1, d.dtype, false), check_heads(d.o, d.o_s, d.B, d.T, d.H, d.Dv, d.dtype, true)})
             if (m) return bad(call, m);
     float *records = (float *)(d.carry ? (uint8_t *)d.carry + state_bytes(s) : (uint8_t *)d.workspace + ranges_workspace(s));
+    float *maps = d.carry ? (float *)((uint8_t *)d.carry + state_bytes(s) + record_bytes(s)) : nullptr;
     seq::DeltaArgs A{};
     static_cast<seq::DeltaIn &>(A) = inputs(d);
     A.s0 = d.s0; A.o = d.o; A.so = strides(d.o_s); A.last = d.s_last; A.states = d.carry; A.records = records;
     hipStream_t st = (hipStream_t)stream;
-    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta<decltype(e), dk.value>(A, d.workspace, st); });
+    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta<decltype(e), dk.value>(A, d.workspace, maps, st); });
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }
 
@@ -266,6 +280,7 @@ int32_t dqn_delta_backward(const dqn_delta_grad_args *args, void *stream)
                               check_heads(d.db, d.db_s, d.B, d.T, d.H, 1, d.dtype, true)})
             if (m) return bad(call, m);
     }
+    const float *maps = (const float *)((const uint8_t *)d.carry + state_bytes(s) + record_bytes(s));
     seq::DeltaGradArgs A{};
     static_cast<seq::DeltaIn &>(A) = inputs(d);
     A.dout = d.dout; A.sdo = strides(d.dout_s); A.states = d.carry; A.records = (const float *)((const uint8_t *)d.carry + state_bytes(s)); A.dlast = d.dlast;
@@ -273,7 +288,7 @@ int32_t dqn_delta_backward(const dqn_delta_grad_args *args, void *stream)
     A.sdq = strides(d.dq_s); A.sdk = strides(d.dk_s); A.sdv = strides(d.dv_s); A.sdf = strides(d.df_s); A.sdb = strides(d.db_s);
     A.ds0 = d.ds0; A.into = (float *)((uint8_t *)d.workspace + ranges_workspace(s)); A.again = (int *)((uint8_t *)A.into + state_bytes(s));
     hipStream_t st = (hipStream_t)stream;
-    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta_grad<decltype(e), dk.value>(A, d.workspace, st); });
+    const bool ok = delta_form(d.dtype, d.Dk, [&](auto e, auto dk) { return launch_delta_grad<decltype(e), dk.value>(A, d.workspace, maps, st); });
     return ok ? launched(call) : dqn_seq_fail(DQN_ERR_HIP, call, "the LDS of a tile was not granted");
 }
 
