@@ -8,9 +8,11 @@
 // Backward, from dO and the gradient D of the state that leaves:
 //   dU = P^T dO + (G_C. K) D,   Y = T^T dU,   dS = g_C D + (scale g Q)^T dO - (beta g K)^T Y,   dv = beta Y,   db = (1 - beta) Y.u
 //   dP = dO U^T, dN = -Y U^T:   dq = scale g S do + (dP scale G) k,   dk = (dP scale G)^T q + G_C. D u - beta g S y + (dN beta G) k + (dN beta G)^T k
-// and, since o_i grows with a_t for every i >= t of the episode while what v_i writes does not shrink with it,
-//   d log a_t = sum_{i >= t} (do_i.o_i - dv_i.v_i) + <D, S'>   (the sum ends with the episode, the last term counts if it lives on),  df = (1 - a) d log a,
-// with do_i.o_i = q_i.dq_i and <D, S'> = g_C <D, S> + sum_j G_Cj u_j.(D^T k_j).
+// and, a_t being a factor of every G_ij with j < t <= i, of every g_i with i >= t and of every G_Cj with j < t,
+//   d log a_t = sum_{j < t <= i} (dP_ij P_ij + dN_ij N_ij) + sum_{i >= t} e_i + sum_{j < t} l_j + g_C <D, S>,   df = (1 - a) d log a,
+//   e_i = g_i (scale q_i.(S do_i) - beta_i k_i.(S y_i)),   l_j = G_Cj u_j.(D^T k_j).
+// (Sums of do_i.o_i - dv_i.v_i, which are fewer, do not have a_t as a factor: they leave the gradient of a gate that is nearly shut as a difference of numbers
+// that it has no part in.)
 //
 // Three kinds of launch: what a tile needs that no state has part in (T, P, the gates), all tiles at once, a wave each; the chain from state to
 // state, forward or backward, a wave per 16 columns of the state; and the gradients, all tiles at once, a workgroup each.
@@ -1221,16 +1223,52 @@ template <class E, int DK> struct DeltaGradTile {
     Rounded<E, CH, COLS> u, y;
     Rounded<E, DK, COLS> state, back;       // the state that enters, the gradient of the one that leaves
     Rounded<E, CH, CH> dp, dn;              // of P's and N's products
-    float qdq[DK / 16][CH], yu[2][4][CH], vdv[2][4][CH];      // sums over 16 columns each of q.dq; for even and odd tiles of Y.u, dv.v
-    float ends[8];                          // of each wave: <D, S'>
+    float enters[DK / 16][CH], yu[2][4][CH], leaves[2][4][CH];      // sums over 16 columns each of e_i; for even and odd tiles of Y.u, l_j
+    float pairs[2][2][4][16];               // for even and odd tiles, of dP P and dN N: gate_pairs'
+    float ends[8];                          // of each wave: g_C <D, S>
     int wrong[8];                           // whether it has met a number that is not finite
 };
 
-// x of the step N later, 0 where that is in another episode or row of 16
-template <int N> __device__ __forceinline__ float after(float x, int cut)
+// Of 16 neighbouring lanes: the sum of those before a lane; of it and those behind.
+template <int CTRL> __device__ __forceinline__ float moved(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xF, 0xF, false)); }
+__device__ __forceinline__ float sum_before(float x)
 {
-    const float o = __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x100 + N, 0xF, 0xF, false));
-    return __builtin_amdgcn_update_dpp(-1, cut, 0x100 + N, 0xF, 0xF, false) == cut ? o : 0.f;
+    x = moved<0x111>(x);
+    x += moved<0x111>(x);
+    x += moved<0x112>(x);
+    x += moved<0x114>(x);
+    return x + moved<0x118>(x);
+}
+__device__ __forceinline__ float sum_from(float x)
+{
+    x += moved<0x101>(x);
+    x += moved<0x102>(x);
+    x += moved<0x104>(x);
+    return x + moved<0x108>(x);
+}
+// The sums of e_ij over j < t <= i for every t, of 16 x 16 as a result holds them, rows i0.. and column j, into four rows of 16: 0 and 3 from the parts on the diagonal,
+// for t of the first and the second 16 steps; from the part below it 1, for t of the first 16, and 2, the rows' sums, whose own sums from t on are for t of the second.
+__device__ __forceinline__ void gate_pairs(f4 e, int i0, int j, bool diagonal, int lane, float (&out)[4][16])
+{
+    const int col = lane & 15;
+    if (diagonal) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = sum_before(e[r]);
+            sum += i0 + r >= j ? x : 0.f;
+        }
+        sum = groups_sum(sum);
+        if (lane < 16) out[j < 16 ? 0 : 3][col] = sum;
+    } else {
+        const float x = sum_before(groups_sum((e[0] + e[1]) + (e[2] + e[3])));
+        if (lane < 16) out[1][col] = x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float sum = group_fold(e[r], 16, add);
+            if (col == 0) out[2][i0 + r - 16] = sum;
+        }
+    }
 }
 
 // All gradients but the state's: workgroups of eight waves, `per` tiles each, one after the other, a tile's loads under way while the one before
@@ -1299,8 +1337,6 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
     };
     Gates last{};
     float f_in = 0.f, b_in = 0.f;
-    int cut = 0;
-    bool still = false;
     auto take = [&]() {         // after the wait for later loads
         f_in = (float)last.f, b_in = (float)last.b;
         asm volatile("" : "+v"(f_in), "+v"(b_in));      // here, not where they are used
@@ -1310,25 +1346,25 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
         int again = 0;
 #pragma unroll
         for (int n = 0; n < 8; ++n) again |= g.wrong[n];
-        const float (&vdv)[4][CH] = g.vdv[(id - 1) & 1], (&yu)[4][CH] = g.yu[(id - 1) & 1];
+        const float (&leaves)[4][CH] = g.leaves[(id - 1) & 1], (&yu)[4][CH] = g.yu[(id - 1) & 1], (&pairs)[2][4][16] = g.pairs[(id - 1) & 1];
         if (lane == 0) A.again[id - 1] = again;
-        float x = 0.f;
+        const bool second = step >= 16;
+        const int at = step & 15;
+        float enters = 0.f, end = 0.f;
 #pragma unroll
-        for (int n = 0; n < DK / 16; ++n) x += g.qdq[n][step];
-        x = step < last.rows ? x - ((vdv[0][step] + vdv[1][step]) + (vdv[2][step] + vdv[3][step])) : 0.f;
-        float end = 0.f;
+        for (int n = 0; n < DK / 16; ++n) enters += g.enters[n][step];
 #pragma unroll
         for (int n = 0; n < 8; ++n) end += g.ends[n];
-        x += step == last.rows - 1 ? end : 0.f;
-        x += after<1>(x, cut);      // sums to the episode's end, of 16 steps, then of 32
-        x += after<2>(x, cut);
-        x += after<4>(x, cut);
-        x += after<8>(x, cut);
-        const float half = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 16));
-        x += step < 16 && cut == __builtin_amdgcn_readlane(cut, 16) ? half : 0.f;
+        const float left = (leaves[0][step] + leaves[1][step]) + (leaves[2][step] + leaves[3][step]);
+        const float own = second ? pairs[0][3][at] + pairs[1][3][at] : pairs[0][0][at] + pairs[1][0][at];
+        const float other = second ? pairs[0][2][at] + pairs[1][2][at] : pairs[0][1][at] + pairs[1][1][at];
+        // of the other 16 steps: what enters the second, what leaves the first.  All lanes take part in every exchange, whichever result they keep.
+        const float from = sum_from(enters), before = sum_before(left), through = before + left, others = sum_from(other);
+        const float entered = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(from), 16)), passed = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(through), 15));
+        const float x = (own + (second ? others : other)) + (from + before) + (end + (second ? passed : entered));
         if (lane < last.rows && !again) {      // else k_delta_grad_steps's
             const float rate = (yu[0][step] + yu[1][step]) + (yu[2][step] + yu[3][step]);
-            *last.df = (E)(still ? 0.f : x * (1.f / (1.f + expf(f_in))));
+            *last.df = (E)(x * (1.f / (1.f + expf(f_in))));
             *last.db = (E)(rate * (1.f / (1.f + expf(b_in))));
         }
     };
@@ -1381,16 +1417,12 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
             if (!for_y) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    const f4 beta = of_steps(s.beta(), m, lane), y = g.y.column(16 * m + 4 * grp, 16 * wc + col);
+                    const f4 y = g.y.column(16 * m + 4 * grp, 16 * wc + col);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = 16 * m + 4 * grp + e;
-                        const float a = group_fold(y[e] * res[m][e], 16, add), b = group_fold(beta[e] * y[e] * val[m][e], 16, add);
-                        if (col == 0) {
-                            float &yu = g.yu[id & 1][wc][i], &vdv = g.vdv[id & 1][wc][i];
-                            yu = sl ? yu + a : a;
-                            vdv = sl ? vdv + b : b;
-                        }
+                        const float a = group_fold(y[e] * res[m][e], 16, add);
+                        float &yu = g.yu[id & 1][wc][16 * m + 4 * grp + e];
+                        if (col == 0) yu = sl ? yu + a : a;
                     }
                 }
             } else {
@@ -1399,7 +1431,11 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
                 for (int m = 0; m < 2; ++m) {
                     const f4 u = g.u.column(16 * m + 4 * grp, 16 * wc + col);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) end = fmaf(res[m][e], u[e], end);
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = group_fold(res[m][e] * u[e], 16, add);
+                        float &leaves = g.leaves[id & 1][wc][16 * m + 4 * grp + e];
+                        if (col == 0) leaves = sl ? leaves + a : a;
+                    }
                 }
                 if (left != 0.f)
 #pragma unroll
@@ -1440,14 +1476,23 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
             const vec<int, 4> cut_i = load<4>(s.cut() + i0);
             const f4 hi_i = load<4>(s.run_hi() + i0), lo_i = load<4>(s.run_lo() + i0), beta = load<4>(s.beta() + i0);
             const float hi_j = s.run_hi()[j], lo_j = s.run_lo()[j];
-            f4 q;
+            f4 q, x = {};       // x: K K^T, or P
+            if (for_y) {
+#pragma unroll
+                for (int p = 0; p < DK / 32; ++p) x = Op::mul(rows_of<E, Tile::LD>(s.k, ti / 16, p, lane), rows_of<E, Tile::LD>(s.k, tj / 16, p, lane), x);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = s.p[(i0 + r) * Tile::LC + j];
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = i0 + r;
                 const float b = j > i || (for_y && j == i) || cut_i[r] != cut_j ? 0.f : between(hi_i[r], lo_i[r], hi_j, lo_j);
                 q[r] = b == 0.f ? 0.f : (for_y ? -beta[r] : A.scale) * b * part[r];
+                x[r] = b == 0.f ? 0.f : (for_y ? q[r] : part[r]) * x[r];
             }
             to.put(i0, j, q);
+            gate_pairs(x, i0, j, ti == tj, lane, g.pairs[id & 1][for_y]);
         } else {
             (for_y ? g.dn : g.dp).put(4 * grp, 16 + col, f4{});     // above the diagonal
             if (for_y) {
@@ -1465,15 +1510,20 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
             E *dq = head_of<E>(A.dq, A.sdq, bi, h) + t0 * A.sdq.ts, *dkp = head_of<E>(A.dk, A.sdk, bi, h) + t0 * A.sdk.ts;
 #pragma unroll
             for (int n = 0; n < NM; ++n) {
-                const int m = m0 + n, i0 = 16 * m;
+                const int m = m0 + n, i0 = 16 * m, i = i0 + 4 * grp;
                 const f4 since = of_steps(s.since(), m, lane), beta = of_steps(s.beta(), m, lane), until = of_steps(s.until(), m, lane);
-                f4 r[2] = {where(since, A.scale * os[n]), where(since, -beta * ys[n]) + where(until, ud[n])};
+                const f4 asked = where(since, A.scale * os[n]), taken = where(since, -beta * ys[n]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float sum = group_fold(fmaf(asked[e], (float)s.q[(i + e) * Tile::LD + dk], taken[e] * (float)s.k[(i + e) * Tile::LD + dk]), 16, add);
+                    if (col == 0) g.enters[d][i + e] = sum;
+                }
+                f4 r[2] = {asked, taken + where(until, ud[n])};
                 r[0] = Op::mul(g.dp.pair(i0, lane), kc, r[0]);
                 r[1] = Op::mul(g.dp.pair_of_columns(i0, lane), qc, r[1]);
                 r[1] = Op::mul(g.dn.pair(i0, lane), kc, r[1]);
                 r[1] = Op::mul(g.dn.pair_of_columns(i0, lane), kc, r[1]);
                 wrong += nothing(r);
-                const int i = 16 * m + 4 * grp;
                 const uint32_t qa = (uint32_t)(i * (int)A.sdq.ts + dk), ka = (uint32_t)(i * (int)A.sdk.ts + dk);
                 if (rows == CH && A.Dk == DK) {
 #pragma unroll
@@ -1489,20 +1539,11 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
                             (dkp + e * A.sdk.ts)[ka] = (E)r[1][e];
                         }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float sum = group_fold(r[0][e] * (float)s.q[(i + e) * Tile::LD + dk], 16, add);
-                    if (col == 0) g.qdq[d][i + e] = sum;
-                }
             }
         }
         end = group_fold(end, 64, add);
         wrong = wrong + end * 0.f;
         if (lane == 0) g.ends[w] = end;
-        if (w == 7) {
-            cut = s.cut()[step];
-            still = starts(s.cut(), step) || s.gate()[step] == 0.f;
-        }
         if (__any(wrong != 0.f) && lane == 0) g.wrong[w] = 1;
         else if (lane == 0) g.wrong[w] = 0;
         lds_barrier();
