@@ -32,6 +32,9 @@ namespace seq {
 
 constexpr int CH = 32;                 // steps of a tile
 constexpr int COLS = 64;               // columns of the state of a workgroup, 16 of each wave
+// A factor between steps where an episode starts in between: what it multiplies counts for nothing, whatever it is.  The 0 of gates that are shut has the other
+// sign: 0 times what is not finite is a NaN, as in the definition.
+constexpr uint32_t CLEARED = 0x80000000u;      // of -0.f
 constexpr float LOG_LEAST = -216.f;    // of a gate, base 2; 2 to it is 0 in fp32: a gate that closes further counts as this, so that differences of sums stay finite
 
 using f4 = vec<float, 4>;
@@ -72,7 +75,7 @@ struct DeltaGradArgs : DeltaIn {
 // What the first launch leaves of a tile.
 struct DeltaRecord {
     float t[CH * CH], p[CH * CH];
-    float since[CH], until[CH], beta[CH];   // g_i, 0 behind an episode's start; G_Ci, 0 before one
+    float since[CH], until[CH], beta[CH];   // g_i, CLEARED behind an episode's start; G_Ci, CLEARED before one
     float gate[CH];                    // a
     float run_hi[CH], run_lo[CH];      // sum of log a, base 2, up to each step, as a multiple of 2^-10 and the rest
     int cut[CH];                       // episodes that have started up to each step
@@ -260,8 +263,8 @@ template <class E, int DK> __global__ __launch_bounds__(256) void k_delta_tiles(
             s.cut[i] = out.cut[i] = cuts;
             s.beta[i] = out.beta[i] = beta;
             out.gate[i] = power((float)la);
-            out.since[i] = cuts ? 0.f : power((float)run);
-            out.until[i] = in && cuts == last ? power((float)(end - run)) : 0.f;
+            out.since[i] = cuts ? -0.f : power((float)run);
+            out.until[i] = in && cuts == last ? power((float)(end - run)) : -0.f;
         }
     }
     wave_sync();
@@ -517,15 +520,15 @@ template <int N> __device__ __forceinline__ float nothing(const f4 (&v)[N])
         for (int e = 0; e < 4; ++e) sum[e] = fmaf(v[i][e], 0.f, sum[e]);
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
-__device__ __forceinline__ f4 where(f4 factor, f4 v)      // factor v, 0 where factor is 0, whatever v is
+__device__ __forceinline__ f4 where(f4 factor, f4 v)      // factor v, 0 where factor is CLEARED, whatever v is
 {
     f4 o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = factor[e] != 0.f ? factor[e] * v[e] : 0.f;
+    for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(factor[e]) != CLEARED ? factor[e] * v[e] : 0.f;
     return o;
 }
 // for a number that is the same in all lanes
-__device__ __forceinline__ bool is_zero(float x) { return (__builtin_amdgcn_readfirstlane(__float_as_uint(x)) & 0x7FFFFFFFu) == 0; }
+__device__ __forceinline__ bool cleared(float x) { return __builtin_amdgcn_readfirstlane(__float_as_uint(x)) == CLEARED; }
 
 // the sum over the four groups of 16 lanes, in all of them
 __device__ __forceinline__ float groups_sum(float x)
@@ -853,7 +856,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<F
                 const float left = s.since()[CH - 1];
 #pragma unroll
                 for (int n = 0; n < DK / 16; ++n) next[n] = left * S.s[n];
-                if (is_zero(left))      // whatever it was
+                if (cleared(left))      // whatever it was
 #pragma unroll
                     for (int n = 0; n < DK / 16; ++n) next[n] = f4{};
 #pragma unroll
@@ -972,7 +975,7 @@ template <class E, int DK, bool MAPS> __global__ __launch_bounds__((threads_of<D
                 const float left = s.since()[CH - 1];
 #pragma unroll
                 for (int n = 0; n < DK / 16; ++n) next[n] = L.state[tile & 1][w][n][lane] + left * D.s[n];
-                if (is_zero(left))      // whatever it was
+                if (cleared(left))      // whatever it was
 #pragma unroll
                     for (int n = 0; n < DK / 16; ++n) next[n] = L.state[tile & 1][w][n][lane];
 #pragma unroll
@@ -1437,7 +1440,7 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
                         if (col == 0) leaves = sl ? leaves + a : a;
                     }
                 }
-                if (left != 0.f)
+                if (!cleared(left))
 #pragma unroll
                     for (int n = 0; n < DK / 16; ++n) {
                         const f4 entered = g.state.column(32 * (n >> 1) + 8 * grp + 4 * (n & 1), 16 * wc + col);
@@ -1635,7 +1638,7 @@ template <class E, int DK> __device__ void delta_grad_steps(const DeltaGradArgs 
             const float gt = s.gate()[t], bt = s.beta()[t];
             const float f = (float)((const E *)A.f)[bi * A.sf.bs + (t0 + t) * A.sf.ts + h * A.sf.hs], b = (float)((const E *)A.b)[bi * A.sb.bs + (t0 + t) * A.sb.ts + h * A.sb.hs];
             const float sr = (g.sums[0][0] + g.sums[0][1]) + (g.sums[0][2] + g.sums[0][3]), sa = (g.sums[1][0] + g.sums[1][1]) + (g.sums[1][2] + g.sums[1][3]);
-            ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(rec.cut, t) || gt == 0.f ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
+            ((E *)A.df)[bi * A.sdf.bs + (t0 + t) * A.sdf.ts + h * A.sdf.hs] = (E)(starts(rec.cut, t) ? 0.f : gt * (1.f / (1.f + expf(f))) * sa);
             ((E *)A.db)[bi * A.sdb.bs + (t0 + t) * A.sdb.ts + h * A.sdb.hs] = (E)(bt * (1.f / (1.f + expf(b))) * sr);
         }
         __syncthreads();

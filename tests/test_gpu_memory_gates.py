@@ -1,10 +1,11 @@
-"""The gates of the matrix memory: the gradient of one that is nearly shut, against its own size."""
+"""The gates of the matrix memory: the gradient of one that is nearly shut, against its own size, and what is not finite in front of one that is shut."""
 import numpy as np
 import pytest
 import torch
 
 import memory_ref as ref
-from test_gpu_memory import Delta, host
+from paper_1804_05834_amd import seq
+from test_gpu_memory import DEV, Delta, host
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +74,40 @@ def test_the_first_gate_has_nothing_to_keep(dtype, B, T, H, Dk, Dv):
     c = Delta(30 + T, dtype, B, T, H, Dk, Dv, state=False, resets=0)
     grads = c.run()[2]
     assert (grads[3][:, 0] == 0).all() and not (grads[3][:, 1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("shut", [-200.0, -100.0])
+@pytest.mark.parametrize("at", [31, 32, 33, 64])
+@pytest.mark.parametrize("B,T,Dk,Dv", [(2, 100, 16, 24), (1, 70, 64, 64), (1, 640, 32, 32)])
+def test_a_gate_that_is_shut_ends_no_episode(dtype, bad, shut, at, B, T, Dk, Dv):
+    """Zero times what is not finite is a NaN, wherever in a tile the gate stands and however the sequence is gone through: a value that is not
+    finite reaches the steps behind the gate, a gradient the steps before it."""
+    for what in ("v", "do", "s0", "dlast"):
+        c = Delta(50 + at, dtype, B, T, 2, Dk, Dv, resets=0)
+        c.reset = torch.zeros(B, T, dtype=torch.uint8, device=DEV)
+        c.reset[:, [2, 67]] = 1
+        c.f[:, at, 0] = shut
+        if what in ("v", "do"):
+            getattr(c, what)[0, 10 if what == "v" else 66, 0, 1] = bad
+        else:
+            c.reset.zero_()
+            getattr(c, what)[0, 0, 3, 1] = bad
+        with np.errstate(all="ignore"):
+            (o, last), _, want, _ = c.exact()
+        got = c.run()
+        for name, x, y in zip(("o", "last", "dq", "dk", "dv", "df", "db", "ds0"), (got[0], got[1], *got[2]), (o, last, *want)):
+            assert (np.isfinite(host(x)) == np.isfinite(y)).all(), (what, name)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("at", [3, 7])
+def test_a_gate_that_is_shut_ends_no_episode_of_few_steps(dtype, at):
+    c = Delta(60, dtype, 2, 8, 2, 16, 16, resets=0)
+    c.f[:, at] = -200.0
+    c.v[0, 1, 0, 5] = float("nan")
+    o, last = seq.delta(*c.inputs(), s0=c.s0, reset=c.reset, scale=c.scale)
+    p, other, _ = seq.delta(*c.inputs(), s0=c.s0, reset=c.reset, scale=c.scale, save=True)
+    assert torch.equal(o.isnan(), p.isnan()) and torch.equal(last.isnan(), other.isnan())
+    assert o[0, 1:, 0, 5].isnan().all() and int(o.isnan().sum()) == 7
