@@ -409,7 +409,9 @@ int32_t dqn_scan_backward(const dqn_scan_grad_args *args, void *stream);
  * for t = 0 .. T-1, S_{-1} = s0.  The state is zero before a step whose reset flag is set
  * (whatever it was, a NaN too).  A step that holds a NaN or an infinity spoils the
  * outputs of its own episode from that step on (a q its own step's) and, in the backward call, the gradients
- * of its own episode, nothing else; a gate that is shut (f = -200, say) does not end that, 0 times a NaN being one.  Keys are taken as they are: the rule contracts the state for
+ * of its own episode, nothing else; a gate that is shut (f = -200, say) does not end that, 0 times a NaN
+ * being one.  32 steps that hold such a number are formed one by one, far slower, and their other results
+ * differ by rounding: padding is better finite.  Keys are taken as they are: the rule contracts the state for
  * beta_t |k_t|^2 <= 2, beyond that it grows.  A stride of a head or of any other
  * dimension of an input may be 0 (heads that share keys); the gradients are per head then as well.
  * T = 1 is the step of an acting agent; s_last may be s0 then, and for any T. */
@@ -418,7 +420,8 @@ typedef struct {
     int32_t dtype;                      /* DQN_F32 / DQN_BF16, of q, k, v, f, b, o  */
     int32_t B, H;                       /* sequences and heads, each 0..65535, the
                                            product of both at most 2^20             */
-    int32_t Dk, Dv;                     /* 1..DQN_DELTA_MAX                         */
+    int32_t Dk, Dv;                     /* 1..DQN_DELTA_MAX; a Dk of 33..63 costs what
+                                           64 costs, of 65..127 what 128 costs      */
     float scale;                        /* finite                                   */
     int64_t T;                          /* steps, >= 0 (0: s_last = s0);
                                            B H ceil(T / 32) at most 2^24            */

@@ -1,8 +1,8 @@
-// The gated delta rule: a memory of one matrix per head, over sequences, forward and backward.
+// The gated delta rule (Yang, Kautz and Hatamizadeh 2024, arXiv 2412.06464): a memory of one matrix per head, over sequences, forward and backward.
 //
 // Per head, with a_t = sigmoid(f_t), beta_t = sigmoid(b_t) and the state S [Dk][Dv] (zero before a step that starts an episode):
 //   S_t = a_t (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T,  o_t = scale S_t^T q_t.
-// Over a tile of CH steps that the state S enters, with g_i = a_1 .. a_i and G_ij = g_i / g_j (0 where an episode starts in between):
+// Over a tile of CH steps (as Yang, Wang, Zhang, Shen and Kim 2024, arXiv 2406.06484, take the rule without gates) that the state S enters, with g_i = a_1 .. a_i and G_ij = g_i / g_j (0 where an episode starts in between):
 //   S_i = g_i S + sum_{j <= i} G_ij k_j u_j^T,   U = T R,   T = (I + N)^-1,   N_ij = beta_i G_ij k_i.k_j (j < i),   R_i = beta_i (v_i - g_i S^T k_i)
 //   O = scale g Q S + P U,   P_ij = scale G_ij q_i.k_j (j <= i),   S' = g_C S + (G_C. K)^T U.
 // Backward, from dO and the gradient D of the state that leaves:
@@ -23,7 +23,8 @@
 // exchanged between lanes from state to state, and left operands (rows of K, Q, T, P in LDS) are read as they lie, 16 bytes a lane.
 //
 // bf16 inputs are exact operands of the bf16 instructions; a state or a U, which is fp32, is taken apart into three bf16 that are
-// exactly its 24 bits, one instruction for each, where it feeds a state, into two (16 bits) where it only feeds results that are rounded to bf16.
+// exactly its 24 bits, one instruction for each, where it feeds a state, into two (16 bits, and without the product of the lower ones 2^-14 of a product at
+// most where both operands are such) where it only feeds results that are rounded to bf16: that changes the last bit of 0.1 % of the outputs, 0.7 % of the gradients.
 // fp32 inputs go through the fp32 instructions, of a sixteenth of the rate.
 #pragma once
 #include "seq_common.h"
@@ -202,7 +203,7 @@ __device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_AC
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 // The factor from step j to step i >= j of an episode: differences of the multiples of 2^-10 are exact, so that a gate that closed long before
-// leaves no rounding in later ones.
+// leaves no rounding in later ones.  The exponent x is one fp32 number, so the factor is |x| ln 2 2^-24 of itself off and what the instruction adds, 2^-23.
 __device__ __forceinline__ float between(float hi_i, float lo_i, float hi_j, float lo_j) { return power((hi_i - hi_j) + (lo_i - lo_j)); }
 
 // ---------------------------------------------------------------- T, P and the gates of every tile
@@ -1277,9 +1278,11 @@ __device__ __forceinline__ void gate_pairs(f4 e, int i0, int j, bool diagonal, i
 // All gradients but the state's: workgroups of eight waves, `per` tiles each, one after the other, a tile's loads under way while the one before
 // is worked on.  Of each 64 columns of the state four waves form U, four Y; then dP and dN; then the products over all columns, a wave having 16 of
 // the columns of dq and dk for half of the steps (DK = 128: for all).
-// 32 x 512 x 8 x 64 in bf16: 111 us, 16 tiles of 64 KB a compute unit, 2.4 TB/s.  What bounds it is the way through a tile, 15000 cycles in four parts between
+// 32 x 512 x 8 x 64 in bf16: 121 us, 16 tiles of 64 KB a compute unit, 2.2 TB/s.  What bounds it is the way through a tile, 16000 cycles in four parts between
 // barriers, in which two waves a SIMD share the vector instructions.  Both directions together: with four waves a workgroup
-// 461 us, with eight 313, with the next tile's loads under way and states as the waves hold them 252, with matrices by columns and arguments read anew 216.
+// 461 us, with eight 313, with the next tile's loads under way and states as the waves hold them 252, with matrices by columns and arguments read anew 216; the gates'
+// gradients from terms that have the gate as a factor, not from differences, took 8 us more.  The form for 128 columns needs more than the 256 registers of a wave and
+// keeps 104 (bf16) or 120 bytes a lane in scratch memory: 32 x 512 x 4 x 128 in bf16 takes 175 us.
 template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_grad(DeltaGradArgs given, int per)
 {
     using Op = Operand<E>;
@@ -1558,7 +1561,8 @@ template <class E, int DK> __global__ __launch_bounds__(512, 2) void k_delta_gra
 }
 
 // The gradients of a tile's steps one by one, as the definition has them: every state is formed again from the first, which takes as many
-// passes as there are steps.  For tiles with numbers that are not finite, which k_delta_grad has left: a workgroup looks at AGAIN tiles.
+// passes as there are steps.  For tiles with numbers that are not finite, which k_delta_grad has left: a workgroup looks at AGAIN tiles.  Such tiles are slow, one after the
+// other in a workgroup: 32 x 512 x 8 x 64 in bf16 with NaN behind the ends of all sequences, a fifth of the steps, takes 16 ms with gradients, with zeros there 0.21.
 constexpr int AGAIN = 64;
 template <class E, int DK> struct DeltaSteps {
     DeltaTile<E, DK, 7> s;

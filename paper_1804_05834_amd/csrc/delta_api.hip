@@ -40,6 +40,7 @@ struct DeltaSizes {
     int64_t T;
 };
 int64_t tiles_of(int64_t T) { return (T + seq::CH - 1) / seq::CH; }
+// Keys of 33 to 64 elements cost what 64 cost, of 65 to 128 what 128 cost: their rows are padded in LDS and registers.
 int width_of(int32_t Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
 
 const char *check_sizes(const DeltaSizes &s)

@@ -1,4 +1,5 @@
-// Queries and keys per head: a root-mean-square norm and the rotation by position in one pass, and its gradients.
+// Queries and keys per head: a root-mean-square norm and the rotation by position (Su et al. 2021, arXiv 2104.09864; elements i and i + R/2 are a pair) in one
+// pass, and its gradients.
 //
 // Per head of D elements: y = weight x rstd, then elements i and i + R/2 (i < R/2) as a point turned by position times turns_i.
 // Bound by memory: everything is read once and written once.  A head belongs to a group of `lanes` lanes; a lane holds K units, a unit

@@ -1,4 +1,5 @@
-// A step for matrices whose momentum is made orthogonal by products of itself.
+// A step for matrices whose momentum is made orthogonal by products of itself: the optimizer, and the three coefficients of its Newton-Schulz rounds, of
+// Jordan et al. 2024, "Muon: An optimizer for hidden layers in neural networks".
 //
 // With m <- mu m + g and u = g + mu m (or m) of r <= c (the transposed where there are more rows than columns): X = u / (|u| + eps), then `rounds`
 // times  A = X X^T,  B = b A + c A^2,  X <- a X + B X, which takes all singular values near one.  At last p <- p (1 - lr decay) - lr s X.

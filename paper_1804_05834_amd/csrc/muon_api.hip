@@ -23,6 +23,7 @@ namespace {
 constexpr int64_t LONGEST = 1 << 20;    // most rows or columns
 // Parts of a product that are enough for 256 compute units, by their size.  us a launch in parts of 64, 128, 256: B X of twelve matrices of 1024 x 4096 and
 // 2048 x 2048 (768 parts of 256) 822, 582, 424, their X X^T (224) 434, 307, 311; of a block of 512 channels (196 parts of 128) 22, 26, 64.
+// The rule counts parts, not how full they are: 200 matrices of 64 x 64 count as 200 parts of 256, each mostly padding, and take 250 us a step.
 constexpr int64_t ENOUGH[3] = {0, 256, 192};
 constexpr int64_t MOST_CUTS = 6;
 
